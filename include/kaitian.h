@@ -558,6 +558,72 @@ int kt_graph_launch(kt_graph *graph, void *stream);
 int64_t kt_graph_nodes(const kt_graph *graph);
 void kt_graph_destroy(kt_graph *graph);
 
+/* ------------------------------------------------------------------------------------------
+ * Operators of a worker's training step, whose gradients the calls above synchronise.  (The
+ * paper trains a network with a stock framework; these calls are this library's own.)
+ *
+ * They need no context: they run on the device that is current in the calling thread, on
+ * `stream`, and touch nothing but their arguments.  All pointers are device pointers.  Matrices are
+ * rows x cols with a row stride in elements (columns contiguous); any element-aligned address,
+ * stride and width is accepted, 128-bit accesses are used where addresses and strides are
+ * multiples of 16 bytes and rows hold whole vectors.  `dtype` is the activations' type (KT_F32 or
+ * KT_BF16), `param_dtype` that of weight, bias and their gradients.  Arithmetic is fp32, each
+ * output is rounded once.  Nothing is reduced with atomics: the same inputs give the same bits.
+ * rows may be 0.  Calls can be recorded (kt_graph_begin or a stream capture).
+ *
+ * 8-bit checkpoints.  A matrix is kept as codes, int8[rows][kt_ckpt_pitch(cols)] (16-byte aligned,
+ * columns past cols are zero), and scales, fp32[rows][kt_ckpt_blocks(cols)], one for each
+ * KT_CKPT_BLOCK columns of a row: with top the block's largest magnitude, scale = top / 127 and
+ * code = x * 127 / top rounded to the nearest whole number (ties to even), so that code * scale
+ * is within scale / 2 of x.  A block whose top is below 2^-100 is kept as zeros; a block with an
+ * infinity or a NaN restores as NaN in all its columns. */
+#define KT_CKPT_BLOCK 128
+
+int64_t kt_ckpt_pitch(int64_t cols);   /* columns of codes: cols rounded up to a multiple of 16 */
+int64_t kt_ckpt_blocks(int64_t cols);  /* scales of a row */
+
+/* Checkpoint of x; and back: out = code * scale [* weight] [+ bias], weight and bias per column,
+ * each may be NULL (with the layer norm's weight and bias, its output is restored from the
+ * checkpoint of the normalised rows).  Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+int kt_ckpt_store(const void *x, int64_t x_stride, int8_t *codes, float *scales, int64_t rows,
+                  int64_t cols, int dtype, void *stream);
+int kt_ckpt_restore(const int8_t *codes, const float *scales, const void *weight, const void *bias,
+                    int param_dtype, void *out, int64_t out_stride, int64_t rows, int64_t cols,
+                    int dtype, void *stream);
+
+/* Layer norm over each row: u = (x - mean) rstd with rstd = 1 / sqrt(variance + eps) and the
+ * variance over all cols, out = u * weight + bias.  weight and bias may be NULL (ones, zeros);
+ * mean and rstd (fp32[rows]) may be NULL; with codes and scales (both or neither) u is kept in 8
+ * bits.  out may be x.
+ * Backward, from x and mean or from the checkpoint of u (codes and scales; the other pair NULL):
+ *   g = dout * weight,  dx = rstd (g - mean(g) - u mean(g u)),
+ *   dweight = sum over rows of dout * u,  dbias = sum over rows of dout.
+ * dweight and dbias may be NULL (frozen); where one is wanted, workspace (16-byte aligned) holds
+ * kt_norm_workspace(rows, cols) bytes, which need no initial value and may be used again by the
+ * next call on the same stream.  dx may be dout.
+ * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+int kt_norm_forward(const void *x, int64_t x_stride, const void *weight, const void *bias,
+                    int param_dtype, void *out, int64_t out_stride, float *mean, float *rstd,
+                    int8_t *codes, float *scales, int64_t rows, int64_t cols, int dtype, float eps,
+                    void *stream);
+int64_t kt_norm_workspace(int64_t rows, int64_t cols);
+int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64_t x_stride,
+                     const float *mean, const int8_t *codes, const float *scales, const float *rstd,
+                     const void *weight, int param_dtype, void *dx, int64_t dx_stride, void *dweight,
+                     void *dbias, void *workspace, int64_t workspace_bytes, int64_t rows,
+                     int64_t cols, int dtype, void *stream);
+
+/* Activations: KT_GELU x Phi(x) (Phi the normal distribution function), KT_SILU x / (1 + exp(-x)).
+ * Forward: out may be x; with codes and scales (both or neither) x is kept in 8 bits by the same
+ * pass.  Backward: dx = dout * act'(x), from x or from its checkpoint (the other NULL); dx may be
+ * dout.  Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+typedef enum { KT_GELU = 0, KT_SILU = 1 } kt_act_kind;
+int kt_act_forward(const void *x, int64_t x_stride, void *out, int64_t out_stride, int8_t *codes,
+                   float *scales, int64_t rows, int64_t cols, int dtype, int kind, void *stream);
+int kt_act_backward(const void *dout, int64_t dout_stride, const void *x, int64_t x_stride,
+                    const int8_t *codes, const float *scales, void *dx, int64_t dx_stride,
+                    int64_t rows, int64_t cols, int dtype, int kind, void *stream);
+
 /* Number of kernels this context has launched so far (for launch accounting). */
 int64_t kt_launch_count(const kt_ctx *ctx);
 

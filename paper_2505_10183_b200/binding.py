@@ -23,6 +23,8 @@ KT_ROUTE_DIRECT, KT_ROUTE_RELAY = 0, 1
 KT_OK, KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN = 0, -1, -2, -3
 KT_ERR_CUDA, KT_ERR_TIMEOUT, KT_ERR_STATE, KT_ERR_NOMEM = -4, -5, -6, -7
 KT_MAX_RANKS, KT_MAX_GROUPS = 64, 16
+KT_CKPT_BLOCK = 128
+KT_GELU, KT_SILU = 0, 1
 
 EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "kt_adapt_state", "kt_adapt_destroy",
            "kt_sampler_steps", "kt_sampler_indices", "kt_graph_begin", "kt_graph_end", "kt_graph_launch",
@@ -30,7 +32,9 @@ EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "k
            "kt_get_coefficients", "kt_set_transport_dtype", "kt_route", "kt_bucket_pack", "kt_plan_buckets", "kt_plan_query", "kt_hier_reduce",
            "kt_stage_to_host", "kt_relay_through_host", "kt_stage_wait", "kt_unpack_scale", "kt_sync_direct", "kt_allreduce", "kt_bcast_send", "kt_bcast_relay", "kt_bcast_recv", "kt_cast", "kt_copy_tensors", "kt_sync_flat_static", "kt_launch_count",
            "kt_last_error", "kt_destroy", "kt_work_unit", "kt_shard_ranges", "kt_shard_bind", "kt_shard_query",
-           "kt_ipc_export", "kt_ipc_open", "kt_ipc_close", "kt_host_register", "kt_host_unregister", "kt_host_barrier", "kt_shard_step", "kt_shard_bcast"]
+           "kt_ipc_export", "kt_ipc_open", "kt_ipc_close", "kt_host_register", "kt_host_unregister", "kt_host_barrier", "kt_shard_step", "kt_shard_bcast",
+           "kt_ckpt_pitch", "kt_ckpt_blocks", "kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_workspace",
+           "kt_norm_backward", "kt_act_forward", "kt_act_backward"]
 
 _DTYPES = {torch.float32: KT_F32, torch.bfloat16: KT_BF16}
 
@@ -49,7 +53,7 @@ def _load() -> C.CDLL:
             "(needs nvcc); this package has no CPU fallback" % path)
     L = C.CDLL(path)
     vp, i32p, i64p, f32p = C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int64), C.POINTER(C.c_float)
-    vpp = C.POINTER(C.c_void_p)
+    vpp, i64 = C.POINTER(C.c_void_p), C.c_int64
     sigs = {
         "kt_schedule": ([C.POINTER(C.c_double), C.c_int, C.c_int, i32p], C.c_int),
         "kt_scores": ([C.POINTER(C.c_double), C.c_int, C.POINTER(C.c_double)], C.c_int),
@@ -99,6 +103,15 @@ def _load() -> C.CDLL:
         "kt_host_barrier": ([vp, C.c_int, C.c_int], C.c_int),
         "kt_shard_step": ([vp, vp, vpp, vpp, vpp, C.c_int, C.c_int, C.c_float, C.c_int, vp, vp, vp, C.c_int], C.c_int),
         "kt_shard_bcast": ([vp, C.c_int, vp, vp, vp, vp, C.c_int, vp, vp, vp, C.c_int], C.c_int),
+        "kt_ckpt_pitch": ([i64], i64),
+        "kt_ckpt_blocks": ([i64], i64),
+        "kt_ckpt_store": ([vp, i64, vp, vp, i64, i64, C.c_int, vp], C.c_int),
+        "kt_ckpt_restore": ([vp, vp, vp, vp, C.c_int, vp, i64, i64, i64, C.c_int, vp], C.c_int),
+        "kt_norm_forward": ([vp, i64, vp, vp, C.c_int, vp, i64, vp, vp, vp, vp, i64, i64, C.c_int, C.c_float, vp], C.c_int),
+        "kt_norm_workspace": ([i64, i64], i64),
+        "kt_norm_backward": ([vp, i64, vp, i64, vp, vp, vp, vp, vp, C.c_int, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int, vp], C.c_int),
+        "kt_act_forward": ([vp, i64, vp, i64, vp, vp, i64, i64, C.c_int, C.c_int, vp], C.c_int),
+        "kt_act_backward": ([vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int, C.c_int, vp], C.c_int),
         "kt_launch_count": ([vp], C.c_int64),
         "kt_last_error": ([vp], C.c_char_p),
         "kt_destroy": ([vp], None),
@@ -645,6 +658,139 @@ def kt_sync_flat_static(group_of: Sequence[int], shares: Sequence[int], grads: S
     _check(_lib.kt_sync_flat_static(_i32(group_of), _i32(shares), K, int(G), ptrs, _DTYPES[grads[0].dtype],
                                     n, C.c_void_p(out.data_ptr()), _DTYPES[out.dtype], C.c_float(scale),
                                     _stream(stream)))
+
+
+# ------------------------------------------------------------- operators of a training step
+def _matrix(t: torch.Tensor, what: str, like: Optional[torch.Tensor] = None):
+    """(address, row stride) of a matrix with contiguous columns, of `like`'s shape and type where given."""
+    if t.dim() != 2 or t.dtype not in _DTYPES or (t.size(1) > 1 and t.stride(1) != 1):
+        raise KtError(KT_ERR_SHAPE, "%s: a float32 or bfloat16 matrix with contiguous columns expected" % what)
+    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+        raise KtError(KT_ERR_SHAPE, "%s: shape or dtype differs" % what)
+    return t.data_ptr(), t.stride(0)
+
+
+def _codes(codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], rows: int, cols: int):
+    """Addresses of a checkpoint (None, None where there is none)."""
+    if codes is None and scales is None:
+        return None, None
+    if codes is None or scales is None:
+        raise KtError(KT_ERR_INVALID, "a checkpoint has codes and scales: one of them is missing")
+    if (codes.dtype != torch.int8 or scales.dtype != torch.float32 or not codes.is_contiguous() or not scales.is_contiguous()
+            or codes.shape != (rows, (cols + 15) // 16 * 16) or scales.shape != (rows, -(-cols // KT_CKPT_BLOCK))):
+        raise KtError(KT_ERR_SHAPE, "codes: int8 [rows, kt_ckpt_pitch(cols)], scales: float32 [rows, kt_ckpt_blocks(cols)], contiguous")
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def _params(cols: int, *tensors: Optional[torch.Tensor]):
+    """Addresses of vectors over the columns (None stays None), and their type."""
+    dtype, got = KT_F32, []
+    given = [t for t in tensors if t is not None]
+    for t in given:
+        if t.dtype not in _DTYPES or t.dtype != given[0].dtype or t.shape != (cols,) or not t.is_contiguous():
+            raise KtError(KT_ERR_SHAPE, "weight, bias and their gradients: contiguous, [cols], all float32 or all bfloat16")
+        dtype = _DTYPES[t.dtype]
+    for t in tensors:
+        got.append(None if t is None else t.data_ptr())
+    return got, dtype
+
+
+def _per_row(t: Optional[torch.Tensor], rows: int, what: str):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.shape != (rows,) or not t.is_contiguous():
+        raise KtError(KT_ERR_SHAPE, "%s: contiguous float32 [rows] expected" % what)
+    return t.data_ptr()
+
+
+def kt_ckpt_pitch(cols: int) -> int:
+    return int(_lib.kt_ckpt_pitch(int(cols)))
+
+
+def kt_ckpt_blocks(cols: int) -> int:
+    return int(_lib.kt_ckpt_blocks(int(cols)))
+
+
+def kt_ckpt_store(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
+    """Keeps x [rows, cols] in 8 bits: codes int8 [rows, kt_ckpt_pitch(cols)], scales float32 [rows, kt_ckpt_blocks(cols)]."""
+    px, sx = _matrix(x, "x")
+    rows, cols = x.shape
+    pc, ps = _codes(codes, scales, rows, cols)
+    _check(_lib.kt_ckpt_store(px, sx, pc, ps, rows, cols, _DTYPES[x.dtype], _stream(stream)))
+
+
+def kt_ckpt_restore(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                    bias: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = the kept values [* weight] [+ bias]."""
+    po, so = _matrix(out, "out")
+    rows, cols = out.shape
+    pc, ps = _codes(codes, scales, rows, cols)
+    (pw, pb), pd = _params(cols, weight, bias)
+    _check(_lib.kt_ckpt_restore(pc, ps, pw, pb, pd, po, so, rows, cols, _DTYPES[out.dtype], _stream(stream)))
+
+
+def kt_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
+                    mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                    codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Layer norm of the rows of x; with codes and scales the normalised rows are kept in 8 bits."""
+    px, sx = _matrix(x, "x")
+    po, so = _matrix(out, "out", x)
+    rows, cols = x.shape
+    (pw, pb), pd = _params(cols, weight, bias)
+    pc, ps = _codes(codes, scales, rows, cols)
+    _check(_lib.kt_norm_forward(px, sx, pw, pb, pd, po, so, _per_row(mean, rows, "mean"), _per_row(rstd, rows, "rstd"), pc, ps,
+                                rows, cols, _DTYPES[x.dtype], eps, _stream(stream)))
+
+
+def kt_norm_workspace(rows: int, cols: int) -> int:
+    """Bytes that kt_norm_backward needs for the gradients of weight and bias."""
+    return int(_lib.kt_norm_workspace(int(rows), int(cols)))
+
+
+def kt_norm_backward(dout: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor, dx: torch.Tensor,
+                     dweight: Optional[torch.Tensor], dbias: Optional[torch.Tensor], workspace: Optional[torch.Tensor],
+                     x: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
+                     codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
+    """From x and mean, or from the checkpoint (codes, scales) that the forward pass left."""
+    pg, sg = _matrix(dout, "dout")
+    pd, sd = _matrix(dx, "dx", dout)
+    px, sx = _matrix(x, "x", dout) if x is not None else (None, 0)
+    rows, cols = dout.shape
+    (pw, pdw, pdb), kind = _params(cols, weight, dweight, dbias)
+    pc, ps = _codes(codes, scales, rows, cols)
+    pws, nws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
+    _check(_lib.kt_norm_backward(pg, sg, px, sx, _per_row(mean, rows, "mean"), pc, ps, _per_row(rstd, rows, "rstd"), pw, kind,
+                                 pd, sd, pdw, pdb, pws, nws, rows, cols, _DTYPES[dout.dtype], _stream(stream)))
+
+
+_ACTS = {"gelu": KT_GELU, "silu": KT_SILU, KT_GELU: KT_GELU, KT_SILU: KT_SILU}
+
+
+def _act_kind(kind) -> int:
+    if kind not in _ACTS:
+        raise KtError(KT_ERR_INVALID, "unknown activation %r" % (kind,))
+    return _ACTS[kind]
+
+
+def kt_act_forward(x: torch.Tensor, out: torch.Tensor, codes: Optional[torch.Tensor] = None,
+                   scales: Optional[torch.Tensor] = None, kind="gelu", stream=None) -> None:
+    """out = GELU or SiLU of x; with codes and scales x is kept in 8 bits by the same pass."""
+    px, sx = _matrix(x, "x")
+    po, so = _matrix(out, "out", x)
+    rows, cols = x.shape
+    pc, ps = _codes(codes, scales, rows, cols)
+    _check(_lib.kt_act_forward(px, sx, po, so, pc, ps, rows, cols, _DTYPES[x.dtype], _act_kind(kind), _stream(stream)))
+
+
+def kt_act_backward(dout: torch.Tensor, codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], dx: torch.Tensor,
+                    kind="gelu", x: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dx = dout * act'(x), x from its checkpoint or (codes and scales None) as it is."""
+    pg, sg = _matrix(dout, "dout")
+    pd, sd = _matrix(dx, "dx", dout)
+    px, sx = _matrix(x, "x", dout) if x is not None else (None, 0)
+    rows, cols = dout.shape
+    pc, ps = _codes(codes, scales, rows, cols)
+    _check(_lib.kt_act_backward(pg, sg, px, sx, pc, ps, pd, sd, rows, cols, _DTYPES[dout.dtype], _act_kind(kind), _stream(stream)))
 
 
 class Graph:

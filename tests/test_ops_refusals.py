@@ -1,0 +1,80 @@
+"""Arguments that the training operators refuse, before anything is launched (no GPU needed: every
+case is turned away on the host)."""
+import pytest
+import torch
+
+F32, BF16, I8 = torch.float32, torch.bfloat16, torch.int8
+
+
+@pytest.fixture(scope="module")
+def kt():
+    from paper_2505_10183_b200 import binding
+    return binding
+
+
+def status(kt, call, *args, **kw):
+    with pytest.raises(kt.KtError) as e:
+        call(*args, stream=0, **kw)
+    assert str(e.value)
+    return e.value.status
+
+
+def test_sizes_of_a_checkpoint(kt):
+    for cols in (1, 15, 16, 17, 127, 128, 129, 1000):
+        assert kt.kt_ckpt_pitch(cols) == -(-cols // 16) * 16 and kt.kt_ckpt_blocks(cols) == -(-cols // 128)
+    assert kt.kt_norm_workspace(0, 64) == 0 and kt.kt_norm_workspace(1, 64) == 2 * 64 * 4
+    assert kt.kt_norm_workspace(10 ** 6, 64) == kt.kt_norm_workspace(10 ** 7, 64)      # bounded in the rows
+
+
+def test_refused_matrices(kt):
+    x, c, s = torch.zeros(4, 32), torch.zeros(4, 32, dtype=I8), torch.zeros(4, 1)
+    w = torch.zeros(32)
+    assert status(kt, kt.kt_norm_forward, x.double(), w, w, x.double()) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w, w, torch.zeros(4, 33)) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w, w, x.to(BF16)) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x.t(), w, w, x.t()) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w, w.to(BF16), x) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w[:31], None, x) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w, w, x, torch.zeros(5)) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_norm_forward, x, w, w, x, codes=c) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_norm_forward, x, w, w, x, eps=float("nan")) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_norm_forward, x, w, w, x, eps=-1.0) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_ckpt_store, x, c[:, :16], s) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_ckpt_store, x, c, torch.zeros(4, 2)) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_ckpt_restore, None, None, x) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_act_forward, x, x, kind="tanh") == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_act_forward, x, x, kind=7) == kt.KT_ERR_INVALID
+    overlapping = torch.zeros(64).as_strided((4, 32), (8, 1))
+    assert status(kt, kt.kt_act_forward, x, overlapping) == kt.KT_ERR_SHAPE
+
+
+def test_refused_backward_sources(kt):
+    x, c, s, r = torch.zeros(4, 32), torch.zeros(4, 32, dtype=I8), torch.zeros(4, 1), torch.zeros(4)
+    w, ws = torch.zeros(32), torch.zeros(kt.kt_norm_workspace(4, 32), dtype=torch.uint8)
+    back = kt.kt_norm_backward
+    assert status(kt, back, x, w, r, x, w, w, ws) == kt.KT_ERR_INVALID                              # neither source
+    assert status(kt, back, x, w, r, x, w, w, ws, x=x, mean=r, codes=c, scales=s) == kt.KT_ERR_INVALID   # both
+    assert status(kt, back, x, w, r, x, w, w, ws, x=x) == kt.KT_ERR_INVALID                         # no mean
+    assert status(kt, back, x, w, None, x, w, w, ws, codes=c, scales=s) == kt.KT_ERR_INVALID        # no rstd
+    assert status(kt, back, x, w, r, x, w, w, None, codes=c, scales=s) == kt.KT_ERR_INVALID
+    assert status(kt, back, x, w, r, x, w, w, ws[:-16], codes=c, scales=s) == kt.KT_ERR_SHAPE
+    assert status(kt, back, x, w, r, x, w, w.to(BF16), ws, codes=c, scales=s) == kt.KT_ERR_SHAPE
+    assert status(kt, kt.kt_act_backward, x, None, None, x) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_act_backward, x, c, s, x, x=x) == kt.KT_ERR_INVALID
+
+
+def test_c_entries_refuse_bad_addresses_and_types(kt):
+    lib = kt._lib
+    x = torch.zeros(4, 32)
+    p = x.data_ptr()
+    c = torch.zeros(256, dtype=I8).data_ptr() // 16 * 16 + 16
+    assert lib.kt_act_forward(p, 32, None, 32, None, None, 4, 32, 0, 0, None) == kt.KT_ERR_INVALID
+    assert lib.kt_act_forward(p + 2, 32, p, 32, None, None, 4, 32, 0, 0, None) == kt.KT_ERR_ALIGN
+    assert lib.kt_act_forward(p, 32, p, 32, c + 8, p, 4, 32, 0, 0, None) == kt.KT_ERR_ALIGN
+    assert lib.kt_act_forward(p, 32, p, 32, None, None, 4, 32, 5, 0, None) == kt.KT_ERR_INVALID
+    assert lib.kt_act_forward(p, 32, p, 32, None, None, -1, 32, 0, 0, None) == kt.KT_ERR_SHAPE
+    assert lib.kt_act_forward(p, 32, p, 32, None, None, 4, 0, 0, 0, None) == kt.KT_ERR_SHAPE
+    assert lib.kt_act_forward(p, 32, p, 32, None, None, 1 << 60, 32, 0, 0, None) == kt.KT_ERR_SHAPE
+    assert lib.kt_ckpt_store(p, 31, c, p, 4, 32, 0, None) == kt.KT_ERR_SHAPE
+    assert lib.kt_norm_forward(p, 32, p, p, 9, p, 32, None, None, None, None, 4, 32, 0, 1e-5, None) == kt.KT_ERR_INVALID
+    assert lib.kt_last_error(None)
