@@ -624,6 +624,45 @@ int kt_act_backward(const void *dout, int64_t dout_stride, const void *x, int64_
                     const int8_t *codes, const float *scales, void *dx, int64_t dx_stride,
                     int64_t rows, int64_t cols, int dtype, int kind, void *stream);
 
+/* Softmax attention on bf16 heads.  Tensors are [batch, tokens, heads, head_dim]; a stride array
+ * (host) holds the strides of batch, token and head in elements, head_dim is contiguous; addresses are
+ * 16-byte aligned and strides multiples of 8 elements (positive: an expanded tensor needs a copy).
+ * heads is a multiple of heads_kv: query head h reads key/value head h / (heads / heads_kv).
+ * used_q, used_kv (device, int32[batch], or NULL for all): tokens in use of each sequence, taken into
+ * [0, len]; query i of a sequence with n queries and m keys sees the keys j < m, with causal those
+ * j <= i + m - n (the last query sees all).  What the tensors hold past the tokens in use does not
+ * matter.  Results there, and for queries that see no key, are zeros (lse: -infinity).
+ * Forward: out = softmax(scale q k^T) v and lse = log of the sum of exponentials, fp32
+ * [batch, heads, len_q] contiguous.  Backward, from what the forward pass was given and wrote: dq, dk,
+ * dv; dk and dv are summed over the heads that share them.  workspace (16-byte aligned) holds
+ * kt_attn_workspace bytes, which need no initial value and may be used again by the next call on the same
+ * stream.  Products of bf16 with fp32 sums; probabilities and their gradients are rounded to bf16 between
+ * two products.  No atomics: the same inputs give the same bits.  Outputs must not overlap inputs.
+ * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+#define KT_ATTN_MAX_DIM 128
+typedef struct {
+    int32_t batch, len_q, len_kv, heads, heads_kv, head_dim; /* head_dim: a multiple of 8, at most KT_ATTN_MAX_DIM */
+    int32_t dtype;                                           /* KT_BF16 */
+    int32_t causal;
+    float scale;                                             /* > 0 */
+    const int32_t *used_q, *used_kv;
+} kt_attn;
+int kt_attn_forward(const kt_attn *desc, const void *q, const int64_t *q_stride, const void *k,
+                    const int64_t *k_stride, const void *v, const int64_t *v_stride, void *out,
+                    const int64_t *out_stride, float *lse, void *stream);
+int64_t kt_attn_workspace(int batch, int heads, int len_q);
+int kt_attn_backward(const kt_attn *desc, const void *dout, const int64_t *dout_stride, const void *q,
+                     const int64_t *q_stride, const void *k, const int64_t *k_stride, const void *v,
+                     const int64_t *v_stride, const void *out, const int64_t *out_stride,
+                     const float *lse, void *dq, const int64_t *dq_stride, void *dk,
+                     const int64_t *dk_stride, void *dv, const int64_t *dv_stride, void *workspace,
+                     int64_t workspace_bytes, void *stream);
+
+/* Every wait inside the attention kernels is bounded: one that lasts two seconds gives up, its kernel ends
+ * without a result and the device stays usable.  *count (host) = how many did since the library was
+ * loaded on the current device (0 unless something is broken); waits for the device. */
+int kt_attn_given_up(int64_t *count);
+
 /* Number of kernels this context has launched so far (for launch accounting). */
 int64_t kt_launch_count(const kt_ctx *ctx);
 

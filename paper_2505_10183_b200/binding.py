@@ -25,6 +25,7 @@ KT_ERR_CUDA, KT_ERR_TIMEOUT, KT_ERR_STATE, KT_ERR_NOMEM = -4, -5, -6, -7
 KT_MAX_RANKS, KT_MAX_GROUPS = 64, 16
 KT_CKPT_BLOCK = 128
 KT_GELU, KT_SILU = 0, 1
+KT_ATTN_MAX_DIM = 128
 
 EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "kt_adapt_state", "kt_adapt_destroy",
            "kt_sampler_steps", "kt_sampler_indices", "kt_graph_begin", "kt_graph_end", "kt_graph_launch",
@@ -34,7 +35,8 @@ EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "k
            "kt_last_error", "kt_destroy", "kt_work_unit", "kt_shard_ranges", "kt_shard_bind", "kt_shard_query",
            "kt_ipc_export", "kt_ipc_open", "kt_ipc_close", "kt_host_register", "kt_host_unregister", "kt_host_barrier", "kt_shard_step", "kt_shard_bcast",
            "kt_ckpt_pitch", "kt_ckpt_blocks", "kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_workspace",
-           "kt_norm_backward", "kt_act_forward", "kt_act_backward"]
+           "kt_norm_backward", "kt_act_forward", "kt_act_backward", "kt_attn_forward", "kt_attn_workspace", "kt_attn_backward",
+           "kt_attn_given_up"]
 
 _DTYPES = {torch.float32: KT_F32, torch.bfloat16: KT_BF16}
 
@@ -43,6 +45,12 @@ class KtError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__("kaitian status %d: %s" % (status, message))
         self.status = status
+
+
+class _Attn(C.Structure):
+    """kt_attn of the header."""
+    _fields_ = [(n, C.c_int32) for n in ("batch", "len_q", "len_kv", "heads", "heads_kv", "head_dim", "dtype", "causal")] + [
+        ("scale", C.c_float), ("used_q", C.c_void_p), ("used_kv", C.c_void_p)]
 
 
 def _load() -> C.CDLL:
@@ -112,6 +120,10 @@ def _load() -> C.CDLL:
         "kt_norm_backward": ([vp, i64, vp, i64, vp, vp, vp, vp, vp, C.c_int, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int, vp], C.c_int),
         "kt_act_forward": ([vp, i64, vp, i64, vp, vp, i64, i64, C.c_int, C.c_int, vp], C.c_int),
         "kt_act_backward": ([vp, i64, vp, i64, vp, vp, vp, i64, i64, i64, C.c_int, C.c_int, vp], C.c_int),
+        "kt_attn_forward": ([vp] * 11, C.c_int),
+        "kt_attn_workspace": ([C.c_int, C.c_int, C.c_int], i64),
+        "kt_attn_backward": ([vp] * 19 + [i64, vp], C.c_int),
+        "kt_attn_given_up": ([i64p], C.c_int),
         "kt_launch_count": ([vp], C.c_int64),
         "kt_last_error": ([vp], C.c_char_p),
         "kt_destroy": ([vp], None),
@@ -791,6 +803,68 @@ def kt_act_backward(dout: torch.Tensor, codes: Optional[torch.Tensor], scales: O
     rows, cols = dout.shape
     pc, ps = _codes(codes, scales, rows, cols)
     _check(_lib.kt_act_backward(pg, sg, px, sx, pc, ps, pd, sd, rows, cols, _DTYPES[dout.dtype], _act_kind(kind), _stream(stream)))
+
+
+_Strides = C.c_int64 * 3
+
+
+def _heads(t: torch.Tensor, what: str, shape):
+    """(address, strides of batch, token and head) of a tensor [batch, tokens, heads, head_dim]."""
+    if t.dtype != torch.bfloat16 or t.shape != shape or (t.size(3) > 1 and t.stride(3) != 1):
+        raise KtError(KT_ERR_SHAPE, "%s: bfloat16 %s with a contiguous last dimension expected" % (what, list(shape)))
+    s = t.stride()
+    return t.data_ptr(), _Strides(s[0], s[1], s[2])
+
+
+def _attn(q: torch.Tensor, k: torch.Tensor, scale, causal, used_q, used_kv) -> _Attn:
+    if q.dim() != 4 or k.dim() != 4 or q.size(0) != k.size(0) or q.size(3) != k.size(3):
+        raise KtError(KT_ERR_SHAPE, "q and k: [batch, tokens, heads, head_dim] with the same batch and head_dim expected")
+    B, Lq, H, D = q.shape
+    for u in (used_q, used_kv):
+        if u is not None and (u.dtype != torch.int32 or u.shape != (B,) or not u.is_contiguous()):
+            raise KtError(KT_ERR_SHAPE, "used_q, used_kv: contiguous int32 [batch] expected")
+    return _Attn(B, Lq, k.size(1), H, k.size(2), D, KT_BF16, bool(causal), D ** -0.5 if scale is None else scale,
+                 None if used_q is None else used_q.data_ptr(), None if used_kv is None else used_kv.data_ptr())
+
+
+def _lse(lse: torch.Tensor, q: torch.Tensor):
+    if lse.dtype != torch.float32 or lse.shape != (q.size(0), q.size(2), q.size(1)) or not lse.is_contiguous():
+        raise KtError(KT_ERR_SHAPE, "lse: contiguous float32 [batch, heads, tokens] expected")
+    return lse.data_ptr()
+
+
+def kt_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                    scale: Optional[float] = None, causal: bool = False, used_q: Optional[torch.Tensor] = None,
+                    used_kv: Optional[torch.Tensor] = None, stream=None) -> None:
+    """out = softmax(scale q k^T) v on bfloat16 [batch, tokens, heads, head_dim] (any strides that are multiples
+    of 8; k and v may have fewer heads), lse float32 [batch, heads, tokens].  scale: 1 / sqrt(head_dim) by default."""
+    desc = _attn(q, k, scale, causal, used_q, used_kv)
+    (pq, sq), (pk, sk), (pv, sv), (po, so) = _heads(q, "q", q.shape), _heads(k, "k", k.shape), _heads(v, "v", k.shape), _heads(out, "out", q.shape)
+    _check(_lib.kt_attn_forward(C.byref(desc), pq, sq, pk, sk, pv, sv, po, so, _lse(lse, q), _stream(stream)))
+
+
+def kt_attn_workspace(q: torch.Tensor, k: torch.Tensor) -> int:
+    """Bytes that kt_attn_backward needs for tensors of q's and k's shape."""
+    return int(_lib.kt_attn_workspace(q.size(0), q.size(2), q.size(1)))
+
+
+def kt_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                     dq: torch.Tensor, dk: torch.Tensor, dv: torch.Tensor, workspace: torch.Tensor, scale: Optional[float] = None,
+                     causal: bool = False, used_q: Optional[torch.Tensor] = None, used_kv: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+    """Gradients of kt_attn_forward from its arguments and results; workspace: kt_attn_workspace bytes."""
+    desc = _attn(q, k, scale, causal, used_q, used_kv)
+    (pg, sg), (pq, sq), (po, so), (pdq, sdq) = (_heads(t, n, q.shape) for t, n in ((dout, "dout"), (q, "q"), (out, "out"), (dq, "dq")))
+    (pk, sk), (pv, sv), (pdk, sdk), (pdv, sdv) = (_heads(t, n, k.shape) for t, n in ((k, "k"), (v, "v"), (dk, "dk"), (dv, "dv")))
+    _check(_lib.kt_attn_backward(C.byref(desc), pg, sg, pq, sq, pk, sk, pv, sv, po, so, _lse(lse, q), pdq, sdq, pdk, sdk, pdv, sdv,
+                                 workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), _stream(stream)))
+
+
+def kt_attn_given_up() -> int:
+    """Waits inside attention kernels that were given up since the library was loaded (0 unless something is broken)."""
+    n = C.c_int64(0)
+    _check(_lib.kt_attn_given_up(C.byref(n)))
+    return int(n.value)
 
 
 class Graph:

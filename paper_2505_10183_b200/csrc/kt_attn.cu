@@ -1,0 +1,900 @@
+// kt_attn.cu -- softmax attention and its backward pass on bf16 heads, for the training step whose
+// gradients the library synchronises.  Contracts: include/kaitian.h.
+//
+// With S = scale Q K^T under the mask, lse_i = log sum_j exp(S_ij) and P = exp(S - lse):
+//   forward    O = P V, one pass over the keys with a running maximum and sum per query
+//   backward   delta_i = sum_d dO_id O_id,  dP = dO V^T,  dS = P (dP - delta),
+//              dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+// The backward pass recomputes P from Q, K and lse.  It is two kernels: one CTA per 128 queries that
+// goes over the keys (dQ), one per 128 keys that goes over the queries of all heads that share them (dK,
+// dV).  Every sum has one owner, so nothing is added with atomics and the result does not depend on
+// the order in which CTAs run; the price is that S and dP are formed twice (7 products, not 5).
+//
+// All products run on the tensor cores (kt_tensor.cuh): operands come in by tile copies, sums stay in
+// tensor memory, and the probabilities (dS) go back to tensor memory as bf16, where they are the first
+// operand of the next product.  One warp issues copies, one issues products, eight compute.
+// Rows past a sequence's length may hold anything: they are cleared in shared memory where they would
+// be multiplied by a zero.
+#include "../../include/kaitian.h"
+
+#include <cuda_bf16.h>
+
+#include <cmath>
+
+#include "kt_internal.h"
+#include "kt_tensor.cuh"
+
+using namespace ktd;
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int WORKERS = 256;                    // threads that compute: two groups of four warps
+constexpr int WARP_MMA = 8, WARP_LOAD = 9, THREADS = 320;
+constexpr uint32_t TMEM_COLUMNS = 512;
+
+struct AttnParams {
+    const int32_t *used_q, *used_kv;
+    const __nv_bfloat16 *o, *dout;
+    __nv_bfloat16 *out, *out2;                  // O, dQ, or dK and dV
+    float *lse, *stats;
+    int64_t o_stride[3], dout_stride[3], out_stride[3], out2_stride[3];     // batch, token, head
+    int batch, heads, heads_kv, len_q, len_kv, dim, causal;
+    int tiles_q, tiles_kv;
+    float scale, scale_log2;
+};
+
+// Tokens in use of a sequence, and how far a query sees.
+struct Seq {
+    int n, m, shift, causal;                    // queries, keys, m - n
+    __device__ Seq(const AttnParams &p, int b) {
+        n = p.used_q ? min(max(p.used_q[b], 0), p.len_q) : p.len_q;
+        m = p.used_kv ? min(max(p.used_kv[b], 0), p.len_kv) : p.len_kv;
+        shift = m - n;
+        causal = p.causal;
+    }
+    __device__ int keys_of(int i) const { return i >= n ? 0 : causal ? max(0, min(m, i + 1 + shift)) : m; }      // keys 0 ... of query i
+    __device__ int first_query_of(int j) const { return causal ? max(0, j - shift) : 0; }                    // the first that sees key j
+};
+
+__device__ __forceinline__ int tiles(int rows) { return (rows + TILE - 1) / TILE; }
+
+// One tile [128 tokens x DH] into shared memory; `full` is arrived at once it is there.  Rows from `used`
+// on that lie inside the tensor (`len`) hold whatever the caller left there: with CLEAN they are
+// cleared first, which the whole warp does (rows past `len` arrive as zeros).
+template <int DH, bool CLEAN>
+__device__ __forceinline__ bool load_tile(uint32_t to, uint8_t *to_ptr, const CUtensorMap *map, uint64_t *full, uint64_t *landed, uint32_t &landed_phase,
+                                          int token, int used, int len, int head, int batch, volatile uint32_t *gave_up) {
+    const int lane = threadIdx.x % 32;
+    const bool dirty = CLEAN && used < min(len, token + TILE);
+    uint64_t *bar = dirty ? landed : full;
+    if (lane == 0) {
+        bar_expect(bar, DH / 64 * CHUNK);
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c) copy_tile(to + c * CHUNK, map, bar, c * 64, token, head, batch);
+    }
+    __syncwarp();
+    if (!dirty) return true;
+    if (!bar_wait(landed, landed_phase, gave_up)) return false;
+    landed_phase ^= 1;
+    const int from = max(0, used - token);
+    for (int i = from * 8 + lane; i < TILE * 8; i += 32)
+#pragma unroll
+        for (int c = 0; c < DH / 64; ++c) *reinterpret_cast<uint4 *>(to_ptr + c * CHUNK + i * 16) = make_uint4(0, 0, 0, 0);
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) bar_arrive(full);
+    return true;
+}
+
+// 32 columns of a row, scaled, as bf16 to `row` (columns from c0 on that exist).
+__device__ __forceinline__ void write_columns(__nv_bfloat16 *row, int c0, int dim, const uint32_t (&r)[32], float by) {
+#pragma unroll
+    for (int c = 0; c < 32; c += 8) {
+        if (c0 + c < dim) {
+            uint4 v;
+            v.x = pack_bf16(__uint_as_float(r[c]) * by, __uint_as_float(r[c + 1]) * by);
+            v.y = pack_bf16(__uint_as_float(r[c + 2]) * by, __uint_as_float(r[c + 3]) * by);
+            v.z = pack_bf16(__uint_as_float(r[c + 4]) * by, __uint_as_float(r[c + 5]) * by);
+            v.w = pack_bf16(__uint_as_float(r[c + 6]) * by, __uint_as_float(r[c + 7]) * by);
+            *reinterpret_cast<uint4 *>(row + c0 + c) = v;
+        }
+    }
+}
+__device__ __forceinline__ void write_zeros(__nv_bfloat16 *row, int c0, int c1) {
+    for (int c = c0; c < c1; c += 8) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
+}
+
+// The end of a kernel whose waits have given up: copies and products in flight get time to finish before
+// the memory that they write is handed back.
+__device__ __forceinline__ void settle(volatile uint32_t *gave_up) {
+    if (*gave_up)
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+}
+
+// ------------------------------------------------------------------------------------ forward
+// Two tiles of 128 queries to a CTA, four warps on each: while one group takes the exponentials of its
+// scores, the tensor cores work for the other.  A thread owns a row: maximum and sum need no exchange.
+// Tensor memory: scores (and over them the probabilities) 0 and 128, sums 256 and 256 + DH.
+constexpr int FWD_SLOTS = 4;                    // K and V tiles in flight
+
+template <int DH>
+struct FwdSmem {
+    static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
+    alignas(1024) uint8_t q[2][TILE_BYTES];
+    alignas(1024) uint8_t kv[FWD_SLOTS][TILE_BYTES];
+    uint64_t q_full, kv_full[FWD_SLOTS], kv_free[FWD_SLOTS], s_full[2], p_ready[2], o_full[2], landed;
+    uint32_t tmem, gave_up;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+               const AttnParams p) {
+    extern __shared__ uint8_t raw[];
+    auto &sm = *reinterpret_cast<FwdSmem<DH> *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int pairs = (p.tiles_q + 1) / 2, bh = blockIdx.x % (p.batch * p.heads);
+    const int row0 = (pairs - 1 - static_cast<int>(blockIdx.x / (p.batch * p.heads))) * 2 * TILE;      // the longest rows first
+    const int b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
+    const Seq seq(p, b);
+    int n_tiles[2];                             // key tiles that a query tile sees
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const int first = row0 + w * TILE;
+        n_tiles[w] = first < seq.n ? tiles(seq.keys_of(min(first + TILE, seq.n) - 1)) : 0;
+    }
+    const int n = max(n_tiles[0], n_tiles[1]);
+
+    if (threadIdx.x == 0) {
+        bar_init(&sm.q_full, 1);
+        bar_init(&sm.landed, 1);
+        for (int i = 0; i < FWD_SLOTS; ++i) bar_init(&sm.kv_full[i], 1), bar_init(&sm.kv_free[i], 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], TILE), bar_init(&sm.o_full[w], 1);
+        sm.gave_up = 0;
+        fence_async_smem();
+    }
+    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t *gave_up = &sm.gave_up;
+
+    if (warp == WARP_LOAD) {
+        if (n > 0) {
+            if (lane == 0) {
+                bar_expect(&sm.q_full, 2 * FwdSmem<DH>::TILE_BYTES);
+                for (int w = 0; w < 2; ++w)
+                    for (int c = 0; c < DH / 64; ++c) copy_tile(smem_addr(sm.q[w]) + c * CHUNK, &map_q, &sm.q_full, c * 64, row0 + w * TILE, h, b);
+            }
+            __syncwarp();
+            uint32_t landed_phase = 0;
+            for (int i = 0; i < 2 * n; ++i) {
+                const int slot = i % FWD_SLOTS;
+                if (!bar_wait(&sm.kv_free[slot], (i / FWD_SLOTS + 1) & 1, gave_up)) break;
+                const bool ok = i % 2 == 0 ? load_tile<DH, false>(smem_addr(sm.kv[slot]), sm.kv[slot], &map_k, &sm.kv_full[slot], &sm.landed, landed_phase, i / 2 * TILE, seq.m, p.len_kv, h_kv, b, gave_up)
+                                           : load_tile<DH, true>(smem_addr(sm.kv[slot]), sm.kv[slot], &map_v, &sm.kv_full[slot], &sm.landed, landed_phase, i / 2 * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
+                if (!ok) break;
+            }
+        }
+    } else if (warp == WARP_MMA) {
+        auto wait_kv = [&](int i) { return bar_wait(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
+        auto scores = [&](int w, int j) {
+            if (lane == 0) {
+                product_rows<DH>(tmem + w * TILE, smem_addr(sm.q[w]), smem_addr(sm.kv[2 * j % FWD_SLOTS]));
+                mma_commit(&sm.s_full[w]);
+            }
+            __syncwarp();
+        };
+        auto free_kv = [&](int i) {
+            if (lane == 0) mma_commit(&sm.kv_free[i % FWD_SLOTS]);
+            __syncwarp();
+        };
+        if (n > 0 && bar_wait(&sm.q_full, 0, gave_up) && wait_kv(0)) {
+            for (int w = 0; w < 2; ++w)
+                if (n_tiles[w] > 0) scores(w, 0);
+            free_kv(0);
+            for (int j = 0; j < n; ++j) {
+                if (!wait_kv(2 * j + 1)) break;
+                bool ok = true;
+                for (int w = 0; w < 2 && ok; ++w) {
+                    if (j >= n_tiles[w]) continue;
+                    ok = bar_wait(&sm.p_ready[w], j & 1, gave_up);
+                    if (!ok) break;
+                    tmem_fence_after();
+                    if (lane == 0) {
+                        product_down<DH>(tmem + 256 + w * DH, tmem + w * TILE, smem_addr(sm.kv[(2 * j + 1) % FWD_SLOTS]), j > 0);
+                        if (j == n_tiles[w] - 1) mma_commit(&sm.o_full[w]);
+                    }
+                    __syncwarp();
+                    if (j + 1 < n_tiles[w]) {
+                        ok = wait_kv(2 * j + 2);
+                        if (ok) scores(w, j + 1);
+                    }
+                }
+                if (!ok) break;
+                free_kv(2 * j + 1);
+                if (j + 1 < n) free_kv(2 * j + 2);
+            }
+        }
+    } else {
+        const int w = warp / 4, row = row0 + w * TILE + threadIdx.x % TILE;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + w * TILE, o_at = lanes + 256 + w * DH;
+        const int limit = seq.keys_of(row), all_see = seq.keys_of(row0 + w * TILE);    // the tile's first row sees least
+        const bool whole = row0 + w * TILE + TILE <= seq.n;
+        float top = -INFINITY, sum = 0.0f;      // in units of log 2, after scaling
+        bool ok = true;
+        for (int j = 0; j < n_tiles[w]; ++j) {
+            if (!(ok = bar_wait(&sm.s_full[w], j & 1, gave_up))) break;
+            tmem_fence_after();
+            uint32_t s[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, s[c]);
+            tmem_wait_loads();
+            if (!whole || (j + 1) * TILE > all_see) {
+                const int left = limit - j * TILE;
+#pragma unroll
+                for (int c = 0; c < TILE; ++c)
+                    if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
+            }
+            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < TILE; ++c) m[c % 4] = fmaxf(m[c % 4], __uint_as_float(s[c / 32][c % 32]));
+            const float here = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
+            // The running maximum follows only when it would grow by 2^8: until then probabilities of up
+            // to 256 are as exact, and the sums in tensor memory need not be rescaled.
+            const bool grow = here > top + 8.0f || (top == -INFINITY && here > -INFINITY);
+            if (__any_sync(0xFFFFFFFFu, grow)) {
+                const float by = grow ? exp2_fast(top - here) : 1.0f;
+                if (grow) top = here;
+                sum *= by;
+                if (j > 0) {
+#pragma unroll
+                    for (int c = 0; c < DH; c += 32) {
+                        uint32_t o[32];
+                        tmem_load32(o_at + c, o);
+                        tmem_wait_loads();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
+                        tmem_store32(o_at + c, o);
+                    }
+                }
+            }
+            const float ref = top == -INFINITY ? 0.0f : top;
+            float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                uint32_t packed[32];
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    const float x = exp2_fast(fmaf(__uint_as_float(s[half * 2 + c / 32][c % 32]), p.scale_log2, -ref));
+                    const float y = exp2_fast(fmaf(__uint_as_float(s[half * 2 + c / 32][c % 32 + 1]), p.scale_log2, -ref));
+                    part[c % 4] += x;
+                    part[c % 4 + 1] += y;
+                    packed[c / 2] = pack_bf16(x, y);
+                }
+                tmem_store32(s_at + half * 64, packed);
+            }
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            tmem_wait_stores();
+            tmem_fence_before();
+            bar_arrive(&sm.p_ready[w]);
+        }
+        const bool any = n_tiles[w] > 0;
+        if (any && ok) ok = bar_wait(&sm.o_full[w], 0, gave_up);
+        tmem_fence_after();
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
+        if (any && ok) {
+#pragma unroll
+            for (int c = 0; c < DH; c += 32) {
+                uint32_t o[32];
+                tmem_load32(o_at + c, o);
+                tmem_wait_loads();
+                if (sum == 0.0f)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0;
+                if (row < p.len_q) write_columns(out, c, p.dim, o, by);
+            }
+        } else if (row < p.len_q) {
+            write_zeros(out, 0, p.dim);
+        }
+        if (row < p.len_q) p.lse[(static_cast<int64_t>(b) * p.heads + h) * p.len_q + row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+    }
+    tmem_fence_before();
+    __syncthreads();
+    settle(gave_up);
+    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+}
+
+// ----------------------------------------------------------------------------------- backward
+// Per query tile, side by side: lse in units of log 2 (+inf where a query sees nothing or is not in
+// use, which makes its probabilities exp2(s - inf) = 0), and delta.  A half warp to a row.
+__global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16;
+    const int lane = threadIdx.x % 16;
+    const int64_t bh = at / (p.tiles_q * TILE);
+    const int row = static_cast<int>(at % (p.tiles_q * TILE));
+    if (bh >= static_cast<int64_t>(p.batch) * p.heads) return;       // whole CTAs: 128 rows to a tile
+    const int b = static_cast<int>(bh / p.heads), h = static_cast<int>(bh % p.heads);
+    const Seq seq(p, b);
+    float delta = 0.0f;
+    if (row < seq.n && lane * 8 < p.dim) {
+        const uint4 x = *reinterpret_cast<const uint4 *>(p.o + b * p.o_stride[0] + row * p.o_stride[1] + h * p.o_stride[2] + lane * 8);
+        const uint4 y = *reinterpret_cast<const uint4 *>(p.dout + b * p.dout_stride[0] + row * p.dout_stride[1] + h * p.dout_stride[2] + lane * 8);
+        const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            delta = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), delta);
+            delta = fmaf(__uint_as_float(u[i] & 0xFFFF0000u), __uint_as_float(v[i] & 0xFFFF0000u), delta);
+        }
+    }
+#pragma unroll
+    for (int d = 8; d > 0; d /= 2) delta += __shfl_xor_sync(0xFFFFFFFFu, delta, d);
+    if (lane == 0) {
+        const float lse = row < seq.n ? p.lse[bh * p.len_q + row] : -INFINITY;
+        float *to = p.stats + at / TILE * 2 * TILE + at % TILE;
+        to[0] = lse == -INFINITY ? INFINITY : lse * LOG2E;
+        to[TILE] = lse == -INFINITY ? 0.0f : delta;
+    }
+}
+
+// dQ: 128 queries to a CTA.  The two groups of four warps share the rows and split the columns (keys) of
+// a tile.  Tensor memory: scores (over them dS) 0 and 128 in turn, dP 256, sums 384.
+template <int DH>
+struct DqSmem {
+    static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
+    static constexpr int K_SLOTS = 3, V_SLOTS = 2;
+    alignas(1024) uint8_t q[TILE_BYTES], dout[TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
+    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], dp_full, dp_taken, ds_ready, dq_full, landed;
+    uint32_t tmem, gave_up;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+          const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
+    extern __shared__ uint8_t raw[];
+    using Smem = DqSmem<DH>;
+    auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int bh = blockIdx.x % (p.batch * p.heads), tile = p.tiles_q - 1 - static_cast<int>(blockIdx.x / (p.batch * p.heads)), row0 = tile * TILE;
+    const int b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
+    const Seq seq(p, b);
+    const int n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
+
+    if (threadIdx.x == 0) {
+        bar_init(&sm.q_full, 1);
+        bar_init(&sm.landed, 1);
+        for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
+        for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
+        bar_init(&sm.s_full[0], 1), bar_init(&sm.s_full[1], 1), bar_init(&sm.dp_full, 1), bar_init(&sm.dq_full, 1);
+        bar_init(&sm.dp_taken, WORKERS), bar_init(&sm.ds_ready, WORKERS);
+        sm.gave_up = 0;
+        fence_async_smem();
+    }
+    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t *gave_up = &sm.gave_up;
+
+    if (warp == WARP_LOAD) {
+        if (n > 0) {
+            if (lane == 0) {
+                bar_expect(&sm.q_full, 2 * Smem::TILE_BYTES);
+                for (int c = 0; c < DH / 64; ++c) {
+                    copy_tile(smem_addr(sm.q) + c * CHUNK, &map_q, &sm.q_full, c * 64, row0, h, b);
+                    copy_tile(smem_addr(sm.dout) + c * CHUNK, &map_do, &sm.q_full, c * 64, row0, h, b);
+                }
+            }
+            __syncwarp();
+            uint32_t landed_phase = 0;
+            for (int j = 0; j < n; ++j) {
+                const int ks = j % Smem::K_SLOTS, vs = j % Smem::V_SLOTS;
+                if (!bar_wait(&sm.k_free[ks], (j / Smem::K_SLOTS + 1) & 1, gave_up)) break;
+                if (!load_tile<DH, true>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
+                if (!bar_wait(&sm.v_free[vs], (j / Smem::V_SLOTS + 1) & 1, gave_up)) break;
+                load_tile<DH, false>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
+            }
+        }
+    } else if (warp == WARP_MMA) {
+        auto scores = [&](int j) {
+            const int ks = j % Smem::K_SLOTS;
+            if (!bar_wait(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
+            if (lane == 0) {
+                product_rows<DH>(tmem + (j & 1) * TILE, smem_addr(sm.q), smem_addr(sm.k[ks]));
+                mma_commit(&sm.s_full[j & 1]);
+            }
+            __syncwarp();
+            return true;
+        };
+        auto dprobs = [&](int j) {
+            const int vs = j % Smem::V_SLOTS;
+            if (!bar_wait(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) return false;
+            if (j > 0 && !bar_wait(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
+            tmem_fence_after();
+            if (lane == 0) {
+                product_rows<DH>(tmem + 2 * TILE, smem_addr(sm.dout), smem_addr(sm.v[vs]));
+                mma_commit(&sm.dp_full);
+                mma_commit(&sm.v_free[vs]);
+            }
+            __syncwarp();
+            return true;
+        };
+        if (n > 0 && bar_wait(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0)) {
+            for (int j = 0; j < n; ++j) {
+                if (j + 1 < n && !(scores(j + 1) && dprobs(j + 1))) break;
+                if (!bar_wait(&sm.ds_ready, j & 1, gave_up)) break;
+                tmem_fence_after();
+                if (lane == 0) {
+                    product_down<DH>(tmem + 3 * TILE, tmem + (j & 1) * TILE, smem_addr(sm.k[j % Smem::K_SLOTS]), j > 0);
+                    mma_commit(&sm.k_free[j % Smem::K_SLOTS]);
+                    if (j == n - 1) mma_commit(&sm.dq_full);
+                }
+                __syncwarp();
+            }
+        }
+    } else {
+        const int g = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+        const int limit = seq.keys_of(row), all_see = seq.keys_of(row0);
+        const bool whole = row0 + TILE <= seq.n;
+        const float *stats = p.stats + (static_cast<int64_t>(bh) * p.tiles_q + tile) * 2 * TILE + in_tile;
+        const float lse = stats[0], delta = stats[TILE];
+        bool ok = true;
+        for (int j = 0; j < n; ++j) {
+            const uint32_t s_at = lanes + (j & 1) * TILE + g * 64;
+            if (!(ok = bar_wait(&sm.s_full[j & 1], j / 2 & 1, gave_up))) break;
+            tmem_fence_after();
+            uint32_t s[2][32], d[2][32];
+            tmem_load32(s_at, s[0]);
+            tmem_load32(s_at + 32, s[1]);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; ++c) s[c / 32][c % 32] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c / 32][c % 32]), p.scale_log2, -lse)));
+            if (!(ok = bar_wait(&sm.dp_full, j & 1, gave_up))) break;
+            tmem_fence_after();
+            tmem_load32(lanes + 2 * TILE + g * 64, d[0]);
+            tmem_load32(lanes + 2 * TILE + g * 64 + 32, d[1]);
+            tmem_wait_loads();
+            tmem_fence_before();
+            bar_arrive(&sm.dp_taken);
+#pragma unroll
+            for (int c = 0; c < 64; ++c) d[c / 32][c % 32] = __float_as_uint(__uint_as_float(s[c / 32][c % 32]) * (__uint_as_float(d[c / 32][c % 32]) - delta));
+            if (!whole || (j + 1) * TILE > all_see) {
+                const int left = limit - j * TILE - g * 64;
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (c >= left) d[c / 32][c % 32] = 0;
+            }
+            uint32_t packed[32];
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(__uint_as_float(d[c / 32][c % 32]), __uint_as_float(d[c / 32][c % 32 + 1]));
+            tmem_store32(s_at, packed);
+            tmem_wait_stores();
+            tmem_fence_before();
+            bar_arrive(&sm.ds_ready);
+        }
+        if (n > 0 && ok) ok = bar_wait(&sm.dq_full, 0, gave_up);
+        tmem_fence_after();
+        __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
+#pragma unroll
+        for (int c = 0; c < DH; c += 64) {            // the groups take turns of 32 columns
+            const int c0 = c + g * 32;
+            if (n > 0 && ok) {
+                uint32_t o[32];
+                tmem_load32(lanes + 3 * TILE + c0, o);
+                tmem_wait_loads();
+                if (limit == 0)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0;
+                if (row < p.len_q) write_columns(out, c0, p.dim, o, p.scale);
+            } else if (row < p.len_q) {
+                write_zeros(out, c0, min(c0 + 32, p.dim));
+            }
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    settle(gave_up);
+    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+}
+
+// dK and dV: 128 keys to a CTA, which goes over the query tiles of every head that shares them.  All
+// products are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor
+// memory.  Tensor memory: scores (over them P^T) 0, dP^T (over it dS^T) 128, sums of dV 256, of dK 384.
+template <int DH>
+struct DkvSmem {
+    static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
+    static constexpr int SLOTS = 2;
+    alignas(1024) uint8_t k[TILE_BYTES], v[TILE_BYTES], q[SLOTS][TILE_BYTES], dout[SLOTS][TILE_BYTES];
+    alignas(16) float stats[SLOTS][2 * TILE];
+    uint64_t kv_full, q_full[SLOTS], q_free[SLOTS], do_full[SLOTS], do_free[SLOTS], s_full, dp_full, p_ready, ds_ready, sums_full, landed;
+    uint32_t tmem, gave_up;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+           const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
+    extern __shared__ uint8_t raw[];
+    using Smem = DkvSmem<DH>;
+    auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int bh = blockIdx.x % (p.batch * p.heads_kv), key0 = static_cast<int>(blockIdx.x / (p.batch * p.heads_kv)) * TILE;    // early keys are seen most
+    const int b = bh / p.heads_kv, h_kv = bh % p.heads_kv, shared = p.heads / p.heads_kv;
+    const Seq seq(p, b);
+    const int first_tile = seq.first_query_of(key0) / TILE;
+    const int per_head = key0 < seq.m ? max(0, tiles(seq.n) - first_tile) : 0, n = per_head * shared;
+
+    if (threadIdx.x == 0) {
+        bar_init(&sm.kv_full, 1);
+        bar_init(&sm.landed, 1);
+        for (int i = 0; i < Smem::SLOTS; ++i)
+            bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1), bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
+        bar_init(&sm.s_full, 1), bar_init(&sm.dp_full, 1), bar_init(&sm.sums_full, 1);
+        bar_init(&sm.p_ready, WORKERS), bar_init(&sm.ds_ready, WORKERS);
+        sm.gave_up = 0;
+        fence_async_smem();
+    }
+    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = sm.tmem;
+    volatile uint32_t *gave_up = &sm.gave_up;
+
+    if (warp == WARP_LOAD) {
+        if (n > 0) {
+            if (lane == 0) {
+                bar_expect(&sm.kv_full, 2 * Smem::TILE_BYTES);
+                for (int c = 0; c < DH / 64; ++c) {
+                    copy_tile(smem_addr(sm.k) + c * CHUNK, &map_k, &sm.kv_full, c * 64, key0, h_kv, b);
+                    copy_tile(smem_addr(sm.v) + c * CHUNK, &map_v, &sm.kv_full, c * 64, key0, h_kv, b);
+                }
+            }
+            __syncwarp();
+            uint32_t landed_phase = 0;
+            for (int i = 0; i < n; ++i) {
+                const int slot = i % Smem::SLOTS, h = h_kv * shared + i / per_head, tile = first_tile + i % per_head;
+                const uint32_t free_parity = (i / Smem::SLOTS + 1) & 1;
+                if (!bar_wait(&sm.q_free[slot], free_parity, gave_up)) break;
+                // the statistics arrive at the queries' barrier: their bytes are announced without an arrival
+                if (lane == 0) {
+                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&sm.q_full[slot])), "r"(static_cast<uint32_t>(sizeof(sm.stats[0]))) : "memory");
+                    copy_bytes(smem_addr(sm.stats[slot]), p.stats + ((static_cast<int64_t>(b) * p.heads + h) * p.tiles_q + tile) * 2 * TILE, sizeof(sm.stats[0]), &sm.q_full[slot]);
+                }
+                __syncwarp();
+                if (!load_tile<DH, true>(smem_addr(sm.q[slot]), sm.q[slot], &map_q, &sm.q_full[slot], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
+                if (!bar_wait(&sm.do_free[slot], free_parity, gave_up)) break;
+                if (!load_tile<DH, true>(smem_addr(sm.dout[slot]), sm.dout[slot], &map_do, &sm.do_full[slot], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
+            }
+        }
+    } else if (warp == WARP_MMA) {
+        auto scores = [&](int i) {
+            const int slot = i % Smem::SLOTS;
+            if (!bar_wait(&sm.q_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
+            if (lane == 0) {
+                product_rows<DH>(tmem, smem_addr(sm.k), smem_addr(sm.q[slot]));
+                mma_commit(&sm.s_full);
+            }
+            __syncwarp();
+            return true;
+        };
+        auto dprobs = [&](int i) {
+            const int slot = i % Smem::SLOTS;
+            if (!bar_wait(&sm.do_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
+            if (lane == 0) {
+                product_rows<DH>(tmem + TILE, smem_addr(sm.v), smem_addr(sm.dout[slot]));
+                mma_commit(&sm.dp_full);
+            }
+            __syncwarp();
+            return true;
+        };
+        if (n > 0 && bar_wait(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0)) {
+            for (int i = 0; i < n; ++i) {
+                const int slot = i % Smem::SLOTS;
+                if (!bar_wait(&sm.p_ready, i & 1, gave_up)) break;
+                tmem_fence_after();
+                if (lane == 0) {
+                    product_down<DH>(tmem + 2 * TILE, tmem, smem_addr(sm.dout[slot]), i > 0);
+                    mma_commit(&sm.do_free[slot]);
+                }
+                __syncwarp();
+                if (i + 1 < n && !scores(i + 1)) break;
+                if (!bar_wait(&sm.ds_ready, i & 1, gave_up)) break;
+                tmem_fence_after();
+                if (lane == 0) {
+                    product_down<DH>(tmem + 3 * TILE, tmem + TILE, smem_addr(sm.q[slot]), i > 0);
+                    mma_commit(&sm.q_free[slot]);
+                    if (i == n - 1) mma_commit(&sm.sums_full);
+                }
+                __syncwarp();
+                if (i + 1 < n && !dprobs(i + 1)) break;
+            }
+        }
+    } else {
+        const int g = warp / 4, key = key0 + threadIdx.x % TILE;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+        bool ok = true;
+        for (int i = 0; i < n; ++i) {
+            const int slot = i % Smem::SLOTS, row0 = (first_tile + i % per_head) * TILE;
+            const float4 *lse = reinterpret_cast<const float4 *>(sm.stats[slot] + g * 64), *delta = reinterpret_cast<const float4 *>(sm.stats[slot] + TILE + g * 64);
+            if (!(ok = bar_wait(&sm.q_full[slot], i / Smem::SLOTS & 1, gave_up) && bar_wait(&sm.s_full, i & 1, gave_up))) break;
+            tmem_fence_after();
+            uint32_t s[2][32], d[2][32], packed[32];
+            tmem_load32(lanes + g * 64, s[0]);
+            tmem_load32(lanes + g * 64 + 32, s[1]);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 l = lse[c / 4];
+                const float at[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) s[c / 32][c % 32 + k] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c / 32][c % 32 + k]), p.scale_log2, -at[k])));
+            }
+            if (seq.causal && row0 < key0 + TILE - 1 - seq.shift) {       // the last key is not seen by the first query
+                const int hidden = key - seq.shift - row0 - g * 64;        // columns before it do not see the key
+#pragma unroll
+                for (int c = 0; c < 64; ++c)
+                    if (c < hidden) s[c / 32][c % 32] = 0;
+            }
+#pragma unroll
+            for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(__uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1]));
+            tmem_store32(lanes + g * 64, packed);
+            tmem_wait_stores();
+            tmem_fence_before();
+            bar_arrive(&sm.p_ready);
+            if (!(ok = bar_wait(&sm.dp_full, i & 1, gave_up))) break;
+            tmem_fence_after();
+            tmem_load32(lanes + TILE + g * 64, d[0]);
+            tmem_load32(lanes + TILE + g * 64 + 32, d[1]);
+            tmem_wait_loads();
+#pragma unroll
+            for (int c = 0; c < 64; c += 4) {
+                const float4 l = delta[c / 4];
+                const float at[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                for (int k = 0; k < 4; k += 2) {
+                    const int e = c + k;
+                    packed[e / 2] = pack_bf16(__uint_as_float(s[e / 32][e % 32]) * (__uint_as_float(d[e / 32][e % 32]) - at[k]),
+                                              __uint_as_float(s[e / 32][e % 32 + 1]) * (__uint_as_float(d[e / 32][e % 32 + 1]) - at[k + 1]));
+                }
+            }
+            tmem_store32(lanes + TILE + g * 64, packed);
+            tmem_wait_stores();
+            tmem_fence_before();
+            bar_arrive(&sm.ds_ready);
+        }
+        if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
+        tmem_fence_after();
+        // one group writes dV, the other dK
+        const int64_t *stride = g == 0 ? p.out2_stride : p.out_stride;
+        __nv_bfloat16 *out = (g == 0 ? p.out2 : p.out) + b * stride[0] + key * stride[1] + h_kv * stride[2];
+#pragma unroll
+        for (int c = 0; c < DH; c += 32) {
+            if (n > 0 && ok) {
+                uint32_t o[32];
+                tmem_load32(lanes + (2 + g) * TILE + c, o);
+                tmem_wait_loads();
+                if (key >= seq.m)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0;
+                if (key < p.len_kv) write_columns(out, c, p.dim, o, g == 0 ? 1.0f : p.scale);
+            } else if (key < p.len_kv) {
+                write_zeros(out, c, min(c + 32, p.dim));
+            }
+        }
+    }
+    tmem_fence_before();
+    __syncthreads();
+    settle(gave_up);
+    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+}
+
+// ---------------------------------------------------------------------------------- host side
+typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+encode_fn encoder() {
+    static const encode_fn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            f = nullptr;
+        }
+        return reinterpret_cast<encode_fn>(f);
+    }();
+    return fn;
+}
+
+int make_map(CUtensorMap *map, const char *what, const void *at, const int64_t *stride, int batch, int tokens, int heads, int dim) {
+    const encode_fn encode = encoder();
+    if (encode == nullptr) return fail(KT_ERR_CUDA, "the driver does not offer cuTensorMapEncodeTiled");
+    const cuuint64_t sizes[4] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(tokens), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(batch)};
+    // the stride of a dimension of one is never used
+    const cuuint64_t strides[3] = {tokens > 1 ? static_cast<cuuint64_t>(stride[1]) * 2 : 16, heads > 1 ? static_cast<cuuint64_t>(stride[2]) * 2 : 16,
+                                   batch > 1 ? static_cast<cuuint64_t>(stride[0]) * 2 : 16};
+    const cuuint32_t box[4] = {64, TILE, 1, 1}, step[4] = {1, 1, 1, 1};
+    const CUresult rc = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(at), sizes, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (rc != CUDA_SUCCESS) return fail(KT_ERR_CUDA, "describing %s to the copy engine failed with driver status %d", what, static_cast<int>(rc));
+    return KT_OK;
+}
+
+int check_heads(const char *what, const void *at, const int64_t *stride, int batch, int tokens, int heads) {
+    if (at == nullptr) return fail(KT_ERR_INVALID, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(at) % 16) return fail(KT_ERR_ALIGN, "%s is not 16-byte aligned", what);
+    const int size[3] = {batch, tokens, heads};
+    for (int i = 0; i < 3; ++i) {
+        if (size[i] <= 1) continue;
+        if (stride[i] % 8) return fail(KT_ERR_ALIGN, "%s: the strides of batch, token and head must be multiples of 8 elements", what);
+        if (stride[i] < 8 || stride[i] >= INT64_C(1) << 38) return fail(KT_ERR_SHAPE, "%s: a stride of %lld elements (expanded tensors need a copy)", what, (long long)stride[i]);
+    }
+    return KT_OK;
+}
+
+int fill(const kt_attn *a, AttnParams *p) {
+    if (a == nullptr) return fail(KT_ERR_INVALID, "the description is NULL");
+    if (a->dtype != KT_BF16) return fail(KT_ERR_INVALID, "attention takes KT_BF16 heads");
+    if (a->batch < 0 || a->len_q < 0 || a->len_kv < 0 || a->heads < 1 || a->heads_kv < 1) return fail(KT_ERR_SHAPE, "negative sizes or no heads");
+    if (a->heads % a->heads_kv) return fail(KT_ERR_SHAPE, "%d query heads cannot share %d key/value heads", a->heads, a->heads_kv);
+    if (a->head_dim < 8 || a->head_dim > KT_ATTN_MAX_DIM || a->head_dim % 8) return fail(KT_ERR_SHAPE, "head_dim %d: a multiple of 8 up to %d expected", a->head_dim, KT_ATTN_MAX_DIM);
+    if (!(a->scale > 0.0f) || !(a->scale < INFINITY)) return fail(KT_ERR_INVALID, "scale must be positive and finite");
+    if (a->len_q > (1 << 30) || a->len_kv > (1 << 30)) return fail(KT_ERR_SHAPE, "more than 2^30 tokens");
+    *p = AttnParams{};
+    p->batch = a->batch, p->heads = a->heads, p->heads_kv = a->heads_kv, p->len_q = a->len_q, p->len_kv = a->len_kv, p->dim = a->head_dim;
+    p->causal = a->causal != 0, p->used_q = a->used_q, p->used_kv = a->used_kv, p->scale = a->scale, p->scale_log2 = a->scale * LOG2E;
+    p->tiles_q = (p->len_q + TILE - 1) / TILE, p->tiles_kv = (p->len_kv + TILE - 1) / TILE;
+    if (static_cast<int64_t>(p->batch) * p->heads * (p->tiles_q > p->tiles_kv ? p->tiles_q : p->tiles_kv) > INT64_C(1) << 27)
+        return fail(KT_ERR_SHAPE, "batch x heads x tokens is too large");
+    for (const int32_t *u : {a->used_q, a->used_kv})
+        if (reinterpret_cast<uintptr_t>(u) % 4) return fail(KT_ERR_ALIGN, "used_q or used_kv is not 4-byte aligned");
+    return KT_OK;
+}
+
+template <typename Smem, typename Kernel>
+int room(Kernel kernel, size_t *bytes) {
+    *bytes = sizeof(Smem) + 1024;                // the tiles start at a multiple of 1024
+    KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*bytes)));
+    return KT_OK;
+}
+
+template <int DH>
+int start_forward(const CUtensorMap (&m)[3], const AttnParams &p, cudaStream_t st) {
+    size_t bytes = 0;
+    if (int rc = room<FwdSmem<DH>>(k_attn_forward<DH>, &bytes)) return rc;
+    k_attn_forward<DH><<<static_cast<unsigned>(p.batch * p.heads * ((p.tiles_q + 1) / 2)), THREADS, bytes, st>>>(m[0], m[1], m[2], p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+
+template <int DH>
+int start_dq(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
+    size_t bytes = 0;
+    if (int rc = room<DqSmem<DH>>(k_attn_dq<DH>, &bytes)) return rc;
+    k_attn_dq<DH><<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q), THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+
+template <int DH>
+int start_dkv(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
+    size_t bytes = 0;
+    if (int rc = room<DkvSmem<DH>>(k_attn_dkv<DH>, &bytes)) return rc;
+    k_attn_dkv<DH><<<static_cast<unsigned>(p.batch * p.heads_kv * p.tiles_kv), THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+
+// Rows of zeros where there is nothing to attend to (no keys at all).
+int clear(__nv_bfloat16 *at, const int64_t *stride, int batch, int tokens, int heads, int dim, cudaStream_t st) {
+    for (int b = 0; b < batch; ++b)
+        for (int h = 0; h < heads; ++h)
+            KT_CUDA(cudaMemset2DAsync(at + b * stride[0] + h * stride[2], static_cast<size_t>(tokens > 1 ? stride[1] : dim) * 2, 0, static_cast<size_t>(dim) * 2, tokens, st));
+    return KT_OK;
+}
+
+void copy_strides(int64_t *to, const int64_t *from) {
+    for (int i = 0; i < 3; ++i) to[i] = from[i];
+}
+
+}  // namespace
+
+extern "C" {
+
+int kt_attn_forward(const kt_attn *a, const void *q, const int64_t *q_stride, const void *k, const int64_t *k_stride, const void *v,
+                    const int64_t *v_stride, void *out, const int64_t *out_stride, float *lse, void *stream) {
+    AttnParams p;
+    if (int rc = fill(a, &p)) return rc;
+    if (p.batch == 0 || p.len_q == 0) return KT_OK;
+    if (!q_stride || !k_stride || !v_stride || !out_stride) return fail(KT_ERR_INVALID, "a stride array is NULL");
+    if (int rc = check_heads("q", q, q_stride, p.batch, p.len_q, p.heads)) return rc;
+    if (int rc = check_heads("out", out, out_stride, p.batch, p.len_q, p.heads)) return rc;
+    if (p.len_kv > 0) {
+        if (int rc = check_heads("k", k, k_stride, p.batch, p.len_kv, p.heads_kv)) return rc;
+        if (int rc = check_heads("v", v, v_stride, p.batch, p.len_kv, p.heads_kv)) return rc;
+    }
+    if (lse == nullptr) return fail(KT_ERR_INVALID, "lse is NULL");
+    if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(KT_ERR_ALIGN, "lse is not 4-byte aligned");
+    p.out = static_cast<__nv_bfloat16 *>(out), p.lse = lse;
+    copy_strides(p.out_stride, out_stride);
+    CUtensorMap m[3];
+    if (int rc = make_map(&m[0], "q", q, q_stride, p.batch, p.len_q, p.heads, p.dim)) return rc;
+    // without keys the kernel copies nothing and only writes its empty rows: any valid map will do
+    const bool keys = p.len_kv > 0;
+    if (int rc = make_map(&m[1], "k", keys ? k : q, keys ? k_stride : q_stride, p.batch, keys ? p.len_kv : p.len_q, keys ? p.heads_kv : p.heads, p.dim)) return rc;
+    if (int rc = make_map(&m[2], "v", keys ? v : q, keys ? v_stride : q_stride, p.batch, keys ? p.len_kv : p.len_q, keys ? p.heads_kv : p.heads, p.dim)) return rc;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return p.dim <= 64 ? start_forward<64>(m, p, st) : start_forward<128>(m, p, st);
+}
+
+int64_t kt_attn_workspace(int batch, int heads, int len_q) {
+    if (batch < 0 || heads < 0 || len_q < 0) return 0;
+    return static_cast<int64_t>(batch) * heads * ((static_cast<int64_t>(len_q) + TILE - 1) / TILE) * 2 * TILE * static_cast<int64_t>(sizeof(float));
+}
+
+int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_stride, const void *q, const int64_t *q_stride, const void *k,
+                     const int64_t *k_stride, const void *v, const int64_t *v_stride, const void *out, const int64_t *out_stride, const float *lse,
+                     void *dq, const int64_t *dq_stride, void *dk, const int64_t *dk_stride, void *dv, const int64_t *dv_stride, void *workspace,
+                     int64_t workspace_bytes, void *stream) {
+    AttnParams p;
+    if (int rc = fill(a, &p)) return rc;
+    if (p.batch == 0 || (p.len_q == 0 && p.len_kv == 0)) return KT_OK;
+    if (!dout_stride || !q_stride || !k_stride || !v_stride || !out_stride || !dq_stride || !dk_stride || !dv_stride) return fail(KT_ERR_INVALID, "a stride array is NULL");
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    struct {
+        const char *what;
+        const void *at;
+        const int64_t *stride;
+        int tokens, heads;
+    } const all[] = {{"dout", dout, dout_stride, p.len_q, p.heads}, {"q", q, q_stride, p.len_q, p.heads}, {"out", out, out_stride, p.len_q, p.heads},
+                     {"dq", dq, dq_stride, p.len_q, p.heads}, {"k", k, k_stride, p.len_kv, p.heads_kv}, {"v", v, v_stride, p.len_kv, p.heads_kv},
+                     {"dk", dk, dk_stride, p.len_kv, p.heads_kv}, {"dv", dv, dv_stride, p.len_kv, p.heads_kv}};
+    for (const auto &t : all)
+        if (t.tokens > 0)
+            if (int rc = check_heads(t.what, t.at, t.stride, p.batch, t.tokens, t.heads)) return rc;
+    if (p.len_kv == 0) return clear(static_cast<__nv_bfloat16 *>(dq), dq_stride, p.batch, p.len_q, p.heads, p.dim, st);
+    if (p.len_q == 0) {
+        if (int rc = clear(static_cast<__nv_bfloat16 *>(dk), dk_stride, p.batch, p.len_kv, p.heads_kv, p.dim, st)) return rc;
+        return clear(static_cast<__nv_bfloat16 *>(dv), dv_stride, p.batch, p.len_kv, p.heads_kv, p.dim, st);
+    }
+    if (lse == nullptr) return fail(KT_ERR_INVALID, "lse is NULL");
+    if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(KT_ERR_ALIGN, "lse is not 4-byte aligned");
+    const int64_t need = kt_attn_workspace(p.batch, p.heads, p.len_q);
+    if (workspace == nullptr) return fail(KT_ERR_INVALID, "workspace is NULL");
+    if (workspace_bytes < need) return fail(KT_ERR_SHAPE, "workspace of %lld bytes: %lld are needed", (long long)workspace_bytes, (long long)need);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(KT_ERR_ALIGN, "workspace is not 16-byte aligned");
+    CUtensorMap m[4];
+    if (int rc = make_map(&m[0], "q", q, q_stride, p.batch, p.len_q, p.heads, p.dim)) return rc;
+    if (int rc = make_map(&m[1], "k", k, k_stride, p.batch, p.len_kv, p.heads_kv, p.dim)) return rc;
+    if (int rc = make_map(&m[2], "v", v, v_stride, p.batch, p.len_kv, p.heads_kv, p.dim)) return rc;
+    if (int rc = make_map(&m[3], "dout", dout, dout_stride, p.batch, p.len_q, p.heads, p.dim)) return rc;
+    p.o = static_cast<const __nv_bfloat16 *>(out), p.dout = static_cast<const __nv_bfloat16 *>(dout), p.lse = const_cast<float *>(lse), p.stats = static_cast<float *>(workspace);
+    copy_strides(p.o_stride, out_stride);
+    copy_strides(p.dout_stride, dout_stride);
+    k_attn_stats<<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q * (TILE / 16)), 256, 0, st>>>(p);
+    KT_CUDA(cudaGetLastError());
+    AttnParams pq = p;
+    pq.out = static_cast<__nv_bfloat16 *>(dq);
+    copy_strides(pq.out_stride, dq_stride);
+    if (int rc = p.dim <= 64 ? start_dq<64>(m, pq, st) : start_dq<128>(m, pq, st)) return rc;
+    p.out = static_cast<__nv_bfloat16 *>(dk), p.out2 = static_cast<__nv_bfloat16 *>(dv);
+    copy_strides(p.out_stride, dk_stride);
+    copy_strides(p.out2_stride, dv_stride);
+    return p.dim <= 64 ? start_dkv<64>(m, p, st) : start_dkv<128>(m, p, st);
+}
+
+int kt_attn_given_up(int64_t *count) {
+    if (count == nullptr) return fail(KT_ERR_INVALID, "count is NULL");
+    unsigned long long n = 0;
+    KT_CUDA(cudaMemcpyFromSymbol(&n, g_waits_given_up, sizeof(n)));
+    *count = static_cast<int64_t>(n);
+    return KT_OK;
+}
+
+}  // extern "C"

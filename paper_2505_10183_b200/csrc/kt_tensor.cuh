@@ -1,0 +1,191 @@
+// kt_tensor.cuh -- what a kernel needs to feed the tensor cores of sm_100a: barriers in shared
+// memory with bounded waits, tile copies (TMA), tensor memory and its accesses, and the matrix
+// instruction on bf16 operands with fp32 sums.
+//
+// Tiles in shared memory are rows of 64 bf16 (128 bytes) in the 128-byte swizzle, 128 rows to a chunk
+// of 16 KB, chunks side by side for wider rows.  A chunk serves as an operand in both
+// directions: with the reduction along the row (K-major) or down the rows (MN-major).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace {
+
+constexpr int TILE = 128;                       // rows of a tile: the M and N of the matrix instruction
+constexpr uint32_t CHUNK = TILE * 128;          // bytes of 128 rows of 64 bf16
+constexpr uint64_t WAIT_NS = 2000000000;        // a wait gives up after this long
+
+// Waits that gave up since the library was loaded; a kernel that counts here ends without a result.
+__device__ unsigned long long g_waits_given_up;
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+// ---------------------------------------------------------------------------------- barriers
+__device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+
+// Waits for the phase of that parity to end; called by whole warps.  False when it gave up, or when
+// another warp of the CTA did: the caller then leaves its loop, and the kernel ends.
+__device__ __noinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
+    const uint64_t start = now_ns();
+    for (uint32_t n = 1;; ++n) {
+        if (bar_try(bar, parity)) return true;
+        if (n % 16 == 0) {
+            if (*gave_up) return false;
+            if (now_ns() - start > WAIT_NS) {
+                *gave_up = 1;
+                atomicAdd(&g_waits_given_up, 1ull);
+                return false;
+            }
+        }
+    }
+}
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
+    bool ok = bar_try(bar, parity);
+    if (!ok) ok = bar_wait_slow(bar, parity, gave_up);
+    return __all_sync(0xFFFFFFFFu, ok);
+}
+
+// ------------------------------------------------------------------------------- tile copies
+// [dim, tokens, heads, batch] -> 128 tokens of 64 elements.
+__device__ __forceinline__ void copy_tile(uint32_t to, const CUtensorMap *map, uint64_t *bar, int dim, int token, int head, int batch) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(to),
+        "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_addr(bar)), "r"(dim), "r"(token), "r"(head), "r"(batch)
+        : "memory");
+}
+// Plain bytes; both addresses and the size are multiples of 16.
+__device__ __forceinline__ void copy_bytes(uint32_t to, const void *from, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes),
+                 "r"(smem_addr(bar))
+                 : "memory");
+}
+// What threads have written to shared memory becomes visible to the tensor cores and copies.
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ------------------------------------------------------------------------------ tensor memory
+__device__ __forceinline__ void tmem_alloc(uint32_t *to, uint32_t columns) {      // one whole warp
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns) {        // the same warp
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+// 32 columns of the 32 lanes that belong to the warp's place in its group of four.
+__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t (&r)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t (&r)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 :
+                 : "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+                   "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+                   "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 :
+                 : "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                   "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Order between tensor memory accesses and barrier traffic: before an arrival, after a wait.
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// -------------------------------------------------------------------------- matrix instruction
+// Instruction word: fp32 sums, bf16 operands, M = 128; bit 16 says that B is MN-major.
+__host__ __device__ constexpr uint32_t mma_word(int n, bool b_down) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(TILE / 16) << 24);
+}
+// Operand words (without the address): groups of 8 rows are 1024 bytes apart; for an MN-major operand
+// chunks of 64 elements along the row are CHUNK apart.
+constexpr uint64_t OPERAND_ALONG = (1ull << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+constexpr uint64_t OPERAND_DOWN = (static_cast<uint64_t>(CHUNK >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+__device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | ((addr >> 4) & 0x3FFF); }
+
+__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t word, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(word), "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t word, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(word), "r"(static_cast<uint32_t>(add))
+        : "memory");
+}
+// An arrival once every matrix instruction that this thread has issued is done.
+__device__ __forceinline__ void mma_commit(uint64_t *bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+
+// D[128 x 128] = A B^T over rows of DH elements: both tiles K-major.
+template <int DH>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b) {
+#pragma unroll
+    for (int k = 0; k < DH / 16; ++k) {
+        const uint32_t off = (k / 4) * CHUNK + (k % 4) * 32;
+        mma_smem(d, operand(OPERAND_ALONG, a + off), operand(OPERAND_ALONG, b + off), mma_word(TILE, false), k > 0);
+    }
+}
+// D[128 x DH] (+)= A B over 128 rows of B: A is bf16 in tensor memory, the first 64 of its reduction
+// index in 32 columns at `a`, the others 64 columns further; B a tile, read down its rows.
+template <int DH>
+__device__ __forceinline__ void product_down(uint32_t d, uint32_t a, uint32_t b, bool add) {
+#pragma unroll
+    for (int k = 0; k < TILE / 16; ++k)
+        mma_tmem(d, a + (k / 4) * 64 + (k % 4) * 8, operand(OPERAND_DOWN, b + k * 2048), mma_word(DH, true), add || k > 0);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+}  // namespace
