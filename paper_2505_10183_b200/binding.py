@@ -172,10 +172,17 @@ def kt_ptrs(tensors: Ptrs) -> PtrArray:
     return tensors if isinstance(tensors, PtrArray) else PtrArray(tensors)
 
 
-def _stream(stream) -> C.c_void_p:
+# The handle of the current stream, without an object around it where torch offers that: building one
+# costs as much as a launch.
+_raw_stream, _device = (getattr(torch._C, n, None) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice"))
+
+
+def _stream(stream):
     if stream is None:
+        if _raw_stream is not None and _device is not None:
+            return _raw_stream(_device())
         stream = torch.cuda.current_stream()
-    return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _i32(values) -> C.Array:
@@ -673,12 +680,17 @@ def kt_sync_flat_static(group_of: Sequence[int], shares: Sequence[int], grads: S
 
 
 # ------------------------------------------------------------- operators of a training step
-def _matrix(t: torch.Tensor, what: str, like: Optional[torch.Tensor] = None):
-    """(address, row stride) of a matrix with contiguous columns, of `like`'s shape and type where given."""
-    if t.dim() != 2 or t.dtype not in _DTYPES or (t.size(1) > 1 and t.stride(1) != 1):
+def _first(t: torch.Tensor, what: str):
+    """(address, row stride, shape, type) of a matrix with contiguous columns."""
+    if t.dtype not in _DTYPES or t.dim() != 2 or (t.stride(1) != 1 and t.size(1) > 1):
         raise KtError(KT_ERR_SHAPE, "%s: a float32 or bfloat16 matrix with contiguous columns expected" % what)
-    if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
-        raise KtError(KT_ERR_SHAPE, "%s: shape or dtype differs" % what)
+    return t.data_ptr(), t.stride(0), t.shape, t.dtype
+
+
+def _like(t: torch.Tensor, what: str, shape, dtype):
+    """(address, row stride) of a matrix of that shape and type with contiguous columns."""
+    if t.dtype != dtype or t.shape != shape or (t.stride(1) != 1 and shape[1] > 1):
+        raise KtError(KT_ERR_SHAPE, "%s: shape, dtype or layout differs" % what)
     return t.data_ptr(), t.stride(0)
 
 
@@ -688,23 +700,25 @@ def _codes(codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], rows: 
         return None, None
     if codes is None or scales is None:
         raise KtError(KT_ERR_INVALID, "a checkpoint has codes and scales: one of them is missing")
-    if (codes.dtype != torch.int8 or scales.dtype != torch.float32 or not codes.is_contiguous() or not scales.is_contiguous()
-            or codes.shape != (rows, (cols + 15) // 16 * 16) or scales.shape != (rows, -(-cols // KT_CKPT_BLOCK))):
+    if (codes.dtype != torch.int8 or scales.dtype != torch.float32 or codes.shape != (rows, (cols + 15) // 16 * 16)
+            or scales.shape != (rows, -(-cols // KT_CKPT_BLOCK)) or not codes.is_contiguous() or not scales.is_contiguous()):
         raise KtError(KT_ERR_SHAPE, "codes: int8 [rows, kt_ckpt_pitch(cols)], scales: float32 [rows, kt_ckpt_blocks(cols)], contiguous")
     return codes.data_ptr(), scales.data_ptr()
 
 
 def _params(cols: int, *tensors: Optional[torch.Tensor]):
     """Addresses of vectors over the columns (None stays None), and their type."""
-    dtype, got = KT_F32, []
-    given = [t for t in tensors if t is not None]
-    for t in given:
-        if t.dtype not in _DTYPES or t.dtype != given[0].dtype or t.shape != (cols,) or not t.is_contiguous():
-            raise KtError(KT_ERR_SHAPE, "weight, bias and their gradients: contiguous, [cols], all float32 or all bfloat16")
-        dtype = _DTYPES[t.dtype]
+    dtype, got = None, []
     for t in tensors:
-        got.append(None if t is None else t.data_ptr())
-    return got, dtype
+        if t is None:
+            got.append(None)
+            continue
+        if dtype is None:
+            dtype = t.dtype
+        if t.dtype != dtype or dtype not in _DTYPES or t.shape != (cols,) or not t.is_contiguous():
+            raise KtError(KT_ERR_SHAPE, "weight, bias and their gradients: contiguous, [cols], all float32 or all bfloat16")
+        got.append(t.data_ptr())
+    return got, KT_F32 if dtype is None else _DTYPES[dtype]
 
 
 def _per_row(t: Optional[torch.Tensor], rows: int, what: str):
@@ -725,33 +739,31 @@ def kt_ckpt_blocks(cols: int) -> int:
 
 def kt_ckpt_store(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
     """Keeps x [rows, cols] in 8 bits: codes int8 [rows, kt_ckpt_pitch(cols)], scales float32 [rows, kt_ckpt_blocks(cols)]."""
-    px, sx = _matrix(x, "x")
-    rows, cols = x.shape
+    px, sx, (rows, cols), dtype = _first(x, "x")
     pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_ckpt_store(px, sx, pc, ps, rows, cols, _DTYPES[x.dtype], _stream(stream)))
+    _check(_lib.kt_ckpt_store(px, sx, pc, ps, rows, cols, _DTYPES[dtype], _stream(stream)))
 
 
 def kt_ckpt_restore(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Tensor] = None,
                     bias: Optional[torch.Tensor] = None, stream=None) -> None:
     """out = the kept values [* weight] [+ bias]."""
-    po, so = _matrix(out, "out")
-    rows, cols = out.shape
+    po, so, (rows, cols), dtype = _first(out, "out")
     pc, ps = _codes(codes, scales, rows, cols)
     (pw, pb), pd = _params(cols, weight, bias)
-    _check(_lib.kt_ckpt_restore(pc, ps, pw, pb, pd, po, so, rows, cols, _DTYPES[out.dtype], _stream(stream)))
+    _check(_lib.kt_ckpt_restore(pc, ps, pw, pb, pd, po, so, rows, cols, _DTYPES[dtype], _stream(stream)))
 
 
 def kt_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
                     mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5,
                     codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
     """Layer norm of the rows of x; with codes and scales the normalised rows are kept in 8 bits."""
-    px, sx = _matrix(x, "x")
-    po, so = _matrix(out, "out", x)
-    rows, cols = x.shape
+    px, sx, shape, dtype = _first(x, "x")
+    po, so = _like(out, "out", shape, dtype)
+    rows, cols = shape
     (pw, pb), pd = _params(cols, weight, bias)
     pc, ps = _codes(codes, scales, rows, cols)
     _check(_lib.kt_norm_forward(px, sx, pw, pb, pd, po, so, _per_row(mean, rows, "mean"), _per_row(rstd, rows, "rstd"), pc, ps,
-                                rows, cols, _DTYPES[x.dtype], eps, _stream(stream)))
+                                rows, cols, _DTYPES[dtype], eps, _stream(stream)))
 
 
 def kt_norm_workspace(rows: int, cols: int) -> int:
@@ -764,15 +776,15 @@ def kt_norm_backward(dout: torch.Tensor, weight: Optional[torch.Tensor], rstd: t
                      x: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
                      codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
     """From x and mean, or from the checkpoint (codes, scales) that the forward pass left."""
-    pg, sg = _matrix(dout, "dout")
-    pd, sd = _matrix(dx, "dx", dout)
-    px, sx = _matrix(x, "x", dout) if x is not None else (None, 0)
-    rows, cols = dout.shape
+    pg, sg, shape, dtype = _first(dout, "dout")
+    pd, sd = _like(dx, "dx", shape, dtype)
+    px, sx = _like(x, "x", shape, dtype) if x is not None else (None, 0)
+    rows, cols = shape
     (pw, pdw, pdb), kind = _params(cols, weight, dweight, dbias)
     pc, ps = _codes(codes, scales, rows, cols)
     pws, nws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
     _check(_lib.kt_norm_backward(pg, sg, px, sx, _per_row(mean, rows, "mean"), pc, ps, _per_row(rstd, rows, "rstd"), pw, kind,
-                                 pd, sd, pdw, pdb, pws, nws, rows, cols, _DTYPES[dout.dtype], _stream(stream)))
+                                 pd, sd, pdw, pdb, pws, nws, rows, cols, _DTYPES[dtype], _stream(stream)))
 
 
 _ACTS = {"gelu": KT_GELU, "silu": KT_SILU, KT_GELU: KT_GELU, KT_SILU: KT_SILU}
@@ -787,50 +799,45 @@ def _act_kind(kind) -> int:
 def kt_act_forward(x: torch.Tensor, out: torch.Tensor, codes: Optional[torch.Tensor] = None,
                    scales: Optional[torch.Tensor] = None, kind="gelu", stream=None) -> None:
     """out = GELU or SiLU of x; with codes and scales x is kept in 8 bits by the same pass."""
-    px, sx = _matrix(x, "x")
-    po, so = _matrix(out, "out", x)
-    rows, cols = x.shape
+    px, sx, shape, dtype = _first(x, "x")
+    po, so = _like(out, "out", shape, dtype)
+    rows, cols = shape
     pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_act_forward(px, sx, po, so, pc, ps, rows, cols, _DTYPES[x.dtype], _act_kind(kind), _stream(stream)))
+    _check(_lib.kt_act_forward(px, sx, po, so, pc, ps, rows, cols, _DTYPES[dtype], _act_kind(kind), _stream(stream)))
 
 
 def kt_act_backward(dout: torch.Tensor, codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], dx: torch.Tensor,
                     kind="gelu", x: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx = dout * act'(x), x from its checkpoint or (codes and scales None) as it is."""
-    pg, sg = _matrix(dout, "dout")
-    pd, sd = _matrix(dx, "dx", dout)
-    px, sx = _matrix(x, "x", dout) if x is not None else (None, 0)
-    rows, cols = dout.shape
+    pg, sg, shape, dtype = _first(dout, "dout")
+    pd, sd = _like(dx, "dx", shape, dtype)
+    px, sx = _like(x, "x", shape, dtype) if x is not None else (None, 0)
+    rows, cols = shape
     pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_act_backward(pg, sg, px, sx, pc, ps, pd, sd, rows, cols, _DTYPES[dout.dtype], _act_kind(kind), _stream(stream)))
+    _check(_lib.kt_act_backward(pg, sg, px, sx, pc, ps, pd, sd, rows, cols, _DTYPES[dtype], _act_kind(kind), _stream(stream)))
 
 
-_Strides = C.c_int64 * 3
-
-
-def _heads(t: torch.Tensor, what: str, shape):
-    """(address, strides of batch, token and head) of a tensor [batch, tokens, heads, head_dim]."""
-    if t.dtype != torch.bfloat16 or t.shape != shape or (t.size(3) > 1 and t.stride(3) != 1):
-        raise KtError(KT_ERR_SHAPE, "%s: bfloat16 %s with a contiguous last dimension expected" % (what, list(shape)))
+def _heads(t: torch.Tensor, what: str, shape, strides: list) -> int:
+    """Address of a tensor [batch, tokens, heads, head_dim]; its strides of batch, token and head join the list."""
     s = t.stride()
-    return t.data_ptr(), _Strides(s[0], s[1], s[2])
+    if t.dtype != torch.bfloat16 or t.shape != shape or (s[3] != 1 and shape[3] > 1):
+        raise KtError(KT_ERR_SHAPE, "%s: bfloat16 %s with a contiguous last dimension expected" % (what, list(shape)))
+    strides += s[:3]
+    return t.data_ptr()
 
 
-def _attn(q: torch.Tensor, k: torch.Tensor, scale, causal, used_q, used_kv) -> _Attn:
-    if q.dim() != 4 or k.dim() != 4 or q.size(0) != k.size(0) or q.size(3) != k.size(3):
+def _attn(sq, sk, lse: torch.Tensor, scale, causal, used_q, used_kv) -> _Attn:
+    """kt_attn from the shapes of q and k, with the address of lse."""
+    if len(sq) != 4 or len(sk) != 4 or sq[0] != sk[0] or sq[3] != sk[3]:
         raise KtError(KT_ERR_SHAPE, "q and k: [batch, tokens, heads, head_dim] with the same batch and head_dim expected")
-    B, Lq, H, D = q.shape
+    B, Lq, H, D = sq
     for u in (used_q, used_kv):
         if u is not None and (u.dtype != torch.int32 or u.shape != (B,) or not u.is_contiguous()):
             raise KtError(KT_ERR_SHAPE, "used_q, used_kv: contiguous int32 [batch] expected")
-    return _Attn(B, Lq, k.size(1), H, k.size(2), D, KT_BF16, bool(causal), D ** -0.5 if scale is None else scale,
-                 None if used_q is None else used_q.data_ptr(), None if used_kv is None else used_kv.data_ptr())
-
-
-def _lse(lse: torch.Tensor, q: torch.Tensor):
-    if lse.dtype != torch.float32 or lse.shape != (q.size(0), q.size(2), q.size(1)) or not lse.is_contiguous():
+    if lse.dtype != torch.float32 or lse.shape != (B, H, Lq) or not lse.is_contiguous():
         raise KtError(KT_ERR_SHAPE, "lse: contiguous float32 [batch, heads, tokens] expected")
-    return lse.data_ptr()
+    return _Attn(B, Lq, sk[1], H, sk[2], D, KT_BF16, bool(causal), D ** -0.5 if scale is None else scale,
+                 None if used_q is None else used_q.data_ptr(), None if used_kv is None else used_kv.data_ptr())
 
 
 def kt_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
@@ -838,14 +845,18 @@ def kt_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torc
                     used_kv: Optional[torch.Tensor] = None, stream=None) -> None:
     """out = softmax(scale q k^T) v on bfloat16 [batch, tokens, heads, head_dim] (any strides that are multiples
     of 8; k and v may have fewer heads), lse float32 [batch, heads, tokens].  scale: 1 / sqrt(head_dim) by default."""
-    desc = _attn(q, k, scale, causal, used_q, used_kv)
-    (pq, sq), (pk, sk), (pv, sv), (po, so) = _heads(q, "q", q.shape), _heads(k, "k", k.shape), _heads(v, "v", k.shape), _heads(out, "out", q.shape)
-    _check(_lib.kt_attn_forward(C.byref(desc), pq, sq, pk, sk, pv, sv, po, so, _lse(lse, q), _stream(stream)))
+    sq, sk, st = q.shape, k.shape, []
+    desc = _attn(sq, sk, lse, scale, causal, used_q, used_kv)
+    pq, pk, pv, po = _heads(q, "q", sq, st), _heads(k, "k", sk, st), _heads(v, "v", sk, st), _heads(out, "out", sq, st)
+    strides = (C.c_int64 * 12)(*st)
+    at = C.addressof(strides)
+    _check(_lib.kt_attn_forward(C.byref(desc), pq, at, pk, at + 24, pv, at + 48, po, at + 72, lse.data_ptr(), _stream(stream)))
 
 
 def kt_attn_workspace(q: torch.Tensor, k: torch.Tensor) -> int:
     """Bytes that kt_attn_backward needs for tensors of q's and k's shape."""
-    return int(_lib.kt_attn_workspace(q.size(0), q.size(2), q.size(1)))
+    B, L, H, _ = q.shape
+    return _lib.kt_attn_workspace(B, H, L)
 
 
 def kt_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
@@ -853,11 +864,15 @@ def kt_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
                      causal: bool = False, used_q: Optional[torch.Tensor] = None, used_kv: Optional[torch.Tensor] = None,
                      stream=None) -> None:
     """Gradients of kt_attn_forward from its arguments and results; workspace: kt_attn_workspace bytes."""
-    desc = _attn(q, k, scale, causal, used_q, used_kv)
-    (pg, sg), (pq, sq), (po, so), (pdq, sdq) = (_heads(t, n, q.shape) for t, n in ((dout, "dout"), (q, "q"), (out, "out"), (dq, "dq")))
-    (pk, sk), (pv, sv), (pdk, sdk), (pdv, sdv) = (_heads(t, n, k.shape) for t, n in ((k, "k"), (v, "v"), (dk, "dk"), (dv, "dv")))
-    _check(_lib.kt_attn_backward(C.byref(desc), pg, sg, pq, sq, pk, sk, pv, sv, po, so, _lse(lse, q), pdq, sdq, pdk, sdk, pdv, sdv,
-                                 workspace.data_ptr() or None, workspace.numel() * workspace.element_size(), _stream(stream)))
+    sq, sk, st = q.shape, k.shape, []
+    desc = _attn(sq, sk, lse, scale, causal, used_q, used_kv)
+    pg, pq, pk, pv = _heads(dout, "dout", sq, st), _heads(q, "q", sq, st), _heads(k, "k", sk, st), _heads(v, "v", sk, st)
+    po, pdq, pdk, pdv = _heads(out, "out", sq, st), _heads(dq, "dq", sq, st), _heads(dk, "dk", sk, st), _heads(dv, "dv", sk, st)
+    strides = (C.c_int64 * 24)(*st)
+    at = C.addressof(strides)
+    _check(_lib.kt_attn_backward(C.byref(desc), pg, at, pq, at + 24, pk, at + 48, pv, at + 72, po, at + 96, lse.data_ptr(),
+                                 pdq, at + 120, pdk, at + 144, pdv, at + 168, workspace.data_ptr() or None,
+                                 workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
 def kt_attn_given_up() -> int:

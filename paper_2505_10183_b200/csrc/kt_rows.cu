@@ -30,7 +30,7 @@ constexpr int BLOCK = KT_CKPT_BLOCK;
 constexpr int E = 16;                    // row elements that a thread keeps in registers
 constexpr int GROUP_MAX = 512;           // threads on one row at most
 constexpr int64_t ROW_MAX = E * GROUP_MAX;   // wider rows are read again instead of kept
-constexpr int PARTS_MAX = 592;           // rows of partial weight gradients: four to an SM
+constexpr int SMS = 148;                 // of a B200: the grids are cut to them
 constexpr float SMALLEST = 7.888609052210118e-31f;   // 2^-100
 
 __device__ __forceinline__ uint4 load16(const void *p) {
@@ -38,6 +38,61 @@ __device__ __forceinline__ uint4 load16(const void *p) {
     asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
+
+// Two fp32 operations in one instruction: these kernels have enough arithmetic to an element for
+// the instruction rate to count beside memory.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmul.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tadd.rn.f32x2 d, a, b;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("{\n\t.reg .b64 a, b, c, d;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %5};\n\tmov.b64 c, {%6, %7};\n\tfma.rn.f32x2 d, a, b, c;\n\tmov.b64 {%0, %1}, d;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 both(float x) { return make_float2(x, x); }
+
+// Maximum and minimum that keep a NaN.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {
+    float d;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float inverse_fast(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Copies into shared memory that the issuing thread alone waits for and reads again.
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(void *to, const void *from) {
+    const unsigned at = static_cast<unsigned>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_issued() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // V consecutive elements of a row in one 16-byte vector, or what there is of them.
 template <typename T>
@@ -75,20 +130,26 @@ struct Elems<__nv_bfloat16> {
     __device__ static float up(__nv_bfloat16 x) { return __bfloat162float(x); }
 };
 
+// One vector of a row as it lies in memory; columns at or past `cols` are zeros.
 template <typename T, bool WIDE>
-__device__ __forceinline__ void load_row(const T *row, int64_t col, int64_t cols, float (&x)[Elems<T>::V]) {
-    constexpr int V = Elems<T>::V;
+__device__ __forceinline__ uint4 load_row(const T *row, int64_t col, int64_t cols) {
+    uint4 r = make_uint4(0, 0, 0, 0);
     if constexpr (WIDE) {
-        if (col < cols) {
-            Elems<T>::widen(load16(row + col), x);
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) x[i] = 0.0f;
-        }
+        if (col < cols) r = load16(row + col);
+    } else if constexpr (sizeof(T) == 4) {
+        const unsigned *at = reinterpret_cast<const unsigned *>(row) + col;
+        if (col < cols) r.x = at[0];
+        if (col + 1 < cols) r.y = at[1];
+        if (col + 2 < cols) r.z = at[2];
+        if (col + 3 < cols) r.w = at[3];
     } else {
+        const unsigned short *at = reinterpret_cast<const unsigned short *>(row) + col;
+        unsigned w[8];
 #pragma unroll
-        for (int i = 0; i < V; ++i) x[i] = col + i < cols ? Elems<T>::up(row[col + i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) w[i] = col + i < cols ? at[i] : 0;
+        r = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
     }
+    return r;
 }
 
 template <typename T, bool WIDE>
@@ -107,29 +168,43 @@ __device__ __forceinline__ void store_row(T *row, int64_t col, int64_t cols, con
 template <int V>
 __device__ __forceinline__ void load_param(const void *p, bool bf16, int64_t col, int64_t cols, float missing, float (&w)[V]) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        w[i] = missing;
-        if (p != nullptr && col + i < cols)
-            w[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[col + i]) : static_cast<const float *>(p)[col + i];
+    for (int i = 0; i < V; ++i) w[i] = missing;
+    if (p == nullptr || col >= cols) return;
+    if (!bf16 && V >= 4 && col + V <= cols && reinterpret_cast<uintptr_t>(p) % 16 == 0) {
+#pragma unroll
+        for (int i = 0; i + 3 < V; i += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(static_cast<const float *>(p) + col + i);
+            w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+        }
+        return;
     }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (col + i < cols) w[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[col + i]) : static_cast<const float *>(p)[col + i];
 }
 
 // The V codes of one vector and the scale of its block.  The 128 / V lanes that hold a block are
-// neighbours; all lanes of the warp call it.  Columns at or past `cols` hold zeros.
+// neighbours; all lanes of the warp call it.  Columns at or past `cols` hold zeros.  Adding 1.5 * 2^23
+// rounds to the nearest whole number and leaves it, as a signed byte, in the sum's lowest bits.
 template <int V>
 __device__ __forceinline__ void encode(const float (&x)[V], uint2 *codes, float *scale) {
-    unsigned top = 0;                    // magnitudes compare like their bit patterns, NaN above all
+    float top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < V; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < V; ++i) top = max_nan(top, fabsf(x[i]));
 #pragma unroll
-    for (int d = BLOCK / V / 2; d > 0; d /= 2) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-    const float t = __uint_as_float(top);
-    const bool fine = top < 0x7F800000u, used = fine && t >= SMALLEST;
-    const float per_unit = used ? __fmul_rn(127.0f, __frcp_rn(t)) : 0.0f;
-    *scale = used ? __fmul_rn(t, 1.0f / 127.0f) : fine ? 0.0f : __int_as_float(0x7FC00000);
+    for (int d = BLOCK / V / 2; d > 0; d /= 2) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+    const bool fine = top < INFINITY, used = fine && top >= SMALLEST;
+    const float per_unit = used ? __fmul_rn(127.0f, __frcp_rn(top)) : 0.0f;
+    *scale = used ? __fmul_rn(top, 1.0f / 127.0f) : fine ? 0.0f : __int_as_float(0x7FC00000);
     unsigned w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i / 4] |= (static_cast<unsigned>(__float2int_rn(used ? __fmul_rn(x[i], per_unit) : 0.0f)) & 0xFFu) << (8 * (i % 4));
+    for (int i = 0; i < V; i += 4) {
+        unsigned q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = __float_as_uint(__fadd_rn(__fmul_rn(x[i + j], per_unit), 12582912.0f));       // two roundings, not one
+        const unsigned lo = __byte_perm(q[0], q[1], 0x0040), hi = __byte_perm(q[2], q[3], 0x0040);
+        w[i / 4] = __byte_perm(lo, hi, 0x5410);
+    }
     *codes = make_uint2(w[0], w[1]);
 }
 
@@ -147,33 +222,34 @@ __device__ __forceinline__ uint2 load_codes(const int8_t *at) {
     return c;
 }
 
+// A byte c + 128 in the lowest bits of 2^23 is 2^23 + 128 + c as a float.
 template <int V>
 __device__ __forceinline__ void decode(const uint2 &c, float scale, float (&x)[V]) {
-    const unsigned w[2] = {c.x, c.y};
+    const unsigned w[2] = {c.x ^ 0x80808080u, c.y ^ 0x80808080u};
 #pragma unroll
-    for (int i = 0; i < V; ++i) x[i] = __fmul_rn(static_cast<float>(static_cast<int>(w[i / 4] << (24 - 8 * (i % 4))) >> 24), scale);
+    for (int i = 0; i < V; i += 2) {
+        const float2 f = make_float2(__uint_as_float(__byte_perm(w[i / 4], 0x4B000000u, 0x7440 + i % 4)), __uint_as_float(__byte_perm(w[i / 4], 0x4B000000u, 0x7440 + i % 4 + 1)));
+        const float2 v = mul2(add2(f, both(-8388736.0f)), both(scale));
+        x[i] = v.x, x[i + 1] = v.y;
+    }
 }
 
 __host__ __device__ constexpr int64_t pitch_of(int64_t cols) { return (cols + 15) / 16 * 16; }
 __host__ __device__ constexpr int64_t blocks_of(int64_t cols) { return (cols + BLOCK - 1) / BLOCK; }
 
-// ---------------------------------------------------------------------------- sums over a row
-// The threads on a row are one warp (several rows to a CTA) or the whole CTA.  `turn` alternates
-// between two sets of slots, so that one barrier per sum is enough.
-template <bool WARP>
-__device__ __forceinline__ float2 row_sum(float2 v, float2 (&slots)[2][GROUP_MAX / 32], int &turn) {
+// The sum over a CTA of two values.  `turn` alternates between two sets of slots, so that one barrier
+// per sum is enough.
+__device__ __forceinline__ float2 cta_sum(float2 v, float2 (&slots)[2][GROUP_MAX / 32], int &turn) {
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) {
         v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, d);
         v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, d);
     }
-    if constexpr (!WARP) {
-        if (threadIdx.x % 32 == 0) slots[turn][threadIdx.x / 32] = v;
-        __syncthreads();
-        v = make_float2(0.0f, 0.0f);
-        for (unsigned w = 0; w < blockDim.x / 32; ++w) v.x += slots[turn][w].x, v.y += slots[turn][w].y;
-        turn ^= 1;
-    }
+    if (threadIdx.x % 32 == 0) slots[turn][threadIdx.x / 32] = v;
+    __syncthreads();
+    v = make_float2(0.0f, 0.0f);
+    for (unsigned w = 0; w < blockDim.x / 32; ++w) v.x += slots[turn][w].x, v.y += slots[turn][w].y;
+    turn ^= 1;
     return v;
 }
 
@@ -191,61 +267,150 @@ struct NormParams {
     int param_bf16, n_parts;
 };
 
-// y = (x - mean) rstd w + b.  Mean first, then the squared distances from it: both from registers.
-template <typename T, bool WIDE, bool WARP, int NV>
-__global__ void __launch_bounds__(GROUP_MAX) k_norm_forward(const NormParams p) {
-    constexpr int V = Elems<T>::V;
-    __shared__ float2 slots[2][GROUP_MAX / 32];
-    int turn = 0;
-    const int group = WARP ? 32 : blockDim.x, at = WARP ? threadIdx.x % 32 : threadIdx.x;
-    const int64_t per_cta = blockDim.x / group, first = blockIdx.x * per_cta + threadIdx.x / group;
+// The threads on a row are a warp (four rows to a CTA) or a CTA of 128, 256 or 512; a thread takes the
+// vectors at, at + GROUP, ... of its row.  A CTA goes over rows blockIdx, blockIdx + grid, ... and keeps
+// its columns' weights (and, backward, their sums) in registers.  Where rows allow 128-bit accesses the
+// rows to come are copied into shared memory ahead of their turn, AHEAD of them at a time, each thread
+// its own vectors: the copies are in flight while the sums over the current row are formed, and only
+// these need a barrier.
+// (Three rows ahead; two where a row and its gradient take 64 KB for the threads of an SM.)
+template <int NV>
+__host__ __device__ constexpr int rows_ahead() { return NV >= 4 ? 2 : 3; }
+
+template <int GROUP>
+__host__ __device__ constexpr int norm_threads() { return GROUP == 32 ? 128 : GROUP; }
+
+// Threads on an SM: as many as the registers of 16 elements to a thread allow.
+template <typename T, int NV>
+__host__ __device__ constexpr int forward_threads() { return NV * Elems<T>::V == E ? 512 : 768; }
+
+template <int GROUP, int NV, int V>
+__device__ __forceinline__ int column(int at, int k) { return (at + k * GROUP) * V; }
+
+// y = (x - mean) rstd w + b.  A warp takes the mean of its part of the row and the squares around that
+// mean; the parts are joined with the exact formula for two samples, so that one barrier is enough
+// and nothing cancels.
+template <typename T, bool WIDE, int GROUP, int NV>
+__global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>() / norm_threads<GROUP>()) k_norm_forward(const NormParams p) {
+    constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
+    extern __shared__ uint4 ring[];              // WIDE: [AHEAD + 1][NV][THREADS]
+    __shared__ float2 slots[2][WARPS];
+    __shared__ float counts[WARPS];
+    const int at = threadIdx.x % GROUP;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (THREADS / GROUP), first = static_cast<int64_t>(blockIdx.x) * (THREADS / GROUP) + threadIdx.x / GROUP;
+    const int cols = static_cast<int>(p.cols), pitch = static_cast<int>(pitch_of(cols)), blocks = static_cast<int>(blocks_of(cols));
+    const float per_col = 1.0f / static_cast<float>(cols);
+    auto slot = [&](int stage, int k) { return ring + (stage * NV + k) * THREADS + threadIdx.x; };
+    auto fetch = [&](int64_t r, int stage) {
+        if (r < p.rows)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (column<GROUP, NV, V>(at, k) < cols) copy_ahead<16>(slot(stage, k), static_cast<const T *>(p.x) + r * p.x_stride + column<GROUP, NV, V>(at, k));
+        copies_issued();
+    };
+    auto part_of = [&](int warp) {               // elements of the row that a warp holds
+        int n = 0;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) n += min(max(cols - column<GROUP, NV, V>(warp * 32, k), 0), 32 * V);
+        return static_cast<float>(n);
+    };
+    uint4 raw[NV];
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) fetch(first + s * step, s);
+    } else {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) raw[k] = first < p.rows ? load_row<T, WIDE>(static_cast<const T *>(p.x) + first * p.x_stride, column<GROUP, NV, V>(at, k), cols) : make_uint4(0, 0, 0, 0);
+    }
     float w[NV][V], b[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        load_param(p.weight, p.param_bf16, static_cast<int64_t>(at + k * group) * V, p.cols, 1.0f, w[k]);
-        load_param(p.bias, p.param_bf16, static_cast<int64_t>(at + k * group) * V, p.cols, 0.0f, b[k]);
+        load_param(p.weight, p.param_bf16, column<GROUP, NV, V>(at, k), cols, 1.0f, w[k]);
+        load_param(p.bias, p.param_bf16, column<GROUP, NV, V>(at, k), cols, 0.0f, b[k]);
     }
-    for (int64_t r = first; r < p.rows; r += gridDim.x * per_cta) {
-        const T *row = static_cast<const T *>(p.x) + r * p.x_stride;
+    const float mine = part_of(at / 32), per_mine = mine > 0.0f ? 1.0f / mine : 0.0f;
+    if (WARPS > 1 && threadIdx.x % 32 == 0) counts[at / 32] = mine;     // read after the first row's barrier
+    int stage = 0, turn = 0;
+    for (int64_t r = first; r < p.rows; r += step) {
         float x[NV][V];
-        float2 s = make_float2(0.0f, 0.0f);
+        float2 s = both(0.0f);
+        if constexpr (WIDE) {
+            wait_copies<AHEAD - 1>();
+#pragma unroll
+            for (int k = 0; k < NV; ++k) raw[k] = column<GROUP, NV, V>(at, k) < cols ? *slot(stage, k) : make_uint4(0, 0, 0, 0);
+        }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            load_row<T, WIDE>(row, static_cast<int64_t>(at + k * group) * V, p.cols, x[k]);
+            Elems<T>::widen(raw[k], x[k]);
 #pragma unroll
-            for (int i = 0; i < V; ++i) s.x += x[k][i];
+            for (int i = 0; i < V; i += 2) s = add2(s, make_float2(x[k][i], x[k][i + 1]));
         }
-        const float mean = row_sum<WARP>(s, slots, turn).x / static_cast<float>(p.cols);
-        s = make_float2(0.0f, 0.0f);
+        if constexpr (WIDE) {
+            fetch(r + AHEAD * step, stage == 0 ? AHEAD : stage - 1);
+            stage = stage == AHEAD ? 0 : stage + 1;
+        } else {
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+            for (int k = 0; k < NV; ++k)
+                if (r + step < p.rows) raw[k] = load_row<T, WIDE>(static_cast<const T *>(p.x) + (r + step) * p.x_stride, column<GROUP, NV, V>(at, k), cols);
+        }
+        float mean = s.x + s.y;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const bool in = WIDE ? static_cast<int64_t>(at + k * group) * V < p.cols : static_cast<int64_t>(at + k * group) * V + i < p.cols;
-                x[k][i] = in ? x[k][i] - mean : 0.0f;
-                s.x += x[k][i] * x[k][i];
+        for (int d = 16; d > 0; d /= 2) mean += __shfl_xor_sync(0xFFFFFFFFu, mean, d);
+        mean *= per_mine;
+        float2 sq = both(0.0f);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int col = column<GROUP, NV, V>(at, k);
+#pragma unroll
+            for (int i = 0; i < V; i += 2) {
+                float2 d = add2(make_float2(x[k][i], x[k][i + 1]), both(-mean));
+                if (WIDE ? col >= cols : col + i >= cols) d.x = 0.0f;
+                if (WIDE ? col >= cols : col + i + 1 >= cols) d.y = 0.0f;
+                sq = fma2(d, d, sq);
             }
-        const float rstd = __frsqrt_rn(row_sum<WARP>(s, slots, turn).x / static_cast<float>(p.cols) + p.eps);
+        }
+        float m2 = sq.x + sq.y;
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) m2 += __shfl_xor_sync(0xFFFFFFFFu, m2, d);
+        if constexpr (WARPS > 1) {
+            if (threadIdx.x % 32 == 0) slots[turn][at / 32] = make_float2(mean, m2);
+            __syncthreads();
+            mean = m2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) mean += counts[i] * slots[turn][i].x;
+            mean *= per_col;
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) {
+                const float2 part = slots[turn][i];
+                m2 += fmaf(counts[i] * (part.x - mean), part.x - mean, part.y);
+            }
+            turn ^= 1;
+        }
+        const float rstd = __frsqrt_rn(m2 * per_col + p.eps);
         if (at == 0) {
             if (p.mean != nullptr) p.mean[r] = mean;
             if (p.rstd != nullptr) p.rstd[r] = rstd;
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t col = static_cast<int64_t>(at + k * group) * V;
+            const int col = column<GROUP, NV, V>(at, k);
             float y[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                x[k][i] *= rstd;
-                y[i] = x[k][i] * w[k][i] + b[k][i];
+            for (int i = 0; i < V; i += 2) {
+                const float2 u = mul2(add2(make_float2(x[k][i], x[k][i + 1]), both(-mean)), both(rstd));
+                const float2 v = fma2(u, make_float2(w[k][i], w[k][i + 1]), make_float2(b[k][i], b[k][i + 1]));
+                x[k][i] = u.x, x[k][i + 1] = u.y, y[i] = v.x, y[i + 1] = v.y;
             }
-            store_row<T, WIDE>(static_cast<T *>(p.out) + r * p.out_stride, col, p.cols, y);
+            store_row<T, WIDE>(static_cast<T *>(p.out) + r * p.out_stride, col, cols, y);
             if (p.codes != nullptr) {
                 uint2 c;
                 float scale;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    if (WIDE ? col >= cols : col + i >= cols) x[k][i] = 0.0f;
                 encode<V>(x[k], &c, &scale);
-                if (col < pitch_of(p.cols)) store_codes<V>(p.codes + r * pitch_of(p.cols) + col, c);
-                if (col % BLOCK == 0 && col < p.cols) p.scales[r * blocks_of(p.cols) + col / BLOCK] = scale;
+                if (col < pitch) store_codes<V>(p.codes + r * pitch + col, c);
+                if (col % BLOCK == 0 && col < cols) p.scales[r * blocks + col / BLOCK] = scale;
             }
         }
     }
@@ -253,68 +418,142 @@ __global__ void __launch_bounds__(GROUP_MAX) k_norm_forward(const NormParams p) 
 
 // With u = (x - mean) rstd (or its 8-bit checkpoint) and g = dout w:
 //   dx = rstd (g - mean(g) - u mean(g u)),  dweight = sum_rows dout u,  dbias = sum_rows dout.
-// A CTA goes over rows blockIdx, blockIdx + grid, ... and keeps its columns' sums in registers;
-// one row of partial sums per CTA is reduced in a fixed order by k_norm_params: no atomics, so that
-// a step gives the same bits when it is run again.
-template <typename T, bool WIDE, bool WARP, int NV, bool KEPT>
-__global__ void __launch_bounds__(GROUP_MAX) k_norm_backward(const NormParams p) {
-    constexpr int V = Elems<T>::V;
-    __shared__ float2 slots[2][GROUP_MAX / 32];
-    extern __shared__ float joined[];     // WARP: [2][32 * NV * V], the sums of the CTA's warps
-    int turn = 0;
-    const int group = WARP ? 32 : blockDim.x, at = WARP ? threadIdx.x % 32 : threadIdx.x;
-    const int64_t per_cta = blockDim.x / group, first = blockIdx.x * per_cta + threadIdx.x / group;
+// One row of partial sums per CTA is reduced in a fixed order by k_norm_params: no atomics, so that a step
+// gives the same bits when it is run again.
+template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
+__global__ void __launch_bounds__(norm_threads<GROUP>(), 512 / norm_threads<GROUP>()) k_norm_backward(const NormParams p) {
+    constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
+    constexpr int SOURCE = KEPT ? V : 16;        // bytes of a vector of u: codes, or x itself
+    // WIDE: [AHEAD + 1][NV][THREADS] vectors of dout, then as many of SOURCE bytes, then (KEPT) scales;
+    // afterwards, with a warp to a row, the sums of the CTA's warps
+    extern __shared__ uint4 ring[];
+    __shared__ float2 slots[2][WARPS];
+    constexpr int CELLS = (AHEAD + 1) * NV * THREADS;
+    char *const ring_u = reinterpret_cast<char *>(ring + CELLS);
+    float *const ring_s = reinterpret_cast<float *>(ring_u + CELLS * SOURCE);
+    const int at = threadIdx.x % GROUP;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * (THREADS / GROUP), first = static_cast<int64_t>(blockIdx.x) * (THREADS / GROUP) + threadIdx.x / GROUP;
+    const int cols = static_cast<int>(p.cols), pitch = static_cast<int>(pitch_of(cols)), blocks = static_cast<int>(blocks_of(cols));
+    const float per_col = 1.0f / static_cast<float>(cols);
+    auto cell = [&](int stage, int k) { return (stage * NV + k) * THREADS + static_cast<int>(threadIdx.x); };
+    auto dout_at = [&](int64_t r, int k) { return static_cast<const T *>(p.dout) + r * p.dout_stride + column<GROUP, NV, V>(at, k); };
+    auto x_at = [&](int64_t r, int k) { return static_cast<const T *>(p.x) + r * p.x_stride + column<GROUP, NV, V>(at, k); };
+    auto codes_at = [&](int64_t r, int k) { return p.codes + r * pitch + column<GROUP, NV, V>(at, k); };
+    auto scale_at = [&](int64_t r, int k) { return p.scales + r * blocks + column<GROUP, NV, V>(at, k) / BLOCK; };
+    auto fetch = [&](int64_t r, int stage) {
+        if (r < p.rows)
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (column<GROUP, NV, V>(at, k) >= cols) continue;
+                const int c = cell(stage, k);
+                copy_ahead<16>(ring + c, dout_at(r, k));
+                if constexpr (KEPT) {
+                    copy_ahead<SOURCE>(ring_u + c * SOURCE, codes_at(r, k));
+                    copy_ahead<4>(ring_s + c, scale_at(r, k));
+                } else {
+                    copy_ahead<16>(ring_u + c * SOURCE, x_at(r, k));
+                }
+            }
+        copies_issued();
+    };
+    if constexpr (WIDE) {
+#pragma unroll
+        for (int s = 0; s < AHEAD; ++s) fetch(first + s * step, s);
+    }
     float w[NV][V], dw[NV][V], db[NV][V];
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-        load_param(p.weight, p.param_bf16, static_cast<int64_t>(at + k * group) * V, p.cols, 1.0f, w[k]);
+        load_param(p.weight, p.param_bf16, column<GROUP, NV, V>(at, k), cols, 1.0f, w[k]);
 #pragma unroll
         for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0.0f;
     }
-    const float per_col = 1.0f / static_cast<float>(p.cols);
-    for (int64_t r = first; r < p.rows; r += gridDim.x * per_cta) {
+    float rstd = first < p.rows ? p.rstd[first] : 0.0f, mean = !KEPT && first < p.rows ? p.mean[first] : 0.0f;
+    int stage = 0, turn = 0;
+    for (int64_t r = first; r < p.rows; r += step) {
         float g[NV][V], u[NV][V];
-        const float rstd = p.rstd[r], mean = KEPT ? 0.0f : p.mean[r];
-        float2 s = make_float2(0.0f, 0.0f);
+        float2 s1 = both(0.0f), s2 = both(0.0f);
+        if constexpr (WIDE) wait_copies<AHEAD - 1>();
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int64_t col = static_cast<int64_t>(at + k * group) * V;
-            load_row<T, WIDE>(static_cast<const T *>(p.dout) + r * p.dout_stride, col, p.cols, g[k]);
+            const bool in = column<GROUP, NV, V>(at, k) < cols;
+            const int c = cell(stage, k);
+            const uint4 zero = make_uint4(0, 0, 0, 0);
+            Elems<T>::widen(WIDE ? in ? ring[c] : zero : load_row<T, WIDE>(static_cast<const T *>(p.dout) + r * p.dout_stride, column<GROUP, NV, V>(at, k), cols), g[k]);
             if constexpr (KEPT) {
-                const bool in = col < p.cols;
-                decode<V>(in ? load_codes<V>(p.codes + r * pitch_of(p.cols) + col) : make_uint2(0, 0),
-                          in ? p.scales[r * blocks_of(p.cols) + col / BLOCK] : 0.0f, u[k]);
+                uint2 codes = make_uint2(0, 0);
+                float scale = 0.0f;
+                if constexpr (WIDE) {
+                    if (in) {
+                        if constexpr (V == 8) codes = *reinterpret_cast<const uint2 *>(ring_u + c * SOURCE);
+                        else codes.x = *reinterpret_cast<const unsigned *>(ring_u + c * SOURCE);
+                        scale = ring_s[c];
+                    }
+                } else if (in) {
+                    codes = load_codes<V>(codes_at(r, k));
+                    scale = *scale_at(r, k);
+                }
+                decode<V>(codes, scale, u[k]);
             } else {
-                load_row<T, WIDE>(static_cast<const T *>(p.x) + r * p.x_stride, col, p.cols, u[k]);
+                Elems<T>::widen(WIDE ? in ? *reinterpret_cast<const uint4 *>(ring_u + c * SOURCE) : zero : load_row<T, WIDE>(static_cast<const T *>(p.x) + r * p.x_stride, column<GROUP, NV, V>(at, k), cols), u[k]);
             }
+        }
+        const float by = rstd, shift = mean;
+        if constexpr (WIDE) {
+            fetch(r + AHEAD * step, stage == 0 ? AHEAD : stage - 1);
+            stage = stage == AHEAD ? 0 : stage + 1;
+        }
+        if (r + step < p.rows) {
+            rstd = p.rstd[r + step];
+            if constexpr (!KEPT) mean = p.mean[r + step];
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if constexpr (!KEPT) u[k][i] = (u[k][i] - mean) * rstd;     // past the row's end g is zero
-                dw[k][i] += g[k][i] * u[k][i];
-                db[k][i] += g[k][i];
-                g[k][i] *= w[k][i];
-                s.x += g[k][i];
-                s.y += g[k][i] * u[k][i];
+            for (int i = 0; i < V; i += 2) {
+                const float2 d = make_float2(g[k][i], g[k][i + 1]);           // zeros past the row's end
+                float2 un = make_float2(u[k][i], u[k][i + 1]);
+                if constexpr (!KEPT) un = mul2(add2(un, both(-shift)), both(by));
+                const float2 a = fma2(d, un, make_float2(dw[k][i], dw[k][i + 1])), c = add2(d, make_float2(db[k][i], db[k][i + 1]));
+                const float2 v = mul2(d, make_float2(w[k][i], w[k][i + 1]));
+                dw[k][i] = a.x, dw[k][i + 1] = a.y, db[k][i] = c.x, db[k][i + 1] = c.y;
+                g[k][i] = v.x, g[k][i + 1] = v.y, u[k][i] = un.x, u[k][i + 1] = un.y;
+                s1 = add2(s1, v);
+                s2 = fma2(v, un, s2);
             }
-        s = row_sum<WARP>(s, slots, turn);
-        s.x *= per_col;
-        s.y *= per_col;
+        float2 s = make_float2(s1.x + s1.y, s2.x + s2.y);
+#pragma unroll
+        for (int d = 16; d > 0; d /= 2) {
+            s.x += __shfl_xor_sync(0xFFFFFFFFu, s.x, d);
+            s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
+        }
+        if constexpr (WARPS > 1) {
+            if (threadIdx.x % 32 == 0) slots[turn][at / 32] = s;
+            __syncthreads();
+            s = both(0.0f);
+#pragma unroll
+            for (int i = 0; i < WARPS; ++i) s = add2(s, slots[turn][i]);
+            turn ^= 1;
+        }
+        const float a = -s.x * per_col * by, c = -s.y * per_col * by;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             float y[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) y[i] = (g[k][i] - s.x - u[k][i] * s.y) * rstd;
-            store_row<T, WIDE>(static_cast<T *>(p.out) + r * p.out_stride, static_cast<int64_t>(at + k * group) * V, p.cols, y);
+            for (int i = 0; i < V; i += 2) {
+                const float2 v = fma2(make_float2(g[k][i], g[k][i + 1]), both(by), fma2(make_float2(u[k][i], u[k][i + 1]), both(c), both(a)));
+                y[i] = v.x, y[i + 1] = v.y;
+            }
+            store_row<T, WIDE>(static_cast<T *>(p.out) + r * p.out_stride, column<GROUP, NV, V>(at, k), cols, y);
         }
     }
     if (p.parts == nullptr) return;
     float *part = p.parts + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
-    if constexpr (WARP) {
+    if constexpr (GROUP == 32) {
         constexpr int N = 32 * NV * V;
-        for (unsigned turn_of = 0; turn_of < blockDim.x / 32; ++turn_of) {
+        float *const joined = reinterpret_cast<float *>(ring);
+        wait_copies<0>();
+        for (unsigned turn_of = 0; turn_of < THREADS / 32; ++turn_of) {
+            __syncthreads();
             if (threadIdx.x / 32 == turn_of) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
@@ -325,15 +564,15 @@ __global__ void __launch_bounds__(GROUP_MAX) k_norm_backward(const NormParams p)
                         joined[N + c] = turn_of == 0 ? db[k][i] : joined[N + c] + db[k][i];
                     }
             }
-            __syncthreads();
         }
-        for (int64_t c = threadIdx.x; c < p.cols; c += blockDim.x) part[c] = joined[c], part[p.cols + c] = joined[N + c];
+        __syncthreads();
+        for (int64_t c = threadIdx.x; c < p.cols; c += THREADS) part[c] = joined[c], part[p.cols + c] = joined[N + c];
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int64_t c = static_cast<int64_t>(at + k * group) * V + i;
+                const int64_t c = column<GROUP, NV, V>(at, k) + i;
                 if (c < p.cols) part[c] = dw[k][i], part[p.cols + c] = db[k][i];
             }
     }
@@ -356,13 +595,13 @@ __global__ void __launch_bounds__(GROUP_MAX) k_norm_forward_any(const NormParams
         T *out = static_cast<T *>(p.out) + r * p.out_stride;
         float2 s = make_float2(0.0f, 0.0f);
         for (int64_t c = threadIdx.x; c < p.cols; c += blockDim.x) s.x += Elems<T>::up(row[c]);
-        const float mean = row_sum<false>(s, slots, turn).x / static_cast<float>(p.cols);
+        const float mean = cta_sum(s, slots, turn).x / static_cast<float>(p.cols);
         s = make_float2(0.0f, 0.0f);
         for (int64_t c = threadIdx.x; c < p.cols; c += blockDim.x) {
             const float d = Elems<T>::up(row[c]) - mean;
             s.x += d * d;
         }
-        const float rstd = __frsqrt_rn(row_sum<false>(s, slots, turn).x / static_cast<float>(p.cols) + p.eps);
+        const float rstd = __frsqrt_rn(cta_sum(s, slots, turn).x / static_cast<float>(p.cols) + p.eps);
         if (threadIdx.x == 0) {
             if (p.mean != nullptr) p.mean[r] = mean;
             if (p.rstd != nullptr) p.rstd[r] = rstd;
@@ -418,7 +657,7 @@ __global__ void __launch_bounds__(GROUP_MAX) k_norm_backward_any(const NormParam
             s.x += g;
             s.y += g * unit_at<T, KEPT>(p, r, c, mean, rstd);
         }
-        s = row_sum<false>(s, slots, turn);
+        s = cta_sum(s, slots, turn);
         for (int64_t c = threadIdx.x; c < p.cols; c += blockDim.x) {
             float w[1];
             load_param(p.weight, p.param_bf16, c, p.cols, 1.0f, w);
@@ -447,31 +686,38 @@ __global__ void k_norm_columns(const NormParams p) {
     part[p.cols + c] = db;
 }
 
-// Sums of the partial rows: 32 columns to a CTA, 16 threads down each, then a tree; blockIdx.y 0
-// writes dweight, 1 dbias.  Rounded once, to the parameters' type.
-__global__ void __launch_bounds__(512) k_norm_params(const NormParams p) {
-    __shared__ float sums[16][33];
+// Sums of the partial rows: 32 columns to a CTA, 32 threads down each with four sums, then a tree;
+// blockIdx.y 0 writes dweight, 1 dbias.  Rounded once, to the parameters' type.
+__global__ void __launch_bounds__(1024) k_norm_params(const NormParams p) {
+    __shared__ float sums[32][33];
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x;
     void *out = blockIdx.y == 0 ? p.dweight : p.dbias;
     if (out == nullptr) return;
-    float s = 0.0f;
-    if (c < p.cols)
-        for (int q = threadIdx.y; q < p.n_parts; q += 16) s += p.parts[(static_cast<int64_t>(q) * 2 + blockIdx.y) * p.cols + c];
-    sums[threadIdx.y][threadIdx.x] = s;
-    __syncthreads();
-    for (int h = 8; h > 0; h /= 2) {
-        if (threadIdx.y < h) sums[threadIdx.y][threadIdx.x] += sums[threadIdx.y + h][threadIdx.x];
-        __syncthreads();
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < p.cols) {
+        const float *at = p.parts + blockIdx.y * p.cols + c;
+        int q = threadIdx.y;
+        for (; q + 96 < p.n_parts; q += 128)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += at[static_cast<int64_t>(q + 32 * i) * 2 * p.cols];
+        for (int i = 0; q < p.n_parts; q += 32, ++i) s[i] += at[static_cast<int64_t>(q) * 2 * p.cols];
     }
-    if (threadIdx.y == 0 && c < p.cols) {
-        if (p.param_bf16) static_cast<__nv_bfloat16 *>(out)[c] = __float2bfloat16_rn(sums[0][threadIdx.x]);
-        else static_cast<float *>(out)[c] = sums[0][threadIdx.x];
+    sums[threadIdx.y][threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    float v = sums[threadIdx.x][threadIdx.y];          // a warp to a column
+#pragma unroll
+    for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const int64_t to = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.y;
+    if (threadIdx.x == 0 && to < p.cols) {
+        if (p.param_bf16) static_cast<__nv_bfloat16 *>(out)[to] = __float2bfloat16_rn(v);
+        else static_cast<float *>(out)[to] = v;
     }
 }
 
 // ------------------------------------------------------------- activations and checkpoints
 // Work is laid out in vectors over rows padded to whole blocks, so that the lanes that hold a block
-// are neighbours; every thread takes U vectors, a CTA's width apart.
+// are neighbours; every thread takes U vectors, a CTA's width apart, and loads all of them before it
+// works on the first.
 constexpr int U = 4;
 constexpr int THREADS = 256;
 
@@ -483,41 +729,70 @@ struct ElemParams {
     int8_t *codes;
     float *scales;
     int64_t rows, cols, in_stride, x_stride, out_stride;
-    int64_t vectors;                      // rows * per_row
-    unsigned per_row;                     // vectors to a padded row
+    unsigned vectors;                     // rows * per_row, below 2^31
+    unsigned per_row, magic, shift;       // vectors to a padded row; i / per_row = (umulhi(i, magic) + i) >> shift
     int param_bf16;
 };
 
-// The normal distribution function from Abramowitz and Stegun, formula 7.1.26
-// (absolute error of erf below 1.5e-7), with e = exp(-x^2 / 2), which the derivative needs as well.
-__device__ __forceinline__ float normal_below(float x, float *e) {
-    const float z = fabsf(x) * 0.70710678118654752f;
-    const float t = __fdividef(1.0f, fmaf(0.3275911f, z, 1.0f));
-    const float q = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    *e = __expf(-z * z);
-    const float tail = 0.5f * q * *e;
-    return x < 0.0f ? tail : 1.0f - tail;
+// A thread's vectors: their rows and columns; past the last one, a column past the row.
+template <int V>
+struct Place {
+    int64_t row, col;
+    __device__ Place(const ElemParams &p, int u) {
+        const unsigned i = blockIdx.x * (U * THREADS) + u * THREADS + threadIdx.x;
+        const unsigned r = (__umulhi(i, p.magic) + i) >> p.shift;
+        row = r;
+        col = i < p.vectors ? static_cast<int64_t>(i - r * p.per_row) * V : static_cast<int64_t>(p.per_row) * V;
+    }
+};
+
+// e (c a - q) for a = |x|: with the tail T = 1 - Phi(a) = e q, e = exp(-a^2 / 2), from Abramowitz and
+// Stegun, formula 7.1.26 (absolute error of erf below 1.5e-7; its coefficients halved).  GELU is
+// max(x, 0) - a T, and its slope the step at 0 plus or minus (a phi(a) - T).  a stops at 64, where e
+// is 0, so that an infinity meets no 0 * inf.
+__device__ __forceinline__ void normal_tail(float2 a, float2 *q, float2 *e) {
+    const float2 den = fma2(a, both(0.3275911f * 0.70710678118654752f), both(1.0f));
+    const float2 t = make_float2(inverse_fast(den.x), inverse_fast(den.y));
+    float2 s = fma2(t, both(0.5f * 1.061405429f), both(0.5f * -1.453152027f));
+    s = fma2(t, s, both(0.5f * 1.421413741f));
+    s = fma2(t, s, both(0.5f * -0.284496736f));
+    s = fma2(t, s, both(0.5f * 0.254829592f));
+    *q = mul2(t, s);
+    const float2 z = mul2(mul2(a, a), both(-0.72134752044448170f));       // - log2(e) / 2
+    *e = make_float2(exp2_fast(z.x), exp2_fast(z.y));
+}
+__device__ __forceinline__ float2 magnitude(float2 x) { return make_float2(min_nan(fabsf(x.x), 64.0f), min_nan(fabsf(x.y), 64.0f)); }
+
+__device__ __forceinline__ float2 sigmoid(float2 x) {
+    const float2 z = mul2(x, both(-1.4426950408889634f));
+    const float2 d = add2(make_float2(exp2_fast(z.x), exp2_fast(z.y)), both(1.0f));
+    return make_float2(inverse_fast(d.x), inverse_fast(d.y));
 }
 
 template <int KIND>
-__device__ __forceinline__ float act(float x) {
+__device__ __forceinline__ float2 act(float2 x) {
     if constexpr (KIND == KT_GELU) {
-        float e;
-        return x * normal_below(x, &e);
+        float2 q, e;
+        const float2 a = magnitude(x);
+        normal_tail(a, &q, &e);
+        const float2 below = mul2(mul2(q, e), make_float2(-a.x, -a.y));
+        return add2(below, make_float2(max_nan(x.x, 0.0f), max_nan(x.y, 0.0f)));
     } else {
-        return __fdividef(x, 1.0f + __expf(-x));
+        return mul2(x, sigmoid(x));
     }
 }
 
 template <int KIND>
-__device__ __forceinline__ float slope(float x) {
+__device__ __forceinline__ float2 slope(float2 x) {
     if constexpr (KIND == KT_GELU) {
-        float e;
-        const float below = normal_below(x, &e);
-        return fmaf(x * 0.39894228040143268f, e, below);
+        float2 q, e;
+        const float2 a = magnitude(x);
+        normal_tail(a, &q, &e);
+        const float2 v = fma2(e, fma2(a, both(0.39894228040143268f), make_float2(-q.x, -q.y)), both(0.5f));
+        return add2(make_float2(copysignf(v.x, x.x), copysignf(v.y, x.y)), both(0.5f));
     } else {
-        const float gate = __fdividef(1.0f, 1.0f + __expf(-x));
-        return gate * fmaf(x, 1.0f - gate, 1.0f);
+        const float2 s = sigmoid(x);
+        return mul2(s, fma2(x, add2(both(1.0f), make_float2(-s.x, -s.y)), both(1.0f)));
     }
 }
 
@@ -526,36 +801,32 @@ enum { KIND_NONE = -1 };                  // a checkpoint alone
 template <typename T, bool WIDE, int KIND, bool KEEP>
 __global__ void __launch_bounds__(THREADS) k_act_forward(const ElemParams p) {
     constexpr int V = Elems<T>::V;
-    const int64_t base = static_cast<int64_t>(blockIdx.x) * (U * THREADS) + threadIdx.x;
-    float x[U][V];
-    int64_t row[U], col[U];
+    uint4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t i = base + u * THREADS;
-        row[u] = i / p.per_row;
-        col[u] = (i - row[u] * p.per_row) * V;
-        if (i < p.vectors) {
-            load_row<T, WIDE>(static_cast<const T *>(p.in) + row[u] * p.in_stride, col[u], p.cols, x[u]);
-        } else {
-            col[u] = p.per_row * V;       // past every row
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = 0.0f;
-        }
+        const Place<V> at(p, u);
+        raw[u] = load_row<T, WIDE>(static_cast<const T *>(p.in) + at.row * p.in_stride, at.col, p.cols);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        const Place<V> at(p, u);
+        float x[V];
+        Elems<T>::widen(raw[u], x);
         if constexpr (KIND != KIND_NONE) {
             float y[V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) y[j] = act<KIND>(x[u][j]);
-            store_row<T, WIDE>(static_cast<T *>(p.out) + row[u] * p.out_stride, col[u], p.cols, y);
+            for (int j = 0; j < V; j += 2) {
+                const float2 v = act<KIND>(make_float2(x[j], x[j + 1]));
+                y[j] = v.x, y[j + 1] = v.y;
+            }
+            store_row<T, WIDE>(static_cast<T *>(p.out) + at.row * p.out_stride, at.col, p.cols, y);
         }
         if constexpr (KEEP) {
             uint2 c;
             float scale;
-            encode<V>(x[u], &c, &scale);
-            if (col[u] < pitch_of(p.cols)) store_codes<V>(p.codes + row[u] * pitch_of(p.cols) + col[u], c);
-            if (col[u] % BLOCK == 0 && col[u] < p.cols) p.scales[row[u] * blocks_of(p.cols) + col[u] / BLOCK] = scale;
+            encode<V>(x, &c, &scale);
+            if (at.col < pitch_of(p.cols)) store_codes<V>(p.codes + at.row * pitch_of(p.cols) + at.col, c);
+            if (at.col % BLOCK == 0 && at.col < p.cols) p.scales[at.row * blocks_of(p.cols) + at.col / BLOCK] = scale;
         }
     }
 }
@@ -563,60 +834,67 @@ __global__ void __launch_bounds__(THREADS) k_act_forward(const ElemParams p) {
 template <typename T, bool WIDE, int KIND, bool KEPT>
 __global__ void __launch_bounds__(THREADS) k_act_backward(const ElemParams p) {
     constexpr int V = Elems<T>::V;
-    const int64_t base = static_cast<int64_t>(blockIdx.x) * (U * THREADS) + threadIdx.x;
-    float x[U][V], d[U][V];
-    int64_t row[U], col[U];
+    uint4 raw[U], raw_x[KEPT ? 1 : U];
+    uint2 codes[KEPT ? U : 1];
+    float scale[KEPT ? U : 1];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t i = base + u * THREADS;
-        row[u] = i / p.per_row;
-        col[u] = (i - row[u] * p.per_row) * V;
-        if (i < p.vectors && col[u] < p.cols) {
-            load_row<T, WIDE>(static_cast<const T *>(p.in) + row[u] * p.in_stride, col[u], p.cols, d[u]);
-            if constexpr (KEPT) decode<V>(load_codes<V>(p.codes + row[u] * pitch_of(p.cols) + col[u]), p.scales[row[u] * blocks_of(p.cols) + col[u] / BLOCK], x[u]);
-            else load_row<T, WIDE>(static_cast<const T *>(p.x) + row[u] * p.x_stride, col[u], p.cols, x[u]);
+        const Place<V> at(p, u);
+        raw[u] = load_row<T, WIDE>(static_cast<const T *>(p.in) + at.row * p.in_stride, at.col, p.cols);
+        if constexpr (KEPT) {
+            codes[u] = make_uint2(0, 0);
+            scale[u] = 0.0f;
+            if (at.col < p.cols) {
+                codes[u] = load_codes<V>(p.codes + at.row * pitch_of(p.cols) + at.col);
+                scale[u] = p.scales[at.row * blocks_of(p.cols) + at.col / BLOCK];
+            }
         } else {
-            col[u] = p.cols;
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = d[u][j] = 0.0f;
+            raw_x[u] = load_row<T, WIDE>(static_cast<const T *>(p.x) + at.row * p.x_stride, at.col, p.cols);
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
+        const Place<V> at(p, u);
+        float d[V], x[V];
+        Elems<T>::widen(raw[u], d);
+        if constexpr (KEPT) decode<V>(codes[u], scale[u], x);
+        else Elems<T>::widen(raw_x[u], x);
 #pragma unroll
-        for (int j = 0; j < V; ++j) d[u][j] *= slope<KIND>(x[u][j]);
-        store_row<T, WIDE>(static_cast<T *>(p.out) + row[u] * p.out_stride, col[u], p.cols, d[u]);
+        for (int j = 0; j < V; j += 2) {
+            const float2 v = mul2(make_float2(d[j], d[j + 1]), slope<KIND>(make_float2(x[j], x[j + 1])));
+            d[j] = v.x, d[j + 1] = v.y;
+        }
+        store_row<T, WIDE>(static_cast<T *>(p.out) + at.row * p.out_stride, at.col, p.cols, d);
     }
 }
 
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(THREADS) k_restore(const ElemParams p) {
     constexpr int V = Elems<T>::V;
-    const int64_t base = static_cast<int64_t>(blockIdx.x) * (U * THREADS) + threadIdx.x;
-    float x[U][V];
-    int64_t row[U], col[U];
+    uint2 codes[U];
+    float scale[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t i = base + u * THREADS;
-        row[u] = i / p.per_row;
-        col[u] = (i - row[u] * p.per_row) * V;
-        if (i < p.vectors && col[u] < p.cols) {
-            decode<V>(load_codes<V>(p.codes + row[u] * pitch_of(p.cols) + col[u]), p.scales[row[u] * blocks_of(p.cols) + col[u] / BLOCK], x[u]);
-        } else {
-            col[u] = p.cols;
+        const Place<V> at(p, u);
+        if (at.col < p.cols) {
+            codes[u] = load_codes<V>(p.codes + at.row * pitch_of(p.cols) + at.col);
+            scale[u] = p.scales[at.row * blocks_of(p.cols) + at.col / BLOCK];
         }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        if (col[u] >= p.cols) continue;
+        const Place<V> at(p, u);
+        if (at.col >= p.cols) continue;
+        float x[V];
+        decode<V>(codes[u], scale[u], x);
         if (p.weight != nullptr || p.bias != nullptr) {
             float w[V], b[V];
-            load_param(p.weight, p.param_bf16, col[u], p.cols, 1.0f, w);
-            load_param(p.bias, p.param_bf16, col[u], p.cols, 0.0f, b);
+            load_param(p.weight, p.param_bf16, at.col, p.cols, 1.0f, w);
+            load_param(p.bias, p.param_bf16, at.col, p.cols, 0.0f, b);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = x[u][j] * w[j] + b[j];
+            for (int j = 0; j < V; ++j) x[j] = x[j] * w[j] + b[j];
         }
-        store_row<T, WIDE>(static_cast<T *>(p.out) + row[u] * p.out_stride, col[u], p.cols, x[u]);
+        store_row<T, WIDE>(static_cast<T *>(p.out) + at.row * p.out_stride, at.col, p.cols, x);
     }
 }
 
@@ -658,63 +936,62 @@ bool wide(const void *p, int64_t stride, int64_t rows, int64_t cols, int dtype) 
     return reinterpret_cast<uintptr_t>(p) % 16 == 0 && cols * es % 16 == 0 && (rows <= 1 || stride * es % 16 == 0);
 }
 
-int sm_count(int *sms) {
-    int dev = 0;
-    KT_CUDA(cudaGetDevice(&dev));
-    KT_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
-    return KT_OK;
-}
-
-// How the threads share a row: one warp where it can hold the row, else a CTA of up to 512.
+// How many threads share a row: a warp where it can hold the row, else a CTA of up to 512.
 struct RowShape {
-    bool warp;
-    int threads, nv, rows_per_cta;
+    int group, nv, threads;
 };
 RowShape row_shape(int64_t cols, int dtype) {
     const int v = dtype == KT_F32 ? 4 : 8;
     const int64_t vectors = (pitch_of(cols) + v - 1) / v;
     RowShape s{};
-    s.warp = vectors <= 32 * (E / v);
-    int group = 32;
-    if (!s.warp)
-        for (group = 128; group < GROUP_MAX && vectors > static_cast<int64_t>(group) * (E / v);) group *= 2;
-    s.threads = s.warp ? 128 : group;
-    s.rows_per_cta = s.threads / group;
-    s.nv = static_cast<int>((vectors + group - 1) / group);
+    s.group = 32;
+    if (vectors > 32 * (E / v))
+        for (s.group = 128; s.group < GROUP_MAX && vectors > static_cast<int64_t>(s.group) * (E / v);) s.group *= 2;
+    s.threads = s.group == 32 ? 128 : s.group;
+    s.nv = static_cast<int>((vectors + s.group - 1) / s.group);
     if (s.nv == 3) s.nv = 4;
     return s;
 }
 
-int64_t norm_parts(int64_t rows, int64_t cols) {
-    (void)cols;
-    return rows < PARTS_MAX ? rows : PARTS_MAX;
+template <typename Kernel>
+int start_norm_kernel(Kernel kernel, const NormParams &p, int grid, int threads, size_t smem, cudaStream_t st) {
+    if (smem > 47 * 1024) KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    kernel<<<grid, threads, smem, st>>>(p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
 }
 
-template <typename T, bool WIDE, bool WARP, int NV>
-void start_norm_forward(const NormParams &p, int grid, int threads, cudaStream_t st) {
-    k_norm_forward<T, WIDE, WARP, NV><<<grid, threads, 0, st>>>(p);
-}
-template <typename T, bool WIDE, bool WARP, int NV>
-void start_norm_backward(const NormParams &p, int grid, int threads, cudaStream_t st) {
-    const size_t smem = WARP ? 2 * 32 * NV * Elems<T>::V * sizeof(float) : 0;
-    if (p.codes != nullptr) k_norm_backward<T, WIDE, WARP, NV, true><<<grid, threads, smem, st>>>(p);
-    else k_norm_backward<T, WIDE, WARP, NV, false><<<grid, threads, smem, st>>>(p);
-}
-
-template <typename T, bool WIDE, bool WARP>
-void start_norm(bool backward, const RowShape &s, const NormParams &p, int grid, cudaStream_t st) {
-#define KT_NV(n)                                                                            \
-    (backward ? start_norm_backward<T, WIDE, WARP, n>(p, grid, s.threads, st) : start_norm_forward<T, WIDE, WARP, n>(p, grid, s.threads, st))
-    if (s.nv == 1) KT_NV(1);
-    else if (s.nv == 2) KT_NV(2);
-    else if constexpr (E / Elems<T>::V >= 4) KT_NV(4);
-#undef KT_NV
+template <typename T, bool WIDE, int GROUP, int NV>
+int start_norm(bool backward, const NormParams &p, int grid, cudaStream_t st) {
+    constexpr int V = Elems<T>::V, T_ = norm_threads<GROUP>(), CELLS = WIDE ? (rows_ahead<NV>() + 1) * NV * T_ : 0;
+    if (!backward) return start_norm_kernel(k_norm_forward<T, WIDE, GROUP, NV>, p, grid, T_, CELLS * sizeof(uint4), st);
+    const size_t joined = GROUP == 32 ? 2 * 32 * NV * V * sizeof(float) : 0;
+    const size_t kept = CELLS * (sizeof(uint4) + V + sizeof(float)), whole = CELLS * 2 * sizeof(uint4);
+    if (p.codes != nullptr) return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, true>, p, grid, T_, kept > joined ? kept : joined, st);
+    return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, false>, p, grid, T_, whole > joined ? whole : joined, st);
 }
 
-template <typename T>
-void start_norm(bool backward, bool wide_, const RowShape &s, const NormParams &p, int grid, cudaStream_t st) {
-    if (wide_) s.warp ? start_norm<T, true, true>(backward, s, p, grid, st) : start_norm<T, true, false>(backward, s, p, grid, st);
-    else s.warp ? start_norm<T, false, true>(backward, s, p, grid, st) : start_norm<T, false, false>(backward, s, p, grid, st);
+template <typename T, bool WIDE, int GROUP>
+int start_norm(bool backward, int nv, const NormParams &p, int grid, cudaStream_t st) {
+    if (nv == 1) return start_norm<T, WIDE, GROUP, 1>(backward, p, grid, st);
+    if (nv == 2) return start_norm<T, WIDE, GROUP, 2>(backward, p, grid, st);
+    if constexpr (E / Elems<T>::V >= 4) return start_norm<T, WIDE, GROUP, 4>(backward, p, grid, st);
+    else return fail(KT_ERR_SHAPE, "no kernel for %d vectors to a thread", nv);
+}
+
+template <typename T, bool WIDE>
+int start_norm(bool backward, const RowShape &s, const NormParams &p, int grid, cudaStream_t st) {
+    switch (s.group) {
+        case 32: return start_norm<T, WIDE, 32>(backward, s.nv, p, grid, st);
+        case 128: return start_norm<T, WIDE, 128>(backward, s.nv, p, grid, st);
+        case 256: return start_norm<T, WIDE, 256>(backward, s.nv, p, grid, st);
+        default: return start_norm<T, WIDE, 512>(backward, s.nv, p, grid, st);
+    }
+}
+
+int start_norm(bool backward, int dtype, bool wide_, const RowShape &s, const NormParams &p, int grid, cudaStream_t st) {
+    if (dtype == KT_F32) return wide_ ? start_norm<float, true>(backward, s, p, grid, st) : start_norm<float, false>(backward, s, p, grid, st);
+    return wide_ ? start_norm<__nv_bfloat16, true>(backward, s, p, grid, st) : start_norm<__nv_bfloat16, false>(backward, s, p, grid, st);
 }
 
 template <typename T>
@@ -733,12 +1010,24 @@ void start_norm_any(bool backward, const NormParams &p, int grid, cudaStream_t s
     }
 }
 
-int elem_grid(ElemParams *p, int dtype, int64_t *ctas) {
-    const int v = dtype == KT_F32 ? 4 : 8;
-    p->per_row = static_cast<unsigned>(blocks_of(p->cols) * (BLOCK / v));
-    p->vectors = p->rows * p->per_row;
-    *ctas = (p->vectors + U * THREADS - 1) / (U * THREADS);
-    if (*ctas > INT_MAX) return fail(KT_ERR_SHAPE, "%lld x %lld elements are too many", (long long)p->rows, (long long)p->cols);
+// Runs start(p, ctas) over the rows, in pieces of fewer than 2^30 vectors.
+template <typename Start>
+int over_rows(ElemParams p, int dtype, Start start) {
+    const int v = dtype == KT_F32 ? 4 : 8, es = elem_size(dtype);
+    p.per_row = static_cast<unsigned>(blocks_of(p.cols) * (BLOCK / v));
+    for (p.shift = 0; (1u << p.shift) < p.per_row;) ++p.shift;
+    p.magic = static_cast<unsigned>(((1ull << 32) * ((1ull << p.shift) - p.per_row)) / p.per_row + 1);
+    const int64_t piece = (INT64_C(1) << 30) / p.per_row, all = p.rows;
+    for (int64_t r = 0; r < all; r += piece) {
+        ElemParams q = p;
+        q.rows = all - r < piece ? all - r : piece;
+        q.vectors = static_cast<unsigned>(q.rows * q.per_row);
+        auto past = [&](const void *at, int64_t stride) { return at ? static_cast<const char *>(at) + r * stride * es : nullptr; };
+        q.in = past(p.in, p.in_stride), q.x = past(p.x, p.x_stride), q.out = const_cast<char *>(past(p.out, p.out_stride));
+        q.codes = p.codes ? p.codes + r * pitch_of(p.cols) : nullptr, q.scales = p.scales ? p.scales + r * blocks_of(p.cols) : nullptr;
+        start(q, static_cast<int>((q.vectors + U * THREADS - 1) / (U * THREADS)));
+        KT_CUDA(cudaGetLastError());
+    }
     return KT_OK;
 }
 
@@ -757,16 +1046,20 @@ void start_act_backward(const ElemParams &p, int kind, int ctas, cudaStream_t st
     else kept ? k_act_backward<T, WIDE, KT_SILU, true><<<ctas, THREADS, 0, st>>>(p) : k_act_backward<T, WIDE, KT_SILU, false><<<ctas, THREADS, 0, st>>>(p);
 }
 
-int act_forward(ElemParams p, int dtype, int kind, bool wide_, void *stream) {
-    int64_t ctas = 0;
-    if (int rc = elem_grid(&p, dtype, &ctas)) return rc;
-    if (ctas == 0) return KT_OK;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == KT_F32) wide_ ? start_act_forward<float, true>(p, kind, ctas, st) : start_act_forward<float, false>(p, kind, ctas, st);
-    else wide_ ? start_act_forward<__nv_bfloat16, true>(p, kind, ctas, st) : start_act_forward<__nv_bfloat16, false>(p, kind, ctas, st);
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
+int act_forward(const ElemParams &all, int dtype, int kind, bool wide_, cudaStream_t st) {
+    return over_rows(all, dtype, [&](const ElemParams &p, int ctas) {
+        if (dtype == KT_F32) wide_ ? start_act_forward<float, true>(p, kind, ctas, st) : start_act_forward<float, false>(p, kind, ctas, st);
+        else wide_ ? start_act_forward<__nv_bfloat16, true>(p, kind, ctas, st) : start_act_forward<__nv_bfloat16, false>(p, kind, ctas, st);
+    });
 }
+
+// Rows of partial sums, one to a CTA: few enough rows that a CTA takes four of its own, so that the
+// partial sums stay small beside what is read.
+int64_t norm_parts(int64_t rows, const RowShape &s) {
+    const int64_t busy = static_cast<int64_t>(SMS) * (512 / s.threads), need = (rows + s.threads / s.group * 4 - 1) / (s.threads / s.group * 4);
+    return need < busy ? need : busy;
+}
+constexpr int64_t ANY_PARTS = 16;
 
 }  // namespace
 
@@ -785,31 +1078,33 @@ int kt_norm_forward(const void *x, int64_t x_stride, const void *weight, const v
     if (int rc = check_matrix("x", x, x_stride, rows, cols, dtype)) return rc;
     if (int rc = check_matrix("out", out, out_stride, rows, cols, dtype)) return rc;
     if (int rc = check_codes(codes, scales, false)) return rc;
-    int sms = 0;
-    if (int rc = sm_count(&sms)) return rc;
     NormParams p{};
     p.x = x, p.weight = weight, p.bias = bias, p.out = out, p.mean = mean, p.rstd = rstd, p.codes = codes, p.scales = scales;
     p.rows = rows, p.cols = cols, p.x_stride = x_stride, p.out_stride = out_stride, p.eps = eps, p.param_bf16 = param_dtype == KT_BF16;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (cols > ROW_MAX) {
-        const int grid = static_cast<int>(rows < sms * 4 ? rows : sms * 4);
+        const int grid = static_cast<int>(rows < SMS * 4 ? rows : SMS * 4);
         if (dtype == KT_F32) start_norm_any<float>(false, p, grid, st);
         else start_norm_any<__nv_bfloat16>(false, p, grid, st);
-    } else {
-        const RowShape s = row_shape(cols, dtype);
-        const bool w = wide(x, x_stride, rows, cols, dtype) && wide(out, out_stride, rows, cols, dtype);
-        const int64_t need = (rows + s.rows_per_cta - 1) / s.rows_per_cta, most = static_cast<int64_t>(sms) * (1024 / s.threads);
-        const int grid = static_cast<int>(need < most ? need : most);
-        if (dtype == KT_F32) start_norm<float>(false, w, s, p, grid, st);
-        else start_norm<__nv_bfloat16>(false, w, s, p, grid, st);
+        KT_CUDA(cudaGetLastError());
+        return KT_OK;
     }
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
+    const RowShape s = row_shape(cols, dtype);
+    const int per_cta = s.threads / s.group;
+    const bool w = wide(x, x_stride, rows, cols, dtype) && wide(out, out_stride, rows, cols, dtype);
+    const int64_t need = (rows + per_cta - 1) / per_cta, most = static_cast<int64_t>(SMS) * ((s.nv * (dtype == KT_F32 ? 4 : 8) == E ? 512 : 768) / s.threads);
+    return start_norm(false, dtype, w, s, p, static_cast<int>(need < most ? need : most), st);
 }
 
 int64_t kt_norm_workspace(int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1) return 0;
-    return norm_parts(rows, cols) * 2 * cols * static_cast<int64_t>(sizeof(float));
+    int64_t parts = rows < ANY_PARTS ? rows : ANY_PARTS;
+    if (cols <= ROW_MAX)                  // room for either type
+        for (int dtype : {KT_F32, KT_BF16}) {
+            const int64_t n = norm_parts(rows, row_shape(cols, dtype));
+            parts = dtype == KT_F32 || n > parts ? n : parts;
+        }
+    return parts * 2 * cols * static_cast<int64_t>(sizeof(float));
 }
 
 int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64_t x_stride, const float *mean, const int8_t *codes,
@@ -838,8 +1133,6 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
             if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(KT_ERR_ALIGN, "workspace is not 16-byte aligned");
         }
     }
-    int sms = 0;
-    if (int rc = sm_count(&sms)) return rc;
     NormParams p{};
     p.dout = dout, p.x = x, p.weight = weight, p.out = dx, p.mean = const_cast<float *>(mean), p.rstd = const_cast<float *>(rstd);
     p.codes = const_cast<int8_t *>(codes), p.scales = const_cast<float *>(scales), p.dweight = dweight, p.dbias = dbias;
@@ -847,23 +1140,19 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
     p.rows = rows, p.cols = cols, p.dout_stride = dout_stride, p.x_stride = x_stride, p.out_stride = dx_stride, p.param_bf16 = param_dtype == KT_BF16;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (rows > 0 && cols > ROW_MAX) {
-        p.n_parts = static_cast<int>(rows < 16 ? rows : 16);
-        const int grid = static_cast<int>(rows < sms * 4 ? rows : sms * 4);
+        p.n_parts = static_cast<int>(rows < ANY_PARTS ? rows : ANY_PARTS);
+        const int grid = static_cast<int>(rows < SMS * 4 ? rows : SMS * 4);
         if (dtype == KT_F32) start_norm_any<float>(true, p, grid, st);
         else start_norm_any<__nv_bfloat16>(true, p, grid, st);
         KT_CUDA(cudaGetLastError());
     } else if (rows > 0) {
         const RowShape s = row_shape(cols, dtype);
         const bool w = wide(dout, dout_stride, rows, cols, dtype) && wide(dx, dx_stride, rows, cols, dtype) && (x == nullptr || wide(x, x_stride, rows, cols, dtype));
-        const int64_t need = (rows + s.rows_per_cta - 1) / s.rows_per_cta;
-        const int64_t busy = static_cast<int64_t>(sms) * (512 / s.threads), most = busy < norm_parts(rows, cols) ? busy : norm_parts(rows, cols);
-        p.n_parts = static_cast<int>(need < most ? need : most);
-        if (dtype == KT_F32) start_norm<float>(true, w, s, p, p.n_parts, st);
-        else start_norm<__nv_bfloat16>(true, w, s, p, p.n_parts, st);
-        KT_CUDA(cudaGetLastError());
+        p.n_parts = static_cast<int>(norm_parts(rows, s));
+        if (int rc = start_norm(true, dtype, w, s, p, p.n_parts, st)) return rc;
     }
     if (sums) {
-        k_norm_params<<<dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 16), 0, st>>>(p);
+        k_norm_params<<<dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st>>>(p);
         KT_CUDA(cudaGetLastError());
     }
     return KT_OK;
@@ -876,7 +1165,7 @@ int kt_ckpt_store(const void *x, int64_t x_stride, int8_t *codes, float *scales,
     if (int rc = check_codes(codes, scales, true)) return rc;
     ElemParams p{};
     p.in = x, p.in_stride = x_stride, p.codes = codes, p.scales = scales, p.rows = rows, p.cols = cols;
-    return act_forward(p, dtype, KIND_NONE, wide(x, x_stride, rows, cols, dtype), stream);
+    return act_forward(p, dtype, KIND_NONE, wide(x, x_stride, rows, cols, dtype), static_cast<cudaStream_t>(stream));
 }
 
 int kt_ckpt_restore(const int8_t *codes, const float *scales, const void *weight, const void *bias, int param_dtype, void *out,
@@ -889,14 +1178,12 @@ int kt_ckpt_restore(const int8_t *codes, const float *scales, const void *weight
     ElemParams p{};
     p.codes = const_cast<int8_t *>(codes), p.scales = const_cast<float *>(scales), p.weight = weight, p.bias = bias;
     p.param_bf16 = param_dtype == KT_BF16, p.out = out, p.out_stride = out_stride, p.rows = rows, p.cols = cols;
-    int64_t ctas = 0;
-    if (int rc = elem_grid(&p, dtype, &ctas)) return rc;
     const bool w = wide(out, out_stride, rows, cols, dtype);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == KT_F32) w ? k_restore<float, true><<<ctas, THREADS, 0, st>>>(p) : k_restore<float, false><<<ctas, THREADS, 0, st>>>(p);
-    else w ? k_restore<__nv_bfloat16, true><<<ctas, THREADS, 0, st>>>(p) : k_restore<__nv_bfloat16, false><<<ctas, THREADS, 0, st>>>(p);
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
+    return over_rows(p, dtype, [&](const ElemParams &q, int ctas) {
+        if (dtype == KT_F32) w ? k_restore<float, true><<<ctas, THREADS, 0, st>>>(q) : k_restore<float, false><<<ctas, THREADS, 0, st>>>(q);
+        else w ? k_restore<__nv_bfloat16, true><<<ctas, THREADS, 0, st>>>(q) : k_restore<__nv_bfloat16, false><<<ctas, THREADS, 0, st>>>(q);
+    });
 }
 
 int kt_act_forward(const void *x, int64_t x_stride, void *out, int64_t out_stride, int8_t *codes, float *scales, int64_t rows,
@@ -909,7 +1196,7 @@ int kt_act_forward(const void *x, int64_t x_stride, void *out, int64_t out_strid
     if (int rc = check_codes(codes, scales, false)) return rc;
     ElemParams p{};
     p.in = x, p.in_stride = x_stride, p.out = out, p.out_stride = out_stride, p.codes = codes, p.scales = scales, p.rows = rows, p.cols = cols;
-    return act_forward(p, dtype, kind, wide(x, x_stride, rows, cols, dtype) && wide(out, out_stride, rows, cols, dtype), stream);
+    return act_forward(p, dtype, kind, wide(x, x_stride, rows, cols, dtype) && wide(out, out_stride, rows, cols, dtype), static_cast<cudaStream_t>(stream));
 }
 
 int kt_act_backward(const void *dout, int64_t dout_stride, const void *x, int64_t x_stride, const int8_t *codes, const float *scales,
@@ -928,14 +1215,12 @@ int kt_act_backward(const void *dout, int64_t dout_stride, const void *x, int64_
     ElemParams p{};
     p.in = dout, p.in_stride = dout_stride, p.x = x, p.x_stride = x_stride, p.out = dx, p.out_stride = dx_stride;
     p.codes = const_cast<int8_t *>(codes), p.scales = const_cast<float *>(scales), p.rows = rows, p.cols = cols;
-    int64_t ctas = 0;
-    if (int rc = elem_grid(&p, dtype, &ctas)) return rc;
     const bool w = wide(dout, dout_stride, rows, cols, dtype) && wide(dx, dx_stride, rows, cols, dtype) && (x == nullptr || wide(x, x_stride, rows, cols, dtype));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == KT_F32) w ? start_act_backward<float, true>(p, kind, ctas, st) : start_act_backward<float, false>(p, kind, ctas, st);
-    else w ? start_act_backward<__nv_bfloat16, true>(p, kind, ctas, st) : start_act_backward<__nv_bfloat16, false>(p, kind, ctas, st);
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
+    return over_rows(p, dtype, [&](const ElemParams &q, int ctas) {
+        if (dtype == KT_F32) w ? start_act_backward<float, true>(q, kind, ctas, st) : start_act_backward<float, false>(q, kind, ctas, st);
+        else w ? start_act_backward<__nv_bfloat16, true>(q, kind, ctas, st) : start_act_backward<__nv_bfloat16, false>(q, kind, ctas, st);
+    });
 }
 
 }  // extern "C"
