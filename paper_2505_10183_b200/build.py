@@ -14,7 +14,7 @@ SOURCES = [os.path.join(_PKG, "csrc", "kaitian.cu"), os.path.join(_PKG, "csrc", 
            os.path.join(_PKG, "csrc", "kt_rows.cu"),
            os.path.join(_PKG, "csrc", "kt_attn.cu")]
 DEPENDS = [os.path.join(_PKG, "csrc", "kt_kernels.cuh"), os.path.join(_PKG, "csrc", "kt_internal.h"),
-           os.path.join(_PKG, "csrc", "kt_tensor.cuh")]
+           os.path.join(_PKG, "csrc", "kt_tensor.cuh"), os.path.join(_PKG, "csrc", "kt_pairs.cuh")]
 HEADERS = [os.path.join(_ROOT, "include", "kaitian.h")]
 LIB = os.path.join(_PKG, "libkaitian_b200.so")
 

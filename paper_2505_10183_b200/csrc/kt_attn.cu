@@ -22,6 +22,7 @@
 #include <cmath>
 
 #include "kt_internal.h"
+#include "kt_pairs.cuh"
 #include "kt_tensor.cuh"
 
 using namespace ktd;
@@ -29,8 +30,10 @@ using namespace ktd;
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int WORKERS = 256;                    // threads that compute: two groups of four warps
-constexpr int WARP_MMA = 8, WARP_LOAD = 9, THREADS = 320;
+constexpr int WARP_MMA = 8, WARP_LOAD = 9, THREADS = 384;      // warps 10 and 11 only fill their group
+// Registers: a block of 384 threads starts with 168 each, 64512 in all; the third group gives back what the
+// eight warps that compute take: 256 x 208 + 128 x 88 = 64512.
+constexpr int REGISTERS_COMPUTE = 208, REGISTERS_HELP = 88;
 constexpr uint32_t TMEM_COLUMNS = 512;
 
 struct AttnParams {
@@ -150,7 +153,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         bar_init(&sm.q_full, 1);
         bar_init(&sm.landed, 1);
         for (int i = 0; i < FWD_SLOTS; ++i) bar_init(&sm.kv_full[i], 1), bar_init(&sm.kv_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], TILE), bar_init(&sm.o_full[w], 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_full[w], 1);
         sm.gave_up = 0;
         fence_async_smem();
     }
@@ -161,6 +164,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
+    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
@@ -181,14 +185,14 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     } else if (warp == WARP_MMA) {
         auto wait_kv = [&](int i) { return bar_wait(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
         auto scores = [&](int w, int j) {
-            if (lane == 0) {
+            if (elected()) {
                 product_rows<DH>(tmem + w * TILE, smem_addr(sm.q[w]), smem_addr(sm.kv[2 * j % FWD_SLOTS]));
                 mma_commit(&sm.s_full[w]);
             }
             __syncwarp();
         };
         auto free_kv = [&](int i) {
-            if (lane == 0) mma_commit(&sm.kv_free[i % FWD_SLOTS]);
+            if (elected()) mma_commit(&sm.kv_free[i % FWD_SLOTS]);
             __syncwarp();
         };
         if (n > 0 && bar_wait(&sm.q_full, 0, gave_up) && wait_kv(0)) {
@@ -203,7 +207,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     ok = bar_wait(&sm.p_ready[w], j & 1, gave_up);
                     if (!ok) break;
                     tmem_fence_after();
-                    if (lane == 0) {
+                    if (elected()) {
                         product_down<DH>(tmem + 256 + w * DH, tmem + w * TILE, smem_addr(sm.kv[(2 * j + 1) % FWD_SLOTS]), j > 0);
                         if (j == n_tiles[w] - 1) mma_commit(&sm.o_full[w]);
                     }
@@ -218,7 +222,8 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (j + 1 < n) free_kv(2 * j + 2);
             }
         }
-    } else {
+    } else if (warp < WARP_MMA) {
+        registers_take<REGISTERS_COMPUTE>();
         const int w = warp / 4, row = row0 + w * TILE + threadIdx.x % TILE;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + w * TILE, o_at = lanes + 256 + w * DH;
         const int limit = seq.keys_of(row), all_see = seq.keys_of(row0 + w * TILE);    // the tile's first row sees least
@@ -229,18 +234,24 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (!(ok = bar_wait(&sm.s_full[w], j & 1, gave_up))) break;
             tmem_fence_after();
             uint32_t s[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_load32(s_at + c * 32, s[c]);
-            tmem_wait_loads();
-            if (!whole || (j + 1) * TILE > all_see) {
-                const int left = limit - j * TILE;
-#pragma unroll
-                for (int c = 0; c < TILE; ++c)
-                    if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
-            }
+            const int left = !whole || (j + 1) * TILE > all_see ? limit - j * TILE : TILE;     // columns that the row sees
             float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            tmem_load32(s_at, s[0]);
+            tmem_load32(s_at + 32, s[1]);
+            tmem_wait_loads();
+            tmem_load32(s_at + 64, s[2]);
+            tmem_load32(s_at + 96, s[3]);
 #pragma unroll
-            for (int c = 0; c < TILE; ++c) m[c % 4] = fmaxf(m[c % 4], __uint_as_float(s[c / 32][c % 32]));
+            for (int half = 0; half < 2; ++half) {
+                if (half == 1) tmem_wait_loads();
+                if (__any_sync(0xFFFFFFFFu, left < (half + 1) * 64)) {
+#pragma unroll
+                    for (int c = half * 64; c < half * 64 + 64; ++c)
+                        if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
+                }
+#pragma unroll
+                for (int c = half * 64; c < half * 64 + 64; ++c) m[c % 4] = fmaxf(m[c % 4], __uint_as_float(s[c / 32][c % 32]));
+            }
             const float here = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
             // The running maximum follows only when it would grow by 2^8: until then probabilities of up
             // to 256 are as exact, and the sums in tensor memory need not be rescaled.
@@ -262,24 +273,23 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 }
             }
             const float ref = top == -INFINITY ? 0.0f : top;
-            float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            float2 part[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 uint32_t packed[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) {
-                    const float x = exp2_fast(fmaf(__uint_as_float(s[half * 2 + c / 32][c % 32]), p.scale_log2, -ref));
-                    const float y = exp2_fast(fmaf(__uint_as_float(s[half * 2 + c / 32][c % 32 + 1]), p.scale_log2, -ref));
-                    part[c % 4] += x;
-                    part[c % 4 + 1] += y;
-                    packed[c / 2] = pack_bf16(x, y);
+                    const float2 x = fma2(pair_of(s[half * 2 + c / 32], c % 32), both(p.scale_log2), both(-ref));
+                    const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                    part[c / 2 % 2] = add2(part[c / 2 % 2], e);
+                    packed[c / 2] = pack_bf16(e);
                 }
                 tmem_store32(s_at + half * 64, packed);
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive(&sm.p_ready[w]);
+            bar_arrive_warp(&sm.p_ready[w]);
         }
         const bool any = n_tiles[w] > 0;
         if (any && ok) ok = bar_wait(&sm.o_full[w], 0, gave_up);
@@ -370,7 +380,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
         for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
         bar_init(&sm.s_full[0], 1), bar_init(&sm.s_full[1], 1), bar_init(&sm.dp_full, 1), bar_init(&sm.dq_full, 1);
-        bar_init(&sm.dp_taken, WORKERS), bar_init(&sm.ds_ready, WORKERS);
+        bar_init(&sm.dp_taken, 8), bar_init(&sm.ds_ready, 8);
         sm.gave_up = 0;
         fence_async_smem();
     }
@@ -381,6 +391,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
+    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
@@ -404,7 +415,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         auto scores = [&](int j) {
             const int ks = j % Smem::K_SLOTS;
             if (!bar_wait(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
-            if (lane == 0) {
+            if (elected()) {
                 product_rows<DH>(tmem + (j & 1) * TILE, smem_addr(sm.q), smem_addr(sm.k[ks]));
                 mma_commit(&sm.s_full[j & 1]);
             }
@@ -416,7 +427,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             if (!bar_wait(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) return false;
             if (j > 0 && !bar_wait(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
             tmem_fence_after();
-            if (lane == 0) {
+            if (elected()) {
                 product_rows<DH>(tmem + 2 * TILE, smem_addr(sm.dout), smem_addr(sm.v[vs]));
                 mma_commit(&sm.dp_full);
                 mma_commit(&sm.v_free[vs]);
@@ -429,7 +440,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 if (j + 1 < n && !(scores(j + 1) && dprobs(j + 1))) break;
                 if (!bar_wait(&sm.ds_ready, j & 1, gave_up)) break;
                 tmem_fence_after();
-                if (lane == 0) {
+                if (elected()) {
                     product_down<DH>(tmem + 3 * TILE, tmem + (j & 1) * TILE, smem_addr(sm.k[j % Smem::K_SLOTS]), j > 0);
                     mma_commit(&sm.k_free[j % Smem::K_SLOTS]);
                     if (j == n - 1) mma_commit(&sm.dq_full);
@@ -437,7 +448,8 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 __syncwarp();
             }
         }
-    } else {
+    } else if (warp < WARP_MMA) {
+        registers_take<REGISTERS_COMPUTE>();
         const int g = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
         const int limit = seq.keys_of(row), all_see = seq.keys_of(row0);
@@ -454,16 +466,22 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             tmem_load32(s_at + 32, s[1]);
             tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < 64; ++c) s[c / 32][c % 32] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c / 32][c % 32]), p.scale_log2, -lse)));
+            for (int c = 0; c < 64; c += 2) {
+                const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
+                s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
+            }
             if (!(ok = bar_wait(&sm.dp_full, j & 1, gave_up))) break;
             tmem_fence_after();
             tmem_load32(lanes + 2 * TILE + g * 64, d[0]);
             tmem_load32(lanes + 2 * TILE + g * 64 + 32, d[1]);
             tmem_wait_loads();
             tmem_fence_before();
-            bar_arrive(&sm.dp_taken);
+            bar_arrive_warp(&sm.dp_taken);
 #pragma unroll
-            for (int c = 0; c < 64; ++c) d[c / 32][c % 32] = __float_as_uint(__uint_as_float(s[c / 32][c % 32]) * (__uint_as_float(d[c / 32][c % 32]) - delta));
+            for (int c = 0; c < 64; c += 2) {
+                const float2 x = mul2(pair_of(s[c / 32], c % 32), add2(pair_of(d[c / 32], c % 32), both(-delta)));
+                d[c / 32][c % 32] = __float_as_uint(x.x), d[c / 32][c % 32 + 1] = __float_as_uint(x.y);
+            }
             if (!whole || (j + 1) * TILE > all_see) {
                 const int left = limit - j * TILE - g * 64;
 #pragma unroll
@@ -476,7 +494,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             tmem_store32(s_at, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive(&sm.ds_ready);
+            bar_arrive_warp(&sm.ds_ready);
         }
         if (n > 0 && ok) ok = bar_wait(&sm.dq_full, 0, gave_up);
         tmem_fence_after();
@@ -536,7 +554,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         for (int i = 0; i < Smem::SLOTS; ++i)
             bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1), bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
         bar_init(&sm.s_full, 1), bar_init(&sm.dp_full, 1), bar_init(&sm.sums_full, 1);
-        bar_init(&sm.p_ready, WORKERS), bar_init(&sm.ds_ready, WORKERS);
+        bar_init(&sm.p_ready, 8), bar_init(&sm.ds_ready, 8);
         sm.gave_up = 0;
         fence_async_smem();
     }
@@ -547,6 +565,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
+    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
@@ -577,7 +596,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         auto scores = [&](int i) {
             const int slot = i % Smem::SLOTS;
             if (!bar_wait(&sm.q_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
-            if (lane == 0) {
+            if (elected()) {
                 product_rows<DH>(tmem, smem_addr(sm.k), smem_addr(sm.q[slot]));
                 mma_commit(&sm.s_full);
             }
@@ -587,7 +606,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         auto dprobs = [&](int i) {
             const int slot = i % Smem::SLOTS;
             if (!bar_wait(&sm.do_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
-            if (lane == 0) {
+            if (elected()) {
                 product_rows<DH>(tmem + TILE, smem_addr(sm.v), smem_addr(sm.dout[slot]));
                 mma_commit(&sm.dp_full);
             }
@@ -599,7 +618,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 const int slot = i % Smem::SLOTS;
                 if (!bar_wait(&sm.p_ready, i & 1, gave_up)) break;
                 tmem_fence_after();
-                if (lane == 0) {
+                if (elected()) {
                     product_down<DH>(tmem + 2 * TILE, tmem, smem_addr(sm.dout[slot]), i > 0);
                     mma_commit(&sm.do_free[slot]);
                 }
@@ -607,7 +626,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 if (i + 1 < n && !scores(i + 1)) break;
                 if (!bar_wait(&sm.ds_ready, i & 1, gave_up)) break;
                 tmem_fence_after();
-                if (lane == 0) {
+                if (elected()) {
                     product_down<DH>(tmem + 3 * TILE, tmem + TILE, smem_addr(sm.q[slot]), i > 0);
                     mma_commit(&sm.q_free[slot]);
                     if (i == n - 1) mma_commit(&sm.sums_full);
@@ -616,7 +635,8 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 if (i + 1 < n && !dprobs(i + 1)) break;
             }
         }
-    } else {
+    } else if (warp < WARP_MMA) {
+        registers_take<REGISTERS_COMPUTE>();
         const int g = warp / 4, key = key0 + threadIdx.x % TILE;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
         bool ok = true;
@@ -647,7 +667,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             tmem_store32(lanes + g * 64, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive(&sm.p_ready);
+            bar_arrive_warp(&sm.p_ready);
             if (!(ok = bar_wait(&sm.dp_full, i & 1, gave_up))) break;
             tmem_fence_after();
             tmem_load32(lanes + TILE + g * 64, d[0]);
@@ -667,7 +687,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             tmem_store32(lanes + TILE + g * 64, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive(&sm.ds_ready);
+            bar_arrive_warp(&sm.ds_ready);
         }
         if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
         tmem_fence_after();

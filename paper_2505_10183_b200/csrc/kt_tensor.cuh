@@ -30,6 +30,11 @@ __device__ __forceinline__ void bar_init(uint64_t *bar, uint32_t count) {
 __device__ __forceinline__ void bar_arrive(uint64_t *bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
+// One arrival for a warp, after what all its lanes have done before.
+__device__ __forceinline__ void bar_arrive_warp(uint64_t *bar) {
+    __syncwarp();
+    if (threadIdx.x % 32 == 0) bar_arrive(bar);
+}
 __device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
 }
@@ -52,7 +57,7 @@ __device__ __forceinline__ uint64_t now_ns() {
 
 // Waits for the phase of that parity to end; called by whole warps.  False when it gave up, or when
 // another warp of the CTA did: the caller then leaves its loop, and the kernel ends.
-__device__ __noinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
+__device__ __forceinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
     const uint64_t start = now_ns();
     for (uint32_t n = 1;; ++n) {
         if (bar_try(bar, parity)) return true;
@@ -71,6 +76,13 @@ __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatil
     if (!ok) ok = bar_wait_slow(bar, parity, gave_up);
     return __all_sync(0xFFFFFFFFu, ok);
 }
+
+// A group of four warps gives registers back, or takes them, all four together.  What is taken has to have been
+// given back out of the block's own registers at launch.
+template <int N>
+__device__ __forceinline__ void registers_give() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void registers_take() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 
 // ------------------------------------------------------------------------------- tile copies
 // [dim, tokens, heads, batch] -> 128 tokens of 64 elements.
@@ -140,18 +152,25 @@ __host__ __device__ constexpr uint32_t mma_word(int n, bool b_down) {
 // chunks of 64 elements along the row are CHUNK apart.
 constexpr uint64_t OPERAND_ALONG = (1ull << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 constexpr uint64_t OPERAND_DOWN = (static_cast<uint64_t>(CHUNK >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-__device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | ((addr >> 4) & 0x3FFF); }
+__device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | (addr >> 4); }     // shared memory ends below 2^18
 
-__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t word, bool add) {
+// One lane of a warp that is whole; the compiler knows it for one thread and keeps what it issues in
+// uniform registers.
+__device__ __forceinline__ bool elected() {
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
+__device__ __forceinline__ void mma_smem(uint32_t d, uint64_t a, uint64_t b, uint32_t word, uint32_t add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(word), "r"(static_cast<uint32_t>(add))
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(word), "r"(add)
         : "memory");
 }
-__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t word, bool add) {
+__device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t word, uint32_t add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(word), "r"(static_cast<uint32_t>(add))
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(word), "r"(add)
         : "memory");
 }
 // An arrival once every matrix instruction that this thread has issued is done.
@@ -162,25 +181,28 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar) {
 // D[128 x 128] = A B^T over rows of DH elements: both tiles K-major.
 template <int DH>
 __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b) {
+    const uint64_t wa = operand(OPERAND_ALONG, a), wb = operand(OPERAND_ALONG, b);
 #pragma unroll
     for (int k = 0; k < DH / 16; ++k) {
-        const uint32_t off = (k / 4) * CHUNK + (k % 4) * 32;
-        mma_smem(d, operand(OPERAND_ALONG, a + off), operand(OPERAND_ALONG, b + off), mma_word(TILE, false), k > 0);
+        const uint64_t off = ((k / 4) * CHUNK + (k % 4) * 32) >> 4;
+        mma_smem(d, wa + off, wb + off, mma_word(TILE, false), k > 0);
     }
 }
 // D[128 x DH] (+)= A B over 128 rows of B: A is bf16 in tensor memory, the first 64 of its reduction
 // index in 32 columns at `a`, the others 64 columns further; B a tile, read down its rows.
 template <int DH>
 __device__ __forceinline__ void product_down(uint32_t d, uint32_t a, uint32_t b, bool add) {
+    const uint64_t wb = operand(OPERAND_DOWN, b);
 #pragma unroll
     for (int k = 0; k < TILE / 16; ++k)
-        mma_tmem(d, a + (k / 4) * 64 + (k % 4) * 8, operand(OPERAND_DOWN, b + k * 2048), mma_word(DH, true), add || k > 0);
+        mma_tmem(d, a + (k / 4) * 64 + (k % 4) * 8, wb + ((k * 2048) >> 4), mma_word(DH, true), k > 0 ? 1 : static_cast<uint32_t>(add));
 }
 
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
+__device__ __forceinline__ float2 pair_of(const uint32_t (&r)[32], int i) { return make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])); }
+__device__ __forceinline__ uint32_t pack_bf16(float2 v) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(v.y), "f"(v.x));
+    return r;
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
