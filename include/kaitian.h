@@ -644,7 +644,7 @@ typedef struct {
     int32_t batch, len_q, len_kv, heads, heads_kv, head_dim; /* head_dim: a multiple of 8, at most KT_ATTN_MAX_DIM */
     int32_t dtype;                                           /* KT_BF16 */
     int32_t causal;
-    float scale;                                             /* > 0 */
+    float scale;                                             /* from 2^-20 to 2^20 */
     const int32_t *used_q, *used_kv;
 } kt_attn;
 int kt_attn_forward(const kt_attn *desc, const void *q, const int64_t *q_stride, const void *k,

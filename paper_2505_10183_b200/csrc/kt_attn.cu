@@ -36,11 +36,14 @@ constexpr int WARP_MMA = 8, WARP_LOAD = 9, THREADS = 384;      // warps 10 and 1
 constexpr int REGISTERS_COMPUTE = 208, REGISTERS_HELP = 88;
 constexpr uint32_t TMEM_COLUMNS = 512;
 
+struct QueryStats;
+
 struct AttnParams {
     const int32_t *used_q, *used_kv;
     const __nv_bfloat16 *o, *dout;
     __nv_bfloat16 *out, *out2;                  // O, dQ, or dK and dV
-    float *lse, *stats;
+    float *lse;
+    QueryStats *stats;
     int64_t o_stride[3], dout_stride[3], out_stride[3], out2_stride[3];     // batch, token, head
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
     int tiles_q, tiles_kv;
@@ -183,10 +186,12 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
         }
     } else if (warp == WARP_MMA) {
+        const uint32_t tm = uniform(tmem), q_at = uniform(smem_addr(sm.q)), kv_at = uniform(smem_addr(sm.kv));
+        const int last_of[2] = {uniform(n_tiles[0]), uniform(n_tiles[1])}, n_all = uniform(n);
         auto wait_kv = [&](int i) { return bar_wait(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
         auto scores = [&](int w, int j) {
             if (elected()) {
-                product_rows<DH>(tmem + w * TILE, smem_addr(sm.q[w]), smem_addr(sm.kv[2 * j % FWD_SLOTS]));
+                product_rows<DH, TILE>(tm + w * TILE, q_at + w * FwdSmem<DH>::TILE_BYTES, kv_at + 2 * j % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES);
                 mma_commit(&sm.s_full[w]);
             }
             __syncwarp();
@@ -195,31 +200,31 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             if (elected()) mma_commit(&sm.kv_free[i % FWD_SLOTS]);
             __syncwarp();
         };
-        if (n > 0 && bar_wait(&sm.q_full, 0, gave_up) && wait_kv(0)) {
+        if (n_all > 0 && bar_wait(&sm.q_full, 0, gave_up) && wait_kv(0)) {
             for (int w = 0; w < 2; ++w)
-                if (n_tiles[w] > 0) scores(w, 0);
+                if (last_of[w] > 0) scores(w, 0);
             free_kv(0);
-            for (int j = 0; j < n; ++j) {
+            for (int j = 0; j < n_all; ++j) {
                 if (!wait_kv(2 * j + 1)) break;
                 bool ok = true;
                 for (int w = 0; w < 2 && ok; ++w) {
-                    if (j >= n_tiles[w]) continue;
+                    if (j >= last_of[w]) continue;
                     ok = bar_wait(&sm.p_ready[w], j & 1, gave_up);
                     if (!ok) break;
                     tmem_fence_after();
                     if (elected()) {
-                        product_down<DH>(tmem + 256 + w * DH, tmem + w * TILE, smem_addr(sm.kv[(2 * j + 1) % FWD_SLOTS]), j > 0);
-                        if (j == n_tiles[w] - 1) mma_commit(&sm.o_full[w]);
+                        product_down<DH, TILE>(tm + 256 + w * DH, tm + w * TILE, kv_at + (2 * j + 1) % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES, j > 0);
+                        if (j == last_of[w] - 1) mma_commit(&sm.o_full[w]);
                     }
                     __syncwarp();
-                    if (j + 1 < n_tiles[w]) {
+                    if (j + 1 < last_of[w]) {
                         ok = wait_kv(2 * j + 2);
                         if (ok) scores(w, j + 1);
                     }
                 }
                 if (!ok) break;
                 free_kv(2 * j + 1);
-                if (j + 1 < n) free_kv(2 * j + 2);
+                if (j + 1 < n_all) free_kv(2 * j + 2);
             }
         }
     } else if (warp < WARP_MMA) {
@@ -284,7 +289,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     part[c / 2 % 2] = add2(part[c / 2 % 2], e);
                     packed[c / 2] = pack_bf16(e);
                 }
-                tmem_store32(s_at + half * 64, packed);
+                tmem_store32(s_at + half * 32, packed);
             }
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_wait_stores();
@@ -319,14 +324,33 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
 }
 
 // ----------------------------------------------------------------------------------- backward
-// Per query tile, side by side: lse in units of log 2 (+inf where a query sees nothing or is not in
-// use, which makes its probabilities exp2(s - inf) = 0), and delta.  A half warp to a row.
+// What the backward kernels need of a query besides its rows, tile by tile:
+//   for dQ, fp32: lse in units of log 2 (+inf where a query sees nothing or is not in use, which makes its
+//   probabilities exp2(s - inf) = 0), and delta;
+//   for dK and dV: -lse / scale and -delta, each as a sum of three bf16 (24 bits), side by side in 16 bytes.  There
+//   queries are columns, and a thread would have to read every column's values from shared memory for
+//   each row; instead the tensor cores add them: one more product over 16 elements, with a row of ones.
+struct QueryStats {
+    float lse[TILE], delta[TILE];
+    uint4 terms[TILE];
+};
+constexpr float HIDDEN = -1e30f;                // in place of -lse / scale where nothing is seen
+
+__device__ __forceinline__ void three_terms(float x, uint16_t (&to)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        const __nv_bfloat16 t = __float2bfloat16_rn(x);
+        to[i] = __bfloat16_as_ushort(t);
+        x -= __bfloat162float(t);
+    }
+}
+
+// A half warp to a row.
 __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
     const int64_t at = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16;
     const int lane = threadIdx.x % 16;
     const int64_t bh = at / (p.tiles_q * TILE);
     const int row = static_cast<int>(at % (p.tiles_q * TILE));
-    if (bh >= static_cast<int64_t>(p.batch) * p.heads) return;       // whole CTAs: 128 rows to a tile
     const int b = static_cast<int>(bh / p.heads), h = static_cast<int>(bh % p.heads);
     const Seq seq(p, b);
     float delta = 0.0f;
@@ -344,20 +368,26 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
     for (int d = 8; d > 0; d /= 2) delta += __shfl_xor_sync(0xFFFFFFFFu, delta, d);
     if (lane == 0) {
         const float lse = row < seq.n ? p.lse[bh * p.len_q + row] : -INFINITY;
-        float *to = p.stats + at / TILE * 2 * TILE + at % TILE;
-        to[0] = lse == -INFINITY ? INFINITY : lse * LOG2E;
-        to[TILE] = lse == -INFINITY ? 0.0f : delta;
+        const bool empty = lse == -INFINITY;
+        QueryStats &to = p.stats[at / TILE];
+        to.lse[at % TILE] = empty ? INFINITY : lse * LOG2E;
+        to.delta[at % TILE] = empty ? 0.0f : delta;
+        uint16_t l[3], d[3];
+        three_terms(empty ? HIDDEN : -lse / p.scale, l);
+        three_terms(empty ? 0.0f : -delta, d);
+        to.terms[at % TILE] = make_uint4(l[0] | l[1] << 16, l[2] | d[0] << 16, d[1] | d[2] << 16, 0);
     }
 }
 
-// dQ: 128 queries to a CTA.  The two groups of four warps share the rows and split the columns (keys) of
-// a tile.  Tensor memory: scores (over them dS) 0 and 128 in turn, dP 256, sums 384.
+// dQ: 128 queries to a CTA, the two groups of four warps take its key tiles in turn.  While one takes the
+// exponentials of its scores the other, with its probabilities done, works on dP.  Tensor memory: scores
+// (over them dS) 0 and 128, dP 256, sums 384.
 template <int DH>
 struct DqSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
     static constexpr int K_SLOTS = 3, V_SLOTS = 2;
     alignas(1024) uint8_t q[TILE_BYTES], dout[TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
-    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], dp_full, dp_taken, ds_ready, dq_full, landed;
+    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], dp_full, dp_taken, ds_ready[2], dq_full, landed;
     uint32_t tmem, gave_up;
 };
 
@@ -379,8 +409,8 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         bar_init(&sm.landed, 1);
         for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
         for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
-        bar_init(&sm.s_full[0], 1), bar_init(&sm.s_full[1], 1), bar_init(&sm.dp_full, 1), bar_init(&sm.dq_full, 1);
-        bar_init(&sm.dp_taken, 8), bar_init(&sm.ds_ready, 8);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.ds_ready[w], 4);
+        bar_init(&sm.dp_full, 1), bar_init(&sm.dp_taken, 4), bar_init(&sm.dq_full, 1);
         sm.gave_up = 0;
         fence_async_smem();
     }
@@ -412,11 +442,13 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             }
         }
     } else if (warp == WARP_MMA) {
+        const uint32_t tm = uniform(tmem), q_at = uniform(smem_addr(sm.q)), do_at = uniform(smem_addr(sm.dout)), k_at = uniform(smem_addr(sm.k)), v_at = uniform(smem_addr(sm.v));
+        const int n_all = uniform(n);
         auto scores = [&](int j) {
             const int ks = j % Smem::K_SLOTS;
             if (!bar_wait(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
             if (elected()) {
-                product_rows<DH>(tmem + (j & 1) * TILE, smem_addr(sm.q), smem_addr(sm.k[ks]));
+                product_rows<DH, TILE>(tm + (j & 1) * TILE, q_at, k_at + ks * Smem::TILE_BYTES);
                 mma_commit(&sm.s_full[j & 1]);
             }
             __syncwarp();
@@ -428,80 +460,89 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             if (j > 0 && !bar_wait(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
             tmem_fence_after();
             if (elected()) {
-                product_rows<DH>(tmem + 2 * TILE, smem_addr(sm.dout), smem_addr(sm.v[vs]));
+                product_rows<DH, TILE>(tm + 2 * TILE, do_at, v_at + vs * Smem::TILE_BYTES);
                 mma_commit(&sm.dp_full);
                 mma_commit(&sm.v_free[vs]);
             }
             __syncwarp();
             return true;
         };
-        if (n > 0 && bar_wait(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0)) {
-            for (int j = 0; j < n; ++j) {
-                if (j + 1 < n && !(scores(j + 1) && dprobs(j + 1))) break;
-                if (!bar_wait(&sm.ds_ready, j & 1, gave_up)) break;
+        if (n_all > 0 && bar_wait(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0) && (n_all == 1 || scores(1))) {
+            for (int j = 0; j < n_all; ++j) {
+                if (j + 1 < n_all && !dprobs(j + 1)) break;
+                if (!bar_wait(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
                 tmem_fence_after();
                 if (elected()) {
-                    product_down<DH>(tmem + 3 * TILE, tmem + (j & 1) * TILE, smem_addr(sm.k[j % Smem::K_SLOTS]), j > 0);
+                    product_down<DH, TILE>(tm + 3 * TILE, tm + (j & 1) * TILE, k_at + j % Smem::K_SLOTS * Smem::TILE_BYTES, j > 0);
                     mma_commit(&sm.k_free[j % Smem::K_SLOTS]);
-                    if (j == n - 1) mma_commit(&sm.dq_full);
+                    if (j == n_all - 1) mma_commit(&sm.dq_full);
                 }
                 __syncwarp();
+                if (j + 2 < n_all && !scores(j + 2)) break;
             }
         }
     } else if (warp < WARP_MMA) {
         registers_take<REGISTERS_COMPUTE>();
-        const int g = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+        const int w = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + w * TILE, dp_at = lanes + 2 * TILE;
         const int limit = seq.keys_of(row), all_see = seq.keys_of(row0);
         const bool whole = row0 + TILE <= seq.n;
-        const float *stats = p.stats + (static_cast<int64_t>(bh) * p.tiles_q + tile) * 2 * TILE + in_tile;
-        const float lse = stats[0], delta = stats[TILE];
+        const QueryStats &stats = p.stats[static_cast<int64_t>(bh) * p.tiles_q + tile];
+        const float lse = stats.lse[in_tile], delta = stats.delta[in_tile];
         bool ok = true;
-        for (int j = 0; j < n; ++j) {
-            const uint32_t s_at = lanes + (j & 1) * TILE + g * 64;
-            if (!(ok = bar_wait(&sm.s_full[j & 1], j / 2 & 1, gave_up))) break;
+        for (int j = w; j < n; j += 2) {
+            if (!(ok = bar_wait(&sm.s_full[w], j / 2 & 1, gave_up))) break;
             tmem_fence_after();
-            uint32_t s[2][32], d[2][32];
+            uint32_t s[4][32];
             tmem_load32(s_at, s[0]);
             tmem_load32(s_at + 32, s[1]);
             tmem_wait_loads();
+            tmem_load32(s_at + 64, s[2]);
+            tmem_load32(s_at + 96, s[3]);
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
-                s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
+            for (int half = 0; half < 2; ++half) {
+                if (half == 1) tmem_wait_loads();
+#pragma unroll
+                for (int c = half * 64; c < half * 64 + 64; c += 2) {
+                    const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
+                    s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
+                }
             }
+            const int left = !whole || (j + 1) * TILE > all_see ? limit - j * TILE : TILE;     // columns that the row sees
             if (!(ok = bar_wait(&sm.dp_full, j & 1, gave_up))) break;
             tmem_fence_after();
-            tmem_load32(lanes + 2 * TILE + g * 64, d[0]);
-            tmem_load32(lanes + 2 * TILE + g * 64 + 32, d[1]);
-            tmem_wait_loads();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.dp_taken);
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
-                const float2 x = mul2(pair_of(s[c / 32], c % 32), add2(pair_of(d[c / 32], c % 32), both(-delta)));
-                d[c / 32][c % 32] = __float_as_uint(x.x), d[c / 32][c % 32 + 1] = __float_as_uint(x.y);
+            for (int half = 0; half < 2; ++half) {
+                uint32_t d[2][32], packed[32];
+                tmem_load32(dp_at + half * 64, d[0]);
+                tmem_load32(dp_at + half * 64 + 32, d[1]);
+                tmem_wait_loads();
+                if (half == 1) {
+                    tmem_fence_before();
+                    bar_arrive_warp(&sm.dp_taken);
+                }
+                const bool some = __any_sync(0xFFFFFFFFu, left < (half + 1) * 64);
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    float2 x = mul2(pair_of(s[half * 2 + c / 32], c % 32), add2(pair_of(d[c / 32], c % 32), both(-delta)));
+                    if (some) {
+                        if (half * 64 + c >= left) x.x = 0.0f;
+                        if (half * 64 + c + 1 >= left) x.y = 0.0f;
+                    }
+                    packed[c / 2] = pack_bf16(x);
+                }
+                tmem_store32(s_at + half * 32, packed);
             }
-            if (!whole || (j + 1) * TILE > all_see) {
-                const int left = limit - j * TILE - g * 64;
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c >= left) d[c / 32][c % 32] = 0;
-            }
-            uint32_t packed[32];
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(__uint_as_float(d[c / 32][c % 32]), __uint_as_float(d[c / 32][c % 32 + 1]));
-            tmem_store32(s_at, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive_warp(&sm.ds_ready);
+            bar_arrive_warp(&sm.ds_ready[w]);
         }
         if (n > 0 && ok) ok = bar_wait(&sm.dq_full, 0, gave_up);
         tmem_fence_after();
         __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
 #pragma unroll
         for (int c = 0; c < DH; c += 64) {            // the groups take turns of 32 columns
-            const int c0 = c + g * 32;
+            const int c0 = c + w * 32;
             if (n > 0 && ok) {
                 uint32_t o[32];
                 tmem_load32(lanes + 3 * TILE + c0, o);
@@ -521,16 +562,25 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
 }
 
-// dK and dV: 128 keys to a CTA, which goes over the query tiles of every head that shares them.  All
-// products are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor
-// memory.  Tensor memory: scores (over them P^T) 0, dP^T (over it dS^T) 128, sums of dV 256, of dK 384.
+// dK and dV: 128 keys to a CTA, which goes over the query tiles of every head that shares them.  All products
+// are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor memory.  Heads
+// of up to 64 leave room there for two tiles of scores: the groups of four warps take tiles in turn
+// (TAKE_TURNS), and while one works out probabilities the other works on dP.  With heads of up to 128
+// the sums fill half of tensor memory: both groups work on one tile, 64 queries each, and the next scores
+// are formed while they work on dP, the next dP while they take the exponentials.  (Steps of 64 queries
+// would leave room for turns there too, but a product of fewer than 128 columns takes as long as one of
+// 128: measured 432 us against 301 us for 4096 tokens and 16/4 heads, at a time when neither had been tuned.)
 template <int DH>
 struct DkvSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
-    static constexpr int SLOTS = 2;
-    alignas(1024) uint8_t k[TILE_BYTES], v[TILE_BYTES], q[SLOTS][TILE_BYTES], dout[SLOTS][TILE_BYTES];
-    alignas(16) float stats[SLOTS][2 * TILE];
-    uint64_t kv_full, q_full[SLOTS], q_free[SLOTS], do_full[SLOTS], do_free[SLOTS], s_full, dp_full, p_ready, ds_ready, sums_full, landed;
+    static constexpr bool TAKE_TURNS = DH == 64;
+    // tensor memory: scores (over them P^T), dP^T, sums.  With turns dS^T lies behind P^T, else over dP^T
+    static constexpr uint32_t DP = TAKE_TURNS ? 2 * TILE : TILE, DV = DP + TILE, DK = DV + DH;
+    static_assert(DK + DH <= TMEM_COLUMNS, "tensor memory");
+    static constexpr int Q_SLOTS = TAKE_TURNS ? 3 : 2, DO_SLOTS = 2;
+    alignas(1024) uint8_t k[TILE_BYTES], v[TILE_BYTES], q[Q_SLOTS][TILE_BYTES], dout[DO_SLOTS][TILE_BYTES];
+    alignas(128) uint4 ones_lse[TILE], ones_delta[TILE], terms[Q_SLOTS][TILE], zeros[TILE];      // zeros come last: product_short
+    uint64_t kv_full, q_full[Q_SLOTS], q_free[Q_SLOTS], do_full[DO_SLOTS], do_free[DO_SLOTS], s_full[2], dp_full, p_ready[2], dp_taken, ds_ready[2], sums_full, landed;
     uint32_t tmem, gave_up;
 };
 
@@ -545,19 +595,24 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     const int bh = blockIdx.x % (p.batch * p.heads_kv), key0 = static_cast<int>(blockIdx.x / (p.batch * p.heads_kv)) * TILE;    // early keys are seen most
     const int b = bh / p.heads_kv, h_kv = bh % p.heads_kv, shared = p.heads / p.heads_kv;
     const Seq seq(p, b);
-    const int first_tile = seq.first_query_of(key0) / TILE;
-    const int per_head = key0 < seq.m ? max(0, tiles(seq.n) - first_tile) : 0, n = per_head * shared;
+    const int first = seq.first_query_of(key0) / TILE, per_head = key0 < seq.m ? max(0, tiles(seq.n) - first) : 0, n = per_head * shared;
 
     if (threadIdx.x == 0) {
         bar_init(&sm.kv_full, 1);
         bar_init(&sm.landed, 1);
-        for (int i = 0; i < Smem::SLOTS; ++i)
-            bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1), bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
-        bar_init(&sm.s_full, 1), bar_init(&sm.dp_full, 1), bar_init(&sm.sums_full, 1);
-        bar_init(&sm.p_ready, 8), bar_init(&sm.ds_ready, 8);
+        for (int i = 0; i < Smem::Q_SLOTS; ++i) bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1);
+        for (int i = 0; i < Smem::DO_SLOTS; ++i) bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.ds_ready[w], 4);
+        bar_init(&sm.dp_full, 1), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
         sm.gave_up = 0;
-        fence_async_smem();
     }
+    if (threadIdx.x < TILE) {
+        constexpr uint32_t ONE = 0x3F80;                 // bf16
+        sm.ones_lse[threadIdx.x] = make_uint4(ONE | ONE << 16, ONE, 0, 0);
+        sm.ones_delta[threadIdx.x] = make_uint4(0, ONE << 16, ONE | ONE << 16, 0);
+        sm.zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
+    }
+    fence_async_smem();
     if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
@@ -578,132 +633,153 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             __syncwarp();
             uint32_t landed_phase = 0;
             for (int i = 0; i < n; ++i) {
-                const int slot = i % Smem::SLOTS, h = h_kv * shared + i / per_head, tile = first_tile + i % per_head;
-                const uint32_t free_parity = (i / Smem::SLOTS + 1) & 1;
-                if (!bar_wait(&sm.q_free[slot], free_parity, gave_up)) break;
-                // the statistics arrive at the queries' barrier: their bytes are announced without an arrival
+                const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS, h = h_kv * shared + i / per_head, tile = first + i % per_head;
+                if (!bar_wait(&sm.q_free[qs], (i / Smem::Q_SLOTS + 1) & 1, gave_up)) break;
+                // the terms arrive at the queries' barrier: their bytes are announced without an arrival
                 if (lane == 0) {
-                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&sm.q_full[slot])), "r"(static_cast<uint32_t>(sizeof(sm.stats[0]))) : "memory");
-                    copy_bytes(smem_addr(sm.stats[slot]), p.stats + ((static_cast<int64_t>(b) * p.heads + h) * p.tiles_q + tile) * 2 * TILE, sizeof(sm.stats[0]), &sm.q_full[slot]);
+                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&sm.q_full[qs])), "r"(static_cast<uint32_t>(sizeof(sm.terms[0]))) : "memory");
+                    copy_bytes(smem_addr(sm.terms[qs]), p.stats[(static_cast<int64_t>(b) * p.heads + h) * p.tiles_q + tile].terms, sizeof(sm.terms[0]), &sm.q_full[qs]);
                 }
                 __syncwarp();
-                if (!load_tile<DH, true>(smem_addr(sm.q[slot]), sm.q[slot], &map_q, &sm.q_full[slot], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
-                if (!bar_wait(&sm.do_free[slot], free_parity, gave_up)) break;
-                if (!load_tile<DH, true>(smem_addr(sm.dout[slot]), sm.dout[slot], &map_do, &sm.do_full[slot], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
+                if (!load_tile<DH, true>(smem_addr(sm.q[qs]), sm.q[qs], &map_q, &sm.q_full[qs], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
+                if (!bar_wait(&sm.do_free[ds], (i / Smem::DO_SLOTS + 1) & 1, gave_up)) break;
+                if (!load_tile<DH, true>(smem_addr(sm.dout[ds]), sm.dout[ds], &map_do, &sm.do_full[ds], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
             }
         }
     } else if (warp == WARP_MMA) {
+        const uint32_t tm = uniform(tmem), zeros = uniform(smem_addr(sm.zeros)), k_at = uniform(smem_addr(sm.k)), v_at = uniform(smem_addr(sm.v)), q_at = uniform(smem_addr(sm.q)),
+                       do_at = uniform(smem_addr(sm.dout)), terms_at = uniform(smem_addr(sm.terms)), ones_lse = uniform(smem_addr(sm.ones_lse)), ones_delta = uniform(smem_addr(sm.ones_delta));
+        const int n_all = uniform(n);
         auto scores = [&](int i) {
-            const int slot = i % Smem::SLOTS;
-            if (!bar_wait(&sm.q_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
+            const int qs = i % Smem::Q_SLOTS, w = Smem::TAKE_TURNS ? i & 1 : 0;
+            if (!bar_wait(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;
             if (elected()) {
-                product_rows<DH>(tmem, smem_addr(sm.k), smem_addr(sm.q[slot]));
-                mma_commit(&sm.s_full);
+                product_short<TILE>(tm + w * TILE, ones_lse, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tm + w * TILE, k_at, q_at + qs * Smem::TILE_BYTES, true);
+                mma_commit(&sm.s_full[w]);
             }
             __syncwarp();
             return true;
         };
         auto dprobs = [&](int i) {
-            const int slot = i % Smem::SLOTS;
-            if (!bar_wait(&sm.do_full[slot], i / Smem::SLOTS & 1, gave_up)) return false;
+            const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
+            if (!bar_wait(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) return false;
+            if (Smem::TAKE_TURNS && i > 0 && !bar_wait(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
+            tmem_fence_after();
             if (elected()) {
-                product_rows<DH>(tmem + TILE, smem_addr(sm.v), smem_addr(sm.dout[slot]));
+                product_short<TILE>(tm + Smem::DP, ones_delta, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tm + Smem::DP, v_at, do_at + ds * Smem::TILE_BYTES, true);
                 mma_commit(&sm.dp_full);
             }
             __syncwarp();
             return true;
         };
-        if (n > 0 && bar_wait(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0)) {
-            for (int i = 0; i < n; ++i) {
-                const int slot = i % Smem::SLOTS;
-                if (!bar_wait(&sm.p_ready, i & 1, gave_up)) break;
+        // sums += A B for tile i, A in tensor memory: the whole tile's, or of each group's 64 queries once they are ready
+        auto add_to = [&](uint32_t sums, uint32_t a, uint32_t rows, uint64_t *ready, int i) {
+            if constexpr (Smem::TAKE_TURNS) {
+                if (!bar_wait(&ready[i & 1], i / 2 & 1, gave_up)) return false;
                 tmem_fence_after();
+                if (elected()) product_down<DH, TILE>(sums, a, rows, i > 0);
+            } else {
+                for (int g = 0; g < 2; ++g) {
+                    if (!bar_wait(&ready[g], i & 1, gave_up)) return false;
+                    tmem_fence_after();
+                    if (elected()) product_down<DH, 64>(sums, a + g * 64, rows + g * 64 * 128, i > 0 || g > 0);
+                }
+            }
+            __syncwarp();
+            return true;
+        };
+        if (n_all > 0 && bar_wait(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0) && (!Smem::TAKE_TURNS || n_all == 1 || scores(1))) {
+            for (int i = 0; i < n_all; ++i) {
+                const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
+                const uint32_t probs = tm + (Smem::TAKE_TURNS ? (i & 1) * TILE : 0), dscores = Smem::TAKE_TURNS ? probs + TILE / 2 : tm + Smem::DP;
+                if (!add_to(tm + Smem::DV, probs, do_at + ds * Smem::TILE_BYTES, sm.p_ready, i)) break;
+                if (elected()) mma_commit(&sm.do_free[ds]);
+                if (i + 1 < n_all && !(Smem::TAKE_TURNS ? dprobs(i + 1) : scores(i + 1))) break;
+                if (!add_to(tm + Smem::DK, dscores, q_at + qs * Smem::TILE_BYTES, sm.ds_ready, i)) break;
                 if (elected()) {
-                    product_down<DH>(tmem + 2 * TILE, tmem, smem_addr(sm.dout[slot]), i > 0);
-                    mma_commit(&sm.do_free[slot]);
+                    mma_commit(&sm.q_free[qs]);
+                    if (i == n_all - 1) mma_commit(&sm.sums_full);
                 }
                 __syncwarp();
-                if (i + 1 < n && !scores(i + 1)) break;
-                if (!bar_wait(&sm.ds_ready, i & 1, gave_up)) break;
-                tmem_fence_after();
-                if (elected()) {
-                    product_down<DH>(tmem + 3 * TILE, tmem + TILE, smem_addr(sm.q[slot]), i > 0);
-                    mma_commit(&sm.q_free[slot]);
-                    if (i == n - 1) mma_commit(&sm.sums_full);
-                }
-                __syncwarp();
-                if (i + 1 < n && !dprobs(i + 1)) break;
+                if (Smem::TAKE_TURNS ? i + 2 < n_all && !scores(i + 2) : i + 1 < n_all && !dprobs(i + 1)) break;
             }
         }
     } else if (warp < WARP_MMA) {
         registers_take<REGISTERS_COMPUTE>();
-        const int g = warp / 4, key = key0 + threadIdx.x % TILE;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+        constexpr int WIDTH = Smem::TAKE_TURNS ? TILE : TILE / 2, EVERY = Smem::TAKE_TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
+        const int w = warp / 4, key = key0 + threadIdx.x % TILE, col0 = Smem::TAKE_TURNS ? 0 : w * WIDTH;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + (Smem::TAKE_TURNS ? w * TILE : col0), dp_at = lanes + Smem::DP + col0;
+        const uint32_t ds_at = Smem::TAKE_TURNS ? s_at + TILE / 2 : dp_at;
+        uint64_t *const s_full = &sm.s_full[Smem::TAKE_TURNS ? w : 0];
         bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            const int slot = i % Smem::SLOTS, row0 = (first_tile + i % per_head) * TILE;
-            const float4 *lse = reinterpret_cast<const float4 *>(sm.stats[slot] + g * 64), *delta = reinterpret_cast<const float4 *>(sm.stats[slot] + TILE + g * 64);
-            if (!(ok = bar_wait(&sm.q_full[slot], i / Smem::SLOTS & 1, gave_up) && bar_wait(&sm.s_full, i & 1, gave_up))) break;
+        for (int i = Smem::TAKE_TURNS ? w : 0; i < n; i += EVERY) {
+            const int row0 = (first + i % per_head) * TILE;
+            // columns before `hidden` do not see the key
+            const int hidden = seq.causal && row0 < key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
+            if (!(ok = bar_wait(s_full, i / EVERY & 1, gave_up))) break;
             tmem_fence_after();
-            uint32_t s[2][32], d[2][32], packed[32];
-            tmem_load32(lanes + g * 64, s[0]);
-            tmem_load32(lanes + g * 64 + 32, s[1]);
+            uint32_t s[WIDTH / 32][32];
+#pragma unroll
+            for (int c = 0; c < WIDTH / 32; ++c) tmem_load32(s_at + c * 32, s[c]);
             tmem_wait_loads();
+            const bool some = __any_sync(0xFFFFFFFFu, hidden > 0);
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 l = lse[c / 4];
-                const float at[4] = {l.x, l.y, l.z, l.w};
+            for (int half = 0; half < WIDTH / 64; ++half) {
+                uint32_t packed[32];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) s[c / 32][c % 32 + k] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c / 32][c % 32 + k]), p.scale_log2, -at[k])));
+                for (int c = 0; c < 64; c += 2) {
+                    uint32_t *const at = &s[half * 2 + c / 32][c % 32];
+                    const float2 x = mul2(pair_of(s[half * 2 + c / 32], c % 32), both(p.scale_log2));
+                    float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                    if (some) {
+                        if (half * 64 + c < hidden) e.x = 0.0f;
+                        if (half * 64 + c + 1 < hidden) e.y = 0.0f;
+                    }
+                    at[0] = __float_as_uint(e.x), at[1] = __float_as_uint(e.y);
+                    packed[c / 2] = pack_bf16(e);
+                }
+                tmem_store32(s_at + half * 32, packed);
             }
-            if (seq.causal && row0 < key0 + TILE - 1 - seq.shift) {       // the last key is not seen by the first query
-                const int hidden = key - seq.shift - row0 - g * 64;        // columns before it do not see the key
-#pragma unroll
-                for (int c = 0; c < 64; ++c)
-                    if (c < hidden) s[c / 32][c % 32] = 0;
-            }
-#pragma unroll
-            for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(__uint_as_float(s[c / 32][c % 32]), __uint_as_float(s[c / 32][c % 32 + 1]));
-            tmem_store32(lanes + g * 64, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive_warp(&sm.p_ready);
+            bar_arrive_warp(&sm.p_ready[w]);
             if (!(ok = bar_wait(&sm.dp_full, i & 1, gave_up))) break;
             tmem_fence_after();
-            tmem_load32(lanes + TILE + g * 64, d[0]);
-            tmem_load32(lanes + TILE + g * 64 + 32, d[1]);
-            tmem_wait_loads();
 #pragma unroll
-            for (int c = 0; c < 64; c += 4) {
-                const float4 l = delta[c / 4];
-                const float at[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-                for (int k = 0; k < 4; k += 2) {
-                    const int e = c + k;
-                    packed[e / 2] = pack_bf16(__uint_as_float(s[e / 32][e % 32]) * (__uint_as_float(d[e / 32][e % 32]) - at[k]),
-                                              __uint_as_float(s[e / 32][e % 32 + 1]) * (__uint_as_float(d[e / 32][e % 32 + 1]) - at[k + 1]));
+            for (int half = 0; half < WIDTH / 64; ++half) {
+                uint32_t d[2][32], packed[32];
+                tmem_load32(dp_at + half * 64, d[0]);
+                tmem_load32(dp_at + half * 64 + 32, d[1]);
+                tmem_wait_loads();
+                if (Smem::TAKE_TURNS && half == WIDTH / 64 - 1) {
+                    tmem_fence_before();
+                    bar_arrive_warp(&sm.dp_taken);
                 }
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[half * 2 + c / 32], c % 32), pair_of(d[c / 32], c % 32)));
+                tmem_store32(ds_at + half * 32, packed);
             }
-            tmem_store32(lanes + TILE + g * 64, packed);
             tmem_wait_stores();
             tmem_fence_before();
-            bar_arrive_warp(&sm.ds_ready);
+            bar_arrive_warp(&sm.ds_ready[w]);
         }
         if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
         tmem_fence_after();
         // one group writes dV, the other dK
-        const int64_t *stride = g == 0 ? p.out2_stride : p.out_stride;
-        __nv_bfloat16 *out = (g == 0 ? p.out2 : p.out) + b * stride[0] + key * stride[1] + h_kv * stride[2];
+        const int64_t *stride = w == 0 ? p.out2_stride : p.out_stride;
+        __nv_bfloat16 *out = (w == 0 ? p.out2 : p.out) + b * stride[0] + key * stride[1] + h_kv * stride[2];
 #pragma unroll
         for (int c = 0; c < DH; c += 32) {
             if (n > 0 && ok) {
                 uint32_t o[32];
-                tmem_load32(lanes + (2 + g) * TILE + c, o);
+                tmem_load32(lanes + (w == 0 ? Smem::DV : Smem::DK) + c, o);
                 tmem_wait_loads();
                 if (key >= seq.m)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = 0;
-                if (key < p.len_kv) write_columns(out, c, p.dim, o, g == 0 ? 1.0f : p.scale);
+                if (key < p.len_kv) write_columns(out, c, p.dim, o, w == 0 ? 1.0f : p.scale);
             } else if (key < p.len_kv) {
                 write_zeros(out, c, min(c + 32, p.dim));
             }
@@ -764,7 +840,7 @@ int fill(const kt_attn *a, AttnParams *p) {
     if (a->batch < 0 || a->len_q < 0 || a->len_kv < 0 || a->heads < 1 || a->heads_kv < 1) return fail(KT_ERR_SHAPE, "negative sizes or no heads");
     if (a->heads % a->heads_kv) return fail(KT_ERR_SHAPE, "%d query heads cannot share %d key/value heads", a->heads, a->heads_kv);
     if (a->head_dim < 8 || a->head_dim > KT_ATTN_MAX_DIM || a->head_dim % 8) return fail(KT_ERR_SHAPE, "head_dim %d: a multiple of 8 up to %d expected", a->head_dim, KT_ATTN_MAX_DIM);
-    if (!(a->scale > 0.0f) || !(a->scale < INFINITY)) return fail(KT_ERR_INVALID, "scale must be positive and finite");
+    if (!(a->scale >= 1.0f / (1 << 20)) || !(a->scale <= 1 << 20)) return fail(KT_ERR_INVALID, "scale must be from 2^-20 to 2^20");
     if (a->len_q > (1 << 30) || a->len_kv > (1 << 30)) return fail(KT_ERR_SHAPE, "more than 2^30 tokens");
     *p = AttnParams{};
     p->batch = a->batch, p->heads = a->heads, p->heads_kv = a->heads_kv, p->len_q = a->len_q, p->len_kv = a->len_kv, p->dim = a->head_dim;
@@ -855,7 +931,7 @@ int kt_attn_forward(const kt_attn *a, const void *q, const int64_t *q_stride, co
 
 int64_t kt_attn_workspace(int batch, int heads, int len_q) {
     if (batch < 0 || heads < 0 || len_q < 0) return 0;
-    return static_cast<int64_t>(batch) * heads * ((static_cast<int64_t>(len_q) + TILE - 1) / TILE) * 2 * TILE * static_cast<int64_t>(sizeof(float));
+    return static_cast<int64_t>(batch) * heads * ((static_cast<int64_t>(len_q) + TILE - 1) / TILE) * static_cast<int64_t>(sizeof(QueryStats));
 }
 
 int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_stride, const void *q, const int64_t *q_stride, const void *k,
@@ -894,7 +970,7 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
     if (int rc = make_map(&m[1], "k", k, k_stride, p.batch, p.len_kv, p.heads_kv, p.dim)) return rc;
     if (int rc = make_map(&m[2], "v", v, v_stride, p.batch, p.len_kv, p.heads_kv, p.dim)) return rc;
     if (int rc = make_map(&m[3], "dout", dout, dout_stride, p.batch, p.len_q, p.heads, p.dim)) return rc;
-    p.o = static_cast<const __nv_bfloat16 *>(out), p.dout = static_cast<const __nv_bfloat16 *>(dout), p.lse = const_cast<float *>(lse), p.stats = static_cast<float *>(workspace);
+    p.o = static_cast<const __nv_bfloat16 *>(out), p.dout = static_cast<const __nv_bfloat16 *>(dout), p.lse = const_cast<float *>(lse), p.stats = static_cast<QueryStats *>(workspace);
     copy_strides(p.o_stride, out_stride);
     copy_strides(p.dout_stride, dout_stride);
     k_attn_stats<<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q * (TILE / 16)), 256, 0, st>>>(p);

@@ -154,6 +154,12 @@ constexpr uint64_t OPERAND_ALONG = (1ull << 16) | (static_cast<uint64_t>(1024 >>
 constexpr uint64_t OPERAND_DOWN = (static_cast<uint64_t>(CHUNK >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 __device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | (addr >> 4); }     // shared memory ends below 2^18
 
+// A value that is the same in all lanes of the warp, in a form from which the compiler knows it: what is
+// computed from it then stays in the registers that the matrix instructions take their words from, while
+// each word out of an ordinary register costs a move of its own.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(0xFFFFFFFFu, static_cast<unsigned>(x))); }
+
 // One lane of a warp that is whole; the compiler knows it for one thread and keeps what it issues in
 // uniform registers.
 __device__ __forceinline__ bool elected() {
@@ -178,24 +184,31 @@ __device__ __forceinline__ void mma_commit(uint64_t *bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar)) : "memory");
 }
 
-// D[128 x 128] = A B^T over rows of DH elements: both tiles K-major.
-template <int DH>
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b) {
+// D[128 x N] (+)= A B^T over rows of DH elements: both tiles K-major, N rows of B.
+template <int DH, int N>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b, bool add = false) {
     const uint64_t wa = operand(OPERAND_ALONG, a), wb = operand(OPERAND_ALONG, b);
 #pragma unroll
     for (int k = 0; k < DH / 16; ++k) {
         const uint64_t off = ((k / 4) * CHUNK + (k % 4) * 32) >> 4;
-        mma_smem(d, wa + off, wb + off, mma_word(TILE, false), k > 0);
+        mma_smem(d, wa + off, wb + off, mma_word(N, false), k > 0 ? 1 : static_cast<uint32_t>(add));
     }
 }
-// D[128 x DH] (+)= A B over 128 rows of B: A is bf16 in tensor memory, the first 64 of its reduction
-// index in 32 columns at `a`, the others 64 columns further; B a tile, read down its rows.
-template <int DH>
+// D[128 x DH] (+)= A B over ROWS rows of B: A is bf16 in ROWS / 2 columns of tensor memory, B is read down
+// its rows.
+template <int DH, int ROWS>
 __device__ __forceinline__ void product_down(uint32_t d, uint32_t a, uint32_t b, bool add) {
     const uint64_t wb = operand(OPERAND_DOWN, b);
 #pragma unroll
-    for (int k = 0; k < TILE / 16; ++k)
-        mma_tmem(d, a + (k / 4) * 64 + (k % 4) * 8, wb + ((k * 2048) >> 4), mma_word(DH, true), k > 0 ? 1 : static_cast<uint32_t>(add));
+    for (int k = 0; k < ROWS / 16; ++k)
+        mma_tmem(d, a + k * 8, wb + ((k * 2048) >> 4), mma_word(DH, true), k > 0 ? 1 : static_cast<uint32_t>(add));
+}
+// D[128 x N] = A B^T over 16 elements a row, of which only the first 8 differ from zero.  Rows of 16 bytes lie one
+// after the other; the second 8 elements of all rows are the zeros at `zeros`, past both.
+template <int N>
+__device__ __forceinline__ void product_short(uint32_t d, uint32_t a, uint32_t b, uint32_t zeros) {
+    auto word = [&](uint32_t at) { return (static_cast<uint64_t>((zeros - at) >> 4) << 16) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46) | (at >> 4); };
+    mma_smem(d, word(a), word(b), mma_word(N, false), 0);
 }
 
 __device__ __forceinline__ float2 pair_of(const uint32_t (&r)[32], int i) { return make_float2(__uint_as_float(r[i]), __uint_as_float(r[i + 1])); }
