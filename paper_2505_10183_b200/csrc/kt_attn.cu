@@ -186,47 +186,40 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
         }
     } else if (warp == WARP_MMA) {
-        const uint32_t tm = uniform(tmem), q_at = uniform(smem_addr(sm.q)), kv_at = uniform(smem_addr(sm.kv));
-        const int last_of[2] = {uniform(n_tiles[0]), uniform(n_tiles[1])}, n_all = uniform(n);
-        auto wait_kv = [&](int i) { return bar_wait(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
-        auto scores = [&](int w, int j) {
-            if (elected()) {
-                product_rows<DH, TILE>(tm + w * TILE, q_at + w * FwdSmem<DH>::TILE_BYTES, kv_at + 2 * j % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES);
+        if (elected()) {
+            const uint32_t q_at = smem_addr(sm.q), kv_at = smem_addr(sm.kv);
+            auto wait_kv = [&](int i) { return bar_wait_one(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
+            auto scores = [&](int w, int j) {
+                product_rows<DH, TILE>(tmem + w * TILE, q_at + w * FwdSmem<DH>::TILE_BYTES, kv_at + 2 * j % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES);
                 mma_commit(&sm.s_full[w]);
-            }
-            __syncwarp();
-        };
-        auto free_kv = [&](int i) {
-            if (elected()) mma_commit(&sm.kv_free[i % FWD_SLOTS]);
-            __syncwarp();
-        };
-        if (n_all > 0 && bar_wait(&sm.q_full, 0, gave_up) && wait_kv(0)) {
-            for (int w = 0; w < 2; ++w)
-                if (last_of[w] > 0) scores(w, 0);
-            free_kv(0);
-            for (int j = 0; j < n_all; ++j) {
-                if (!wait_kv(2 * j + 1)) break;
-                bool ok = true;
-                for (int w = 0; w < 2 && ok; ++w) {
-                    if (j >= last_of[w]) continue;
-                    ok = bar_wait(&sm.p_ready[w], j & 1, gave_up);
+            };
+            auto free_kv = [&](int i) { mma_commit(&sm.kv_free[i % FWD_SLOTS]); };
+            if (n > 0 && bar_wait_one(&sm.q_full, 0, gave_up) && wait_kv(0)) {
+                for (int w = 0; w < 2; ++w)
+                    if (n_tiles[w] > 0) scores(w, 0);
+                free_kv(0);
+                for (int j = 0; j < n; ++j) {
+                    if (!wait_kv(2 * j + 1)) break;
+                    bool ok = true;
+                    for (int w = 0; w < 2 && ok; ++w) {
+                        if (j >= n_tiles[w]) continue;
+                        ok = bar_wait_one(&sm.p_ready[w], j & 1, gave_up);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        product_down<DH, TILE>(tmem + 256 + w * DH, tmem + w * TILE, kv_at + (2 * j + 1) % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES, j > 0);
+                        if (j == n_tiles[w] - 1) mma_commit(&sm.o_full[w]);
+                        if (j + 1 < n_tiles[w]) {
+                            ok = wait_kv(2 * j + 2);
+                            if (ok) scores(w, j + 1);
+                        }
+                    }
                     if (!ok) break;
-                    tmem_fence_after();
-                    if (elected()) {
-                        product_down<DH, TILE>(tm + 256 + w * DH, tm + w * TILE, kv_at + (2 * j + 1) % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES, j > 0);
-                        if (j == last_of[w] - 1) mma_commit(&sm.o_full[w]);
-                    }
-                    __syncwarp();
-                    if (j + 1 < last_of[w]) {
-                        ok = wait_kv(2 * j + 2);
-                        if (ok) scores(w, j + 1);
-                    }
+                    free_kv(2 * j + 1);
+                    if (j + 1 < n) free_kv(2 * j + 2);
                 }
-                if (!ok) break;
-                free_kv(2 * j + 1);
-                if (j + 1 < n_all) free_kv(2 * j + 2);
             }
         }
+        __syncwarp();
     } else if (warp < WARP_MMA) {
         registers_take<REGISTERS_COMPUTE>();
         const int w = warp / 4, row = row0 + w * TILE + threadIdx.x % TILE;
@@ -442,45 +435,38 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             }
         }
     } else if (warp == WARP_MMA) {
-        const uint32_t tm = uniform(tmem), q_at = uniform(smem_addr(sm.q)), do_at = uniform(smem_addr(sm.dout)), k_at = uniform(smem_addr(sm.k)), v_at = uniform(smem_addr(sm.v));
-        const int n_all = uniform(n);
-        auto scores = [&](int j) {
-            const int ks = j % Smem::K_SLOTS;
-            if (!bar_wait(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
-            if (elected()) {
-                product_rows<DH, TILE>(tm + (j & 1) * TILE, q_at, k_at + ks * Smem::TILE_BYTES);
+        if (elected()) {
+            const uint32_t q_at = smem_addr(sm.q), do_at = smem_addr(sm.dout), k_at = smem_addr(sm.k), v_at = smem_addr(sm.v);
+            auto scores = [&](int j) {
+                const int ks = j % Smem::K_SLOTS;
+                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
+                product_rows<DH, TILE>(tmem + (j & 1) * TILE, q_at, k_at + ks * Smem::TILE_BYTES);
                 mma_commit(&sm.s_full[j & 1]);
-            }
-            __syncwarp();
-            return true;
-        };
-        auto dprobs = [&](int j) {
-            const int vs = j % Smem::V_SLOTS;
-            if (!bar_wait(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) return false;
-            if (j > 0 && !bar_wait(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
-            tmem_fence_after();
-            if (elected()) {
-                product_rows<DH, TILE>(tm + 2 * TILE, do_at, v_at + vs * Smem::TILE_BYTES);
+                return true;
+            };
+            auto dprobs = [&](int j) {
+                const int vs = j % Smem::V_SLOTS;
+                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) return false;
+                if (j > 0 && !bar_wait_one(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
+                tmem_fence_after();
+                product_rows<DH, TILE>(tmem + 2 * TILE, do_at, v_at + vs * Smem::TILE_BYTES);
                 mma_commit(&sm.dp_full);
                 mma_commit(&sm.v_free[vs]);
-            }
-            __syncwarp();
-            return true;
-        };
-        if (n_all > 0 && bar_wait(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0) && (n_all == 1 || scores(1))) {
-            for (int j = 0; j < n_all; ++j) {
-                if (j + 1 < n_all && !dprobs(j + 1)) break;
-                if (!bar_wait(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
-                tmem_fence_after();
-                if (elected()) {
-                    product_down<DH, TILE>(tm + 3 * TILE, tm + (j & 1) * TILE, k_at + j % Smem::K_SLOTS * Smem::TILE_BYTES, j > 0);
+                return true;
+            };
+            if (n > 0 && bar_wait_one(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0) && (n == 1 || scores(1))) {
+                for (int j = 0; j < n; ++j) {
+                    if (j + 1 < n && !dprobs(j + 1)) break;
+                    if (!bar_wait_one(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
+                    tmem_fence_after();
+                    product_down<DH, TILE>(tmem + 3 * TILE, tmem + (j & 1) * TILE, k_at + j % Smem::K_SLOTS * Smem::TILE_BYTES, j > 0);
                     mma_commit(&sm.k_free[j % Smem::K_SLOTS]);
-                    if (j == n_all - 1) mma_commit(&sm.dq_full);
+                    if (j == n - 1) mma_commit(&sm.dq_full);
+                    if (j + 2 < n && !scores(j + 2)) break;
                 }
-                __syncwarp();
-                if (j + 2 < n_all && !scores(j + 2)) break;
             }
         }
+        __syncwarp();
     } else if (warp < WARP_MMA) {
         registers_take<REGISTERS_COMPUTE>();
         const int w = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
@@ -647,65 +633,57 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             }
         }
     } else if (warp == WARP_MMA) {
-        const uint32_t tm = uniform(tmem), zeros = uniform(smem_addr(sm.zeros)), k_at = uniform(smem_addr(sm.k)), v_at = uniform(smem_addr(sm.v)), q_at = uniform(smem_addr(sm.q)),
-                       do_at = uniform(smem_addr(sm.dout)), terms_at = uniform(smem_addr(sm.terms)), ones_lse = uniform(smem_addr(sm.ones_lse)), ones_delta = uniform(smem_addr(sm.ones_delta));
-        const int n_all = uniform(n);
-        auto scores = [&](int i) {
-            const int qs = i % Smem::Q_SLOTS, w = Smem::TAKE_TURNS ? i & 1 : 0;
-            if (!bar_wait(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;
-            if (elected()) {
-                product_short<TILE>(tm + w * TILE, ones_lse, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tm + w * TILE, k_at, q_at + qs * Smem::TILE_BYTES, true);
+        if (elected()) {
+            const uint32_t zeros = smem_addr(sm.zeros), k_at = smem_addr(sm.k), v_at = smem_addr(sm.v), q_at = smem_addr(sm.q),
+                           do_at = smem_addr(sm.dout), terms_at = smem_addr(sm.terms), ones_lse = smem_addr(sm.ones_lse), ones_delta = smem_addr(sm.ones_delta);
+            auto scores = [&](int i) {
+                const int qs = i % Smem::Q_SLOTS, w = Smem::TAKE_TURNS ? i & 1 : 0;
+                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;
+                product_short<TILE>(tmem + w * TILE, ones_lse, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tmem + w * TILE, k_at, q_at + qs * Smem::TILE_BYTES, true);
                 mma_commit(&sm.s_full[w]);
-            }
-            __syncwarp();
-            return true;
-        };
-        auto dprobs = [&](int i) {
-            const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
-            if (!bar_wait(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) return false;
-            if (Smem::TAKE_TURNS && i > 0 && !bar_wait(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
-            tmem_fence_after();
-            if (elected()) {
-                product_short<TILE>(tm + Smem::DP, ones_delta, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tm + Smem::DP, v_at, do_at + ds * Smem::TILE_BYTES, true);
-                mma_commit(&sm.dp_full);
-            }
-            __syncwarp();
-            return true;
-        };
-        // sums += A B for tile i, A in tensor memory: the whole tile's, or of each group's 64 queries once they are ready
-        auto add_to = [&](uint32_t sums, uint32_t a, uint32_t rows, uint64_t *ready, int i) {
-            if constexpr (Smem::TAKE_TURNS) {
-                if (!bar_wait(&ready[i & 1], i / 2 & 1, gave_up)) return false;
-                tmem_fence_after();
-                if (elected()) product_down<DH, TILE>(sums, a, rows, i > 0);
-            } else {
-                for (int g = 0; g < 2; ++g) {
-                    if (!bar_wait(&ready[g], i & 1, gave_up)) return false;
-                    tmem_fence_after();
-                    if (elected()) product_down<DH, 64>(sums, a + g * 64, rows + g * 64 * 128, i > 0 || g > 0);
-                }
-            }
-            __syncwarp();
-            return true;
-        };
-        if (n_all > 0 && bar_wait(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0) && (!Smem::TAKE_TURNS || n_all == 1 || scores(1))) {
-            for (int i = 0; i < n_all; ++i) {
+                return true;
+            };
+            auto dprobs = [&](int i) {
                 const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
-                const uint32_t probs = tm + (Smem::TAKE_TURNS ? (i & 1) * TILE : 0), dscores = Smem::TAKE_TURNS ? probs + TILE / 2 : tm + Smem::DP;
-                if (!add_to(tm + Smem::DV, probs, do_at + ds * Smem::TILE_BYTES, sm.p_ready, i)) break;
-                if (elected()) mma_commit(&sm.do_free[ds]);
-                if (i + 1 < n_all && !(Smem::TAKE_TURNS ? dprobs(i + 1) : scores(i + 1))) break;
-                if (!add_to(tm + Smem::DK, dscores, q_at + qs * Smem::TILE_BYTES, sm.ds_ready, i)) break;
-                if (elected()) {
-                    mma_commit(&sm.q_free[qs]);
-                    if (i == n_all - 1) mma_commit(&sm.sums_full);
+                if (!bar_wait_one(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) return false;
+                if (Smem::TAKE_TURNS && i > 0 && !bar_wait_one(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
+                tmem_fence_after();
+                product_short<TILE>(tmem + Smem::DP, ones_delta, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tmem + Smem::DP, v_at, do_at + ds * Smem::TILE_BYTES, true);
+                mma_commit(&sm.dp_full);
+                return true;
+            };
+            // sums += A B for tile i, A in tensor memory: the whole tile's, or of each group's 64 queries once they are ready
+            auto add_to = [&](uint32_t sums, uint32_t a, uint32_t rows, uint64_t *ready, int i) {
+                if constexpr (Smem::TAKE_TURNS) {
+                    if (!bar_wait_one(&ready[i & 1], i / 2 & 1, gave_up)) return false;
+                    tmem_fence_after();
+                    product_down<DH, TILE>(sums, a, rows, i > 0);
+                } else {
+                    for (int g = 0; g < 2; ++g) {
+                        if (!bar_wait_one(&ready[g], i & 1, gave_up)) return false;
+                        tmem_fence_after();
+                        product_down<DH, 64>(sums, a + g * 64, rows + g * 64 * 128, i > 0 || g > 0);
+                    }
                 }
-                __syncwarp();
-                if (Smem::TAKE_TURNS ? i + 2 < n_all && !scores(i + 2) : i + 1 < n_all && !dprobs(i + 1)) break;
+                return true;
+            };
+            if (n > 0 && bar_wait_one(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0) && (!Smem::TAKE_TURNS || n == 1 || scores(1))) {
+                for (int i = 0; i < n; ++i) {
+                    const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
+                    const uint32_t probs = tmem + (Smem::TAKE_TURNS ? (i & 1) * TILE : 0), dscores = Smem::TAKE_TURNS ? probs + TILE / 2 : tmem + Smem::DP;
+                    if (!add_to(tmem + Smem::DV, probs, do_at + ds * Smem::TILE_BYTES, sm.p_ready, i)) break;
+                    mma_commit(&sm.do_free[ds]);
+                    if (i + 1 < n && !(Smem::TAKE_TURNS ? dprobs(i + 1) : scores(i + 1))) break;
+                    if (!add_to(tmem + Smem::DK, dscores, q_at + qs * Smem::TILE_BYTES, sm.ds_ready, i)) break;
+                    mma_commit(&sm.q_free[qs]);
+                    if (i == n - 1) mma_commit(&sm.sums_full);
+                    if (Smem::TAKE_TURNS ? i + 2 < n && !scores(i + 2) : i + 1 < n && !dprobs(i + 1)) break;
+                }
             }
         }
+        __syncwarp();
     } else if (warp < WARP_MMA) {
         registers_take<REGISTERS_COMPUTE>();
         constexpr int WIDTH = Smem::TAKE_TURNS ? TILE : TILE / 2, EVERY = Smem::TAKE_TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile

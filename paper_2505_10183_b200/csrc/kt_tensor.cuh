@@ -55,8 +55,8 @@ __device__ __forceinline__ uint64_t now_ns() {
     return t;
 }
 
-// Waits for the phase of that parity to end; called by whole warps.  False when it gave up, or when
-// another warp of the CTA did: the caller then leaves its loop, and the kernel ends.
+// Waits for the phase of that parity to end.  False when it gave up, or when another warp of the CTA did: the
+// caller then leaves its loop, and the kernel ends.  Called by one thread, or (bar_wait) by whole warps.
 __device__ __forceinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
     const uint64_t start = now_ns();
     for (uint32_t n = 1;; ++n) {
@@ -70,6 +70,9 @@ __device__ __forceinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, vo
             }
         }
     }
+}
+__device__ __forceinline__ bool bar_wait_one(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
+    return bar_try(bar, parity) || bar_wait_slow(bar, parity, gave_up);
 }
 __device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
     bool ok = bar_try(bar, parity);
@@ -154,14 +157,7 @@ constexpr uint64_t OPERAND_ALONG = (1ull << 16) | (static_cast<uint64_t>(1024 >>
 constexpr uint64_t OPERAND_DOWN = (static_cast<uint64_t>(CHUNK >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 __device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | (addr >> 4); }     // shared memory ends below 2^18
 
-// A value that is the same in all lanes of the warp, in a form from which the compiler knows it: what is
-// computed from it then stays in the registers that the matrix instructions take their words from, while
-// each word out of an ordinary register costs a move of its own.
-__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xFFFFFFFFu, x); }
-__device__ __forceinline__ int uniform(int x) { return static_cast<int>(__reduce_or_sync(0xFFFFFFFFu, static_cast<unsigned>(x))); }
-
-// One lane of a warp that is whole; the compiler knows it for one thread and keeps what it issues in
-// uniform registers.
+// One lane of a warp that is whole.
 __device__ __forceinline__ bool elected() {
     uint32_t is;
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
