@@ -30,7 +30,11 @@ using namespace ktd;
 namespace {
 
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int WARP_MMA = 8, WARP_LOAD = 9, THREADS = 384;      // warps 10 and 11 only fill their group
+// The third group of warps: one brings tiles, the others issue products, each its own kind.  What a thread issues
+// after a product waits until that has all but run (measured: some 500 cycles for 8 instructions of 64), so
+// a thread that then waited for a barrier would leave the tensor cores idle meanwhile; another has queued its
+// product by then.
+constexpr int WARP_SCORES = 8, WARP_LOAD = 9, WARP_DP = 10, WARP_SUMS = 11, THREADS = 384;
 // Registers: a block of 384 threads starts with 168 each, 64512 in all; the third group gives back what the
 // eight warps that compute take: 256 x 208 + 128 x 88 = 64512.
 constexpr int REGISTERS_COMPUTE = 208, REGISTERS_HELP = 88;
@@ -119,17 +123,17 @@ __device__ __forceinline__ void settle(volatile uint32_t *gave_up) {
 }
 
 // ------------------------------------------------------------------------------------ forward
-// Two tiles of 128 queries to a CTA, four warps on each: while one group takes the exponentials of its
-// scores, the tensor cores work for the other.  A thread owns a row: maximum and sum need no exchange.
-// Tensor memory: scores (and over them the probabilities) 0 and 128, sums 256 and 256 + DH.
-constexpr int FWD_SLOTS = 4;                    // K and V tiles in flight
-
+// Two tiles of 128 queries to a CTA, four warps on each.  A thread owns a row: maximum and sum need no
+// exchange.  A group takes its scores into registers at once, and their place in tensor memory is free for
+// the other group's next ones: scores are formed up to three steps ahead, and neither a group nor the tensor
+// cores wait for the other in turn.  Tensor memory: scores 0, probabilities 128 and 192, sums 256 and 256 + DH.
 template <int DH>
 struct FwdSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
     alignas(1024) uint8_t q[2][TILE_BYTES];
-    alignas(1024) uint8_t kv[FWD_SLOTS][TILE_BYTES];
-    uint64_t q_full, kv_full[FWD_SLOTS], kv_free[FWD_SLOTS], s_full[2], p_ready[2], o_full[2], landed;
+    static constexpr int K_SLOTS = 3, V_SLOTS = 2;
+    alignas(1024) uint8_t k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
+    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, p_ready[2], o_done[2], landed;
     uint32_t tmem, gave_up;
 };
 
@@ -138,7 +142,8 @@ __global__ void __launch_bounds__(THREADS, 1)
 k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                const AttnParams p) {
     extern __shared__ uint8_t raw[];
-    auto &sm = *reinterpret_cast<FwdSmem<DH> *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    using Smem = FwdSmem<DH>;
+    auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int pairs = (p.tiles_q + 1) / 2, bh = blockIdx.x % (p.batch * p.heads);
     const int row0 = (pairs - 1 - static_cast<int>(blockIdx.x / (p.batch * p.heads))) * 2 * TILE;      // the longest rows first
@@ -151,79 +156,82 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         n_tiles[w] = first < seq.n ? tiles(seq.keys_of(min(first + TILE, seq.n) - 1)) : 0;
     }
     const int n = max(n_tiles[0], n_tiles[1]);
+    // Steps: the tiles' groups in turn while both have keys left, then the one that has more.
+    const int common = min(n_tiles[0], n_tiles[1]), longer = n_tiles[1] > n_tiles[0] ? 1 : 0, steps = n_tiles[0] + n_tiles[1];
 
     if (threadIdx.x == 0) {
         bar_init(&sm.q_full, 1);
         bar_init(&sm.landed, 1);
-        for (int i = 0; i < FWD_SLOTS; ++i) bar_init(&sm.kv_full[i], 1), bar_init(&sm.kv_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_full[w], 1);
+        for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
+        for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_done[w], 1);
+        bar_init(&sm.s_taken, 4);
         sm.gave_up = 0;
         fence_async_smem();
     }
-    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
-    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
+    if (warp >= 8) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
-                bar_expect(&sm.q_full, 2 * FwdSmem<DH>::TILE_BYTES);
+                bar_expect(&sm.q_full, 2 * Smem::TILE_BYTES);
                 for (int w = 0; w < 2; ++w)
                     for (int c = 0; c < DH / 64; ++c) copy_tile(smem_addr(sm.q[w]) + c * CHUNK, &map_q, &sm.q_full, c * 64, row0 + w * TILE, h, b);
             }
             __syncwarp();
             uint32_t landed_phase = 0;
-            for (int i = 0; i < 2 * n; ++i) {
-                const int slot = i % FWD_SLOTS;
-                if (!bar_wait(&sm.kv_free[slot], (i / FWD_SLOTS + 1) & 1, gave_up)) break;
-                const bool ok = i % 2 == 0 ? load_tile<DH, false>(smem_addr(sm.kv[slot]), sm.kv[slot], &map_k, &sm.kv_full[slot], &sm.landed, landed_phase, i / 2 * TILE, seq.m, p.len_kv, h_kv, b, gave_up)
-                                           : load_tile<DH, true>(smem_addr(sm.kv[slot]), sm.kv[slot], &map_v, &sm.kv_full[slot], &sm.landed, landed_phase, i / 2 * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
-                if (!ok) break;
-            }
-        }
-    } else if (warp == WARP_MMA) {
-        if (elected()) {
-            const uint32_t q_at = smem_addr(sm.q), kv_at = smem_addr(sm.kv);
-            auto wait_kv = [&](int i) { return bar_wait_one(&sm.kv_full[i % FWD_SLOTS], i / FWD_SLOTS & 1, gave_up); };
-            auto scores = [&](int w, int j) {
-                product_rows<DH, TILE>(tmem + w * TILE, q_at + w * FwdSmem<DH>::TILE_BYTES, kv_at + 2 * j % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES);
-                mma_commit(&sm.s_full[w]);
-            };
-            auto free_kv = [&](int i) { mma_commit(&sm.kv_free[i % FWD_SLOTS]); };
-            if (n > 0 && bar_wait_one(&sm.q_full, 0, gave_up) && wait_kv(0)) {
-                for (int w = 0; w < 2; ++w)
-                    if (n_tiles[w] > 0) scores(w, 0);
-                free_kv(0);
-                for (int j = 0; j < n; ++j) {
-                    if (!wait_kv(2 * j + 1)) break;
-                    bool ok = true;
-                    for (int w = 0; w < 2 && ok; ++w) {
-                        if (j >= n_tiles[w]) continue;
-                        ok = bar_wait_one(&sm.p_ready[w], j & 1, gave_up);
-                        if (!ok) break;
-                        tmem_fence_after();
-                        product_down<DH, TILE>(tmem + 256 + w * DH, tmem + w * TILE, kv_at + (2 * j + 1) % FWD_SLOTS * FwdSmem<DH>::TILE_BYTES, j > 0);
-                        if (j == n_tiles[w] - 1) mma_commit(&sm.o_full[w]);
-                        if (j + 1 < n_tiles[w]) {
-                            ok = wait_kv(2 * j + 2);
-                            if (ok) scores(w, j + 1);
-                        }
-                    }
-                    if (!ok) break;
-                    free_kv(2 * j + 1);
-                    if (j + 1 < n) free_kv(2 * j + 2);
+            for (int j = 0; j <= n; ++j) {              // keys a tile ahead of values
+                if (j < n) {
+                    const int ks = j % Smem::K_SLOTS;
+                    if (!bar_wait(&sm.k_free[ks], (j / Smem::K_SLOTS + 1) & 1, gave_up)) break;
+                    load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
+                }
+                if (j > 0) {
+                    const int vs = (j - 1) % Smem::V_SLOTS;
+                    if (!bar_wait(&sm.v_free[vs], ((j - 1) / Smem::V_SLOTS + 1) & 1, gave_up)) break;
+                    if (!load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (j - 1) * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
                 }
             }
         }
+    } else if (warp == WARP_SCORES) {
+        if (elected()) {
+            const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
+            for (int u = 0; u < steps; ++u) {
+                const int j = u < 2 * common ? u / 2 : u - common, w = u < 2 * common ? u & 1 : longer, ks = j % Smem::K_SLOTS;
+                if (u == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
+                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
+                if (u > 0 && !bar_wait_one(&sm.s_taken, (u - 1) & 1, gave_up)) break;
+                tmem_fence_after();
+                product_rows<DH, TILE>(tmem, q_at + w * Smem::TILE_BYTES, k_at + ks * Smem::TILE_BYTES);
+                mma_commit(&sm.s_full[w]);
+                if (w == 1 || j >= n_tiles[1]) mma_commit(&sm.k_free[ks]);
+            }
+        }
         __syncwarp();
-    } else if (warp < WARP_MMA) {
+    } else if (warp == WARP_SUMS) {
+        if (elected()) {
+            const uint32_t v_at = smem_addr(sm.v);
+            for (int u = 0; u < steps; ++u) {
+                const int j = u < 2 * common ? u / 2 : u - common, w = u < 2 * common ? u & 1 : longer, vs = j % Smem::V_SLOTS;
+                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) break;
+                if (!bar_wait_one(&sm.p_ready[w], j & 1, gave_up)) break;
+                tmem_fence_after();
+                product_down<DH, TILE>(tmem + 256 + w * DH, tmem + TILE + w * 64, v_at + vs * Smem::TILE_BYTES, j > 0);
+                mma_commit(&sm.o_done[w]);
+                if (w == 1 || j >= n_tiles[1]) mma_commit(&sm.v_free[vs]);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 8) {
         registers_take<REGISTERS_COMPUTE>();
         const int w = warp / 4, row = row0 + w * TILE + threadIdx.x % TILE;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + w * TILE, o_at = lanes + 256 + w * DH;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, p_at = lanes + TILE + w * 64, o_at = lanes + 256 + w * DH;
         const int limit = seq.keys_of(row), all_see = seq.keys_of(row0 + w * TILE);    // the tile's first row sees least
         const bool whole = row0 + w * TILE + TILE <= seq.n;
         float top = -INFINITY, sum = 0.0f;      // in units of log 2, after scaling
@@ -241,7 +249,11 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             tmem_load32(s_at + 96, s[3]);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                if (half == 1) tmem_wait_loads();
+                if (half == 1) {
+                    tmem_wait_loads();
+                    tmem_fence_before();
+                    bar_arrive_warp(&sm.s_taken);
+                }
                 if (__any_sync(0xFFFFFFFFu, left < (half + 1) * 64)) {
 #pragma unroll
                     for (int c = half * 64; c < half * 64 + 64; ++c)
@@ -259,6 +271,8 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (grow) top = here;
                 sum *= by;
                 if (j > 0) {
+                    if (!(ok = bar_wait(&sm.o_done[w], (j - 1) & 1, gave_up))) break;
+                    tmem_fence_after();
 #pragma unroll
                     for (int c = 0; c < DH; c += 32) {
                         uint32_t o[32];
@@ -272,25 +286,30 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             const float ref = top == -INFINITY ? 0.0f : top;
             float2 part[2] = {both(0.0f), both(0.0f)};
+            uint32_t packed[2][32];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                uint32_t packed[32];
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) {
                     const float2 x = fma2(pair_of(s[half * 2 + c / 32], c % 32), both(p.scale_log2), both(-ref));
                     const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
                     part[c / 2 % 2] = add2(part[c / 2 % 2], e);
-                    packed[c / 2] = pack_bf16(e);
+                    packed[half][c / 2] = pack_bf16(e);
                 }
-                tmem_store32(s_at + half * 32, packed);
             }
+            if (j > 0) {                        // the last probabilities have been used
+                if (!(ok = bar_wait(&sm.o_done[w], (j - 1) & 1, gave_up))) break;
+                tmem_fence_after();
+            }
+            tmem_store32(p_at, packed[0]);
+            tmem_store32(p_at + 32, packed[1]);
             sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
             tmem_wait_stores();
             tmem_fence_before();
             bar_arrive_warp(&sm.p_ready[w]);
         }
         const bool any = n_tiles[w] > 0;
-        if (any && ok) ok = bar_wait(&sm.o_full[w], 0, gave_up);
+        if (any && ok) ok = bar_wait(&sm.o_done[w], (n_tiles[w] - 1) & 1, gave_up);
         tmem_fence_after();
         const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
         __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
@@ -313,7 +332,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     tmem_fence_before();
     __syncthreads();
     settle(gave_up);
-    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
 }
 
 // ----------------------------------------------------------------------------------- backward
@@ -372,15 +391,15 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
     }
 }
 
-// dQ: 128 queries to a CTA, the two groups of four warps take its key tiles in turn.  While one takes the
-// exponentials of its scores the other, with its probabilities done, works on dP.  Tensor memory: scores
-// (over them dS) 0 and 128, dP 256, sums 384.
+// dQ: 128 queries to a CTA, the two groups of four warps take its key tiles in turn.  Scores and dP are taken
+// into registers as soon as they are there, which frees their place for the next tile's.  Tensor memory:
+// scores 0, dP 128, dS 256 and 320, sums 384.
 template <int DH>
 struct DqSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
     static constexpr int K_SLOTS = 3, V_SLOTS = 2;
     alignas(1024) uint8_t q[TILE_BYTES], dout[TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
-    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], dp_full, dp_taken, ds_ready[2], dq_full, landed;
+    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, dp_full[2], dp_taken, ds_ready[2], dq_done[2], sums_full, landed;
     uint32_t tmem, gave_up;
 };
 
@@ -402,19 +421,19 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
         bar_init(&sm.landed, 1);
         for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
         for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.ds_ready[w], 4);
-        bar_init(&sm.dp_full, 1), bar_init(&sm.dp_taken, 4), bar_init(&sm.dq_full, 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.dp_full[w], 1), bar_init(&sm.dq_done[w], 1), bar_init(&sm.ds_ready[w], 4);
+        bar_init(&sm.s_taken, 4), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
         sm.gave_up = 0;
         fence_async_smem();
     }
-    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
-    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
+    if (warp >= 8) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
@@ -434,43 +453,54 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 load_tile<DH, false>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
             }
         }
-    } else if (warp == WARP_MMA) {
+    } else if (warp == WARP_SCORES) {
         if (elected()) {
-            const uint32_t q_at = smem_addr(sm.q), do_at = smem_addr(sm.dout), k_at = smem_addr(sm.k), v_at = smem_addr(sm.v);
-            auto scores = [&](int j) {
+            const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
+            for (int j = 0; j < n; ++j) {
                 const int ks = j % Smem::K_SLOTS;
-                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) return false;
-                product_rows<DH, TILE>(tmem + (j & 1) * TILE, q_at, k_at + ks * Smem::TILE_BYTES);
-                mma_commit(&sm.s_full[j & 1]);
-                return true;
-            };
-            auto dprobs = [&](int j) {
-                const int vs = j % Smem::V_SLOTS;
-                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) return false;
-                if (j > 0 && !bar_wait_one(&sm.dp_taken, (j - 1) & 1, gave_up)) return false;
+                if (j == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
+                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
+                if (j > 0 && !bar_wait_one(&sm.s_taken, (j - 1) & 1, gave_up)) break;
                 tmem_fence_after();
-                product_rows<DH, TILE>(tmem + 2 * TILE, do_at, v_at + vs * Smem::TILE_BYTES);
-                mma_commit(&sm.dp_full);
-                mma_commit(&sm.v_free[vs]);
-                return true;
-            };
-            if (n > 0 && bar_wait_one(&sm.q_full, 0, gave_up) && scores(0) && dprobs(0) && (n == 1 || scores(1))) {
-                for (int j = 0; j < n; ++j) {
-                    if (j + 1 < n && !dprobs(j + 1)) break;
-                    if (!bar_wait_one(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
-                    tmem_fence_after();
-                    product_down<DH, TILE>(tmem + 3 * TILE, tmem + (j & 1) * TILE, k_at + j % Smem::K_SLOTS * Smem::TILE_BYTES, j > 0);
-                    mma_commit(&sm.k_free[j % Smem::K_SLOTS]);
-                    if (j == n - 1) mma_commit(&sm.dq_full);
-                    if (j + 2 < n && !scores(j + 2)) break;
-                }
+                product_rows<DH, TILE>(tmem, q_at, k_at + ks * Smem::TILE_BYTES);
+                mma_commit(&sm.s_full[j & 1]);
             }
         }
         __syncwarp();
-    } else if (warp < WARP_MMA) {
+    } else if (warp == WARP_DP) {
+        if (elected()) {
+            const uint32_t do_at = smem_addr(sm.dout), v_at = smem_addr(sm.v);
+            for (int j = 0; j < n; ++j) {
+                const int vs = j % Smem::V_SLOTS;
+                if (j == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
+                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) break;
+                if (j > 0 && !bar_wait_one(&sm.dp_taken, (j - 1) & 1, gave_up)) break;
+                tmem_fence_after();
+                product_rows<DH, TILE>(tmem + TILE, do_at, v_at + vs * Smem::TILE_BYTES);
+                mma_commit(&sm.dp_full[j & 1]);
+                mma_commit(&sm.v_free[vs]);
+            }
+        }
+        __syncwarp();
+    } else if (warp == WARP_SUMS) {
+        if (elected()) {
+            const uint32_t k_at = smem_addr(sm.k);
+            for (int j = 0; j < n; ++j) {
+                const int ks = j % Smem::K_SLOTS;
+                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
+                if (!bar_wait_one(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
+                tmem_fence_after();
+                product_down<DH, TILE>(tmem + 3 * TILE, tmem + 2 * TILE + (j & 1) * 64, k_at + ks * Smem::TILE_BYTES, j > 0);
+                mma_commit(&sm.dq_done[j & 1]);
+                mma_commit(&sm.k_free[ks]);                // dS came from the scores: that product is done as well
+                if (j == n - 1) mma_commit(&sm.sums_full);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 8) {
         registers_take<REGISTERS_COMPUTE>();
         const int w = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + w * TILE, dp_at = lanes + 2 * TILE;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, dp_at = lanes + TILE, ds_at = lanes + 2 * TILE + w * 64;
         const int limit = seq.keys_of(row), all_see = seq.keys_of(row0);
         const bool whole = row0 + TILE <= seq.n;
         const QueryStats &stats = p.stats[static_cast<int64_t>(bh) * p.tiles_q + tile];
@@ -487,7 +517,11 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             tmem_load32(s_at + 96, s[3]);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-                if (half == 1) tmem_wait_loads();
+                if (half == 1) {
+                    tmem_wait_loads();
+                    tmem_fence_before();
+                    bar_arrive_warp(&sm.s_taken);
+                }
 #pragma unroll
                 for (int c = half * 64; c < half * 64 + 64; c += 2) {
                     const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
@@ -495,35 +529,41 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 }
             }
             const int left = !whole || (j + 1) * TILE > all_see ? limit - j * TILE : TILE;     // columns that the row sees
-            if (!(ok = bar_wait(&sm.dp_full, j & 1, gave_up))) break;
+            if (!(ok = bar_wait(&sm.dp_full[w], j / 2 & 1, gave_up))) break;
             tmem_fence_after();
+            uint32_t d[2][32], packed[4][16];
+            tmem_load32(dp_at, d[0]);
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t d[2][32], packed[32];
-                tmem_load32(dp_at + half * 64, d[0]);
-                tmem_load32(dp_at + half * 64 + 32, d[1]);
+            for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
                 tmem_wait_loads();
-                if (half == 1) {
+                if (q < 3) {
+                    tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
+                } else {
                     tmem_fence_before();
                     bar_arrive_warp(&sm.dp_taken);
                 }
-                const bool some = __any_sync(0xFFFFFFFFu, left < (half + 1) * 64);
+                const bool some = __any_sync(0xFFFFFFFFu, left < (q + 1) * 32);
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    float2 x = mul2(pair_of(s[half * 2 + c / 32], c % 32), add2(pair_of(d[c / 32], c % 32), both(-delta)));
+                for (int c = 0; c < 32; c += 2) {
+                    float2 x = mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta)));
                     if (some) {
-                        if (half * 64 + c >= left) x.x = 0.0f;
-                        if (half * 64 + c + 1 >= left) x.y = 0.0f;
+                        if (q * 32 + c >= left) x.x = 0.0f;
+                        if (q * 32 + c + 1 >= left) x.y = 0.0f;
                     }
-                    packed[c / 2] = pack_bf16(x);
+                    packed[q][c / 2] = pack_bf16(x);
                 }
-                tmem_store32(s_at + half * 32, packed);
             }
+            if (j > 1) {                         // its last dS has been used
+                if (!(ok = bar_wait(&sm.dq_done[w], (j / 2 - 1) & 1, gave_up))) break;
+                tmem_fence_after();
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
             tmem_wait_stores();
             tmem_fence_before();
             bar_arrive_warp(&sm.ds_ready[w]);
         }
-        if (n > 0 && ok) ok = bar_wait(&sm.dq_full, 0, gave_up);
+        if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
         tmem_fence_after();
         __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
 #pragma unroll
@@ -545,28 +585,28 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
     tmem_fence_before();
     __syncthreads();
     settle(gave_up);
-    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
 }
 
 // dK and dV: 128 keys to a CTA, which goes over the query tiles of every head that shares them.  All products
-// are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor memory.  Heads
-// of up to 64 leave room there for two tiles of scores: the groups of four warps take tiles in turn
-// (TAKE_TURNS), and while one works out probabilities the other works on dP.  With heads of up to 128
-// the sums fill half of tensor memory: both groups work on one tile, 64 queries each, and the next scores
-// are formed while they work on dP, the next dP while they take the exponentials.  (Steps of 64 queries
-// would leave room for turns there too, but a product of fewer than 128 columns takes as long as one of
-// 128: measured 432 us against 301 us for 4096 tokens and 16/4 heads, at a time when neither had been tuned.)
+// are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor memory.  Scores
+// and dP are taken into registers as soon as they are there.
+//   Heads of up to 64: the groups of four warps take tiles in turn.  Tensor memory: scores 0, dP 128, a
+//   place of each group for P and then, once that is used, dS 256 and 320, sums 384 and 448.
+//   Heads of up to 128, whose sums fill half of tensor memory: both groups work on one tile, 64 queries each.
+//   Scores 0, dP 128, which P and dS then take, sums 256 and 384.  The next scores are formed meanwhile,
+//   and exponentials taken while the products with P and dS run; only dP is waited for.
+// (Steps of 64 queries would leave room for turns there too, but a product of fewer than 128 columns takes
+// as long as one of 128.)
 template <int DH>
 struct DkvSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
-    static constexpr bool TAKE_TURNS = DH == 64;
-    // tensor memory: scores (over them P^T), dP^T, sums.  With turns dS^T lies behind P^T, else over dP^T
-    static constexpr uint32_t DP = TAKE_TURNS ? 2 * TILE : TILE, DV = DP + TILE, DK = DV + DH;
-    static_assert(DK + DH <= TMEM_COLUMNS, "tensor memory");
-    static constexpr int Q_SLOTS = TAKE_TURNS ? 3 : 2, DO_SLOTS = 2;
+    static constexpr bool TURNS = DH == 64;
+    static constexpr uint32_t DP = TILE, MINE = 2 * TILE, DV = TURNS ? 384 : 256, DK = DV + DH;
+    static constexpr int Q_SLOTS = TURNS ? 4 : 2, DO_SLOTS = TURNS ? 3 : 2;
     alignas(1024) uint8_t k[TILE_BYTES], v[TILE_BYTES], q[Q_SLOTS][TILE_BYTES], dout[DO_SLOTS][TILE_BYTES];
     alignas(128) uint4 ones_lse[TILE], ones_delta[TILE], terms[Q_SLOTS][TILE], zeros[TILE];      // zeros come last: product_short
-    uint64_t kv_full, q_full[Q_SLOTS], q_free[Q_SLOTS], do_full[DO_SLOTS], do_free[DO_SLOTS], s_full[2], dp_full, p_ready[2], dp_taken, ds_ready[2], sums_full, landed;
+    uint64_t kv_full, q_full[Q_SLOTS], q_free[Q_SLOTS], do_full[DO_SLOTS], do_free[DO_SLOTS], s_full[2], s_taken, dp_full[2], p_ready[2], dp_taken, ds_ready[2], dv_done[2], dk_done[2], sums_full, landed;
     uint32_t tmem, gave_up;
 };
 
@@ -588,8 +628,8 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         bar_init(&sm.landed, 1);
         for (int i = 0; i < Smem::Q_SLOTS; ++i) bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1);
         for (int i = 0; i < Smem::DO_SLOTS; ++i) bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.ds_ready[w], 4);
-        bar_init(&sm.dp_full, 1), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.dp_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.ds_ready[w], 4), bar_init(&sm.dv_done[w], 1), bar_init(&sm.dk_done[w], 1);
+        bar_init(&sm.s_taken, Smem::TURNS ? 4 : 8), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
         sm.gave_up = 0;
     }
     if (threadIdx.x < TILE) {
@@ -599,14 +639,14 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         sm.zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
-    if (warp == WARP_MMA && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
-    if (warp >= WARP_MMA) registers_give<REGISTERS_HELP>();
+    if (warp >= 8) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
         if (n > 0) {
             if (lane == 0) {
@@ -632,80 +672,109 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 if (!load_tile<DH, true>(smem_addr(sm.dout[ds]), sm.dout[ds], &map_do, &sm.do_full[ds], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
             }
         }
-    } else if (warp == WARP_MMA) {
+    } else if (warp == WARP_SCORES) {
         if (elected()) {
-            const uint32_t zeros = smem_addr(sm.zeros), k_at = smem_addr(sm.k), v_at = smem_addr(sm.v), q_at = smem_addr(sm.q),
-                           do_at = smem_addr(sm.dout), terms_at = smem_addr(sm.terms), ones_lse = smem_addr(sm.ones_lse), ones_delta = smem_addr(sm.ones_delta);
-            auto scores = [&](int i) {
-                const int qs = i % Smem::Q_SLOTS, w = Smem::TAKE_TURNS ? i & 1 : 0;
-                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;
-                product_short<TILE>(tmem + w * TILE, ones_lse, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tmem + w * TILE, k_at, q_at + qs * Smem::TILE_BYTES, true);
-                mma_commit(&sm.s_full[w]);
-                return true;
-            };
+            const uint32_t zeros = smem_addr(sm.zeros), k_at = smem_addr(sm.k), q_at = smem_addr(sm.q), terms_at = smem_addr(sm.terms), ones = smem_addr(sm.ones_lse);
+            for (int i = 0; i < n; ++i) {
+                const int qs = i % Smem::Q_SLOTS;
+                if (i == 0 && !bar_wait_one(&sm.kv_full, 0, gave_up)) break;
+                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) break;
+                if (i > 0 && !bar_wait_one(&sm.s_taken, (i - 1) & 1, gave_up)) break;
+                tmem_fence_after();
+                product_short<TILE>(tmem, ones, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tmem, k_at, q_at + qs * Smem::TILE_BYTES, true);
+                mma_commit(&sm.s_full[Smem::TURNS ? i & 1 : 0]);
+            }
+        }
+        __syncwarp();
+    } else if (warp == WARP_DP || warp == WARP_SUMS) {
+        if (elected()) {
+            const uint32_t zeros = smem_addr(sm.zeros), v_at = smem_addr(sm.v), q_at = smem_addr(sm.q), do_at = smem_addr(sm.dout), terms_at = smem_addr(sm.terms),
+                           ones = smem_addr(sm.ones_delta);
             auto dprobs = [&](int i) {
                 const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
+                if (i == 0 && !bar_wait_one(&sm.kv_full, 0, gave_up)) return false;
+                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;        // delta comes with the queries
                 if (!bar_wait_one(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) return false;
-                if (Smem::TAKE_TURNS && i > 0 && !bar_wait_one(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
+                if (Smem::TURNS && i > 0 && !bar_wait_one(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
                 tmem_fence_after();
-                product_short<TILE>(tmem + Smem::DP, ones_delta, terms_at + qs * TILE * 16, zeros);
+                product_short<TILE>(tmem + Smem::DP, ones, terms_at + qs * TILE * 16, zeros);
                 product_rows<DH, TILE>(tmem + Smem::DP, v_at, do_at + ds * Smem::TILE_BYTES, true);
-                mma_commit(&sm.dp_full);
+                mma_commit(&sm.dp_full[Smem::TURNS ? i & 1 : 0]);
                 return true;
             };
-            // sums += A B for tile i, A in tensor memory: the whole tile's, or of each group's 64 queries once they are ready
-            auto add_to = [&](uint32_t sums, uint32_t a, uint32_t rows, uint64_t *ready, int i) {
-                if constexpr (Smem::TAKE_TURNS) {
-                    if (!bar_wait_one(&ready[i & 1], i / 2 & 1, gave_up)) return false;
+            if (Smem::TURNS && warp == WARP_DP) {
+                for (int i = 0; i < n; ++i)
+                    if (!dprobs(i)) break;
+            } else if (Smem::TURNS) {
+                for (int i = 0; i < n; ++i) {
+                    const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS, w = i & 1;
+                    if (!bar_wait_one(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) break;
+                    if (!bar_wait_one(&sm.p_ready[w], i / 2 & 1, gave_up)) break;
                     tmem_fence_after();
-                    product_down<DH, TILE>(sums, a, rows, i > 0);
-                } else {
-                    for (int g = 0; g < 2; ++g) {
-                        if (!bar_wait_one(&ready[g], i & 1, gave_up)) return false;
-                        tmem_fence_after();
-                        product_down<DH, 64>(sums, a + g * 64, rows + g * 64 * 128, i > 0 || g > 0);
-                    }
+                    product_down<DH, TILE>(tmem + Smem::DV, tmem + Smem::MINE + w * 64, do_at + ds * Smem::TILE_BYTES, i > 0);
+                    mma_commit(&sm.dv_done[w]);
+                    if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) break;
+                    if (!bar_wait_one(&sm.ds_ready[w], i / 2 & 1, gave_up)) break;
+                    tmem_fence_after();
+                    product_down<DH, TILE>(tmem + Smem::DK, tmem + Smem::MINE + w * 64, q_at + qs * Smem::TILE_BYTES, i > 0);
+                    mma_commit(&sm.dk_done[w]);
+                    mma_commit(&sm.q_free[qs]);           // dS came from scores and dP: all products with the two tiles are done
+                    mma_commit(&sm.do_free[ds]);
+                    if (i == n - 1) mma_commit(&sm.sums_full);
                 }
-                return true;
-            };
-            if (n > 0 && bar_wait_one(&sm.kv_full, 0, gave_up) && scores(0) && dprobs(0) && (!Smem::TAKE_TURNS || n == 1 || scores(1))) {
+            } else if (warp == WARP_SUMS && n > 0 && dprobs(0)) {      // dP takes the place of P and dS: one thread, in order
                 for (int i = 0; i < n; ++i) {
                     const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
-                    const uint32_t probs = tmem + (Smem::TAKE_TURNS ? (i & 1) * TILE : 0), dscores = Smem::TAKE_TURNS ? probs + TILE / 2 : tmem + Smem::DP;
-                    if (!add_to(tmem + Smem::DV, probs, do_at + ds * Smem::TILE_BYTES, sm.p_ready, i)) break;
+                    bool ok = true;
+                    for (int g = 0; g < 2 && ok; ++g) {           // each group's 64 queries
+                        ok = bar_wait_one(&sm.ds_ready[g], i & 1, gave_up);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        product_down<DH, 64>(tmem + Smem::DV, tmem + Smem::DP + g * 64, do_at + ds * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
+                        product_down<DH, 64>(tmem + Smem::DK, tmem + Smem::DP + g * 64 + 32, q_at + qs * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
+                    }
+                    if (!ok) break;
                     mma_commit(&sm.do_free[ds]);
-                    if (i + 1 < n && !(Smem::TAKE_TURNS ? dprobs(i + 1) : scores(i + 1))) break;
-                    if (!add_to(tmem + Smem::DK, dscores, q_at + qs * Smem::TILE_BYTES, sm.ds_ready, i)) break;
                     mma_commit(&sm.q_free[qs]);
                     if (i == n - 1) mma_commit(&sm.sums_full);
-                    if (Smem::TAKE_TURNS ? i + 2 < n && !scores(i + 2) : i + 1 < n && !dprobs(i + 1)) break;
+                    if (i + 1 < n && !dprobs(i + 1)) break;
                 }
             }
         }
         __syncwarp();
-    } else if (warp < WARP_MMA) {
+    } else if (warp < 8) {
         registers_take<REGISTERS_COMPUTE>();
-        constexpr int WIDTH = Smem::TAKE_TURNS ? TILE : TILE / 2, EVERY = Smem::TAKE_TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
-        const int w = warp / 4, key = key0 + threadIdx.x % TILE, col0 = Smem::TAKE_TURNS ? 0 : w * WIDTH;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + (Smem::TAKE_TURNS ? w * TILE : col0), dp_at = lanes + Smem::DP + col0;
-        const uint32_t ds_at = Smem::TAKE_TURNS ? s_at + TILE / 2 : dp_at;
-        uint64_t *const s_full = &sm.s_full[Smem::TAKE_TURNS ? w : 0];
+        constexpr int WIDTH = Smem::TURNS ? TILE : TILE / 2, EVERY = Smem::TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
+        const int w = warp / 4, key = key0 + threadIdx.x % TILE, col0 = Smem::TURNS ? 0 : w * WIDTH;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + col0, dp_at = lanes + Smem::DP + col0;
+        // A group that takes turns has barriers of its own: one that is waited for only every other time would
+        // tell its phases apart by nothing.
+        uint64_t *const s_full = &sm.s_full[Smem::TURNS ? w : 0], *const dp_full = &sm.dp_full[Smem::TURNS ? w : 0];
+        const uint32_t p_at = Smem::TURNS ? lanes + Smem::MINE + w * 64 : dp_at, ds_at = Smem::TURNS ? p_at : dp_at + 32;
         bool ok = true;
-        for (int i = Smem::TAKE_TURNS ? w : 0; i < n; i += EVERY) {
+        for (int i = Smem::TURNS ? w : 0; i < n; i += EVERY) {
             const int row0 = (first + i % per_head) * TILE;
             // columns before `hidden` do not see the key
             const int hidden = seq.causal && row0 < key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
             if (!(ok = bar_wait(s_full, i / EVERY & 1, gave_up))) break;
             tmem_fence_after();
-            uint32_t s[WIDTH / 32][32];
-#pragma unroll
-            for (int c = 0; c < WIDTH / 32; ++c) tmem_load32(s_at + c * 32, s[c]);
+            uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
+            tmem_load32(s_at, s[0]);
+            tmem_load32(s_at + 32, s[1]);
             tmem_wait_loads();
+            if constexpr (WIDTH == TILE) {
+                tmem_load32(s_at + 64, s[2]);
+                tmem_load32(s_at + 96, s[3]);
+            }
             const bool some = __any_sync(0xFFFFFFFFu, hidden > 0);
 #pragma unroll
             for (int half = 0; half < WIDTH / 64; ++half) {
-                uint32_t packed[32];
+                if (half == 1) tmem_wait_loads();
+                if (half == WIDTH / 64 - 1) {
+                    tmem_fence_before();
+                    bar_arrive_warp(&sm.s_taken);
+                }
 #pragma unroll
                 for (int c = 0; c < 64; c += 2) {
                     uint32_t *const at = &s[half * 2 + c / 32][c % 32];
@@ -716,28 +785,51 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                         if (half * 64 + c + 1 < hidden) e.y = 0.0f;
                     }
                     at[0] = __float_as_uint(e.x), at[1] = __float_as_uint(e.y);
-                    packed[c / 2] = pack_bf16(e);
+                    probs[half][c / 2] = pack_bf16(e);
                 }
-                tmem_store32(s_at + half * 32, packed);
             }
-            tmem_wait_stores();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.p_ready[w]);
-            if (!(ok = bar_wait(&sm.dp_full, i & 1, gave_up))) break;
-            tmem_fence_after();
-#pragma unroll
-            for (int half = 0; half < WIDTH / 64; ++half) {
-                uint32_t d[2][32], packed[32];
-                tmem_load32(dp_at + half * 64, d[0]);
-                tmem_load32(dp_at + half * 64 + 32, d[1]);
-                tmem_wait_loads();
-                if (Smem::TAKE_TURNS && half == WIDTH / 64 - 1) {
-                    tmem_fence_before();
-                    bar_arrive_warp(&sm.dp_taken);
+            if constexpr (Smem::TURNS) {
+                if (i > 1) {                         // its last dS has been used
+                    if (!(ok = bar_wait(&sm.dk_done[w], (i / 2 - 1) & 1, gave_up))) break;
+                    tmem_fence_after();
                 }
+                tmem_store32(p_at, probs[0]);
+                tmem_store32(p_at + 32, probs[WIDTH / 64 - 1]);
+                tmem_wait_stores();
+                tmem_fence_before();
+                bar_arrive_warp(&sm.p_ready[w]);
+            }
+            if (!(ok = bar_wait(dp_full, i / EVERY & 1, gave_up))) break;
+            tmem_fence_after();
+            uint32_t d[2][32];
+            if constexpr (Smem::TURNS) {
+                uint32_t packed[4][16];
+                tmem_load32(dp_at, d[0]);
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[half * 2 + c / 32], c % 32), pair_of(d[c / 32], c % 32)));
-                tmem_store32(ds_at + half * 32, packed);
+                for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
+                    tmem_wait_loads();
+                    if (q < 3) {
+                        tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
+                    } else {
+                        tmem_fence_before();
+                        bar_arrive_warp(&sm.dp_taken);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), pair_of(d[q % 2], c)));
+                }
+                if (!(ok = bar_wait(&sm.dv_done[w], i / 2 & 1, gave_up))) break;        // P has been used
+                tmem_fence_after();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
+            } else {
+                tmem_load32(dp_at, d[0]);
+                tmem_load32(dp_at + 32, d[1]);
+                tmem_wait_loads();
+                tmem_store32(p_at, probs[0]);
+                uint32_t packed[32];
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[c / 32], c % 32), pair_of(d[c / 32], c % 32)));
+                tmem_store32(ds_at, packed);
             }
             tmem_wait_stores();
             tmem_fence_before();
@@ -766,7 +858,7 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     tmem_fence_before();
     __syncthreads();
     settle(gave_up);
-    if (warp == WARP_MMA && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
 }
 
 // ---------------------------------------------------------------------------------- host side
