@@ -450,7 +450,7 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                 if (!bar_wait(&sm.k_free[ks], (j / Smem::K_SLOTS + 1) & 1, gave_up)) break;
                 if (!load_tile<DH, true>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
                 if (!bar_wait(&sm.v_free[vs], (j / Smem::V_SLOTS + 1) & 1, gave_up)) break;
-                load_tile<DH, false>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
+                if (!load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
             }
         }
     } else if (warp == WARP_SCORES) {
@@ -510,25 +510,22 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
             if (!(ok = bar_wait(&sm.s_full[w], j / 2 & 1, gave_up))) break;
             tmem_fence_after();
             uint32_t s[4][32];
-            tmem_load32(s_at, s[0]);
-            tmem_load32(s_at + 32, s[1]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
             tmem_wait_loads();
-            tmem_load32(s_at + 64, s[2]);
-            tmem_load32(s_at + 96, s[3]);
+            tmem_fence_before();
+            bar_arrive_warp(&sm.s_taken);
+            if (!whole || (j + 1) * TILE > all_see) {
+                const int left = limit - j * TILE;           // columns that the row sees
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (half == 1) {
-                    tmem_wait_loads();
-                    tmem_fence_before();
-                    bar_arrive_warp(&sm.s_taken);
-                }
-#pragma unroll
-                for (int c = half * 64; c < half * 64 + 64; c += 2) {
-                    const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
-                    s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
-                }
+                for (int c = 0; c < TILE; ++c)
+                    if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
             }
-            const int left = !whole || (j + 1) * TILE > all_see ? limit - j * TILE : TILE;     // columns that the row sees
+#pragma unroll
+            for (int c = 0; c < TILE; c += 2) {
+                const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
+                s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
+            }
             if (!(ok = bar_wait(&sm.dp_full[w], j / 2 & 1, gave_up))) break;
             tmem_fence_after();
             uint32_t d[2][32], packed[4][16];
@@ -542,16 +539,8 @@ k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUt
                     tmem_fence_before();
                     bar_arrive_warp(&sm.dp_taken);
                 }
-                const bool some = __any_sync(0xFFFFFFFFu, left < (q + 1) * 32);
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    float2 x = mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta)));
-                    if (some) {
-                        if (q * 32 + c >= left) x.x = 0.0f;
-                        if (q * 32 + c + 1 >= left) x.y = 0.0f;
-                    }
-                    packed[q][c / 2] = pack_bf16(x);
-                }
+                for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta))));
             }
             if (j > 1) {                         // its last dS has been used
                 if (!(ok = bar_wait(&sm.dq_done[w], (j / 2 - 1) & 1, gave_up))) break;
@@ -727,16 +716,17 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
                 for (int i = 0; i < n; ++i) {
                     const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
                     bool ok = true;
-                    for (int g = 0; g < 2 && ok; ++g) {           // each group's 64 queries
+                    for (int g = 0; g < 2 && ok; ++g) {           // each group's 64 queries; dK first: there is room for two query tiles only
                         ok = bar_wait_one(&sm.ds_ready[g], i & 1, gave_up);
                         if (!ok) break;
                         tmem_fence_after();
-                        product_down<DH, 64>(tmem + Smem::DV, tmem + Smem::DP + g * 64, do_at + ds * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
                         product_down<DH, 64>(tmem + Smem::DK, tmem + Smem::DP + g * 64 + 32, q_at + qs * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
                     }
                     if (!ok) break;
-                    mma_commit(&sm.do_free[ds]);
                     mma_commit(&sm.q_free[qs]);
+                    for (int g = 0; g < 2; ++g)
+                        product_down<DH, 64>(tmem + Smem::DV, tmem + Smem::DP + g * 64, do_at + ds * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
+                    mma_commit(&sm.do_free[ds]);
                     if (i == n - 1) mma_commit(&sm.sums_full);
                     if (i + 1 < n && !dprobs(i + 1)) break;
                 }
@@ -760,33 +750,22 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
             if (!(ok = bar_wait(s_full, i / EVERY & 1, gave_up))) break;
             tmem_fence_after();
             uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
-            tmem_load32(s_at, s[0]);
-            tmem_load32(s_at + 32, s[1]);
+#pragma unroll
+            for (int q = 0; q < WIDTH / 32; ++q) tmem_load32(s_at + q * 32, s[q]);
             tmem_wait_loads();
-            if constexpr (WIDTH == TILE) {
-                tmem_load32(s_at + 64, s[2]);
-                tmem_load32(s_at + 96, s[3]);
+            tmem_fence_before();
+            bar_arrive_warp(&sm.s_taken);
+            if (__any_sync(0xFFFFFFFFu, hidden > 0)) {
+#pragma unroll
+                for (int c = 0; c < WIDTH; ++c)
+                    if (c < hidden) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
             }
-            const bool some = __any_sync(0xFFFFFFFFu, hidden > 0);
 #pragma unroll
-            for (int half = 0; half < WIDTH / 64; ++half) {
-                if (half == 1) tmem_wait_loads();
-                if (half == WIDTH / 64 - 1) {
-                    tmem_fence_before();
-                    bar_arrive_warp(&sm.s_taken);
-                }
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    uint32_t *const at = &s[half * 2 + c / 32][c % 32];
-                    const float2 x = mul2(pair_of(s[half * 2 + c / 32], c % 32), both(p.scale_log2));
-                    float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-                    if (some) {
-                        if (half * 64 + c < hidden) e.x = 0.0f;
-                        if (half * 64 + c + 1 < hidden) e.y = 0.0f;
-                    }
-                    at[0] = __float_as_uint(e.x), at[1] = __float_as_uint(e.y);
-                    probs[half][c / 2] = pack_bf16(e);
-                }
+            for (int c = 0; c < WIDTH; c += 2) {
+                const float2 x = mul2(pair_of(s[c / 32], c % 32), both(p.scale_log2));
+                const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                s[c / 32][c % 32] = __float_as_uint(e.x), s[c / 32][c % 32 + 1] = __float_as_uint(e.y);
+                probs[c / 64][c % 64 / 2] = pack_bf16(e);
             }
             if constexpr (Smem::TURNS) {
                 if (i > 1) {                         // its last dS has been used
