@@ -5,10 +5,10 @@
 //   forward    O = P V, one pass over the keys with a running maximum and sum per query
 //   backward   delta_i = sum_d dO_id O_id,  dP = dO V^T,  dS = P (dP - delta),
 //              dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
-// The backward pass recomputes P from Q, K and lse.  It is two kernels: one CTA per 128 queries that
-// goes over the keys (dQ), one per 128 keys that goes over the queries of all heads that share them (dK,
-// dV).  Every sum has one owner, so nothing is added with atomics and the result does not depend on
-// the order in which CTAs run; the price is that S and dP are formed twice (7 products, not 5).
+// The backward pass recomputes P from Q, K and lse, twice: one CTA per 128 queries goes over the keys (dQ), one
+// per 128 keys over the queries of all heads that share them (dK, dV).  Every sum has one owner, so nothing
+// is added with atomics and the result does not depend on the order in which CTAs run; the price is that
+// S and dP are formed twice (7 products, not 5).
 //
 // All products run on the tensor cores (kt_tensor.cuh): operands come in by tile copies, sums stay in
 // tensor memory, and the probabilities (dS) go back to tensor memory as bf16, where they are the first
@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "kt_internal.h"
 #include "kt_pairs.cuh"
@@ -45,10 +46,10 @@ struct QueryStats;
 struct AttnParams {
     const int32_t *used_q, *used_kv;
     const __nv_bfloat16 *o, *dout;
-    __nv_bfloat16 *out, *out2;                  // O, dQ, or dK and dV
+    __nv_bfloat16 *out, *dk, *dv;               // O or dQ
     float *lse;
     QueryStats *stats;
-    int64_t o_stride[3], dout_stride[3], out_stride[3], out2_stride[3];     // batch, token, head
+    int64_t o_stride[3], dout_stride[3], out_stride[3], dk_stride[3], dv_stride[3];     // batch, token, head
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
     int tiles_q, tiles_kv;
     float scale, scale_log2;
@@ -397,21 +398,19 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
 template <int DH>
 struct DqSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
-    static constexpr int K_SLOTS = 3, V_SLOTS = 2;
+    static constexpr int K_SLOTS = DH == 64 ? 5 : 3, V_SLOTS = DH == 64 ? 3 : 2;
     alignas(1024) uint8_t q[TILE_BYTES], dout[TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
     uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, dp_full[2], dp_taken, ds_ready[2], dq_done[2], sums_full, landed;
     uint32_t tmem, gave_up;
 };
 
 template <int DH>
-__global__ void __launch_bounds__(THREADS, 1)
-k_attn_dq(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-          const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
-    extern __shared__ uint8_t raw[];
+__device__ __forceinline__ void dq_tile(uint8_t *raw, const int block, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, const CUtensorMap &map_do,
+                                        const AttnParams &p) {
     using Smem = DqSmem<DH>;
     auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int bh = blockIdx.x % (p.batch * p.heads), tile = p.tiles_q - 1 - static_cast<int>(blockIdx.x / (p.batch * p.heads)), row0 = tile * TILE;
+    const int bh = block % (p.batch * p.heads), tile = p.tiles_q - 1 - block / (p.batch * p.heads), row0 = tile * TILE;
     const int b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
     const Seq seq(p, b);
     const int n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
@@ -600,14 +599,12 @@ struct DkvSmem {
 };
 
 template <int DH>
-__global__ void __launch_bounds__(THREADS, 1)
-k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-           const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
-    extern __shared__ uint8_t raw[];
+__device__ __forceinline__ void dkv_tile(uint8_t *raw, const int block, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, const CUtensorMap &map_do,
+                                        const AttnParams &p) {
     using Smem = DkvSmem<DH>;
     auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int bh = blockIdx.x % (p.batch * p.heads_kv), key0 = static_cast<int>(blockIdx.x / (p.batch * p.heads_kv)) * TILE;    // early keys are seen most
+    const int bh = block % (p.batch * p.heads_kv), key0 = block / (p.batch * p.heads_kv) * TILE;    // early keys are seen most
     const int b = bh / p.heads_kv, h_kv = bh % p.heads_kv, shared = p.heads / p.heads_kv;
     const Seq seq(p, b);
     const int first = seq.first_query_of(key0) / TILE, per_head = key0 < seq.m ? max(0, tiles(seq.n) - first) : 0, n = per_head * shared;
@@ -817,8 +814,8 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
         if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
         tmem_fence_after();
         // one group writes dV, the other dK
-        const int64_t *stride = w == 0 ? p.out2_stride : p.out_stride;
-        __nv_bfloat16 *out = (w == 0 ? p.out2 : p.out) + b * stride[0] + key * stride[1] + h_kv * stride[2];
+        const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
+        __nv_bfloat16 *out = (w == 0 ? p.dv : p.dk) + b * stride[0] + key * stride[1] + h_kv * stride[2];
 #pragma unroll
         for (int c = 0; c < DH; c += 32) {
             if (n > 0 && ok) {
@@ -838,6 +835,18 @@ k_attn_dkv(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CU
     __syncthreads();
     settle(gave_up);
     if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+}
+
+// Both in one launch, which fills the SMs better than one after the other: first the key tiles, whose work
+// is the larger, then the query tiles, each kind in the order of what a causal mask leaves it.
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
+    extern __shared__ uint8_t raw[];
+    const int key_tiles = p.batch * p.heads_kv * p.tiles_kv, block = static_cast<int>(blockIdx.x);
+    if (block < key_tiles) dkv_tile<DH>(raw, block, map_q, map_k, map_v, map_do, p);
+    else dq_tile<DH>(raw, block - key_tiles, map_q, map_k, map_v, map_do, p);
 }
 
 // ---------------------------------------------------------------------------------- host side
@@ -919,19 +928,11 @@ int start_forward(const CUtensorMap (&m)[3], const AttnParams &p, cudaStream_t s
 }
 
 template <int DH>
-int start_dq(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
+int start_backward(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
-    if (int rc = room<DqSmem<DH>>(k_attn_dq<DH>, &bytes)) return rc;
-    k_attn_dq<DH><<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q), THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
-}
-
-template <int DH>
-int start_dkv(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
-    size_t bytes = 0;
-    if (int rc = room<DkvSmem<DH>>(k_attn_dkv<DH>, &bytes)) return rc;
-    k_attn_dkv<DH><<<static_cast<unsigned>(p.batch * p.heads_kv * p.tiles_kv), THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
+    if (int rc = room<std::conditional_t<(sizeof(DqSmem<DH>) > sizeof(DkvSmem<DH>)), DqSmem<DH>, DkvSmem<DH>>>(k_attn_backward<DH>, &bytes)) return rc;
+    const unsigned ctas = static_cast<unsigned>(p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q));
+    k_attn_backward<DH><<<ctas, THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
     KT_CUDA(cudaGetLastError());
     return KT_OK;
 }
@@ -1024,14 +1025,11 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
     copy_strides(p.dout_stride, dout_stride);
     k_attn_stats<<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q * (TILE / 16)), 256, 0, st>>>(p);
     KT_CUDA(cudaGetLastError());
-    AttnParams pq = p;
-    pq.out = static_cast<__nv_bfloat16 *>(dq);
-    copy_strides(pq.out_stride, dq_stride);
-    if (int rc = p.dim <= 64 ? start_dq<64>(m, pq, st) : start_dq<128>(m, pq, st)) return rc;
-    p.out = static_cast<__nv_bfloat16 *>(dk), p.out2 = static_cast<__nv_bfloat16 *>(dv);
-    copy_strides(p.out_stride, dk_stride);
-    copy_strides(p.out2_stride, dv_stride);
-    return p.dim <= 64 ? start_dkv<64>(m, p, st) : start_dkv<128>(m, p, st);
+    p.out = static_cast<__nv_bfloat16 *>(dq), p.dk = static_cast<__nv_bfloat16 *>(dk), p.dv = static_cast<__nv_bfloat16 *>(dv);
+    copy_strides(p.out_stride, dq_stride);
+    copy_strides(p.dk_stride, dk_stride);
+    copy_strides(p.dv_stride, dv_stride);
+    return p.dim <= 64 ? start_backward<64>(m, p, st) : start_backward<128>(m, p, st);
 }
 
 int kt_attn_given_up(int64_t *count) {
