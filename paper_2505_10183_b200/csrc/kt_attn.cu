@@ -20,7 +20,6 @@
 #include <cuda_bf16.h>
 
 #include <cmath>
-#include <type_traits>
 
 #include "kt_internal.h"
 #include "kt_pairs.cuh"
@@ -40,6 +39,7 @@ constexpr int WARP_SCORES = 8, WARP_LOAD = 9, WARP_DP = 10, WARP_SUMS = 11, THRE
 // eight warps that compute take: 256 x 208 + 128 x 88 = 64512.
 constexpr int REGISTERS_COMPUTE = 208, REGISTERS_HELP = 88;
 constexpr uint32_t TMEM_COLUMNS = 512;
+constexpr int SMS = 148;                        // of a B200, one CTA to each
 
 struct QueryStats;
 
@@ -49,6 +49,7 @@ struct AttnParams {
     __nv_bfloat16 *out, *dk, *dv;               // O or dQ
     float *lse;
     QueryStats *stats;
+    unsigned *next_item;
     int64_t o_stride[3], dout_stride[3], out_stride[3], dk_stride[3], dv_stride[3];     // batch, token, head
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
     int tiles_q, tiles_kv;
@@ -124,18 +125,42 @@ __device__ __forceinline__ void settle(volatile uint32_t *gave_up) {
 }
 
 // ------------------------------------------------------------------------------------ forward
-// Two tiles of 128 queries to a CTA, four warps on each.  A thread owns a row: maximum and sum need no
-// exchange.  A group takes its scores into registers at once, and their place in tensor memory is free for
-// the other group's next ones: scores are formed up to three steps ahead, and neither a group nor the tensor
-// cores wait for the other in turn.  Tensor memory: scores 0, probabilities 128 and 192, sums 256 and 256 + DH.
+// Two tiles of 128 queries to a work item, four warps on each.  A thread owns a row: maximum and sum need
+// no exchange.  A group takes its scores into registers at once, and their place in tensor memory is free for
+// the other group's next ones, so that neither a group nor the tensor cores wait for the other in turn.
+// CTAs stay (Queue): the next item's tiles are fetched and its first scores formed while the last item's
+// output is written, which short sequences need most.  Every barrier's phases are counted on from item to item.
+// Tensor memory: scores 0, probabilities 128 and 192, sums 256 and 256 + DH.
 template <int DH>
 struct FwdSmem {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
-    alignas(1024) uint8_t q[2][TILE_BYTES];
-    static constexpr int K_SLOTS = 3, V_SLOTS = 2;
-    alignas(1024) uint8_t k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
-    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, p_ready[2], o_done[2], landed;
+    static constexpr int SETS = DH == 64 ? 2 : 1, K_SLOTS = 3, V_SLOTS = 2;       // of query tiles: two where there is room
+    alignas(1024) uint8_t q[SETS][2][TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
+    Queue queue;
+    uint64_t q_full[SETS], q_free[SETS], k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, p_ready[2], o_done[2], o_taken[2], landed;
     uint32_t tmem, gave_up;
+};
+
+// A work item: the pair of query tiles, and the key tiles that each of them sees.
+struct FwdItem {
+    int row0, b, h, h_kv, n_tiles[2], n, common, longer, steps;
+    __device__ FwdItem(const AttnParams &p, int block) {
+        const int pairs = (p.tiles_q + 1) / 2, all = p.batch * p.heads, bh = block % all;
+        row0 = (pairs - 1 - block / all) * 2 * TILE;               // the longest rows first
+        b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
+        const Seq seq(p, b);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+            const int first = row0 + w * TILE;
+            n_tiles[w] = first < seq.n ? tiles(seq.keys_of(min(first + TILE, seq.n) - 1)) : 0;
+        }
+        n = max(n_tiles[0], n_tiles[1]);
+        // Steps: the two tiles in turn while both have keys left, then the one that has more.
+        common = min(n_tiles[0], n_tiles[1]), longer = n_tiles[1] > n_tiles[0] ? 1 : 0, steps = n_tiles[0] + n_tiles[1];
+    }
+    __device__ int key_tile(int u) const { return u < 2 * common ? u / 2 : u - common; }
+    __device__ int group(int u) const { return u < 2 * common ? u & 1 : longer; }
+    __device__ bool last_use(int u) const { return group(u) == 1 || key_tile(u) >= n_tiles[1]; }      // of its key tile
 };
 
 template <int DH>
@@ -144,196 +169,220 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                const AttnParams p) {
     extern __shared__ uint8_t raw[];
     using Smem = FwdSmem<DH>;
+    constexpr int SETS = Smem::SETS, K_SLOTS = Smem::K_SLOTS, V_SLOTS = Smem::V_SLOTS;
     auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int pairs = (p.tiles_q + 1) / 2, bh = blockIdx.x % (p.batch * p.heads);
-    const int row0 = (pairs - 1 - static_cast<int>(blockIdx.x / (p.batch * p.heads))) * 2 * TILE;      // the longest rows first
-    const int b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
-    const Seq seq(p, b);
-    int n_tiles[2];                             // key tiles that a query tile sees
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int first = row0 + w * TILE;
-        n_tiles[w] = first < seq.n ? tiles(seq.keys_of(min(first + TILE, seq.n) - 1)) : 0;
-    }
-    const int n = max(n_tiles[0], n_tiles[1]);
-    // Steps: the tiles' groups in turn while both have keys left, then the one that has more.
-    const int common = min(n_tiles[0], n_tiles[1]), longer = n_tiles[1] > n_tiles[0] ? 1 : 0, steps = n_tiles[0] + n_tiles[1];
 
     if (threadIdx.x == 0) {
-        bar_init(&sm.q_full, 1);
-        bar_init(&sm.landed, 1);
-        for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
-        for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_done[w], 1);
-        bar_init(&sm.s_taken, 4);
+        queue_init(sm.queue, 3 + 8);
+        for (int i = 0; i < SETS; ++i) bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1);
+        for (int i = 0; i < K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
+        for (int i = 0; i < V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
+        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_done[w], 1), bar_init(&sm.o_taken[w], 4);
+        bar_init(&sm.s_taken, 4), bar_init(&sm.landed, 1);
         sm.gave_up = 0;
         fence_async_smem();
     }
-    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
     volatile uint32_t *gave_up = &sm.gave_up;
 
-    if (warp >= 8) registers_give<REGISTERS_HELP>();
     if (warp == WARP_LOAD) {
-        if (n > 0) {
+        registers_give<REGISTERS_HELP>();
+        uint32_t asked = 0, sets = 0, tiles_in = 0, landed_phase = 0;      // counts over all items
+        bool ok = true;
+        for (int block = blockIdx.x; ok && block >= 0; block = queue_next<false>(sm.queue, asked - 1, gave_up)) {
+            const FwdItem it(p, block);
+            const Seq seq(p, it.b);
+            if (!(ok = bar_wait(&sm.queue.free[asked % QUEUE], (asked / QUEUE + 1) & 1, gave_up))) break;
+            if (lane == 0) queue_ask(sm.queue, asked);
+            ++asked;
+            if (it.n == 0) continue;
+            const int set = sets % SETS;
+            if (!(ok = bar_wait(&sm.q_free[set], (sets / SETS + 1) & 1, gave_up))) break;
+            ++sets;
             if (lane == 0) {
-                bar_expect(&sm.q_full, 2 * Smem::TILE_BYTES);
+                bar_expect(&sm.q_full[set], 2 * Smem::TILE_BYTES);
                 for (int w = 0; w < 2; ++w)
-                    for (int c = 0; c < DH / 64; ++c) copy_tile(smem_addr(sm.q[w]) + c * CHUNK, &map_q, &sm.q_full, c * 64, row0 + w * TILE, h, b);
+                    for (int c = 0; c < DH / 64; ++c) copy_tile(smem_addr(sm.q[set][w]) + c * CHUNK, &map_q, &sm.q_full[set], c * 64, it.row0 + w * TILE, it.h, it.b);
             }
             __syncwarp();
-            uint32_t landed_phase = 0;
-            for (int j = 0; j <= n; ++j) {              // keys a tile ahead of values
-                if (j < n) {
-                    const int ks = j % Smem::K_SLOTS;
-                    if (!bar_wait(&sm.k_free[ks], (j / Smem::K_SLOTS + 1) & 1, gave_up)) break;
-                    load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up);
+            for (int j = 0; ok && j <= it.n; ++j) {              // keys a tile ahead of values
+                if (j < it.n) {
+                    const uint32_t i = tiles_in + j, ks = i % K_SLOTS;
+                    ok = bar_wait(&sm.k_free[ks], (i / K_SLOTS + 1) & 1, gave_up) &&
+                         load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                 }
-                if (j > 0) {
-                    const int vs = (j - 1) % Smem::V_SLOTS;
-                    if (!bar_wait(&sm.v_free[vs], ((j - 1) / Smem::V_SLOTS + 1) & 1, gave_up)) break;
-                    if (!load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (j - 1) * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
+                if (ok && j > 0) {
+                    const uint32_t i = tiles_in + j - 1, vs = i % V_SLOTS;
+                    ok = bar_wait(&sm.v_free[vs], (i / V_SLOTS + 1) & 1, gave_up) &&
+                         load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (j - 1) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                 }
             }
+            tiles_in += it.n;
         }
     } else if (warp == WARP_SCORES) {
+        registers_give<REGISTERS_HELP>();
         if (elected()) {
             const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
-            for (int u = 0; u < steps; ++u) {
-                const int j = u < 2 * common ? u / 2 : u - common, w = u < 2 * common ? u & 1 : longer, ks = j % Smem::K_SLOTS;
-                if (u == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
-                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
-                if (u > 0 && !bar_wait_one(&sm.s_taken, (u - 1) & 1, gave_up)) break;
-                tmem_fence_after();
-                product_rows<DH, TILE>(tmem, q_at + w * Smem::TILE_BYTES, k_at + ks * Smem::TILE_BYTES);
-                mma_commit(&sm.s_full[w]);
-                if (w == 1 || j >= n_tiles[1]) mma_commit(&sm.k_free[ks]);
+            uint32_t items = 0, sets = 0, tiles_in = 0, steps = 0;
+            bool ok = true;
+            for (int block = blockIdx.x; ok && block >= 0; block = queue_next_one<false>(sm.queue, items++, gave_up)) {
+                const FwdItem it(p, block);
+                if (it.n == 0) continue;
+                const uint32_t set = sets % SETS;
+                ok = bar_wait_one(&sm.q_full[set], sets / SETS & 1, gave_up);
+                ++sets;
+                for (int u = 0; ok && u < it.steps; ++u, ++steps) {
+                    const int w = it.group(u);
+                    const uint32_t i = tiles_in + it.key_tile(u), ks = i % K_SLOTS;
+                    ok = bar_wait_one(&sm.k_full[ks], i / K_SLOTS & 1, gave_up) && (steps == 0 || bar_wait_one(&sm.s_taken, (steps - 1) & 1, gave_up));
+                    if (!ok) break;
+                    tmem_fence_after();
+                    product_rows<DH, TILE>(tmem, q_at + (set * 2 + w) * Smem::TILE_BYTES, k_at + ks * Smem::TILE_BYTES);
+                    mma_commit(&sm.s_full[w]);
+                    if (it.last_use(u)) mma_commit(&sm.k_free[ks]);
+                    if (u == it.steps - 1) mma_commit(&sm.q_free[set]);
+                }
+                tiles_in += it.n;
             }
         }
         __syncwarp();
     } else if (warp == WARP_SUMS) {
+        registers_give<REGISTERS_HELP>();
         if (elected()) {
             const uint32_t v_at = smem_addr(sm.v);
-            for (int u = 0; u < steps; ++u) {
-                const int j = u < 2 * common ? u / 2 : u - common, w = u < 2 * common ? u & 1 : longer, vs = j % Smem::V_SLOTS;
-                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) break;
-                if (!bar_wait_one(&sm.p_ready[w], j & 1, gave_up)) break;
-                tmem_fence_after();
-                product_down<DH, TILE>(tmem + 256 + w * DH, tmem + TILE + w * 64, v_at + vs * Smem::TILE_BYTES, j > 0);
-                mma_commit(&sm.o_done[w]);
-                if (w == 1 || j >= n_tiles[1]) mma_commit(&sm.v_free[vs]);
+            uint32_t items = 0, tiles_in = 0, mine[2] = {0, 0}, outputs[2] = {0, 0};
+            bool ok = true;
+            for (int block = blockIdx.x; ok && block >= 0; block = queue_next_one<false>(sm.queue, items++, gave_up)) {
+                const FwdItem it(p, block);
+                for (int u = 0; ok && u < it.steps; ++u) {
+                    const int w = it.group(u), j = it.key_tile(u);
+                    const uint32_t i = tiles_in + j, vs = i % V_SLOTS;
+                    ok = bar_wait_one(&sm.v_full[vs], i / V_SLOTS & 1, gave_up) && bar_wait_one(&sm.p_ready[w], (mine[w] + j) & 1, gave_up) &&
+                         (j > 0 || outputs[w] == 0 || bar_wait_one(&sm.o_taken[w], (outputs[w] - 1) & 1, gave_up));       // the last item's sums have been read
+                    if (!ok) break;
+                    tmem_fence_after();
+                    product_down<DH, TILE>(tmem + 256 + w * DH, tmem + TILE + w * 64, v_at + vs * Smem::TILE_BYTES, j > 0);
+                    mma_commit(&sm.o_done[w]);
+                    if (it.last_use(u)) mma_commit(&sm.v_free[vs]);
+                }
+                tiles_in += it.n;
+                for (int w = 0; w < 2; ++w) mine[w] += it.n_tiles[w], outputs[w] += it.n_tiles[w] > 0;
             }
         }
         __syncwarp();
     } else if (warp < 8) {
         registers_take<REGISTERS_COMPUTE>();
-        const int w = warp / 4, row = row0 + w * TILE + threadIdx.x % TILE;
+        const int w = warp / 4;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, p_at = lanes + TILE + w * 64, o_at = lanes + 256 + w * DH;
-        const int limit = seq.keys_of(row), all_see = seq.keys_of(row0 + w * TILE);    // the tile's first row sees least
-        const bool whole = row0 + w * TILE + TILE <= seq.n;
-        float top = -INFINITY, sum = 0.0f;      // in units of log 2, after scaling
+        uint32_t items = 0, mine = 0;
         bool ok = true;
-        for (int j = 0; j < n_tiles[w]; ++j) {
-            if (!(ok = bar_wait(&sm.s_full[w], j & 1, gave_up))) break;
-            tmem_fence_after();
-            uint32_t s[4][32];
-            const int left = !whole || (j + 1) * TILE > all_see ? limit - j * TILE : TILE;     // columns that the row sees
-            float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            tmem_load32(s_at, s[0]);
-            tmem_load32(s_at + 32, s[1]);
-            tmem_wait_loads();
-            tmem_load32(s_at + 64, s[2]);
-            tmem_load32(s_at + 96, s[3]);
+        for (int block = blockIdx.x; ok && block >= 0; block = queue_next<false>(sm.queue, items++, gave_up)) {
+            const FwdItem it(p, block);
+            const Seq seq(p, it.b);
+            const int row = it.row0 + w * TILE + threadIdx.x % TILE, n_mine = w == 0 ? it.n_tiles[0] : it.n_tiles[1];
+            const int limit = seq.keys_of(row), all_see = seq.keys_of(it.row0 + w * TILE);    // the tile's first row sees least
+            const bool whole = it.row0 + w * TILE + TILE <= seq.n;
+            float top = -INFINITY, sum = 0.0f;      // in units of log 2, after scaling
+            for (int j = 0; j < n_mine; ++j) {
+                const uint32_t i = mine + j;
+                if (!(ok = bar_wait(&sm.s_full[w], i & 1, gave_up))) break;
+                tmem_fence_after();
+                uint32_t s[4][32];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                if (half == 1) {
-                    tmem_wait_loads();
-                    tmem_fence_before();
-                    bar_arrive_warp(&sm.s_taken);
-                }
-                if (__any_sync(0xFFFFFFFFu, left < (half + 1) * 64)) {
+                for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
+                tmem_wait_loads();
+                tmem_fence_before();
+                bar_arrive_warp(&sm.s_taken);
+                if (!whole || (j + 1) * TILE > all_see) {
+                    const int left = limit - j * TILE;           // columns that the row sees
 #pragma unroll
-                    for (int c = half * 64; c < half * 64 + 64; ++c)
+                    for (int c = 0; c < TILE; ++c)
                         if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
                 }
+                float m[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = half * 64; c < half * 64 + 64; ++c) m[c % 4] = fmaxf(m[c % 4], __uint_as_float(s[c / 32][c % 32]));
-            }
-            const float here = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
-            // The running maximum follows only when it would grow by 2^8: until then probabilities of up
-            // to 256 are as exact, and the sums in tensor memory need not be rescaled.
-            const bool grow = here > top + 8.0f || (top == -INFINITY && here > -INFINITY);
-            if (__any_sync(0xFFFFFFFFu, grow)) {
-                const float by = grow ? exp2_fast(top - here) : 1.0f;
-                if (grow) top = here;
-                sum *= by;
-                if (j > 0) {
-                    if (!(ok = bar_wait(&sm.o_done[w], (j - 1) & 1, gave_up))) break;
-                    tmem_fence_after();
+                for (int c = 0; c < TILE; ++c) m[c % 4] = fmaxf(m[c % 4], __uint_as_float(s[c / 32][c % 32]));
+                const float here = fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * p.scale_log2;
+                // The running maximum follows only when it would grow by 2^8: until then probabilities of up
+                // to 256 are as exact, and the sums in tensor memory need not be rescaled.
+                const bool grow = here > top + 8.0f || (top == -INFINITY && here > -INFINITY);
+                if (__any_sync(0xFFFFFFFFu, grow)) {
+                    const float by = grow ? exp2_fast(top - here) : 1.0f;
+                    if (grow) top = here;
+                    sum *= by;
+                    if (j > 0) {
+                        if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, gave_up))) break;
+                        tmem_fence_after();
 #pragma unroll
-                    for (int c = 0; c < DH; c += 32) {
-                        uint32_t o[32];
-                        tmem_load32(o_at + c, o);
-                        tmem_wait_loads();
+                        for (int c = 0; c < DH; c += 32) {
+                            uint32_t o[32];
+                            tmem_load32(o_at + c, o);
+                            tmem_wait_loads();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
-                        tmem_store32(o_at + c, o);
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+                            tmem_store32(o_at + c, o);
+                        }
                     }
                 }
-            }
-            const float ref = top == -INFINITY ? 0.0f : top;
-            float2 part[2] = {both(0.0f), both(0.0f)};
-            uint32_t packed[2][32];
+                const float ref = top == -INFINITY ? 0.0f : top;
+                float2 part[2] = {both(0.0f), both(0.0f)};
+                uint32_t packed[2][32];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) {
-                    const float2 x = fma2(pair_of(s[half * 2 + c / 32], c % 32), both(p.scale_log2), both(-ref));
+                for (int c = 0; c < TILE; c += 2) {
+                    const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-ref));
                     const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
                     part[c / 2 % 2] = add2(part[c / 2 % 2], e);
-                    packed[half][c / 2] = pack_bf16(e);
+                    packed[c / 64][c % 64 / 2] = pack_bf16(e);
                 }
+                if (j > 0) {                        // the last probabilities have been used
+                    if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, gave_up))) break;
+                    tmem_fence_after();
+                }
+                tmem_store32(p_at, packed[0]);
+                tmem_store32(p_at + 32, packed[1]);
+                sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
+                tmem_wait_stores();
+                tmem_fence_before();
+                bar_arrive_warp(&sm.p_ready[w]);
             }
-            if (j > 0) {                        // the last probabilities have been used
-                if (!(ok = bar_wait(&sm.o_done[w], (j - 1) & 1, gave_up))) break;
+            mine += n_mine;
+            __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
+            if (ok && n_mine > 0) {
+                if (!(ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up))) break;
                 tmem_fence_after();
-            }
-            tmem_store32(p_at, packed[0]);
-            tmem_store32(p_at + 32, packed[1]);
-            sum += (part[0].x + part[0].y) + (part[1].x + part[1].y);
-            tmem_wait_stores();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.p_ready[w]);
-        }
-        const bool any = n_tiles[w] > 0;
-        if (any && ok) ok = bar_wait(&sm.o_done[w], (n_tiles[w] - 1) & 1, gave_up);
-        tmem_fence_after();
-        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
-        __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
-        if (any && ok) {
+                const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
-            for (int c = 0; c < DH; c += 32) {
-                uint32_t o[32];
-                tmem_load32(o_at + c, o);
-                tmem_wait_loads();
-                if (sum == 0.0f)
+                for (int c = 0; c < DH; c += 64) {
+                    uint32_t o[2][32];
+                    tmem_load32(o_at + c, o[0]);
+                    tmem_load32(o_at + c + 32, o[1]);
+                    tmem_wait_loads();
+                    if (c == DH - 64) {
+                        tmem_fence_before();
+                        bar_arrive_warp(&sm.o_taken[w]);
+                    }
+                    if (sum == 0.0f)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0;
-                if (row < p.len_q) write_columns(out, c, p.dim, o, by);
+                        for (int e = 0; e < 64; ++e) o[e / 32][e % 32] = 0;
+                    if (row < p.len_q) write_columns(out, c, p.dim, o[0], by), write_columns(out, c + 32, p.dim, o[1], by);
+                }
+            } else if (ok && row < p.len_q) {
+                write_zeros(out, 0, p.dim);
             }
-        } else if (row < p.len_q) {
-            write_zeros(out, 0, p.dim);
+            if (ok && row < p.len_q) p.lse[(static_cast<int64_t>(it.b) * p.heads + it.h) * p.len_q + row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
         }
-        if (row < p.len_q) p.lse[(static_cast<int64_t>(b) * p.heads + h) * p.len_q + row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+    } else {
+        registers_give<REGISTERS_HELP>();       // WARP_DP has nothing to do here, but its group gives back together
     }
     tmem_fence_before();
     __syncthreads();
     settle(gave_up);
-    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
 }
 
 // ----------------------------------------------------------------------------------- backward
@@ -388,195 +437,57 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
         uint16_t l[3], d[3];
         three_terms(empty ? HIDDEN : -lse / p.scale, l);
         three_terms(empty ? 0.0f : -delta, d);
+        if (at == 0) *p.next_item = 0;
         to.terms[at % TILE] = make_uint4(l[0] | l[1] << 16, l[2] | d[0] << 16, d[1] | d[2] << 16, 0);
     }
 }
 
-// dQ: 128 queries to a CTA, the two groups of four warps take its key tiles in turn.  Scores and dP are taken
-// into registers as soon as they are there, which frees their place for the next tile's.  Tensor memory:
-// scores 0, dP 128, dS 256 and 320, sums 384.
-template <int DH>
-struct DqSmem {
-    static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
-    static constexpr int K_SLOTS = DH == 64 ? 5 : 3, V_SLOTS = DH == 64 ? 3 : 2;
-    alignas(1024) uint8_t q[TILE_BYTES], dout[TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
-    uint64_t q_full, k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, dp_full[2], dp_taken, ds_ready[2], dq_done[2], sums_full, landed;
+// The backward pass in one launch, whose CTAs stay (Queue, with a counter: a CTA must not be handed a key tile
+// after a query tile): first the key tiles, whose work is the larger, then
+// the query tiles, each kind in the order of what a causal mask leaves it.  A CTA does key tiles until
+// it is handed its first query tile.  Barriers of both kinds are made at the start, and their phases are
+// counted on from item to item: the next item's tiles are fetched and its first products formed
+// while the last one's sums are written.
+struct DqBars {
+    static constexpr int K_MOST = 5, V_MOST = 3;
+    uint64_t q_full[2], q_free[2], k_full[K_MOST], k_free[K_MOST], v_full[V_MOST], v_free[V_MOST], s_full[2], s_taken, dp_full[2], dp_taken, ds_ready[2], dq_done[2], sums_full, sums_taken;
+};
+struct DkvBars {
+    static constexpr int Q_MOST = 4, DO_MOST = 3;
+    uint64_t kv_full[2], kv_free[2], q_full[Q_MOST], q_free[Q_MOST], do_full[DO_MOST], do_free[DO_MOST], s_full[2], s_taken, dp_full[2], dp_taken, p_ready[2], ds_ready[2], dv_done[2], dk_done[2],
+        sums_full, sums_taken;
+};
+struct BwdCommon {
+    Queue queue;
+    DqBars dq;
+    DkvBars dkv;
+    uint64_t landed;
     uint32_t tmem, gave_up;
 };
+constexpr uint32_t QUEUE_READERS = 4 + 8;       // the four warps of the third group, the eight that compute
 
+// dQ: 128 queries to an item, the two groups of four warps take its key tiles in turn (counted over all
+// items).  Scores and dP are taken into registers as soon as they are there, which frees their place for the
+// next tile's.  Tensor memory: scores 0, dP 128, dS 256 and 320, sums 384.
 template <int DH>
-__device__ __forceinline__ void dq_tile(uint8_t *raw, const int block, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, const CUtensorMap &map_do,
-                                        const AttnParams &p) {
-    using Smem = DqSmem<DH>;
-    auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int bh = block % (p.batch * p.heads), tile = p.tiles_q - 1 - block / (p.batch * p.heads), row0 = tile * TILE;
-    const int b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
-    const Seq seq(p, b);
-    const int n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
+struct DqTiles {
+    static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
+    static constexpr int SETS = DH == 64 ? 2 : 1, K_SLOTS = DH == 64 ? 5 : 3, V_SLOTS = DH == 64 ? 3 : 2;
+    alignas(1024) uint8_t q[SETS][TILE_BYTES], dout[SETS][TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
+};
 
-    if (threadIdx.x == 0) {
-        bar_init(&sm.q_full, 1);
-        bar_init(&sm.landed, 1);
-        for (int i = 0; i < Smem::K_SLOTS; ++i) bar_init(&sm.k_full[i], 1), bar_init(&sm.k_free[i], 1);
-        for (int i = 0; i < Smem::V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.dp_full[w], 1), bar_init(&sm.dq_done[w], 1), bar_init(&sm.ds_ready[w], 4);
-        bar_init(&sm.s_taken, 4), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
-        sm.gave_up = 0;
-        fence_async_smem();
+struct DqItem {
+    int tile, row0, b, h, h_kv, bh, n;          // n: key tiles
+    __device__ DqItem(const AttnParams &p, int block) {
+        const int all = p.batch * p.heads;
+        bh = block % all, tile = p.tiles_q - 1 - block / all, row0 = tile * TILE;
+        b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
+        const Seq seq(p, b);
+        n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
     }
-    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
-    tmem_fence_before();
-    __syncthreads();
-    tmem_fence_after();
-    const uint32_t tmem = sm.tmem;
-    volatile uint32_t *gave_up = &sm.gave_up;
+};
 
-    if (warp >= 8) registers_give<REGISTERS_HELP>();
-    if (warp == WARP_LOAD) {
-        if (n > 0) {
-            if (lane == 0) {
-                bar_expect(&sm.q_full, 2 * Smem::TILE_BYTES);
-                for (int c = 0; c < DH / 64; ++c) {
-                    copy_tile(smem_addr(sm.q) + c * CHUNK, &map_q, &sm.q_full, c * 64, row0, h, b);
-                    copy_tile(smem_addr(sm.dout) + c * CHUNK, &map_do, &sm.q_full, c * 64, row0, h, b);
-                }
-            }
-            __syncwarp();
-            uint32_t landed_phase = 0;
-            for (int j = 0; j < n; ++j) {
-                const int ks = j % Smem::K_SLOTS, vs = j % Smem::V_SLOTS;
-                if (!bar_wait(&sm.k_free[ks], (j / Smem::K_SLOTS + 1) & 1, gave_up)) break;
-                if (!load_tile<DH, true>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
-                if (!bar_wait(&sm.v_free[vs], (j / Smem::V_SLOTS + 1) & 1, gave_up)) break;
-                if (!load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, h_kv, b, gave_up)) break;
-            }
-        }
-    } else if (warp == WARP_SCORES) {
-        if (elected()) {
-            const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
-            for (int j = 0; j < n; ++j) {
-                const int ks = j % Smem::K_SLOTS;
-                if (j == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
-                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
-                if (j > 0 && !bar_wait_one(&sm.s_taken, (j - 1) & 1, gave_up)) break;
-                tmem_fence_after();
-                product_rows<DH, TILE>(tmem, q_at, k_at + ks * Smem::TILE_BYTES);
-                mma_commit(&sm.s_full[j & 1]);
-            }
-        }
-        __syncwarp();
-    } else if (warp == WARP_DP) {
-        if (elected()) {
-            const uint32_t do_at = smem_addr(sm.dout), v_at = smem_addr(sm.v);
-            for (int j = 0; j < n; ++j) {
-                const int vs = j % Smem::V_SLOTS;
-                if (j == 0 && !bar_wait_one(&sm.q_full, 0, gave_up)) break;
-                if (!bar_wait_one(&sm.v_full[vs], j / Smem::V_SLOTS & 1, gave_up)) break;
-                if (j > 0 && !bar_wait_one(&sm.dp_taken, (j - 1) & 1, gave_up)) break;
-                tmem_fence_after();
-                product_rows<DH, TILE>(tmem + TILE, do_at, v_at + vs * Smem::TILE_BYTES);
-                mma_commit(&sm.dp_full[j & 1]);
-                mma_commit(&sm.v_free[vs]);
-            }
-        }
-        __syncwarp();
-    } else if (warp == WARP_SUMS) {
-        if (elected()) {
-            const uint32_t k_at = smem_addr(sm.k);
-            for (int j = 0; j < n; ++j) {
-                const int ks = j % Smem::K_SLOTS;
-                if (!bar_wait_one(&sm.k_full[ks], j / Smem::K_SLOTS & 1, gave_up)) break;
-                if (!bar_wait_one(&sm.ds_ready[j & 1], j / 2 & 1, gave_up)) break;
-                tmem_fence_after();
-                product_down<DH, TILE>(tmem + 3 * TILE, tmem + 2 * TILE + (j & 1) * 64, k_at + ks * Smem::TILE_BYTES, j > 0);
-                mma_commit(&sm.dq_done[j & 1]);
-                mma_commit(&sm.k_free[ks]);                // dS came from the scores: that product is done as well
-                if (j == n - 1) mma_commit(&sm.sums_full);
-            }
-        }
-        __syncwarp();
-    } else if (warp < 8) {
-        registers_take<REGISTERS_COMPUTE>();
-        const int w = warp / 4, in_tile = threadIdx.x % TILE, row = row0 + in_tile;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, dp_at = lanes + TILE, ds_at = lanes + 2 * TILE + w * 64;
-        const int limit = seq.keys_of(row), all_see = seq.keys_of(row0);
-        const bool whole = row0 + TILE <= seq.n;
-        const QueryStats &stats = p.stats[static_cast<int64_t>(bh) * p.tiles_q + tile];
-        const float lse = stats.lse[in_tile], delta = stats.delta[in_tile];
-        bool ok = true;
-        for (int j = w; j < n; j += 2) {
-            if (!(ok = bar_wait(&sm.s_full[w], j / 2 & 1, gave_up))) break;
-            tmem_fence_after();
-            uint32_t s[4][32];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
-            tmem_wait_loads();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.s_taken);
-            if (!whole || (j + 1) * TILE > all_see) {
-                const int left = limit - j * TILE;           // columns that the row sees
-#pragma unroll
-                for (int c = 0; c < TILE; ++c)
-                    if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
-            }
-#pragma unroll
-            for (int c = 0; c < TILE; c += 2) {
-                const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
-                s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
-            }
-            if (!(ok = bar_wait(&sm.dp_full[w], j / 2 & 1, gave_up))) break;
-            tmem_fence_after();
-            uint32_t d[2][32], packed[4][16];
-            tmem_load32(dp_at, d[0]);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
-                tmem_wait_loads();
-                if (q < 3) {
-                    tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
-                } else {
-                    tmem_fence_before();
-                    bar_arrive_warp(&sm.dp_taken);
-                }
-#pragma unroll
-                for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta))));
-            }
-            if (j > 1) {                         // its last dS has been used
-                if (!(ok = bar_wait(&sm.dq_done[w], (j / 2 - 1) & 1, gave_up))) break;
-                tmem_fence_after();
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
-            tmem_wait_stores();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.ds_ready[w]);
-        }
-        if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
-        tmem_fence_after();
-        __nv_bfloat16 *out = p.out + b * p.out_stride[0] + row * p.out_stride[1] + h * p.out_stride[2];
-#pragma unroll
-        for (int c = 0; c < DH; c += 64) {            // the groups take turns of 32 columns
-            const int c0 = c + w * 32;
-            if (n > 0 && ok) {
-                uint32_t o[32];
-                tmem_load32(lanes + 3 * TILE + c0, o);
-                tmem_wait_loads();
-                if (limit == 0)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0;
-                if (row < p.len_q) write_columns(out, c0, p.dim, o, p.scale);
-            } else if (row < p.len_q) {
-                write_zeros(out, c0, min(c0 + 32, p.dim));
-            }
-        }
-    }
-    tmem_fence_before();
-    __syncthreads();
-    settle(gave_up);
-    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
-}
-
-// dK and dV: 128 keys to a CTA, which goes over the query tiles of every head that shares them.  All products
+// dK and dV: 128 keys to an item, which goes over the query tiles of every head that shares them.  All products
 // are taken transposed (rows are keys), so that P^T and dS^T are first operands from tensor memory.  Scores
 // and dP are taken into registers as soon as they are there.
 //   Heads of up to 64: the groups of four warps take tiles in turn.  Tensor memory: scores 0, dP 128, a
@@ -587,266 +498,552 @@ __device__ __forceinline__ void dq_tile(uint8_t *raw, const int block, const CUt
 // (Steps of 64 queries would leave room for turns there too, but a product of fewer than 128 columns takes
 // as long as one of 128.)
 template <int DH>
-struct DkvSmem {
+struct DkvTiles {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
     static constexpr bool TURNS = DH == 64;
     static constexpr uint32_t DP = TILE, MINE = 2 * TILE, DV = TURNS ? 384 : 256, DK = DV + DH;
-    static constexpr int Q_SLOTS = TURNS ? 4 : 2, DO_SLOTS = TURNS ? 3 : 2;
-    alignas(1024) uint8_t k[TILE_BYTES], v[TILE_BYTES], q[Q_SLOTS][TILE_BYTES], dout[DO_SLOTS][TILE_BYTES];
+    static constexpr int SETS = TURNS ? 2 : 1, Q_SLOTS = TURNS ? 4 : 2, DO_SLOTS = TURNS ? 3 : 2;
+    alignas(1024) uint8_t k[SETS][TILE_BYTES], v[SETS][TILE_BYTES], q[Q_SLOTS][TILE_BYTES], dout[DO_SLOTS][TILE_BYTES];
     alignas(128) uint4 ones_lse[TILE], ones_delta[TILE], terms[Q_SLOTS][TILE], zeros[TILE];      // zeros come last: product_short
-    uint64_t kv_full, q_full[Q_SLOTS], q_free[Q_SLOTS], do_full[DO_SLOTS], do_free[DO_SLOTS], s_full[2], s_taken, dp_full[2], p_ready[2], dp_taken, ds_ready[2], dv_done[2], dk_done[2], sums_full, landed;
-    uint32_t tmem, gave_up;
+};
+
+struct DkvItem {
+    int key0, b, h_kv, shared, first, per_head, n;       // query tiles: from `first` on, so many to a head, over all heads
+    __device__ DkvItem(const AttnParams &p, int block) {
+        const int all = p.batch * p.heads_kv, bh = block % all;
+        key0 = block / all * TILE;                        // early keys are seen most
+        b = bh / p.heads_kv, h_kv = bh % p.heads_kv, shared = p.heads / p.heads_kv;
+        const Seq seq(p, b);
+        first = seq.first_query_of(key0) / TILE;
+        per_head = key0 < seq.m ? max(0, tiles(seq.n) - first) : 0;
+        n = per_head * shared;
+    }
 };
 
 template <int DH>
-__device__ __forceinline__ void dkv_tile(uint8_t *raw, const int block, const CUtensorMap &map_q, const CUtensorMap &map_k, const CUtensorMap &map_v, const CUtensorMap &map_do,
-                                        const AttnParams &p) {
-    using Smem = DkvSmem<DH>;
-    auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int bh = block % (p.batch * p.heads_kv), key0 = block / (p.batch * p.heads_kv) * TILE;    // early keys are seen most
-    const int b = bh / p.heads_kv, h_kv = bh % p.heads_kv, shared = p.heads / p.heads_kv;
-    const Seq seq(p, b);
-    const int first = seq.first_query_of(key0) / TILE, per_head = key0 < seq.m ? max(0, tiles(seq.n) - first) : 0, n = per_head * shared;
+struct BwdSmem {
+    union {
+        DqTiles<DH> dq;
+        DkvTiles<DH> dkv;
+    };
+    BwdCommon common;
+};
+
+template <int DH>
+__global__ void __launch_bounds__(THREADS, 1)
+k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
+    extern __shared__ uint8_t raw[];
+    using Dq = DqTiles<DH>;
+    using Dkv = DkvTiles<DH>;
+    constexpr uint32_t TILE_BYTES = Dq::TILE_BYTES;
+    auto &sm = *reinterpret_cast<BwdSmem<DH> *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    BwdCommon &cm = sm.common;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, key_items = p.batch * p.heads_kv * p.tiles_kv, all_items = key_items + p.batch * p.heads * p.tiles_q;
 
     if (threadIdx.x == 0) {
-        bar_init(&sm.kv_full, 1);
-        bar_init(&sm.landed, 1);
-        for (int i = 0; i < Smem::Q_SLOTS; ++i) bar_init(&sm.q_full[i], 1), bar_init(&sm.q_free[i], 1);
-        for (int i = 0; i < Smem::DO_SLOTS; ++i) bar_init(&sm.do_full[i], 1), bar_init(&sm.do_free[i], 1);
-        for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.dp_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.ds_ready[w], 4), bar_init(&sm.dv_done[w], 1), bar_init(&sm.dk_done[w], 1);
-        bar_init(&sm.s_taken, Smem::TURNS ? 4 : 8), bar_init(&sm.dp_taken, 4), bar_init(&sm.sums_full, 1);
-        sm.gave_up = 0;
+        queue_init(cm.queue, QUEUE_READERS);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&cm.dq.q_full[i], 1), bar_init(&cm.dq.q_free[i], 1), bar_init(&cm.dkv.kv_full[i], 1), bar_init(&cm.dkv.kv_free[i], 1);
+            bar_init(&cm.dq.s_full[i], 1), bar_init(&cm.dq.dp_full[i], 1), bar_init(&cm.dq.ds_ready[i], 4), bar_init(&cm.dq.dq_done[i], 1);
+            bar_init(&cm.dkv.s_full[i], 1), bar_init(&cm.dkv.dp_full[i], 1), bar_init(&cm.dkv.p_ready[i], 4), bar_init(&cm.dkv.ds_ready[i], 4);
+            bar_init(&cm.dkv.dv_done[i], 1), bar_init(&cm.dkv.dk_done[i], 1);
+        }
+        for (int i = 0; i < DqBars::K_MOST; ++i) bar_init(&cm.dq.k_full[i], 1), bar_init(&cm.dq.k_free[i], 1);
+        for (int i = 0; i < DqBars::V_MOST; ++i) bar_init(&cm.dq.v_full[i], 1), bar_init(&cm.dq.v_free[i], 1);
+        for (int i = 0; i < DkvBars::Q_MOST; ++i) bar_init(&cm.dkv.q_full[i], 1), bar_init(&cm.dkv.q_free[i], 1);
+        for (int i = 0; i < DkvBars::DO_MOST; ++i) bar_init(&cm.dkv.do_full[i], 1), bar_init(&cm.dkv.do_free[i], 1);
+        bar_init(&cm.dq.s_taken, 4), bar_init(&cm.dq.dp_taken, 4), bar_init(&cm.dq.sums_full, 1), bar_init(&cm.dq.sums_taken, 8);
+        bar_init(&cm.dkv.s_taken, Dkv::TURNS ? 4 : 8), bar_init(&cm.dkv.dp_taken, 4), bar_init(&cm.dkv.sums_full, 1), bar_init(&cm.dkv.sums_taken, 8);
+        bar_init(&cm.landed, 1);
+        cm.gave_up = 0;
     }
-    if (threadIdx.x < TILE) {
+    if (threadIdx.x < TILE && static_cast<int>(blockIdx.x) < key_items) {
         constexpr uint32_t ONE = 0x3F80;                 // bf16
-        sm.ones_lse[threadIdx.x] = make_uint4(ONE | ONE << 16, ONE, 0, 0);
-        sm.ones_delta[threadIdx.x] = make_uint4(0, ONE << 16, ONE | ONE << 16, 0);
-        sm.zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
+        sm.dkv.ones_lse[threadIdx.x] = make_uint4(ONE | ONE << 16, ONE, 0, 0);
+        sm.dkv.ones_delta[threadIdx.x] = make_uint4(0, ONE << 16, ONE | ONE << 16, 0);
+        sm.dkv.zeros[threadIdx.x] = make_uint4(0, 0, 0, 0);
     }
     fence_async_smem();
-    if (warp == WARP_SCORES && n > 0) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
+    if (warp == WARP_SCORES) tmem_alloc(&cm.tmem, TMEM_COLUMNS);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const uint32_t tmem = sm.tmem;
-    volatile uint32_t *gave_up = &sm.gave_up;
+    const uint32_t tmem = cm.tmem;
+    volatile uint32_t *gave_up = &cm.gave_up;
 
-    if (warp >= 8) registers_give<REGISTERS_HELP>();
-    if (warp == WARP_LOAD) {
-        if (n > 0) {
-            if (lane == 0) {
-                bar_expect(&sm.kv_full, 2 * Smem::TILE_BYTES);
-                for (int c = 0; c < DH / 64; ++c) {
-                    copy_tile(smem_addr(sm.k) + c * CHUNK, &map_k, &sm.kv_full, c * 64, key0, h_kv, b);
-                    copy_tile(smem_addr(sm.v) + c * CHUNK, &map_v, &sm.kv_full, c * 64, key0, h_kv, b);
+    int block = blockIdx.x;                     // every role goes through the same items
+    uint32_t items = 0, landed_phase = 0;       // answers read
+    bool ok = true;
+    auto next = [&] { block = queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto next_one = [&] { block = queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto all_done = [&] {                       // of the key tiles, in all roles
+        fence_async_smem();
+        tmem_fence_before();
+        asm volatile("barrier.sync 1, %0;" ::"n"(THREADS) : "memory");
+        tmem_fence_after();
+        if (*gave_up) ok = false;
+    };
+    auto ask = [&] {                            // once to an item, by the warp that brings the tiles
+        if (!bar_wait(&cm.queue.free[items % QUEUE], (items / QUEUE + 1) & 1, gave_up)) return false;
+        if (lane == 0) queue_count(cm.queue, items, p.next_item, all_items);
+        __syncwarp();
+        return true;
+    };
+
+    // dP, or the sums (with heads of up to 128 both, in the sums' thread), of the key tiles
+    auto dkv_products = [&](const bool sums) {
+        if (elected()) {
+            DkvBars &bars = cm.dkv;
+            const uint32_t zeros = smem_addr(sm.dkv.zeros), v_at = smem_addr(sm.dkv.v), q_at = smem_addr(sm.dkv.q), do_at = smem_addr(sm.dkv.dout), terms_at = smem_addr(sm.dkv.terms),
+                           ones = smem_addr(sm.dkv.ones_delta);
+            uint32_t sets = 0, tiles_in = 0;
+            auto dprobs = [&](uint32_t g, uint32_t set) {
+                const uint32_t qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
+                if (!bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up)) return false;        // delta comes with the queries
+                if (!bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, gave_up)) return false;
+                if (Dkv::TURNS && g > 0 && !bar_wait_one(&bars.dp_taken, (g - 1) & 1, gave_up)) return false;
+                tmem_fence_after();
+                product_short<TILE>(tmem + Dkv::DP, ones, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tmem + Dkv::DP, v_at + set * TILE_BYTES, do_at + ds * TILE_BYTES, true);
+                mma_commit(&bars.dp_full[Dkv::TURNS ? g & 1 : 0]);
+                return true;
+            };
+            while (ok && block < key_items) {
+                const DkvItem it(p, block);
+                const uint32_t set = sets % Dkv::SETS;
+                if (it.n > 0 && (sums || Dkv::TURNS)) {
+                    ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up);
+                    if (sums && sets > 0 && ok) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
+                    ++sets;
                 }
+                if (!sums) {
+                    if (Dkv::TURNS)
+                        for (int i = 0; ok && i < it.n; ++i) ok = dprobs(tiles_in + i, set);
+                } else if (Dkv::TURNS) {
+                    for (int i = 0; ok && i < it.n; ++i) {
+                        const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS, w = g & 1;
+                        ok = bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, gave_up) && bar_wait_one(&bars.p_ready[w], g / 2 & 1, gave_up);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        product_down<DH, TILE>(tmem + Dkv::DV, tmem + Dkv::MINE + w * 64, do_at + ds * TILE_BYTES, i > 0);
+                        mma_commit(&bars.dv_done[w]);
+                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up) && bar_wait_one(&bars.ds_ready[w], g / 2 & 1, gave_up);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        product_down<DH, TILE>(tmem + Dkv::DK, tmem + Dkv::MINE + w * 64, q_at + qs * TILE_BYTES, i > 0);
+                        mma_commit(&bars.dk_done[w]);
+                        mma_commit(&bars.q_free[qs]);           // dS came from scores and dP: all products with the two tiles are done
+                        mma_commit(&bars.do_free[ds]);
+                    }
+                } else if (it.n > 0 && ok) {                     // dP takes the place of P and dS: one thread, in order
+                    ok = dprobs(tiles_in, set);
+                    for (int i = 0; ok && i < it.n; ++i) {
+                        const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
+                        for (int w = 0; w < 2 && ok; ++w) {     // each group's 64 queries; dK first: there is room for two query tiles only
+                            ok = bar_wait_one(&bars.ds_ready[w], g & 1, gave_up);
+                            if (!ok) break;
+                            tmem_fence_after();
+                            product_down<DH, 64>(tmem + Dkv::DK, tmem + Dkv::DP + w * 64 + 32, q_at + qs * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
+                        }
+                        if (!ok) break;
+                        mma_commit(&bars.q_free[qs]);
+                        for (int w = 0; w < 2; ++w) product_down<DH, 64>(tmem + Dkv::DV, tmem + Dkv::DP + w * 64, do_at + ds * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
+                        mma_commit(&bars.do_free[ds]);
+                        if (i + 1 < it.n) ok = dprobs(g + 1, set);
+                    }
+                }
+                if (sums && it.n > 0 && ok) {
+                    mma_commit(&bars.sums_full);
+                    mma_commit(&bars.kv_free[set]);
+                }
+                tiles_in += it.n;
+                if (ok) next_one();
             }
-            __syncwarp();
-            uint32_t landed_phase = 0;
-            for (int i = 0; i < n; ++i) {
-                const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS, h = h_kv * shared + i / per_head, tile = first + i % per_head;
-                if (!bar_wait(&sm.q_free[qs], (i / Smem::Q_SLOTS + 1) & 1, gave_up)) break;
-                // the terms arrive at the queries' barrier: their bytes are announced without an arrival
-                if (lane == 0) {
-                    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&sm.q_full[qs])), "r"(static_cast<uint32_t>(sizeof(sm.terms[0]))) : "memory");
-                    copy_bytes(smem_addr(sm.terms[qs]), p.stats[(static_cast<int64_t>(b) * p.heads + h) * p.tiles_q + tile].terms, sizeof(sm.terms[0]), &sm.q_full[qs]);
+        }
+        __syncwarp();
+    };
+    // scores, or dP, of the query tiles: products of one form
+    auto dq_products = [&](const bool is_dp) {
+        if (elected()) {
+            // two products of the same form: scores from Q and K, dP from dO and V
+            DqBars &bars = cm.dq;
+            const uint32_t a_at = is_dp ? smem_addr(sm.dq.dout) : smem_addr(sm.dq.q), b_at = is_dp ? smem_addr(sm.dq.v) : smem_addr(sm.dq.k), slots = is_dp ? Dq::V_SLOTS : Dq::K_SLOTS;
+            uint64_t *const full = is_dp ? bars.v_full : bars.k_full, *const taken = is_dp ? &bars.dp_taken : &bars.s_taken, *const done = is_dp ? bars.dp_full : bars.s_full;
+            uint32_t sets = 0, tiles_in = 0;
+            while (ok) {
+                const DqItem it(p, block - key_items);
+                const uint32_t set = sets % Dq::SETS;
+                if (it.n > 0) ok = bar_wait_one(&bars.q_full[set], sets / Dq::SETS & 1, gave_up), ++sets;
+                for (int j = 0; ok && j < it.n; ++j) {
+                    const uint32_t g = tiles_in + j, slot = g % slots;
+                    ok = bar_wait_one(&full[slot], g / slots & 1, gave_up) && (g == 0 || bar_wait_one(taken, (g - 1) & 1, gave_up));
+                    if (!ok) break;
+                    tmem_fence_after();
+                    product_rows<DH, TILE>(tmem + (is_dp ? TILE : 0), a_at + set * TILE_BYTES, b_at + slot * TILE_BYTES);
+                    mma_commit(&done[g & 1]);
+                    if (is_dp) mma_commit(&bars.v_free[slot]);
                 }
-                __syncwarp();
-                if (!load_tile<DH, true>(smem_addr(sm.q[qs]), sm.q[qs], &map_q, &sm.q_full[qs], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
-                if (!bar_wait(&sm.do_free[ds], (i / Smem::DO_SLOTS + 1) & 1, gave_up)) break;
-                if (!load_tile<DH, true>(smem_addr(sm.dout[ds]), sm.dout[ds], &map_do, &sm.do_full[ds], &sm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, b, gave_up)) break;
+                tiles_in += it.n;
+                if (ok) next_one();
+            }
+        }
+        __syncwarp();
+    };
+    if (warp == WARP_LOAD) {
+        registers_give<REGISTERS_HELP>();
+        {
+            DkvBars &bars = cm.dkv;
+            uint32_t sets = 0, tiles_in = 0;        // counts over all items
+            while (ok && block < key_items) {
+                if (!(ok = ask())) break;
+                const DkvItem it(p, block);
+                const Seq seq(p, it.b);
+                if (it.n > 0) {
+                    const uint32_t set = sets % Dkv::SETS;
+                    if (!(ok = bar_wait(&bars.kv_free[set], (sets / Dkv::SETS + 1) & 1, gave_up))) break;
+                    ++sets;
+                    if (lane == 0) {
+                        bar_expect(&bars.kv_full[set], 2 * TILE_BYTES);
+                        for (int c = 0; c < DH / 64; ++c) {
+                            copy_tile(smem_addr(sm.dkv.k[set]) + c * CHUNK, &map_k, &bars.kv_full[set], c * 64, it.key0, it.h_kv, it.b);
+                            copy_tile(smem_addr(sm.dkv.v[set]) + c * CHUNK, &map_v, &bars.kv_full[set], c * 64, it.key0, it.h_kv, it.b);
+                        }
+                    }
+                    __syncwarp();
+                    for (int i = 0; ok && i < it.n; ++i) {
+                        const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
+                        const int h = it.h_kv * it.shared + i / it.per_head, tile = it.first + i % it.per_head;
+                        if (!(ok = bar_wait(&bars.q_free[qs], (g / Dkv::Q_SLOTS + 1) & 1, gave_up))) break;
+                        // the terms arrive at the queries' barrier: their bytes are announced without an arrival
+                        if (lane == 0) {
+                            asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&bars.q_full[qs])), "r"(static_cast<uint32_t>(sizeof(sm.dkv.terms[0]))) : "memory");
+                            copy_bytes(smem_addr(sm.dkv.terms[qs]), p.stats[(static_cast<int64_t>(it.b) * p.heads + h) * p.tiles_q + tile].terms, sizeof(sm.dkv.terms[0]), &bars.q_full[qs]);
+                        }
+                        __syncwarp();
+                        ok = load_tile<DH, true>(smem_addr(sm.dkv.q[qs]), sm.dkv.q[qs], &map_q, &bars.q_full[qs], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, gave_up) &&
+                             bar_wait(&bars.do_free[ds], (g / Dkv::DO_SLOTS + 1) & 1, gave_up) &&
+                             load_tile<DH, true>(smem_addr(sm.dkv.dout[ds]), sm.dkv.dout[ds], &map_do, &bars.do_full[ds], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, gave_up);
+                    }
+                    tiles_in += it.n;
+                }
+                if (ok) next();
+            }
+        }
+        // Query tiles next, whose data comes where that of the key tiles was: dQ.
+        all_done();
+        {
+            DqBars &bars = cm.dq;
+            uint32_t sets = 0, tiles_in = 0;
+            while (ok) {
+                if (!(ok = ask())) break;
+                const DqItem it(p, block - key_items);
+                const Seq seq(p, it.b);
+                if (it.n > 0) {
+                    const uint32_t set = sets % Dq::SETS;
+                    if (!(ok = bar_wait(&bars.q_free[set], (sets / Dq::SETS + 1) & 1, gave_up))) break;
+                    ++sets;
+                    if (lane == 0) {
+                        bar_expect(&bars.q_full[set], 2 * TILE_BYTES);
+                        for (int c = 0; c < DH / 64; ++c) {
+                            copy_tile(smem_addr(sm.dq.q[set]) + c * CHUNK, &map_q, &bars.q_full[set], c * 64, it.row0, it.h, it.b);
+                            copy_tile(smem_addr(sm.dq.dout[set]) + c * CHUNK, &map_do, &bars.q_full[set], c * 64, it.row0, it.h, it.b);
+                        }
+                    }
+                    __syncwarp();
+                    for (int j = 0; ok && j < it.n; ++j) {
+                        const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS, vs = g % Dq::V_SLOTS;
+                        ok = bar_wait(&bars.k_free[ks], (g / Dq::K_SLOTS + 1) & 1, gave_up) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
+                             bar_wait(&bars.v_free[vs], (g / Dq::V_SLOTS + 1) & 1, gave_up) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                    }
+                    tiles_in += it.n;
+                }
+                if (ok) next();
             }
         }
     } else if (warp == WARP_SCORES) {
-        if (elected()) {
-            const uint32_t zeros = smem_addr(sm.zeros), k_at = smem_addr(sm.k), q_at = smem_addr(sm.q), terms_at = smem_addr(sm.terms), ones = smem_addr(sm.ones_lse);
-            for (int i = 0; i < n; ++i) {
-                const int qs = i % Smem::Q_SLOTS;
-                if (i == 0 && !bar_wait_one(&sm.kv_full, 0, gave_up)) break;
-                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) break;
-                if (i > 0 && !bar_wait_one(&sm.s_taken, (i - 1) & 1, gave_up)) break;
-                tmem_fence_after();
-                product_short<TILE>(tmem, ones, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tmem, k_at, q_at + qs * Smem::TILE_BYTES, true);
-                mma_commit(&sm.s_full[Smem::TURNS ? i & 1 : 0]);
-            }
-        }
-        __syncwarp();
-    } else if (warp == WARP_DP || warp == WARP_SUMS) {
-        if (elected()) {
-            const uint32_t zeros = smem_addr(sm.zeros), v_at = smem_addr(sm.v), q_at = smem_addr(sm.q), do_at = smem_addr(sm.dout), terms_at = smem_addr(sm.terms),
-                           ones = smem_addr(sm.ones_delta);
-            auto dprobs = [&](int i) {
-                const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
-                if (i == 0 && !bar_wait_one(&sm.kv_full, 0, gave_up)) return false;
-                if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) return false;        // delta comes with the queries
-                if (!bar_wait_one(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) return false;
-                if (Smem::TURNS && i > 0 && !bar_wait_one(&sm.dp_taken, (i - 1) & 1, gave_up)) return false;
-                tmem_fence_after();
-                product_short<TILE>(tmem + Smem::DP, ones, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tmem + Smem::DP, v_at, do_at + ds * Smem::TILE_BYTES, true);
-                mma_commit(&sm.dp_full[Smem::TURNS ? i & 1 : 0]);
-                return true;
-            };
-            if (Smem::TURNS && warp == WARP_DP) {
-                for (int i = 0; i < n; ++i)
-                    if (!dprobs(i)) break;
-            } else if (Smem::TURNS) {
-                for (int i = 0; i < n; ++i) {
-                    const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS, w = i & 1;
-                    if (!bar_wait_one(&sm.do_full[ds], i / Smem::DO_SLOTS & 1, gave_up)) break;
-                    if (!bar_wait_one(&sm.p_ready[w], i / 2 & 1, gave_up)) break;
-                    tmem_fence_after();
-                    product_down<DH, TILE>(tmem + Smem::DV, tmem + Smem::MINE + w * 64, do_at + ds * Smem::TILE_BYTES, i > 0);
-                    mma_commit(&sm.dv_done[w]);
-                    if (!bar_wait_one(&sm.q_full[qs], i / Smem::Q_SLOTS & 1, gave_up)) break;
-                    if (!bar_wait_one(&sm.ds_ready[w], i / 2 & 1, gave_up)) break;
-                    tmem_fence_after();
-                    product_down<DH, TILE>(tmem + Smem::DK, tmem + Smem::MINE + w * 64, q_at + qs * Smem::TILE_BYTES, i > 0);
-                    mma_commit(&sm.dk_done[w]);
-                    mma_commit(&sm.q_free[qs]);           // dS came from scores and dP: all products with the two tiles are done
-                    mma_commit(&sm.do_free[ds]);
-                    if (i == n - 1) mma_commit(&sm.sums_full);
-                }
-            } else if (warp == WARP_SUMS && n > 0 && dprobs(0)) {      // dP takes the place of P and dS: one thread, in order
-                for (int i = 0; i < n; ++i) {
-                    const int qs = i % Smem::Q_SLOTS, ds = i % Smem::DO_SLOTS;
-                    bool ok = true;
-                    for (int g = 0; g < 2 && ok; ++g) {           // each group's 64 queries; dK first: there is room for two query tiles only
-                        ok = bar_wait_one(&sm.ds_ready[g], i & 1, gave_up);
+        registers_give<REGISTERS_HELP>();
+        {
+            if (elected()) {
+                DkvBars &bars = cm.dkv;
+                const uint32_t zeros = smem_addr(sm.dkv.zeros), k_at = smem_addr(sm.dkv.k), q_at = smem_addr(sm.dkv.q), terms_at = smem_addr(sm.dkv.terms), ones = smem_addr(sm.dkv.ones_lse);
+                uint32_t sets = 0, tiles_in = 0;
+                while (ok && block < key_items) {
+                    const DkvItem it(p, block);
+                    const uint32_t set = sets % Dkv::SETS;
+                    if (it.n > 0) ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up), ++sets;
+                    for (int i = 0; ok && i < it.n; ++i) {
+                        const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS;
+                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up) && (g == 0 || bar_wait_one(&bars.s_taken, (g - 1) & 1, gave_up));
                         if (!ok) break;
                         tmem_fence_after();
-                        product_down<DH, 64>(tmem + Smem::DK, tmem + Smem::DP + g * 64 + 32, q_at + qs * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
+                        product_short<TILE>(tmem, ones, terms_at + qs * TILE * 16, zeros);
+                        product_rows<DH, TILE>(tmem, k_at + set * TILE_BYTES, q_at + qs * TILE_BYTES, true);
+                        mma_commit(&bars.s_full[Dkv::TURNS ? g & 1 : 0]);
                     }
-                    if (!ok) break;
-                    mma_commit(&sm.q_free[qs]);
-                    for (int g = 0; g < 2; ++g)
-                        product_down<DH, 64>(tmem + Smem::DV, tmem + Smem::DP + g * 64, do_at + ds * Smem::TILE_BYTES + g * 64 * 128, i > 0 || g > 0);
-                    mma_commit(&sm.do_free[ds]);
-                    if (i == n - 1) mma_commit(&sm.sums_full);
-                    if (i + 1 < n && !dprobs(i + 1)) break;
+                    tiles_in += it.n;
+                    if (ok) next_one();
                 }
             }
+            __syncwarp();
         }
-        __syncwarp();
-    } else if (warp < 8) {
+        // Query tiles next, whose data comes where that of the key tiles was: dQ.
+        all_done();
+        dq_products(false);
+    } else if (warp == WARP_DP) {
+        registers_give<REGISTERS_HELP>();
+        dkv_products(false);
+        // Query tiles next, whose data comes where that of the key tiles was: dQ.
+        all_done();
+        dq_products(true);
+    } else if (warp == WARP_SUMS) {
+        registers_give<REGISTERS_HELP>();
+        dkv_products(true);
+        // Query tiles next, whose data comes where that of the key tiles was: dQ.
+        all_done();
+        {
+            if (elected()) {
+                DqBars &bars = cm.dq;
+                const uint32_t k_at = smem_addr(sm.dq.k);
+                uint32_t sets = 0, tiles_in = 0;
+                while (ok) {
+                    const DqItem it(p, block - key_items);
+                    if (it.n > 0 && sets > 0) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
+                    for (int j = 0; ok && j < it.n; ++j) {
+                        const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS;
+                        ok = bar_wait_one(&bars.k_full[ks], g / Dq::K_SLOTS & 1, gave_up) && bar_wait_one(&bars.ds_ready[g & 1], g / 2 & 1, gave_up);
+                        if (!ok) break;
+                        tmem_fence_after();
+                        product_down<DH, TILE>(tmem + 3 * TILE, tmem + 2 * TILE + (g & 1) * 64, k_at + ks * TILE_BYTES, j > 0);
+                        mma_commit(&bars.dq_done[g & 1]);
+                        mma_commit(&bars.k_free[ks]);                // dS came from the scores: that product is done as well
+                    }
+                    if (it.n > 0 && ok) {
+                        mma_commit(&bars.sums_full);
+                        mma_commit(&bars.q_free[sets % Dq::SETS]);
+                        ++sets;
+                    }
+                    tiles_in += it.n;
+                    if (ok) next_one();
+                }
+            }
+            __syncwarp();
+        }
+    } else {
         registers_take<REGISTERS_COMPUTE>();
-        constexpr int WIDTH = Smem::TURNS ? TILE : TILE / 2, EVERY = Smem::TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
-        const int w = warp / 4, key = key0 + threadIdx.x % TILE, col0 = Smem::TURNS ? 0 : w * WIDTH;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + col0, dp_at = lanes + Smem::DP + col0;
-        // A group that takes turns has barriers of its own: one that is waited for only every other time would
-        // tell its phases apart by nothing.
-        uint64_t *const s_full = &sm.s_full[Smem::TURNS ? w : 0], *const dp_full = &sm.dp_full[Smem::TURNS ? w : 0];
-        const uint32_t p_at = Smem::TURNS ? lanes + Smem::MINE + w * 64 : dp_at, ds_at = Smem::TURNS ? p_at : dp_at + 32;
-        bool ok = true;
-        for (int i = Smem::TURNS ? w : 0; i < n; i += EVERY) {
-            const int row0 = (first + i % per_head) * TILE;
-            // columns before `hidden` do not see the key
-            const int hidden = seq.causal && row0 < key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
-            if (!(ok = bar_wait(s_full, i / EVERY & 1, gave_up))) break;
-            tmem_fence_after();
-            uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
-#pragma unroll
-            for (int q = 0; q < WIDTH / 32; ++q) tmem_load32(s_at + q * 32, s[q]);
-            tmem_wait_loads();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.s_taken);
-            if (__any_sync(0xFFFFFFFFu, hidden > 0)) {
-#pragma unroll
-                for (int c = 0; c < WIDTH; ++c)
-                    if (c < hidden) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
-            }
-#pragma unroll
-            for (int c = 0; c < WIDTH; c += 2) {
-                const float2 x = mul2(pair_of(s[c / 32], c % 32), both(p.scale_log2));
-                const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
-                s[c / 32][c % 32] = __float_as_uint(e.x), s[c / 32][c % 32 + 1] = __float_as_uint(e.y);
-                probs[c / 64][c % 64 / 2] = pack_bf16(e);
-            }
-            if constexpr (Smem::TURNS) {
-                if (i > 1) {                         // its last dS has been used
-                    if (!(ok = bar_wait(&sm.dk_done[w], (i / 2 - 1) & 1, gave_up))) break;
+        {
+            DkvBars &bars = cm.dkv;
+            constexpr int WIDTH = Dkv::TURNS ? TILE : TILE / 2, EVERY = Dkv::TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
+            const int w = warp / 4, col0 = Dkv::TURNS ? 0 : w * WIDTH;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + col0, dp_at = lanes + Dkv::DP + col0;
+            // A group that takes turns has barriers of its own: one that is waited for only every other time would
+            // tell its phases apart by nothing.
+            uint64_t *const s_full = &bars.s_full[Dkv::TURNS ? w : 0], *const dp_full = &bars.dp_full[Dkv::TURNS ? w : 0];
+            const uint32_t p_at = Dkv::TURNS ? lanes + Dkv::MINE + w * 64 : dp_at, ds_at = Dkv::TURNS ? p_at : dp_at + 32;
+            uint32_t tiles_in = 0, outputs = 0;
+            while (ok && block < key_items) {
+                const DkvItem it(p, block);
+                const Seq seq(p, it.b);
+                const int key = it.key0 + threadIdx.x % TILE;
+                int i = Dkv::TURNS ? static_cast<int>((tiles_in + w) & 1) : 0, column = i;                       // query tile of its head
+                for (; i < it.n; i += EVERY, column += EVERY) {
+                    const uint32_t g = tiles_in + i;
+                    while (column >= it.per_head) column -= it.per_head;
+                    const int row0 = (it.first + column) * TILE;
+                    // columns before `hidden` do not see the key
+                    const int hidden = seq.causal && row0 < it.key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
+                    if (!(ok = bar_wait(s_full, g / EVERY & 1, gave_up))) break;
                     tmem_fence_after();
-                }
-                tmem_store32(p_at, probs[0]);
-                tmem_store32(p_at + 32, probs[WIDTH / 64 - 1]);
-                tmem_wait_stores();
-                tmem_fence_before();
-                bar_arrive_warp(&sm.p_ready[w]);
-            }
-            if (!(ok = bar_wait(dp_full, i / EVERY & 1, gave_up))) break;
-            tmem_fence_after();
-            uint32_t d[2][32];
-            if constexpr (Smem::TURNS) {
-                uint32_t packed[4][16];
-                tmem_load32(dp_at, d[0]);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
+                    uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
+    #pragma unroll
+                    for (int q = 0; q < WIDTH / 32; ++q) tmem_load32(s_at + q * 32, s[q]);
                     tmem_wait_loads();
-                    if (q < 3) {
-                        tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
-                    } else {
-                        tmem_fence_before();
-                        bar_arrive_warp(&sm.dp_taken);
+                    tmem_fence_before();
+                    bar_arrive_warp(&bars.s_taken);
+                    if (__any_sync(0xFFFFFFFFu, hidden > 0)) {
+    #pragma unroll
+                        for (int c = 0; c < WIDTH; ++c)
+                            if (c < hidden) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
                     }
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), pair_of(d[q % 2], c)));
+    #pragma unroll
+                    for (int c = 0; c < WIDTH; c += 2) {
+                        const float2 x = mul2(pair_of(s[c / 32], c % 32), both(p.scale_log2));
+                        const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
+                        s[c / 32][c % 32] = __float_as_uint(e.x), s[c / 32][c % 32 + 1] = __float_as_uint(e.y);
+                        probs[c / 64][c % 64 / 2] = pack_bf16(e);
+                    }
+                    if constexpr (Dkv::TURNS) {
+                        if (g > 1) {                         // its last dS has been used
+                            if (!(ok = bar_wait(&bars.dk_done[w], (g / 2 - 1) & 1, gave_up))) break;
+                            tmem_fence_after();
+                        }
+                        tmem_store32(p_at, probs[0]);
+                        tmem_store32(p_at + 32, probs[WIDTH / 64 - 1]);
+                        tmem_wait_stores();
+                        tmem_fence_before();
+                        bar_arrive_warp(&bars.p_ready[w]);
+                    }
+                    if (!(ok = bar_wait(dp_full, g / EVERY & 1, gave_up))) break;
+                    tmem_fence_after();
+                    uint32_t d[2][32];
+                    if constexpr (Dkv::TURNS) {
+                        uint32_t packed[4][16];
+                        tmem_load32(dp_at, d[0]);
+    #pragma unroll
+                        for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
+                            tmem_wait_loads();
+                            if (q < 3) {
+                                tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
+                            } else {
+                                tmem_fence_before();
+                                bar_arrive_warp(&bars.dp_taken);
+                            }
+    #pragma unroll
+                            for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), pair_of(d[q % 2], c)));
+                        }
+                        if (!(ok = bar_wait(&bars.dv_done[w], g / 2 & 1, gave_up))) break;        // P has been used
+                        tmem_fence_after();
+    #pragma unroll
+                        for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
+                    } else {
+                        tmem_load32(dp_at, d[0]);
+                        tmem_load32(dp_at + 32, d[1]);
+                        tmem_wait_loads();
+                        tmem_store32(p_at, probs[0]);
+                        uint32_t packed[32];
+    #pragma unroll
+                        for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[c / 32], c % 32), pair_of(d[c / 32], c % 32)));
+                        tmem_store32(ds_at, packed);
+                    }
+                    tmem_wait_stores();
+                    tmem_fence_before();
+                    bar_arrive_warp(&bars.ds_ready[w]);
                 }
-                if (!(ok = bar_wait(&sm.dv_done[w], i / 2 & 1, gave_up))) break;        // P has been used
-                tmem_fence_after();
-#pragma unroll
-                for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
-            } else {
-                tmem_load32(dp_at, d[0]);
-                tmem_load32(dp_at + 32, d[1]);
-                tmem_wait_loads();
-                tmem_store32(p_at, probs[0]);
-                uint32_t packed[32];
-#pragma unroll
-                for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[c / 32], c % 32), pair_of(d[c / 32], c % 32)));
-                tmem_store32(ds_at, packed);
+                if (!ok) break;
+                tiles_in += it.n;
+                // one group writes dV, the other dK
+                const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
+                __nv_bfloat16 *out = (w == 0 ? p.dv : p.dk) + it.b * stride[0] + key * stride[1] + it.h_kv * stride[2];
+                if (it.n > 0) {
+                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
+                    ++outputs;
+                    tmem_fence_after();
+    #pragma unroll
+                    for (int c = 0; c < DH; c += 64) {
+                        uint32_t o[2][32];
+                        tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c, o[0]);
+                        tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c + 32, o[1]);
+                        tmem_wait_loads();
+                        if (c == DH - 64) {
+                            tmem_fence_before();
+                            bar_arrive_warp(&bars.sums_taken);
+                        }
+                        if (key >= seq.m)
+    #pragma unroll
+                            for (int e = 0; e < 64; ++e) o[e / 32][e % 32] = 0;
+                        const float by = w == 0 ? 1.0f : p.scale;
+                        if (key < p.len_kv) write_columns(out, c, p.dim, o[0], by), write_columns(out, c + 32, p.dim, o[1], by);
+                    }
+                } else if (key < p.len_kv) {
+                    write_zeros(out, 0, p.dim);
+                }
+                next();
             }
-            tmem_wait_stores();
-            tmem_fence_before();
-            bar_arrive_warp(&sm.ds_ready[w]);
         }
-        if (n > 0 && ok) ok = bar_wait(&sm.sums_full, 0, gave_up);
-        tmem_fence_after();
-        // one group writes dV, the other dK
-        const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
-        __nv_bfloat16 *out = (w == 0 ? p.dv : p.dk) + b * stride[0] + key * stride[1] + h_kv * stride[2];
-#pragma unroll
-        for (int c = 0; c < DH; c += 32) {
-            if (n > 0 && ok) {
-                uint32_t o[32];
-                tmem_load32(lanes + (w == 0 ? Smem::DV : Smem::DK) + c, o);
-                tmem_wait_loads();
-                if (key >= seq.m)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0;
-                if (key < p.len_kv) write_columns(out, c, p.dim, o, w == 0 ? 1.0f : p.scale);
-            } else if (key < p.len_kv) {
-                write_zeros(out, c, min(c + 32, p.dim));
+        // Query tiles next, whose data comes where that of the key tiles was: dQ.
+        all_done();
+        {
+            DqBars &bars = cm.dq;
+            const int w = warp / 4, in_tile = threadIdx.x % TILE;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, dp_at = lanes + TILE, ds_at = lanes + 2 * TILE + w * 64;
+            uint32_t tiles_in = 0, outputs = 0;
+            while (ok) {
+                const DqItem it(p, block - key_items);
+                const Seq seq(p, it.b);
+                const int row = it.row0 + in_tile, limit = seq.keys_of(row), all_see = seq.keys_of(it.row0);
+                const bool whole = it.row0 + TILE <= seq.n;
+                const QueryStats &stats = p.stats[static_cast<int64_t>(it.bh) * p.tiles_q + it.tile];
+                const float lse = stats.lse[in_tile], delta = stats.delta[in_tile];
+                for (int j = static_cast<int>((tiles_in + w) & 1); j < it.n; j += 2) {
+                    const uint32_t g = tiles_in + j;
+                    if (!(ok = bar_wait(&bars.s_full[w], g / 2 & 1, gave_up))) break;
+                    tmem_fence_after();
+                    uint32_t s[4][32];
+    #pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
+                    tmem_wait_loads();
+                    tmem_fence_before();
+                    bar_arrive_warp(&bars.s_taken);
+                    if (!whole || (j + 1) * TILE > all_see) {
+                        const int left = limit - j * TILE;           // columns that the row sees
+    #pragma unroll
+                        for (int c = 0; c < TILE; ++c)
+                            if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
+                    }
+    #pragma unroll
+                    for (int c = 0; c < TILE; c += 2) {
+                        const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
+                        s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
+                    }
+                    if (!(ok = bar_wait(&bars.dp_full[w], g / 2 & 1, gave_up))) break;
+                    tmem_fence_after();
+                    uint32_t d[2][32], packed[4][16];
+                    tmem_load32(dp_at, d[0]);
+    #pragma unroll
+                    for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
+                        tmem_wait_loads();
+                        if (q < 3) {
+                            tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
+                        } else {
+                            tmem_fence_before();
+                            bar_arrive_warp(&bars.dp_taken);
+                        }
+    #pragma unroll
+                        for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta))));
+                    }
+                    if (g > 1) {                         // its last dS has been used
+                        if (!(ok = bar_wait(&bars.dq_done[w], (g / 2 - 1) & 1, gave_up))) break;
+                        tmem_fence_after();
+                    }
+    #pragma unroll
+                    for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
+                    tmem_wait_stores();
+                    tmem_fence_before();
+                    bar_arrive_warp(&bars.ds_ready[w]);
+                }
+                if (!ok) break;
+                tiles_in += it.n;
+                __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
+                if (it.n > 0) {
+                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
+                    ++outputs;
+                    tmem_fence_after();
+                    uint32_t o[DH / 64][32];                 // a group writes half of the columns
+    #pragma unroll
+                    for (int c = 0; c < DH / 64; ++c) tmem_load32(lanes + 3 * TILE + w * (DH / 2) + c * 32, o[c]);
+                    tmem_wait_loads();
+                    tmem_fence_before();
+                    bar_arrive_warp(&bars.sums_taken);
+    #pragma unroll
+                    for (int c = 0; c < DH / 64; ++c) {
+                        if (limit == 0)
+    #pragma unroll
+                            for (int e = 0; e < 32; ++e) o[c][e] = 0;
+                        if (row < p.len_q) write_columns(out, w * (DH / 2) + c * 32, p.dim, o[c], p.scale);
+                    }
+                } else if (row < p.len_q) {
+                    write_zeros(out, w * (DH / 2), min((w + 1) * (DH / 2), p.dim));
+                }
+                next();
             }
         }
     }
     tmem_fence_before();
     __syncthreads();
     settle(gave_up);
-    if (warp == WARP_SCORES && n > 0) tmem_free(tmem, TMEM_COLUMNS);
-}
-
-// Both in one launch, which fills the SMs better than one after the other: first the key tiles, whose work
-// is the larger, then the query tiles, each kind in the order of what a causal mask leaves it.
-template <int DH>
-__global__ void __launch_bounds__(THREADS, 1)
-k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
-    extern __shared__ uint8_t raw[];
-    const int key_tiles = p.batch * p.heads_kv * p.tiles_kv, block = static_cast<int>(blockIdx.x);
-    if (block < key_tiles) dkv_tile<DH>(raw, block, map_q, map_k, map_v, map_do, p);
-    else dq_tile<DH>(raw, block - key_tiles, map_q, map_k, map_v, map_do, p);
+    if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
 }
 
 // ---------------------------------------------------------------------------------- host side
@@ -930,9 +1127,9 @@ int start_forward(const CUtensorMap (&m)[3], const AttnParams &p, cudaStream_t s
 template <int DH>
 int start_backward(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
-    if (int rc = room<std::conditional_t<(sizeof(DqSmem<DH>) > sizeof(DkvSmem<DH>)), DqSmem<DH>, DkvSmem<DH>>>(k_attn_backward<DH>, &bytes)) return rc;
-    const unsigned ctas = static_cast<unsigned>(p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q));
-    k_attn_backward<DH><<<ctas, THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
+    if (int rc = room<BwdSmem<DH>>(k_attn_backward<DH>, &bytes)) return rc;
+    const int items = p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q);
+    k_attn_backward<DH><<<items < SMS ? items : SMS, THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
     KT_CUDA(cudaGetLastError());
     return KT_OK;
 }
@@ -981,7 +1178,7 @@ int kt_attn_forward(const kt_attn *a, const void *q, const int64_t *q_stride, co
 
 int64_t kt_attn_workspace(int batch, int heads, int len_q) {
     if (batch < 0 || heads < 0 || len_q < 0) return 0;
-    return static_cast<int64_t>(batch) * heads * ((static_cast<int64_t>(len_q) + TILE - 1) / TILE) * static_cast<int64_t>(sizeof(QueryStats));
+    return static_cast<int64_t>(batch) * heads * ((static_cast<int64_t>(len_q) + TILE - 1) / TILE) * static_cast<int64_t>(sizeof(QueryStats)) + 16;      // and the counter of items
 }
 
 int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_stride, const void *q, const int64_t *q_stride, const void *k,
@@ -1021,6 +1218,7 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
     if (int rc = make_map(&m[2], "v", v, v_stride, p.batch, p.len_kv, p.heads_kv, p.dim)) return rc;
     if (int rc = make_map(&m[3], "dout", dout, dout_stride, p.batch, p.len_q, p.heads, p.dim)) return rc;
     p.o = static_cast<const __nv_bfloat16 *>(out), p.dout = static_cast<const __nv_bfloat16 *>(dout), p.lse = const_cast<float *>(lse), p.stats = static_cast<QueryStats *>(workspace);
+    p.next_item = reinterpret_cast<unsigned *>(static_cast<char *>(workspace) + need - 16);
     copy_strides(p.o_stride, out_stride);
     copy_strides(p.dout_stride, dout_stride);
     k_attn_stats<<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q * (TILE / 16)), 256, 0, st>>>(p);

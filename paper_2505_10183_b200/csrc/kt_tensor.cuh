@@ -104,6 +104,63 @@ __device__ __forceinline__ void copy_bytes(uint32_t to, const void *from, uint32
 // What threads have written to shared memory becomes visible to the tensor cores and copies.
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
+// ------------------------------------------------------------------------------- work to come
+// A CTA that stays: one thread finds out what it does next (up to QUEUE items ahead), every role of the CTA
+// reads each answer and says so.
+constexpr int QUEUE = 4;
+struct Queue {
+    alignas(16) uint4 answer[QUEUE];
+    uint64_t full[QUEUE], free[QUEUE];
+};
+__device__ __forceinline__ void queue_init(Queue &q, uint32_t readers) {
+    for (int i = 0; i < QUEUE; ++i) bar_init(&q.full[i], 1), bar_init(&q.free[i], readers);
+}
+// Answers from the launch itself: the next block of the grid that has not been started, whose place the
+// CTA takes.  (free[k % QUEUE] has been waited for.)
+__device__ __forceinline__ void queue_ask(Queue &q, uint32_t k) {
+    bar_expect(&q.full[k % QUEUE], sizeof(uint4));
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(smem_addr(&q.answer[k % QUEUE])),
+                 "r"(smem_addr(&q.full[k % QUEUE]))
+                 : "memory");
+}
+// The block of answer k, or -1 where there is none left.
+__device__ __forceinline__ int queue_read(const Queue &q, uint32_t k) {
+    uint32_t x, given;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b128 a;\n\t"
+        "mov.u32 %0, 0;\n\t"
+        "ld.shared.b128 a, [%2];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n\t"
+        "selp.u32 %1, 1, 0, p;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%0, _, _, _}, a;\n\t}"
+        : "=&r"(x), "=&r"(given)
+        : "r"(smem_addr(&q.answer[k % QUEUE]))
+        : "memory");
+    fence_async_smem();
+    return given ? static_cast<int>(x) : -1;
+}
+// Answers from a counter in device memory, where items have to come in their order.
+__device__ __forceinline__ void queue_count(Queue &q, uint32_t k, unsigned *counter, int most) {
+    const unsigned block = gridDim.x + atomicAdd(counter, 1u);
+    q.answer[k % QUEUE].x = block < static_cast<unsigned>(most) ? block : 0xFFFFFFFFu;
+    bar_arrive(&q.full[k % QUEUE]);
+}
+// For roles of one thread, and of a whole warp.
+template <bool COUNTED>
+__device__ __forceinline__ int queue_next_one(Queue &q, uint32_t k, volatile uint32_t *gave_up) {
+    if (!bar_wait_one(&q.full[k % QUEUE], k / QUEUE & 1, gave_up)) return -1;
+    const int block = COUNTED ? static_cast<int>(q.answer[k % QUEUE].x) : queue_read(q, k);
+    bar_arrive(&q.free[k % QUEUE]);
+    return block;
+}
+template <bool COUNTED>
+__device__ __forceinline__ int queue_next(Queue &q, uint32_t k, volatile uint32_t *gave_up) {
+    if (!bar_wait(&q.full[k % QUEUE], k / QUEUE & 1, gave_up)) return -1;
+    const int block = COUNTED ? static_cast<int>(q.answer[k % QUEUE].x) : queue_read(q, k);
+    bar_arrive_warp(&q.free[k % QUEUE]);
+    return block;
+}
+
 // ------------------------------------------------------------------------------ tensor memory
 __device__ __forceinline__ void tmem_alloc(uint32_t *to, uint32_t columns) {      // one whole warp
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(to)), "r"(columns) : "memory");
