@@ -407,39 +407,54 @@ __device__ __forceinline__ void three_terms(float x, uint16_t (&to)[3]) {
     }
 }
 
-// A half warp to a row.
+// A tile to a CTA, LANES neighbours to a row.  Bound by memory: O and dO are read once, all of a thread's
+// vectors before the first is used.
+template <int LANES>
 __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 16 + threadIdx.x / 16;
-    const int lane = threadIdx.x % 16;
-    const int64_t bh = at / (p.tiles_q * TILE);
-    const int row = static_cast<int>(at % (p.tiles_q * TILE));
-    const int b = static_cast<int>(bh / p.heads), h = static_cast<int>(bh % p.heads);
+    constexpr int ROWS = 256 / LANES, PASSES = TILE / ROWS;
+    const int bh = blockIdx.x / p.tiles_q, tile = blockIdx.x % p.tiles_q, b = bh / p.heads, h = bh % p.heads;
+    const int lane = threadIdx.x % LANES, in_pass = threadIdx.x / LANES;
     const Seq seq(p, b);
-    float delta = 0.0f;
-    if (row < seq.n && lane * 8 < p.dim) {
-        const uint4 x = *reinterpret_cast<const uint4 *>(p.o + b * p.o_stride[0] + row * p.o_stride[1] + h * p.o_stride[2] + lane * 8);
-        const uint4 y = *reinterpret_cast<const uint4 *>(p.dout + b * p.dout_stride[0] + row * p.dout_stride[1] + h * p.dout_stride[2] + lane * 8);
-        const uint32_t u[4] = {x.x, x.y, x.z, x.w}, v[4] = {y.x, y.y, y.z, y.w};
+    const __nv_bfloat16 *o = p.o + b * p.o_stride[0] + h * p.o_stride[2] + lane * 8, *dout = p.dout + b * p.dout_stride[0] + h * p.dout_stride[2] + lane * 8;
+    __shared__ float deltas[TILE];
+    float lse = -INFINITY;
+    if (threadIdx.x < TILE && tile * TILE + static_cast<int>(threadIdx.x) < seq.n) lse = p.lse[static_cast<int64_t>(bh) * p.len_q + tile * TILE + threadIdx.x];
+    uint4 x[PASSES], y[PASSES];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            delta = fmaf(__uint_as_float(u[i] << 16), __uint_as_float(v[i] << 16), delta);
-            delta = fmaf(__uint_as_float(u[i] & 0xFFFF0000u), __uint_as_float(v[i] & 0xFFFF0000u), delta);
+    for (int i = 0; i < PASSES; ++i) {
+        const int64_t row = tile * TILE + i * ROWS + in_pass;
+        x[i] = y[i] = make_uint4(0, 0, 0, 0);
+        if (row < seq.n && lane * 8 < p.dim) {
+            x[i] = *reinterpret_cast<const uint4 *>(o + row * p.o_stride[1]);
+            y[i] = *reinterpret_cast<const uint4 *>(dout + row * p.dout_stride[1]);
         }
     }
 #pragma unroll
-    for (int d = 8; d > 0; d /= 2) delta += __shfl_xor_sync(0xFFFFFFFFu, delta, d);
-    if (lane == 0) {
-        const float lse = row < seq.n ? p.lse[bh * p.len_q + row] : -INFINITY;
+    for (int i = 0; i < PASSES; ++i) {
+        const uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w}, v[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+        float delta = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            delta = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(v[e] << 16), delta);
+            delta = fmaf(__uint_as_float(u[e] & 0xFFFF0000u), __uint_as_float(v[e] & 0xFFFF0000u), delta);
+        }
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d /= 2) delta += __shfl_xor_sync(0xFFFFFFFFu, delta, d);
+        if (lane == 0) deltas[i * ROWS + in_pass] = delta;
+    }
+    __syncthreads();
+    if (threadIdx.x < TILE) {
         const bool empty = lse == -INFINITY;
-        QueryStats &to = p.stats[at / TILE];
-        to.lse[at % TILE] = empty ? INFINITY : lse * LOG2E;
-        to.delta[at % TILE] = empty ? 0.0f : delta;
+        const float delta = empty ? 0.0f : deltas[threadIdx.x];
+        QueryStats &to = p.stats[blockIdx.x];
+        to.lse[threadIdx.x] = empty ? INFINITY : lse * LOG2E;
+        to.delta[threadIdx.x] = delta;
         uint16_t l[3], d[3];
         three_terms(empty ? HIDDEN : -lse / p.scale, l);
-        three_terms(empty ? 0.0f : -delta, d);
-        if (at == 0) *p.next_item = 0;
-        to.terms[at % TILE] = make_uint4(l[0] | l[1] << 16, l[2] | d[0] << 16, d[1] | d[2] << 16, 0);
+        three_terms(-delta, d);
+        to.terms[threadIdx.x] = make_uint4(l[0] | l[1] << 16, l[2] | d[0] << 16, d[1] | d[2] << 16, 0);
     }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.next_item = 0;
 }
 
 // The backward pass in one launch, whose CTAs stay (Queue, with a counter: a CTA must not be handed a key tile
@@ -1221,7 +1236,8 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
     p.next_item = reinterpret_cast<unsigned *>(static_cast<char *>(workspace) + need - 16);
     copy_strides(p.o_stride, out_stride);
     copy_strides(p.dout_stride, dout_stride);
-    k_attn_stats<<<static_cast<unsigned>(p.batch * p.heads * p.tiles_q * (TILE / 16)), 256, 0, st>>>(p);
+    const unsigned tiles_of_all = static_cast<unsigned>(p.batch * p.heads * p.tiles_q);
+    p.dim <= 64 ? k_attn_stats<8><<<tiles_of_all, 256, 0, st>>>(p) : k_attn_stats<16><<<tiles_of_all, 256, 0, st>>>(p);
     KT_CUDA(cudaGetLastError());
     p.out = static_cast<__nv_bfloat16 *>(dq), p.dk = static_cast<__nv_bfloat16 *>(dk), p.dv = static_cast<__nv_bfloat16 *>(dv);
     copy_strides(p.out_stride, dq_stride);
