@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
     constexpr int ROWS = 256 / LANES, PASSES = TILE / ROWS;
     const int bh = blockIdx.x / p.tiles_q, tile = blockIdx.x % p.tiles_q, b = bh / p.heads, h = bh % p.heads;
     const int lane = threadIdx.x % LANES, in_pass = threadIdx.x / LANES;
+    let_next_begin();
     const Seq seq(p, b);
     const __nv_bfloat16 *o = p.o + b * p.o_stride[0] + h * p.o_stride[2] + lane * 8, *dout = p.dout + b * p.dout_stride[0] + h * p.dout_stride[2] + lane * 8;
     __shared__ float deltas[TILE];
@@ -586,6 +587,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     tmem_fence_after();
     const uint32_t tmem = cm.tmem;
     volatile uint32_t *gave_up = &cm.gave_up;
+    after_previous();                           // k_attn_stats
 
     int block = blockIdx.x;                     // every role goes through the same items
     uint32_t items = 0, landed_phase = 0;       // answers read
@@ -1144,8 +1146,7 @@ int start_backward(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t 
     size_t bytes = 0;
     if (int rc = room<BwdSmem<DH>>(k_attn_backward<DH>, &bytes)) return rc;
     const int items = p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q);
-    k_attn_backward<DH><<<items < SMS ? items : SMS, THREADS, bytes, st>>>(m[0], m[1], m[2], m[3], p);
-    KT_CUDA(cudaGetLastError());
+    KT_CUDA(launch_behind(k_attn_backward<DH>, dim3(items < SMS ? items : SMS), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
     return KT_OK;
 }
 

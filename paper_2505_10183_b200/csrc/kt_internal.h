@@ -34,6 +34,23 @@ int check_shares(const int32_t *shares, int K);
 
 }  // namespace ktd
 
+// A launch that may begin while the one before it in the stream ends: its blocks come up as places become
+// free, and call after_previous() before they touch what the one before writes.
+#ifdef __CUDACC__
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute behind{};
+    behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    behind.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = block, config.dynamicSmemBytes = smem, config.stream = stream;
+    config.attrs = &behind, config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+__device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+#endif
+
 #define KT_CUDA(call)                                                                       \
     do {                                                                                    \
         cudaError_t e_ = (call);                                                            \

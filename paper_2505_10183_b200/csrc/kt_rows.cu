@@ -117,24 +117,76 @@ __device__ __forceinline__ uint4 load_row(const T *row, int64_t col, int64_t col
         if (col + 2 < cols) r.z = at[2];
         if (col + 3 < cols) r.w = at[3];
     } else {
-        const unsigned short *at = reinterpret_cast<const unsigned short *>(row) + col;
-        unsigned w[8];
+        // whole words, of which the first and the last may be shared with other rows: half as many loads as elements
+        const unsigned off = reinterpret_cast<uintptr_t>(row + col) & 2;
+        const unsigned *at = reinterpret_cast<const unsigned *>(reinterpret_cast<const char *>(row + col) - off);
+        const int left = static_cast<int>(cols - col > 8 ? 16 : (cols - col) * 2), end = left + static_cast<int>(off);       // bytes wanted, and where they end
+        unsigned w[5];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = col + i < cols ? at[i] : 0;
-        r = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+        for (int i = 0; i < 5; ++i) w[i] = left > 0 && 4 * i < end ? at[i] : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = __funnelshift_r(w[i], w[i + 1], off * 8);
+            if (left < 4 * i + 4) w[i] = left <= 4 * i ? 0 : w[i] & 0xFFFFu;
+        }
+        r = make_uint4(w[0], w[1], w[2], w[3]);
     }
     return r;
 }
 
+// Rows of bf16 that are not made of aligned vectors are written in aligned 16-byte pieces all the same: a lane
+// writes the piece in which its vector starts, with the end of its left neighbour's vector in it (the lanes of
+// a warp hold vectors that follow one another, and all of them call); what no lane can write as a
+// whole piece goes element by element.
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store_row(T *row, int64_t col, int64_t cols, const float (&x)[Elems<T>::V]) {
     constexpr int V = Elems<T>::V;
+    const uint4 r = Elems<T>::narrow(x);
     if constexpr (WIDE) {
-        if (col < cols) *reinterpret_cast<uint4 *>(row + col) = Elems<T>::narrow(x);
-    } else {
+        if (col < cols) *reinterpret_cast<uint4 *>(row + col) = r;
+    } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (col + i < cols) row[col + i] = Elems<T>::one(x[i]);
+            if (col + i < cols) row[col + i] = x[i];
+    } else {
+        const unsigned off = reinterpret_cast<uintptr_t>(row + col) & 15;
+        const int first = 16 - static_cast<int>(off);                                   // bytes in the first piece
+        const int64_t left = (cols - col) * static_cast<int64_t>(sizeof(T));
+        uint4 l;
+        l.x = __shfl_up_sync(0xFFFFFFFFu, r.x, 1), l.y = __shfl_up_sync(0xFFFFFFFFu, r.y, 1);
+        l.z = __shfl_up_sync(0xFFFFFFFFu, r.z, 1), l.w = __shfl_up_sync(0xFFFFFFFFu, r.w, 1);
+        if (left <= 0) return;
+        const bool whole = left >= first && (off == 0 || (threadIdx.x % 32 > 0 && col > 0));
+        if (whole) {
+            unsigned w[8] = {l.x, l.y, l.z, l.w, r.x, r.y, r.z, r.w};                  // bytes 16 - off ... 32 - off of the two
+            if (first & 16) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = w[i + 4];
+            } else {
+                if (first & 8) {
+#pragma unroll
+                    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+                }
+                if (first & 4) {
+#pragma unroll
+                    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                }
+                if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (first & 2) * 8);
+                }
+            }
+            *reinterpret_cast<uint4 *>(reinterpret_cast<char *>(row + col) - off) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        // the right neighbour takes the end along if it writes a whole piece
+        const bool taken = off == 0 || (threadIdx.x % 32 < 31 && left - 16 >= first);
+        if (!whole || !taken) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int at = i * static_cast<int>(sizeof(T));
+                if (at < left && (at < first ? !whole : !taken)) row[col + i] = Elems<T>::one(x[i]);
+            }
+        }
     }
 }
 
@@ -257,6 +309,12 @@ __host__ __device__ constexpr int norm_threads() { return GROUP == 32 ? 128 : GR
 // Threads on an SM: as many as the registers of 16 elements to a thread allow.
 template <typename T, int NV>
 __host__ __device__ constexpr int forward_threads() { return NV * Elems<T>::V == E ? 512 : 768; }
+
+// Waits for the threads on a row; a CTA with several rows has a barrier for each.
+template <int GROUP>
+__device__ __forceinline__ void group_barrier(int group) {
+    asm volatile("barrier.sync %0, %1;" ::"r"(group + 1), "n"(GROUP) : "memory");
+}
 
 template <int GROUP, int NV, int V>
 __device__ __forceinline__ int column(int at, int k) { return (at + k * GROUP) * V; }
@@ -392,23 +450,26 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
 
 // With u = (x - mean) rstd (or its 8-bit checkpoint) and g = dout w:
 //   dx = rstd (g - mean(g) - u mean(g u)),  dweight = sum_rows dout u,  dbias = sum_rows dout.
-// One row of partial sums per CTA is reduced in a fixed order by k_norm_params: no atomics, so that a step
-// gives the same bits when it is run again.
+// A CTA of 512 threads fills an SM's registers; its groups join their columns' sums at the end, and one row of partial
+// sums per CTA is reduced in a fixed order by k_norm_params: no atomics, so that a step gives the same bits
+// when it is run again.  (With a CTA to a group, four times as many partial sums: 47.6 instead of 38.6 us for
+// 16384 x 2048 bf16 from a checkpoint.)
 template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
-__global__ void __launch_bounds__(norm_threads<GROUP>(), 512 / norm_threads<GROUP>()) k_norm_backward(const NormParams p) {
-    constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
+__global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams p) {
+    constexpr int V = Elems<T>::V, THREADS = GROUP_MAX, GROUPS = THREADS / GROUP, WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
     constexpr int SOURCE = KEPT ? V : 16;        // bytes of a vector of u: codes, or x itself
     // WIDE: [AHEAD + 1][NV][THREADS] vectors of dout, then as many of SOURCE bytes, then (KEPT) scales;
-    // afterwards, with a warp to a row, the sums of the CTA's warps
+    // afterwards the sums of the CTA's groups
     extern __shared__ uint4 ring[];
-    __shared__ float2 slots[2][WARPS];
+    __shared__ float2 slots[GROUPS][2][WARPS];
     constexpr int CELLS = (AHEAD + 1) * NV * THREADS;
     char *const ring_u = reinterpret_cast<char *>(ring + CELLS);
     float *const ring_s = reinterpret_cast<float *>(ring_u + CELLS * SOURCE);
-    const int at = threadIdx.x % GROUP;
+    const int at = threadIdx.x % GROUP, group = threadIdx.x / GROUP;
     const int64_t step = static_cast<int64_t>(gridDim.x) * (THREADS / GROUP), first = static_cast<int64_t>(blockIdx.x) * (THREADS / GROUP) + threadIdx.x / GROUP;
     const int cols = static_cast<int>(p.cols), pitch = static_cast<int>(pitch_of(cols)), blocks = static_cast<int>(blocks_of(cols));
     const float per_col = 1.0f / static_cast<float>(cols);
+    let_next_begin();
     auto cell = [&](int stage, int k) { return (stage * NV + k) * THREADS + static_cast<int>(threadIdx.x); };
     auto dout_at = [&](int64_t r, int k) { return static_cast<const T *>(p.dout) + r * p.dout_stride + column<GROUP, NV, V>(at, k); };
     auto x_at = [&](int64_t r, int k) { return static_cast<const T *>(p.x) + r * p.x_stride + column<GROUP, NV, V>(at, k); };
@@ -501,11 +562,11 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), 512 / norm_threads<GROU
             s.y += __shfl_xor_sync(0xFFFFFFFFu, s.y, d);
         }
         if constexpr (WARPS > 1) {
-            if (threadIdx.x % 32 == 0) slots[turn][at / 32] = s;
-            __syncthreads();
+            if (threadIdx.x % 32 == 0) slots[group][turn][at / 32] = s;
+            group_barrier<GROUP>(group);
             s = both(0.0f);
 #pragma unroll
-            for (int i = 0; i < WARPS; ++i) s = add2(s, slots[turn][i]);
+            for (int i = 0; i < WARPS; ++i) s = add2(s, slots[group][turn][i]);
             turn ^= 1;
         }
         const float a = -s.x * per_col * by, c = -s.y * per_col * by;
@@ -522,32 +583,36 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), 512 / norm_threads<GROU
     }
     if (p.parts == nullptr) return;
     float *part = p.parts + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
-    if constexpr (GROUP == 32) {
-        constexpr int N = 32 * NV * V;
+    if constexpr (GROUPS > 1) {
+        constexpr int N = GROUP * NV * V;
         float *const joined = reinterpret_cast<float *>(ring);
         wait_copies<0>();
-        for (unsigned turn_of = 0; turn_of < THREADS / 32; ++turn_of) {
+        for (int turn_of = 0; turn_of < GROUPS; ++turn_of) {
             __syncthreads();
-            if (threadIdx.x / 32 == turn_of) {
+            if (group == turn_of) {
 #pragma unroll
                 for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        const int c = (at + k * 32) * V + i;
-                        joined[c] = turn_of == 0 ? dw[k][i] : joined[c] + dw[k][i];
-                        joined[N + c] = turn_of == 0 ? db[k][i] : joined[N + c] + db[k][i];
+                    for (int i = 0; i < V; i += 4) {
+                        float4 *const a = reinterpret_cast<float4 *>(joined + column<GROUP, NV, V>(at, k) + i), *const c = a + N / 4;
+                        float4 x = make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]), y = make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]);
+                        if (turn_of > 0) {
+                            const float4 p = *a, q = *c;
+                            x.x += p.x, x.y += p.y, x.z += p.z, x.w += p.w, y.x += q.x, y.y += q.y, y.z += q.z, y.w += q.w;
+                        }
+                        *a = x, *c = y;
                     }
             }
         }
         __syncthreads();
-        for (int64_t c = threadIdx.x; c < p.cols; c += THREADS) part[c] = joined[c], part[p.cols + c] = joined[N + c];
+        for (int c = threadIdx.x; c < cols; c += THREADS) part[c] = joined[c], part[p.cols + c] = joined[N + c];
     } else {
 #pragma unroll
         for (int k = 0; k < NV; ++k)
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int64_t c = column<GROUP, NV, V>(at, k) + i;
-                if (c < p.cols) part[c] = dw[k][i], part[p.cols + c] = db[k][i];
+                const int c = column<GROUP, NV, V>(at, k) + i;
+                if (c < cols) part[c] = dw[k][i], part[p.cols + c] = db[k][i];
             }
     }
 }
@@ -666,6 +731,7 @@ __global__ void __launch_bounds__(1024) k_norm_params(const NormParams p) {
     __shared__ float sums[32][33];
     const int64_t c = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.x;
     void *out = blockIdx.y == 0 ? p.dweight : p.dbias;
+    after_previous();
     if (out == nullptr) return;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < p.cols) {
@@ -850,6 +916,8 @@ __global__ void __launch_bounds__(THREADS) k_restore(const ElemParams p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const Place<V> at(p, u);
+        codes[u] = make_uint2(0, 0);
+        scale[u] = 0.0f;
         if (at.col < p.cols) {
             codes[u] = load_codes<V>(p.codes + at.row * pitch_of(p.cols) + at.col);
             scale[u] = p.scales[at.row * blocks_of(p.cols) + at.col / BLOCK];
@@ -858,10 +926,9 @@ __global__ void __launch_bounds__(THREADS) k_restore(const ElemParams p) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const Place<V> at(p, u);
-        if (at.col >= p.cols) continue;
         float x[V];
         decode<V>(codes[u], scale[u], x);
-        if (p.weight != nullptr || p.bias != nullptr) {
+        if ((p.weight != nullptr || p.bias != nullptr) && at.col < p.cols) {
             float w[V], b[V];
             load_param(p.weight, p.param_bf16, at.col, p.cols, 1.0f, w);
             load_param(p.bias, p.param_bf16, at.col, p.cols, 0.0f, b);
@@ -937,12 +1004,12 @@ int start_norm_kernel(Kernel kernel, const NormParams &p, int grid, int threads,
 
 template <typename T, bool WIDE, int GROUP, int NV>
 int start_norm(bool backward, const NormParams &p, int grid, cudaStream_t st) {
-    constexpr int V = Elems<T>::V, T_ = norm_threads<GROUP>(), CELLS = WIDE ? (rows_ahead<NV>() + 1) * NV * T_ : 0;
-    if (!backward) return start_norm_kernel(k_norm_forward<T, WIDE, GROUP, NV>, p, grid, T_, CELLS * sizeof(uint4), st);
-    const size_t joined = GROUP == 32 ? 2 * 32 * NV * V * sizeof(float) : 0;
-    const size_t kept = CELLS * (sizeof(uint4) + V + sizeof(float)), whole = CELLS * 2 * sizeof(uint4);
-    if (p.codes != nullptr) return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, true>, p, grid, T_, kept > joined ? kept : joined, st);
-    return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, false>, p, grid, T_, whole > joined ? whole : joined, st);
+    constexpr int V = Elems<T>::V, SLOTS = WIDE ? (rows_ahead<NV>() + 1) * NV : 0, FORWARD = norm_threads<GROUP>();
+    if (!backward) return start_norm_kernel(k_norm_forward<T, WIDE, GROUP, NV>, p, grid, FORWARD, SLOTS * FORWARD * sizeof(uint4), st);
+    const size_t joined = GROUP < GROUP_MAX ? 2 * GROUP * NV * V * sizeof(float) : 0;
+    const size_t kept = SLOTS * GROUP_MAX * (sizeof(uint4) + V + sizeof(float)), whole = SLOTS * GROUP_MAX * 2 * sizeof(uint4);
+    if (p.codes != nullptr) return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, true>, p, grid, GROUP_MAX, kept > joined ? kept : joined, st);
+    return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, false>, p, grid, GROUP_MAX, whole > joined ? whole : joined, st);
 }
 
 template <typename T, bool WIDE, int GROUP>
@@ -1027,11 +1094,11 @@ int act_forward(const ElemParams &all, int dtype, int kind, bool wide_, cudaStre
     });
 }
 
-// Rows of partial sums, one to a CTA: few enough rows that a CTA takes four of its own, so that the
+// Rows of partial sums, one to a CTA of the backward pass; a group has two rows at least, so that the
 // partial sums stay small beside what is read.
 int64_t norm_parts(int64_t rows, const RowShape &s) {
-    const int64_t busy = static_cast<int64_t>(SMS) * (512 / s.threads), need = (rows + s.threads / s.group * 4 - 1) / (s.threads / s.group * 4);
-    return need < busy ? need : busy;
+    const int64_t per_cta = GROUP_MAX / s.group * 2, need = (rows + per_cta - 1) / per_cta;
+    return need < SMS ? need : SMS;
 }
 constexpr int64_t ANY_PARTS = 16;
 
@@ -1126,8 +1193,7 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
         if (int rc = start_norm(true, dtype, w, s, p, p.n_parts, st)) return rc;
     }
     if (sums) {
-        k_norm_params<<<dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st>>>(p);
-        KT_CUDA(cudaGetLastError());
+        KT_CUDA(launch_behind(k_norm_params, dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st, p));
     }
     return KT_OK;
 }
