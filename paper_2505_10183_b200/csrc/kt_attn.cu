@@ -19,6 +19,7 @@
 
 #include <cuda_bf16.h>
 
+#include <atomic>
 #include <cmath>
 
 #include "kt_internal.h"
@@ -874,17 +875,17 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     if (!(ok = bar_wait(s_full, g / EVERY & 1, gave_up))) break;
                     tmem_fence_after();
                     uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
-    #pragma unroll
+#pragma unroll
                     for (int q = 0; q < WIDTH / 32; ++q) tmem_load32(s_at + q * 32, s[q]);
                     tmem_wait_loads();
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
                     if (__any_sync(0xFFFFFFFFu, hidden > 0)) {
-    #pragma unroll
+#pragma unroll
                         for (int c = 0; c < WIDTH; ++c)
                             if (c < hidden) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
                     }
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < WIDTH; c += 2) {
                         const float2 x = mul2(pair_of(s[c / 32], c % 32), both(p.scale_log2));
                         const float2 e = make_float2(exp2_fast(x.x), exp2_fast(x.y));
@@ -908,7 +909,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     if constexpr (Dkv::TURNS) {
                         uint32_t packed[4][16];
                         tmem_load32(dp_at, d[0]);
-    #pragma unroll
+#pragma unroll
                         for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
                             tmem_wait_loads();
                             if (q < 3) {
@@ -917,12 +918,12 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                                 tmem_fence_before();
                                 bar_arrive_warp(&bars.dp_taken);
                             }
-    #pragma unroll
+#pragma unroll
                             for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), pair_of(d[q % 2], c)));
                         }
                         if (!(ok = bar_wait(&bars.dv_done[w], g / 2 & 1, gave_up))) break;        // P has been used
                         tmem_fence_after();
-    #pragma unroll
+#pragma unroll
                         for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
                     } else {
                         tmem_load32(dp_at, d[0]);
@@ -930,7 +931,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         tmem_wait_loads();
                         tmem_store32(p_at, probs[0]);
                         uint32_t packed[32];
-    #pragma unroll
+#pragma unroll
                         for (int c = 0; c < 64; c += 2) packed[c / 2] = pack_bf16(mul2(pair_of(s[c / 32], c % 32), pair_of(d[c / 32], c % 32)));
                         tmem_store32(ds_at, packed);
                     }
@@ -947,7 +948,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
                     ++outputs;
                     tmem_fence_after();
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < DH; c += 64) {
                         uint32_t o[2][32];
                         tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c, o[0]);
@@ -958,7 +959,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                             bar_arrive_warp(&bars.sums_taken);
                         }
                         if (key >= seq.m)
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 64; ++e) o[e / 32][e % 32] = 0;
                         const float by = w == 0 ? 1.0f : p.scale;
                         if (key < p.len_kv) write_columns(out, c, p.dim, o[0], by), write_columns(out, c + 32, p.dim, o[1], by);
@@ -988,18 +989,18 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     if (!(ok = bar_wait(&bars.s_full[w], g / 2 & 1, gave_up))) break;
                     tmem_fence_after();
                     uint32_t s[4][32];
-    #pragma unroll
+#pragma unroll
                     for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
                     tmem_wait_loads();
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
                     if (!whole || (j + 1) * TILE > all_see) {
                         const int left = limit - j * TILE;           // columns that the row sees
-    #pragma unroll
+#pragma unroll
                         for (int c = 0; c < TILE; ++c)
                             if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
                     }
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < TILE; c += 2) {
                         const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
                         s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
@@ -1008,7 +1009,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     tmem_fence_after();
                     uint32_t d[2][32], packed[4][16];
                     tmem_load32(dp_at, d[0]);
-    #pragma unroll
+#pragma unroll
                     for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
                         tmem_wait_loads();
                         if (q < 3) {
@@ -1017,14 +1018,14 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                             tmem_fence_before();
                             bar_arrive_warp(&bars.dp_taken);
                         }
-    #pragma unroll
+#pragma unroll
                         for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta))));
                     }
                     if (g > 1) {                         // its last dS has been used
                         if (!(ok = bar_wait(&bars.dq_done[w], (g / 2 - 1) & 1, gave_up))) break;
                         tmem_fence_after();
                     }
-    #pragma unroll
+#pragma unroll
                     for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
                     tmem_wait_stores();
                     tmem_fence_before();
@@ -1038,15 +1039,15 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     ++outputs;
                     tmem_fence_after();
                     uint32_t o[DH / 64][32];                 // a group writes half of the columns
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < DH / 64; ++c) tmem_load32(lanes + 3 * TILE + w * (DH / 2) + c * 32, o[c]);
                     tmem_wait_loads();
                     tmem_fence_before();
                     bar_arrive_warp(&bars.sums_taken);
-    #pragma unroll
+#pragma unroll
                     for (int c = 0; c < DH / 64; ++c) {
                         if (limit == 0)
-    #pragma unroll
+#pragma unroll
                             for (int e = 0; e < 32; ++e) o[c][e] = 0;
                         if (row < p.len_q) write_columns(out, w * (DH / 2) + c * 32, p.dim, o[c], p.scale);
                     }
@@ -1127,8 +1128,15 @@ int fill(const kt_attn *a, AttnParams *p) {
 
 template <typename Smem, typename Kernel>
 int room(Kernel kernel, size_t *bytes) {
+    static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
     *bytes = sizeof(Smem) + 1024;                // the tiles start at a multiple of 1024
-    KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*bytes)));
+    int dev = 0;
+    KT_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+        KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*bytes)));
+        raised.fetch_or(bit, std::memory_order_relaxed);
+    }
     return KT_OK;
 }
 
