@@ -47,12 +47,6 @@ class KtError(RuntimeError):
         self.status = status
 
 
-class _Attn(C.Structure):
-    """kt_attn of the header."""
-    _fields_ = [(n, C.c_int32) for n in ("batch", "len_q", "len_kv", "heads", "heads_kv", "head_dim", "dtype", "causal")] + [
-        ("scale", C.c_float), ("used_q", C.c_void_p), ("used_kv", C.c_void_p)]
-
-
 def _load() -> C.CDLL:
     path = _build.LIB
     if not os.path.exists(path):
@@ -680,53 +674,19 @@ def kt_sync_flat_static(group_of: Sequence[int], shares: Sequence[int], grads: S
 
 
 # ------------------------------------------------------------- operators of a training step
-def _first(t: torch.Tensor, what: str):
-    """(address, row stride, shape, type) of a matrix with contiguous columns."""
-    if t.dtype not in _DTYPES or t.dim() != 2 or (t.stride(1) != 1 and t.size(1) > 1):
-        raise KtError(KT_ERR_SHAPE, "%s: a float32 or bfloat16 matrix with contiguous columns expected" % what)
-    return t.data_ptr(), t.stride(0), t.shape, t.dtype
+# Their arguments are checked and passed on by a module of their own (csrc/kt_fast.cpp): a call costs about as
+# much as its launches.
+def _load_fast():
+    if not os.path.exists(_build.FAST):
+        raise ImportError("%s is missing: build it with `python -m paper_2505_10183_b200.build`" % _build.FAST)
+    from . import _fast
+    names = ("kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_backward", "kt_act_forward", "kt_act_backward",
+             "kt_attn_forward", "kt_attn_backward", "kt_last_error")
+    _fast.bind(KtError, *(C.cast(getattr(_lib, n), C.c_void_p).value for n in names))
+    return _fast
 
 
-def _like(t: torch.Tensor, what: str, shape, dtype):
-    """(address, row stride) of a matrix of that shape and type with contiguous columns."""
-    if t.dtype != dtype or t.shape != shape or (t.stride(1) != 1 and shape[1] > 1):
-        raise KtError(KT_ERR_SHAPE, "%s: shape, dtype or layout differs" % what)
-    return t.data_ptr(), t.stride(0)
-
-
-def _codes(codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], rows: int, cols: int):
-    """Addresses of a checkpoint (None, None where there is none)."""
-    if codes is None and scales is None:
-        return None, None
-    if codes is None or scales is None:
-        raise KtError(KT_ERR_INVALID, "a checkpoint has codes and scales: one of them is missing")
-    if (codes.dtype != torch.int8 or scales.dtype != torch.float32 or codes.shape != (rows, (cols + 15) // 16 * 16)
-            or scales.shape != (rows, -(-cols // KT_CKPT_BLOCK)) or not codes.is_contiguous() or not scales.is_contiguous()):
-        raise KtError(KT_ERR_SHAPE, "codes: int8 [rows, kt_ckpt_pitch(cols)], scales: float32 [rows, kt_ckpt_blocks(cols)], contiguous")
-    return codes.data_ptr(), scales.data_ptr()
-
-
-def _params(cols: int, *tensors: Optional[torch.Tensor]):
-    """Addresses of vectors over the columns (None stays None), and their type."""
-    dtype, got = None, []
-    for t in tensors:
-        if t is None:
-            got.append(None)
-            continue
-        if dtype is None:
-            dtype = t.dtype
-        if t.dtype != dtype or dtype not in _DTYPES or t.shape != (cols,) or not t.is_contiguous():
-            raise KtError(KT_ERR_SHAPE, "weight, bias and their gradients: contiguous, [cols], all float32 or all bfloat16")
-        got.append(t.data_ptr())
-    return got, KT_F32 if dtype is None else _DTYPES[dtype]
-
-
-def _per_row(t: Optional[torch.Tensor], rows: int, what: str):
-    if t is None:
-        return None
-    if t.dtype != torch.float32 or t.shape != (rows,) or not t.is_contiguous():
-        raise KtError(KT_ERR_SHAPE, "%s: contiguous float32 [rows] expected" % what)
-    return t.data_ptr()
+_fast = _load_fast()
 
 
 def kt_ckpt_pitch(cols: int) -> int:
@@ -739,36 +699,25 @@ def kt_ckpt_blocks(cols: int) -> int:
 
 def kt_ckpt_store(x: torch.Tensor, codes: torch.Tensor, scales: torch.Tensor, stream=None) -> None:
     """Keeps x [rows, cols] in 8 bits: codes int8 [rows, kt_ckpt_pitch(cols)], scales float32 [rows, kt_ckpt_blocks(cols)]."""
-    px, sx, (rows, cols), dtype = _first(x, "x")
-    pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_ckpt_store(px, sx, pc, ps, rows, cols, _DTYPES[dtype], _stream(stream)))
+    _fast.ckpt_store(x, codes, scales, stream)
 
 
 def kt_ckpt_restore(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor, weight: Optional[torch.Tensor] = None,
                     bias: Optional[torch.Tensor] = None, stream=None) -> None:
     """out = the kept values [* weight] [+ bias]."""
-    po, so, (rows, cols), dtype = _first(out, "out")
-    pc, ps = _codes(codes, scales, rows, cols)
-    (pw, pb), pd = _params(cols, weight, bias)
-    _check(_lib.kt_ckpt_restore(pc, ps, pw, pb, pd, po, so, rows, cols, _DTYPES[dtype], _stream(stream)))
+    _fast.ckpt_restore(codes, scales, out, weight, bias, stream)
 
 
 def kt_norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor], bias: Optional[torch.Tensor], out: torch.Tensor,
                     mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, eps: float = 1e-5,
                     codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
     """Layer norm of the rows of x; with codes and scales the normalised rows are kept in 8 bits."""
-    px, sx, shape, dtype = _first(x, "x")
-    po, so = _like(out, "out", shape, dtype)
-    rows, cols = shape
-    (pw, pb), pd = _params(cols, weight, bias)
-    pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_norm_forward(px, sx, pw, pb, pd, po, so, _per_row(mean, rows, "mean"), _per_row(rstd, rows, "rstd"), pc, ps,
-                                rows, cols, _DTYPES[dtype], eps, _stream(stream)))
+    _fast.norm_forward(x, weight, bias, out, mean, rstd, eps, codes, scales, stream)
 
 
 def kt_norm_workspace(rows: int, cols: int) -> int:
     """Bytes that kt_norm_backward needs for the gradients of weight and bias."""
-    return int(_lib.kt_norm_workspace(int(rows), int(cols)))
+    return _lib.kt_norm_workspace(rows, cols)
 
 
 def kt_norm_backward(dout: torch.Tensor, weight: Optional[torch.Tensor], rstd: torch.Tensor, dx: torch.Tensor,
@@ -776,15 +725,7 @@ def kt_norm_backward(dout: torch.Tensor, weight: Optional[torch.Tensor], rstd: t
                      x: Optional[torch.Tensor] = None, mean: Optional[torch.Tensor] = None,
                      codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None) -> None:
     """From x and mean, or from the checkpoint (codes, scales) that the forward pass left."""
-    pg, sg, shape, dtype = _first(dout, "dout")
-    pd, sd = _like(dx, "dx", shape, dtype)
-    px, sx = _like(x, "x", shape, dtype) if x is not None else (None, 0)
-    rows, cols = shape
-    (pw, pdw, pdb), kind = _params(cols, weight, dweight, dbias)
-    pc, ps = _codes(codes, scales, rows, cols)
-    pws, nws = (workspace.data_ptr(), workspace.numel() * workspace.element_size()) if workspace is not None else (None, 0)
-    _check(_lib.kt_norm_backward(pg, sg, px, sx, _per_row(mean, rows, "mean"), pc, ps, _per_row(rstd, rows, "rstd"), pw, kind,
-                                 pd, sd, pdw, pdb, pws, nws, rows, cols, _DTYPES[dtype], _stream(stream)))
+    _fast.norm_backward(dout, weight, rstd, dx, dweight, dbias, workspace, x, mean, codes, scales, stream)
 
 
 _ACTS = {"gelu": KT_GELU, "silu": KT_SILU, KT_GELU: KT_GELU, KT_SILU: KT_SILU}
@@ -799,45 +740,13 @@ def _act_kind(kind) -> int:
 def kt_act_forward(x: torch.Tensor, out: torch.Tensor, codes: Optional[torch.Tensor] = None,
                    scales: Optional[torch.Tensor] = None, kind="gelu", stream=None) -> None:
     """out = GELU or SiLU of x; with codes and scales x is kept in 8 bits by the same pass."""
-    px, sx, shape, dtype = _first(x, "x")
-    po, so = _like(out, "out", shape, dtype)
-    rows, cols = shape
-    pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_act_forward(px, sx, po, so, pc, ps, rows, cols, _DTYPES[dtype], _act_kind(kind), _stream(stream)))
+    _fast.act_forward(x, out, codes, scales, _act_kind(kind), stream)
 
 
 def kt_act_backward(dout: torch.Tensor, codes: Optional[torch.Tensor], scales: Optional[torch.Tensor], dx: torch.Tensor,
                     kind="gelu", x: Optional[torch.Tensor] = None, stream=None) -> None:
     """dx = dout * act'(x), x from its checkpoint or (codes and scales None) as it is."""
-    pg, sg, shape, dtype = _first(dout, "dout")
-    pd, sd = _like(dx, "dx", shape, dtype)
-    px, sx = _like(x, "x", shape, dtype) if x is not None else (None, 0)
-    rows, cols = shape
-    pc, ps = _codes(codes, scales, rows, cols)
-    _check(_lib.kt_act_backward(pg, sg, px, sx, pc, ps, pd, sd, rows, cols, _DTYPES[dtype], _act_kind(kind), _stream(stream)))
-
-
-def _heads(t: torch.Tensor, what: str, shape, strides: list) -> int:
-    """Address of a tensor [batch, tokens, heads, head_dim]; its strides of batch, token and head join the list."""
-    s = t.stride()
-    if t.dtype != torch.bfloat16 or t.shape != shape or (s[3] != 1 and shape[3] > 1):
-        raise KtError(KT_ERR_SHAPE, "%s: bfloat16 %s with a contiguous last dimension expected" % (what, list(shape)))
-    strides += s[:3]
-    return t.data_ptr()
-
-
-def _attn(sq, sk, lse: torch.Tensor, scale, causal, used_q, used_kv) -> _Attn:
-    """kt_attn from the shapes of q and k, with the address of lse."""
-    if len(sq) != 4 or len(sk) != 4 or sq[0] != sk[0] or sq[3] != sk[3]:
-        raise KtError(KT_ERR_SHAPE, "q and k: [batch, tokens, heads, head_dim] with the same batch and head_dim expected")
-    B, Lq, H, D = sq
-    for u in (used_q, used_kv):
-        if u is not None and (u.dtype != torch.int32 or u.shape != (B,) or not u.is_contiguous()):
-            raise KtError(KT_ERR_SHAPE, "used_q, used_kv: contiguous int32 [batch] expected")
-    if lse.dtype != torch.float32 or lse.shape != (B, H, Lq) or not lse.is_contiguous():
-        raise KtError(KT_ERR_SHAPE, "lse: contiguous float32 [batch, heads, tokens] expected")
-    return _Attn(B, Lq, sk[1], H, sk[2], D, KT_BF16, bool(causal), D ** -0.5 if scale is None else scale,
-                 None if used_q is None else used_q.data_ptr(), None if used_kv is None else used_kv.data_ptr())
+    _fast.act_backward(dout, codes, scales, dx, _act_kind(kind), x, stream)
 
 
 def kt_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
@@ -845,12 +754,7 @@ def kt_attn_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torc
                     used_kv: Optional[torch.Tensor] = None, stream=None) -> None:
     """out = softmax(scale q k^T) v on bfloat16 [batch, tokens, heads, head_dim] (any strides that are multiples
     of 8; k and v may have fewer heads), lse float32 [batch, heads, tokens].  scale: 1 / sqrt(head_dim) by default."""
-    sq, sk, st = q.shape, k.shape, []
-    desc = _attn(sq, sk, lse, scale, causal, used_q, used_kv)
-    pq, pk, pv, po = _heads(q, "q", sq, st), _heads(k, "k", sk, st), _heads(v, "v", sk, st), _heads(out, "out", sq, st)
-    strides = (C.c_int64 * 12)(*st)
-    at = C.addressof(strides)
-    _check(_lib.kt_attn_forward(C.byref(desc), pq, at, pk, at + 24, pv, at + 48, po, at + 72, lse.data_ptr(), _stream(stream)))
+    _fast.attn_forward(q, k, v, out, lse, scale, causal, used_q, used_kv, stream)
 
 
 def kt_attn_workspace(q: torch.Tensor, k: torch.Tensor) -> int:
@@ -864,15 +768,7 @@ def kt_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
                      causal: bool = False, used_q: Optional[torch.Tensor] = None, used_kv: Optional[torch.Tensor] = None,
                      stream=None) -> None:
     """Gradients of kt_attn_forward from its arguments and results; workspace: kt_attn_workspace bytes."""
-    sq, sk, st = q.shape, k.shape, []
-    desc = _attn(sq, sk, lse, scale, causal, used_q, used_kv)
-    pg, pq, pk, pv = _heads(dout, "dout", sq, st), _heads(q, "q", sq, st), _heads(k, "k", sk, st), _heads(v, "v", sk, st)
-    po, pdq, pdk, pdv = _heads(out, "out", sq, st), _heads(dq, "dq", sq, st), _heads(dk, "dk", sk, st), _heads(dv, "dv", sk, st)
-    strides = (C.c_int64 * 24)(*st)
-    at = C.addressof(strides)
-    _check(_lib.kt_attn_backward(C.byref(desc), pg, at, pq, at + 24, pk, at + 48, pv, at + 72, po, at + 96, lse.data_ptr(),
-                                 pdq, at + 120, pdk, at + 144, pdv, at + 168, workspace.data_ptr() or None,
-                                 workspace.numel() * workspace.element_size(), _stream(stream)))
+    _fast.attn_backward(dout, q, k, v, out, lse, dq, dk, dv, workspace, scale, causal, used_q, used_kv, stream)
 
 
 def kt_attn_given_up() -> int:

@@ -1,5 +1,5 @@
 """Arguments that the training operators refuse, before anything is launched (no GPU needed: every
-case is turned away on the host)."""
+case is turned away on the host; where there is a GPU the tensors are there)."""
 import pytest
 import torch
 
@@ -10,6 +10,12 @@ F32, BF16, I8 = torch.float32, torch.bfloat16, torch.int8
 def kt():
     from paper_2505_10183_b200 import binding
     return binding
+
+
+@pytest.fixture(autouse=True)
+def where():
+    with torch.device("cuda" if torch.cuda.is_available() else "cpu"):
+        yield
 
 
 def status(kt, call, *args, **kw):
@@ -61,6 +67,16 @@ def test_refused_backward_sources(kt):
     assert status(kt, back, x, w, r, x, w, w.to(BF16), ws, codes=c, scales=s) == kt.KT_ERR_SHAPE
     assert status(kt, kt.kt_act_backward, x, None, None, x) == kt.KT_ERR_INVALID
     assert status(kt, kt.kt_act_backward, x, c, s, x, x=x) == kt.KT_ERR_INVALID
+
+
+def test_tensors_in_host_memory_are_refused_where_there_is_a_device(kt):
+    if not torch.cuda.is_available():
+        pytest.skip("needs a device that they could be mistaken for")
+    x, host = torch.zeros(4, 32), torch.zeros(4, 32, device="cpu")
+    assert status(kt, kt.kt_act_forward, host, host) == kt.KT_ERR_INVALID
+    assert status(kt, kt.kt_act_forward, x, host) == kt.KT_ERR_INVALID
+    with pytest.raises(kt.KtError):
+        kt.kt_act_forward([1.0], x, stream=0)
 
 
 def test_c_entries_refuse_bad_addresses_and_types(kt):
