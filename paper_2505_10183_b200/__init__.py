@@ -9,10 +9,10 @@ from __future__ import annotations
 
 import importlib
 
-__all__ = ["binding", "workloads", "build"]
+__all__ = ["binding", "workloads", "build", "block_step"]
 
 
 def __getattr__(name):
-    if name in ("binding", "workloads", "build"):
+    if name in ("binding", "workloads", "build", "block_step"):
         return importlib.import_module("." + name, __name__)
     raise AttributeError(name)
