@@ -17,6 +17,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <climits>
 #include <cmath>
 
@@ -209,6 +210,26 @@ __device__ __forceinline__ void load_param(const void *p, bool bf16, int64_t col
         if (col + i < cols) w[i] = bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[col + i]) : static_cast<const float *>(p)[col + i];
 }
 
+__device__ __forceinline__ void store_param(void *p, bool bf16, int64_t col, float x) {
+    if (p == nullptr) return;
+    if (bf16) static_cast<__nv_bfloat16 *>(p)[col] = __float2bfloat16_rn(x);
+    else static_cast<float *>(p)[col] = x;
+}
+
+// A barrier of the cluster's CTAs, and a value at the same place in another one's shared memory.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+__device__ __forceinline__ float of_cta(const float *mine, unsigned rank) {
+    float x;
+    asm volatile(
+        "{\n\t.reg .b32 at;\n\tmapa.shared::cluster.u32 at, %1, %2;\n\tld.shared::cluster.f32 %0, [at];\n\t}"
+        : "=f"(x)
+        : "r"(static_cast<unsigned>(__cvta_generic_to_shared(mine))), "r"(rank)
+        : "memory");
+    return x;
+}
+
 // The V codes of one vector and the scale of its block.  The 128 / V lanes that hold a block are
 // neighbours; all lanes of the warp call it, those without columns of the row with `in` false.  Columns
 // past the row's end in a vector that has some hold zeros.  Adding 1.5 * 2^23
@@ -292,7 +313,7 @@ struct NormParams {
     void *dweight, *dbias;
     int64_t rows, cols, x_stride, dout_stride, out_stride;
     float eps;
-    int param_bf16, n_parts;
+    int param_bf16, n_parts, joint;       // joint: the backward pass' CTAs are one cluster
 };
 
 // The threads on a row are a warp (four rows to a CTA) or a CTA of 128, 256 or 512; a thread takes the
@@ -454,8 +475,9 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
 
 // With u = (x - mean) rstd (or its 8-bit checkpoint) and g = dout w:
 //   dx = rstd (g - mean(g) - u mean(g u)),  dweight = sum_rows dout u,  dbias = sum_rows dout.
-// A CTA of 512 threads fills an SM's registers; its groups join their columns' sums at the end, and one row of partial
-// sums per CTA is reduced in a fixed order by k_norm_params: no atomics, so that a step gives the same bits
+// A CTA of 512 threads fills an SM's registers; its groups join their columns' sums at the end.  With few rows the CTAs
+// are one cluster that joins its sums through distributed shared memory; else one row of partial
+// sums per CTA is reduced in a fixed order by k_norm_params: no atomics either way, so that a step gives the same bits
 // when it is run again.  (With a CTA to a group, four times as many partial sums: 47.6 instead of 38.6 us for
 // 16384 x 2048 bf16 from a checkpoint.)
 template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
@@ -585,40 +607,39 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
             store_row<T, WIDE>(static_cast<T *>(p.out) + r * p.out_stride, column<GROUP, NV, V>(at, k), cols, y);
         }
     }
-    if (p.parts == nullptr) return;
-    float *part = p.parts + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
-    if constexpr (GROUPS > 1) {
-        constexpr int N = GROUP * NV * V;
-        float *const joined = reinterpret_cast<float *>(ring);
-        wait_copies<0>();
-        for (int turn_of = 0; turn_of < GROUPS; ++turn_of) {
-            __syncthreads();
-            if (group == turn_of) {
+    if (p.dweight == nullptr && p.dbias == nullptr) return;
+    constexpr int N = GROUP * NV * V;
+    float *const joined = reinterpret_cast<float *>(ring);      // [GROUPS][2][N]
+    wait_copies<0>();
+    __syncthreads();
 #pragma unroll
-                for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
-                    for (int i = 0; i < V; i += 4) {
-                        float4 *const a = reinterpret_cast<float4 *>(joined + column<GROUP, NV, V>(at, k) + i), *const c = a + N / 4;
-                        float4 x = make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]), y = make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]);
-                        if (turn_of > 0) {
-                            const float4 p = *a, q = *c;
-                            x.x += p.x, x.y += p.y, x.z += p.z, x.w += p.w, y.x += q.x, y.y += q.y, y.z += q.z, y.w += q.w;
-                        }
-                        *a = x, *c = y;
-                    }
-            }
+        for (int i = 0; i < V; i += 4) {
+            float4 *const to = reinterpret_cast<float4 *>(joined + group * 2 * N + column<GROUP, NV, V>(at, k) + i);
+            to[0] = make_float4(dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]);
+            to[N / 4] = make_float4(db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]);
         }
-        __syncthreads();
-        for (int c = threadIdx.x; c < cols; c += THREADS) part[c] = joined[c], part[p.cols + c] = joined[N + c];
-    } else {
+    __syncthreads();
+    float *const part = p.joint ? joined : p.parts + static_cast<int64_t>(blockIdx.x) * 2 * p.cols;
+    const int half = p.joint ? N : cols;
+    for (int c = threadIdx.x; c < cols; c += THREADS) {
+        float w = 0.0f, b = 0.0f;
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int c = column<GROUP, NV, V>(at, k) + i;
-                if (c < cols) part[c] = dw[k][i], part[p.cols + c] = db[k][i];
-            }
+        for (int g = 0; g < GROUPS; ++g) w += joined[g * 2 * N + c], b += joined[g * 2 * N + N + c];
+        part[c] = w, part[half + c] = b;
     }
+    if (!p.joint) return;
+    // few rows: the CTAs are a cluster, and each takes its share of the columns from all of them
+    cluster_sync();
+    const unsigned ctas = gridDim.x;
+    for (int c = blockIdx.x * THREADS + threadIdx.x; c < cols; c += ctas * THREADS) {
+        float w = 0.0f, b = 0.0f;
+        for (unsigned r = 0; r < ctas; ++r) w += of_cta(joined + c, r), b += of_cta(joined + N + c, r);
+        store_param(p.dweight, p.param_bf16, c, w);
+        store_param(p.dbias, p.param_bf16, c, b);
+    }
+    cluster_sync();                              // until all have read
 }
 
 // Rows too wide for registers: the row is read again for each of its passes (from L2, where a row
@@ -752,10 +773,7 @@ __global__ void __launch_bounds__(1024) k_norm_params(const NormParams p) {
 #pragma unroll
     for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     const int64_t to = static_cast<int64_t>(blockIdx.x) * 32 + threadIdx.y;
-    if (threadIdx.x == 0 && to < p.cols) {
-        if (p.param_bf16) static_cast<__nv_bfloat16 *>(out)[to] = __float2bfloat16_rn(v);
-        else static_cast<float *>(out)[to] = v;
-    }
+    if (threadIdx.x == 0 && to < p.cols) store_param(out, p.param_bf16, to, v);
 }
 
 // ------------------------------------------------------------- activations and checkpoints
@@ -1008,22 +1026,35 @@ RowShape row_shape(int64_t cols, int dtype) {
     return s;
 }
 
-template <typename Kernel>
-int start_norm_kernel(Kernel kernel, const NormParams &p, int grid, int threads, size_t smem, cudaStream_t st) {
-    if (smem > 47 * 1024) KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    kernel<<<grid, threads, smem, st>>>(p);
-    KT_CUDA(cudaGetLastError());
+// (A kernel's limit of shared memory is raised once per device: the call costs a third of a launch.)
+template <auto KERNEL>
+int start_norm_kernel(const NormParams &p, int grid, int threads, size_t smem, cudaStream_t st) {
+    static std::atomic<uint64_t> raised{0};
+    int dev = 0;
+    KT_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (smem > 47 * 1024 && (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit))) {
+        KT_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+        raised.fetch_or(bit, std::memory_order_relaxed);
+    }
+    cudaLaunchAttribute joint{};
+    joint.id = cudaLaunchAttributeClusterDimension;
+    joint.val.clusterDim.x = grid, joint.val.clusterDim.y = joint.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = threads, config.dynamicSmemBytes = smem, config.stream = st;
+    config.attrs = &joint, config.numAttrs = p.joint ? 1 : 0;
+    KT_CUDA(cudaLaunchKernelEx(&config, KERNEL, p));
     return KT_OK;
 }
 
 template <typename T, bool WIDE, int GROUP, int NV>
 int start_norm(bool backward, const NormParams &p, int grid, cudaStream_t st) {
     constexpr int V = Elems<T>::V, SLOTS = WIDE ? (rows_ahead<NV>() + 1) * NV : 0, FORWARD = norm_threads<GROUP>();
-    if (!backward) return start_norm_kernel(k_norm_forward<T, WIDE, GROUP, NV>, p, grid, FORWARD, SLOTS * FORWARD * sizeof(uint4), st);
-    const size_t joined = GROUP < GROUP_MAX ? 2 * GROUP * NV * V * sizeof(float) : 0;
+    if (!backward) return start_norm_kernel<k_norm_forward<T, WIDE, GROUP, NV>>(p, grid, FORWARD, SLOTS * FORWARD * sizeof(uint4), st);
+    const size_t joined = 2 * GROUP_MAX * NV * V * sizeof(float);
     const size_t kept = SLOTS * GROUP_MAX * (sizeof(uint4) + V + sizeof(float)), whole = SLOTS * GROUP_MAX * 2 * sizeof(uint4);
-    if (p.codes != nullptr) return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, true>, p, grid, GROUP_MAX, kept > joined ? kept : joined, st);
-    return start_norm_kernel(k_norm_backward<T, WIDE, GROUP, NV, false>, p, grid, GROUP_MAX, whole > joined ? whole : joined, st);
+    if (p.codes != nullptr) return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, true>>(p, grid, GROUP_MAX, kept > joined ? kept : joined, st);
+    return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, false>>(p, grid, GROUP_MAX, whole > joined ? whole : joined, st);
 }
 
 template <typename T, bool WIDE, int GROUP>
@@ -1139,11 +1170,15 @@ int act_backward(const ElemParams &all, int dtype, int kind, bool wide_, cudaStr
 int restore(const ElemParams &all, int dtype, int kind, bool wide_, cudaStream_t st) { return over_rows(all, dtype, wide_, KT_EACH(start_restore)); }
 #undef KT_EACH
 
-// Rows of partial sums, one to a CTA of the backward pass; a group has two rows at least, so that the
-// partial sums stay small beside what is read.
-int64_t norm_parts(int64_t rows, const RowShape &s) {
-    const int64_t per_cta = GROUP_MAX / s.group * 2, need = (rows + per_cta - 1) / per_cta;
-    return need < SMS ? need : SMS;
+// CTAs of the backward pass.  Up to CLUSTER of them, with up to four rows to a group, are a cluster, which saves the
+// second kernel (109 rows of 512, both together: 13.1 -> 6.9 us); else there is a row of partial sums to each, and a group has
+// two rows at least, so that these stay small beside what is read.
+constexpr int64_t CLUSTER = 8;
+int64_t norm_parts(int64_t rows, const RowShape &s, bool *joint) {
+    const int64_t groups = GROUP_MAX / s.group;
+    *joint = rows <= CLUSTER * groups * 4;
+    const int64_t need = *joint ? (rows + groups - 1) / groups : (rows + groups * 2 - 1) / (groups * 2), most = *joint ? CLUSTER : SMS;
+    return need < most ? need : most;
 }
 constexpr int64_t ANY_PARTS = 16;
 
@@ -1187,7 +1222,8 @@ int64_t kt_norm_workspace(int64_t rows, int64_t cols) {
     int64_t parts = rows < ANY_PARTS ? rows : ANY_PARTS;
     if (cols <= ROW_MAX)                  // room for either type
         for (int dtype : {KT_F32, KT_BF16}) {
-            const int64_t n = norm_parts(rows, row_shape(cols, dtype));
+            bool joint = false;
+            const int64_t n = norm_parts(rows, row_shape(cols, dtype), &joint);
             parts = dtype == KT_F32 || n > parts ? n : parts;
         }
     return parts * 2 * cols * static_cast<int64_t>(sizeof(float));
@@ -1234,10 +1270,12 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
     } else if (rows > 0) {
         const RowShape s = row_shape(cols, dtype);
         const bool w = wide(dout, dout_stride, rows, cols, dtype) && wide(dx, dx_stride, rows, cols, dtype) && (x == nullptr || wide(x, x_stride, rows, cols, dtype));
-        p.n_parts = static_cast<int>(norm_parts(rows, s));
+        bool joint = false;
+        p.n_parts = static_cast<int>(norm_parts(rows, s, &joint));
+        p.joint = joint && sums;
         if (int rc = start_norm(true, dtype, w, s, p, p.n_parts, st)) return rc;
     }
-    if (sums) {
+    if (sums && !p.joint) {
         KT_CUDA(launch_behind(k_norm_params, dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st, p));
     }
     return KT_OK;
