@@ -12,7 +12,7 @@
 //
 // All products run on the tensor cores (kt_tensor.cuh): operands come in by tile copies, sums stay in
 // tensor memory, and the probabilities (dS) go back to tensor memory as bf16, where they are the first
-// operand of the next product.  One warp issues copies, one issues products, eight compute.
+// operand of the next product.  One warp brings tiles, three issue products, eight compute.
 // Rows past a sequence's length may hold anything: they are cleared in shared memory where they would
 // be multiplied by a zero.
 #include "../../include/kaitian.h"
@@ -21,6 +21,7 @@
 
 #include <atomic>
 #include <cmath>
+#include <cstddef>
 
 #include "kt_internal.h"
 #include "kt_pairs.cuh"
@@ -53,7 +54,7 @@ struct AttnParams {
     unsigned *next_item;
     int64_t o_stride[3], dout_stride[3], out_stride[3], dk_stride[3], dv_stride[3];     // batch, token, head
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
-    int tiles_q, tiles_kv;
+    int tiles_q, tiles_kv, parts;               // parts: CTAs that share a work item of the forward pass
     float scale, scale_log2;
 };
 
@@ -131,6 +132,8 @@ __device__ __forceinline__ void settle(volatile uint32_t *gave_up) {
 // the other group's next ones, so that neither a group nor the tensor cores wait for the other in turn.
 // CTAs stay (Queue): the next item's tiles are fetched and its first scores formed while the last item's
 // output is written, which short sequences need most.  Every barrier's phases are counted on from item to item.
+// With SPLIT, for few long items, the CTAs of a cluster share the keys of one item and join what each has of it
+// through distributed shared memory: no workspace, and the same bits every time.
 // Tensor memory: scores 0, probabilities 128 and 192, sums 256 and 256 + DH.
 template <int DH>
 struct FwdSmem {
@@ -142,9 +145,10 @@ struct FwdSmem {
     uint32_t tmem, gave_up;
 };
 
-// A work item: the pair of query tiles, and the key tiles that each of them sees.
+// A work item: the pair of query tiles, and the key tiles that each of them sees; with SPLIT, a CTA's share of these.
+template <bool SPLIT>
 struct FwdItem {
-    int row0, b, h, h_kv, n_tiles[2], n, common, longer, steps;
+    int row0, b, h, h_kv, from, n_tiles[2], n, common, longer, steps;
     __device__ FwdItem(const AttnParams &p, int block) {
         const int pairs = (p.tiles_q + 1) / 2, all = p.batch * p.heads, bh = block % all;
         row0 = (pairs - 1 - block / all) * 2 * TILE;               // the longest rows first
@@ -155,7 +159,13 @@ struct FwdItem {
             const int first = row0 + w * TILE;
             n_tiles[w] = first < seq.n ? tiles(seq.keys_of(min(first + TILE, seq.n) - 1)) : 0;
         }
-        n = max(n_tiles[0], n_tiles[1]);
+        n = max(n_tiles[0], n_tiles[1]), from = 0;
+        if constexpr (SPLIT) {
+            const int rank = blockIdx.x % p.parts, to = n * (rank + 1) / p.parts;
+            from = n * rank / p.parts, n = to - from;
+#pragma unroll
+            for (int w = 0; w < 2; ++w) n_tiles[w] = max(0, min(n_tiles[w], to) - from);
+        }
         // Steps: the two tiles in turn while both have keys left, then the one that has more.
         common = min(n_tiles[0], n_tiles[1]), longer = n_tiles[1] > n_tiles[0] ? 1 : 0, steps = n_tiles[0] + n_tiles[1];
     }
@@ -164,12 +174,54 @@ struct FwdItem {
     __device__ bool last_use(int u) const { return group(u) == 1 || key_tile(u) >= n_tiles[1]; }      // of its key tile
 };
 
-template <int DH>
+// A row of a split item: sums O_r and s_r over share r of the keys, taken with maxima m_r, give
+// O = (sum_r 2^(m_r - m) O_r) / (sum_r 2^(m_r - m) s_r) with m the largest.  Every CTA of the cluster takes its share of the
+// rows, reads them from all, in their order, and writes them; 8 columns to a thread.
+template <int DH, int PARTS>
+__device__ __forceinline__ void join_parts(const AttnParams &p, const FwdItem<true> &it, uint32_t at) {
+    static_assert(2 * TILE * (DH * 4 + 8) <= offsetof(FwdSmem<DH>, queue));
+    constexpr int LANES = DH / 8, SHARE = 2 * TILE / PARTS;
+    const int from = blockIdx.x % PARTS * SHARE, c = threadIdx.x % LANES;
+    for (int r = from + threadIdx.x / LANES; r < from + SHARE; r += 2 * TILE / LANES) {
+        const int row = it.row0 + r;
+        if (row >= p.len_q) break;
+        const uint32_t stats = at + 2 * TILE * DH * 4 + r * 8, sums = at + r * DH * 4;
+        float2 s[PARTS];
+        float4 x[PARTS][2];                     // all on their way before the first is used
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            s[i] = of_cta2(stats, i);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[i][e] = of_cta4(sums + (2 * c / 8 * 8 + ((2 * c + e) % 8 ^ r % 8)) * 16, i);
+        }
+        float top = -INFINITY, sum = 0.0f, o[8] = {};
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) top = fmaxf(top, s[i].x);
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) {
+            const float by = s[i].y == 0.0f ? 0.0f : exp2_fast(s[i].x - top);
+            sum = fmaf(s[i].y, by, sum);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                o[e * 4] = fmaf(x[i][e].x, by, o[e * 4]), o[e * 4 + 1] = fmaf(x[i][e].y, by, o[e * 4 + 1]);
+                o[e * 4 + 2] = fmaf(x[i][e].z, by, o[e * 4 + 2]), o[e * 4 + 3] = fmaf(x[i][e].w, by, o[e * 4 + 3]);
+            }
+        }
+        const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
+        if (c * 8 < p.dim)
+            *reinterpret_cast<uint4 *>(p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2] + c * 8) =
+                make_uint4(pack_bf16(o[0] * by, o[1] * by), pack_bf16(o[2] * by, o[3] * by), pack_bf16(o[4] * by, o[5] * by), pack_bf16(o[6] * by, o[7] * by));
+        if (c == 0) p.lse[(static_cast<int64_t>(it.b) * p.heads + it.h) * p.len_q + row] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * LN2;
+    }
+}
+
+template <int DH, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                const AttnParams p) {
     extern __shared__ uint8_t raw[];
     using Smem = FwdSmem<DH>;
+    using Item = FwdItem<SPLIT>;
     constexpr int SETS = Smem::SETS, K_SLOTS = Smem::K_SLOTS, V_SLOTS = Smem::V_SLOTS;
     auto &sm = *reinterpret_cast<Smem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -189,18 +241,21 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
+    const int first_block = SPLIT ? blockIdx.x / p.parts : blockIdx.x;       // and the only one, with SPLIT
     volatile uint32_t *gave_up = &sm.gave_up;
 
     if (warp == WARP_LOAD) {
         registers_give<REGISTERS_HELP>();
         uint32_t asked = 0, sets = 0, tiles_in = 0, landed_phase = 0;      // counts over all items
         bool ok = true;
-        for (int block = blockIdx.x; ok && block >= 0; block = queue_next<false>(sm.queue, asked - 1, gave_up)) {
-            const FwdItem it(p, block);
+        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, asked - 1, gave_up)) {
+            const Item it(p, block);
             const Seq seq(p, it.b);
-            if (!(ok = bar_wait(&sm.queue.free[asked % QUEUE], (asked / QUEUE + 1) & 1, gave_up))) break;
-            if (lane == 0) queue_ask(sm.queue, asked);
-            ++asked;
+            if constexpr (!SPLIT) {
+                if (!(ok = bar_wait(&sm.queue.free[asked % QUEUE], (asked / QUEUE + 1) & 1, gave_up))) break;
+                if (lane == 0) queue_ask(sm.queue, asked);
+                ++asked;
+            }
             if (it.n == 0) continue;
             const int set = sets % SETS;
             if (!(ok = bar_wait(&sm.q_free[set], (sets / SETS + 1) & 1, gave_up))) break;
@@ -215,12 +270,12 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (j < it.n) {
                     const uint32_t i = tiles_in + j, ks = i % K_SLOTS;
                     ok = bar_wait(&sm.k_free[ks], (i / K_SLOTS + 1) & 1, gave_up) &&
-                         load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                         load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                 }
                 if (ok && j > 0) {
                     const uint32_t i = tiles_in + j - 1, vs = i % V_SLOTS;
                     ok = bar_wait(&sm.v_free[vs], (i / V_SLOTS + 1) & 1, gave_up) &&
-                         load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (j - 1) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                         load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (it.from + j - 1) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                 }
             }
             tiles_in += it.n;
@@ -231,8 +286,8 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
             uint32_t items = 0, sets = 0, tiles_in = 0, steps = 0;
             bool ok = true;
-            for (int block = blockIdx.x; ok && block >= 0; block = queue_next_one<false>(sm.queue, items++, gave_up)) {
-                const FwdItem it(p, block);
+            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, gave_up)) {
+                const Item it(p, block);
                 if (it.n == 0) continue;
                 const uint32_t set = sets % SETS;
                 ok = bar_wait_one(&sm.q_full[set], sets / SETS & 1, gave_up);
@@ -258,8 +313,8 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const uint32_t v_at = smem_addr(sm.v);
             uint32_t items = 0, tiles_in = 0, mine[2] = {0, 0}, outputs[2] = {0, 0};
             bool ok = true;
-            for (int block = blockIdx.x; ok && block >= 0; block = queue_next_one<false>(sm.queue, items++, gave_up)) {
-                const FwdItem it(p, block);
+            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, gave_up)) {
+                const Item it(p, block);
                 for (int u = 0; ok && u < it.steps; ++u) {
                     const int w = it.group(u), j = it.key_tile(u);
                     const uint32_t i = tiles_in + j, vs = i % V_SLOTS;
@@ -282,8 +337,8 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, p_at = lanes + TILE + w * 64, o_at = lanes + 256 + w * DH;
         uint32_t items = 0, mine = 0;
         bool ok = true;
-        for (int block = blockIdx.x; ok && block >= 0; block = queue_next<false>(sm.queue, items++, gave_up)) {
-            const FwdItem it(p, block);
+        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, items++, gave_up)) {
+            const Item it(p, block);
             const Seq seq(p, it.b);
             const int row = it.row0 + w * TILE + threadIdx.x % TILE, n_mine = w == 0 ? it.n_tiles[0] : it.n_tiles[1];
             const int limit = seq.keys_of(row), all_see = seq.keys_of(it.row0 + w * TILE);    // the tile's first row sees least
@@ -296,11 +351,11 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 uint32_t s[4][32];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
-                tmem_wait_loads();
+                tmem_wait_loads(s);
                 tmem_fence_before();
                 bar_arrive_warp(&sm.s_taken);
-                if (!whole || (j + 1) * TILE > all_see) {
-                    const int left = limit - j * TILE;           // columns that the row sees
+                if (!whole || (it.from + j + 1) * TILE > all_see) {
+                    const int left = limit - (it.from + j) * TILE;           // columns that the row sees
 #pragma unroll
                     for (int c = 0; c < TILE; ++c)
                         if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
@@ -323,7 +378,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                         for (int c = 0; c < DH; c += 32) {
                             uint32_t o[32];
                             tmem_load32(o_at + c, o);
-                            tmem_wait_loads();
+                            tmem_wait_loads(o);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
                             tmem_store32(o_at + c, o);
@@ -352,6 +407,26 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 bar_arrive_warp(&sm.p_ready[w]);
             }
             mine += n_mine;
+            if constexpr (SPLIT) {                  // what the CTA has of the row, over the tiles that are done with
+                if (ok && n_mine > 0) ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up);
+                tmem_fence_after();
+                asm volatile("barrier.sync 1, 256;" ::: "memory");
+                float4 *const to = reinterpret_cast<float4 *>(&sm) + threadIdx.x * (DH / 4);
+#pragma unroll
+                for (int c = 0; c < DH; c += 32) {
+                    uint32_t o[32];
+                    tmem_load32(o_at + c, o);        // (whatever is there if the CTA has no keys)
+                    tmem_wait_loads(o);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        if (sum != 0.0f) v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+                        to[c / 4 + (e / 4 ^ threadIdx.x % 8)] = v;
+                    }
+                }
+                reinterpret_cast<float2 *>(reinterpret_cast<float *>(&sm) + 2 * TILE * DH)[threadIdx.x] = make_float2(top, sum);
+                break;
+            }
             __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
             if (ok && n_mine > 0) {
                 if (!(ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up))) break;
@@ -362,7 +437,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     uint32_t o[2][32];
                     tmem_load32(o_at + c, o[0]);
                     tmem_load32(o_at + c + 32, o[1]);
-                    tmem_wait_loads();
+                    tmem_wait_loads(o);
                     if (c == DH - 64) {
                         tmem_fence_before();
                         bar_arrive_warp(&sm.o_taken[w]);
@@ -381,6 +456,16 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         registers_give<REGISTERS_HELP>();       // WARP_DP has nothing to do here, but its group gives back together
     }
     tmem_fence_before();
+    if constexpr (SPLIT) {
+        cluster_sync();
+        if (warp < 8) {
+            const Item it(p, first_block);
+            if (p.parts == 2) join_parts<DH, 2>(p, it, smem_addr(&sm));
+            else if (p.parts == 4) join_parts<DH, 4>(p, it, smem_addr(&sm));
+            else join_parts<DH, 8>(p, it, smem_addr(&sm));
+        }
+        cluster_sync();                         // the others have read what is here
+    }
     __syncthreads();
     settle(gave_up);
     if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
@@ -877,7 +962,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
 #pragma unroll
                     for (int q = 0; q < WIDTH / 32; ++q) tmem_load32(s_at + q * 32, s[q]);
-                    tmem_wait_loads();
+                    tmem_wait_loads(s);
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
                     if (__any_sync(0xFFFFFFFFu, hidden > 0)) {
@@ -911,7 +996,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         tmem_load32(dp_at, d[0]);
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
-                            tmem_wait_loads();
+                            tmem_wait_loads(d[q % 2]);
                             if (q < 3) {
                                 tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
                             } else {
@@ -928,7 +1013,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     } else {
                         tmem_load32(dp_at, d[0]);
                         tmem_load32(dp_at + 32, d[1]);
-                        tmem_wait_loads();
+                        tmem_wait_loads(d);
                         tmem_store32(p_at, probs[0]);
                         uint32_t packed[32];
 #pragma unroll
@@ -953,7 +1038,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         uint32_t o[2][32];
                         tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c, o[0]);
                         tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c + 32, o[1]);
-                        tmem_wait_loads();
+                        tmem_wait_loads(o);
                         if (c == DH - 64) {
                             tmem_fence_before();
                             bar_arrive_warp(&bars.sums_taken);
@@ -991,7 +1076,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     uint32_t s[4][32];
 #pragma unroll
                     for (int q = 0; q < 4; ++q) tmem_load32(s_at + q * 32, s[q]);
-                    tmem_wait_loads();
+                    tmem_wait_loads(s);
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
                     if (!whole || (j + 1) * TILE > all_see) {
@@ -1011,7 +1096,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     tmem_load32(dp_at, d[0]);
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {        // while 32 columns are worked on, the next are on their way
-                        tmem_wait_loads();
+                        tmem_wait_loads(d[q % 2]);
                         if (q < 3) {
                             tmem_load32(dp_at + (q + 1) * 32, d[(q + 1) % 2]);
                         } else {
@@ -1041,7 +1126,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     uint32_t o[DH / 64][32];                 // a group writes half of the columns
 #pragma unroll
                     for (int c = 0; c < DH / 64; ++c) tmem_load32(lanes + 3 * TILE + w * (DH / 2) + c * 32, o[c]);
-                    tmem_wait_loads();
+                    tmem_wait_loads(o);
                     tmem_fence_before();
                     bar_arrive_warp(&bars.sums_taken);
 #pragma unroll
@@ -1126,33 +1211,68 @@ int fill(const kt_attn *a, AttnParams *p) {
     return KT_OK;
 }
 
-template <typename Smem, typename Kernel>
-int room(Kernel kernel, size_t *bytes) {
+template <typename Smem, auto KERNEL>
+int room(size_t *bytes) {
     static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
     *bytes = sizeof(Smem) + 1024;                // the tiles start at a multiple of 1024
     int dev = 0;
     KT_CUDA(cudaGetDevice(&dev));
     const uint64_t bit = 1ull << (dev & 63);
     if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
-        KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*bytes)));
+        KT_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(*bytes)));
         raised.fetch_or(bit, std::memory_order_relaxed);
     }
     return KT_OK;
 }
 
+// CTAs to a work item of the forward pass (1, 2, 4 or 8): few long items leave SMs without work, yet a CTA of a split
+// item costs its start, which nothing overlaps, and the join.  Estimated in steps of one key tile (some 1.6 us),
+// from the sizes alone, with the figures of the join fitted to these times in us (1, 2, 4, 8 CTAs):
+//   1 query, 8192 keys, 8 heads of 128          97   52   31   20
+//   2048 queries and keys, 8 heads of 64        31   23   35   75
+//   2 x 6499 causal, 2 heads of 64              80   48   73  124
+//   2 x 4096, 8 heads of 64 (256 items)        103  129  176  310
+int parts_of(const AttnParams &p) {
+    const int64_t pairs = (p.tiles_q + 1) / 2, all = static_cast<int64_t>(p.batch) * p.heads, items = pairs * all;
+    if (items > 4 * SMS) return 1;
+    int64_t longest = 0, sum = 0;
+    for (int64_t i = 0; i < pairs; ++i) {
+        const int64_t last = (i + 1) * 2 * TILE < p.len_q ? (i + 1) * 2 * TILE : p.len_q, seen = last + p.len_kv - p.len_q;
+        const int64_t n = !p.causal ? p.tiles_kv : seen > 0 ? (seen + TILE - 1) / TILE : 0;
+        sum += n, longest = n > longest ? n : longest;
+    }
+    const double mean = static_cast<double>(sum) / pairs, rows = p.len_q < 2 * TILE ? p.len_q : 2 * TILE;
+    int best = 1;
+    double least = 0.0;
+    for (int parts = 1; parts <= 8; parts *= 2) {
+        const double each = parts == 1 ? 0.0 : 4.0 + parts * rows / (2 * TILE), rounds = static_cast<double>((items * parts + SMS - 1) / SMS);
+        const double all_rounds = rounds * (mean / parts + each), one = static_cast<double>(longest) / parts + each;
+        const double cost = (all_rounds > one ? all_rounds : one) + (parts == 1 ? 3.0 : 0.0);
+        if (parts == 1 || cost < least) best = parts, least = cost;
+    }
+    return best;
+}
+
 template <int DH>
-int start_forward(const CUtensorMap (&m)[3], const AttnParams &p, cudaStream_t st) {
+int start_forward(const CUtensorMap (&m)[3], AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
-    if (int rc = room<FwdSmem<DH>>(k_attn_forward<DH>, &bytes)) return rc;
-    k_attn_forward<DH><<<static_cast<unsigned>(p.batch * p.heads * ((p.tiles_q + 1) / 2)), THREADS, bytes, st>>>(m[0], m[1], m[2], p);
-    KT_CUDA(cudaGetLastError());
+    p.parts = parts_of(p);
+    const unsigned grid = static_cast<unsigned>(p.batch * p.heads * ((p.tiles_q + 1) / 2) * p.parts);
+    if (p.parts == 1) {
+        if (int rc = room<FwdSmem<DH>, k_attn_forward<DH, false>>(&bytes)) return rc;
+        k_attn_forward<DH, false><<<grid, THREADS, bytes, st>>>(m[0], m[1], m[2], p);
+        KT_CUDA(cudaGetLastError());
+        return KT_OK;
+    }
+    if (int rc = room<FwdSmem<DH>, k_attn_forward<DH, true>>(&bytes)) return rc;
+    KT_CUDA(launch_joint(k_attn_forward<DH, true>, p.parts, dim3(grid), dim3(THREADS), bytes, st, m[0], m[1], m[2], p));
     return KT_OK;
 }
 
 template <int DH>
 int start_backward(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
-    if (int rc = room<BwdSmem<DH>>(k_attn_backward<DH>, &bytes)) return rc;
+    if (int rc = room<BwdSmem<DH>, k_attn_backward<DH>>(&bytes)) return rc;
     const int items = p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q);
     KT_CUDA(launch_behind(k_attn_backward<DH>, dim3(items < SMS ? items : SMS), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
     return KT_OK;

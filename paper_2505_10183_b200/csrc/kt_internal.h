@@ -47,6 +47,41 @@ cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size
     config.attrs = &behind, config.numAttrs = 1;
     return cudaLaunchKernelEx(&config, kernel, args...);
 }
+// A launch whose blocks come in clusters of `joint`, next to each other in x.
+template <typename... Params, typename... Args>
+cudaError_t launch_joint(void (*kernel)(Params...), unsigned joint, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute cluster{};
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = joint, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = grid, config.blockDim = block, config.dynamicSmemBytes = smem, config.stream = stream;
+    config.attrs = &cluster, config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, args...);
+}
+// A barrier of the cluster's threads, and values in another CTA's shared memory, at this one's address.
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t address_in(uint32_t mine, unsigned rank) {
+    uint32_t at;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(mine), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ float of_cta(uint32_t mine, unsigned rank) {
+    float x;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(address_in(mine, rank)) : "memory");
+    return x;
+}
+__device__ __forceinline__ float2 of_cta2(uint32_t mine, unsigned rank) {
+    float2 x;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(address_in(mine, rank)) : "memory");
+    return x;
+}
+__device__ __forceinline__ float4 of_cta4(uint32_t mine, unsigned rank) {
+    float4 x;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(address_in(mine, rank)) : "memory");
+    return x;
+}
 __device__ __forceinline__ void after_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void let_next_begin() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 #endif

@@ -216,20 +216,6 @@ __device__ __forceinline__ void store_param(void *p, bool bf16, int64_t col, flo
     else static_cast<float *>(p)[col] = x;
 }
 
-// A barrier of the cluster's CTAs, and a value at the same place in another one's shared memory.
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive;\n\tbarrier.cluster.wait;" ::: "memory");
-}
-__device__ __forceinline__ float of_cta(const float *mine, unsigned rank) {
-    float x;
-    asm volatile(
-        "{\n\t.reg .b32 at;\n\tmapa.shared::cluster.u32 at, %1, %2;\n\tld.shared::cluster.f32 %0, [at];\n\t}"
-        : "=f"(x)
-        : "r"(static_cast<unsigned>(__cvta_generic_to_shared(mine))), "r"(rank)
-        : "memory");
-    return x;
-}
-
 // The V codes of one vector and the scale of its block.  The 128 / V lanes that hold a block are
 // neighbours; all lanes of the warp call it, those without columns of the row with `in` false.  Columns
 // past the row's end in a vector that has some hold zeros.  Adding 1.5 * 2^23
@@ -632,10 +618,10 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
     if (!p.joint) return;
     // few rows: the CTAs are a cluster, and each takes its share of the columns from all of them
     cluster_sync();
-    const unsigned ctas = gridDim.x;
+    const unsigned ctas = gridDim.x, at_all = static_cast<unsigned>(__cvta_generic_to_shared(joined));
     for (int c = blockIdx.x * THREADS + threadIdx.x; c < cols; c += ctas * THREADS) {
         float w = 0.0f, b = 0.0f;
-        for (unsigned r = 0; r < ctas; ++r) w += of_cta(joined + c, r), b += of_cta(joined + N + c, r);
+        for (unsigned r = 0; r < ctas; ++r) w += of_cta(at_all + c * 4, r), b += of_cta(at_all + (N + c) * 4, r);
         store_param(p.dweight, p.param_bf16, c, w);
         store_param(p.dbias, p.param_bf16, c, b);
     }
@@ -1037,13 +1023,12 @@ int start_norm_kernel(const NormParams &p, int grid, int threads, size_t smem, c
         KT_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
         raised.fetch_or(bit, std::memory_order_relaxed);
     }
-    cudaLaunchAttribute joint{};
-    joint.id = cudaLaunchAttributeClusterDimension;
-    joint.val.clusterDim.x = grid, joint.val.clusterDim.y = joint.val.clusterDim.z = 1;
-    cudaLaunchConfig_t config{};
-    config.gridDim = grid, config.blockDim = threads, config.dynamicSmemBytes = smem, config.stream = st;
-    config.attrs = &joint, config.numAttrs = p.joint ? 1 : 0;
-    KT_CUDA(cudaLaunchKernelEx(&config, KERNEL, p));
+    if (p.joint) {
+        KT_CUDA(launch_joint(KERNEL, grid, dim3(grid), dim3(threads), smem, st, p));
+        return KT_OK;
+    }
+    KERNEL<<<grid, threads, smem, st>>>(p);
+    KT_CUDA(cudaGetLastError());
     return KT_OK;
 }
 

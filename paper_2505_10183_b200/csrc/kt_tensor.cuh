@@ -197,7 +197,23 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const uint32_t (&r)[16
                    "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
 }
-__device__ __forceinline__ void tmem_wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// The values are tied to the wait, or the compiler could move what uses them ahead of it.
+__device__ __forceinline__ void tmem_loaded(uint32_t (&r)[32]) {
+    asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                      "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]),
+                      "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]),
+                      "+r"(r[30]), "+r"(r[31]));
+}
+__device__ __forceinline__ void tmem_wait_loads(uint32_t (&r)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    tmem_loaded(r);
+}
+template <int N>
+__device__ __forceinline__ void tmem_wait_loads(uint32_t (&r)[N][32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) tmem_loaded(r[i]);
+}
 __device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // Order between tensor memory accesses and barrier traffic: before an arrival, after a wait.
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -212,7 +228,8 @@ __host__ __device__ constexpr uint32_t mma_word(int n, bool b_down) {
 // chunks of 64 elements along the row are CHUNK apart.
 constexpr uint64_t OPERAND_ALONG = (1ull << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
 constexpr uint64_t OPERAND_DOWN = (static_cast<uint64_t>(CHUNK >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
-__device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | (addr >> 4); }     // shared memory ends below 2^18
+__device__ __forceinline__ uint32_t in_word(uint32_t addr) { return (addr & 0x3FFFF) >> 4; }      // without the CTA's rank in its cluster
+__device__ __forceinline__ uint64_t operand(uint64_t word, uint32_t addr) { return word | in_word(addr); }
 
 // One lane of a warp that is whole.
 __device__ __forceinline__ bool elected() {
@@ -260,7 +277,7 @@ __device__ __forceinline__ void product_down(uint32_t d, uint32_t a, uint32_t b,
 // after the other; the second 8 elements of all rows are the zeros at `zeros`, past both.
 template <int N>
 __device__ __forceinline__ void product_short(uint32_t d, uint32_t a, uint32_t b, uint32_t zeros) {
-    auto word = [&](uint32_t at) { return (static_cast<uint64_t>((zeros - at) >> 4) << 16) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46) | (at >> 4); };
+    auto word = [&](uint32_t at) { return (static_cast<uint64_t>((zeros - at) >> 4) << 16) | (static_cast<uint64_t>(128 >> 4) << 32) | (1ull << 46) | in_word(at); };
     mma_smem(d, word(a), word(b), mma_word(N, false), 0);
 }
 

@@ -159,6 +159,21 @@ def test_sequences_of_different_lengths(kt, used_q, used_kv, dim, causal):
     run_case(kt, 4, 300, 300, 4, 2, dim, causal, used_q, used_kv, seed=7)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [48, 128])
+@pytest.mark.parametrize("Lq,Lk,H,Hk", [(1, 1100, 2, 1), (1, 4100, 20, 5), (5, 2049, 4, 4), (260, 1500, 3, 1), (900, 1024, 12, 12)])
+def test_few_long_rows(kt, Lq, Lk, H, Hk, dim, causal):
+    """Fewer query tiles than SMs: several CTAs share the keys of one (2, 4 and 8 at these sizes)."""
+    run_case(kt, 2, Lq, Lk, H, Hk, dim, causal, seed=Lq + Lk)
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("used_q,used_kv", [([3, 1, 0, 3], [2000, 1, 700, 0]), (None, [129, 0, 2000, 128]), ([3, 2, 1, 3], None)])
+def test_few_long_rows_of_different_lengths(kt, used_q, used_kv, dim):
+    for causal in (False, True):
+        run_case(kt, 4, 3, 2000, 2, 2, dim, causal, used_q, used_kv, layout="gaps", seed=dim)
+
+
 @pytest.mark.parametrize("Lq,Lk", [(5, 0), (0, 5), (0, 0)])
 def test_no_tokens(kt, Lq, Lk):
     q, kv = torch.ones(2, Lq, 2, 64, dtype=BF16, device="cuda"), torch.ones(2, Lk, 2, 64, dtype=BF16, device="cuda")
