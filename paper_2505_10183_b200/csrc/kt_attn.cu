@@ -54,7 +54,7 @@ struct AttnParams {
     unsigned *next_item;
     int64_t o_stride[3], dout_stride[3], out_stride[3], dk_stride[3], dv_stride[3];     // batch, token, head
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
-    int tiles_q, tiles_kv, parts;               // parts: CTAs that share a work item of the forward pass
+    int tiles_q, tiles_kv, parts;               // parts: CTAs that share a work item, where they do
     float scale, scale_log2;
 };
 
@@ -145,6 +145,29 @@ struct FwdSmem {
     uint32_t tmem, gave_up;
 };
 
+// What a CTA takes of n steps that the CTAs of its cluster share.
+__device__ __forceinline__ void take_share(const AttnParams &p, int &from, int &n) {
+    const int64_t rank = blockIdx.x % p.parts, all = n;
+    from = static_cast<int>(all * rank / p.parts);
+    n = static_cast<int>(all * (rank + 1) / p.parts) - from;
+}
+
+// Sums of a row in fp32, 32 columns at a time, to where the others of the cluster read them.  Rows follow
+// one another; the 16-byte pieces of 32 columns change places from row to row, so that neighbours meet different banks.
+__device__ __forceinline__ void put_sums(void *tiles, int dh, int row, int c, const uint32_t (&o)[32], bool zeros) {
+    float4 *const to = static_cast<float4 *>(tiles) + row * (dh / 4) + c / 4;
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (!zeros) v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
+        to[e / 4 ^ row % 8] = v;
+    }
+}
+// 8 columns of it, v = 0 or 1: the first four or the others.
+__device__ __forceinline__ float4 get_sums(uint32_t tiles, int dh, int row, int c8, int v, unsigned rank) {
+    return of_cta4(tiles + row * dh * 4 + (2 * c8 / 8 * 8 + ((2 * c8 + v) % 8 ^ row % 8)) * 16, rank);
+}
+
 // A work item: the pair of query tiles, and the key tiles that each of them sees; with SPLIT, a CTA's share of these.
 template <bool SPLIT>
 struct FwdItem {
@@ -161,10 +184,9 @@ struct FwdItem {
         }
         n = max(n_tiles[0], n_tiles[1]), from = 0;
         if constexpr (SPLIT) {
-            const int rank = blockIdx.x % p.parts, to = n * (rank + 1) / p.parts;
-            from = n * rank / p.parts, n = to - from;
+            take_share(p, from, n);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) n_tiles[w] = max(0, min(n_tiles[w], to) - from);
+            for (int w = 0; w < 2; ++w) n_tiles[w] = max(0, min(n_tiles[w] - from, n));
         }
         // Steps: the two tiles in turn while both have keys left, then the one that has more.
         common = min(n_tiles[0], n_tiles[1]), longer = n_tiles[1] > n_tiles[0] ? 1 : 0, steps = n_tiles[0] + n_tiles[1];
@@ -185,14 +207,14 @@ __device__ __forceinline__ void join_parts(const AttnParams &p, const FwdItem<tr
     for (int r = from + threadIdx.x / LANES; r < from + SHARE; r += 2 * TILE / LANES) {
         const int row = it.row0 + r;
         if (row >= p.len_q) break;
-        const uint32_t stats = at + 2 * TILE * DH * 4 + r * 8, sums = at + r * DH * 4;
+        const uint32_t stats = at + 2 * TILE * DH * 4 + r * 8;
         float2 s[PARTS];
         float4 x[PARTS][2];                     // all on their way before the first is used
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) {
             s[i] = of_cta2(stats, i);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) x[i][e] = of_cta4(sums + (2 * c / 8 * 8 + ((2 * c + e) % 8 ^ r % 8)) * 16, i);
+            for (int e = 0; e < 2; ++e) x[i][e] = get_sums(at, DH, r, c, e, i);
         }
         float top = -INFINITY, sum = 0.0f, o[8] = {};
 #pragma unroll
@@ -411,18 +433,12 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                 if (ok && n_mine > 0) ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up);
                 tmem_fence_after();
                 asm volatile("barrier.sync 1, 256;" ::: "memory");
-                float4 *const to = reinterpret_cast<float4 *>(&sm) + threadIdx.x * (DH / 4);
 #pragma unroll
                 for (int c = 0; c < DH; c += 32) {
                     uint32_t o[32];
                     tmem_load32(o_at + c, o);        // (whatever is there if the CTA has no keys)
                     tmem_wait_loads(o);
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        if (sum != 0.0f) v = make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]));
-                        to[c / 4 + (e / 4 ^ threadIdx.x % 8)] = v;
-                    }
+                    put_sums(&sm, DH, threadIdx.x, c, o, sum == 0.0f);
                 }
                 reinterpret_cast<float2 *>(reinterpret_cast<float *>(&sm) + 2 * TILE * DH)[threadIdx.x] = make_float2(top, sum);
                 break;
@@ -578,14 +594,16 @@ struct DqTiles {
     alignas(1024) uint8_t q[SETS][TILE_BYTES], dout[SETS][TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
 };
 
+template <bool SPLIT>
 struct DqItem {
-    int tile, row0, b, h, h_kv, bh, n;          // n: key tiles
+    int tile, row0, b, h, h_kv, bh, from, n;    // key tiles: n from `from` on
     __device__ DqItem(const AttnParams &p, int block) {
         const int all = p.batch * p.heads;
         bh = block % all, tile = p.tiles_q - 1 - block / all, row0 = tile * TILE;
         b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
         const Seq seq(p, b);
-        n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
+        n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0, from = 0;
+        if constexpr (SPLIT) take_share(p, from, n);
     }
 };
 
@@ -609,8 +627,9 @@ struct DkvTiles {
     alignas(128) uint4 ones_lse[TILE], ones_delta[TILE], terms[Q_SLOTS][TILE], zeros[TILE];      // zeros come last: product_short
 };
 
+template <bool SPLIT>
 struct DkvItem {
-    int key0, b, h_kv, shared, first, per_head, n;       // query tiles: from `first` on, so many to a head, over all heads
+    int key0, b, h_kv, shared, first, per_head, from, n;       // query tiles: from `first` on, so many to a head; of those of all heads, n from `from` on
     __device__ DkvItem(const AttnParams &p, int block) {
         const int all = p.batch * p.heads_kv, bh = block % all;
         key0 = block / all * TILE;                        // early keys are seen most
@@ -618,7 +637,8 @@ struct DkvItem {
         const Seq seq(p, b);
         first = seq.first_query_of(key0) / TILE;
         per_head = key0 < seq.m ? max(0, tiles(seq.n) - first) : 0;
-        n = per_head * shared;
+        n = per_head * shared, from = 0;
+        if constexpr (SPLIT) take_share(p, from, n);
     }
 };
 
@@ -631,17 +651,48 @@ struct BwdSmem {
     BwdCommon common;
 };
 
+// With SPLIT two CTAs, a cluster, share an item; each adds their sums (dV and dK of 128 keys, or dQ of 128 queries) of
+// half of the rows, always in the same order, and writes them.
+constexpr int BWD_PARTS = 2;
 template <int DH>
+__device__ __forceinline__ void join_sums(const AttnParams &p, int block, int key_items, uint32_t at) {
+    static_assert(2 * TILE * DH * 4 <= offsetof(BwdSmem<DH>, common));
+    constexpr int LANES = DH / 8;
+    const bool keys = block < key_items;
+    const int share = (keys ? 2 * TILE : TILE) / BWD_PARTS, from = blockIdx.x % BWD_PARTS * share, c = threadIdx.x % LANES;
+    const DkvItem<true> of_keys(p, keys ? block : 0);
+    const DqItem<true> of_queries(p, keys ? 0 : block - key_items);
+    for (int r = from + threadIdx.x / LANES; r < from + share; r += 2 * TILE / LANES) {
+        const bool dv = keys && r < TILE;
+        const int row = keys ? of_keys.key0 + r % TILE : of_queries.row0 + r;
+        if (row >= (keys ? p.len_kv : p.len_q) || c * 8 >= p.dim) continue;
+        const float by = dv ? 1.0f : p.scale;
+        const int64_t *stride = !keys ? p.out_stride : dv ? p.dv_stride : p.dk_stride;
+        __nv_bfloat16 *out = (!keys ? p.out : dv ? p.dv : p.dk) + (keys ? of_keys.b : of_queries.b) * stride[0] + row * stride[1] + (keys ? of_keys.h_kv : of_queries.h) * stride[2];
+        uint32_t to[4];
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+            const float4 x = get_sums(at, DH, r, c, v, 0), y = get_sums(at, DH, r, c, v, 1);
+            to[2 * v] = pack_bf16((x.x + y.x) * by, (x.y + y.y) * by), to[2 * v + 1] = pack_bf16((x.z + y.z) * by, (x.w + y.w) * by);
+        }
+        *reinterpret_cast<uint4 *>(out + c * 8) = make_uint4(to[0], to[1], to[2], to[3]);
+    }
+}
+
+template <int DH, bool SPLIT>
 __global__ void __launch_bounds__(THREADS, 1)
 k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                 const __grid_constant__ CUtensorMap map_do, const AttnParams p) {
     extern __shared__ uint8_t raw[];
     using Dq = DqTiles<DH>;
     using Dkv = DkvTiles<DH>;
+    using QueryItem = DqItem<SPLIT>;
+    using KeyItem = DkvItem<SPLIT>;
     constexpr uint32_t TILE_BYTES = Dq::TILE_BYTES;
     auto &sm = *reinterpret_cast<BwdSmem<DH> *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     BwdCommon &cm = sm.common;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, key_items = p.batch * p.heads_kv * p.tiles_kv, all_items = key_items + p.batch * p.heads * p.tiles_q;
+    const int first_block = SPLIT ? blockIdx.x / p.parts : blockIdx.x;       // and the only one, with SPLIT
 
     if (threadIdx.x == 0) {
         queue_init(cm.queue, QUEUE_READERS);
@@ -660,7 +711,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         bar_init(&cm.landed, 1);
         cm.gave_up = 0;
     }
-    if (threadIdx.x < TILE && static_cast<int>(blockIdx.x) < key_items) {
+    if (threadIdx.x < TILE && first_block < key_items) {
         constexpr uint32_t ONE = 0x3F80;                 // bf16
         sm.dkv.ones_lse[threadIdx.x] = make_uint4(ONE | ONE << 16, ONE, 0, 0);
         sm.dkv.ones_delta[threadIdx.x] = make_uint4(0, ONE << 16, ONE | ONE << 16, 0);
@@ -675,11 +726,11 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     volatile uint32_t *gave_up = &cm.gave_up;
     after_previous();                           // k_attn_stats
 
-    int block = blockIdx.x;                     // every role goes through the same items
+    int block = first_block;                    // every role goes through the same items
     uint32_t items = 0, landed_phase = 0;       // answers read
     bool ok = true;
-    auto next = [&] { block = queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
-    auto next_one = [&] { block = queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto next = [&] { block = SPLIT ? -1 : queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto next_one = [&] { block = SPLIT ? -1 : queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
     auto all_done = [&] {                       // of the key tiles, in all roles
         fence_async_smem();
         tmem_fence_before();
@@ -688,6 +739,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         if (*gave_up) ok = false;
     };
     auto ask = [&] {                            // once to an item, by the warp that brings the tiles
+        if constexpr (SPLIT) return true;
         if (!bar_wait(&cm.queue.free[items % QUEUE], (items / QUEUE + 1) & 1, gave_up)) return false;
         if (lane == 0) queue_count(cm.queue, items, p.next_item, all_items);
         __syncwarp();
@@ -713,7 +765,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 return true;
             };
             while (ok && block < key_items) {
-                const DkvItem it(p, block);
+                const KeyItem it(p, block);
                 const uint32_t set = sets % Dkv::SETS;
                 if (it.n > 0 && (sums || Dkv::TURNS)) {
                     ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up);
@@ -775,7 +827,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             uint64_t *const full = is_dp ? bars.v_full : bars.k_full, *const taken = is_dp ? &bars.dp_taken : &bars.s_taken, *const done = is_dp ? bars.dp_full : bars.s_full;
             uint32_t sets = 0, tiles_in = 0;
             while (ok) {
-                const DqItem it(p, block - key_items);
+                const QueryItem it(p, block - key_items);
                 const uint32_t set = sets % Dq::SETS;
                 if (it.n > 0) ok = bar_wait_one(&bars.q_full[set], sets / Dq::SETS & 1, gave_up), ++sets;
                 for (int j = 0; ok && j < it.n; ++j) {
@@ -799,8 +851,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             DkvBars &bars = cm.dkv;
             uint32_t sets = 0, tiles_in = 0;        // counts over all items
             while (ok && block < key_items) {
-                if (!(ok = ask())) break;
-                const DkvItem it(p, block);
+                ok = ask();
+                if (!ok) break;
+                const KeyItem it(p, block);
                 const Seq seq(p, it.b);
                 if (it.n > 0) {
                     const uint32_t set = sets % Dkv::SETS;
@@ -816,7 +869,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     __syncwarp();
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
-                        const int h = it.h_kv * it.shared + i / it.per_head, tile = it.first + i % it.per_head;
+                        const int h = it.h_kv * it.shared + (it.from + i) / it.per_head, tile = it.first + (it.from + i) % it.per_head;
                         if (!(ok = bar_wait(&bars.q_free[qs], (g / Dkv::Q_SLOTS + 1) & 1, gave_up))) break;
                         // the terms arrive at the queries' barrier: their bytes are announced without an arrival
                         if (lane == 0) {
@@ -839,8 +892,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             DqBars &bars = cm.dq;
             uint32_t sets = 0, tiles_in = 0;
             while (ok) {
-                if (!(ok = ask())) break;
-                const DqItem it(p, block - key_items);
+                ok = ask();
+                if (!ok) break;
+                const QueryItem it(p, block - key_items);
                 const Seq seq(p, it.b);
                 if (it.n > 0) {
                     const uint32_t set = sets % Dq::SETS;
@@ -857,9 +911,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS, vs = g % Dq::V_SLOTS;
                         ok = bar_wait(&bars.k_free[ks], (g / Dq::K_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
                              bar_wait(&bars.v_free[vs], (g / Dq::V_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                     }
                     tiles_in += it.n;
                 }
@@ -874,7 +928,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const uint32_t zeros = smem_addr(sm.dkv.zeros), k_at = smem_addr(sm.dkv.k), q_at = smem_addr(sm.dkv.q), terms_at = smem_addr(sm.dkv.terms), ones = smem_addr(sm.dkv.ones_lse);
                 uint32_t sets = 0, tiles_in = 0;
                 while (ok && block < key_items) {
-                    const DkvItem it(p, block);
+                    const KeyItem it(p, block);
                     const uint32_t set = sets % Dkv::SETS;
                     if (it.n > 0) ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up), ++sets;
                     for (int i = 0; ok && i < it.n; ++i) {
@@ -912,7 +966,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const uint32_t k_at = smem_addr(sm.dq.k);
                 uint32_t sets = 0, tiles_in = 0;
                 while (ok) {
-                    const DqItem it(p, block - key_items);
+                    const QueryItem it(p, block - key_items);
                     if (it.n > 0 && sets > 0) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS;
@@ -947,10 +1001,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             const uint32_t p_at = Dkv::TURNS ? lanes + Dkv::MINE + w * 64 : dp_at, ds_at = Dkv::TURNS ? p_at : dp_at + 32;
             uint32_t tiles_in = 0, outputs = 0;
             while (ok && block < key_items) {
-                const DkvItem it(p, block);
+                const KeyItem it(p, block);
                 const Seq seq(p, it.b);
                 const int key = it.key0 + threadIdx.x % TILE;
-                int i = Dkv::TURNS ? static_cast<int>((tiles_in + w) & 1) : 0, column = i;                       // query tile of its head
+                int i = Dkv::TURNS ? static_cast<int>((tiles_in + w) & 1) : 0, column = it.from + i;             // query tile of its head
                 for (; i < it.n; i += EVERY, column += EVERY) {
                     const uint32_t g = tiles_in + i;
                     while (column >= it.per_head) column -= it.per_head;
@@ -1026,6 +1080,19 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 }
                 if (!ok) break;
                 tiles_in += it.n;
+                if constexpr (SPLIT) {               // all products that read the tiles are done with the sums
+                    if (it.n > 0) ok = bar_wait(&bars.sums_full, 0, gave_up);
+                    tmem_fence_after();
+#pragma unroll
+                    for (int c = 0; c < DH; c += 32) {
+                        uint32_t o[32];
+                        tmem_load32(lanes + (w == 0 ? Dkv::DV : Dkv::DK) + c, o);
+                        tmem_wait_loads(o);
+                        put_sums(&sm, DH, threadIdx.x, c, o, it.n == 0 || key >= seq.m);
+                    }
+                    next();
+                    break;
+                }
                 // one group writes dV, the other dK
                 const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
                 __nv_bfloat16 *out = (w == 0 ? p.dv : p.dk) + it.b * stride[0] + key * stride[1] + it.h_kv * stride[2];
@@ -1063,7 +1130,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, dp_at = lanes + TILE, ds_at = lanes + 2 * TILE + w * 64;
             uint32_t tiles_in = 0, outputs = 0;
             while (ok) {
-                const DqItem it(p, block - key_items);
+                const QueryItem it(p, block - key_items);
                 const Seq seq(p, it.b);
                 const int row = it.row0 + in_tile, limit = seq.keys_of(row), all_see = seq.keys_of(it.row0);
                 const bool whole = it.row0 + TILE <= seq.n;
@@ -1079,8 +1146,8 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     tmem_wait_loads(s);
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
-                    if (!whole || (j + 1) * TILE > all_see) {
-                        const int left = limit - j * TILE;           // columns that the row sees
+                    if (!whole || (it.from + j + 1) * TILE > all_see) {
+                        const int left = limit - (it.from + j) * TILE;           // columns that the row sees
 #pragma unroll
                         for (int c = 0; c < TILE; ++c)
                             if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
@@ -1118,6 +1185,18 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 }
                 if (!ok) break;
                 tiles_in += it.n;
+                if constexpr (SPLIT) {
+                    if (it.n > 0) ok = bar_wait(&bars.sums_full, 0, gave_up);
+                    tmem_fence_after();
+#pragma unroll
+                    for (int c = w * (DH / 2); c < (w + 1) * (DH / 2); c += 32) {
+                        uint32_t o[32];
+                        tmem_load32(lanes + 3 * TILE + c, o);
+                        tmem_wait_loads(o);
+                        put_sums(&sm, DH, in_tile, c, o, it.n == 0 || limit == 0);
+                    }
+                    break;
+                }
                 __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
                 if (it.n > 0) {
                     if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
@@ -1144,6 +1223,11 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
     }
     tmem_fence_before();
+    if constexpr (SPLIT) {
+        cluster_sync();
+        if (warp < 8) join_sums<DH>(p, first_block, key_items, smem_addr(&sm));
+        cluster_sync();                         // the others have read what is here
+    }
     __syncthreads();
     settle(gave_up);
     if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
@@ -1269,12 +1353,39 @@ int start_forward(const CUtensorMap (&m)[3], AttnParams &p, cudaStream_t st) {
     return KT_OK;
 }
 
+// Whether two CTAs share each item of the backward pass.  Key tiles whose queries come from many heads are few and
+// long: where they leave 40% of the SMs or more to the query tiles, which take half as long, the longest decides.  A CTA
+// of a split item costs some 4 steps besides (its start, which nothing overlaps, and the join).  Measured in us, whole
+// and split:
+//   4 x 700 causal, 8 heads of 128 on 1        91    51      (24 key tiles, 48 steps the longest)
+//   4832, 8 heads of 64 on 2                  273   208      (76, 152 steps)
+//   2 x 1536 causal, 3 heads of 64             24    27      (72, 12 steps)
+//   8192, 2 heads of 128                      187   203      (128, 64 steps)
+bool split_backward(const AttnParams &p) {
+    const int64_t all = static_cast<int64_t>(p.batch) * p.heads_kv, key_tiles = all * p.tiles_kv, shared = p.heads / p.heads_kv;
+    if (key_tiles * 10 > SMS * 6) return false;
+    const int64_t gap = p.len_kv - p.len_q, query_tiles = all * shared * p.tiles_q;
+    int64_t longest = 0, sum = 0;
+    for (int64_t i = 0; i < p.tiles_kv; ++i) {
+        const int64_t unseen = p.causal && i * TILE > gap ? (i * TILE - gap) / TILE : 0, n = unseen < p.tiles_q ? (p.tiles_q - unseen) * shared : 0;
+        sum += n, longest = n > longest ? n : longest;
+    }
+    const double busy = (1.5 * (sum * all) + 4.0 * BWD_PARTS * (key_tiles + query_tiles)) / SMS, one = static_cast<double>(longest) / BWD_PARTS + 4.0;
+    return (busy > one ? busy : one) < 0.92 * longest;
+}
+
 template <int DH>
-int start_backward(const CUtensorMap (&m)[4], const AttnParams &p, cudaStream_t st) {
+int start_backward(const CUtensorMap (&m)[4], AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
-    if (int rc = room<BwdSmem<DH>, k_attn_backward<DH>>(&bytes)) return rc;
     const int items = p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q);
-    KT_CUDA(launch_behind(k_attn_backward<DH>, dim3(items < SMS ? items : SMS), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
+    p.parts = split_backward(p) ? BWD_PARTS : 1;
+    if (p.parts > 1) {
+        if (int rc = room<BwdSmem<DH>, k_attn_backward<DH, true>>(&bytes)) return rc;
+        KT_CUDA(launch_behind(k_attn_backward<DH, true>, p.parts, dim3(items * p.parts), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
+        return KT_OK;
+    }
+    if (int rc = room<BwdSmem<DH>, k_attn_backward<DH, false>>(&bytes)) return rc;
+    KT_CUDA(launch_behind(k_attn_backward<DH, false>, 1, dim3(items < SMS ? items : SMS), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
     return KT_OK;
 }
 

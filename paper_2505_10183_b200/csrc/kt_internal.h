@@ -34,17 +34,12 @@ int check_shares(const int32_t *shares, int K);
 
 }  // namespace ktd
 
-// A launch that may begin while the one before it in the stream ends: its blocks come up as places become
-// free, and call after_previous() before they touch what the one before writes.
 #ifdef __CUDACC__
 template <typename... Params, typename... Args>
-cudaError_t launch_behind(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args) {
-    cudaLaunchAttribute behind{};
-    behind.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    behind.val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_with(cudaLaunchAttribute *attrs, int n, void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args) {
     cudaLaunchConfig_t config{};
     config.gridDim = grid, config.blockDim = block, config.dynamicSmemBytes = smem, config.stream = stream;
-    config.attrs = &behind, config.numAttrs = 1;
+    config.attrs = attrs, config.numAttrs = n;
     return cudaLaunchKernelEx(&config, kernel, args...);
 }
 // A launch whose blocks come in clusters of `joint`, next to each other in x.
@@ -53,10 +48,18 @@ cudaError_t launch_joint(void (*kernel)(Params...), unsigned joint, dim3 grid, d
     cudaLaunchAttribute cluster{};
     cluster.id = cudaLaunchAttributeClusterDimension;
     cluster.val.clusterDim.x = joint, cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    cudaLaunchConfig_t config{};
-    config.gridDim = grid, config.blockDim = block, config.dynamicSmemBytes = smem, config.stream = stream;
-    config.attrs = &cluster, config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, kernel, args...);
+    return launch_with(&cluster, 1, kernel, grid, block, smem, stream, args...);
+}
+// A launch that may begin while the one before it in the stream ends: its blocks come up as places become
+// free, and call after_previous() before they touch what the one before writes.  In clusters where joint > 1.
+template <typename... Params, typename... Args>
+cudaError_t launch_behind(void (*kernel)(Params...), unsigned joint, dim3 grid, dim3 block, size_t smem, cudaStream_t stream, const Args &...args) {
+    cudaLaunchAttribute attrs[2] = {};
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = joint, attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    return launch_with(attrs, joint > 1 ? 2 : 1, kernel, grid, block, smem, stream, args...);
 }
 // A barrier of the cluster's threads, and values in another CTA's shared memory, at this one's address.
 __device__ __forceinline__ void cluster_sync() {

@@ -1261,7 +1261,7 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
         if (int rc = start_norm(true, dtype, w, s, p, p.n_parts, st)) return rc;
     }
     if (sums && !p.joint) {
-        KT_CUDA(launch_behind(k_norm_params, dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st, p));
+        KT_CUDA(launch_behind(k_norm_params, 1, dim3(static_cast<unsigned>((cols + 31) / 32), 2), dim3(32, 32), 0, st, p));
     }
     return KT_OK;
 }

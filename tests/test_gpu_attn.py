@@ -167,6 +167,14 @@ def test_few_long_rows(kt, Lq, Lk, H, Hk, dim, causal):
     run_case(kt, 2, Lq, Lk, H, Hk, dim, causal, seed=Lq + Lk)
 
 
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("dim", [64, 112])
+@pytest.mark.parametrize("Lq,Lk,H,Hk,used_q,used_kv", [(700, 700, 8, 1, None, None), (1500, 300, 2, 2, None, None), (400, 140, 12, 2, [400, 0], None), (1300, 1300, 3, 1, [7, 1200], [1300, 129])])
+def test_few_long_columns(kt, Lq, Lk, H, Hk, used_q, used_kv, dim, causal):
+    """Few key tiles that many query tiles see: two CTAs share the queries of one in the backward pass."""
+    run_case(kt, 2, Lq, Lk, H, Hk, dim, causal, used_q, used_kv, seed=Lq + H)
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("used_q,used_kv", [([3, 1, 0, 3], [2000, 1, 700, 0]), (None, [129, 0, 2000, 128]), ([3, 2, 1, 3], None)])
 def test_few_long_rows_of_different_lengths(kt, used_q, used_kv, dim):
