@@ -594,16 +594,14 @@ struct DqTiles {
     alignas(1024) uint8_t q[SETS][TILE_BYTES], dout[SETS][TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
 };
 
-template <bool SPLIT>
 struct DqItem {
-    int tile, row0, b, h, h_kv, bh, from, n;    // key tiles: n from `from` on
+    int tile, row0, b, h, h_kv, bh, n;          // n: key tiles
     __device__ DqItem(const AttnParams &p, int block) {
         const int all = p.batch * p.heads;
         bh = block % all, tile = p.tiles_q - 1 - block / all, row0 = tile * TILE;
         b = bh / p.heads, h = bh % p.heads, h_kv = h / (p.heads / p.heads_kv);
         const Seq seq(p, b);
-        n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0, from = 0;
-        if constexpr (SPLIT) take_share(p, from, n);
+        n = row0 < seq.n ? tiles(seq.keys_of(min(row0 + TILE, seq.n) - 1)) : 0;
     }
 };
 
@@ -651,31 +649,31 @@ struct BwdSmem {
     BwdCommon common;
 };
 
-// With SPLIT two CTAs, a cluster, share an item; each adds their sums (dV and dK of 128 keys, or dQ of 128 queries) of
-// half of the rows, always in the same order, and writes them.
-constexpr int BWD_PARTS = 2;
-template <int DH>
-__device__ __forceinline__ void join_sums(const AttnParams &p, int block, int key_items, uint32_t at) {
+// With SPLIT, where key tiles are few, the CTAs of a cluster share the queries of one and add their sums, each those of its
+// share of the rows (dV and dK of 128 keys), always in the same order; then they go on with the query tiles.
+template <int DH, int PARTS>
+__device__ __forceinline__ void join_sums(const AttnParams &p, int block, uint32_t at) {
     static_assert(2 * TILE * DH * 4 <= offsetof(BwdSmem<DH>, common));
-    constexpr int LANES = DH / 8;
-    const bool keys = block < key_items;
-    const int share = (keys ? 2 * TILE : TILE) / BWD_PARTS, from = blockIdx.x % BWD_PARTS * share, c = threadIdx.x % LANES;
-    const DkvItem<true> of_keys(p, keys ? block : 0);
-    const DqItem<true> of_queries(p, keys ? 0 : block - key_items);
-    for (int r = from + threadIdx.x / LANES; r < from + share; r += 2 * TILE / LANES) {
-        const bool dv = keys && r < TILE;
-        const int row = keys ? of_keys.key0 + r % TILE : of_queries.row0 + r;
-        if (row >= (keys ? p.len_kv : p.len_q) || c * 8 >= p.dim) continue;
-        const float by = dv ? 1.0f : p.scale;
-        const int64_t *stride = !keys ? p.out_stride : dv ? p.dv_stride : p.dk_stride;
-        __nv_bfloat16 *out = (!keys ? p.out : dv ? p.dv : p.dk) + (keys ? of_keys.b : of_queries.b) * stride[0] + row * stride[1] + (keys ? of_keys.h_kv : of_queries.h) * stride[2];
-        uint32_t to[4];
+    constexpr int LANES = DH / 8, SHARE = 2 * TILE / PARTS;
+    const int from = blockIdx.x % PARTS * SHARE, c = threadIdx.x % LANES;
+    const DkvItem<true> it(p, block);
+    for (int r = from + threadIdx.x / LANES; r < from + SHARE; r += 2 * TILE / LANES) {
+        const bool dv = r < TILE;
+        const int key = it.key0 + r % TILE;
+        if (key >= p.len_kv || c * 8 >= p.dim) continue;
+        float4 x[PARTS][2];                     // all on their way before the first is used
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-            const float4 x = get_sums(at, DH, r, c, v, 0), y = get_sums(at, DH, r, c, v, 1);
-            to[2 * v] = pack_bf16((x.x + y.x) * by, (x.y + y.y) * by), to[2 * v + 1] = pack_bf16((x.z + y.z) * by, (x.w + y.w) * by);
+        for (int i = 0; i < PARTS; ++i) x[i][0] = get_sums(at, DH, r, c, 0, i), x[i][1] = get_sums(at, DH, r, c, 1, i);
+        float4 lo = x[0][0], hi = x[0][1];
+#pragma unroll
+        for (int i = 1; i < PARTS; ++i) {
+            lo.x += x[i][0].x, lo.y += x[i][0].y, lo.z += x[i][0].z, lo.w += x[i][0].w;
+            hi.x += x[i][1].x, hi.y += x[i][1].y, hi.z += x[i][1].z, hi.w += x[i][1].w;
         }
-        *reinterpret_cast<uint4 *>(out + c * 8) = make_uint4(to[0], to[1], to[2], to[3]);
+        const float by = dv ? 1.0f : p.scale;
+        const int64_t *stride = dv ? p.dv_stride : p.dk_stride;
+        *reinterpret_cast<uint4 *>((dv ? p.dv : p.dk) + it.b * stride[0] + key * stride[1] + it.h_kv * stride[2] + c * 8) =
+            make_uint4(pack_bf16(lo.x * by, lo.y * by), pack_bf16(lo.z * by, lo.w * by), pack_bf16(hi.x * by, hi.y * by), pack_bf16(hi.z * by, hi.w * by));
     }
 }
 
@@ -686,13 +684,12 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     extern __shared__ uint8_t raw[];
     using Dq = DqTiles<DH>;
     using Dkv = DkvTiles<DH>;
-    using QueryItem = DqItem<SPLIT>;
     using KeyItem = DkvItem<SPLIT>;
     constexpr uint32_t TILE_BYTES = Dq::TILE_BYTES;
     auto &sm = *reinterpret_cast<BwdSmem<DH> *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     BwdCommon &cm = sm.common;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, key_items = p.batch * p.heads_kv * p.tiles_kv, all_items = key_items + p.batch * p.heads * p.tiles_q;
-    const int first_block = SPLIT ? blockIdx.x / p.parts : blockIdx.x;       // and the only one, with SPLIT
+    const int first_block = SPLIT ? blockIdx.x / p.parts : blockIdx.x;       // with SPLIT a key tile, or none
 
     if (threadIdx.x == 0) {
         queue_init(cm.queue, QUEUE_READERS);
@@ -729,19 +726,29 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     int block = first_block;                    // every role goes through the same items
     uint32_t items = 0, landed_phase = 0;       // answers read
     bool ok = true;
-    auto next = [&] { block = SPLIT ? -1 : queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
-    auto next_one = [&] { block = SPLIT ? -1 : queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
-    auto all_done = [&] {                       // of the key tiles, in all roles
+    const bool no_key_tile = SPLIT && first_block >= key_items;
+    auto next = [&] { block = queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto next_one = [&] { block = queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto all_done = [&](const bool joins) {     // of the key tiles, in all roles
         fence_async_smem();
         tmem_fence_before();
         asm volatile("barrier.sync 1, %0;" ::"n"(THREADS) : "memory");
+        if constexpr (SPLIT) {
+            cluster_sync();
+            if (joins && first_block < key_items) {
+                if (p.parts == 2) join_sums<DH, 2>(p, first_block, smem_addr(&sm));
+                else if (p.parts == 4) join_sums<DH, 4>(p, first_block, smem_addr(&sm));
+                else join_sums<DH, 8>(p, first_block, smem_addr(&sm));
+            }
+            fence_async_smem();
+            cluster_sync();                     // the others have read what is here
+        }
         tmem_fence_after();
         if (*gave_up) ok = false;
     };
     auto ask = [&] {                            // once to an item, by the warp that brings the tiles
-        if constexpr (SPLIT) return true;
         if (!bar_wait(&cm.queue.free[items % QUEUE], (items / QUEUE + 1) & 1, gave_up)) return false;
-        if (lane == 0) queue_count(cm.queue, items, p.next_item, all_items);
+        if (lane == 0) queue_count(cm.queue, items, p.next_item, SPLIT ? key_items : gridDim.x, all_items);
         __syncwarp();
         return true;
     };
@@ -753,6 +760,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             const uint32_t zeros = smem_addr(sm.dkv.zeros), v_at = smem_addr(sm.dkv.v), q_at = smem_addr(sm.dkv.q), do_at = smem_addr(sm.dkv.dout), terms_at = smem_addr(sm.dkv.terms),
                            ones = smem_addr(sm.dkv.ones_delta);
             uint32_t sets = 0, tiles_in = 0;
+            if (no_key_tile) next_one();
             auto dprobs = [&](uint32_t g, uint32_t set) {
                 const uint32_t qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
                 if (!bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up)) return false;        // delta comes with the queries
@@ -827,7 +835,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             uint64_t *const full = is_dp ? bars.v_full : bars.k_full, *const taken = is_dp ? &bars.dp_taken : &bars.s_taken, *const done = is_dp ? bars.dp_full : bars.s_full;
             uint32_t sets = 0, tiles_in = 0;
             while (ok) {
-                const QueryItem it(p, block - key_items);
+                const DqItem it(p, block - key_items);
                 const uint32_t set = sets % Dq::SETS;
                 if (it.n > 0) ok = bar_wait_one(&bars.q_full[set], sets / Dq::SETS & 1, gave_up), ++sets;
                 for (int j = 0; ok && j < it.n; ++j) {
@@ -850,6 +858,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         {
             DkvBars &bars = cm.dkv;
             uint32_t sets = 0, tiles_in = 0;        // counts over all items
+            if (no_key_tile) {
+                ok = ask();
+                if (ok) next();
+            }
             while (ok && block < key_items) {
                 ok = ask();
                 if (!ok) break;
@@ -887,14 +899,14 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             }
         }
         // Query tiles next, whose data comes where that of the key tiles was: dQ.
-        all_done();
+        all_done(false);
         {
             DqBars &bars = cm.dq;
             uint32_t sets = 0, tiles_in = 0;
             while (ok) {
                 ok = ask();
                 if (!ok) break;
-                const QueryItem it(p, block - key_items);
+                const DqItem it(p, block - key_items);
                 const Seq seq(p, it.b);
                 if (it.n > 0) {
                     const uint32_t set = sets % Dq::SETS;
@@ -911,9 +923,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS, vs = g % Dq::V_SLOTS;
                         ok = bar_wait(&bars.k_free[ks], (g / Dq::K_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
                              bar_wait(&bars.v_free[vs], (g / Dq::V_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
                     }
                     tiles_in += it.n;
                 }
@@ -927,6 +939,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 DkvBars &bars = cm.dkv;
                 const uint32_t zeros = smem_addr(sm.dkv.zeros), k_at = smem_addr(sm.dkv.k), q_at = smem_addr(sm.dkv.q), terms_at = smem_addr(sm.dkv.terms), ones = smem_addr(sm.dkv.ones_lse);
                 uint32_t sets = 0, tiles_in = 0;
+                if (no_key_tile) next_one();
                 while (ok && block < key_items) {
                     const KeyItem it(p, block);
                     const uint32_t set = sets % Dkv::SETS;
@@ -947,26 +960,26 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             __syncwarp();
         }
         // Query tiles next, whose data comes where that of the key tiles was: dQ.
-        all_done();
+        all_done(false);
         dq_products(false);
     } else if (warp == WARP_DP) {
         registers_give<REGISTERS_HELP>();
         dkv_products(false);
         // Query tiles next, whose data comes where that of the key tiles was: dQ.
-        all_done();
+        all_done(false);
         dq_products(true);
     } else if (warp == WARP_SUMS) {
         registers_give<REGISTERS_HELP>();
         dkv_products(true);
         // Query tiles next, whose data comes where that of the key tiles was: dQ.
-        all_done();
+        all_done(false);
         {
             if (elected()) {
                 DqBars &bars = cm.dq;
                 const uint32_t k_at = smem_addr(sm.dq.k);
                 uint32_t sets = 0, tiles_in = 0;
                 while (ok) {
-                    const QueryItem it(p, block - key_items);
+                    const DqItem it(p, block - key_items);
                     if (it.n > 0 && sets > 0) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS;
@@ -1000,6 +1013,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             uint64_t *const s_full = &bars.s_full[Dkv::TURNS ? w : 0], *const dp_full = &bars.dp_full[Dkv::TURNS ? w : 0];
             const uint32_t p_at = Dkv::TURNS ? lanes + Dkv::MINE + w * 64 : dp_at, ds_at = Dkv::TURNS ? p_at : dp_at + 32;
             uint32_t tiles_in = 0, outputs = 0;
+            if (no_key_tile) next();
             while (ok && block < key_items) {
                 const KeyItem it(p, block);
                 const Seq seq(p, it.b);
@@ -1090,8 +1104,8 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         tmem_wait_loads(o);
                         put_sums(&sm, DH, threadIdx.x, c, o, it.n == 0 || key >= seq.m);
                     }
-                    next();
-                    break;
+                    if (ok) next();
+                    continue;
                 }
                 // one group writes dV, the other dK
                 const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
@@ -1123,14 +1137,14 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             }
         }
         // Query tiles next, whose data comes where that of the key tiles was: dQ.
-        all_done();
+        all_done(true);
         {
             DqBars &bars = cm.dq;
             const int w = warp / 4, in_tile = threadIdx.x % TILE;
             const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, dp_at = lanes + TILE, ds_at = lanes + 2 * TILE + w * 64;
             uint32_t tiles_in = 0, outputs = 0;
             while (ok) {
-                const QueryItem it(p, block - key_items);
+                const DqItem it(p, block - key_items);
                 const Seq seq(p, it.b);
                 const int row = it.row0 + in_tile, limit = seq.keys_of(row), all_see = seq.keys_of(it.row0);
                 const bool whole = it.row0 + TILE <= seq.n;
@@ -1146,8 +1160,8 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     tmem_wait_loads(s);
                     tmem_fence_before();
                     bar_arrive_warp(&bars.s_taken);
-                    if (!whole || (it.from + j + 1) * TILE > all_see) {
-                        const int left = limit - (it.from + j) * TILE;           // columns that the row sees
+                    if (!whole || (j + 1) * TILE > all_see) {
+                        const int left = limit - j * TILE;           // columns that the row sees
 #pragma unroll
                         for (int c = 0; c < TILE; ++c)
                             if (c >= left) s[c / 32][c % 32] = __float_as_uint(-INFINITY);
@@ -1185,18 +1199,6 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 }
                 if (!ok) break;
                 tiles_in += it.n;
-                if constexpr (SPLIT) {
-                    if (it.n > 0) ok = bar_wait(&bars.sums_full, 0, gave_up);
-                    tmem_fence_after();
-#pragma unroll
-                    for (int c = w * (DH / 2); c < (w + 1) * (DH / 2); c += 32) {
-                        uint32_t o[32];
-                        tmem_load32(lanes + 3 * TILE + c, o);
-                        tmem_wait_loads(o);
-                        put_sums(&sm, DH, in_tile, c, o, it.n == 0 || limit == 0);
-                    }
-                    break;
-                }
                 __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
                 if (it.n > 0) {
                     if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
@@ -1223,11 +1225,6 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         }
     }
     tmem_fence_before();
-    if constexpr (SPLIT) {
-        cluster_sync();
-        if (warp < 8) join_sums<DH>(p, first_block, key_items, smem_addr(&sm));
-        cluster_sync();                         // the others have read what is here
-    }
     __syncthreads();
     settle(gave_up);
     if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
@@ -1353,35 +1350,42 @@ int start_forward(const CUtensorMap (&m)[3], AttnParams &p, cudaStream_t st) {
     return KT_OK;
 }
 
-// Whether two CTAs share each item of the backward pass.  Key tiles whose queries come from many heads are few and
-// long: where they leave 40% of the SMs or more to the query tiles, which take half as long, the longest decides.  A CTA
-// of a split item costs some 4 steps besides (its start, which nothing overlaps, and the join).  Measured in us, whole
-// and split:
-//   4 x 700 causal, 8 heads of 128 on 1        91    51      (24 key tiles, 48 steps the longest)
-//   4832, 8 heads of 64 on 2                  273   208      (76, 152 steps)
-//   2 x 1536 causal, 3 heads of 64             24    27      (72, 12 steps)
-//   8192, 2 heads of 128                      187   203      (128, 64 steps)
-bool split_backward(const AttnParams &p) {
-    const int64_t all = static_cast<int64_t>(p.batch) * p.heads_kv, key_tiles = all * p.tiles_kv, shared = p.heads / p.heads_kv;
-    if (key_tiles * 10 > SMS * 6) return false;
-    const int64_t gap = p.len_kv - p.len_q, query_tiles = all * shared * p.tiles_q;
+// CTAs that share a key tile in the backward pass (1, 2, 4 or 8).  Key tiles that many queries see, of many heads, are
+// long, and where they are few the longest decides.  Estimated in steps of one query tile, from the sizes alone: the
+// longest key tile, or all work over all SMs; a share costs some 5 + parts steps besides, for the join and the
+// wait for it.  Measured in us with 1, 2, 4 and 8:
+//   2048 causal, 8 heads of 128 on 1           185   125    85    67      (16 key tiles, 128 steps the longest)
+//   4 x 700 causal, 8 heads of 128 on 1         91    60    47            (24, 48 steps)
+//   4096 queries on 77 keys, 8 heads of 64      48    34    28    26      (8, 32 steps)
+//   2 x 578 causal, 4 heads of 64 on 2          20    24    26            (20, 10 steps)
+int parts_of_keys(const AttnParams &p) {
+    const int64_t all = static_cast<int64_t>(p.batch) * p.heads_kv, key_tiles = all * p.tiles_kv, gap = p.len_kv - p.len_q;
+    if (key_tiles * 2 > SMS) return 1;
     int64_t longest = 0, sum = 0;
     for (int64_t i = 0; i < p.tiles_kv; ++i) {
-        const int64_t unseen = p.causal && i * TILE > gap ? (i * TILE - gap) / TILE : 0, n = unseen < p.tiles_q ? (p.tiles_q - unseen) * shared : 0;
+        const int64_t unseen = p.causal && i * TILE > gap ? (i * TILE - gap) / TILE : 0, n = unseen < p.tiles_q ? (p.tiles_q - unseen) * (p.heads / p.heads_kv) : 0;
         sum += n, longest = n > longest ? n : longest;
     }
-    const double busy = (1.5 * (sum * all) + 4.0 * BWD_PARTS * (key_tiles + query_tiles)) / SMS, one = static_cast<double>(longest) / BWD_PARTS + 4.0;
-    return (busy > one ? busy : one) < 0.92 * longest;
+    const double busy = 1.5 * (sum * all) / SMS;          // a step of a query tile is half of one of a key tile
+    int best = 1;
+    double least = 0.0;
+    for (int parts = 1; parts <= 8 && key_tiles * parts <= (parts < 8 ? SMS : 128); parts *= 2) {      // 16 clusters of 8 have a place at once
+        const double each = static_cast<double>(longest) / parts, cost = (each > busy ? each : busy) + (parts > 1 ? 5 + parts : 0);
+        if (parts == 1 || cost < least) best = parts, least = cost;
+    }
+    return best;
 }
 
 template <int DH>
 int start_backward(const CUtensorMap (&m)[4], AttnParams &p, cudaStream_t st) {
     size_t bytes = 0;
     const int items = p.batch * (p.heads_kv * p.tiles_kv + p.heads * p.tiles_q);
-    p.parts = split_backward(p) ? BWD_PARTS : 1;
+    p.parts = parts_of_keys(p);
     if (p.parts > 1) {
         if (int rc = room<BwdSmem<DH>, k_attn_backward<DH, true>>(&bytes)) return rc;
-        KT_CUDA(launch_behind(k_attn_backward<DH, true>, p.parts, dim3(items * p.parts), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
+        const int key_ctas = p.batch * p.heads_kv * p.tiles_kv * p.parts, useful = key_ctas + p.batch * p.heads * p.tiles_q;
+        const int grid = (useful < SMS ? useful : SMS) / p.parts * p.parts;       // key_ctas at least: parts_of_keys
+        KT_CUDA(launch_behind(k_attn_backward<DH, true>, p.parts, dim3(grid), dim3(THREADS), bytes, st, m[0], m[1], m[2], m[3], p));
         return KT_OK;
     }
     if (int rc = room<BwdSmem<DH>, k_attn_backward<DH, false>>(&bytes)) return rc;

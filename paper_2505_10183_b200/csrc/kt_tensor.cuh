@@ -140,8 +140,8 @@ __device__ __forceinline__ int queue_read(const Queue &q, uint32_t k) {
     return given ? static_cast<int>(x) : -1;
 }
 // Answers from a counter in device memory, where items have to come in their order.
-__device__ __forceinline__ void queue_count(Queue &q, uint32_t k, unsigned *counter, int most) {
-    const unsigned block = gridDim.x + atomicAdd(counter, 1u);
+__device__ __forceinline__ void queue_count(Queue &q, uint32_t k, unsigned *counter, unsigned first, int most) {
+    const unsigned block = first + atomicAdd(counter, 1u);
     q.answer[k % QUEUE].x = block < static_cast<unsigned>(most) ? block : 0xFFFFFFFFu;
     bar_arrive(&q.full[k % QUEUE]);
 }
