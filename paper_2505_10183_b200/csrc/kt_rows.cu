@@ -138,7 +138,7 @@ __device__ __forceinline__ uint4 load_row(const T *row, int64_t col, int64_t col
 // Rows of bf16 that are not made of aligned vectors are written in aligned 16-byte pieces all the same: a lane
 // writes the piece in which its vector starts, with the end of its left neighbour's vector in it (the lanes of
 // a warp hold vectors that follow one another, and all of them call); what no lane can write as a
-// whole piece goes element by element.
+// whole piece goes in aligned parts of 8, 4 and 2 bytes, and at the row's end element by element.
 template <typename T, bool WIDE>
 __device__ __forceinline__ void store_row(T *row, int64_t col, int64_t cols, const float (&x)[Elems<T>::V]) {
     constexpr int V = Elems<T>::V;
@@ -181,12 +181,27 @@ __device__ __forceinline__ void store_row(T *row, int64_t col, int64_t cols, con
         }
         // the right neighbour takes the end along if it writes a whole piece
         const bool taken = off == 0 || (threadIdx.x % 32 < 31 && left - 16 >= first);
-        if (!whole || !taken) {
+        if (whole && taken) return;
+        char *const to = reinterpret_cast<char *>(row + col);
+        if (left < 16) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const int at = i * static_cast<int>(sizeof(T));
-                if (at < left && (at < first ? !whole : !taken)) row[col + i] = Elems<T>::one(x[i]);
-            }
+            for (int i = 0; i < V; ++i)
+                if (2 * i < left && (2 * i < first ? !whole : !taken)) row[col + i] = Elems<T>::one(x[i]);
+            return;
+        }
+        const bool odd = off & 2;
+        if (!whole) {                                // `first` bytes, up to a multiple of 16: 2, 4, 8 of them
+            if (odd) *reinterpret_cast<unsigned short *>(to) = static_cast<unsigned short>(r.x);
+            const unsigned w[3] = {odd ? __funnelshift_r(r.x, r.y, 16) : r.x, odd ? __funnelshift_r(r.y, r.z, 16) : r.y, odd ? __funnelshift_r(r.z, r.w, 16) : r.z};
+            char *const at = to + (off & 2);
+            if (first & 4) *reinterpret_cast<unsigned *>(at) = w[0];
+            if (first & 8) *reinterpret_cast<uint2 *>(at + (first & 4)) = first & 4 ? make_uint2(w[1], w[2]) : make_uint2(w[0], w[1]);
+        }
+        if (!taken) {                                // the last `off` bytes, from a multiple of 16 on: 8, 4, 2 of them
+            const unsigned w[3] = {odd ? __funnelshift_r(r.x, r.y, 16) : r.y, odd ? __funnelshift_r(r.y, r.z, 16) : r.z, odd ? __funnelshift_r(r.z, r.w, 16) : r.w};
+            if (off & 8) *reinterpret_cast<uint2 *>(to + first) = off & 4 ? make_uint2(w[0], w[1]) : make_uint2(w[1], w[2]);
+            if (off & 4) *reinterpret_cast<unsigned *>(to + 12 - (off & 2)) = w[2];
+            if (odd) *reinterpret_cast<unsigned short *>(to + 14) = static_cast<unsigned short>(r.w >> 16);
         }
     }
 }
@@ -328,6 +343,48 @@ __device__ __forceinline__ void group_barrier(int group) {
 template <int GROUP, int NV, int V>
 __device__ __forceinline__ int column(int at, int k) { return (at + k * GROUP) * V; }
 
+// Rows of bf16 whose vectors do not start at multiples of 16 bytes are copied ahead as well, in the aligned pieces that hold
+// them: a lane copies the piece in which its vector starts, the last one that behind too, and a vector is put together
+// from two pieces.  (The ends of a row's first and last piece belong to others and are not looked at.)  Against loads
+// by words, a row ahead in the forward pass only: 125 instead of 147 us for the backward pass on 8192 x 5669, 52 instead of 59 for
+// the forward pass on 16384 x 1111.  What is left there is the vectors' assembly and the stores (store_row).
+// Rows of fp32 take loads by elements.
+template <typename T, bool WIDE>
+__host__ __device__ constexpr bool in_ring() { return WIDE || sizeof(T) == 2; }
+template <bool WIDE>
+__host__ __device__ constexpr int cells_of_warp() { return WIDE ? 32 : 33; }
+template <bool WIDE, int THREADS>
+__device__ __forceinline__ int cell_of(int set) { return (set * (THREADS / 32) + threadIdx.x / 32) * cells_of_warp<WIDE>() + threadIdx.x % 32; }
+
+template <typename T, bool WIDE>
+__device__ __forceinline__ void copy_vector(uint4 *to, const T *row, int col, int cols) {
+    if constexpr (WIDE) {
+        if (col < cols) copy_ahead<16>(to, row + col);
+    } else {
+        const uintptr_t from = reinterpret_cast<uintptr_t>(row + col) & ~static_cast<uintptr_t>(15), end = reinterpret_cast<uintptr_t>(row + cols);
+        if (from < end) copy_ahead<16>(to, reinterpret_cast<const void *>(from));
+        if (threadIdx.x % 32 == 31 && from + 16 < end) copy_ahead<16>(to + 1, reinterpret_cast<const void *>(from + 16));
+    }
+}
+template <typename T, bool WIDE>
+__device__ __forceinline__ uint4 take_vector(const uint4 *from, const T *row, int col, int cols) {
+    if (col >= cols) return make_uint4(0, 0, 0, 0);
+    if constexpr (WIDE) return *from;
+    const unsigned off = reinterpret_cast<uintptr_t>(row) & 15;        // where the vector starts in its piece
+    const unsigned *const words = reinterpret_cast<const unsigned *>(from) + off / 4;
+    unsigned w[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) w[i] = words[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], (off & 2) * 8);
+    const int left = (cols - col) * static_cast<int>(sizeof(T));
+    if (left < 16)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (left < 4 * i + 4) w[i] = left <= 4 * i ? 0 : w[i] & 0xFFFFu;
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // y = (x - mean) rstd w + b.  A warp takes the mean of its part of the row and the squares around that
 // mean; the parts are joined with the exact formula for two samples, so that one barrier is enough
 // and nothing cancels.  Bound by memory: 16384 x 4096 bf16 in 52 us (5190 GB/s; a plain copy reaches 6530), 73 us with the
@@ -335,19 +392,19 @@ __device__ __forceinline__ int column(int at, int k) { return (at + k * GROUP) *
 template <typename T, bool WIDE, int GROUP, int NV>
 __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>() / norm_threads<GROUP>()) k_norm_forward(const NormParams p) {
     constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
-    extern __shared__ uint4 ring[];              // WIDE: [AHEAD + 1][NV][THREADS]
+    constexpr bool RING = in_ring<T, WIDE>();
+    extern __shared__ uint4 ring[];              // RING: [AHEAD + 1][NV][THREADS / 32][cells_of_warp]
     __shared__ float2 slots[2][WARPS];
     __shared__ float counts[WARPS];
     const int at = threadIdx.x % GROUP;
     const int64_t step = static_cast<int64_t>(gridDim.x) * (THREADS / GROUP), first = static_cast<int64_t>(blockIdx.x) * (THREADS / GROUP) + threadIdx.x / GROUP;
     const int cols = static_cast<int>(p.cols), pitch = static_cast<int>(pitch_of(cols)), blocks = static_cast<int>(blocks_of(cols));
     const float per_col = 1.0f / static_cast<float>(cols);
-    auto slot = [&](int stage, int k) { return ring + (stage * NV + k) * THREADS + threadIdx.x; };
+    auto slot = [&](int stage, int k) { return ring + cell_of<WIDE, THREADS>(stage * NV + k); };
     auto fetch = [&](int64_t r, int stage) {
         if (r < p.rows)
 #pragma unroll
-            for (int k = 0; k < NV; ++k)
-                if (column<GROUP, NV, V>(at, k) < cols) copy_ahead<16>(slot(stage, k), static_cast<const T *>(p.x) + r * p.x_stride + column<GROUP, NV, V>(at, k));
+            for (int k = 0; k < NV; ++k) copy_vector<T, WIDE>(slot(stage, k), static_cast<const T *>(p.x) + r * p.x_stride, column<GROUP, NV, V>(at, k), cols);
         copies_issued();
     };
     auto part_of = [&](int warp) {               // elements of the row that a warp holds
@@ -357,7 +414,7 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
         return static_cast<float>(n);
     };
     uint4 raw[NV];
-    if constexpr (WIDE) {
+    if constexpr (RING) {
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) fetch(first + s * step, s);
     } else {
@@ -376,10 +433,11 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
     for (int64_t r = first; r < p.rows; r += step) {
         float x[NV][V];
         float2 s = both(0.0f);
-        if constexpr (WIDE) {
+        if constexpr (RING) {
             wait_copies<AHEAD - 1>();
+            if constexpr (!WIDE) __syncwarp();       // lanes read their neighbours' pieces
 #pragma unroll
-            for (int k = 0; k < NV; ++k) raw[k] = column<GROUP, NV, V>(at, k) < cols ? *slot(stage, k) : make_uint4(0, 0, 0, 0);
+            for (int k = 0; k < NV; ++k) raw[k] = take_vector<T, WIDE>(slot(stage, k), static_cast<const T *>(p.x) + r * p.x_stride, column<GROUP, NV, V>(at, k), cols);
         }
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
@@ -387,7 +445,7 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
 #pragma unroll
             for (int i = 0; i < V; i += 2) s = add2(s, make_float2(x[k][i], x[k][i + 1]));
         }
-        if constexpr (WIDE) {
+        if constexpr (RING) {
             fetch(r + AHEAD * step, stage == 0 ? AHEAD : stage - 1);
             stage = stage == AHEAD ? 0 : stage + 1;
         } else {
@@ -466,17 +524,18 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
 // are one cluster that joins its sums through distributed shared memory; else one row of partial
 // sums per CTA is reduced in a fixed order by k_norm_params: no atomics either way, so that a step gives the same bits
 // when it is run again.  (With a CTA to a group, four times as many partial sums: 47.6 instead of 38.6 us for
-// 16384 x 2048 bf16 from a checkpoint.)  Bound by memory where rows are many: 16384 x 4096 bf16 in 74 us (5460 GB/s), 16384 x
+// 16384 x 2048 bf16 from a checkpoint.)  Bound by memory where rows are many: 16384 x 4096 bf16 in 69 us (5830 GB/s), 16384 x
 // 2048 from a checkpoint in 38 (4440 GB/s); 4999 x 1000 fp32 in 16, some 4 of them the second kernel's.
 template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
 __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams p) {
     constexpr int V = Elems<T>::V, THREADS = GROUP_MAX, GROUPS = THREADS / GROUP, WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
     constexpr int SOURCE = KEPT ? V : 16;        // bytes of a vector of u: codes, or x itself
-    // WIDE: [AHEAD + 1][NV][THREADS] vectors of dout, then as many of SOURCE bytes, then (KEPT) scales;
+    // RING: [AHEAD + 1][NV][THREADS / 32][cells_of_warp] vectors of dout, then as many of SOURCE bytes, then (KEPT) scales;
     // afterwards the sums of the CTA's groups
     extern __shared__ uint4 ring[];
     __shared__ float2 slots[GROUPS][2][WARPS];
-    constexpr int CELLS = (AHEAD + 1) * NV * THREADS;
+    constexpr bool RING = in_ring<T, WIDE>();
+    constexpr int CELLS = (AHEAD + 1) * NV * (THREADS / 32) * cells_of_warp<WIDE>();
     char *const ring_u = reinterpret_cast<char *>(ring + CELLS);
     float *const ring_s = reinterpret_cast<float *>(ring_u + CELLS * SOURCE);
     const int at = threadIdx.x % GROUP, group = threadIdx.x / GROUP;
@@ -484,28 +543,32 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
     const int cols = static_cast<int>(p.cols), pitch = static_cast<int>(pitch_of(cols)), blocks = static_cast<int>(blocks_of(cols));
     const float per_col = 1.0f / static_cast<float>(cols);
     let_next_begin();
-    auto cell = [&](int stage, int k) { return (stage * NV + k) * THREADS + static_cast<int>(threadIdx.x); };
-    auto dout_at = [&](int64_t r, int k) { return static_cast<const T *>(p.dout) + r * p.dout_stride + column<GROUP, NV, V>(at, k); };
-    auto x_at = [&](int64_t r, int k) { return static_cast<const T *>(p.x) + r * p.x_stride + column<GROUP, NV, V>(at, k); };
+    // Whether any of a warp's k-th vectors lies in the row.  (From a checkpoint, which leaves less to do for a vector, the
+    // branches cost more than they save in full rows: 39.4 against 37.9 us for 16384 x 2048; from x they save even there,
+    // 69 against 74 for 16384 x 4096.)
+    auto some = [&](int k) { return KEPT || k == 0 || column<GROUP, NV, V>(at & ~31, k) < cols; };
+    auto cell = [&](int stage, int k) { return cell_of<WIDE, THREADS>(stage * NV + k); };
+    auto dout_at = [&](int64_t r) { return static_cast<const T *>(p.dout) + r * p.dout_stride; };
+    auto x_at = [&](int64_t r) { return static_cast<const T *>(p.x) + r * p.x_stride; };
     auto codes_at = [&](int64_t r, int k) { return p.codes + r * pitch + column<GROUP, NV, V>(at, k); };
     auto scale_at = [&](int64_t r, int k) { return p.scales + r * blocks + column<GROUP, NV, V>(at, k) / BLOCK; };
     auto fetch = [&](int64_t r, int stage) {
         if (r < p.rows)
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
-                if (column<GROUP, NV, V>(at, k) >= cols) continue;
-                const int c = cell(stage, k);
-                copy_ahead<16>(ring + c, dout_at(r, k));
-                if constexpr (KEPT) {
+                if (!some(k)) continue;
+                const int c = cell(stage, k), col = column<GROUP, NV, V>(at, k);
+                copy_vector<T, WIDE>(ring + c, dout_at(r), col, cols);
+                if constexpr (!KEPT) {
+                    copy_vector<T, WIDE>(reinterpret_cast<uint4 *>(ring_u) + c, x_at(r), col, cols);
+                } else if (col < cols) {
                     copy_ahead<SOURCE>(ring_u + c * SOURCE, codes_at(r, k));
                     copy_ahead<4>(ring_s + c, scale_at(r, k));
-                } else {
-                    copy_ahead<16>(ring_u + c * SOURCE, x_at(r, k));
                 }
             }
         copies_issued();
     };
-    if constexpr (WIDE) {
+    if constexpr (RING) {
 #pragma unroll
         for (int s = 0; s < AHEAD; ++s) fetch(first + s * step, s);
     }
@@ -521,17 +584,18 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
     for (int64_t r = first; r < p.rows; r += step) {
         float g[NV][V], u[NV][V];
         float2 s1 = both(0.0f), s2 = both(0.0f);
-        if constexpr (WIDE) wait_copies<AHEAD - 1>();
+        if constexpr (RING) wait_copies<AHEAD - 1>();
+        if constexpr (RING && !WIDE) __syncwarp();       // lanes read their neighbours' pieces
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const bool in = column<GROUP, NV, V>(at, k) < cols;
-            const int c = cell(stage, k);
-            const uint4 zero = make_uint4(0, 0, 0, 0);
-            Elems<T>::widen(WIDE ? in ? ring[c] : zero : load_row<T, WIDE>(static_cast<const T *>(p.dout) + r * p.dout_stride, column<GROUP, NV, V>(at, k), cols), g[k]);
+            if (!some(k)) continue;
+            const int c = cell(stage, k), col = column<GROUP, NV, V>(at, k);
+            const bool in = col < cols;
+            Elems<T>::widen(RING ? take_vector<T, WIDE>(ring + c, dout_at(r), col, cols) : load_row<T, WIDE>(dout_at(r), col, cols), g[k]);
             if constexpr (KEPT) {
                 uint2 codes = make_uint2(0, 0);
                 float scale = 0.0f;
-                if constexpr (WIDE) {
+                if constexpr (RING) {
                     if (in) {
                         if constexpr (V == 8) codes = *reinterpret_cast<const uint2 *>(ring_u + c * SOURCE);
                         else codes.x = *reinterpret_cast<const unsigned *>(ring_u + c * SOURCE);
@@ -543,11 +607,11 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
                 }
                 decode<V>(codes, scale, u[k]);
             } else {
-                Elems<T>::widen(WIDE ? in ? *reinterpret_cast<const uint4 *>(ring_u + c * SOURCE) : zero : load_row<T, WIDE>(static_cast<const T *>(p.x) + r * p.x_stride, column<GROUP, NV, V>(at, k), cols), u[k]);
+                Elems<T>::widen(RING ? take_vector<T, WIDE>(reinterpret_cast<const uint4 *>(ring_u) + c, x_at(r), col, cols) : load_row<T, WIDE>(x_at(r), col, cols), u[k]);
             }
         }
         const float by = rstd, shift = mean;
-        if constexpr (WIDE) {
+        if constexpr (RING) {
             fetch(r + AHEAD * step, stage == 0 ? AHEAD : stage - 1);
             stage = stage == AHEAD ? 0 : stage + 1;
         }
@@ -556,7 +620,8 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
             if constexpr (!KEPT) mean = p.mean[r + step];
         }
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
+        for (int k = 0; k < NV; ++k) {
+            if (!some(k)) continue;
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
                 const float2 d = make_float2(g[k][i], g[k][i + 1]);           // zeros past the row's end
@@ -569,6 +634,7 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
                 s1 = add2(s1, v);
                 s2 = fma2(v, un, s2);
             }
+        }
         float2 s = make_float2(s1.x + s1.y, s2.x + s2.y);
 #pragma unroll
         for (int d = 16; d > 0; d /= 2) {
@@ -586,6 +652,7 @@ __global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams
         const float a = -s.x * per_col * by, c = -s.y * per_col * by;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
+            if (!some(k)) continue;
             float y[V];
 #pragma unroll
             for (int i = 0; i < V; i += 2) {
@@ -1041,10 +1108,10 @@ int start_norm_kernel(const NormParams &p, int grid, int threads, size_t smem, c
 
 template <typename T, bool WIDE, int GROUP, int NV>
 int start_norm(bool backward, const NormParams &p, int grid, cudaStream_t st) {
-    constexpr int V = Elems<T>::V, SLOTS = WIDE ? (rows_ahead<NV>() + 1) * NV : 0, FORWARD = norm_threads<GROUP>();
-    if (!backward) return start_norm_kernel<k_norm_forward<T, WIDE, GROUP, NV>>(p, grid, FORWARD, SLOTS * FORWARD * sizeof(uint4), st);
+    constexpr int V = Elems<T>::V, FORWARD = norm_threads<GROUP>(), WARP = in_ring<T, WIDE>() ? (rows_ahead<NV>() + 1) * NV * cells_of_warp<WIDE>() : 0;      // a warp's cells
+    if (!backward) return start_norm_kernel<k_norm_forward<T, WIDE, GROUP, NV>>(p, grid, FORWARD, WARP * FORWARD / 32 * sizeof(uint4), st);
     const size_t joined = 2 * GROUP_MAX * NV * V * sizeof(float);
-    const size_t kept = SLOTS * GROUP_MAX * (sizeof(uint4) + V + sizeof(float)), whole = SLOTS * GROUP_MAX * 2 * sizeof(uint4);
+    const size_t kept = WARP * GROUP_MAX / 32 * (sizeof(uint4) + V + sizeof(float)), whole = WARP * GROUP_MAX / 32 * 2 * sizeof(uint4);
     if (p.codes != nullptr) return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, true>>(p, grid, GROUP_MAX, kept > joined ? kept : joined, st);
     return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, false>>(p, grid, GROUP_MAX, whole > joined ? whole : joined, st);
 }
