@@ -317,7 +317,8 @@ struct NormParams {
     int param_bf16, n_parts, joint;       // joint: the backward pass' CTAs are one cluster
 };
 
-// The threads on a row are a warp (four rows to a CTA) or a CTA of 128, 256 or 512; a thread takes the
+// The threads on a row are a warp or a group of 64 to 512 (GROUPS_OF_ROW); forward, a CTA is a group, or four
+// warps, backward as many groups as 512 threads hold.  A thread takes the
 // vectors at, at + GROUP, ... of its row.  A CTA goes over rows blockIdx, blockIdx + grid, ... and keeps
 // its columns' weights (and, backward, their sums) in registers.  Where rows allow 128-bit accesses the
 // rows to come are copied into shared memory ahead of their turn, AHEAD of them at a time, each thread
@@ -330,9 +331,11 @@ __host__ __device__ constexpr int rows_ahead() { return NV >= 4 ? 2 : 3; }
 template <int GROUP>
 __host__ __device__ constexpr int norm_threads() { return GROUP == 32 ? 128 : GROUP; }
 
-// Threads on an SM: as many as the registers of 16 elements to a thread allow.
-template <typename T, int NV>
-__host__ __device__ constexpr int forward_threads() { return NV * Elems<T>::V == E ? 512 : 768; }
+template <int GROUP>
+__host__ __device__ constexpr int backward_threads() { return GROUP_MAX / GROUP * GROUP; }
+
+// Threads on an SM in the forward pass: as many as the registers of 16 elements to a thread allow.
+__host__ __device__ constexpr int forward_threads(int elements) { return elements == E ? 640 : 768; }
 
 // Waits for the threads on a row; a CTA with several rows has a barrier for each.
 template <int GROUP>
@@ -390,7 +393,7 @@ __device__ __forceinline__ uint4 take_vector(const uint4 *from, const T *row, in
 // and nothing cancels.  Bound by memory: 16384 x 4096 bf16 in 52 us (5190 GB/s; a plain copy reaches 6530), 73 us with the
 // checkpoint; 64 x 512 in 2.7 us, a launch.
 template <typename T, bool WIDE, int GROUP, int NV>
-__global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>() / norm_threads<GROUP>()) k_norm_forward(const NormParams p) {
+__global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads(NV * Elems<T>::V) / norm_threads<GROUP>()) k_norm_forward(const NormParams p) {
     constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
     constexpr bool RING = in_ring<T, WIDE>();
     extern __shared__ uint4 ring[];              // RING: [AHEAD + 1][NV][THREADS / 32][cells_of_warp]
@@ -520,15 +523,15 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads<T, NV>(
 
 // With u = (x - mean) rstd (or its 8-bit checkpoint) and g = dout w:
 //   dx = rstd (g - mean(g) - u mean(g u)),  dweight = sum_rows dout u,  dbias = sum_rows dout.
-// A CTA of 512 threads fills an SM's registers; its groups join their columns' sums at the end.  With few rows the CTAs
+// A CTA of up to 512 threads fills an SM's registers; its groups join their columns' sums at the end.  With few rows the CTAs
 // are one cluster that joins its sums through distributed shared memory; else one row of partial
 // sums per CTA is reduced in a fixed order by k_norm_params: no atomics either way, so that a step gives the same bits
 // when it is run again.  (With a CTA to a group, four times as many partial sums: 47.6 instead of 38.6 us for
 // 16384 x 2048 bf16 from a checkpoint.)  Bound by memory where rows are many: 16384 x 4096 bf16 in 69 us (5830 GB/s), 16384 x
 // 2048 from a checkpoint in 38 (4440 GB/s); 4999 x 1000 fp32 in 16, some 4 of them the second kernel's.
 template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
-__global__ void __launch_bounds__(GROUP_MAX, 1) k_norm_backward(const NormParams p) {
-    constexpr int V = Elems<T>::V, THREADS = GROUP_MAX, GROUPS = THREADS / GROUP, WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
+__global__ void __launch_bounds__(backward_threads<GROUP>(), 1) k_norm_backward(const NormParams p) {
+    constexpr int V = Elems<T>::V, THREADS = backward_threads<GROUP>(), GROUPS = THREADS / GROUP, WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
     constexpr int SOURCE = KEPT ? V : 16;        // bytes of a vector of u: codes, or x itself
     // RING: [AHEAD + 1][NV][THREADS / 32][cells_of_warp] vectors of dout, then as many of SOURCE bytes, then (KEPT) scales;
     // afterwards the sums of the CTA's groups
@@ -1073,15 +1076,20 @@ bool wide(const void *p, int64_t stride, int64_t rows, int64_t cols, int dtype) 
 struct RowShape {
     int group, nv, threads;
 };
+// The least that holds the row: what a row takes hardly depends on how many of its threads have columns (16384 rows bf16, with
+// 128, 256 or 512 threads only and now, in us: forward on 2560 columns 50 and 35, on 5120 columns 123 and 74; backward from a
+// checkpoint on 2560 columns 63 and 49, on 640 columns 25 and 20).
+constexpr int GROUPS_OF_ROW[] = {64, 96, 128, 160, 192, 256, 320, 384, 512};
 RowShape row_shape(int64_t cols, int dtype) {
     const int v = dtype == KT_F32 ? 4 : 8;
     const int64_t vectors = (pitch_of(cols) + v - 1) / v;
     RowShape s{};
     s.group = 32;
     if (vectors > 32 * (E / v))
-        for (s.group = 128; s.group < GROUP_MAX && vectors > static_cast<int64_t>(s.group) * (E / v);) s.group *= 2;
+        for (int group : GROUPS_OF_ROW)
+            if (vectors <= static_cast<int64_t>(s.group = group) * (E / v)) break;
     s.threads = s.group == 32 ? 128 : s.group;
-    s.nv = static_cast<int>((vectors + s.group - 1) / s.group);
+    s.nv = s.group == 32 ? static_cast<int>((vectors + 31) / 32) : E / v;
     if (s.nv == 3) s.nv = 4;
     return s;
 }
@@ -1110,27 +1118,30 @@ template <typename T, bool WIDE, int GROUP, int NV>
 int start_norm(bool backward, const NormParams &p, int grid, cudaStream_t st) {
     constexpr int V = Elems<T>::V, FORWARD = norm_threads<GROUP>(), WARP = in_ring<T, WIDE>() ? (rows_ahead<NV>() + 1) * NV * cells_of_warp<WIDE>() : 0;      // a warp's cells
     if (!backward) return start_norm_kernel<k_norm_forward<T, WIDE, GROUP, NV>>(p, grid, FORWARD, WARP * FORWARD / 32 * sizeof(uint4), st);
-    const size_t joined = 2 * GROUP_MAX * NV * V * sizeof(float);
-    const size_t kept = WARP * GROUP_MAX / 32 * (sizeof(uint4) + V + sizeof(float)), whole = WARP * GROUP_MAX / 32 * 2 * sizeof(uint4);
-    if (p.codes != nullptr) return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, true>>(p, grid, GROUP_MAX, kept > joined ? kept : joined, st);
-    return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, false>>(p, grid, GROUP_MAX, whole > joined ? whole : joined, st);
-}
-
-template <typename T, bool WIDE, int GROUP>
-int start_norm(bool backward, int nv, const NormParams &p, int grid, cudaStream_t st) {
-    if (nv == 1) return start_norm<T, WIDE, GROUP, 1>(backward, p, grid, st);
-    if (nv == 2) return start_norm<T, WIDE, GROUP, 2>(backward, p, grid, st);
-    if constexpr (E / Elems<T>::V >= 4) return start_norm<T, WIDE, GROUP, 4>(backward, p, grid, st);
-    else return fail(KT_ERR_SHAPE, "no kernel for %d vectors to a thread", nv);
+    constexpr int BACKWARD = backward_threads<GROUP>();
+    const size_t joined = 2 * BACKWARD * NV * V * sizeof(float);
+    const size_t kept = WARP * BACKWARD / 32 * (sizeof(uint4) + V + sizeof(float)), whole = WARP * BACKWARD / 32 * 2 * sizeof(uint4);
+    if (p.codes != nullptr) return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, true>>(p, grid, BACKWARD, kept > joined ? kept : joined, st);
+    return start_norm_kernel<k_norm_backward<T, WIDE, GROUP, NV, false>>(p, grid, BACKWARD, whole > joined ? whole : joined, st);
 }
 
 template <typename T, bool WIDE>
 int start_norm(bool backward, const RowShape &s, const NormParams &p, int grid, cudaStream_t st) {
+    constexpr int MOST = E / Elems<T>::V;
     switch (s.group) {
-        case 32: return start_norm<T, WIDE, 32>(backward, s.nv, p, grid, st);
-        case 128: return start_norm<T, WIDE, 128>(backward, s.nv, p, grid, st);
-        case 256: return start_norm<T, WIDE, 256>(backward, s.nv, p, grid, st);
-        default: return start_norm<T, WIDE, 512>(backward, s.nv, p, grid, st);
+        case 32:
+            if (s.nv == 1) return start_norm<T, WIDE, 32, 1>(backward, p, grid, st);
+            if (s.nv == 2) return start_norm<T, WIDE, 32, 2>(backward, p, grid, st);
+            return start_norm<T, WIDE, 32, MOST>(backward, p, grid, st);
+        case 64: return start_norm<T, WIDE, 64, MOST>(backward, p, grid, st);
+        case 96: return start_norm<T, WIDE, 96, MOST>(backward, p, grid, st);
+        case 128: return start_norm<T, WIDE, 128, MOST>(backward, p, grid, st);
+        case 160: return start_norm<T, WIDE, 160, MOST>(backward, p, grid, st);
+        case 192: return start_norm<T, WIDE, 192, MOST>(backward, p, grid, st);
+        case 256: return start_norm<T, WIDE, 256, MOST>(backward, p, grid, st);
+        case 320: return start_norm<T, WIDE, 320, MOST>(backward, p, grid, st);
+        case 384: return start_norm<T, WIDE, 384, MOST>(backward, p, grid, st);
+        default: return start_norm<T, WIDE, 512, MOST>(backward, p, grid, st);
     }
 }
 
@@ -1272,7 +1283,7 @@ int kt_norm_forward(const void *x, int64_t x_stride, const void *weight, const v
     const RowShape s = row_shape(cols, dtype);
     const int per_cta = s.threads / s.group;
     const bool w = wide(x, x_stride, rows, cols, dtype) && wide(out, out_stride, rows, cols, dtype);
-    const int64_t need = (rows + per_cta - 1) / per_cta, most = static_cast<int64_t>(SMS) * ((s.nv * (dtype == KT_F32 ? 4 : 8) == E ? 512 : 768) / s.threads);
+    const int64_t need = (rows + per_cta - 1) / per_cta, most = static_cast<int64_t>(SMS) * (forward_threads(s.nv * (dtype == KT_F32 ? 4 : 8)) / s.threads);
     return start_norm(false, dtype, w, s, p, static_cast<int>(need < most ? need : most), st);
 }
 

@@ -141,6 +141,15 @@ def test_norm(kt, rows, cols, dtype, pdtype, layout):
             assert ((got.double() - terms.sum(0)).abs() <= (n + 4) * U32 * terms.abs().sum(0) + rounding(pdtype) * terms.sum(0).abs()).all()
 
 
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols", [1000, 1029, 1500, 2000, 2500, 2561, 2700, 4000, 5120, 5121, 6000, 8000])
+def test_norm_on_each_number_of_threads(kt, cols, dtype, layout):
+    """Rows of 64, 96, 128, 160, 192, 256, 320, 384 and 512 threads; one cluster, and a row of partial sums to a CTA."""
+    for rows in (21, 330):
+        test_norm(kt, rows, cols, dtype, F32, layout)
+
+
 def test_norm_against_differences(kt):
     """dx, dweight and dbias against central differences of the forward kernel itself (fp32).
 
