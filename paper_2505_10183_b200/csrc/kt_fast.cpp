@@ -86,6 +86,13 @@ void *stream_of(PyObject *o) {
 
 void *address(const at::Tensor *t) { return t == nullptr ? nullptr : t->data_ptr(); }
 
+// (A workspace of any type and shape; an expanded or strided one would count bytes that are not its own.)
+int64_t workspace_bytes(const at::Tensor *t) {
+    if (t == nullptr) return 0;
+    if (!t->is_contiguous()) refuse(KT_ERR_SHAPE, "workspace: a contiguous tensor expected");
+    return static_cast<int64_t>(t->nbytes());
+}
+
 // ------------------------------------------------------------------------------- row operators
 struct Matrix {
     void *at = nullptr;
@@ -172,7 +179,7 @@ PyObject *norm_backward(PyObject *const *a) {   // dout, weight, rstd, dx, dweig
     check_codes(codes, scales, dout.rows, dout.cols);
     const float *const m = per_row(mean, dout.rows, "mean"), *const r = per_row(rstd, dout.rows, "rstd");
     return done(c_norm_backward(dout.at, dout.stride, x.at, x.stride, m, static_cast<int8_t *>(address(codes)), static_cast<float *>(address(scales)), r, address(weight), type, dx.at, dx.stride,
-                                address(dweight), address(dbias), address(workspace), workspace == nullptr ? 0 : static_cast<int64_t>(workspace->nbytes()), dout.rows, dout.cols, dout.type,
+                                address(dweight), address(dbias), address(workspace), workspace_bytes(workspace), dout.rows, dout.cols, dout.type,
                                 stream_of(a[11])));
 }
 
@@ -260,7 +267,7 @@ PyObject *attn_backward(PyObject *const *a) {   // dout, q, k, v, out, lse, dq, 
     const Heads hg = heads(dout, "dout", q), hq = heads(q, "q", q), hk = heads(k, "k", k), hv = heads(v, "v", k), ho = heads(out, "out", q), hdq = heads(dq, "dq", q), hdk = heads(dk, "dk", k),
                 hdv = heads(dv, "dv", k);
     return done(c_attn_backward(&d, hg.at, hg.stride, hq.at, hq.stride, hk.at, hk.stride, hv.at, hv.stride, ho.at, ho.stride, static_cast<float *>(lse->data_ptr()), hdq.at, hdq.stride, hdk.at,
-                                hdk.stride, hdv.at, hdv.stride, workspace->data_ptr(), static_cast<int64_t>(workspace->nbytes()), stream_of(a[14])));
+                                hdk.stride, hdv.at, hdv.stride, workspace->data_ptr(), workspace_bytes(workspace), stream_of(a[14])));
 }
 
 // ---------------------------------------------------------------------------------- the module

@@ -94,3 +94,27 @@ def test_c_entries_refuse_bad_addresses_and_types(kt):
     assert lib.kt_ckpt_store(p, 31, c, p, 4, 32, 0, None) == kt.KT_ERR_SHAPE
     assert lib.kt_norm_forward(p, 32, p, p, 9, p, 32, None, None, None, None, 4, 32, 0, 1e-5, None) == kt.KT_ERR_INVALID
     assert lib.kt_last_error(None)
+
+
+def heads(*shape):
+    return torch.zeros(*shape, dtype=BF16)
+
+
+def attention(kt, len_q=16, len_kv=16, dim=64):
+    """Arguments of kt_attn_backward in their order, for 2 sequences, 4 heads on 2; those of the forward pass are 1 ... 5 of them."""
+    q, k = heads(2, len_q, 4, dim), heads(2, len_kv, 2, dim)
+    work = torch.zeros(max(1, kt.kt_attn_workspace(q, k)), dtype=torch.uint8)
+    return [heads(2, len_q, 4, dim), q, k, heads(2, len_kv, 2, dim), heads(2, len_q, 4, dim), torch.zeros(2, 4, len_q), heads(2, len_q, 4, dim),
+            heads(2, len_kv, 2, dim), heads(2, len_kv, 2, dim), work]
+
+
+def test_workspaces_that_are_smaller_than_they_look(kt):
+    """An expanded tensor counts bytes that it does not have, a strided one bytes between those of others."""
+    x, c, s, r, w = torch.zeros(4, 32), torch.zeros(4, 32, dtype=I8), torch.zeros(4, 1), torch.zeros(4), torch.zeros(32)
+    need = kt.kt_norm_workspace(4, 32)
+    for work in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2]):
+        assert status(kt, kt.kt_norm_backward, x, w, r, x, w, w, work, codes=c, scales=s) == kt.KT_ERR_SHAPE
+    args = attention(kt)
+    need = args[9].numel()
+    for work in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2]):
+        assert status(kt, kt.kt_attn_backward, *args[:9], work) == kt.KT_ERR_SHAPE
