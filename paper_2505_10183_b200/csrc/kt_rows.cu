@@ -1066,6 +1066,12 @@ int check_params(const void *a, const void *b, int dtype) {
     return KT_OK;
 }
 
+int check_per_row(const float *mean, const float *rstd) {
+    for (const float *p : {mean, rstd})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return fail(KT_ERR_ALIGN, "mean or rstd is not 4-byte aligned");
+    return KT_OK;
+}
+
 // 128-bit accesses: base and row stride multiples of 16 bytes, whole vectors in a row.
 bool wide(const void *p, int64_t stride, int64_t rows, int64_t cols, int dtype) {
     const int64_t es = elem_size(dtype);
@@ -1271,6 +1277,7 @@ int kt_norm_forward(const void *x, int64_t x_stride, const void *weight, const v
     if (int rc = check_matrix("x", x, x_stride, rows, cols, dtype)) return rc;
     if (int rc = check_matrix("out", out, out_stride, rows, cols, dtype)) return rc;
     if (int rc = check_codes(codes, scales, false)) return rc;
+    if (int rc = check_per_row(mean, rstd)) return rc;
     NormParams p{};
     p.x = x, p.weight = weight, p.bias = bias, p.out = out, p.mean = mean, p.rstd = rstd, p.codes = codes, p.scales = scales;
     p.rows = rows, p.cols = cols, p.x_stride = x_stride, p.out_stride = out_stride, p.eps = eps, p.param_bf16 = param_dtype == KT_BF16;
@@ -1320,6 +1327,7 @@ int kt_norm_backward(const void *dout, int64_t dout_stride, const void *x, int64
             return rc;
         }
         if (rstd == nullptr) return fail(KT_ERR_INVALID, "rstd is NULL");
+        if (int rc = check_per_row(mean, rstd)) return rc;
         if (sums) {
             const int64_t need = kt_norm_workspace(rows, cols);
             if (workspace == nullptr) return fail(KT_ERR_INVALID, "workspace is NULL");

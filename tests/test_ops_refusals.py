@@ -118,3 +118,19 @@ def test_workspaces_that_are_smaller_than_they_look(kt):
     need = args[9].numel()
     for work in (torch.zeros(1, dtype=torch.uint8).expand(need), torch.zeros(2 * need, dtype=torch.uint8)[::2]):
         assert status(kt, kt.kt_attn_backward, *args[:9], work) == kt.KT_ERR_SHAPE
+
+
+def test_c_entries_refuse_row_statistics_at_odd_addresses(kt):
+    lib = kt._lib
+    x, w, ws = torch.zeros(4, 32), torch.zeros(32), torch.zeros(kt.kt_norm_workspace(4, 32) + 16, dtype=torch.uint8)
+    p, r, at = x.data_ptr(), torch.zeros(8).data_ptr(), ws.data_ptr() // 16 * 16 + 16
+
+    def forward(mean, rstd):
+        return lib.kt_norm_forward(p, 32, w.data_ptr(), None, 0, p, 32, mean, rstd, None, None, 4, 32, 0, 1e-5, None)
+
+    def backward(mean, rstd):
+        return lib.kt_norm_backward(p, 32, p, 32, mean, None, None, rstd, None, 0, p, 32, None, None, at, ws.numel() - 16, 4, 32, 0, None)
+
+    for call in (forward, backward):
+        assert call(r + 1, r) == kt.KT_ERR_ALIGN
+        assert call(r, r + 2) == kt.KT_ERR_ALIGN
