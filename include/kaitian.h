@@ -626,7 +626,8 @@ int kt_act_backward(const void *dout, int64_t dout_stride, const void *x, int64_
 
 /* Softmax attention on bf16 heads.  Tensors are [batch, tokens, heads, head_dim]; a stride array
  * (host) holds the strides of batch, token and head in elements, head_dim is contiguous; addresses are
- * 16-byte aligned and strides multiples of 8 elements (positive: an expanded tensor needs a copy).
+ * 16-byte aligned and strides multiples of 8 elements (positive: an expanded tensor needs a copy).  Rows
+ * of an output do not overlap: its strides, in rising order, each clear what those before them span.
  * heads is a multiple of heads_kv: query head h reads key/value head h / (heads / heads_kv).
  * used_q, used_kv (device, int32[batch], or NULL for all): tokens in use of each sequence, taken into
  * [0, len]; query i of a sequence with n queries and m keys sees the keys j < m, with causal those

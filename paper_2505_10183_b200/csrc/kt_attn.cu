@@ -19,6 +19,7 @@
 
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <cstddef>
@@ -1267,7 +1268,9 @@ int make_map(CUtensorMap *map, const char *what, const void *at, const int64_t *
     return KT_OK;
 }
 
-int check_heads(const char *what, const void *at, const int64_t *stride, int batch, int tokens, int heads) {
+// `written`: an output, no two rows of which may share elements (the bits would depend on who writes last): each
+// stride, in rising order, clears what those before it span.
+int check_heads(const char *what, const void *at, const int64_t *stride, int batch, int tokens, int heads, int dim, bool written) {
     if (at == nullptr) return fail(KT_ERR_INVALID, "%s is NULL", what);
     if (reinterpret_cast<uintptr_t>(at) % 16) return fail(KT_ERR_ALIGN, "%s is not 16-byte aligned", what);
     const int size[3] = {batch, tokens, heads};
@@ -1275,6 +1278,15 @@ int check_heads(const char *what, const void *at, const int64_t *stride, int bat
         if (size[i] <= 1) continue;
         if (stride[i] % 8) return fail(KT_ERR_ALIGN, "%s: the strides of batch, token and head must be multiples of 8 elements", what);
         if (stride[i] < 8 || stride[i] >= INT64_C(1) << 38) return fail(KT_ERR_SHAPE, "%s: a stride of %lld elements (expanded tensors need a copy)", what, (long long)stride[i]);
+    }
+    if (!written) return KT_OK;
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return stride[a] < stride[b]; });
+    __int128 span = dim;                        // (2^30 steps of 2^38 elements, three times)
+    for (int i : order) {
+        if (size[i] <= 1) continue;
+        if (stride[i] < span) return fail(KT_ERR_SHAPE, "%s: tokens, heads or sequences of an output overlap (a stride of %lld elements)", what, (long long)stride[i]);
+        span += static_cast<__int128>(stride[i]) * (size[i] - 1);
     }
     return KT_OK;
 }
@@ -1421,11 +1433,11 @@ int kt_attn_forward(const kt_attn *a, const void *q, const int64_t *q_stride, co
     if (int rc = fill(a, &p)) return rc;
     if (p.batch == 0 || p.len_q == 0) return KT_OK;
     if (!q_stride || !k_stride || !v_stride || !out_stride) return fail(KT_ERR_INVALID, "a stride array is NULL");
-    if (int rc = check_heads("q", q, q_stride, p.batch, p.len_q, p.heads)) return rc;
-    if (int rc = check_heads("out", out, out_stride, p.batch, p.len_q, p.heads)) return rc;
+    if (int rc = check_heads("q", q, q_stride, p.batch, p.len_q, p.heads, p.dim, false)) return rc;
+    if (int rc = check_heads("out", out, out_stride, p.batch, p.len_q, p.heads, p.dim, true)) return rc;
     if (p.len_kv > 0) {
-        if (int rc = check_heads("k", k, k_stride, p.batch, p.len_kv, p.heads_kv)) return rc;
-        if (int rc = check_heads("v", v, v_stride, p.batch, p.len_kv, p.heads_kv)) return rc;
+        if (int rc = check_heads("k", k, k_stride, p.batch, p.len_kv, p.heads_kv, p.dim, false)) return rc;
+        if (int rc = check_heads("v", v, v_stride, p.batch, p.len_kv, p.heads_kv, p.dim, false)) return rc;
     }
     if (lse == nullptr) return fail(KT_ERR_INVALID, "lse is NULL");
     if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(KT_ERR_ALIGN, "lse is not 4-byte aligned");
@@ -1460,12 +1472,13 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
         const void *at;
         const int64_t *stride;
         int tokens, heads;
-    } const all[] = {{"dout", dout, dout_stride, p.len_q, p.heads}, {"q", q, q_stride, p.len_q, p.heads}, {"out", out, out_stride, p.len_q, p.heads},
-                     {"dq", dq, dq_stride, p.len_q, p.heads}, {"k", k, k_stride, p.len_kv, p.heads_kv}, {"v", v, v_stride, p.len_kv, p.heads_kv},
-                     {"dk", dk, dk_stride, p.len_kv, p.heads_kv}, {"dv", dv, dv_stride, p.len_kv, p.heads_kv}};
+        bool written;
+    } const all[] = {{"dout", dout, dout_stride, p.len_q, p.heads, false}, {"q", q, q_stride, p.len_q, p.heads, false}, {"out", out, out_stride, p.len_q, p.heads, false},
+                     {"dq", dq, dq_stride, p.len_q, p.heads, true}, {"k", k, k_stride, p.len_kv, p.heads_kv, false}, {"v", v, v_stride, p.len_kv, p.heads_kv, false},
+                     {"dk", dk, dk_stride, p.len_kv, p.heads_kv, true}, {"dv", dv, dv_stride, p.len_kv, p.heads_kv, true}};
     for (const auto &t : all)
         if (t.tokens > 0)
-            if (int rc = check_heads(t.what, t.at, t.stride, p.batch, t.tokens, t.heads)) return rc;
+            if (int rc = check_heads(t.what, t.at, t.stride, p.batch, t.tokens, t.heads, p.dim, t.written)) return rc;
     if (p.len_kv == 0) return clear(static_cast<__nv_bfloat16 *>(dq), dq_stride, p.batch, p.len_q, p.heads, p.dim, st);
     if (p.len_q == 0) {
         if (int rc = clear(static_cast<__nv_bfloat16 *>(dk), dk_stride, p.batch, p.len_kv, p.heads_kv, p.dim, st)) return rc;

@@ -134,3 +134,41 @@ def test_c_entries_refuse_row_statistics_at_odd_addresses(kt):
     for call in (forward, backward):
         assert call(r + 1, r) == kt.KT_ERR_ALIGN
         assert call(r, r + 2) == kt.KT_ERR_ALIGN
+
+
+@pytest.mark.parametrize("which,name", [(3, "out"), (6, "dq"), (7, "dk"), (8, "dv")])
+def test_attention_outputs_that_overlap_themselves(kt, which, name):
+    """Tokens, heads or sequences that share elements would be written by several CTAs at once; inputs may do so."""
+    for len_q, len_kv in ((16, 16), (0, 16), (16, 0)):
+        args = attention(kt, len_q, len_kv)
+        if name == "out":                                              # of the forward pass
+            args = [args[1], args[2], args[3], args[6], args[5]]
+            call = kt.kt_attn_forward
+        else:
+            call = kt.kt_attn_backward
+        B, L, H, D = args[which].shape
+        if L == 0:
+            continue
+        room = torch.zeros(4 * B * L * H * D, dtype=BF16)
+        for strides in ((L * H * D, H * D, 8, 1),                      # heads
+                        (L * H * D, 8, L * D, 1),                      # tokens
+                        (L * H * D, D, D, 1),                          # a token's second head is the next token's first
+                        (H * D, H * D, D, 1),                          # sequences
+                        (L * H * D, (H - 1) * D + 8, D, 1),            # a token begins inside the last one
+                        (L * H * D - 8, H * D, D, 1)):
+            args[which] = room.as_strided((B, L, H, D), strides)
+            assert status(kt, call, *args) == kt.KT_ERR_SHAPE, strides
+
+
+def test_attention_outputs_in_any_order_of_dimensions(kt):
+    """Layouts without overlaps get past the checks: without a device the call then ends for want of one."""
+    if torch.cuda.is_available():
+        pytest.skip("runs as a whole there (test_layouts)")
+    B, L, H, D = 2, 16, 4, 64
+    for strides in ((L * H * D, H * D, D, 1), (L * H * D, D, L * D, 1), (D, B * D, L * B * D, 1), (L * H * 72 + 8, H * 72, 72, 1)):
+        args = attention(kt)
+        args[6] = torch.zeros(2 * B * L * H * 72, dtype=BF16).as_strided((B, L, H, D), strides)
+        assert status(kt, kt.kt_attn_backward, *args) == kt.KT_ERR_CUDA, strides
+    args = attention(kt)
+    args[2] = torch.zeros(2 * 16 * 2 * 64, dtype=BF16).as_strided((2, 16, 2, 64), (16 * 64, 64, 8, 1))       # an input
+    assert status(kt, kt.kt_attn_backward, *args) == kt.KT_ERR_CUDA
