@@ -806,7 +806,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         mma_commit(&bars.q_free[qs]);           // dS came from scores and dP: all products with the two tiles are done
                         mma_commit(&bars.do_free[ds]);
                     }
-                } else if (it.n > 0 && ok) {                     // dP takes the place of P and dS: one thread, in order
+                } else if (it.n > 0 && ok) {
                     ok = dprobs(tiles_in, set);
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
@@ -820,7 +820,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         mma_commit(&bars.q_free[qs]);
                         for (int w = 0; w < 2; ++w) product_down<DH, 64>(tmem + Dkv::DV, tmem + Dkv::DP + w * 64, do_at + ds * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
                         mma_commit(&bars.do_free[ds]);
-                        if (i + 1 < it.n) ok = dprobs(g + 1, set);
+                        // dP takes the place of P and dS, which products with other sums still read: nothing but
+                        // their end (the same that frees dO's place) orders the two.
+                        if (i + 1 < it.n) ok = bar_wait_one(&bars.do_free[ds], g / Dkv::DO_SLOTS & 1, gave_up) && dprobs(g + 1, set);
                     }
                 }
                 if (sums && it.n > 0 && ok) {

@@ -314,3 +314,18 @@ def test_refused(kt):
     with pytest.raises(kt.KtError) as e:
         kt.kt_attn_backward(q, q, k, k, out, lse, torch.empty_like(q), torch.empty_like(k), torch.empty_like(k), work)
     assert e.value.status == kt.KT_ERR_SHAPE
+
+
+@pytest.mark.parametrize("Lq,Lk,H,Hk,causal", [(2100, 2100, 4, 1, True), (3000, 900, 6, 2, False)])
+def test_many_query_tiles_to_a_key_tile(kt, Lq, Lk, H, Hk, causal):
+    """Heads of 128: dP of a query tile takes the place of the last one's P and dS. Dozens of tiles in a row, against the
+    formulas, and the same bits every time while another stream keeps the device busy."""
+    want = run_case(kt, 1, Lq, Lk, H, Hk, 128, causal, seed=Lq)
+    s = torch.cuda.Stream()
+    for i in range(4):
+        with torch.cuda.stream(s):
+            a = torch.randn(2048, 2048, device="cuda", dtype=BF16)
+            for _ in range(i):
+                a = a @ a * 0.01
+        got = run_case(kt, 1, Lq, Lk, H, Hk, 128, causal, seed=Lq)
+        assert all(torch.equal(x.nan_to_num(nan=0.0), y.nan_to_num(nan=0.0)) for x, y in zip(got, want))
