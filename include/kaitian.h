@@ -659,9 +659,13 @@ int kt_attn_backward(const kt_attn *desc, const void *dout, const int64_t *dout_
                      const int64_t *dk_stride, void *dv, const int64_t *dv_stride, void *workspace,
                      int64_t workspace_bytes, void *stream);
 
-/* Every wait inside the attention kernels is bounded: one that lasts two seconds gives up, its kernel ends
- * without a result and the device stays usable.  *count (host) = how many did since the library was
+/* Every wait inside the attention kernels is bounded.  One that lasts longer than the limit (two seconds,
+ * the time that another context holds the device included) gives up: the device stays usable, the call has
+ * returned KT_OK, and its results (out and lse, or dq, dk and dv) are NaN wherever they are not right.
+ * kt_attn_wait_limit sets the limit of the calls to come in this process, 0 to 60 s (with 0 all that is not there
+ * at once is given up; KT_ERR_INVALID outside).  *count (host) = how many waits gave up since the library was
  * loaded on the current device (0 unless something is broken); waits for the device. */
+int kt_attn_wait_limit(int64_t nanoseconds);
 int kt_attn_given_up(int64_t *count);
 
 /* Number of kernels this context has launched so far (for launch accounting). */

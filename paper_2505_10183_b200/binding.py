@@ -36,7 +36,7 @@ EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "k
            "kt_ipc_export", "kt_ipc_open", "kt_ipc_close", "kt_host_register", "kt_host_unregister", "kt_host_barrier", "kt_shard_step", "kt_shard_bcast",
            "kt_ckpt_pitch", "kt_ckpt_blocks", "kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_workspace",
            "kt_norm_backward", "kt_act_forward", "kt_act_backward", "kt_attn_forward", "kt_attn_workspace", "kt_attn_backward",
-           "kt_attn_given_up"]
+           "kt_attn_wait_limit", "kt_attn_given_up"]
 
 _DTYPES = {torch.float32: KT_F32, torch.bfloat16: KT_BF16}
 
@@ -117,6 +117,7 @@ def _load() -> C.CDLL:
         "kt_attn_forward": ([vp] * 11, C.c_int),
         "kt_attn_workspace": ([C.c_int, C.c_int, C.c_int], i64),
         "kt_attn_backward": ([vp] * 19 + [i64, vp], C.c_int),
+        "kt_attn_wait_limit": ([i64], C.c_int),
         "kt_attn_given_up": ([i64p], C.c_int),
         "kt_launch_count": ([vp], C.c_int64),
         "kt_last_error": ([vp], C.c_char_p),
@@ -771,8 +772,14 @@ def kt_attn_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: to
     _fast.attn_backward(dout, q, k, v, out, lse, dq, dk, dv, workspace, scale, causal, used_q, used_kv, stream)
 
 
+def kt_attn_wait_limit(nanoseconds: int) -> None:
+    """How long a wait inside the attention kernels of the calls to come may last before it gives up (2 s at first)."""
+    _check(_lib.kt_attn_wait_limit(int(nanoseconds)))
+
+
 def kt_attn_given_up() -> int:
-    """Waits inside attention kernels that were given up since the library was loaded (0 unless something is broken)."""
+    """Waits inside attention kernels that were given up since the library was loaded (0 unless something is broken;
+    the results of such a call are NaN wherever they are not right).  Waits for the device."""
     n = C.c_int64(0)
     _check(_lib.kt_attn_given_up(C.byref(n)))
     return int(n.value)

@@ -160,7 +160,7 @@ def synchronised_step(shape: Shape, params: Dict[str, torch.Tensor], x: torch.Te
                       group_of: List[int], used: Optional[torch.Tensor] = None) -> Dict[str, torch.Tensor]:
     """Gradients of the mean over all sequences of x: rank r does the next shares[r] of them.  dz: gradient of
     one sequence's loss with respect to its output."""
-    lists, at = [], 0
+    lists, at, given_up = [], 0, kt.kt_attn_given_up()
     for share in shares:
         mine = slice(at, at + share)
         at += share
@@ -168,6 +168,8 @@ def synchronised_step(shape: Shape, params: Dict[str, torch.Tensor], x: torch.Te
         block.forward(x[mine], None if used is None else used[mine])
         block.backward((dz[mine].float() / share).to(dz.dtype))
         lists.append([block.grads[n] for n in NAMES])
+    if kt.kt_attn_given_up() != given_up:           # gradients that are not right reach no replica
+        raise RuntimeError("a wait inside an attention kernel was given up: the step has no result")
     ctx = kt.kt_groups_init(group_of, shares)
     kt.kt_bucket_pack(ctx, lists, 25 << 20)
     out = [torch.empty_like(params[n]) for n in NAMES]

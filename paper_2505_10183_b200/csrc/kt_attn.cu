@@ -57,6 +57,7 @@ struct AttnParams {
     int batch, heads, heads_kv, len_q, len_kv, dim, causal;
     int tiles_q, tiles_kv, parts;               // parts: CTAs that share a work item, where they do
     float scale, scale_log2;
+    uint64_t wait_ns;                           // how long a wait may last
 };
 
 // Tokens in use of a sequence, and how far a query sees.
@@ -79,7 +80,7 @@ __device__ __forceinline__ int tiles(int rows) { return (rows + TILE - 1) / TILE
 // cleared first, which the whole warp does (rows past `len` arrive as zeros).
 template <int DH, bool CLEAN>
 __device__ __forceinline__ bool load_tile(uint32_t to, uint8_t *to_ptr, const CUtensorMap *map, uint64_t *full, uint64_t *landed, uint32_t &landed_phase,
-                                          int token, int used, int len, int head, int batch, volatile uint32_t *gave_up) {
+                                          int token, int used, int len, int head, int batch, volatile Patience *waits) {
     const int lane = threadIdx.x % 32;
     const bool dirty = CLEAN && used < min(len, token + TILE);
     uint64_t *bar = dirty ? landed : full;
@@ -90,7 +91,7 @@ __device__ __forceinline__ bool load_tile(uint32_t to, uint8_t *to_ptr, const CU
     }
     __syncwarp();
     if (!dirty) return true;
-    if (!bar_wait(landed, landed_phase, gave_up)) return false;
+    if (!bar_wait(landed, landed_phase, waits)) return false;
     landed_phase ^= 1;
     const int from = max(0, used - token);
     for (int i = from * 8 + lane; i < TILE * 8; i += 32)
@@ -120,11 +121,20 @@ __device__ __forceinline__ void write_zeros(__nv_bfloat16 *row, int c0, int c1) 
     for (int c = c0; c < c1; c += 8) *reinterpret_cast<uint4 *>(row + c) = make_uint4(0, 0, 0, 0);
 }
 
-// The end of a kernel whose waits have given up: copies and products in flight get time to finish before
-// the memory that they write is handed back.
-__device__ __forceinline__ void settle(volatile uint32_t *gave_up) {
-    if (*gave_up)
-        for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+// The end of a CTA one of whose waits has given up.  Copies, products and answers in flight get two milliseconds to
+// finish before the memory that they write is handed back.  Then all results of the call become NaN (fill_nan, by the
+// eight warps that compute): the CTA has taken items that nobody else will do, and what others write later is right.
+__device__ __forceinline__ void settle() {
+    const uint64_t start = now_ns();
+    for (int i = 0; i < 100000 && now_ns() - start < 2000000; ++i) __nanosleep(1000);
+}
+__device__ __forceinline__ void fill_nan(__nv_bfloat16 *at, const int64_t (&stride)[3], int batch, int tokens, int heads, int dim) {
+    const int64_t pieces = dim / 8, all = static_cast<int64_t>(batch) * tokens * heads * pieces;
+    for (int64_t i = threadIdx.x; i < all; i += 256) {
+        const int64_t row = i / pieces, token = row / heads;
+        *reinterpret_cast<uint4 *>(at + token / tokens * stride[0] + token % tokens * stride[1] + row % heads * stride[2] + i % pieces * 8) =
+            make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);
+    }
 }
 
 // ------------------------------------------------------------------------------------ forward
@@ -146,7 +156,8 @@ struct FwdSmem {
     alignas(1024) uint8_t q[SETS][2][TILE_BYTES], k[K_SLOTS][TILE_BYTES], v[V_SLOTS][TILE_BYTES];
     Queue queue;
     uint64_t q_full[SETS], q_free[SETS], k_full[K_SLOTS], k_free[K_SLOTS], v_full[V_SLOTS], v_free[V_SLOTS], s_full[2], s_taken, p_ready[2], o_done[2], o_taken[2], landed;
-    uint32_t tmem, gave_up;
+    uint32_t tmem;
+    Patience waits;
 };
 
 // What a CTA takes of n steps that the CTAs of its cluster share.
@@ -259,7 +270,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         for (int i = 0; i < V_SLOTS; ++i) bar_init(&sm.v_full[i], 1), bar_init(&sm.v_free[i], 1);
         for (int w = 0; w < 2; ++w) bar_init(&sm.s_full[w], 1), bar_init(&sm.p_ready[w], 4), bar_init(&sm.o_done[w], 1), bar_init(&sm.o_taken[w], 4);
         bar_init(&sm.s_taken, 4), bar_init(&sm.landed, 1);
-        sm.gave_up = 0;
+        sm.waits = {p.wait_ns, 0};
         fence_async_smem();
     }
     if (warp == WARP_SCORES) tmem_alloc(&sm.tmem, TMEM_COLUMNS);
@@ -268,23 +279,23 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
     tmem_fence_after();
     const uint32_t tmem = sm.tmem;
     const int first_block = SPLIT ? blockIdx.x / p.parts : blockIdx.x;       // and the only one, with SPLIT
-    volatile uint32_t *gave_up = &sm.gave_up;
+    volatile Patience *waits = &sm.waits;
 
     if (warp == WARP_LOAD) {
         registers_give<REGISTERS_HELP>();
         uint32_t asked = 0, sets = 0, tiles_in = 0, landed_phase = 0;      // counts over all items
         bool ok = true;
-        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, asked - 1, gave_up)) {
+        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, asked - 1, waits)) {
             const Item it(p, block);
             const Seq seq(p, it.b);
             if constexpr (!SPLIT) {
-                if (!(ok = bar_wait(&sm.queue.free[asked % QUEUE], (asked / QUEUE + 1) & 1, gave_up))) break;
+                if (!(ok = bar_wait(&sm.queue.free[asked % QUEUE], (asked / QUEUE + 1) & 1, waits))) break;
                 if (lane == 0) queue_ask(sm.queue, asked);
                 ++asked;
             }
             if (it.n == 0) continue;
             const int set = sets % SETS;
-            if (!(ok = bar_wait(&sm.q_free[set], (sets / SETS + 1) & 1, gave_up))) break;
+            if (!(ok = bar_wait(&sm.q_free[set], (sets / SETS + 1) & 1, waits))) break;
             ++sets;
             if (lane == 0) {
                 bar_expect(&sm.q_full[set], 2 * Smem::TILE_BYTES);
@@ -295,13 +306,13 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             for (int j = 0; ok && j <= it.n; ++j) {              // keys a tile ahead of values
                 if (j < it.n) {
                     const uint32_t i = tiles_in + j, ks = i % K_SLOTS;
-                    ok = bar_wait(&sm.k_free[ks], (i / K_SLOTS + 1) & 1, gave_up) &&
-                         load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                    ok = bar_wait(&sm.k_free[ks], (i / K_SLOTS + 1) & 1, waits) &&
+                         load_tile<DH, false>(smem_addr(sm.k[ks]), sm.k[ks], &map_k, &sm.k_full[ks], &sm.landed, landed_phase, (it.from + j) * TILE, seq.m, p.len_kv, it.h_kv, it.b, waits);
                 }
                 if (ok && j > 0) {
                     const uint32_t i = tiles_in + j - 1, vs = i % V_SLOTS;
-                    ok = bar_wait(&sm.v_free[vs], (i / V_SLOTS + 1) & 1, gave_up) &&
-                         load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (it.from + j - 1) * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                    ok = bar_wait(&sm.v_free[vs], (i / V_SLOTS + 1) & 1, waits) &&
+                         load_tile<DH, true>(smem_addr(sm.v[vs]), sm.v[vs], &map_v, &sm.v_full[vs], &sm.landed, landed_phase, (it.from + j - 1) * TILE, seq.m, p.len_kv, it.h_kv, it.b, waits);
                 }
             }
             tiles_in += it.n;
@@ -312,16 +323,16 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const uint32_t q_at = smem_addr(sm.q), k_at = smem_addr(sm.k);
             uint32_t items = 0, sets = 0, tiles_in = 0, steps = 0;
             bool ok = true;
-            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, gave_up)) {
+            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, waits)) {
                 const Item it(p, block);
                 if (it.n == 0) continue;
                 const uint32_t set = sets % SETS;
-                ok = bar_wait_one(&sm.q_full[set], sets / SETS & 1, gave_up);
+                ok = bar_wait_one(&sm.q_full[set], sets / SETS & 1, waits);
                 ++sets;
                 for (int u = 0; ok && u < it.steps; ++u, ++steps) {
                     const int w = it.group(u);
                     const uint32_t i = tiles_in + it.key_tile(u), ks = i % K_SLOTS;
-                    ok = bar_wait_one(&sm.k_full[ks], i / K_SLOTS & 1, gave_up) && (steps == 0 || bar_wait_one(&sm.s_taken, (steps - 1) & 1, gave_up));
+                    ok = bar_wait_one(&sm.k_full[ks], i / K_SLOTS & 1, waits) && (steps == 0 || bar_wait_one(&sm.s_taken, (steps - 1) & 1, waits));
                     if (!ok) break;
                     tmem_fence_after();
                     product_rows<DH, TILE>(tmem, q_at + (set * 2 + w) * Smem::TILE_BYTES, k_at + ks * Smem::TILE_BYTES);
@@ -339,13 +350,13 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             const uint32_t v_at = smem_addr(sm.v);
             uint32_t items = 0, tiles_in = 0, mine[2] = {0, 0}, outputs[2] = {0, 0};
             bool ok = true;
-            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, gave_up)) {
+            for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next_one<false>(sm.queue, items++, waits)) {
                 const Item it(p, block);
                 for (int u = 0; ok && u < it.steps; ++u) {
                     const int w = it.group(u), j = it.key_tile(u);
                     const uint32_t i = tiles_in + j, vs = i % V_SLOTS;
-                    ok = bar_wait_one(&sm.v_full[vs], i / V_SLOTS & 1, gave_up) && bar_wait_one(&sm.p_ready[w], (mine[w] + j) & 1, gave_up) &&
-                         (j > 0 || outputs[w] == 0 || bar_wait_one(&sm.o_taken[w], (outputs[w] - 1) & 1, gave_up));       // the last item's sums have been read
+                    ok = bar_wait_one(&sm.v_full[vs], i / V_SLOTS & 1, waits) && bar_wait_one(&sm.p_ready[w], (mine[w] + j) & 1, waits) &&
+                         (j > 0 || outputs[w] == 0 || bar_wait_one(&sm.o_taken[w], (outputs[w] - 1) & 1, waits));       // the last item's sums have been read
                     if (!ok) break;
                     tmem_fence_after();
                     product_down<DH, TILE>(tmem + 256 + w * DH, tmem + TILE + w * 64, v_at + vs * Smem::TILE_BYTES, j > 0);
@@ -363,7 +374,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes, p_at = lanes + TILE + w * 64, o_at = lanes + 256 + w * DH;
         uint32_t items = 0, mine = 0;
         bool ok = true;
-        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, items++, gave_up)) {
+        for (int block = first_block; ok && block >= 0; block = SPLIT ? -1 : queue_next<false>(sm.queue, items++, waits)) {
             const Item it(p, block);
             const Seq seq(p, it.b);
             const int row = it.row0 + w * TILE + threadIdx.x % TILE, n_mine = w == 0 ? it.n_tiles[0] : it.n_tiles[1];
@@ -372,7 +383,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             float top = -INFINITY, sum = 0.0f;      // in units of log 2, after scaling
             for (int j = 0; j < n_mine; ++j) {
                 const uint32_t i = mine + j;
-                if (!(ok = bar_wait(&sm.s_full[w], i & 1, gave_up))) break;
+                if (!(ok = bar_wait(&sm.s_full[w], i & 1, waits))) break;
                 tmem_fence_after();
                 uint32_t s[4][32];
 #pragma unroll
@@ -398,7 +409,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     if (grow) top = here;
                     sum *= by;
                     if (j > 0) {
-                        if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, gave_up))) break;
+                        if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, waits))) break;
                         tmem_fence_after();
 #pragma unroll
                         for (int c = 0; c < DH; c += 32) {
@@ -422,7 +433,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
                     packed[c / 64][c % 64 / 2] = pack_bf16(e);
                 }
                 if (j > 0) {                        // the last probabilities have been used
-                    if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&sm.o_done[w], (i - 1) & 1, waits))) break;
                     tmem_fence_after();
                 }
                 tmem_store32(p_at, packed[0]);
@@ -434,7 +445,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             mine += n_mine;
             if constexpr (SPLIT) {                  // what the CTA has of the row, over the tiles that are done with
-                if (ok && n_mine > 0) ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up);
+                if (ok && n_mine > 0) ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, waits);
                 tmem_fence_after();
                 asm volatile("barrier.sync 1, 256;" ::: "memory");
 #pragma unroll
@@ -449,7 +460,7 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
             }
             __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
             if (ok && n_mine > 0) {
-                if (!(ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, gave_up))) break;
+                if (!(ok = bar_wait(&sm.o_done[w], (mine - 1) & 1, waits))) break;
                 tmem_fence_after();
                 const float by = sum == 0.0f ? 0.0f : 1.0f / sum;
 #pragma unroll
@@ -487,7 +498,14 @@ k_attn_forward(const __grid_constant__ CUtensorMap map_q, const __grid_constant_
         cluster_sync();                         // the others have read what is here
     }
     __syncthreads();
-    settle(gave_up);
+    if (waits->gave_up) {
+        settle();
+        if (warp < 8) {
+            fill_nan(p.out, p.out_stride, p.batch, p.len_q, p.heads, p.dim);
+            const int64_t rows = static_cast<int64_t>(p.batch) * p.heads * p.len_q;
+            for (int64_t i = threadIdx.x; i < rows; i += 256) p.lse[i] = __int_as_float(0x7FFFFFFF);
+        }
+    }
     if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
 }
 
@@ -587,7 +605,8 @@ struct BwdCommon {
     DqBars dq;
     DkvBars dkv;
     uint64_t landed;
-    uint32_t tmem, gave_up;
+    uint32_t tmem;
+    Patience waits;
 };
 constexpr uint32_t QUEUE_READERS = 4 + 8;       // the four warps of the third group, the eight that compute
 
@@ -713,7 +732,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
         bar_init(&cm.dq.s_taken, 4), bar_init(&cm.dq.dp_taken, 4), bar_init(&cm.dq.sums_full, 1), bar_init(&cm.dq.sums_taken, 8);
         bar_init(&cm.dkv.s_taken, Dkv::TURNS ? 4 : 8), bar_init(&cm.dkv.dp_taken, 4), bar_init(&cm.dkv.sums_full, 1), bar_init(&cm.dkv.sums_taken, 8);
         bar_init(&cm.landed, 1);
-        cm.gave_up = 0;
+        cm.waits = {p.wait_ns, 0};
     }
     if (threadIdx.x < TILE && first_block < key_items) {
         constexpr uint32_t ONE = 0x3F80;                 // bf16
@@ -727,15 +746,15 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = cm.tmem;
-    volatile uint32_t *gave_up = &cm.gave_up;
+    volatile Patience *waits = &cm.waits;
     after_previous();                           // k_attn_stats
 
     int block = first_block;                    // every role goes through the same items
     uint32_t items = 0, landed_phase = 0;       // answers read
     bool ok = true;
     const bool no_key_tile = SPLIT && first_block >= key_items;
-    auto next = [&] { block = queue_next<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
-    auto next_one = [&] { block = queue_next_one<true>(cm.queue, items++, gave_up), ok = ok && block >= 0; };
+    auto next = [&] { block = queue_next<true>(cm.queue, items++, waits), ok = ok && block >= 0; };
+    auto next_one = [&] { block = queue_next_one<true>(cm.queue, items++, waits), ok = ok && block >= 0; };
     auto all_done = [&](const bool joins) {     // of the key tiles, in all roles
         fence_async_smem();
         tmem_fence_before();
@@ -751,10 +770,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             cluster_sync();                     // the others have read what is here
         }
         tmem_fence_after();
-        if (*gave_up) ok = false;
+        if (waits->gave_up) ok = false;
     };
     auto ask = [&] {                            // once to an item, by the warp that brings the tiles
-        if (!bar_wait(&cm.queue.free[items % QUEUE], (items / QUEUE + 1) & 1, gave_up)) return false;
+        if (!bar_wait(&cm.queue.free[items % QUEUE], (items / QUEUE + 1) & 1, waits)) return false;
         if (lane == 0) queue_count(cm.queue, items, p.next_item, SPLIT ? key_items : gridDim.x, all_items);
         __syncwarp();
         return true;
@@ -770,9 +789,9 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             if (no_key_tile) next_one();
             auto dprobs = [&](uint32_t g, uint32_t set) {
                 const uint32_t qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
-                if (!bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up)) return false;        // delta comes with the queries
-                if (!bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, gave_up)) return false;
-                if (Dkv::TURNS && g > 0 && !bar_wait_one(&bars.dp_taken, (g - 1) & 1, gave_up)) return false;
+                if (!bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits)) return false;        // delta comes with the queries
+                if (!bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, waits)) return false;
+                if (Dkv::TURNS && g > 0 && !bar_wait_one(&bars.dp_taken, (g - 1) & 1, waits)) return false;
                 tmem_fence_after();
                 product_short<TILE>(tmem + Dkv::DP, ones, terms_at + qs * TILE * 16, zeros);
                 product_rows<DH, TILE>(tmem + Dkv::DP, v_at + set * TILE_BYTES, do_at + ds * TILE_BYTES, true);
@@ -783,8 +802,8 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const KeyItem it(p, block);
                 const uint32_t set = sets % Dkv::SETS;
                 if (it.n > 0 && (sums || Dkv::TURNS)) {
-                    ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up);
-                    if (sums && sets > 0 && ok) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
+                    ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, waits);
+                    if (sums && sets > 0 && ok) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, waits);      // the last item's sums have been read
                     ++sets;
                 }
                 if (!sums) {
@@ -793,12 +812,12 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 } else if (Dkv::TURNS) {
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS, w = g & 1;
-                        ok = bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, gave_up) && bar_wait_one(&bars.p_ready[w], g / 2 & 1, gave_up);
+                        ok = bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, waits) && bar_wait_one(&bars.p_ready[w], g / 2 & 1, waits);
                         if (!ok) break;
                         tmem_fence_after();
                         product_down<DH, TILE>(tmem + Dkv::DV, tmem + Dkv::MINE + w * 64, do_at + ds * TILE_BYTES, i > 0);
                         mma_commit(&bars.dv_done[w]);
-                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up) && bar_wait_one(&bars.ds_ready[w], g / 2 & 1, gave_up);
+                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits) && bar_wait_one(&bars.ds_ready[w], g / 2 & 1, waits);
                         if (!ok) break;
                         tmem_fence_after();
                         product_down<DH, TILE>(tmem + Dkv::DK, tmem + Dkv::MINE + w * 64, q_at + qs * TILE_BYTES, i > 0);
@@ -811,7 +830,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
                         for (int w = 0; w < 2 && ok; ++w) {     // each group's 64 queries; dK first: there is room for two query tiles only
-                            ok = bar_wait_one(&bars.ds_ready[w], g & 1, gave_up);
+                            ok = bar_wait_one(&bars.ds_ready[w], g & 1, waits);
                             if (!ok) break;
                             tmem_fence_after();
                             product_down<DH, 64>(tmem + Dkv::DK, tmem + Dkv::DP + w * 64 + 32, q_at + qs * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
@@ -822,7 +841,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         mma_commit(&bars.do_free[ds]);
                         // dP takes the place of P and dS, which products with other sums still read: nothing but
                         // their end (the same that frees dO's place) orders the two.
-                        if (i + 1 < it.n) ok = bar_wait_one(&bars.do_free[ds], g / Dkv::DO_SLOTS & 1, gave_up) && dprobs(g + 1, set);
+                        if (i + 1 < it.n) ok = bar_wait_one(&bars.do_free[ds], g / Dkv::DO_SLOTS & 1, waits) && dprobs(g + 1, set);
                     }
                 }
                 if (sums && it.n > 0 && ok) {
@@ -846,10 +865,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             while (ok) {
                 const DqItem it(p, block - key_items);
                 const uint32_t set = sets % Dq::SETS;
-                if (it.n > 0) ok = bar_wait_one(&bars.q_full[set], sets / Dq::SETS & 1, gave_up), ++sets;
+                if (it.n > 0) ok = bar_wait_one(&bars.q_full[set], sets / Dq::SETS & 1, waits), ++sets;
                 for (int j = 0; ok && j < it.n; ++j) {
                     const uint32_t g = tiles_in + j, slot = g % slots;
-                    ok = bar_wait_one(&full[slot], g / slots & 1, gave_up) && (g == 0 || bar_wait_one(taken, (g - 1) & 1, gave_up));
+                    ok = bar_wait_one(&full[slot], g / slots & 1, waits) && (g == 0 || bar_wait_one(taken, (g - 1) & 1, waits));
                     if (!ok) break;
                     tmem_fence_after();
                     product_rows<DH, TILE>(tmem + (is_dp ? TILE : 0), a_at + set * TILE_BYTES, b_at + slot * TILE_BYTES);
@@ -878,7 +897,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const Seq seq(p, it.b);
                 if (it.n > 0) {
                     const uint32_t set = sets % Dkv::SETS;
-                    if (!(ok = bar_wait(&bars.kv_free[set], (sets / Dkv::SETS + 1) & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.kv_free[set], (sets / Dkv::SETS + 1) & 1, waits))) break;
                     ++sets;
                     if (lane == 0) {
                         bar_expect(&bars.kv_full[set], 2 * TILE_BYTES);
@@ -891,16 +910,16 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
                         const int h = it.h_kv * it.shared + (it.from + i) / it.per_head, tile = it.first + (it.from + i) % it.per_head;
-                        if (!(ok = bar_wait(&bars.q_free[qs], (g / Dkv::Q_SLOTS + 1) & 1, gave_up))) break;
+                        if (!(ok = bar_wait(&bars.q_free[qs], (g / Dkv::Q_SLOTS + 1) & 1, waits))) break;
                         // the terms arrive at the queries' barrier: their bytes are announced without an arrival
                         if (lane == 0) {
                             asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(&bars.q_full[qs])), "r"(static_cast<uint32_t>(sizeof(sm.dkv.terms[0]))) : "memory");
                             copy_bytes(smem_addr(sm.dkv.terms[qs]), p.stats[(static_cast<int64_t>(it.b) * p.heads + h) * p.tiles_q + tile].terms, sizeof(sm.dkv.terms[0]), &bars.q_full[qs]);
                         }
                         __syncwarp();
-                        ok = load_tile<DH, true>(smem_addr(sm.dkv.q[qs]), sm.dkv.q[qs], &map_q, &bars.q_full[qs], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, gave_up) &&
-                             bar_wait(&bars.do_free[ds], (g / Dkv::DO_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dkv.dout[ds]), sm.dkv.dout[ds], &map_do, &bars.do_full[ds], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, gave_up);
+                        ok = load_tile<DH, true>(smem_addr(sm.dkv.q[qs]), sm.dkv.q[qs], &map_q, &bars.q_full[qs], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, waits) &&
+                             bar_wait(&bars.do_free[ds], (g / Dkv::DO_SLOTS + 1) & 1, waits) &&
+                             load_tile<DH, true>(smem_addr(sm.dkv.dout[ds]), sm.dkv.dout[ds], &map_do, &bars.do_full[ds], &cm.landed, landed_phase, tile * TILE, seq.n, p.len_q, h, it.b, waits);
                     }
                     tiles_in += it.n;
                 }
@@ -919,7 +938,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const Seq seq(p, it.b);
                 if (it.n > 0) {
                     const uint32_t set = sets % Dq::SETS;
-                    if (!(ok = bar_wait(&bars.q_free[set], (sets / Dq::SETS + 1) & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.q_free[set], (sets / Dq::SETS + 1) & 1, waits))) break;
                     ++sets;
                     if (lane == 0) {
                         bar_expect(&bars.q_full[set], 2 * TILE_BYTES);
@@ -931,10 +950,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     __syncwarp();
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS, vs = g % Dq::V_SLOTS;
-                        ok = bar_wait(&bars.k_free[ks], (g / Dq::K_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up) &&
-                             bar_wait(&bars.v_free[vs], (g / Dq::V_SLOTS + 1) & 1, gave_up) &&
-                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, gave_up);
+                        ok = bar_wait(&bars.k_free[ks], (g / Dq::K_SLOTS + 1) & 1, waits) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.k[ks]), sm.dq.k[ks], &map_k, &bars.k_full[ks], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, waits) &&
+                             bar_wait(&bars.v_free[vs], (g / Dq::V_SLOTS + 1) & 1, waits) &&
+                             load_tile<DH, true>(smem_addr(sm.dq.v[vs]), sm.dq.v[vs], &map_v, &bars.v_full[vs], &cm.landed, landed_phase, j * TILE, seq.m, p.len_kv, it.h_kv, it.b, waits);
                     }
                     tiles_in += it.n;
                 }
@@ -952,10 +971,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 while (ok && block < key_items) {
                     const KeyItem it(p, block);
                     const uint32_t set = sets % Dkv::SETS;
-                    if (it.n > 0) ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, gave_up), ++sets;
+                    if (it.n > 0) ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, waits), ++sets;
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS;
-                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, gave_up) && (g == 0 || bar_wait_one(&bars.s_taken, (g - 1) & 1, gave_up));
+                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits) && (g == 0 || bar_wait_one(&bars.s_taken, (g - 1) & 1, waits));
                         if (!ok) break;
                         tmem_fence_after();
                         product_short<TILE>(tmem, ones, terms_at + qs * TILE * 16, zeros);
@@ -989,10 +1008,10 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 uint32_t sets = 0, tiles_in = 0;
                 while (ok) {
                     const DqItem it(p, block - key_items);
-                    if (it.n > 0 && sets > 0) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, gave_up);      // the last item's sums have been read
+                    if (it.n > 0 && sets > 0) ok = bar_wait_one(&bars.sums_taken, (sets - 1) & 1, waits);      // the last item's sums have been read
                     for (int j = 0; ok && j < it.n; ++j) {
                         const uint32_t g = tiles_in + j, ks = g % Dq::K_SLOTS;
-                        ok = bar_wait_one(&bars.k_full[ks], g / Dq::K_SLOTS & 1, gave_up) && bar_wait_one(&bars.ds_ready[g & 1], g / 2 & 1, gave_up);
+                        ok = bar_wait_one(&bars.k_full[ks], g / Dq::K_SLOTS & 1, waits) && bar_wait_one(&bars.ds_ready[g & 1], g / 2 & 1, waits);
                         if (!ok) break;
                         tmem_fence_after();
                         product_down<DH, TILE>(tmem + 3 * TILE, tmem + 2 * TILE + (g & 1) * 64, k_at + ks * TILE_BYTES, j > 0);
@@ -1034,7 +1053,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     const int row0 = (it.first + column) * TILE;
                     // columns before `hidden` do not see the key
                     const int hidden = seq.causal && row0 < it.key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
-                    if (!(ok = bar_wait(s_full, g / EVERY & 1, gave_up))) break;
+                    if (!(ok = bar_wait(s_full, g / EVERY & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
 #pragma unroll
@@ -1056,7 +1075,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     }
                     if constexpr (Dkv::TURNS) {
                         if (g > 1) {                         // its last dS has been used
-                            if (!(ok = bar_wait(&bars.dk_done[w], (g / 2 - 1) & 1, gave_up))) break;
+                            if (!(ok = bar_wait(&bars.dk_done[w], (g / 2 - 1) & 1, waits))) break;
                             tmem_fence_after();
                         }
                         tmem_store32(p_at, probs[0]);
@@ -1065,7 +1084,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         tmem_fence_before();
                         bar_arrive_warp(&bars.p_ready[w]);
                     }
-                    if (!(ok = bar_wait(dp_full, g / EVERY & 1, gave_up))) break;
+                    if (!(ok = bar_wait(dp_full, g / EVERY & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t d[2][32];
                     if constexpr (Dkv::TURNS) {
@@ -1083,7 +1102,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 #pragma unroll
                             for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), pair_of(d[q % 2], c)));
                         }
-                        if (!(ok = bar_wait(&bars.dv_done[w], g / 2 & 1, gave_up))) break;        // P has been used
+                        if (!(ok = bar_wait(&bars.dv_done[w], g / 2 & 1, waits))) break;        // P has been used
                         tmem_fence_after();
 #pragma unroll
                         for (int q = 0; q < 4; ++q) tmem_store16(ds_at + q * 16, packed[q]);
@@ -1104,7 +1123,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 if (!ok) break;
                 tiles_in += it.n;
                 if constexpr (SPLIT) {               // all products that read the tiles are done with the sums
-                    if (it.n > 0) ok = bar_wait(&bars.sums_full, 0, gave_up);
+                    if (it.n > 0) ok = bar_wait(&bars.sums_full, 0, waits);
                     tmem_fence_after();
 #pragma unroll
                     for (int c = 0; c < DH; c += 32) {
@@ -1120,7 +1139,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const int64_t *stride = w == 0 ? p.dv_stride : p.dk_stride;
                 __nv_bfloat16 *out = (w == 0 ? p.dv : p.dk) + it.b * stride[0] + key * stride[1] + it.h_kv * stride[2];
                 if (it.n > 0) {
-                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, waits))) break;
                     ++outputs;
                     tmem_fence_after();
 #pragma unroll
@@ -1161,7 +1180,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const float lse = stats.lse[in_tile], delta = stats.delta[in_tile];
                 for (int j = static_cast<int>((tiles_in + w) & 1); j < it.n; j += 2) {
                     const uint32_t g = tiles_in + j;
-                    if (!(ok = bar_wait(&bars.s_full[w], g / 2 & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.s_full[w], g / 2 & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t s[4][32];
 #pragma unroll
@@ -1180,7 +1199,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         const float2 x = fma2(pair_of(s[c / 32], c % 32), both(p.scale_log2), both(-lse));
                         s[c / 32][c % 32] = __float_as_uint(exp2_fast(x.x)), s[c / 32][c % 32 + 1] = __float_as_uint(exp2_fast(x.y));
                     }
-                    if (!(ok = bar_wait(&bars.dp_full[w], g / 2 & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.dp_full[w], g / 2 & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t d[2][32], packed[4][16];
                     tmem_load32(dp_at, d[0]);
@@ -1197,7 +1216,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         for (int c = 0; c < 32; c += 2) packed[q][c / 2] = pack_bf16(mul2(pair_of(s[q], c), add2(pair_of(d[q % 2], c), both(-delta))));
                     }
                     if (g > 1) {                         // its last dS has been used
-                        if (!(ok = bar_wait(&bars.dq_done[w], (g / 2 - 1) & 1, gave_up))) break;
+                        if (!(ok = bar_wait(&bars.dq_done[w], (g / 2 - 1) & 1, waits))) break;
                         tmem_fence_after();
                     }
 #pragma unroll
@@ -1210,7 +1229,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 tiles_in += it.n;
                 __nv_bfloat16 *out = p.out + it.b * p.out_stride[0] + row * p.out_stride[1] + it.h * p.out_stride[2];
                 if (it.n > 0) {
-                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, gave_up))) break;
+                    if (!(ok = bar_wait(&bars.sums_full, outputs & 1, waits))) break;
                     ++outputs;
                     tmem_fence_after();
                     uint32_t o[DH / 64][32];                 // a group writes half of the columns
@@ -1235,7 +1254,14 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
     }
     tmem_fence_before();
     __syncthreads();
-    settle(gave_up);
+    if (waits->gave_up) {
+        settle();
+        if (warp < 8) {
+            fill_nan(p.out, p.out_stride, p.batch, p.len_q, p.heads, p.dim);
+            fill_nan(p.dk, p.dk_stride, p.batch, p.len_kv, p.heads_kv, p.dim);
+            fill_nan(p.dv, p.dv_stride, p.batch, p.len_kv, p.heads_kv, p.dim);
+        }
+    }
     if (warp == WARP_SCORES) tmem_free(tmem, TMEM_COLUMNS);
 }
 
@@ -1293,6 +1319,8 @@ int check_heads(const char *what, const void *at, const int64_t *stride, int bat
     return KT_OK;
 }
 
+std::atomic<int64_t> wait_limit{2000000000};
+
 int fill(const kt_attn *a, AttnParams *p) {
     if (a == nullptr) return fail(KT_ERR_INVALID, "the description is NULL");
     if (a->dtype != KT_BF16) return fail(KT_ERR_INVALID, "attention takes KT_BF16 heads");
@@ -1303,7 +1331,7 @@ int fill(const kt_attn *a, AttnParams *p) {
     if (a->len_q > (1 << 30) || a->len_kv > (1 << 30)) return fail(KT_ERR_SHAPE, "more than 2^30 tokens");
     *p = AttnParams{};
     p->batch = a->batch, p->heads = a->heads, p->heads_kv = a->heads_kv, p->len_q = a->len_q, p->len_kv = a->len_kv, p->dim = a->head_dim;
-    p->causal = a->causal != 0, p->used_q = a->used_q, p->used_kv = a->used_kv, p->scale = a->scale, p->scale_log2 = a->scale * LOG2E;
+    p->causal = a->causal != 0, p->used_q = a->used_q, p->used_kv = a->used_kv, p->scale = a->scale, p->scale_log2 = a->scale * LOG2E, p->wait_ns = static_cast<uint64_t>(wait_limit.load(std::memory_order_relaxed));
     p->tiles_q = (p->len_q + TILE - 1) / TILE, p->tiles_kv = (p->len_kv + TILE - 1) / TILE;
     if (static_cast<int64_t>(p->batch) * p->heads * (p->tiles_q > p->tiles_kv ? p->tiles_q : p->tiles_kv) > INT64_C(1) << 27)
         return fail(KT_ERR_SHAPE, "batch x heads x tokens is too large");
@@ -1509,6 +1537,12 @@ int kt_attn_backward(const kt_attn *a, const void *dout, const int64_t *dout_str
     copy_strides(p.dk_stride, dk_stride);
     copy_strides(p.dv_stride, dv_stride);
     return p.dim <= 64 ? start_backward<64>(m, p, st) : start_backward<128>(m, p, st);
+}
+
+int kt_attn_wait_limit(int64_t nanoseconds) {
+    if (nanoseconds < 0 || nanoseconds > INT64_C(60000000000)) return fail(KT_ERR_INVALID, "a limit of %lld ns: 0 to 60 s expected", (long long)nanoseconds);
+    wait_limit.store(nanoseconds, std::memory_order_relaxed);
+    return KT_OK;
 }
 
 int kt_attn_given_up(int64_t *count) {

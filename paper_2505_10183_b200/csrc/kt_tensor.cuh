@@ -16,10 +16,15 @@ namespace {
 
 constexpr int TILE = 128;                       // rows of a tile: the M and N of the matrix instruction
 constexpr uint32_t CHUNK = TILE * 128;          // bytes of 128 rows of 64 bf16
-constexpr uint64_t WAIT_NS = 2000000000;        // a wait gives up after this long
 
-// Waits that gave up since the library was loaded; a kernel that counts here ends without a result.
+// Waits that gave up since the library was loaded; the results of a kernel that counts here are not valid.
 __device__ unsigned long long g_waits_given_up;
+
+// A CTA's waits: how long one may last, and whether one has given up.
+struct Patience {
+    uint64_t limit_ns;
+    uint32_t gave_up;
+};
 
 __device__ __forceinline__ uint32_t smem_addr(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
@@ -37,6 +42,18 @@ __device__ __forceinline__ void bar_arrive_warp(uint64_t *bar) {
 }
 __device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+// Whether the phase of that parity has ended: at once, and (bar_try) after a while, unless it ends before.
+__device__ __forceinline__ bool bar_test(uint64_t *bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return done != 0;
 }
 __device__ __forceinline__ bool bar_try(uint64_t *bar, uint32_t parity) {
     uint32_t done;
@@ -57,26 +74,27 @@ __device__ __forceinline__ uint64_t now_ns() {
 
 // Waits for the phase of that parity to end.  False when it gave up, or when another warp of the CTA did: the
 // caller then leaves its loop, and the kernel ends.  Called by one thread, or (bar_wait) by whole warps.
-__device__ __forceinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
+// With a limit of 0 whatever is not there at the first look is given up.
+__device__ __forceinline__ bool bar_wait_slow(uint64_t *bar, uint32_t parity, volatile Patience *waits) {
     const uint64_t start = now_ns();
-    for (uint32_t n = 1;; ++n) {
-        if (bar_try(bar, parity)) return true;
+    for (uint32_t n = 0;; ++n) {
         if (n % 16 == 0) {
-            if (*gave_up) return false;
-            if (now_ns() - start > WAIT_NS) {
-                *gave_up = 1;
+            if (waits->gave_up) return false;
+            if (now_ns() - start >= waits->limit_ns) {
+                waits->gave_up = 1;
                 atomicAdd(&g_waits_given_up, 1ull);
                 return false;
             }
         }
+        if (bar_try(bar, parity)) return true;
     }
 }
-__device__ __forceinline__ bool bar_wait_one(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
-    return bar_try(bar, parity) || bar_wait_slow(bar, parity, gave_up);
+__device__ __forceinline__ bool bar_wait_one(uint64_t *bar, uint32_t parity, volatile Patience *waits) {
+    return bar_test(bar, parity) || bar_wait_slow(bar, parity, waits);
 }
-__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile uint32_t *gave_up) {
-    bool ok = bar_try(bar, parity);
-    if (!ok) ok = bar_wait_slow(bar, parity, gave_up);
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity, volatile Patience *waits) {
+    bool ok = bar_test(bar, parity);
+    if (!ok) ok = bar_wait_slow(bar, parity, waits);
     return __all_sync(0xFFFFFFFFu, ok);
 }
 
@@ -147,15 +165,15 @@ __device__ __forceinline__ void queue_count(Queue &q, uint32_t k, unsigned *coun
 }
 // For roles of one thread, and of a whole warp.
 template <bool COUNTED>
-__device__ __forceinline__ int queue_next_one(Queue &q, uint32_t k, volatile uint32_t *gave_up) {
-    if (!bar_wait_one(&q.full[k % QUEUE], k / QUEUE & 1, gave_up)) return -1;
+__device__ __forceinline__ int queue_next_one(Queue &q, uint32_t k, volatile Patience *waits) {
+    if (!bar_wait_one(&q.full[k % QUEUE], k / QUEUE & 1, waits)) return -1;
     const int block = COUNTED ? static_cast<int>(q.answer[k % QUEUE].x) : queue_read(q, k);
     bar_arrive(&q.free[k % QUEUE]);
     return block;
 }
 template <bool COUNTED>
-__device__ __forceinline__ int queue_next(Queue &q, uint32_t k, volatile uint32_t *gave_up) {
-    if (!bar_wait(&q.full[k % QUEUE], k / QUEUE & 1, gave_up)) return -1;
+__device__ __forceinline__ int queue_next(Queue &q, uint32_t k, volatile Patience *waits) {
+    if (!bar_wait(&q.full[k % QUEUE], k / QUEUE & 1, waits)) return -1;
     const int block = COUNTED ? static_cast<int>(q.answer[k % QUEUE].x) : queue_read(q, k);
     bar_arrive_warp(&q.free[k % QUEUE]);
     return block;

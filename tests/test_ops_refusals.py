@@ -172,3 +172,11 @@ def test_attention_outputs_in_any_order_of_dimensions(kt):
     args = attention(kt)
     args[2] = torch.zeros(2 * 16 * 2 * 64, dtype=BF16).as_strided((2, 16, 2, 64), (16 * 64, 64, 8, 1))       # an input
     assert status(kt, kt.kt_attn_backward, *args) == kt.KT_ERR_CUDA
+
+
+def test_limits_of_a_wait(kt):
+    for limit in (-1, 60 * 10 ** 9 + 1):
+        with pytest.raises(kt.KtError) as e:
+            kt.kt_attn_wait_limit(limit)
+        assert e.value.status == kt.KT_ERR_INVALID
+    kt.kt_attn_wait_limit(2 * 10 ** 9)              # what it is at first
