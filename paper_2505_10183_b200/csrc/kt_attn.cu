@@ -1548,6 +1548,7 @@ int kt_attn_wait_limit(int64_t nanoseconds) {
 int kt_attn_given_up(int64_t *count) {
     if (count == nullptr) return fail(KT_ERR_INVALID, "count is NULL");
     unsigned long long n = 0;
+    KT_CUDA(cudaDeviceSynchronize());           // the copy alone waits for no stream that does not block
     KT_CUDA(cudaMemcpyFromSymbol(&n, g_waits_given_up, sizeof(n)));
     *count = static_cast<int64_t>(n);
     return KT_OK;

@@ -89,6 +89,23 @@ assert all(torch.equal(got[n], want[n]) for n in step.NAMES)
 print("done")
 """
 
+COUNT = START + """
+gen = torch.Generator().manual_seed(5)
+q = heads(1, 300, 4, 64)
+out, lse = buffer(1, 300, 4, 64), buffer(1, 4, 300, dtype=torch.float32)
+kt.kt_attn_forward(q, q, q, out, lse)
+assert kt.kt_attn_given_up() == 0
+kt.kt_attn_wait_limit(0)
+s = torch.cuda.Stream()
+with torch.cuda.stream(s):
+    torch.cuda._sleep(200 * 1000 * 1000)                    # the kernel starts a tenth of a second after the call has returned
+    kt.kt_attn_forward(q, q, q, out, lse)
+count = kt.kt_attn_given_up()
+torch.cuda.synchronize()
+assert count == kt.kt_attn_given_up() > 0, count
+print("done")
+"""
+
 
 def run(source):
     done = subprocess.run([sys.executable, "-c", source], cwd=ROOT, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
@@ -101,3 +118,7 @@ def test_results_that_are_not_right_are_nan():
 
 def test_a_step_whose_waits_gave_up_synchronises_nothing():
     run(STEP)
+
+
+def test_the_count_waits_for_every_stream():
+    run(COUNT)
