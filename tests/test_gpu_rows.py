@@ -358,3 +358,27 @@ def test_on_another_stream_and_recorded(kt):
     torch.cuda.synchronize()
     for got in (other, recorded):
         assert all(torch.equal(a, c) for a, c in zip(got[:8], want[:8]))
+
+
+@pytest.mark.parametrize("kept", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows", [300, 6000])
+def test_sums_over_many_wide_rows(kt, rows, dtype, kept):
+    """Rows of more than 8192 columns: dweight and dbias of one 2^24 and then ones, of which a sum that takes one row after the
+    other loses every one.  A column passes through 64 additions in a block of rows, one for each of its range's two
+    blocks, and 12 over the partial sums: 80 of them at most, each off by at most u32 of all terms."""
+    cols = 8200
+    dout = torch.ones(rows, cols, dtype=dtype, device="cuda")
+    dout[0] = 2.0 ** 24
+    ones = torch.ones(rows, device="cuda")
+    if kept:
+        codes, scales = checkpoint(kt, rows, cols)
+        source = {"codes": codes.fill_(1), "scales": scales.fill_(1.0)}
+    else:
+        source = {"x": torch.ones_like(dout), "mean": torch.zeros_like(ones)}
+    dx, dw, db = torch.empty_like(dout), torch.full((cols,), math.nan, device="cuda"), torch.full((cols,), math.nan, device="cuda")
+    work = torch.full((kt.kt_norm_workspace(rows, cols),), 255, dtype=torch.uint8, device="cuda")
+    kt.kt_norm_backward(dout, None, ones, dx, dw, db, work, **source)
+    want = 2.0 ** 24 + rows - 1
+    for got in (dw, db):
+        assert ((got.double() - want).abs() <= 80 * U32 * want).all()
