@@ -382,3 +382,38 @@ def test_sums_over_many_wide_rows(kt, rows, dtype, kept):
     want = 2.0 ** 24 + rows - 1
     for got in (dw, db):
         assert ((got.double() - want).abs() <= 80 * U32 * want).all()
+
+
+def test_gelu_of_fp32_rows(kt):
+    """fp32 rows get the normal tail T(a) = Phi(-a) to fp32 as well.
+
+    In units of u32: T comes from a reciprocal and a polynomial of nine terms (24 at most) and an exponential (4) of a^2 / 2,
+    whose three roundings are 1.5 a^2 of it: 32 + 2 a^2 of T; the density's share a phi is off by 8 + 2 a^2 of itself.
+    Below 1 in magnitude Phi is a polynomial in x^2 around 1/2, off by 3 in all.  Above 1, 1 - T is rounded once; below -1
+    nothing is: there the tolerance falls with the value."""
+    gen = torch.Generator().manual_seed(17)
+    x = torch.cat([torch.linspace(-12, 12, 24 * 1024 + 1), torch.randn(65535, generator=gen) * 2]).cuda().view(2, -1)
+    dout = torch.randn(x.shape, generator=gen).cuda()
+    out, dx = torch.empty_like(x), torch.empty_like(x)
+    kt.kt_act_forward(x, out, kind="gelu")
+    kt.kt_act_backward(dout, None, None, dx, "gelu", x=x)
+    X, D = x.double(), dout.double()
+    A = X.abs()
+
+    def normal(v):                                   # torch's ndtr is (1 + erf) / 2, which has no tail
+        return torch.special.erfc(-v / math.sqrt(2)) / 2
+
+    T, phi = normal(-A), torch.exp(-A * A / 2) / math.sqrt(2 * math.pi)
+    e_tail = T * (32 + 2 * A * A)
+    want = X * normal(X)
+    tol = U32 * (torch.where(A < 1, 4 * A, A * e_tail) + 2 * want.abs())
+    assert ((out.double() - want).abs() <= tol + 2.0 ** -126).all()
+    want = D * (normal(X) + X * phi)
+    tol = U32 * (D.abs() * (torch.where(A < 1, 4.0, torch.where(X > 0, 2.0, 0.0) + e_tail) + A * phi * (8 + 2 * A * A)) + 2 * want.abs())
+    assert ((dx.double() - want).abs() <= tol + D.abs() * 2.0 ** -120).all()
+    edge = torch.tensor([[0.0, -0.0, math.inf, -math.inf, math.nan, 3e38, -3e38, 1e-40]], device="cuda")
+    out, dx = torch.empty_like(edge), torch.empty_like(edge)
+    kt.kt_act_forward(edge, out, kind="gelu")
+    kt.kt_act_backward(torch.ones_like(edge), None, None, dx, "gelu", x=edge)
+    assert torch.equal(out[0, [0, 1, 2, 3, 5, 6]].abs(), torch.tensor([0.0, 0.0, math.inf, 0.0, 3e38, 0.0], device="cuda")) and torch.isnan(out[0, 4])
+    assert torch.equal(dx[0, [0, 1, 2, 3, 5, 6, 7]], torch.tensor([0.5, 0.5, 1.0, 0.0, 1.0, 0.0, 0.5], device="cuda")) and torch.isnan(dx[0, 4])
