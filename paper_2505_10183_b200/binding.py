@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import sys
 from dataclasses import dataclass
 from typing import List, Optional, Sequence, Union
 
@@ -676,10 +677,14 @@ def kt_sync_flat_static(group_of: Sequence[int], shares: Sequence[int], grads: S
 
 # ------------------------------------------------------------- operators of a training step
 # Their arguments are checked and passed on by a module of their own (csrc/kt_fast.cpp): a call costs about as
-# much as its launches.
+# much as its launches.  It is built against one torch, so it is loaded when the first of them is called: nothing
+# else here needs it.
 def _load_fast():
+    rebuild = "build it with `python -m paper_2505_10183_b200.build` (needs g++ and torch's headers)"
     if not os.path.exists(_build.FAST):
-        raise ImportError("%s is missing: build it with `python -m paper_2505_10183_b200.build`" % _build.FAST)
+        raise ImportError("%s is missing: %s" % (_build.FAST, rebuild))
+    if _build.fast_is_of_another():
+        raise ImportError("%s was built for another torch or Python than torch %s and %s: %s" % (_build.FAST, _build.torch_version(), sys.implementation.cache_tag, rebuild))
     from . import _fast
     names = ("kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_backward", "kt_act_forward", "kt_act_backward",
              "kt_attn_forward", "kt_attn_backward", "kt_last_error")
@@ -687,7 +692,14 @@ def _load_fast():
     return _fast
 
 
-_fast = _load_fast()
+class _LoadedOnUse:
+    def __getattr__(self, name):
+        global _fast
+        _fast = _load_fast()
+        return getattr(_fast, name)
+
+
+_fast = _LoadedOnUse()
 
 
 def kt_ckpt_pitch(cols: int) -> int:

@@ -1,7 +1,8 @@
 // kt_fast.cpp -- argument marshalling of the training operators (the functions of binding.py with the same names):
 // torch tensors in, one call of the C entry out.  A Python module of its own because their calls are short:
 // checking and converting the arguments in Python takes as long as the kernels of a small batch.  No
-// arithmetic, no state: the C entries' addresses are handed over by binding.py when it is imported.
+// arithmetic, no state: the C entries' addresses are handed over by binding.py, which loads the module when the first
+// operator is called.  KT_BELONGS (build.py) names the torch and Python whose binary interfaces it is built for.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/core/Tensor.h>
@@ -315,7 +316,7 @@ PyMethodDef methods[] = {{"bind", reinterpret_cast<PyCFunction>(reinterpret_cast
                          KT_METHOD(attn_forward, 10),
                          KT_METHOD(attn_backward, 15),
                          {nullptr, nullptr, 0, nullptr}};
-PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_fast", "Argument marshalling of the training operators.", -1, methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_fast", KT_BELONGS, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
