@@ -417,3 +417,46 @@ def test_gelu_of_fp32_rows(kt):
     kt.kt_act_backward(torch.ones_like(edge), None, None, dx, "gelu", x=edge)
     assert torch.equal(out[0, [0, 1, 2, 3, 5, 6]].abs(), torch.tensor([0.0, 0.0, math.inf, 0.0, 3e38, 0.0], device="cuda")) and torch.isnan(out[0, 4])
     assert torch.equal(dx[0, [0, 1, 2, 3, 5, 6, 7]], torch.tensor([0.5, 0.5, 1.0, 0.0, 1.0, 0.0, 0.5], device="cuda")) and torch.isnan(dx[0, 4])
+
+
+@pytest.mark.parametrize("layout", ["plain", "odd"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cols,group", [(72, 32), (250, 32), (500, 32), (1000, 64), (1500, 96), (2000, 128), (2500, 160), (3000, 192), (4000, 256), (5000, 320),
+                                        (6000, 384), (8000, 512)])
+def test_norm_with_rows_ahead(kt, cols, group, dtype, layout):
+    """At least six rows to every group of threads (of which an SM holds 768 / group): the places of the rows that are copied ahead, three or
+    four of them, are filled a second time, and all of it is compared."""
+    test_norm(kt, 6 * 148 * (768 // group), cols, dtype, F32, layout)
+
+
+def in_parts(kt, call, rows, cols, dtype, parts):
+    """What `call` makes of a matrix in one call and in several calls on parts of its rows: the same bits."""
+    gen = torch.Generator("cuda").manual_seed(rows + cols)
+    x = torch.randn(rows, cols, generator=gen, dtype=dtype, device="cuda")
+    got = []
+    for pieces in (1, parts):
+        out = [torch.full_like(x, math.nan), *checkpoint(kt, rows, cols), torch.full_like(x, math.nan)]
+        for k in range(pieces):
+            mine = slice(rows * k // pieces, rows * (k + 1) // pieces)
+            call(x[mine], *(o[mine] for o in out))
+        got.append(out)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert not torch.isnan(got[0][0]).any() and not torch.isnan(got[0][3]).any()
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [(BF16, 1030, 1 << 17), (BF16, (1 << 26) + 3, 8), (BF16, (1 << 26) + 3, 1), (F32, (1 << 25) + 3, 4)])
+def test_activations_in_more_than_one_piece(kt, dtype, rows, cols):
+    """Sizes that one call goes through in two pieces: 2^27 elements of a gapless matrix, 2^30 vectors (of rows padded to whole
+    blocks) of another, by vectors and by elements."""
+    def call(x, out, codes, scales, dx):
+        kt.kt_act_forward(x, out, codes, scales, "gelu")
+        kt.kt_act_backward(x, codes, scales, dx, "gelu")
+
+    in_parts(kt, call, rows, cols, dtype, 5)
+
+    def restore(x, out, codes, scales, dx):
+        kt.kt_ckpt_store(x, codes, scales)
+        kt.kt_ckpt_restore(codes, scales, out)
+        kt.kt_act_backward(x, None, None, dx, "silu", x=x)
+
+    in_parts(kt, restore, rows, cols, dtype, 5)
