@@ -637,15 +637,19 @@ struct DqItem {
 //   Heads of up to 64: the groups of four warps take tiles in turn.  Tensor memory: scores 0, dP 128, a
 //   place of each group for P and then, once that is used, dS 256 and 320, sums 384 and 448.
 //   Heads of up to 128, whose sums fill half of tensor memory: both groups work on one tile, 64 queries each.
-//   Scores 0, dP 128, which P and dS then take, sums 256 and 384.  The next scores are formed meanwhile,
-//   and exponentials taken while the products with P and dS run; only dP is waited for.
+//   A tile has a place, 0 or 128 in turn, that its scores, then dP, then P and dS take; sums 256 and 384.  Exponentials are
+//   taken while the products with the last tile's P and dS run; only dP is waited for.  (The next tile but one gets
+//   the place when these products have ended, which nothing else would order.  With one place for the dP of all
+//   tiles every tile waited for that end: 2048 tokens causal, 8 heads of 128 on 1, in 72 us, now 67.)
 // (Steps of 64 queries would leave room for turns there too, but a product of fewer than 128 columns takes
 // as long as one of 128.)
 template <int DH>
 struct DkvTiles {
     static constexpr uint32_t TILE_BYTES = DH / 64 * CHUNK;
     static constexpr bool TURNS = DH == 64;
-    static constexpr uint32_t DP = TILE, MINE = 2 * TILE, DV = TURNS ? 384 : 256, DK = DV + DH;
+    static constexpr uint32_t MINE = 2 * TILE, DV = TURNS ? 384 : 256, DK = DV + DH;
+    __device__ static uint32_t scores(uint32_t g) { return TURNS ? 0 : (g & 1) * TILE; }            // of the g-th query tile
+    __device__ static uint32_t dprobs(uint32_t g) { return TURNS ? TILE : (g & 1) * TILE; }
     static constexpr int SETS = TURNS ? 2 : 1, Q_SLOTS = TURNS ? 4 : 2, DO_SLOTS = TURNS ? 3 : 2;
     alignas(1024) uint8_t k[SETS][TILE_BYTES], v[SETS][TILE_BYTES], q[Q_SLOTS][TILE_BYTES], dout[DO_SLOTS][TILE_BYTES];
     alignas(128) uint4 ones_lse[TILE], ones_delta[TILE], terms[Q_SLOTS][TILE], zeros[TILE];      // zeros come last: product_short
@@ -791,11 +795,12 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 const uint32_t qs = g % Dkv::Q_SLOTS, ds = g % Dkv::DO_SLOTS;
                 if (!bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits)) return false;        // delta comes with the queries
                 if (!bar_wait_one(&bars.do_full[ds], g / Dkv::DO_SLOTS & 1, waits)) return false;
+                if (!Dkv::TURNS && !bar_wait_one(&bars.s_taken, g & 1, waits)) return false;
                 if (Dkv::TURNS && g > 0 && !bar_wait_one(&bars.dp_taken, (g - 1) & 1, waits)) return false;
                 tmem_fence_after();
-                product_short<TILE>(tmem + Dkv::DP, ones, terms_at + qs * TILE * 16, zeros);
-                product_rows<DH, TILE>(tmem + Dkv::DP, v_at + set * TILE_BYTES, do_at + ds * TILE_BYTES, true);
-                mma_commit(&bars.dp_full[Dkv::TURNS ? g & 1 : 0]);
+                product_short<TILE>(tmem + Dkv::dprobs(g), ones, terms_at + qs * TILE * 16, zeros);
+                product_rows<DH, TILE>(tmem + Dkv::dprobs(g), v_at + set * TILE_BYTES, do_at + ds * TILE_BYTES, true);
+                mma_commit(&bars.dp_full[g & 1]);
                 return true;
             };
             while (ok && block < key_items) {
@@ -833,15 +838,13 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                             ok = bar_wait_one(&bars.ds_ready[w], g & 1, waits);
                             if (!ok) break;
                             tmem_fence_after();
-                            product_down<DH, 64>(tmem + Dkv::DK, tmem + Dkv::DP + w * 64 + 32, q_at + qs * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
+                            product_down<DH, 64>(tmem + Dkv::DK, tmem + Dkv::dprobs(g) + w * 64 + 32, q_at + qs * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
                         }
                         if (!ok) break;
                         mma_commit(&bars.q_free[qs]);
-                        for (int w = 0; w < 2; ++w) product_down<DH, 64>(tmem + Dkv::DV, tmem + Dkv::DP + w * 64, do_at + ds * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
+                        for (int w = 0; w < 2; ++w) product_down<DH, 64>(tmem + Dkv::DV, tmem + Dkv::dprobs(g) + w * 64, do_at + ds * TILE_BYTES + w * 64 * 128, i > 0 || w > 0);
                         mma_commit(&bars.do_free[ds]);
-                        // dP takes the place of P and dS, which products with other sums still read: nothing but
-                        // their end (the same that frees dO's place) orders the two.
-                        if (i + 1 < it.n) ok = bar_wait_one(&bars.do_free[ds], g / Dkv::DO_SLOTS & 1, waits) && dprobs(g + 1, set);
+                        if (i + 1 < it.n) ok = dprobs(g + 1, set);
                     }
                 }
                 if (sums && it.n > 0 && ok) {
@@ -974,12 +977,15 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                     if (it.n > 0) ok = bar_wait_one(&bars.kv_full[set], sets / Dkv::SETS & 1, waits), ++sets;
                     for (int i = 0; ok && i < it.n; ++i) {
                         const uint32_t g = tiles_in + i, qs = g % Dkv::Q_SLOTS;
-                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits) && (g == 0 || bar_wait_one(&bars.s_taken, (g - 1) & 1, waits));
+                        ok = bar_wait_one(&bars.q_full[qs], g / Dkv::Q_SLOTS & 1, waits);
+                        if (Dkv::TURNS && g > 0) ok = ok && bar_wait_one(&bars.s_taken, (g - 1) & 1, waits);
+                        // the products that read P and dS of tile g - 2 have ended
+                        if (!Dkv::TURNS && g > 1) ok = ok && bar_wait_one(&bars.do_free[(g - 2) % Dkv::DO_SLOTS], (g - 2) / Dkv::DO_SLOTS & 1, waits);
                         if (!ok) break;
                         tmem_fence_after();
-                        product_short<TILE>(tmem, ones, terms_at + qs * TILE * 16, zeros);
-                        product_rows<DH, TILE>(tmem, k_at + set * TILE_BYTES, q_at + qs * TILE_BYTES, true);
-                        mma_commit(&bars.s_full[Dkv::TURNS ? g & 1 : 0]);
+                        product_short<TILE>(tmem + Dkv::scores(g), ones, terms_at + qs * TILE * 16, zeros);
+                        product_rows<DH, TILE>(tmem + Dkv::scores(g), k_at + set * TILE_BYTES, q_at + qs * TILE_BYTES, true);
+                        mma_commit(&bars.s_full[g & 1]);
                     }
                     tiles_in += it.n;
                     if (ok) next_one();
@@ -1035,11 +1041,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
             DkvBars &bars = cm.dkv;
             constexpr int WIDTH = Dkv::TURNS ? TILE : TILE / 2, EVERY = Dkv::TURNS ? 2 : 1;      // columns of a tile that a group takes, of every EVERYth tile
             const int w = warp / 4, col0 = Dkv::TURNS ? 0 : w * WIDTH;
-            const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16), s_at = lanes + col0, dp_at = lanes + Dkv::DP + col0;
-            // A group that takes turns has barriers of its own: one that is waited for only every other time would
-            // tell its phases apart by nothing.
-            uint64_t *const s_full = &bars.s_full[Dkv::TURNS ? w : 0], *const dp_full = &bars.dp_full[Dkv::TURNS ? w : 0];
-            const uint32_t p_at = Dkv::TURNS ? lanes + Dkv::MINE + w * 64 : dp_at, ds_at = Dkv::TURNS ? p_at : dp_at + 32;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
             uint32_t tiles_in = 0, outputs = 0;
             if (no_key_tile) next();
             while (ok && block < key_items) {
@@ -1049,11 +1051,16 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                 int i = Dkv::TURNS ? static_cast<int>((tiles_in + w) & 1) : 0, column = it.from + i;             // query tile of its head
                 for (; i < it.n; i += EVERY, column += EVERY) {
                     const uint32_t g = tiles_in + i;
+                    // Tiles in turn have barriers in turn: a group that waited for one of them only every other time would
+                    // tell its phases apart by nothing.
+                    uint64_t *const s_full = &bars.s_full[g & 1], *const dp_full = &bars.dp_full[g & 1];
+                    const uint32_t s_at = lanes + Dkv::scores(g) + col0, dp_at = lanes + Dkv::dprobs(g) + col0;
+                    const uint32_t p_at = Dkv::TURNS ? lanes + Dkv::MINE + w * 64 : dp_at, ds_at = Dkv::TURNS ? p_at : dp_at + 32;
                     while (column >= it.per_head) column -= it.per_head;
                     const int row0 = (it.first + column) * TILE;
                     // columns before `hidden` do not see the key
                     const int hidden = seq.causal && row0 < it.key0 + TILE - 1 - seq.shift ? key - seq.shift - row0 - col0 : 0;
-                    if (!(ok = bar_wait(s_full, g / EVERY & 1, waits))) break;
+                    if (!(ok = bar_wait(s_full, g / 2 & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t s[WIDTH / 32][32], probs[WIDTH / 64][32];
 #pragma unroll
@@ -1084,7 +1091,7 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
                         tmem_fence_before();
                         bar_arrive_warp(&bars.p_ready[w]);
                     }
-                    if (!(ok = bar_wait(dp_full, g / EVERY & 1, waits))) break;
+                    if (!(ok = bar_wait(dp_full, g / 2 & 1, waits))) break;
                     tmem_fence_after();
                     uint32_t d[2][32];
                     if constexpr (Dkv::TURNS) {
@@ -1405,7 +1412,7 @@ int start_forward(const CUtensorMap (&m)[3], AttnParams &p, cudaStream_t st) {
 //   2048 causal, 8 heads of 128 on 1           185   125    85    67      (16 key tiles, 128 steps the longest)
 //   4 x 700 causal, 8 heads of 128 on 1         91    60    47            (24, 48 steps)
 //   4096 queries on 77 keys, 8 heads of 64      48    34    28    26      (8, 32 steps)
-//   2 x 578 causal, 4 heads of 64 on 2          20    24    26            (20, 10 steps)
+//   2 x 578 causal, 4 heads of 64 on 2          20    19    25            (20, 10 steps)
 int parts_of_keys(const AttnParams &p) {
     const int64_t all = static_cast<int64_t>(p.batch) * p.heads_kv, key_tiles = all * p.tiles_kv, gap = p.len_kv - p.len_q;
     if (key_tiles * 2 > SMS) return 1;
