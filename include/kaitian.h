@@ -563,7 +563,9 @@ void kt_graph_destroy(kt_graph *graph);
  * paper trains a network with a stock framework; these calls are this library's own.)
  *
  * They need no context: they run on the device that is current in the calling thread, on
- * `stream`, and touch nothing but their arguments.  All pointers are device pointers.  Matrices are
+ * `stream`, and change nothing but their outputs and workspaces.  (Rows of KT_BF16 that do not start at multiples
+ * of 16 bytes are read in the aligned 16-byte pieces that hold them: up to 14 bytes before and behind
+ * a matrix are read as well, whatever they hold.)  All pointers are device pointers.  Matrices are
  * rows x cols with a row stride in elements (columns contiguous); any element-aligned address,
  * stride and width is accepted, 128-bit accesses are used where addresses and strides are
  * multiples of 16 bytes and rows hold whole vectors.  `dtype` is the activations' type (KT_F32 or

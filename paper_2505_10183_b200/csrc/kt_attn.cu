@@ -588,7 +588,7 @@ __global__ void __launch_bounds__(256) k_attn_stats(const AttnParams p) {
 // it is handed its first query tile.  Barriers of both kinds are made at the start, and their phases are
 // counted on from item to item: the next item's tiles are fetched and its first products formed
 // while the last one's sums are written.
-// 8192 tokens causal, 16 heads of 128 on 4: 707 us, 970 TFLOP/s by the formulas' five products, 1360 by the seven that are
+// 8192 tokens causal, 16 heads of 128 on 4: 718 us, 955 TFLOP/s by the formulas' five products, 1335 by the seven that are
 // formed, at the power limit.  8 x 1024 causal, 16 heads of 64: 134 us; there a product of 64 columns costs as much as one
 // of 128, and the two groups' exponentials and the ends of items take the rest.
 struct DqBars {

@@ -3,9 +3,10 @@
 // weight's and the bias' gradient over all rows), GELU / SiLU forward and backward, and the 8-bit
 // checkpoints that both can leave for the backward pass.  Contracts: include/kaitian.h.
 //
-// All of it is bound by memory: a row is read once with 128-bit loads, stays in registers as fp32
+// Memory sets the floor of all of it: a row is read once with 128-bit loads, stays in registers as fp32
 // for its statistics and its result, and is written once.  Rows whose address or width does not
-// allow 128-bit accesses take the same kernels with element accesses (template argument WIDE).
+// allow 128-bit accesses take the same kernels with narrower accesses (template argument WIDE), rows
+// of layer norm above ROW_MAX columns kernels of their own; instructions bound these, and layer norm with checkpoints.
 //
 // 8-bit checkpoints.  A block of KT_CKPT_BLOCK = 128 columns of a row shares one fp32 scale:
 //   top = max |x|,  scale = top / 127,  code = rint(x * 127 / top) in -127 ... 127,
@@ -390,8 +391,8 @@ __device__ __forceinline__ uint4 take_vector(const uint4 *from, const T *row, in
 
 // y = (x - mean) rstd w + b.  A warp takes the mean of its part of the row and the squares around that
 // mean; the parts are joined with the exact formula for two samples, so that one barrier is enough
-// and nothing cancels.  Bound by memory: 16384 x 4096 bf16 in 52 us (5190 GB/s; a plain copy reaches 6530), 73 us with the
-// checkpoint; 64 x 512 in 2.7 us, a launch.
+// and nothing cancels.  Bound by memory: 16384 x 4096 bf16 in 53 us (5080 GB/s; a plain copy reaches 6530); with the
+// checkpoint by instructions (2.4 a cycle, DRAM at 43 % of its cycles): 73 us, 4600 GB/s.  64 x 512 in 2.8 us, a launch.
 template <typename T, bool WIDE, int GROUP, int NV>
 __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads(NV * Elems<T>::V) / norm_threads<GROUP>()) k_norm_forward(const NormParams p) {
     constexpr int V = Elems<T>::V, THREADS = norm_threads<GROUP>(), WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
@@ -527,8 +528,9 @@ __global__ void __launch_bounds__(norm_threads<GROUP>(), forward_threads(NV * El
 // are one cluster that joins its sums through distributed shared memory; else one row of partial
 // sums per CTA is reduced in a fixed order by k_norm_params: no atomics either way, so that a step gives the same bits
 // when it is run again.  (With a CTA to a group, four times as many partial sums: 47.6 instead of 38.6 us for
-// 16384 x 2048 bf16 from a checkpoint.)  Bound by memory where rows are many: 16384 x 4096 bf16 in 69 us (5830 GB/s), 16384 x
-// 2048 from a checkpoint in 38 (4440 GB/s); 4999 x 1000 fp32 in 16, some 4 of them the second kernel's.
+// 16384 x 2048 bf16 from a checkpoint.)  Bound by memory where rows are many: 16384 x 4096 bf16 in 69 us (5830 GB/s); from
+// a checkpoint by instructions (2.2 a cycle, DRAM 43 %): 16384 x 2048 in 38 us (4400 GB/s); 4999 x 1000 fp32 in 16, some 4 of
+// them the second kernel's.
 template <typename T, bool WIDE, int GROUP, int NV, bool KEPT>
 __global__ void __launch_bounds__(backward_threads<GROUP>(), 1) k_norm_backward(const NormParams p) {
     constexpr int V = Elems<T>::V, THREADS = backward_threads<GROUP>(), GROUPS = THREADS / GROUP, WARPS = GROUP / 32, AHEAD = rows_ahead<NV>();
@@ -989,7 +991,7 @@ __device__ __forceinline__ float2 slope(float2 x) {
 // The kernels on elements: U vectors to a thread, all loads before the first use, no shared memory; sixteen lanes (a warp,
 // fp32) hold a checkpoint's block, whose largest magnitude goes through shuffles.  Bound by memory, on 16384 x 8192 bf16: GELU
 // with checkpoint 120 us, its backward pass from the checkpoint 118 us (5715 GB/s), restore 68 us (5980 GB/s).
-// At odd addresses and widths shuffles and word accesses bound them: SiLU's backward pass on 16384 x 8191 bf16 takes 234 us.
+// At odd addresses and widths shuffles and word accesses bound them: SiLU's backward pass on 16384 x 8191 bf16 takes 221 us.
 enum { KIND_NONE = -1 };                  // a checkpoint alone
 
 template <typename T, int MODE, int KIND, bool KEEP>
