@@ -667,9 +667,75 @@ int kt_attn_backward(const kt_attn *desc, const void *dout, const int64_t *dout_
  * returned KT_OK, and its results (out and lse, or dq, dk and dv) are NaN wherever they are not right.
  * kt_attn_wait_limit sets the limit of the calls to come in this process, 0 to 60 s (with 0 all that is not there
  * at once is given up; KT_ERR_INVALID outside).  *count (host) = how many waits gave up since the library was
- * loaded on the current device (0 unless something is broken); waits for the device. */
+ * loaded on the current device (0 unless something is broken); waits for the device.
+ * The kernels of kt_xent_* and kt_orth_update wait in the same way, under the same limit; kt_waits_given_up counts theirs too. */
 int kt_attn_wait_limit(int64_t nanoseconds);
 int kt_attn_given_up(int64_t *count);
+int kt_waits_given_up(int64_t *count);
+
+/* Embedding: rows of a table, weight[vocab][cols] of `param_dtype`, for the tokens of a batch, out[tokens][cols] of
+ * `dtype` (KT_F32 or KT_BF16 each); ids (device, int64[tokens]).
+ * Forward: out_i = scale * weight[ids_i].  A negative id (padding) gives a row of zeros, one at or past
+ * vocab a row of NaN.
+ * Backward: dweight_v = [base_v +] scale * sum over the tokens with ids_i = v of dout_i; other ids have no part in it.  All
+ * of dweight is written.  base (or NULL) has dweight's type and may be dweight itself, with the same stride: the
+ * gradient is then added to what is there (of a table that is the output layer too, what kt_xent_backward left), and rows that
+ * no token has are not touched.  workspace (16-byte aligned) holds kt_embed_workspace bytes, which need no initial value and
+ * may be used again by the next call on the same stream.  Sums in fp32, in an order that the ids alone set.
+ * Rows at any element-aligned address and stride; those at multiples of 16 bytes are faster.  Outputs must not overlap
+ * inputs (base aside).  At most 2^30 tokens, 2^24 columns and a vocabulary of 2^24.
+ * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+int kt_embed_forward(const int64_t *ids, const void *weight, int64_t weight_stride, int param_dtype, void *out,
+                     int64_t out_stride, int64_t tokens, int64_t cols, int64_t vocab, int dtype, float scale,
+                     void *stream);
+int64_t kt_embed_workspace(int64_t tokens, int64_t cols, int64_t vocab);
+int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids, const void *base,
+                      int64_t base_stride, void *dweight, int64_t dweight_stride, int param_dtype,
+                      void *workspace, int64_t workspace_bytes, int64_t tokens, int64_t cols, int64_t vocab,
+                      int dtype, float scale, void *stream);
+
+/* Softmax cross entropy of hidden rows against the weights of a vocabulary, without keeping the logits.
+ * hidden[rows][dim] and weight[vocab][dim] are KT_BF16, as are their gradients; addresses are 16-byte aligned, row
+ * strides multiples of 8 elements, dim a multiple of 8 up to 2^16; at most 2^20 rows and a vocabulary of 2^24.
+ * targets (device, int64[rows]).  With logits l_iv = scale * hidden_i . weight_v:
+ *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, targets_i}      (fp32[rows])
+ * A row whose target is negative does not count: its loss, lse and gradients are zeros, and what hidden holds there does
+ * not matter.  A target at or past vocab makes the row's loss NaN, and its gradients, all of dweight among them.
+ * Backward, from lse as the forward pass wrote it and dloss (fp32[rows]), and dlse (fp32[rows] or NULL: zeros) where
+ * lse itself is part of the loss:
+ *   P_iv = scale ((dloss_i + dlse_i) exp(l_iv - lse_i) - dloss_i [v = targets_i]),  dhidden = P weight,  dweight = P^T hidden
+ * dhidden or dweight may be NULL (not both).  P is rounded to bf16, a piece of the vocabulary at a time; sums are fp32.
+ * workspace (16-byte aligned) holds kt_xent_workspace bytes (for the forward or the backward pass), which need no
+ * initial value and may be used again by the next call on the same stream.  No atomics: the same inputs give the same
+ * bits.  Outputs must not overlap inputs.  A wait that gives up (above) leaves NaN where results are not right.
+ * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+int kt_xent_forward(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                    const int64_t *targets, float *loss, float *lse, void *workspace,
+                    int64_t workspace_bytes, int64_t rows, int64_t dim, int64_t vocab, int dtype, float scale,
+                    void *stream);
+int64_t kt_xent_workspace(int64_t rows, int64_t dim, int64_t vocab, int backward);
+int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, int64_t hidden_stride,
+                     const void *weight, int64_t weight_stride, const int64_t *targets, const float *lse,
+                     void *dhidden, int64_t dhidden_stride, void *dweight, int64_t dweight_stride,
+                     void *workspace, int64_t workspace_bytes, int64_t rows, int64_t dim, int64_t vocab,
+                     int dtype, float scale, void *stream);
+
+/* A matrix-shaped update orthogonalised by Newton-Schulz products: with X = x / |x|_F, `steps` times
+ *   A = X X^T,  X <- (a I + b A + c A^2) X      (a, b, c = coefficients[3], host),
+ * then out = scale * X.  x is [batch][rows][cols] of KT_F32 or KT_BF16 and out KT_BF16; a stride array (host) holds the
+ * strides of matrix and row in elements, columns are contiguous, any element-aligned address.  Each matrix is on its own;
+ * one of zeros gives zeros, one with an infinity or a NaN gives NaN.  Whatever the size of x, results are the same
+ * but for rounding.  steps: 1 to 64; coefficients that would take a singular value above 1.9 are refused.  Products
+ * of fp16 (what is held between them has a known range) with fp32 sums: directions in which x has less than 2^-12 of
+ * |x|_F are those of roundings.  Up to 2^16 rows and columns, 2^15 matrices.
+ * workspace (16-byte aligned) holds kt_orth_workspace bytes, which need no initial value and may be used again by the
+ * next call on the same stream.  out must not overlap x, nor its own rows each other.  No atomics: the same inputs
+ * give the same bits.  A wait that gives up (above) leaves NaN where results are not right.
+ * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
+int64_t kt_orth_workspace(int64_t batch, int64_t rows, int64_t cols);
+int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out, const int64_t *out_stride,
+                   void *workspace, int64_t workspace_bytes, int64_t batch, int64_t rows, int64_t cols,
+                   int steps, const float *coefficients, float scale, void *stream);
 
 /* Number of kernels this context has launched so far (for launch accounting). */
 int64_t kt_launch_count(const kt_ctx *ctx);

@@ -37,7 +37,8 @@ EXPORTS = ["kt_schedule", "kt_scores", "kt_adapt_create", "kt_adapt_observe", "k
            "kt_ipc_export", "kt_ipc_open", "kt_ipc_close", "kt_host_register", "kt_host_unregister", "kt_host_barrier", "kt_shard_step", "kt_shard_bcast",
            "kt_ckpt_pitch", "kt_ckpt_blocks", "kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_workspace",
            "kt_norm_backward", "kt_act_forward", "kt_act_backward", "kt_attn_forward", "kt_attn_workspace", "kt_attn_backward",
-           "kt_attn_wait_limit", "kt_attn_given_up"]
+           "kt_attn_wait_limit", "kt_attn_given_up", "kt_waits_given_up", "kt_embed_forward", "kt_embed_workspace", "kt_embed_backward",
+           "kt_xent_forward", "kt_xent_workspace", "kt_xent_backward", "kt_orth_workspace", "kt_orth_update"]
 
 _DTYPES = {torch.float32: KT_F32, torch.bfloat16: KT_BF16}
 
@@ -120,6 +121,15 @@ def _load() -> C.CDLL:
         "kt_attn_backward": ([vp] * 19 + [i64, vp], C.c_int),
         "kt_attn_wait_limit": ([i64], C.c_int),
         "kt_attn_given_up": ([i64p], C.c_int),
+        "kt_waits_given_up": ([i64p], C.c_int),
+        "kt_embed_forward": ([vp, vp, i64, C.c_int, vp, i64, i64, i64, i64, C.c_int, C.c_float, vp], C.c_int),
+        "kt_embed_workspace": ([i64, i64, i64], i64),
+        "kt_embed_backward": ([vp, i64, vp, vp, i64, vp, i64, C.c_int, vp, i64, i64, i64, i64, C.c_int, C.c_float, vp], C.c_int),
+        "kt_xent_forward": ([vp, i64, vp, i64, vp, vp, vp, vp, i64, i64, i64, i64, C.c_int, C.c_float, vp], C.c_int),
+        "kt_xent_workspace": ([i64, i64, i64, C.c_int], i64),
+        "kt_xent_backward": ([vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, i64, i64, i64, i64, C.c_int, C.c_float, vp], C.c_int),
+        "kt_orth_workspace": ([i64, i64, i64], i64),
+        "kt_orth_update": ([vp, i64p, C.c_int, vp, i64p, vp, i64, i64, i64, i64, C.c_int, f32p, C.c_float, vp], C.c_int),
         "kt_launch_count": ([vp], C.c_int64),
         "kt_last_error": ([vp], C.c_char_p),
         "kt_destroy": ([vp], None),
@@ -687,7 +697,8 @@ def _load_fast():
         raise ImportError("%s was built for another torch or Python than torch %s and %s: %s" % (_build.FAST, _build.torch_version(), sys.implementation.cache_tag, rebuild))
     from . import _fast
     names = ("kt_ckpt_store", "kt_ckpt_restore", "kt_norm_forward", "kt_norm_backward", "kt_act_forward", "kt_act_backward",
-             "kt_attn_forward", "kt_attn_backward", "kt_last_error")
+             "kt_attn_forward", "kt_attn_backward", "kt_embed_forward", "kt_embed_backward", "kt_xent_forward", "kt_xent_backward",
+             "kt_orth_update", "kt_last_error")
     _fast.bind(KtError, *(C.cast(getattr(_lib, n), C.c_void_p).value for n in names))
     return _fast
 
@@ -795,6 +806,63 @@ def kt_attn_given_up() -> int:
     n = C.c_int64(0)
     _check(_lib.kt_attn_given_up(C.byref(n)))
     return int(n.value)
+
+
+def kt_waits_given_up() -> int:
+    """As kt_attn_given_up, with the waits of the loss and of matrix updates."""
+    n = C.c_int64(0)
+    _check(_lib.kt_waits_given_up(C.byref(n)))
+    return int(n.value)
+
+
+def kt_embed_forward(ids: torch.Tensor, weight: torch.Tensor, out: torch.Tensor, scale: float = 1.0, stream=None) -> None:
+    """out = scale * weight[ids]: ids int64 [tokens], weight [vocab, cols], out [tokens, cols].  A negative id gives
+    zeros, one past the vocabulary NaN."""
+    _fast.embed_forward(ids, weight, out, scale, stream)
+
+
+def kt_embed_workspace(tokens: int, cols: int, vocab: int) -> int:
+    """Bytes that kt_embed_backward needs."""
+    return _lib.kt_embed_workspace(tokens, cols, vocab)
+
+
+def kt_embed_backward(dout: torch.Tensor, ids: torch.Tensor, dweight: torch.Tensor, workspace: torch.Tensor, scale: float = 1.0,
+                      base: Optional[torch.Tensor] = None, stream=None) -> None:
+    """dweight = scale * the sums of dout over the tokens of each row [+ base, which may be dweight itself]."""
+    _fast.embed_backward(dout, ids, dweight, workspace, scale, base, stream)
+
+
+def kt_xent_workspace(rows: int, dim: int, vocab: int, backward: bool = False) -> int:
+    """Bytes that kt_xent_forward, or kt_xent_backward, needs."""
+    return _lib.kt_xent_workspace(rows, dim, vocab, bool(backward))
+
+
+def kt_xent_forward(hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, loss: torch.Tensor, lse: torch.Tensor,
+                    workspace: torch.Tensor, scale: float = 1.0, stream=None) -> None:
+    """Cross entropy of the logits scale * hidden weight^T against targets, row by row, without keeping the logits:
+    hidden [rows, dim] and weight [vocab, dim] bfloat16, targets int64 [rows] (negative: the row does not count), loss
+    and lse float32 [rows]."""
+    _fast.xent_forward(hidden, weight, targets, loss, lse, workspace, scale, stream)
+
+
+def kt_xent_backward(dloss: torch.Tensor, hidden: torch.Tensor, weight: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                     dhidden: Optional[torch.Tensor], dweight: Optional[torch.Tensor], workspace: torch.Tensor, scale: float = 1.0,
+                     dlse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Gradients of kt_xent_forward from its arguments, its lse and the gradients of loss (and lse)."""
+    _fast.xent_backward(dloss, hidden, weight, targets, lse, dhidden, dweight, workspace, scale, dlse, stream)
+
+
+def kt_orth_workspace(batch: int, rows: int, cols: int) -> int:
+    """Bytes that kt_orth_update needs."""
+    return _lib.kt_orth_workspace(batch, rows, cols)
+
+
+def kt_orth_update(x: torch.Tensor, out: torch.Tensor, workspace: torch.Tensor, steps: int = 5,
+                   coefficients: Sequence[float] = (3.4445, -4.7750, 2.0315), scale: float = 1.0, stream=None) -> None:
+    """out = scale * x orthogonalised by Newton-Schulz products; x float32 or bfloat16 [rows, cols] or [batch, rows,
+    cols], out bfloat16 of its shape."""
+    a, b, c = coefficients
+    _fast.orth_update(x, out, workspace, steps, a, b, c, scale, stream)
 
 
 class Graph:

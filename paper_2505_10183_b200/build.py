@@ -18,9 +18,11 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 SOURCES = [os.path.join(_PKG, "csrc", "kaitian.cu"), os.path.join(_PKG, "csrc", "kt_host.cu"),
            os.path.join(_PKG, "csrc", "kt_rows.cu"),
-           os.path.join(_PKG, "csrc", "kt_attn.cu")]
+           os.path.join(_PKG, "csrc", "kt_attn.cu"), os.path.join(_PKG, "csrc", "kt_embed.cu"),
+           os.path.join(_PKG, "csrc", "kt_xent.cu"), os.path.join(_PKG, "csrc", "kt_orth.cu")]
 DEPENDS = [os.path.join(_PKG, "csrc", "kt_kernels.cuh"), os.path.join(_PKG, "csrc", "kt_internal.h"),
-           os.path.join(_PKG, "csrc", "kt_tensor.cuh"), os.path.join(_PKG, "csrc", "kt_pairs.cuh")]
+           os.path.join(_PKG, "csrc", "kt_tensor.cuh"), os.path.join(_PKG, "csrc", "kt_pairs.cuh"),
+           os.path.join(_PKG, "csrc", "kt_eight.cuh"), os.path.join(_PKG, "csrc", "kt_product.cuh")]
 HEADERS = [os.path.join(_ROOT, "include", "kaitian.h")]
 LIB = os.path.join(_PKG, "libkaitian_b200.so")
 FAST_SOURCE = os.path.join(_PKG, "csrc", "kt_fast.cpp")

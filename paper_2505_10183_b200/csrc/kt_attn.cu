@@ -1273,22 +1273,6 @@ k_attn_backward(const __grid_constant__ CUtensorMap map_q, const __grid_constant
 }
 
 // ---------------------------------------------------------------------------------- host side
-typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-encode_fn encoder() {
-    static const encode_fn fn = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
-            cudaGetLastError();
-            f = nullptr;
-        }
-        return reinterpret_cast<encode_fn>(f);
-    }();
-    return fn;
-}
-
 int make_map(CUtensorMap *map, const char *what, const void *at, const int64_t *stride, int batch, int tokens, int heads, int dim) {
     const encode_fn encode = encoder();
     if (encode == nullptr) return fail(KT_ERR_CUDA, "the driver does not offer cuTensorMapEncodeTiled");
@@ -1326,7 +1310,7 @@ int check_heads(const char *what, const void *at, const int64_t *stride, int bat
     return KT_OK;
 }
 
-std::atomic<int64_t> wait_limit{2000000000};
+std::atomic<int64_t> wait_limit{2000000000};     // of all kernels that wait
 
 int fill(const kt_attn *a, AttnParams *p) {
     if (a == nullptr) return fail(KT_ERR_INVALID, "the description is NULL");
@@ -1462,6 +1446,8 @@ void copy_strides(int64_t *to, const int64_t *from) {
 
 }  // namespace
 
+uint64_t ktd::wait_limit_ns() { return static_cast<uint64_t>(wait_limit.load(std::memory_order_relaxed)); }
+
 extern "C" {
 
 int kt_attn_forward(const kt_attn *a, const void *q, const int64_t *q_stride, const void *k, const int64_t *k_stride, const void *v,
@@ -1558,6 +1544,16 @@ int kt_attn_given_up(int64_t *count) {
     KT_CUDA(cudaDeviceSynchronize());           // the copy alone waits for no stream that does not block
     KT_CUDA(cudaMemcpyFromSymbol(&n, g_waits_given_up, sizeof(n)));
     *count = static_cast<int64_t>(n);
+    return KT_OK;
+}
+
+int kt_waits_given_up(int64_t *count) {
+    if (int rc = kt_attn_given_up(count)) return rc;
+    unsigned long long n = 0;
+    for (auto of : {xent_given_up, orth_given_up}) {
+        if (int rc = of(&n)) return rc;
+        *count += static_cast<int64_t>(n);
+    }
     return KT_OK;
 }
 

@@ -1,0 +1,419 @@
+// kt_embed.cu -- rows of a table for the tokens of a batch, and the table's gradient.  Contracts: include/kaitian.h.
+//
+//   forward    out_i = scale w[ids_i]
+//   backward   dw_v = [base_v +] scale sum over the tokens i with ids_i = v of dout_i
+// Both are bound by memory.  The gradient is summed from a list of the tokens in which those of one row stand next to
+// each other, in their order in the batch; the list is cut into pieces of equal length whatever the text, and a row
+// whose tokens fall into several pieces is joined from their sums.  No atomics on data: the same inputs give the same bits.
+#include "../../include/kaitian.h"
+
+#include <cuda_bf16.h>
+
+#include <algorithm>
+
+#include "kt_eight.cuh"
+#include "kt_internal.h"
+
+using namespace ktd;
+
+namespace {
+
+constexpr int SMS = 148;                        // of a B200
+constexpr int64_t MAX_TOKENS = INT64_C(1) << 30, MAX_VOCAB = 1 << 24, MAX_COLS = 1 << 24;
+
+__device__ __forceinline__ void zeros(float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+}
+
+// ------------------------------------------------------------------------------------ forward
+struct LookupParams {
+    const int64_t *ids;
+    const void *weight;
+    void *out;
+    int64_t weight_stride, out_stride, tokens, cols;
+    int vocab;
+    float scale;
+};
+
+// A warp takes 1024 columns of a token, four pieces to a lane that are asked for before the first is used.
+template <typename W, typename O, bool WHOLE>
+__global__ void __launch_bounds__(256) k_embed_forward(const LookupParams p) {
+    const int64_t token = static_cast<int64_t>(blockIdx.x) * 8 + threadIdx.x / 32;
+    if (token >= p.tokens) return;
+    const int64_t id = p.ids[token], c0 = static_cast<int64_t>(blockIdx.y) * 1024 + threadIdx.x % 32 * 8;
+    O *const to = static_cast<O *>(p.out) + token * p.out_stride;
+    const bool known = id >= 0 && id < p.vocab;
+    const W *const row = static_cast<const W *>(p.weight) + (known ? id : 0) * p.weight_stride;
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (known && c0 + i * 256 < p.cols) {
+            read_eight<W, WHOLE>(row, c0 + i * 256, p.cols, v[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] = id < 0 ? 0.0f : __int_as_float(0x7FFFFFFF);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (c0 + i * 256 >= p.cols) break;
+        if (known)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i][e] *= p.scale;
+        write_eight<O, WHOLE>(to, c0 + i * 256, p.cols, v[i]);
+    }
+}
+
+// ----------------------------------------------------------------------------------- the list
+struct ListParams {
+    const int64_t *ids;
+    int *token, *row, *count;                   // the list, and its length
+    const void *base;
+    void *dweight;
+    int64_t base_stride, dweight_stride, cols;
+    int n, vocab, owners, most;                 // owners: CTAs; most: rows of the table to each
+    unsigned per;                               // floor(2^32 / owners)
+};
+constexpr int LIST_THREADS = 512, LIST_WARPS = 16, REMEMBERED = 96, MOST_ROWS = 2048;
+
+// The ids of a CTA are those with the same remainder by the number of CTAs: common tokens, which often lie next to each
+// other in a table, are spread.  Every CTA goes over all ids: those with a smaller remainder say where its tokens
+// begin in the list, so no CTA waits for another (64 thousand ids: some 5 us).  Counts are kept by row and warp;
+// a warp has the ids of a run of the batch, which keeps the order.
+// Rows of the table that no token has are written here: zeros, or the base's.
+template <typename T, bool WHOLE>
+__global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p) {
+    extern __shared__ int counts[];             // [LIST_WARPS][most]
+    __shared__ int remembered[LIST_WARPS][REMEMBERED], sums[LIST_WARPS];
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, mine = blockIdx.x, owners = p.owners;
+    let_next_begin();
+    for (int i = tid; i < LIST_WARPS * p.most; i += LIST_THREADS) counts[i] = 0;
+    __syncthreads();
+    int *const of_warp = counts + warp * p.most;
+    const int run = ((p.n + LIST_WARPS - 1) / LIST_WARPS + 31) / 32 * 32, begin = min(p.n, warp * run), end = min(p.n, begin + run);
+    // id -> (row among the CTA's, or -1); smaller: its remainder comes before the CTA's
+    auto look = [&](int64_t id, bool &smaller) {
+        smaller = false;
+        if (id < 0 || id >= p.vocab) return -1;
+        unsigned q = __umulhi(static_cast<unsigned>(id), p.per), r = static_cast<unsigned>(id) - q * owners;
+        if (r >= static_cast<unsigned>(owners)) ++q, r -= owners;
+        smaller = r < static_cast<unsigned>(mine);
+        return r == static_cast<unsigned>(mine) ? static_cast<int>(q) : -1;
+    };
+    int before = 0, found = 0;
+    for (int i = begin; i < end; i += 128) {
+        int64_t id[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) id[u] = i + u * 32 + lane < end ? p.ids[i + u * 32 + lane] : -1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            bool smaller;
+            const int q = look(id[u], smaller);
+            before += smaller;
+            const unsigned mask = __ballot_sync(0xFFFFFFFFu, q >= 0);
+            if (q >= 0) {
+                atomicAdd(&of_warp[q], 1);
+                const int at = found + __popc(mask & ((1u << lane) - 1));
+                if (at < REMEMBERED) remembered[warp][at] = i + u * 32 + lane;
+            }
+            found += __popc(mask);
+        }
+    }
+    before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (lane == 0) sums[warp] = before;
+    __syncthreads();
+    int base = 0;
+    for (int w = 0; w < LIST_WARPS; ++w) base += sums[w];
+    __syncthreads();
+    // where the tokens of each row and warp begin
+    for (int q0 = 0; q0 < p.most; q0 += LIST_THREADS) {
+        const int q = q0 + tid;
+        int total = 0;
+        if (q < p.most)
+            for (int w = 0; w < LIST_WARPS; ++w) total += counts[w * p.most + q];
+        int up = total;
+#pragma unroll
+        for (int far = 1; far < 32; far *= 2) {
+            const int x = __shfl_up_sync(0xFFFFFFFFu, up, far);
+            if (lane >= far) up += x;
+        }
+        if (lane == 31) sums[warp] = up;
+        __syncthreads();
+        int at = base + up - total, all = 0;
+        for (int w = 0; w < LIST_WARPS; ++w) {
+            if (w < warp) at += sums[w];
+            all += sums[w];
+        }
+        base += all;
+        if (q < p.most)
+            for (int w = 0; w < LIST_WARPS; ++w) {
+                const int here = counts[w * p.most + q];
+                counts[w * p.most + q] = total == 0 ? -1 : at;
+                at += here;
+            }
+        __syncthreads();
+    }
+    if (mine == owners - 1 && tid == 0) *p.count = base;
+    // the tokens to their places, 32 at a time in order: those that were remembered, or the whole run again
+    const bool all_remembered = found <= REMEMBERED;
+    const int from = all_remembered ? 0 : begin, past = all_remembered ? found : end;
+    for (int i = from; i < past; i += 32) {
+        const int token = i + lane < past ? (all_remembered ? remembered[warp][i + lane] : i + lane) : -1;
+        bool smaller;
+        const int64_t id = token >= 0 ? p.ids[token] : -1;
+        const int q = look(id, smaller);
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, q);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        if (q >= 0) {
+            const int at = of_warp[q] + rank;
+            p.token[at] = token, p.row[at] = static_cast<int>(id);
+        }
+        __syncwarp();
+        if (q >= 0 && rank == 0) of_warp[q] += __popc(same);
+        __syncwarp();
+    }
+    if (p.base == p.dweight) return;            // untouched rows are what they have to be
+    const int64_t pieces = (p.cols + 7) / 8;
+    for (int q = warp; q < p.most; q += LIST_WARPS) {
+        const int64_t v = static_cast<int64_t>(q) * owners + mine;
+        if (v >= p.vocab || counts[(LIST_WARPS - 1) * p.most + q] >= 0) continue;
+        T *const to = static_cast<T *>(p.dweight) + v * p.dweight_stride;
+        const T *const like = p.base != nullptr ? static_cast<const T *>(p.base) + v * p.base_stride : nullptr;
+#pragma unroll 4
+        for (int64_t c = lane; c < pieces; c += 32) {
+            float x[8];
+            zeros(x);
+            if (like != nullptr) read_eight<T, WHOLE>(like, c * 8, p.cols, x);
+            write_eight<T, WHOLE>(to, c * 8, p.cols, x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------ the sums
+struct SumParams {
+    const int *token, *row, *count;
+    const void *dout, *base;
+    void *dweight;
+    float *parts;                               // [pieces][2][cols]: of the row that began before, and of the one that goes on
+    int64_t dout_stride, base_stride, dweight_stride, cols, pitch;
+    int length;                                 // of a piece
+    float scale;
+};
+constexpr int MAX_LENGTH = 256, AHEAD = 8;
+
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void write_row(const SumParams &p, int row, int64_t c, const float (&sum)[8]) {
+    float v[8];
+    zeros(v);
+    if (p.base != nullptr) read_eight<T, WHOLE>(static_cast<const T *>(p.base) + row * p.base_stride, c, p.cols, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = fmaf(sum[e], p.scale, v[e]);
+    write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + row * p.dweight_stride, c, p.cols, v);
+}
+
+// A piece of the list to a CTA, eight columns to a thread, AHEAD rows of dout on their way at a time.
+template <typename D, typename T, bool WHOLE>
+__global__ void __launch_bounds__(256) k_embed_sum(const SumParams p) {
+    __shared__ int token[MAX_LENGTH], row[MAX_LENGTH + 2];       // row[0], row[n + 1]: the neighbours' (-1: none)
+    let_next_begin();
+    after_previous();
+    const int all = *p.count, begin = blockIdx.x * p.length, n = min(p.length, all - begin);
+    if (n <= 0) return;
+    for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {
+        const int at = begin + i - 1;
+        row[i] = at >= 0 && at < all ? p.row[at] : -1;
+        if (i >= 1 && i <= n) token[i - 1] = p.token[at];
+    }
+    __syncthreads();
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 8;
+    if (c >= p.cols) return;
+    const D *const dout = static_cast<const D *>(p.dout);
+    float sum[8];
+    zeros(sum);
+    bool whole = row[0] != row[1];              // the row's tokens begin in this piece
+    for (int i0 = 0; i0 < n; i0 += AHEAD) {
+        float v[AHEAD][8];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            if (i0 + u < n) read_eight<D, WHOLE>(dout + token[i0 + u] * p.dout_stride, c, p.cols, v[u]);
+            else zeros(v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int i = i0 + u;
+            if (i >= n) break;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+            const int now = row[i + 1], next = row[i + 2];
+            if (next == now && i + 1 < n) continue;
+            if (whole && next != now) {
+                write_row<T, WHOLE>(p, now, c, sum);
+            } else {
+                float *const to = p.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (whole ? 1 : 0)) * p.pitch + c;       // pitch: whole vectors
+                *reinterpret_cast<float4 *>(to) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                *reinterpret_cast<float4 *>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            }
+            zeros(sum);
+            whole = true;
+        }
+    }
+}
+
+// A row whose tokens go on behind the piece in which they begin: that piece's sum, then the next ones', in order.
+template <typename T, bool WHOLE>
+__global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
+    let_next_begin();
+    after_previous();
+    const int all = *p.count, begin = blockIdx.x * p.length, end = begin + p.length;
+    if (end >= all) return;
+    const int row = p.row[end - 1];
+    if (p.row[end] != row || (begin > 0 && p.row[begin - 1] == row)) return;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 8;
+    if (c >= p.cols) return;
+    auto part = [&](int64_t at, float (&v)[8]) {
+        const float4 a = *reinterpret_cast<const float4 *>(p.parts + at * p.pitch + c), b = *reinterpret_cast<const float4 *>(p.parts + at * p.pitch + c + 4);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+    };
+    float sum[8];
+    part(static_cast<int64_t>(blockIdx.x) * 2 + 1, sum);
+    for (int at = end, piece = blockIdx.x + 1; at < all && p.row[at] == row;) {       // four pieces at a time
+        float v[4][8];
+        bool there[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t first = static_cast<int64_t>(at) + static_cast<int64_t>(u) * p.length;
+            there[u] = first < all && p.row[first] == row;
+            if (there[u]) part((static_cast<int64_t>(piece) + u) * 2, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (there[u])
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+        if (!there[3]) break;
+        at += 4 * p.length, piece += 4;         // (at most 2^30 + 4 pieces)
+    }
+    write_row<T, WHOLE>(p, row, c, sum);
+}
+
+// ---------------------------------------------------------------------------------- host side
+int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// How the gradient's work is cut: from the sizes alone.
+struct Plan {
+    int64_t owners, most, threads, across, length, pieces, pitch, at_row, at_parts, bytes;
+    Plan(int64_t tokens, int64_t cols, int64_t vocab) {
+        // a CTA for each SM, more where a CTA's counts would not fit its shared memory
+        owners = std::max<int64_t>(SMS, (vocab + MOST_ROWS - 1) / MOST_ROWS), most = (vocab + owners - 1) / owners;
+        const int64_t vectors = (cols + 7) / 8;
+        threads = std::min<int64_t>(256, up(vectors, 32)), across = (vectors + threads - 1) / threads;
+        // six CTAs of 256 threads to an SM or fewer; short pieces leave more rows to be joined
+        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(32, tokens * across / (SMS * 6 * 256 / threads)));
+        pieces = (tokens + length - 1) / length;
+        pitch = up(cols, 8);
+        int64_t at = 1024 + up(tokens * 4, 1024);      // the list's length and tokens
+        at_row = at, at += up(tokens * 4, 1024);
+        at_parts = at, at += pieces > 1 ? pieces * 2 * pitch * 4 : 0;
+        bytes = at;
+    }
+};
+
+int check_matrix(const char *what, const void *at, int64_t stride, int64_t rows, int64_t cols, int dtype) {
+    if (rows == 0 || cols == 0) return KT_OK;
+    if (at == nullptr) return fail(KT_ERR_INVALID, "%s is NULL", what);
+    if (reinterpret_cast<uintptr_t>(at) % (dtype == KT_F32 ? 4 : 2)) return fail(KT_ERR_ALIGN, "%s is not aligned to its elements", what);
+    if (rows > 1 && (stride < cols || stride > INT64_C(1) << 38)) return fail(KT_ERR_SHAPE, "%s: rows of %lld elements cannot be %lld apart", what, (long long)cols, (long long)stride);
+    return KT_OK;
+}
+int check_common(int64_t tokens, int64_t cols, int64_t vocab, int dtype, int param_dtype, float scale, const int64_t *ids) {
+    for (int t : {dtype, param_dtype})
+        if (t != KT_F32 && t != KT_BF16) return fail(KT_ERR_INVALID, "unknown dtype %d", t);
+    if (tokens < 0 || tokens > MAX_TOKENS || cols < 1 || cols > MAX_COLS || vocab < 1 || vocab > MAX_VOCAB)
+        return fail(KT_ERR_SHAPE, "%lld tokens, %lld columns, a vocabulary of %lld", (long long)tokens, (long long)cols, (long long)vocab);
+    if (!(scale - scale == 0.0f)) return fail(KT_ERR_INVALID, "scale must be finite");
+    if (tokens > 0 && ids == nullptr) return fail(KT_ERR_INVALID, "ids is NULL");
+    if (reinterpret_cast<uintptr_t>(ids) % 8) return fail(KT_ERR_ALIGN, "ids is not aligned to its elements");
+    return KT_OK;
+}
+bool whole(const void *at, int64_t stride, int64_t rows, int dtype) {
+    return reinterpret_cast<uintptr_t>(at) % 16 == 0 && (rows <= 1 || stride * (dtype == KT_F32 ? 4 : 2) % 16 == 0);
+}
+
+template <typename W, typename O>
+int lookup(const LookupParams &p, bool vectors, cudaStream_t st) {
+    const dim3 grid(static_cast<unsigned>((p.tokens + 7) / 8), static_cast<unsigned>((p.cols + 1023) / 1024));
+    vectors ? k_embed_forward<W, O, true><<<grid, 256, 0, st>>>(p) : k_embed_forward<W, O, false><<<grid, 256, 0, st>>>(p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+
+template <typename T, bool WHOLE>
+int start_list(const ListParams &l, const Plan &plan, cudaStream_t st) {
+    const size_t bytes = static_cast<size_t>(LIST_WARPS * plan.most * 4);
+    if (bytes > 40 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list<T, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB with what is static need no leave
+    k_embed_list<T, WHOLE><<<static_cast<unsigned>(plan.owners), LIST_THREADS, bytes, st>>>(l);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+
+template <typename D, typename T, bool WHOLE>
+int gradient(const ListParams &l, const SumParams &s, const Plan &plan, cudaStream_t st) {
+    if (int rc = start_list<T, WHOLE>(l, plan, st)) return rc;
+    if (plan.pieces == 0) return KT_OK;
+    const dim3 grid(static_cast<unsigned>(plan.pieces), static_cast<unsigned>(plan.across)), block(static_cast<unsigned>(plan.threads));
+    KT_CUDA(launch_behind(k_embed_sum<D, T, WHOLE>, 1, grid, block, 0, st, s));
+    if (plan.pieces > 1) KT_CUDA(launch_behind(k_embed_join<T, WHOLE>, 1, grid, block, 0, st, s));
+    return KT_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kt_embed_forward(const int64_t *ids, const void *weight, int64_t weight_stride, int param_dtype, void *out, int64_t out_stride, int64_t tokens, int64_t cols, int64_t vocab, int dtype, float scale,
+                     void *stream) {
+    if (int rc = check_common(tokens, cols, vocab, dtype, param_dtype, scale, ids)) return rc;
+    if (tokens == 0) return KT_OK;
+    if (int rc = check_matrix("weight", weight, weight_stride, vocab, cols, param_dtype)) return rc;
+    if (int rc = check_matrix("out", out, out_stride, tokens, cols, dtype)) return rc;
+    const LookupParams p{ids, weight, out, weight_stride, out_stride, tokens, cols, static_cast<int>(vocab), scale};
+    const bool vectors = whole(weight, weight_stride, vocab, param_dtype) && whole(out, out_stride, tokens, dtype);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (param_dtype == KT_F32) return dtype == KT_F32 ? lookup<float, float>(p, vectors, st) : lookup<float, __nv_bfloat16>(p, vectors, st);
+    return dtype == KT_F32 ? lookup<__nv_bfloat16, float>(p, vectors, st) : lookup<__nv_bfloat16, __nv_bfloat16>(p, vectors, st);
+}
+
+int64_t kt_embed_workspace(int64_t tokens, int64_t cols, int64_t vocab) {
+    if (tokens < 0 || tokens > MAX_TOKENS || cols < 1 || cols > MAX_COLS || vocab < 1 || vocab > MAX_VOCAB) return 0;
+    return Plan(tokens, cols, vocab).bytes;
+}
+
+int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids, const void *base, int64_t base_stride, void *dweight, int64_t dweight_stride, int param_dtype, void *workspace,
+                      int64_t workspace_bytes, int64_t tokens, int64_t cols, int64_t vocab, int dtype, float scale, void *stream) {
+    if (int rc = check_common(tokens, cols, vocab, dtype, param_dtype, scale, ids)) return rc;
+    if (int rc = check_matrix("dout", dout, dout_stride, tokens, cols, dtype)) return rc;
+    if (int rc = check_matrix("dweight", dweight, dweight_stride, vocab, cols, param_dtype)) return rc;
+    if (base != nullptr)
+        if (int rc = check_matrix("base", base, base_stride, vocab, cols, param_dtype)) return rc;
+    if (base == dweight && vocab > 1 && base_stride != dweight_stride) return fail(KT_ERR_SHAPE, "base is dweight, with another stride");
+    const Plan plan(tokens, cols, vocab);
+    if (workspace == nullptr) return fail(KT_ERR_INVALID, "workspace is NULL");
+    if (workspace_bytes < plan.bytes) return fail(KT_ERR_SHAPE, "workspace of %lld bytes: %lld are needed", (long long)workspace_bytes, (long long)plan.bytes);
+    if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(KT_ERR_ALIGN, "workspace is not 16-byte aligned");
+    char *const ws = static_cast<char *>(workspace);
+    int *const count = reinterpret_cast<int *>(ws), *const token = reinterpret_cast<int *>(ws + 1024), *const row = reinterpret_cast<int *>(ws + plan.at_row);
+    const ListParams l{ids, token, row, count, base, dweight, base_stride, dweight_stride, cols, static_cast<int>(tokens), static_cast<int>(vocab), static_cast<int>(plan.owners), static_cast<int>(plan.most),
+                       static_cast<unsigned>((UINT64_C(1) << 32) / static_cast<uint64_t>(plan.owners))};
+    const SumParams s{token, row, count, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(plan.length), scale};
+    const bool vectors = (tokens == 0 || whole(dout, dout_stride, tokens, dtype)) && whole(dweight, dweight_stride, vocab, param_dtype) && (base == nullptr || whole(base, base_stride, vocab, param_dtype));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (param_dtype == KT_F32) {
+        if (dtype == KT_F32) return vectors ? gradient<float, float, true>(l, s, plan, st) : gradient<float, float, false>(l, s, plan, st);
+        return vectors ? gradient<__nv_bfloat16, float, true>(l, s, plan, st) : gradient<__nv_bfloat16, float, false>(l, s, plan, st);
+    }
+    if (dtype == KT_F32) return vectors ? gradient<float, __nv_bfloat16, true>(l, s, plan, st) : gradient<float, __nv_bfloat16, false>(l, s, plan, st);
+    return vectors ? gradient<__nv_bfloat16, __nv_bfloat16, true>(l, s, plan, st) : gradient<__nv_bfloat16, __nv_bfloat16, false>(l, s, plan, st);
+}
+
+}  // extern "C"

@@ -26,6 +26,11 @@ decltype(&kt_act_forward) c_act_forward;
 decltype(&kt_act_backward) c_act_backward;
 decltype(&kt_attn_forward) c_attn_forward;
 decltype(&kt_attn_backward) c_attn_backward;
+decltype(&kt_embed_forward) c_embed_forward;
+decltype(&kt_embed_backward) c_embed_backward;
+decltype(&kt_xent_forward) c_xent_forward;
+decltype(&kt_xent_backward) c_xent_backward;
+decltype(&kt_orth_update) c_orth_update;
 decltype(&kt_last_error) c_last_error;
 PyObject *error_class;
 
@@ -271,6 +276,93 @@ PyObject *attn_backward(PyObject *const *a) {   // dout, q, k, v, out, lse, dq, 
                                 hdk.stride, hdv.at, hdv.stride, workspace->data_ptr(), workspace_bytes(workspace), stream_of(a[14])));
 }
 
+// ------------------------------------------------------------- embedding, loss and matrix updates
+const int64_t *indices(const at::Tensor *t, const char *what, int64_t rows) {
+    if (t->scalar_type() != at::kLong || t->dim() != 1 || (rows >= 0 && t->size(0) != rows) || !t->is_contiguous()) refuse(KT_ERR_SHAPE, "%s: contiguous int64, one to a row, expected", what);
+    return static_cast<const int64_t *>(t->data_ptr());
+}
+float number(PyObject *o) {
+    const double x = PyFloat_AsDouble(o);
+    if (x == -1.0 && PyErr_Occurred()) throw Refused();
+    return static_cast<float>(x);
+}
+void check_cols(const Matrix &m, const char *what, int64_t cols) {
+    if (m.cols != cols) refuse(KT_ERR_SHAPE, "%s: %lld columns expected", what, (long long)cols);
+}
+
+PyObject *embed_forward(PyObject *const *a) {   // ids, weight, out, scale, stream
+    Call c;
+    const at::Tensor *ids = c.tensor(a[0], "ids");
+    const Matrix weight = matrix(c.tensor(a[1], "weight"), "weight"), out = matrix(c.tensor(a[2], "out"), "out");
+    check_cols(weight, "weight", out.cols);
+    return done(c_embed_forward(indices(ids, "ids", out.rows), weight.at, weight.stride, weight.type, out.at, out.stride, out.rows, out.cols, weight.rows, out.type, number(a[3]), stream_of(a[4])));
+}
+
+PyObject *embed_backward(PyObject *const *a) {  // dout, ids, dweight, workspace, scale, base, stream
+    Call c;
+    const Matrix dout = matrix(c.tensor(a[0], "dout"), "dout");
+    const at::Tensor *ids = c.tensor(a[1], "ids"), *workspace = c.tensor(a[3], "workspace", true);
+    const Matrix dweight = matrix(c.tensor(a[2], "dweight"), "dweight"), base = matrix(c.tensor(a[5], "base", true), "base", &dweight);
+    check_cols(dweight, "dweight", dout.cols);
+    return done(c_embed_backward(dout.at, dout.stride, indices(ids, "ids", dout.rows), base.at, base.stride, dweight.at, dweight.stride, dweight.type, address(workspace), workspace_bytes(workspace), dout.rows,
+                                 dout.cols, dweight.rows, dout.type, number(a[4]), stream_of(a[6])));
+}
+
+PyObject *xent_forward(PyObject *const *a) {    // hidden, weight, targets, loss, lse, workspace, scale, stream
+    Call c;
+    const Matrix hidden = matrix(c.tensor(a[0], "hidden"), "hidden"), weight = matrix(c.tensor(a[1], "weight"), "weight");
+    const at::Tensor *targets = c.tensor(a[2], "targets"), *loss = c.tensor(a[3], "loss"), *lse = c.tensor(a[4], "lse"), *workspace = c.tensor(a[5], "workspace", true);
+    check_cols(weight, "weight", hidden.cols);
+    if (hidden.type != weight.type) refuse(KT_ERR_SHAPE, "hidden and weight: one dtype expected");
+    const int64_t *const t = indices(targets, "targets", hidden.rows);
+    float *const to_loss = per_row(loss, hidden.rows, "loss"), *const to_lse = per_row(lse, hidden.rows, "lse");
+    return done(c_xent_forward(hidden.at, hidden.stride, weight.at, weight.stride, t, to_loss, to_lse, address(workspace), workspace_bytes(workspace), hidden.rows, hidden.cols, weight.rows, hidden.type,
+                               number(a[6]), stream_of(a[7])));
+}
+
+PyObject *xent_backward(PyObject *const *a) {   // dloss, hidden, weight, targets, lse, dhidden, dweight, workspace, scale, dlse, stream
+    Call c;
+    const at::Tensor *dloss = c.tensor(a[0], "dloss");
+    const Matrix hidden = matrix(c.tensor(a[1], "hidden"), "hidden"), weight = matrix(c.tensor(a[2], "weight"), "weight");
+    const at::Tensor *targets = c.tensor(a[3], "targets"), *lse = c.tensor(a[4], "lse"), *workspace = c.tensor(a[7], "workspace", true), *dlse = c.tensor(a[9], "dlse", true);
+    const Matrix dhidden = matrix(c.tensor(a[5], "dhidden", true), "dhidden", &hidden), dweight = matrix(c.tensor(a[6], "dweight", true), "dweight", &weight);
+    check_cols(weight, "weight", hidden.cols);
+    if (hidden.type != weight.type) refuse(KT_ERR_SHAPE, "hidden and weight: one dtype expected");
+    const int64_t *const t = indices(targets, "targets", hidden.rows);
+    const float *const g = per_row(dloss, hidden.rows, "dloss"), *const z = per_row(dlse, hidden.rows, "dlse"), *const l = per_row(lse, hidden.rows, "lse");
+    return done(c_xent_backward(g, z, hidden.at, hidden.stride, weight.at, weight.stride, t, l, dhidden.at, dhidden.stride, dweight.at, dweight.stride, address(workspace), workspace_bytes(workspace),
+                                hidden.rows, hidden.cols, weight.rows, hidden.type, number(a[8]), stream_of(a[10])));
+}
+
+// Matrices of two or three dimensions.
+struct Matrices {
+    void *at;
+    int64_t stride[2], size[3];
+    int type;
+};
+Matrices matrices(const at::Tensor *t, const char *what) {
+    const int64_t d = t->dim();
+    Matrices m{};
+    if ((d != 2 && d != 3) || (m.type = type_of(*t)) < 0 || (t->size(d - 1) > 1 && t->stride(d - 1) != 1))
+        refuse(KT_ERR_SHAPE, "%s: float32 or bfloat16 [rows, cols] or [batch, rows, cols] with contiguous columns expected", what);
+    m.at = t->data_ptr();
+    m.size[0] = d == 3 ? t->size(0) : 1, m.size[1] = t->size(d - 2), m.size[2] = t->size(d - 1);
+    m.stride[0] = d == 3 ? t->stride(0) : 0, m.stride[1] = t->stride(d - 2);
+    return m;
+}
+
+PyObject *orth_update(PyObject *const *a) {     // x, out, workspace, steps, a, b, c, scale, stream
+    Call c;
+    const at::Tensor *tx = c.tensor(a[0], "x"), *tout = c.tensor(a[1], "out"), *workspace = c.tensor(a[2], "workspace", true);
+    const Matrices x = matrices(tx, "x"), out = matrices(tout, "out");
+    if (tx->sizes() != tout->sizes() || out.type != KT_BF16) refuse(KT_ERR_SHAPE, "out: bfloat16 of x's shape expected");
+    const long steps = PyLong_AsLong(a[3]);
+    if (steps == -1 && PyErr_Occurred()) throw Refused();
+    const float coefficients[3] = {number(a[4]), number(a[5]), number(a[6])};
+    return done(c_orth_update(x.at, x.stride, x.type, out.at, out.stride, address(workspace), workspace_bytes(workspace), x.size[0], x.size[1], x.size[2],
+                              static_cast<int>(steps < -1 ? -1 : steps > 1000 ? 1000 : steps), coefficients, number(a[7]), stream_of(a[8])));
+}
+
 // ---------------------------------------------------------------------------------- the module
 // No C++ exception leaves a call: torch's own become Python errors too.
 template <PyObject *(*FN)(PyObject *const *), int N>
@@ -292,7 +384,9 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {         // the error class, then the addresses of the C entries
     void **const to[] = {reinterpret_cast<void **>(&c_ckpt_store), reinterpret_cast<void **>(&c_ckpt_restore), reinterpret_cast<void **>(&c_norm_forward),
                          reinterpret_cast<void **>(&c_norm_backward), reinterpret_cast<void **>(&c_act_forward), reinterpret_cast<void **>(&c_act_backward),
-                         reinterpret_cast<void **>(&c_attn_forward), reinterpret_cast<void **>(&c_attn_backward), reinterpret_cast<void **>(&c_last_error)};
+                         reinterpret_cast<void **>(&c_attn_forward), reinterpret_cast<void **>(&c_attn_backward), reinterpret_cast<void **>(&c_embed_forward), reinterpret_cast<void **>(&c_embed_backward),
+                         reinterpret_cast<void **>(&c_xent_forward), reinterpret_cast<void **>(&c_xent_backward), reinterpret_cast<void **>(&c_orth_update),
+                         reinterpret_cast<void **>(&c_last_error)};
     constexpr Py_ssize_t ENTRIES = sizeof(to) / sizeof(to[0]);
     if (n != ENTRIES + 1) return PyErr_Format(PyExc_TypeError, "%zd arguments expected, %zd given", ENTRIES + 1, n);
     for (Py_ssize_t i = 0; i < ENTRIES; ++i) {
@@ -315,6 +409,11 @@ PyMethodDef methods[] = {{"bind", reinterpret_cast<PyCFunction>(reinterpret_cast
                          KT_METHOD(act_backward, 7),
                          KT_METHOD(attn_forward, 10),
                          KT_METHOD(attn_backward, 15),
+                         KT_METHOD(embed_forward, 5),
+                         KT_METHOD(embed_backward, 7),
+                         KT_METHOD(xent_forward, 8),
+                         KT_METHOD(xent_backward, 11),
+                         KT_METHOD(orth_update, 9),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_fast", KT_BELONGS, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

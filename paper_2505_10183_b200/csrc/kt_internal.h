@@ -32,6 +32,12 @@ void member_units(int64_t U, int member, int M, int64_t *first, int64_t *past);
 // KT_OK, or KT_ERR_INVALID with a message when a share is missing or below one.
 int check_shares(const int32_t *shares, int K);
 
+// How long a wait inside a kernel may last (kt_attn_wait_limit), and how many gave up on the current device in the
+// kernels of the other files that wait (kt_waits_given_up).
+uint64_t wait_limit_ns();
+int xent_given_up(unsigned long long *count);
+int orth_given_up(unsigned long long *count);
+
 }  // namespace ktd
 
 #ifdef __CUDACC__
