@@ -10,6 +10,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <cstring>
 
 #include "kt_eight.cuh"
 #include "kt_internal.h"
@@ -69,9 +70,7 @@ __global__ void __launch_bounds__(256) k_embed_forward(const LookupParams p) {
 struct ListParams {
     const int64_t *ids;
     int *token, *row, *count;                   // the list, and its length
-    const void *base;
-    void *dweight;
-    int64_t base_stride, dweight_stride, cols;
+    int *past;                                  // where a row's tokens end in the list (0: it has none)
     int n, vocab, owners, most;                 // owners: CTAs; most: rows of the table to each
     unsigned per;                               // floor(2^32 / owners)
 };
@@ -81,8 +80,6 @@ constexpr int LIST_THREADS = 512, LIST_WARPS = 16, REMEMBERED = 96, MOST_ROWS = 
 // other in a table, are spread.  Every CTA goes over all ids: those with a smaller remainder say where its tokens
 // begin in the list, so no CTA waits for another (64 thousand ids: some 5 us).  Counts are kept by row and warp;
 // a warp has the ids of a run of the batch, which keeps the order.
-// Rows of the table that no token has are written here: zeros, or the base's.
-template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p) {
     extern __shared__ int counts[];             // [LIST_WARPS][most]
     __shared__ int remembered[LIST_WARPS][REMEMBERED], sums[LIST_WARPS];
@@ -146,12 +143,15 @@ __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p)
             all += sums[w];
         }
         base += all;
-        if (q < p.most)
+        if (q < p.most) {
+            const int64_t v = static_cast<int64_t>(q) * owners + mine;
+            if (v < p.vocab) p.past[v] = total > 0 ? at + total : 0;
             for (int w = 0; w < LIST_WARPS; ++w) {
                 const int here = counts[w * p.most + q];
-                counts[w * p.most + q] = total == 0 ? -1 : at;
+                counts[w * p.most + q] = at;
                 at += here;
             }
+        }
         __syncthreads();
     }
     if (mine == owners - 1 && tid == 0) *p.count = base;
@@ -173,52 +173,88 @@ __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p)
         if (q >= 0 && rank == 0) of_warp[q] += __popc(same);
         __syncwarp();
     }
-    if (p.base == p.dweight) return;            // untouched rows are what they have to be
-    const int64_t pieces = (p.cols + 7) / 8;
-    for (int q = warp; q < p.most; q += LIST_WARPS) {
-        const int64_t v = static_cast<int64_t>(q) * owners + mine;
-        if (v >= p.vocab || counts[(LIST_WARPS - 1) * p.most + q] >= 0) continue;
-        T *const to = static_cast<T *>(p.dweight) + v * p.dweight_stride;
-        const T *const like = p.base != nullptr ? static_cast<const T *>(p.base) + v * p.base_stride : nullptr;
-#pragma unroll 4
-        for (int64_t c = lane; c < pieces; c += 32) {
-            float x[8];
-            zeros(x);
-            if (like != nullptr) read_eight<T, WHOLE>(like, c * 8, p.cols, x);
-            write_eight<T, WHOLE>(to, c * 8, p.cols, x);
-        }
-    }
 }
 
 // ------------------------------------------------------------------------------------ the sums
 struct SumParams {
     const int *token, *row, *count;
+    const int *past;
     const void *dout, *base;
     void *dweight;
-    float *parts;                               // [pieces][2][cols]: of the row that began before, and of the one that goes on
+    float *parts;                               // [pieces][2][pitch]: of the row that began before, and of the one that goes on
     int64_t dout_stride, base_stride, dweight_stride, cols, pitch;
-    int length;                                 // of a piece
+    int length, pieces, across;                 // tokens of a piece, pieces, CTAs across a row
+    int vocab, rows_each;                       // rows of the table to a CTA that fills
     float scale;
 };
-constexpr int MAX_LENGTH = 256, AHEAD = 8;
+constexpr int MAX_LENGTH = 256, AHEAD = 4;
 
+// Eight neighbouring elements as they come from memory.
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void write_row(const SumParams &p, int row, int64_t c, const float (&sum)[8]) {
-    float v[8];
-    zeros(v);
-    if (p.base != nullptr) read_eight<T, WHOLE>(static_cast<const T *>(p.base) + row * p.base_stride, c, p.cols, v);
+struct Raw {
+    uint4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void read(const T *row, int64_t c, int64_t cols) {
+        if (WHOLE && c + 8 <= cols) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = fmaf(sum[e], p.scale, v[e]);
-    write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + row * p.dweight_stride, c, p.cols, v);
+            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) v[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+        } else {
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : T(0.0f);
+            memcpy(v, e, sizeof(e));
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
+        const uint32_t *const w = reinterpret_cast<const uint32_t *>(v);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[2 * i] += __uint_as_float(w[i] << 16), sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
+        }
+    }
+};
+
+// Rows of the table that no token has: zeros, or the base's.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void fill_rows(const SumParams &p, int64_t first, int threads) {
+    const int vectors = static_cast<int>((p.cols + 7) / 8), all = static_cast<int>(min(static_cast<int64_t>(p.rows_each), p.vocab - first)) * vectors;
+    for (int i0 = threadIdx.x; i0 < all; i0 += 4 * threads) {
+        Raw<T, WHOLE> v[4];
+        bool there[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int i = i0 + u * threads, r = i / vectors;
+            there[u] = i < all && p.past[first + r] == 0;
+            v[u] = {};
+            if (there[u] && p.base != nullptr) v[u].read(static_cast<const T *>(p.base) + (first + r) * p.base_stride, (i - r * vectors) * 8, p.cols);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (!there[u]) continue;
+            const int i = i0 + u * threads, r = i / vectors;
+            float x[8];
+            zeros(x);
+            v[u].add_to(x);
+            write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + (first + r) * p.dweight_stride, (i - r * vectors) * 8, p.cols, x);
+        }
+    }
 }
 
-// A piece of the list to a CTA, eight columns to a thread, AHEAD rows of dout on their way at a time.
+// A piece of the list to a CTA, eight columns to a thread, AHEAD rows of dout (and of the base, where a row's tokens
+// end) on their way at a time; behind those, CTAs that fill the rows without tokens.
 template <typename D, typename T, bool WHOLE>
-__global__ void __launch_bounds__(256) k_embed_sum(const SumParams p) {
+__global__ void __launch_bounds__(256, 3) k_embed_sum(const SumParams p) {
     __shared__ int token[MAX_LENGTH], row[MAX_LENGTH + 2];       // row[0], row[n + 1]: the neighbours' (-1: none)
     let_next_begin();
     after_previous();
-    const int all = *p.count, begin = blockIdx.x * p.length, n = min(p.length, all - begin);
+    const int summing = p.pieces * p.across;
+    if (static_cast<int>(blockIdx.x) >= summing) {
+        fill_rows<T, WHOLE>(p, (static_cast<int64_t>(blockIdx.x) - summing) * p.rows_each, blockDim.x);
+        return;
+    }
+    const int piece = blockIdx.x / p.across, all = *p.count, begin = piece * p.length, n = min(p.length, all - begin);
     if (n <= 0) return;
     for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {
         const int at = begin + i - 1;
@@ -226,31 +262,39 @@ __global__ void __launch_bounds__(256) k_embed_sum(const SumParams p) {
         if (i >= 1 && i <= n) token[i - 1] = p.token[at];
     }
     __syncthreads();
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 8;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x - piece * p.across) * blockDim.x + threadIdx.x) * 8;
     if (c >= p.cols) return;
     const D *const dout = static_cast<const D *>(p.dout);
+    const T *const base = static_cast<const T *>(p.base);
     float sum[8];
     zeros(sum);
     bool whole = row[0] != row[1];              // the row's tokens begin in this piece
     for (int i0 = 0; i0 < n; i0 += AHEAD) {
-        float v[AHEAD][8];
+        Raw<D, WHOLE> v[AHEAD];
+        Raw<T, WHOLE> before[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            if (i0 + u < n) read_eight<D, WHOLE>(dout + token[i0 + u] * p.dout_stride, c, p.cols, v[u]);
-            else zeros(v[u]);
+            const int i = i0 + u;
+            if (i < n) v[u].read(dout + token[i] * p.dout_stride, c, p.cols);
+            before[u] = {};
+            if (base != nullptr && i < n && row[i + 2] != row[i + 1]) before[u].read(base + row[i + 1] * p.base_stride, c, p.cols);
         }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int i = i0 + u;
             if (i >= n) break;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
+            v[u].add_to(sum);
             const int now = row[i + 1], next = row[i + 2];
             if (next == now && i + 1 < n) continue;
             if (whole && next != now) {
-                write_row<T, WHOLE>(p, now, c, sum);
+                float x[8];
+                zeros(x);
+                before[u].add_to(x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = fmaf(sum[e], p.scale, x[e]);
+                write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + now * p.dweight_stride, c, p.cols, x);
             } else {
-                float *const to = p.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (whole ? 1 : 0)) * p.pitch + c;       // pitch: whole vectors
+                float *const to = p.parts + (static_cast<int64_t>(piece) * 2 + (whole ? 1 : 0)) * p.pitch + c;       // pitch: whole vectors
                 *reinterpret_cast<float4 *>(to) = make_float4(sum[0], sum[1], sum[2], sum[3]);
                 *reinterpret_cast<float4 *>(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
             }
@@ -260,7 +304,9 @@ __global__ void __launch_bounds__(256) k_embed_sum(const SumParams p) {
     }
 }
 
-// A row whose tokens go on behind the piece in which they begin: that piece's sum, then the next ones', in order.
+// A row whose tokens go on behind the piece in which they begin: that piece's sum, then the next ones', in order, four
+// columns to a thread and up to JOINED pieces on their way at a time.
+constexpr int JOINED = 16;
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
     let_next_begin();
@@ -269,32 +315,30 @@ __global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
     if (end >= all) return;
     const int row = p.row[end - 1];
     if (p.row[end] != row || (begin > 0 && p.row[begin - 1] == row)) return;
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 8;
+    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 4;
     if (c >= p.cols) return;
-    auto part = [&](int64_t at, float (&v)[8]) {
-        const float4 a = *reinterpret_cast<const float4 *>(p.parts + at * p.pitch + c), b = *reinterpret_cast<const float4 *>(p.parts + at * p.pitch + c + 4);
-        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-    };
-    float sum[8];
-    part(static_cast<int64_t>(blockIdx.x) * 2 + 1, sum);
-    for (int at = end, piece = blockIdx.x + 1; at < all && p.row[at] == row;) {       // four pieces at a time
-        float v[4][8];
-        bool there[4];
+    const float *const parts = p.parts + c;
+    const int64_t last = (p.past[row] - 1) / p.length;       // the piece in which the row's tokens end
+    float4 sum = *reinterpret_cast<const float4 *>(parts + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * p.pitch);
+    for (int64_t piece = blockIdx.x + 1; piece <= last; piece += JOINED) {
+        float4 v[JOINED];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t first = static_cast<int64_t>(at) + static_cast<int64_t>(u) * p.length;
-            there[u] = first < all && p.row[first] == row;
-            if (there[u]) part((static_cast<int64_t>(piece) + u) * 2, v[u]);
-        }
+        for (int u = 0; u < JOINED; ++u)       // (past the last: that again, and not added)
+            v[u] = *reinterpret_cast<const float4 *>(parts + min(piece + u, last) * 2 * p.pitch);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (there[u])
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] += v[u][e];
-        if (!there[3]) break;
-        at += 4 * p.length, piece += 4;         // (at most 2^30 + 4 pieces)
+        for (int u = 0; u < JOINED; ++u)
+            if (piece + u <= last) sum.x += v[u].x, sum.y += v[u].y, sum.z += v[u].z, sum.w += v[u].w;
     }
-    write_row<T, WHOLE>(p, row, c, sum);
+    const float add[4] = {sum.x, sum.y, sum.z, sum.w};
+    T *const to = static_cast<T *>(p.dweight) + row * p.dweight_stride + c;
+    const T *const base = p.base != nullptr ? static_cast<const T *>(p.base) + row * p.base_stride + c : nullptr;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < p.cols) {
+            const float x = fmaf(add[e], p.scale, base != nullptr ? static_cast<float>(base[e]) : 0.0f);
+            if constexpr (sizeof(T) == 2) to[e] = __float2bfloat16_rn(x);
+            else to[e] = x;
+        }
 }
 
 // ---------------------------------------------------------------------------------- host side
@@ -302,18 +346,19 @@ int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // How the gradient's work is cut: from the sizes alone.
 struct Plan {
-    int64_t owners, most, threads, across, length, pieces, pitch, at_row, at_parts, bytes;
+    int64_t owners, most, threads, across, length, pieces, pitch, at_row, at_past, at_parts, bytes;
     Plan(int64_t tokens, int64_t cols, int64_t vocab) {
         // a CTA for each SM, more where a CTA's counts would not fit its shared memory
         owners = std::max<int64_t>(SMS, (vocab + MOST_ROWS - 1) / MOST_ROWS), most = (vocab + owners - 1) / owners;
         const int64_t vectors = (cols + 7) / 8;
         threads = std::min<int64_t>(256, up(vectors, 32)), across = (vectors + threads - 1) / threads;
         // six CTAs of 256 threads to an SM or fewer; short pieces leave more rows to be joined
-        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(32, tokens * across / (SMS * 6 * 256 / threads)));
+        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(16, tokens * across / (SMS * 6 * 256 / threads)));
         pieces = (tokens + length - 1) / length;
         pitch = up(cols, 8);
         int64_t at = 1024 + up(tokens * 4, 1024);      // the list's length and tokens
         at_row = at, at += up(tokens * 4, 1024);
+        at_past = at, at += up(vocab * 4, 1024);
         at_parts = at, at += pieces > 1 ? pieces * 2 * pitch * 4 : 0;
         bytes = at;
     }
@@ -348,22 +393,20 @@ int lookup(const LookupParams &p, bool vectors, cudaStream_t st) {
     return KT_OK;
 }
 
-template <typename T, bool WHOLE>
-int start_list(const ListParams &l, const Plan &plan, cudaStream_t st) {
-    const size_t bytes = static_cast<size_t>(LIST_WARPS * plan.most * 4);
-    if (bytes > 40 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list<T, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB with what is static need no leave
-    k_embed_list<T, WHOLE><<<static_cast<unsigned>(plan.owners), LIST_THREADS, bytes, st>>>(l);
-    KT_CUDA(cudaGetLastError());
-    return KT_OK;
-}
-
 template <typename D, typename T, bool WHOLE>
 int gradient(const ListParams &l, const SumParams &s, const Plan &plan, cudaStream_t st) {
-    if (int rc = start_list<T, WHOLE>(l, plan, st)) return rc;
-    if (plan.pieces == 0) return KT_OK;
-    const dim3 grid(static_cast<unsigned>(plan.pieces), static_cast<unsigned>(plan.across)), block(static_cast<unsigned>(plan.threads));
-    KT_CUDA(launch_behind(k_embed_sum<D, T, WHOLE>, 1, grid, block, 0, st, s));
-    if (plan.pieces > 1) KT_CUDA(launch_behind(k_embed_join<T, WHOLE>, 1, grid, block, 0, st, s));
+    const size_t bytes = static_cast<size_t>(LIST_WARPS * plan.most * 4);
+    if (bytes > 40 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB with what is static need no leave
+    k_embed_list<<<static_cast<unsigned>(plan.owners), LIST_THREADS, bytes, st>>>(l);
+    KT_CUDA(cudaGetLastError());
+    const int64_t fillers = s.base == s.dweight ? 0 : (s.vocab + s.rows_each - 1) / s.rows_each, blocks = plan.pieces * plan.across + fillers;
+    if (blocks > INT32_MAX) return fail(KT_ERR_SHAPE, "tokens x columns are too many");
+    if (blocks == 0) return KT_OK;
+    KT_CUDA(launch_behind(k_embed_sum<D, T, WHOLE>, 1, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(plan.threads)), 0, st, s));
+    if (plan.pieces > 1) {
+        const int64_t fours = (s.cols + 3) / 4, threads = std::min<int64_t>(256, up(fours, 32));
+        KT_CUDA(launch_behind(k_embed_join<T, WHOLE>, 1, dim3(static_cast<unsigned>(plan.pieces), static_cast<unsigned>((fours + threads - 1) / threads)), dim3(static_cast<unsigned>(threads)), 0, st, s));
+    }
     return KT_OK;
 }
 
@@ -403,9 +446,13 @@ int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids,
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return fail(KT_ERR_ALIGN, "workspace is not 16-byte aligned");
     char *const ws = static_cast<char *>(workspace);
     int *const count = reinterpret_cast<int *>(ws), *const token = reinterpret_cast<int *>(ws + 1024), *const row = reinterpret_cast<int *>(ws + plan.at_row);
-    const ListParams l{ids, token, row, count, base, dweight, base_stride, dweight_stride, cols, static_cast<int>(tokens), static_cast<int>(vocab), static_cast<int>(plan.owners), static_cast<int>(plan.most),
+    int *const past = reinterpret_cast<int *>(ws + plan.at_past);
+    const ListParams l{ids, token, row, count, past, static_cast<int>(tokens), static_cast<int>(vocab), static_cast<int>(plan.owners), static_cast<int>(plan.most),
                        static_cast<unsigned>((UINT64_C(1) << 32) / static_cast<uint64_t>(plan.owners))};
-    const SumParams s{token, row, count, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(plan.length), scale};
+    // CTAs that fill take 16 vectors to a thread
+    const int64_t rows_each = std::max<int64_t>(1, plan.threads * 16 * 8 / cols);
+    const SumParams s{token, row, count, past, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(plan.length),
+                      static_cast<int>(plan.pieces), static_cast<int>(plan.across), static_cast<int>(vocab), static_cast<int>(rows_each), scale};
     const bool vectors = (tokens == 0 || whole(dout, dout_stride, tokens, dtype)) && whole(dweight, dweight_stride, vocab, param_dtype) && (base == nullptr || whole(base, base_stride, vocab, param_dtype));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (param_dtype == KT_F32) {

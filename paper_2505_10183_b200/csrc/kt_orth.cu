@@ -19,6 +19,7 @@
 
 #include "kt_eight.cuh"
 #include "kt_internal.h"
+#include "kt_pairs.cuh"
 #include "kt_product.cuh"
 
 using namespace ktd;
@@ -26,7 +27,7 @@ using namespace ktd;
 namespace {
 
 constexpr float X_UNIT = 128.0f, A_UNIT = 16384.0f, FACTOR_UNIT = 8192.0f;
-constexpr int SUM_BLOCKS = 64;                  // partial sums of squares to a matrix
+constexpr int SUM_BLOCKS = 256;                 // partial sums of squares to a matrix, at most: a thread reads one
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
     uint32_t r;
@@ -40,6 +41,7 @@ struct StartParams {
     int64_t stride[2];                          // matrix, row
     int64_t rows, cols, pitch;                  // pitch: of X, in elements
     double *sums;
+    int sum_blocks;                             // CTAs, each with a sum, to a matrix
     __half *to;
 };
 
@@ -48,54 +50,79 @@ template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_orth_squares(const StartParams p) {
     __shared__ double of_warp[8];
     let_next_begin();
-    const int64_t pieces = (p.cols + 7) / 8, all = p.rows * pieces;
+    const uint32_t cols = static_cast<uint32_t>(p.cols), pieces = (cols + 7) / 8, all = static_cast<uint32_t>(p.rows) * pieces, step = gridDim.x * 256;      // 2^29 pieces at most
     const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0];
-    double sum = 0.0;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += SUM_BLOCKS * 256) {
-        const int64_t r = i / pieces, c = (i - r * pieces) * 8;
-        float v[8];
-        read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v);
+    double sum[2] = {0.0, 0.0};
+    for (uint32_t i0 = blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
+        float v[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += static_cast<double>(v[e]) * v[e];
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t i = i0 + u * step, r = i < all ? i / pieces : 0, c = i < all ? (i - r * pieces) * 8 : cols;      // (past the last column: zeros)
+            read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const double d = v[u][e];
+                sum[e % 2] = fma(d, d, sum[e % 2]);
+            }
     }
+    double all_of = sum[0] + sum[1];
 #pragma unroll
-    for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
-    if (threadIdx.x % 32 == 0) of_warp[threadIdx.x / 32] = sum;
+    for (int far = 16; far; far /= 2) all_of += __shfl_xor_sync(0xFFFFFFFFu, all_of, far);
+    if (threadIdx.x % 32 == 0) of_warp[threadIdx.x / 32] = all_of;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) sum += of_warp[w];
-        p.sums[blockIdx.y * SUM_BLOCKS + blockIdx.x] = sum;
+        for (int w = 1; w < 8; ++w) all_of += of_warp[w];
+        p.sums[blockIdx.y * gridDim.x + blockIdx.x] = all_of;
     }
 }
 
 // X = G / |G| in fp16.  A matrix of zeros stays one; one with an infinity or a NaN becomes NaN throughout.
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_orth_start(const StartParams p) {
+    __shared__ double of_warp[8];
     let_next_begin();
     after_previous();
-    const int64_t pieces = (p.cols + 7) / 8, all = p.rows * pieces;
-    double sum = 0.0;
-    for (int i = 0; i < SUM_BLOCKS; ++i) sum += p.sums[blockIdx.y * SUM_BLOCKS + i];
+    const uint32_t cols = static_cast<uint32_t>(p.cols), pieces = (cols + 7) / 8, all = static_cast<uint32_t>(p.rows) * pieces, step = gridDim.x * 256;      // 2^29 pieces at most
+    double sum = static_cast<int>(threadIdx.x) < p.sum_blocks ? p.sums[blockIdx.y * p.sum_blocks + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
+    if (threadIdx.x % 32 == 0) of_warp[threadIdx.x / 32] = sum;
+    __syncthreads();
+    sum = of_warp[0];
+    for (int w = 1; w < 8; ++w) sum += of_warp[w];
     const double by = sum == 0.0 ? 0.0 : isfinite(sum) ? X_UNIT / sqrt(sum) : __longlong_as_double(0x7FF8000000000000ll);
+    const bool narrow = by < 1e30 && by > 1e-30;       // fp32 holds the factor
+    const float by32 = static_cast<float>(by);
     const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0];
     __half *const to = p.to + blockIdx.y * p.rows * p.pitch;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int64_t r = i / pieces, c = (i - r * pieces) * 8;
-        float v[8];
-        read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v);
+    for (uint32_t i0 = blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
+        float v[4][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(v[e] * by);
-        uint4 u;
-        u.x = pack_half(v[0], v[1]), u.y = pack_half(v[2], v[3]), u.z = pack_half(v[4], v[5]), u.w = pack_half(v[6], v[7]);
-        *reinterpret_cast<uint4 *>(to + r * p.pitch + c) = u;
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t i = i0 + u * step, r = i < all ? i / pieces : 0, c = i < all ? (i - r * pieces) * 8 : cols;
+            read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t i = i0 + u * step, r = i / pieces, c = (i - r * pieces) * 8;
+            if (i >= all) break;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[u][e] = narrow ? v[u][e] * by32 : static_cast<float>(v[u][e] * by);
+            uint4 w;
+            w.x = pack_half(v[u][0], v[u][1]), w.y = pack_half(v[u][2], v[u][3]), w.z = pack_half(v[u][4], v[u][5]), w.w = pack_half(v[u][6], v[u][7]);
+            *reinterpret_cast<uint4 *>(to + r * p.pitch + c) = w;
+        }
     }
 }
 
 // ------------------------------------------------------------------------------------ products
 struct OrthParams {
     int rows, cols, tiles_m, tiles_n, batch, steps;        // of the result; stages of the reduction
+    int whole;                                  // both sides of a symmetric result are computed
     int64_t pitch;                              // of a symmetric result, in elements
-    __half *result;                             // the symmetric result, whose mirrored side is written to memory as it is
     const __half *gram;                         // A, for the factor
     float a, b, c;
     void *out;                                  // of the last product
@@ -103,102 +130,110 @@ struct OrthParams {
 };
 
 // 32 values of the thread's row as fp16 into half of the store's rows.
-__device__ __forceinline__ void pack_halves(const Part &part, int c, const float (&x)[32]) {
+__device__ __forceinline__ void pack_halves(const Part &part, int half, const float (&x)[32]) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         uint4 v;
         v.x = pack_half(x[u * 8], x[u * 8 + 1]), v.y = pack_half(x[u * 8 + 2], x[u * 8 + 3]), v.z = pack_half(x[u * 8 + 4], x[u * 8 + 5]), v.w = pack_half(x[u * 8 + 6], x[u * 8 + 7]);
-        *part.piece((c % 64) / 8 + u) = v;
+        *part.piece(half * 4 + u) = v;
     }
 }
 
 // A symmetric matrix: A (FACTOR false, from X along or down its rows) or the factor a I + b A + c A^2 (from A).
+// The mirrored side of 32 x 32 values goes through shared memory, where lanes are columns: two lanes swap halves, so
+// that each writes two neighbours of one row.  (Two-byte stores straight to memory took 27 us to a tile, more than its product.)
 template <bool PAIR_, bool DOWN, bool FACTOR>
-struct SymmetricTask {
+struct SymmetricTask : InTurn<SymmetricTask<PAIR_, DOWN, FACTOR>, OrthParams> {
     using Params = OrthParams;
-    static constexpr bool PAIR = PAIR_, A_DOWN = DOWN, B_DOWN = DOWN, HALF = true;
+    static constexpr bool PAIR = PAIR_, HALF = true;
     static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles(const Params &p) { return p.tiles_m * (p.tiles_m + 1) / 2 * p.batch; }
-    __device__ static bool second_a(const Params &) { return false; }
-    __device__ static bool second_b(const Params &) { return false; }
-    __device__ static Tile tile(const Params &p, int i) {
-        const int each = p.tiles_m * (p.tiles_m + 1) / 2, z = i / each;
-        int m = 0, n = i - z * each;
+    __device__ static int each(const Params &p) { return p.whole ? p.tiles_m * p.tiles_m : p.tiles_m * (p.tiles_m + 1) / 2; }
+    __device__ static int tiles(const Params &p) { return each(p) * p.batch; }
+    __device__ static bool a_down(const Tile &) { return DOWN; }
+    __device__ static bool b_down(const Tile &) { return DOWN; }
+    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &) { return &maps.a; }
+    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
+    __device__ static Tile tile_at(const Params &p, int i) {
+        const int z = i / each(p);
+        int m = 0, n = i - z * each(p);
+        if (p.whole) return {n / p.tiles_m * SIDE, n % p.tiles_m * SIDE, z, 0, p.steps, 0, 0};
         for (; n >= p.tiles_m - m; ++m) n -= p.tiles_m - m;
-        return {m * SIDE, (m + n) * SIDE, z, 0, p.steps, 0};
+        return {m * SIDE, (m + n) * SIDE, z, 0, p.steps, 0, 0};
     }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, const Part &part) {
+    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
         if (part.warp_row >= p.rows) return;
-        const int64_t matrix = static_cast<int64_t>(t.z) * p.rows * p.pitch;
         const int lane = threadIdx.x % 32;
-        over_columns<SIDE>(part, [&](int c, uint32_t (&r)[32]) {
+        const bool mirrored = !p.whole && t.n != t.m;
+        uint4 g[4] = {};
+        auto of_gram = [&](int c0) {            // (rows of A are whole vectors, whatever lies past their last element)
+            if (!FACTOR || part.row >= p.rows || c0 >= p.rows) return;
+            const uint4 *from = reinterpret_cast<const uint4 *>(p.gram + (static_cast<int64_t>(t.z) * p.rows + part.row) * p.pitch + c0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) g[u] = from[u];
+        };
+        of_gram(t.n);
+        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
             const int c0 = t.n + c;
-            if (c0 - c % 64 >= p.rows) return;
-            if (c % 64 == 0) part.store_free();
-            float x[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(r[e]);
-            if constexpr (FACTOR) {
-                uint4 g[4] = {};
-                if (part.row < p.rows && c0 < p.rows) {       // (rows of A are whole vectors, whatever lies past their last element)
-                    const uint4 *from = reinterpret_cast<const uint4 *>(p.gram + matrix + part.row * p.pitch + c0);
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) g[u] = from[u];
-                }
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const uint32_t w = e % 8 / 2 == 0 ? g[e / 8].x : e % 8 / 2 == 1 ? g[e / 8].y : e % 8 / 2 == 2 ? g[e / 8].z : g[e / 8].w;
-                    const float in = __half2float(__ushort_as_half(static_cast<unsigned short>(e % 2 ? w >> 16 : w & 0xFFFF)));
-                    x[e] = fmaf(in, p.b * (FACTOR_UNIT / A_UNIT), x[e] * (p.c * (FACTOR_UNIT / A_UNIT / A_UNIT)));
-                }
-                const int d = part.row - c0;
-                if (static_cast<unsigned>(d) < 32u)
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (e == d) x[e] += p.a * FACTOR_UNIT;
-            }
-            pack_halves(part, c, x);
-            if (c % 64 == 32) part.send(&maps.out, c0 - 32, part.warp_row, t.z);
-            if (t.n == t.m) return;
-            // the mirrored side: lanes are columns there.  Two lanes swap so that each writes two columns of one row.
-            __half *const to = p.result + matrix;
-            const int even = part.warp_row + (lane & ~1);
+            if (c0 >= p.rows) return;
+            uint32_t v[16];
+            [[maybe_unused]] const int d = part.row - c0;
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-                const uint32_t mine = pack_half(x[e], x[e + 1]), theirs = __shfl_xor_sync(0xFFFFFFFFu, mine, 1);
-                const uint32_t v = lane & 1 ? (theirs >> 16) | (mine & 0xFFFF0000u) : (mine & 0xFFFFu) | (theirs << 16);
-                const int row = c0 + e + (lane & 1);
-                if (row < p.rows && even < p.rows) *reinterpret_cast<uint32_t *>(to + row * p.pitch + even) = v;      // (an even pitch: the second may be the padding's)
+                float2 x = pair_of(r, e);
+                if constexpr (FACTOR) {
+                    const uint32_t w = e % 8 / 2 == 0 ? g[e / 8].x : e % 8 / 2 == 1 ? g[e / 8].y : e % 8 / 2 == 2 ? g[e / 8].z : g[e / 8].w;
+                    const float2 in = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+                    x = fma2(in, both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(x, both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
+                    if (e == d) x.x += p.a * FACTOR_UNIT;
+                    if (e + 1 == d) x.y += p.a * FACTOR_UNIT;
+                }
+                v[e / 2] = pack_half(x.x, x.y);
             }
+            of_gram(c0 + 32);
+            part.store_next();
+#pragma unroll
+            for (int u = 0; u < 4; ++u)         // rows of 64 bytes, in the 64-byte swizzle
+                *reinterpret_cast<uint4 *>(part.store + lane * 64 + ((u ^ (lane / 2 & 3)) << 4)) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
+            if (mirrored) {
+                uint8_t *const mirror = part.store + STORE_BYTES / 2 + (lane & 1) * 64 + (lane & ~1) * 2;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t theirs = __shfl_xor_sync(0xFFFFFFFFu, v[e], 1);
+                    *reinterpret_cast<uint32_t *>(mirror + e * 128) = lane & 1 ? (theirs >> 16) | (v[e] & 0xFFFF0000u) : (v[e] & 0xFFFFu) | (theirs << 16);
+                }
+            }
+            part.send(&maps.out, c0, part.warp_row, t.z, false, mirrored ? &maps.out2 : nullptr, STORE_BYTES / 2, part.warp_row, c0);
         });
     }
 };
 
 // The next X: factor times X (WIDE), or X times factor; the last time to the result.
 template <bool PAIR_, bool WIDE, bool LAST>
-struct ApplyTask {
+struct ApplyTask : InTurn<ApplyTask<PAIR_, WIDE, LAST>, OrthParams> {
     using Params = OrthParams;
-    static constexpr bool PAIR = PAIR_, A_DOWN = false, B_DOWN = WIDE, HALF = true;
+    static constexpr bool PAIR = PAIR_, HALF = true;
     static constexpr int SIDE = PAIR ? 256 : 128;
     __device__ static int tiles(const Params &p) { return p.tiles_m * p.tiles_n * p.batch; }
-    __device__ static bool second_a(const Params &) { return false; }
-    __device__ static bool second_b(const Params &) { return false; }
-    __device__ static Tile tile(const Params &p, int i) {
+    __device__ static bool a_down(const Tile &) { return false; }
+    __device__ static bool b_down(const Tile &) { return WIDE; }
+    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &) { return &maps.a; }
+    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
+    __device__ static Tile tile_at(const Params &p, int i) {
         const int each = p.tiles_m * p.tiles_n, z = i / each, in = i - z * each, band = in / (8 * p.tiles_n), left = in - band * 8 * p.tiles_n, high = min(8, p.tiles_m - band * 8);
-        return {(band * 8 + left % high) * SIDE, left / high * SIDE, z, 0, p.steps, 0};
+        return {(band * 8 + left % high) * SIDE, left / high * SIDE, z, 0, p.steps, 0, 0};
     }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, const Part &part) {
+    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
         if (part.warp_row >= p.rows) return;
-        over_columns<SIDE>(part, [&](int c, uint32_t (&r)[32]) {
+        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
             const int c0 = t.n + c;
-            if (c0 - c % 64 >= p.cols) return;
+            if (c0 - half * 32 >= p.cols) return;
             float x[32];
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(r[e]) * p.a;
             if constexpr (!LAST) {
-                if (c % 64 == 0) part.store_free();
-                pack_halves(part, c, x);
-                if (c % 64 == 32) part.send(&maps.out, c0 - 32, part.warp_row, t.z);
+                if (half == 0) part.store_next();
+                pack_halves(part, half, x);
+                if (half == 1) part.send(&maps.out, c0 - 32, part.warp_row, t.z);
             } else if (part.row < p.rows && c0 < p.cols) {
                 __nv_bfloat16 *const row = static_cast<__nv_bfloat16 *>(p.out) + t.z * p.out_stride[0] + part.row * p.out_stride[1] + c0;
                 if (c0 + 32 <= p.cols && reinterpret_cast<uintptr_t>(row) % 16 == 0) {
@@ -260,21 +295,25 @@ int run(const Plan &plan, char *ws, int steps, float a, float b, float c, float 
     char *const gram = ws + plan.at_gram, *const factor = ws + plan.at_factor;
     ProductMaps g{}, f{}, x{};
     const CUtensorMapDataType half = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    if (int rc = describe_matrix(&g.out, "the workspace", half, 2, gram, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a, 64, 32)) return rc;
+    for (int i = 0; i < 4; ++i)       // what both write, and its mirrored side
+        if (int rc = describe_matrix(i == 0 ? &g.out : i == 1 ? &g.out2 : i == 2 ? &f.out : &f.out2, "the workspace", half, 2, i < 2 ? gram : factor, plan.side, plan.side, plan.batch, plan.pitch_a * 2,
+                                     matrix_a, 32, 32, i % 2 == 0))
+            return rc;
     if (int rc = describe_operand(&f.a, "the workspace", true, false, gram, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a)) return rc;
     f.b = f.a;
-    if (int rc = describe_matrix(&f.out, "the workspace", half, 2, factor, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a, 64, 32)) return rc;
     CUtensorMap of_factor;
     if (int rc = describe_operand(&of_factor, "the workspace", true, false, factor, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a)) return rc;
     OrthParams pg{};
     pg.rows = pg.cols = static_cast<int>(plan.side), pg.tiles_m = pg.tiles_n = static_cast<int>(symmetric), pg.batch = static_cast<int>(plan.batch), pg.pitch = plan.pitch_a;
+    // Where every tile of the whole square gets a worker of its own, mirroring would only make each take longer.
+    pg.whole = symmetric * symmetric * plan.batch <= PRODUCT_SMS / (PAIR ? 2 : 1);
     OrthParams pf = pg, px{};
-    pg.steps = static_cast<int>(tiles_of(plan.wide ? plan.cols : plan.rows, K_STEP)), pg.result = reinterpret_cast<__half *>(gram);
-    pf.steps = static_cast<int>(tiles_of(plan.side, K_STEP)), pf.result = reinterpret_cast<__half *>(factor), pf.gram = reinterpret_cast<const __half *>(gram);
+    pg.steps = static_cast<int>(tiles_of(plan.wide ? plan.cols : plan.rows, K_STEP));
+    pf.steps = static_cast<int>(tiles_of(plan.side, K_STEP)), pf.gram = reinterpret_cast<const __half *>(gram);
     pf.a = a, pf.b = b, pf.c = c;
     px.rows = static_cast<int>(plan.rows), px.cols = static_cast<int>(plan.cols), px.tiles_m = static_cast<int>(tiles_of(plan.rows, SIDE)), px.tiles_n = static_cast<int>(tiles_of(plan.cols, SIDE));
     px.batch = pg.batch, px.steps = pf.steps, px.out = out, px.out_stride[0] = out_stride[0], px.out_stride[1] = out_stride[1];
-    const int64_t tiles_a = symmetric * (symmetric + 1) / 2 * plan.batch, tiles_x = static_cast<int64_t>(px.tiles_m) * px.tiles_n * plan.batch;
+    const int64_t tiles_a = (pg.whole ? symmetric * symmetric : symmetric * (symmetric + 1) / 2) * plan.batch, tiles_x = static_cast<int64_t>(px.tiles_m) * px.tiles_n * plan.batch;
     for (int i = 0; i < steps; ++i) {
         char *const now = ws + plan.at_x[i % 2], *const next = ws + plan.at_x[(i + 1) % 2];
         const bool last = i + 1 == steps;
@@ -296,9 +335,11 @@ int run(const Plan &plan, char *ws, int steps, float a, float b, float c, float 
 }
 
 template <typename T>
-int start(const StartParams &p, const Plan &plan, bool whole, cudaStream_t st) {
-    const int64_t blocks = (plan.rows * ((plan.cols + 7) / 8) + 255) / 256, most = 4 * PRODUCT_SMS;
-    const dim3 sums(SUM_BLOCKS, static_cast<unsigned>(plan.batch)), grid(static_cast<unsigned>(blocks < most ? blocks : most), static_cast<unsigned>(plan.batch));
+int start(StartParams &p, const Plan &plan, bool whole, cudaStream_t st) {
+    // a thread takes four pieces at a time; eight CTAs to an SM over all matrices
+    const int64_t blocks = (plan.rows * ((plan.cols + 7) / 8) + 1023) / 1024, most = (8 * PRODUCT_SMS + plan.batch - 1) / plan.batch, used = blocks < most ? blocks : most;
+    p.sum_blocks = static_cast<int>(used < SUM_BLOCKS ? used : SUM_BLOCKS);
+    const dim3 sums(static_cast<unsigned>(p.sum_blocks), static_cast<unsigned>(plan.batch)), grid(static_cast<unsigned>(used), static_cast<unsigned>(plan.batch));
     whole ? k_orth_squares<T, true><<<sums, 256, 0, st>>>(p) : k_orth_squares<T, false><<<sums, 256, 0, st>>>(p);
     KT_CUDA(cudaGetLastError());
     KT_CUDA(launch_behind(whole ? k_orth_start<T, true> : k_orth_start<T, false>, 1, grid, dim3(256), 0, st, p));

@@ -12,13 +12,18 @@
 // reduction runs from row to row).  What lies outside of a matrix arrives as zeros.
 //
 // A Task says what the tiles are and what becomes of their sums:
-//   Params, PAIR, A_DOWN, B_DOWN, HALF (fp16 operands instead of bf16)
-//   int tiles(p)             how many tiles there are
-//   Tile tile(p, i)          the i-th
-//   bool second_a / b(p)     whether operand A / B is read through its second description
+//   Params, PAIR, HALF (fp16 operands instead of bf16)
+//   int count(p, worker, workers)                  how many tiles a worker (a CTA or a pair) does
+//   Tile tile(p, worker, workers, i)               its i-th
+//   bool a_down / b_down(tile)                     how the operands are read
+//   const CUtensorMap *map_a / map_b(maps, p, tile)
 //   void finish(p, maps, tile, part)
 // Waits are bounded (kt_tensor.cuh).  A tile whose sums never came is finished with NaN in their place.
 #pragma once
+
+#include <algorithm>
+#include <atomic>
+#include <cstring>
 
 #include "kt_internal.h"
 #include "kt_tensor.cuh"
@@ -26,23 +31,30 @@
 namespace {
 
 constexpr int K_STEP = 64;                                // elements of the reduction to a stage: 128 bytes
-constexpr int STAGES = 6;
+constexpr int STAGES = 5;
 constexpr uint32_t OPERAND_BYTES = TILE * K_STEP * 2, STAGE_BYTES = 2 * OPERAND_BYTES, STORE_BYTES = 32 * 128;
 constexpr int PRODUCT_THREADS = 384, PRODUCT_LOAD = 0, PRODUCT_ISSUE = 1, PRODUCT_MEMORY = 2, PRODUCT_FINISH = 4;      // warps
 constexpr int PRODUCT_SMS = 148;                          // of a B200, one CTA to each
 
 struct Tile {
     int m, n, z, k, steps;                                // first row and column, matrix of the batch, first element and stages of the reduction (0: zeros)
-    int share;                                            // the Task's own
+    int kind, share;                                      // the Task's own
 };
 
 // One 16-bit or fp32 matrix (or a batch of them) as the copy engine sees it, and the operands of a product.
 struct ProductMaps {
-    CUtensorMap a, a2, b, b2, out;
+    CUtensorMap a, a2, b, b2, b3, out, out2;
+};
+
+// Tiles that all workers do in turn: a Task with tiles(p) and tile_at(p, i).
+template <class Task, class Params>
+struct InTurn {
+    __device__ static int count(const Params &p, int worker, int workers) { return (Task::tiles(p) - worker + workers - 1) / workers; }
+    __device__ static Tile tile(const Params &p, int worker, int workers, int i) { return Task::tile_at(p, worker + i * workers); }
 };
 
 struct ProductSmem {
-    alignas(1024) uint8_t a[STAGES][OPERAND_BYTES], b[STAGES][OPERAND_BYTES], store[8][STORE_BYTES];
+    alignas(1024) uint8_t a[STAGES][OPERAND_BYTES], b[STAGES][OPERAND_BYTES], store[8][2][STORE_BYTES];
     uint64_t full[STAGES], free[STAGES], sums_full[2], sums_taken[2];
     uint32_t tmem;
     Patience waits;
@@ -70,9 +82,9 @@ __device__ __forceinline__ void store_box(const CUtensorMap *map, uint32_t from,
         asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(from), "r"(x), "r"(y), "r"(z) : "memory");
     else
         asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(from), "r"(x), "r"(y), "r"(z) : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
-__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }      // their places may be filled again
+__device__ __forceinline__ void stores_sent() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read_but_one() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }      // the places of those before may be filled again
 __device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 template <bool PAIR>
@@ -110,22 +122,45 @@ __device__ __forceinline__ void arrive_at(uint32_t bar) {       // a barrier of 
 
 // Words of the matrix instruction and of the operands.  Both operands' rows (or, read down, their 16 K rows) are 128
 // bytes in the 128-byte swizzle; read down, chunks of 64 columns are 64 rows apart.
-template <bool PAIR, bool A_DOWN, bool B_DOWN, bool HALF>
-__host__ __device__ constexpr uint32_t product_word() {
-    return (1u << 4) | (HALF ? 0u : (1u << 7) | (1u << 10)) | (A_DOWN ? 1u << 15 : 0u) | (B_DOWN ? 1u << 16 : 0u) | (static_cast<uint32_t>((PAIR ? 256 : 128) / 8) << 17) |
+template <bool PAIR, bool HALF>
+__device__ __forceinline__ uint32_t product_word(bool a_down, bool b_down) {
+    return (1u << 4) | (HALF ? 0u : (1u << 7) | (1u << 10)) | (a_down ? 1u << 15 : 0u) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>((PAIR ? 256 : 128) / 8) << 17) |
            (static_cast<uint32_t>((PAIR ? 256 : 128) / 16) << 24);
 }
 constexpr uint64_t PRODUCT_DOWN = (static_cast<uint64_t>((K_STEP * 128) >> 4) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+
+// One operand's part of a stage: 128 rows of 64 elements of the reduction, or 64 rows (of the reduction) of 128.
+template <bool PAIR>
+__device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap *map, uint32_t bar, bool down, int row, int k, int z) {
+    if (down) {
+        load_box<PAIR>(to, map, bar, row, k, z);
+        load_box<PAIR>(to + OPERAND_BYTES / 2, map, bar, row + 64, k, z);
+    } else {
+        load_box<PAIR>(to, map, bar, k, row, z);
+    }
+}
 
 // ----------------------------------------------------------------------------- finishing
 // What a thread of the finishing warps has of a tile: a row, and its sums 32 columns at a time.
 struct Part {
     int row;                                    // of C
     uint32_t at;                                // its sums in tensor memory
-    uint8_t *store;                             // of the warp: 32 rows of 128 bytes
+    uint8_t *store;                             // of the warp: 32 rows of 128 bytes, of two places the one in turn
+    int turn;
     int warp_row;                               // the warp's first row of C
     bool there;                                 // else NaN
     bool zero;                                  // nothing to sum
+    uint64_t *full;                             // what the sums are waited for with
+    uint32_t parity;
+    volatile Patience *waits;
+    bool waited;
+    // The sums are there (a Task may do something else before; over_columns waits by itself).
+    __device__ __forceinline__ void wait() {
+        if (waited) return;
+        waited = true;
+        there = there && bar_wait(full, parity, waits);
+        tmem_fence_after();
+    }
     __device__ __forceinline__ void ask(int c, uint32_t (&r)[32]) const {
         if (there && !zero) tmem_load32(at + c, r);
     }
@@ -142,27 +177,44 @@ struct Part {
         const int r = threadIdx.x % 32;
         return reinterpret_cast<uint4 *>(store + r * 128 + ((unit ^ (r & 7)) << 4));
     }
-    __device__ __forceinline__ void store_free() const {
-        if (threadIdx.x % 32 == 0) stores_read();
+    // The other place, once what was sent from it has been read.
+    __device__ __forceinline__ void store_next() {
+        if (threadIdx.x % 32 == 0) stores_read_but_one();
         __syncwarp();
+        turn ^= 1;
+        store += turn ? static_cast<int>(STORE_BYTES) : -static_cast<int>(STORE_BYTES);
     }
-    __device__ __forceinline__ void send(const CUtensorMap *map, int x, int y, int z, bool add = false) const {
+    // What the warp has put there goes to (x, y, z); and, from `second` on, to (x2, y2, z) of a second matrix.
+    __device__ __forceinline__ void send(const CUtensorMap *map, int x, int y, int z, bool add = false, const CUtensorMap *map2 = nullptr, int second = 0, int x2 = 0, int y2 = 0) const {
         fence_async_smem();
         __syncwarp();
-        if (threadIdx.x % 32 == 0) store_box(map, smem_addr(store), x, y, z, add);
+        if (threadIdx.x % 32 == 0) {
+            store_box(map, smem_addr(store), x, y, z, add);
+            if (map2 != nullptr) store_box(map2, smem_addr(store) + second, x2, y2, z, false);
+            stores_sent();
+        }
     }
 };
 
-// f(column, sums of 32 columns) for COLS columns of the thread's row; the next columns are on their way meanwhile.
+// f(column, whether it is the second of two, sums of 32 columns) for COLS columns of the thread's row, 64 at a time; the next
+// columns are on their way meanwhile.
+template <int N>
+struct Constant {
+    __device__ constexpr operator int() const { return N; }
+};
 template <int COLS, typename F>
-__device__ __forceinline__ void over_columns(const Part &part, F f) {
+__device__ __forceinline__ void over_columns(Part &part, F f) {
     uint32_t r[2][32];
+    part.wait();
     part.ask(0, r[0]);
-#pragma unroll
-    for (int c = 0; c < COLS; c += 32) {
-        part.get(r[c / 32 % 2]);
-        if (c + 32 < COLS) part.ask(c + 32, r[(c / 32 + 1) % 2]);
-        f(c, r[c / 32 % 2]);
+#pragma unroll 1
+    for (int c = 0; c < COLS; c += 64) {
+        part.get(r[0]);
+        part.ask(c + 32, r[1]);
+        f(c, Constant<0>(), r[0]);
+        part.get(r[1]);
+        if (c + 64 < COLS) part.ask(c + 64, r[0]);
+        f(c + 32, Constant<1>(), r[1]);
     }
 }
 
@@ -176,7 +228,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     auto &sm = *reinterpret_cast<ProductSmem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = PAIR ? rank_in_pair() : 0;
-    const int first = PAIR ? blockIdx.x / 2 : blockIdx.x, stride = PAIR ? gridDim.x / 2 : gridDim.x;
+    const int worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
 
     let_next_begin();
     if (threadIdx.x == 0) {
@@ -186,6 +238,8 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
+    if (warp == PRODUCT_LOAD && lane < static_cast<int>(sizeof(ProductMaps) / sizeof(CUtensorMap)))       
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a + lane)) : "memory");
     if (warp == PRODUCT_MEMORY) sums_alloc<PAIR>(&sm.tmem, COLUMNS);
     tmem_fence_before();
     if constexpr (PAIR) cluster_sync();
@@ -194,54 +248,44 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     const uint32_t tmem = sm.tmem;
     volatile Patience *waits = &sm.waits;
     after_previous();
-    const int tiles = Task::tiles(p);
+    const int tiles = Task::count(p, worker, workers);
 
     if (warp == PRODUCT_LOAD) {
         if (lane == 0) {
-            const CUtensorMap *const map_a = Task::second_a(p) ? &maps.a2 : &maps.a, *const map_b = Task::second_b(p) ? &maps.b2 : &maps.b;
             uint32_t stage = 0, round = 0;
             bool ok = true;
-            for (int i = first; ok && i < tiles; i += stride) {
-                const Tile t = Task::tile(p, i);
+            for (int i = 0; ok && i < tiles; ++i) {
+                const Tile t = Task::tile(p, worker, workers, i);
+                const CUtensorMap *const map_a = Task::map_a(maps, p, t), *const map_b = Task::map_b(maps, p, t);
                 const int m = t.m + static_cast<int>(rank) * TILE, n = t.n + static_cast<int>(rank) * TILE;
                 for (int s = 0; s < t.steps; ++s) {
                     if (!(ok = bar_wait_one(&sm.free[stage], (round + 1) & 1, waits))) break;
                     const uint32_t bar = PAIR ? address_in(smem_addr(&sm.full[stage]), 0) : smem_addr(&sm.full[stage]);
                     if (rank == 0) bar_expect(&sm.full[stage], PAIR ? 2 * STAGE_BYTES : STAGE_BYTES);
                     const int k = t.k + s * K_STEP;
-                    const uint32_t a = smem_addr(sm.a[stage]), b = smem_addr(sm.b[stage]);
-                    if constexpr (Task::A_DOWN) {
-                        load_box<PAIR>(a, map_a, bar, m, k, t.z);
-                        load_box<PAIR>(a + OPERAND_BYTES / 2, map_a, bar, m + 64, k, t.z);
-                    } else {
-                        load_box<PAIR>(a, map_a, bar, k, m, t.z);
-                    }
-                    if constexpr (Task::B_DOWN) {
-                        load_box<PAIR>(b, map_b, bar, n, k, t.z);
-                        load_box<PAIR>(b + OPERAND_BYTES / 2, map_b, bar, n + 64, k, t.z);
-                    } else {
-                        load_box<PAIR>(b, map_b, bar, k, n, t.z);
-                    }
+                    load_operand<PAIR>(smem_addr(sm.a[stage]), map_a, bar, Task::a_down(t), m, k, t.z);
+                    load_operand<PAIR>(smem_addr(sm.b[stage]), map_b, bar, Task::b_down(t), n, k, t.z);
                     if (++stage == STAGES) stage = 0, ++round;
                 }
             }
         }
     } else if (warp == PRODUCT_ISSUE) {
         if (rank == 0 && elected()) {
-            constexpr uint32_t word = product_word<PAIR, Task::A_DOWN, Task::B_DOWN, Task::HALF>();
-            constexpr uint32_t step_a = Task::A_DOWN ? 2048 >> 4 : 32 >> 4, step_b = Task::B_DOWN ? 2048 >> 4 : 32 >> 4;
-            uint32_t stage = 0, round = 0, done = 0;
+            uint32_t stage = 0, round = 0;
             bool ok = true;
-            for (int i = first; ok && i < tiles; i += stride, ++done) {
-                const Tile t = Task::tile(p, i);
+            for (int done = 0; ok && done < tiles; ++done) {
+                const Tile t = Task::tile(p, worker, workers, done);
+                const bool a_down = Task::a_down(t), b_down = Task::b_down(t);
+                const uint32_t word = product_word<PAIR, Task::HALF>(a_down, b_down), step_a = a_down ? 2048 >> 4 : 32 >> 4, step_b = b_down ? 2048 >> 4 : 32 >> 4;
+                const uint64_t word_a = a_down ? PRODUCT_DOWN : OPERAND_ALONG, word_b = b_down ? PRODUCT_DOWN : OPERAND_ALONG;
                 if (!(ok = bar_wait_one(&sm.sums_taken[done & 1], (done / 2 + 1) & 1, waits))) break;
                 tmem_fence_after();
                 const uint32_t d = tmem + (done & 1) * SIDE;
                 for (int s = 0; s < t.steps; ++s) {
                     if (!(ok = bar_wait_one(&sm.full[stage], round & 1, waits))) break;
                     tmem_fence_after();
-                    const uint64_t a = operand(Task::A_DOWN ? PRODUCT_DOWN : OPERAND_ALONG, smem_addr(sm.a[stage]));
-                    const uint64_t b = operand(Task::B_DOWN ? PRODUCT_DOWN : OPERAND_ALONG, smem_addr(sm.b[stage]));
+                    const uint64_t a = operand(word_a, smem_addr(sm.a[stage]));
+                    const uint64_t b = operand(word_b, smem_addr(sm.b[stage]));
 #pragma unroll
                     for (uint32_t k = 0; k < K_STEP / 16; ++k) multiply<PAIR>(d, a + k * step_a, b + k * step_b, word, s > 0 || k > 0);
                     multiplied<PAIR>(&sm.free[stage]);
@@ -252,20 +296,18 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
         }
     } else if (warp >= PRODUCT_FINISH) {
         const uint32_t group = (warp - PRODUCT_FINISH) / 4, quarter = warp % 4;
-        uint32_t done = 0;
         Part part;
         part.at = tmem + group * SIDE + ((quarter * 32) << 16);
-        part.store = sm.store[warp - PRODUCT_FINISH];
-        part.there = true;
-        for (int i = first; i < tiles; i += stride, ++done) {
-            if ((done & 1) != group) continue;
-            const Tile t = Task::tile(p, i);
+        part.store = sm.store[warp - PRODUCT_FINISH][0], part.turn = 0;
+        part.there = true, part.full = &sm.sums_full[group], part.waits = waits;
+        for (int done = static_cast<int>(group); done < tiles; done += 2) {
+            const Tile t = Task::tile(p, worker, workers, done);
             part.warp_row = t.m + static_cast<int>(rank * TILE + quarter * 32);
             part.row = part.warp_row + lane;
             part.zero = t.steps == 0;
-            part.there = part.there && bar_wait(&sm.sums_full[group], done / 2 & 1, waits);
-            tmem_fence_after();
+            part.parity = done / 2 & 1, part.waited = false;
             Task::finish(p, maps, t, part);
+            part.wait();
             if (part.there) {
                 tmem_fence_before();
                 __syncwarp();
@@ -287,16 +329,17 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
 }
 
 // ---------------------------------------------------------------------------------- host side
-// Matrix z of [matrices][rows][cols], pitches in bytes; boxes of box_cols x box_rows.
+// Matrix z of [matrices][rows][cols], pitches in bytes; boxes of box_cols x box_rows whose rows of 128 (64) bytes are in the
+// 128-byte (64-byte) swizzle, or as they are.
 inline int describe_matrix(CUtensorMap *map, const char *what, CUtensorMapDataType type, int size, const void *at, int64_t cols, int64_t rows, int64_t matrices, int64_t pitch,
-                           int64_t matrix_pitch, int box_cols, int box_rows) {
+                           int64_t matrix_pitch, int box_cols, int box_rows, bool swizzled = true) {
     const encode_fn encode = encoder();
     if (encode == nullptr) return ktd::fail(KT_ERR_CUDA, "the driver does not offer cuTensorMapEncodeTiled");
     const cuuint64_t sizes[3] = {static_cast<cuuint64_t>(cols), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(matrices)};
     const cuuint64_t strides[2] = {rows > 1 ? static_cast<cuuint64_t>(pitch) : 16, matrices > 1 ? static_cast<cuuint64_t>(matrix_pitch) : 16};      // that of a dimension of one is never used
     const cuuint32_t box[3] = {static_cast<cuuint32_t>(box_cols), static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
-    if (box_cols * size != 128) return ktd::fail(KT_ERR_INVALID, "%s: boxes of 128 bytes a row expected", what);
-    const CUresult rc = encode(map, type, 3, const_cast<void *>(at), sizes, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+    const CUtensorMapSwizzle swizzle = !swizzled ? CU_TENSOR_MAP_SWIZZLE_NONE : box_cols * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    const CUresult rc = encode(map, type, 3, const_cast<void *>(at), sizes, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (rc != CUDA_SUCCESS) return ktd::fail(KT_ERR_CUDA, "describing %s to the copy engine failed with driver status %d", what, static_cast<int>(rc));
     return KT_OK;
@@ -306,9 +349,10 @@ inline int describe_operand(CUtensorMap *map, const char *what, bool half, bool 
     return describe_matrix(map, what, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, at, cols, rows, matrices, pitch, matrix_pitch, 64, down ? K_STEP : TILE);
 }
 
-// Starts a product of at most `tiles` tiles behind what is in the stream.
+// Starts a product of at most `tiles` tiles: behind a kernel of the same call, or as the call's first, which may not begin
+// before all that is in the stream has ended.
 template <class Task>
-int start_product(const ProductMaps &maps, const typename Task::Params &p, int64_t tiles, cudaStream_t st) {
+int start_product(ProductMaps maps, const typename Task::Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
     static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
     constexpr size_t bytes = sizeof(ProductSmem) + 1024;
     static_assert(bytes <= 227 * 1024, "the ring and the stores have to fit");
@@ -320,9 +364,18 @@ int start_product(const ProductMaps &maps, const typename Task::Params &p, int64
         raised.fetch_or(bit, std::memory_order_relaxed);
     }
     if (tiles == 0) return KT_OK;
+    // every description is fetched ahead, so those that the Task does not use are copies of one that it does
+    const CUtensorMap none{};
+    CUtensorMap *const first = &maps.a, *const past = first + sizeof(maps) / sizeof(CUtensorMap);
+    const CUtensorMap *described = std::find_if(first, past, [&](const CUtensorMap &m) { return std::memcmp(&m, &none, sizeof(m)) != 0; });
+    if (described == past) return ktd::fail(KT_ERR_INVALID, "a product without operands");
+    for (CUtensorMap *m = first; m < past; ++m)
+        if (std::memcmp(m, &none, sizeof(none)) == 0) *m = *described;
     constexpr int CTAS = Task::PAIR ? 2 : 1;
     const int64_t places = PRODUCT_SMS / CTAS;
-    KT_CUDA(launch_behind(k_product<Task>, CTAS, dim3(static_cast<unsigned>(CTAS * (tiles < places ? tiles : places))), dim3(PRODUCT_THREADS), bytes, st, maps, p, ktd::wait_limit_ns()));
+    const dim3 grid(static_cast<unsigned>(CTAS * (tiles < places ? tiles : places)));
+    if (behind) KT_CUDA(launch_behind(k_product<Task>, CTAS, grid, dim3(PRODUCT_THREADS), bytes, st, maps, p, ktd::wait_limit_ns()));
+    else KT_CUDA(launch_joint(k_product<Task>, CTAS, grid, dim3(PRODUCT_THREADS), bytes, st, maps, p, ktd::wait_limit_ns()));
     return KT_OK;
 }
 

@@ -9,7 +9,7 @@
 //   loss   a tile of logits becomes a maximum, a sum of exponentials and perhaps the target's logit of each row
 //   grad   the logits are formed again, and leave the chip as P in bf16, a piece of the vocabulary at a time (the second
 //          products of the tensor cores take 16-bit operands; bf16 because P spans the range of probabilities)
-//   dh, dW from the piece.  dW of the piece's rows is whole; dh is summed over the pieces in fp32.
+//   back   dh and dW from the piece.  dW of the piece's rows is whole; dh is summed over the pieces in fp32.
 // Rows that do not count are left out before the products: the rows that do are numbered in order, and where any are
 // missing their hidden rows are copied next to each other, so what the others hold is never multiplied.
 #include "../../include/kaitian.h"
@@ -75,6 +75,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
     let_next_begin();
     const int begin = min(p.n, static_cast<int>(blockIdx.x) * p.each), end = min(p.n, begin + p.each);
     int before = 0, all = 0;
+#pragma unroll 8
     for (int i = tid; i < p.n; i += 256) {
         const int counts = p.targets[i] >= 0;
         all += counts;
@@ -121,6 +122,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
             if (to >= 0) {
                 const uint4 *from = reinterpret_cast<const uint4 *>(p.hidden + (base + r) * p.hidden_stride);
                 uint4 *const row = reinterpret_cast<uint4 *>(p.packed + static_cast<int64_t>(to) * p.dim);
+#pragma unroll 8
                 for (int c = lane; c < pieces; c += 32) row[c] = from[c];
             } else if (p.dhidden != nullptr) {
                 uint4 *const row = reinterpret_cast<uint4 *>(p.dhidden + (base + r) * p.dhidden_stride);
@@ -141,38 +143,47 @@ __device__ __forceinline__ void in_bands(int i, int tiles_m, int tiles_n, int ba
 }
 
 struct LogitsParams {
-    const int *count;
+    const int *count, *index;
     const Row *rows;
+    const int64_t *targets;                     // where nothing was left out, because one tile holds all rows: instead of the three
     float2 *parts;                              // [tiles of columns][n]: maximum (units of log 2) and sum
     float *at_target;                           // the target's logit (units of log 2)
     int n, vocab, steps, from, past, band;      // columns from ... past of the vocabulary
     float scale_log2;
+    __device__ __forceinline__ int counted() const { return targets != nullptr ? n : *count; }
+    __device__ __forceinline__ Row row(int i) const {
+        if (targets == nullptr) return rows[i];
+        const int64_t t = targets[i];
+        return {t < 0 ? -1 : t < vocab ? static_cast<int>(t) : PAST_VOCAB, 0.0f, 0.0f, 0.0f};
+    }
 };
 
 template <bool PAIR_>
-struct LogitsTask {
+struct LogitsTask : InTurn<LogitsTask<PAIR_>, LogitsParams> {
     using Params = LogitsParams;
-    static constexpr bool PAIR = PAIR_, A_DOWN = false, B_DOWN = false, HALF = false;
+    static constexpr bool PAIR = PAIR_, HALF = false;
     static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles_m(const Params &p) { return (*p.count + SIDE - 1) / SIDE; }
+    __device__ static int tiles_m(const Params &p) { return (p.counted() + SIDE - 1) / SIDE; }
     __device__ static int tiles(const Params &p) { return tiles_m(p) * ((p.past - p.from + SIDE - 1) / SIDE); }
-    __device__ static bool second_a(const Params &p) { return *p.count < p.n; }
-    __device__ static bool second_b(const Params &) { return false; }
-    __device__ static Tile tile(const Params &p, int i) {
+    __device__ static bool a_down(const Tile &) { return false; }
+    __device__ static bool b_down(const Tile &) { return false; }
+    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &p, const Tile &) { return p.counted() < p.n ? &maps.a2 : &maps.a; }
+    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
+    __device__ static Tile tile_at(const Params &p, int i) {
         int m, n;
         in_bands(i, tiles_m(p), (p.past - p.from + SIDE - 1) / SIDE, p.band, &m, &n);
-        return {m * SIDE, p.from + n * SIDE, 0, 0, p.steps, 0};
+        return {m * SIDE, p.from + n * SIDE, 0, 0, p.steps, 0, 0};
     }
 };
 
 template <bool PAIR_>
 struct LossTask : LogitsTask<PAIR_> {
     using Base = LogitsTask<PAIR_>;
-    __device__ static void finish(const LogitsParams &p, const ProductMaps &, const Tile &t, const Part &part) {
-        const bool counts = part.row < *p.count;
-        const int target = counts ? p.rows[part.row].target : -1;
+    __device__ static void finish(const LogitsParams &p, const ProductMaps &, const Tile &t, Part &part) {
+        const bool counts = part.row < p.counted();
+        const int target = counts ? p.row(part.row).target : -1;
         float top = -INFINITY, sum = 0.0f;
-        over_columns<Base::SIDE>(part, [&](int c, uint32_t (&r)[32]) {
+        over_columns<Base::SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
             const int v0 = t.n + c;
             if (v0 >= p.vocab) return;
             if (v0 + 32 > p.vocab)
@@ -210,28 +221,28 @@ struct LossTask : LogitsTask<PAIR_> {
 
 // 64 columns of a row, as 16-bit values, through the store to a matrix.
 template <typename F>
-__device__ __forceinline__ void pack_row(const Part &part, int c, F value) {
+__device__ __forceinline__ void pack_row(const Part &part, int half, F value) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         uint4 v;
         v.x = pack_bf16(value(u * 8), value(u * 8 + 1)), v.y = pack_bf16(value(u * 8 + 2), value(u * 8 + 3));
         v.z = pack_bf16(value(u * 8 + 4), value(u * 8 + 5)), v.w = pack_bf16(value(u * 8 + 6), value(u * 8 + 7));
-        *part.piece((c % 64) / 8 + u) = v;
+        *part.piece(half * 4 + u) = v;
     }
 }
 
 template <bool PAIR_>
 struct GradTask : LogitsTask<PAIR_> {
     using Base = LogitsTask<PAIR_>;
-    __device__ static void finish(const LogitsParams &p, const ProductMaps &maps, const Tile &t, const Part &part) {
-        const int count = *p.count;
+    __device__ static void finish(const LogitsParams &p, const ProductMaps &maps, const Tile &t, Part &part) {
+        const int count = p.counted();
         if (part.warp_row >= round_to(count, TILE)) return;
         const bool counts = part.row < count;
         const Row row = counts ? p.rows[part.row] : Row{-1, 0.0f, 0.0f, 0.0f};
-        over_columns<Base::SIDE>(part, [&](int c, uint32_t (&r)[32]) {
+        over_columns<Base::SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
             const int v0 = t.n + c;
-            if (v0 - c % 64 >= p.past) return;
-            if (c % 64 == 0) part.store_free();
+            if (v0 - half * 32 >= p.past) return;
+            if (half == 0) part.store_next();
             const int d = row.target - v0, left = p.past - v0;
             float x[32];
 #pragma unroll
@@ -248,130 +259,163 @@ struct GradTask : LogitsTask<PAIR_> {
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                     if (!counts || e >= left) x[e] = 0.0f;
-            pack_row(part, c, [&](int e) { return x[e]; });
-            if (c % 64 == 32) part.send(&maps.out, v0 - 32 - p.from, part.warp_row, 0);
+            pack_row(part, half, [&](int e) { return x[e]; });
+            if (half == 1) part.send(&maps.out, v0 - 32 - p.from, part.warp_row, 0);
         });
     }
 };
 
-// dW of a piece: [columns of the piece] x [dim], reduced over the counted rows.
-struct WeightParams {
-    const int *count;
-    int n, tiles_m, tiles_n, band, vocab, dim, from;
-};
-template <bool PAIR_>
-struct WeightTask {
-    using Params = WeightParams;
-    static constexpr bool PAIR = PAIR_, A_DOWN = true, B_DOWN = true, HALF = false;
-    static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles(const Params &p) { return p.tiles_m * p.tiles_n; }
-    __device__ static bool second_a(const Params &) { return false; }
-    __device__ static bool second_b(const Params &p) { return *p.count < p.n; }
-    __device__ static Tile tile(const Params &p, int i) {
-        int m, n;
-        in_bands(i, p.tiles_m, p.tiles_n, p.band, &m, &n);
-        return {m * SIDE, n * SIDE, 0, 0, (*p.count + K_STEP - 1) / K_STEP, 0};
-    }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, const Part &part) {
-        if (p.from + part.warp_row >= p.vocab) return;
-        over_columns<SIDE>(part, [&](int c, uint32_t (&r)[32]) {
-            if (t.n + c - c % 64 >= p.dim) return;
-            if (c % 64 == 0) part.store_free();
-            pack_row(part, c, [&](int e) { return __uint_as_float(r[e]); });
-            if (c % 64 == 32) part.send(&maps.out, t.n + c - 32, p.from + part.warp_row, 0);
-        });
-    }
-};
-
-// dh of a piece, reduced over a share of its columns: added to, or the first of, the share's own sums; or (to != NULL)
-// all there is, to the rows themselves.  (The description of W begins with the piece's first row.)
-struct HiddenParams {
+// Both products of a piece of P in one launch, since neither waits for the other: first the tiles of dh, reduced over the
+// piece's columns or a share of them, then those of dW, reduced over the counted rows.  A tile of dh takes long where the piece is wide,
+// and there are few of them: workers that do one less of them do more of dW's.
+struct BackParams {
     const int *count, *index;
-    __nv_bfloat16 *to;
+    __nv_bfloat16 *to;                          // dh where a tile has all of it; else NULL, and its shares are added up in fp32
     int64_t to_stride;
-    int tiles_n, band, dim, shares, steps, add;       // steps of the piece
+    int n, dim, from, past;                     // columns of the vocabulary
+    int tiles_n, tiles_w, shares, steps, add;   // tiles across dim and (dW) across the piece; shares of the piece's stages; whether to add
+    int hidden;                                 // whether dh is wanted
 };
 template <bool PAIR_>
-struct HiddenTask {
-    using Params = HiddenParams;
-    static constexpr bool PAIR = PAIR_, A_DOWN = false, B_DOWN = true, HALF = false;
-    static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles_m(const Params &p) { return (*p.count + SIDE - 1) / SIDE; }
-    __device__ static int tiles(const Params &p) { return tiles_m(p) * p.tiles_n * p.shares; }
-    __device__ static bool second_a(const Params &) { return false; }
-    __device__ static bool second_b(const Params &) { return false; }
-    __device__ static Tile tile(const Params &p, int i) {
-        int m, n;
-        const int share = i % p.shares, begin = static_cast<int>(static_cast<int64_t>(p.steps) * share / p.shares), end = static_cast<int>(static_cast<int64_t>(p.steps) * (share + 1) / p.shares);
-        in_bands(i / p.shares, tiles_m(p), p.tiles_n, p.band, &m, &n);
-        return {m * SIDE, n * SIDE, 0, begin * K_STEP, end - begin, share};
+struct BackTask {
+    using Params = BackParams;
+    static constexpr bool PAIR = PAIR_, HALF = false;
+    static constexpr int SIDE = PAIR ? 256 : 128, BAND = 8;
+    struct Cut {
+        int hidden, each, longer, more, weight, weight_steps;
+        // each: tiles of dh to a worker, one more to the first `longer`; more: tiles of dW that the others do meanwhile
+        __device__ Cut(const Params &p, int workers) {
+            const int count = *p.count;
+            hidden = p.hidden ? (count + SIDE - 1) / SIDE * p.tiles_n * p.shares : 0;
+            weight = p.tiles_w * p.tiles_n, weight_steps = (count + K_STEP - 1) / K_STEP;
+            each = hidden / workers, longer = hidden - each * workers;
+            const int others = workers - longer;
+            more = longer == 0 ? 0 : min((p.steps / p.shares + FINISH) / (weight_steps + FINISH), (weight + others - 1) / others);
+        }
+    };
+    static constexpr int FINISH = 2;            // stages' time that a tile's end takes
+    __device__ static int count(const Params &p, int worker, int workers) {
+        const Cut c(p, workers);
+        const int others = workers - c.longer, meanwhile = min(c.weight, others * c.more), rest = c.weight - meanwhile;
+        int n = c.each + (worker < c.longer ? 1 : 0);
+        if (worker >= c.longer) n += (meanwhile - (worker - c.longer) + others - 1) / others;
+        return n + (rest - (workers - 1 - worker) + workers - 1) / workers;
     }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, const Part &part) {
+    __device__ static Tile tile(const Params &p, int worker, int workers, int i) {
+        const Cut c(p, workers);
+        const int mine = c.each + (worker < c.longer ? 1 : 0);
+        if (i < mine) {
+            const int at = worker + i * workers, share = at % p.shares;
+            const int begin = static_cast<int>(static_cast<int64_t>(p.steps) * share / p.shares), end = static_cast<int>(static_cast<int64_t>(p.steps) * (share + 1) / p.shares);
+            int m, n;
+            in_bands(at / p.shares, (*p.count + SIDE - 1) / SIDE, p.tiles_n, BAND, &m, &n);
+            return {m * SIDE, n * SIDE, 0, begin * K_STEP, end - begin, 0, share};
+        }
+        i -= mine;
+        const int others = workers - c.longer, meanwhile = min(c.weight, others * c.more);
+        int at;
+        const int early = worker >= c.longer ? (meanwhile - (worker - c.longer) + others - 1) / others : 0;
+        if (i < early) at = worker - c.longer + i * others;
+        else at = meanwhile + (workers - 1 - worker) + (i - early) * workers;
+        int m, n;
+        in_bands(at, p.tiles_w, p.tiles_n, BAND, &m, &n);
+        return {m * SIDE, n * SIDE, 0, 0, c.weight_steps, 1, 0};
+    }
+    __device__ static bool a_down(const Tile &t) { return t.kind == 1; }
+    __device__ static bool b_down(const Tile &) { return true; }
+    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &t) { return t.kind == 0 ? &maps.a : &maps.a2; }
+    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &p, const Tile &t) { return t.kind == 0 ? &maps.b : *p.count < p.n ? &maps.b3 : &maps.b2; }
+    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
         const int count = *p.count;
-        if (part.warp_row >= count) return;
-        __nv_bfloat16 *const row = p.to != nullptr && part.row < count ? p.to + p.index[part.row] * p.to_stride : nullptr;
-        over_columns<SIDE>(part, [&](int c, uint32_t (&r)[32]) {
+        const bool weight = t.kind == 1;
+        if (weight ? p.from + part.warp_row >= p.past : part.warp_row >= count) return;
+        __nv_bfloat16 *const row = !weight && p.to != nullptr && part.row < count ? p.to + p.index[part.row] * p.to_stride : nullptr;
+        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
             const int c0 = t.n + c;
-            if (c0 >= p.dim) return;
-            if (p.to != nullptr) {
-                if (row != nullptr)
+            if (weight) {
+                if (c0 - half * 32 >= p.dim) return;
+                if (half == 0) part.store_next();
+                pack_row(part, half, [&](int e) { return __uint_as_float(r[e]); });
+                if (half == 1) part.send(&maps.out, c0 - 32, p.from + part.warp_row, 0);
+            } else if (p.to == nullptr) {
+                if (c0 >= p.dim) return;
+                part.store_next();
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8)
-                        if (c0 + e < p.dim) {
-                            uint4 v;
-                            v.x = pack_bf16(pair_of(r, e)), v.y = pack_bf16(pair_of(r, e + 2)), v.z = pack_bf16(pair_of(r, e + 4)), v.w = pack_bf16(pair_of(r, e + 6));
-                            *reinterpret_cast<uint4 *>(row + c0 + e) = v;
-                        }
-                return;
+                for (int u = 0; u < 8; ++u) *part.piece(u) = make_uint4(r[u * 4], r[u * 4 + 1], r[u * 4 + 2], r[u * 4 + 3]);
+                part.send(&maps.out2, c0, part.warp_row, t.share, p.add != 0);
+            } else if (row != nullptr) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 8)
+                    if (c0 + e < p.dim) {
+                        uint4 v;
+                        v.x = pack_bf16(pair_of(r, e)), v.y = pack_bf16(pair_of(r, e + 2)), v.z = pack_bf16(pair_of(r, e + 4)), v.w = pack_bf16(pair_of(r, e + 6));
+                        *reinterpret_cast<uint4 *>(row + c0 + e) = v;
+                    }
             }
-            part.store_free();
-#pragma unroll
-            for (int u = 0; u < 8; ++u) *part.piece(u) = make_uint4(r[u * 4], r[u * 4 + 1], r[u * 4 + 2], r[u * 4 + 3]);
-            part.send(&maps.out, c0, part.warp_row, t.share, p.add != 0);
         });
     }
 };
 
 // ------------------------------------------------------------------------------------- ends
-// The parts of a row joined; 8 rows to a CTA, 32 threads to a row.
-__global__ void __launch_bounds__(256) k_xent_join(const int *count, const int *index, const Row *rows, const float2 *parts, const float *at_target, int n, int tiles, float *loss, float *lse) {
+// The parts of a row joined; 8 rows to a CTA, 32 threads to a row, eight parts on their way to a thread at a time.
+__global__ void __launch_bounds__(256) k_xent_join(const LogitsParams p, int tiles, float *loss, float *lse) {
     __shared__ float2 of_warp[8][8];
     let_next_begin();
     after_previous();
     const int tid = threadIdx.x, r = tid % 8, row = blockIdx.x * 8 + r;
-    const bool counts = row < *count;
+    const bool there = row < p.counted();
     float top = -INFINITY, sum = 0.0f;
     auto join = [&](float2 x) {
         const float high = fmaxf(top, x.x), zero = high == -INFINITY ? 0.0f : high;
-        sum = sum * exp2f(top - zero) + x.y * exp2f(x.x - zero);
+        sum = sum * exp2_fast(top - zero) + x.y * exp2_fast(x.x - zero);
         top = high;
     };
-    if (counts)
-#pragma unroll 4
-        for (int i = tid / 8; i < tiles; i += 32) join(parts[static_cast<int64_t>(i) * n + row]);
+    const Row mine = there ? p.row(row) : Row{-1, 0.0f, 0.0f, 0.0f};
+    const float at = there ? p.at_target[row] : 0.0f;
+    const int to = there && p.index != nullptr ? p.index[row] : row;
+    if (there)
+        for (int i0 = tid / 8; i0 < tiles; i0 += 8 * 32) {
+            float2 x[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] = i0 + u * 32 < tiles ? p.parts[static_cast<int64_t>(i0 + u * 32) * p.n + row] : make_float2(-INFINITY, 0.0f);
+            float high = -INFINITY, part = 0.0f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) high = fmaxf(high, x[u].x);
+            const float zero = high == -INFINITY ? 0.0f : high;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) part += x[u].y * exp2_fast(x[u].x - zero);
+            join(make_float2(high, part));
+        }
 #pragma unroll
     for (int far = 8; far < 32; far *= 2) join(make_float2(__shfl_xor_sync(0xFFFFFFFFu, top, far), __shfl_xor_sync(0xFFFFFFFFu, sum, far)));
     if (tid % 32 < 8) of_warp[tid / 32][r] = make_float2(top, sum);
     __syncthreads();
-    if (tid >= 8 || !counts) return;
+    if (tid >= 8 || !there) return;
     top = -INFINITY, sum = 0.0f;
+#pragma unroll
     for (int w = 0; w < 8; ++w) join(of_warp[w][r]);
     const float high = log2f(sum);
-    const int i = index[row];
-    lse[i] = (top + high) * LN2;
+    const bool counts = mine.target >= 0;       // (a row that does not count is among these where nothing was left out)
+    lse[to] = counts ? (top + high) * LN2 : 0.0f;
     // the maximum and the target's logit first: they are close where the loss is small
-    loss[i] = rows[row].target == PAST_VOCAB ? __int_as_float(0x7FFFFFFF) : ((top - at_target[row]) + high) * LN2;
+    loss[to] = !counts ? 0.0f : mine.target == PAST_VOCAB ? __int_as_float(0x7FFFFFFF) : ((top - at) + high) * LN2;
 }
 
 // The shares of dh added up, in order.
 __global__ void __launch_bounds__(256) k_xent_dhidden(const int *count, const int *index, const float *sums, int shares, int64_t share, int dim, __nv_bfloat16 *to, int64_t stride) {
     let_next_begin();
     after_previous();
-    const int pieces = dim / 8, all = *count;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < static_cast<int64_t>(all) * pieces; i += static_cast<int64_t>(gridDim.x) * 256) {
-        const int row = static_cast<int>(i / pieces), c = static_cast<int>(i - static_cast<int64_t>(row) * pieces) * 8;
+    const uint32_t pieces = dim / 8, all = *count, step = gridDim.x * 256, step_rows = step / pieces, step_pieces = step % pieces, first = blockIdx.x * 256 + threadIdx.x;
+    uint32_t piece = first % pieces;
+    for (uint32_t row = first / pieces; row < all; row += step_rows, piece += step_pieces) {
+        if (piece >= pieces) {
+            piece -= pieces;
+            if (++row >= all) break;
+        }
+        const int c = piece * 8;
         const float *from = sums + static_cast<int64_t>(row) * dim + c;
         float4 a = *reinterpret_cast<const float4 *>(from), b = *reinterpret_cast<const float4 *>(from + 4);
+#pragma unroll 4
         for (int s = 1; s < shares; ++s) {
             const float4 c0 = *reinterpret_cast<const float4 *>(from + s * share), c1 = *reinterpret_cast<const float4 *>(from + s * share + 4);
             a.x += c0.x, a.y += c0.y, a.z += c0.z, a.w += c0.w, b.x += c1.x, b.y += c1.y, b.z += c1.z, b.w += c1.w;
@@ -387,8 +431,8 @@ int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 int64_t tiles_of(int64_t x, int side) { return (x + side - 1) / side; }
 
 // Whether a product of m x n results is worked on by pairs of CTAs: where tiles of 256 x 256 give every pair
-// at least one.
-bool by_pairs(int64_t m, int64_t n) { return tiles_of(m, 256) * tiles_of(n, 256) >= PRODUCT_SMS / 2; }
+// at least one, and not where half of a tile would be empty rows.
+bool by_pairs(int64_t m, int64_t n) { return m > TILE && tiles_of(m, 256) * tiles_of(n, 256) >= PRODUCT_SMS / 2; }
 
 constexpr int64_t PIECE_BYTES = INT64_C(512) << 20;        // of P, at most
 
@@ -397,7 +441,7 @@ struct Plan {
     int64_t n, dim, vocab;
     bool backward;
     int64_t piece, pieces, shares;              // columns of the vocabulary to a piece; shares of dh's reduction
-    bool pairs_logits, pairs_hidden, pairs_weight;
+    bool pairs_logits, pairs_back;
     int64_t at_index, at_rows, at_packed, at_parts, at_target, at_p, at_sums, bytes;
     Plan(int64_t rows, int64_t dims, int64_t words, bool back) : n(rows), dim(dims), vocab(words), backward(back) {
         int64_t at = 0;
@@ -413,13 +457,14 @@ struct Plan {
         pieces = backward ? tiles_of(vocab, static_cast<int>(most)) : 1;
         piece = backward ? up((vocab + pieces - 1) / pieces, 256) : vocab;
         pieces = (vocab + piece - 1) / piece;
-        pairs_logits = by_pairs(n, piece), pairs_hidden = by_pairs(n, dim), pairs_weight = by_pairs(piece, dim);
-        // dh: few tiles share the reduction over the vocabulary among several CTAs, at least 16 stages to each
-        const int side = pairs_hidden ? 256 : 128;
-        const int64_t tiles = tiles_of(n, side) * tiles_of(dim, side), places = PRODUCT_SMS / (pairs_hidden ? 2 : 1), steps = (piece + K_STEP - 1) / K_STEP;
-        shares = places / tiles;
-        if (shares > steps / 16) shares = steps / 16;
-        if (shares < 1) shares = 1;
+        pairs_logits = by_pairs(n, piece);
+        const int64_t steps = (piece + K_STEP - 1) / K_STEP, over_rows = (n + K_STEP - 1) / K_STEP;
+        pairs_back = tiles_of(dim, 256) * (tiles_of(n, 256) + tiles_of(piece, 256)) >= PRODUCT_SMS / 2;
+        // dh: shares of the piece such that a tile takes no longer than all work on all workers, but 16 stages at least
+        const int side = pairs_back ? 256 : 128;
+        const int64_t workers = pairs_back ? PRODUCT_SMS / 2 : PRODUCT_SMS, hidden = tiles_of(n, side) * tiles_of(dim, side), weight = tiles_of(piece, side) * tiles_of(dim, side);
+        const int64_t mean = (hidden * steps + weight * over_rows) / workers, longest = mean < 16 ? 16 : mean;
+        shares = (steps + longest - 1) / longest;
         at_parts = take(backward ? 0 : 8 * n * tiles_of(vocab, pairs_logits ? 256 : 128)), at_target = take(backward ? 0 : 4 * n);
         at_p = take(backward ? 2 * up(n, TILE) * piece : 0);
         at_sums = take(backward && (pieces > 1 || shares > 1) ? 4 * shares * n * dim : 0);
@@ -459,7 +504,8 @@ int start_rows(RowsParams &q, const Plan &plan, char *ws, cudaStream_t st) {
     q.count = reinterpret_cast<int *>(ws), q.index = reinterpret_cast<int *>(ws + plan.at_index), q.rows = reinterpret_cast<Row *>(ws + plan.at_rows);
     q.packed = reinterpret_cast<__nv_bfloat16 *>(ws + plan.at_packed);
     q.n = static_cast<int>(plan.n), q.dim = static_cast<int>(plan.dim), q.vocab = static_cast<int>(plan.vocab);
-    q.each = static_cast<int>((plan.n + PRODUCT_SMS - 1) / PRODUCT_SMS);
+    q.each = static_cast<int>((plan.n + 4 * PRODUCT_SMS - 1) / (4 * PRODUCT_SMS));      // four CTAs to an SM
+    if (q.each < 8) q.each = 8;                 // a row to a warp
     k_xent_rows<<<static_cast<unsigned>((plan.n + q.each - 1) / q.each), 256, 0, st>>>(q);
     KT_CUDA(cudaGetLastError());
     return KT_OK;
@@ -471,17 +517,15 @@ int band_of(int64_t dim, int side) {
     return rows < side ? 1 : rows / side > 1 << 20 ? 1 << 20 : static_cast<int>(rows / side);
 }
 
-int describe_rows(ProductMaps *maps, const Plan &plan, const void *hidden, int64_t hidden_stride, const char *ws, bool down) {
-    CUtensorMap *const own = down ? &maps->b : &maps->a, *const packed = down ? &maps->b2 : &maps->a2;
+// The counted rows: hidden itself where all count, and where they have been copied to.
+int describe_rows(CUtensorMap *own, CUtensorMap *packed, const Plan &plan, const void *hidden, int64_t hidden_stride, const char *ws, bool down) {
     if (int rc = describe_operand(own, "hidden", false, down, hidden, plan.dim, plan.n, 1, hidden_stride * 2, 0)) return rc;
     return describe_operand(packed, "the workspace", false, down, ws + plan.at_packed, plan.dim, up(plan.n, K_STEP), 1, plan.dim * 2, 0);
 }
 
 template <template <bool> class Task, typename Params>
-int start_either(bool pairs, const ProductMaps &maps, const Params &p, int64_t m, int64_t n, int64_t shares, cudaStream_t st) {
-    const int side = pairs ? 256 : 128;
-    const int64_t tiles = tiles_of(m, side) * tiles_of(n, side) * shares;
-    return pairs ? start_product<Task<true>>(maps, p, tiles, st) : start_product<Task<false>>(maps, p, tiles, st);
+int start_either(bool pairs, const ProductMaps &maps, const Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
+    return pairs ? start_product<Task<true>>(maps, p, tiles, st, behind) : start_product<Task<false>>(maps, p, tiles, st, behind);
 }
 
 }  // namespace
@@ -512,18 +556,23 @@ int kt_xent_forward(const void *hidden, int64_t hidden_stride, const void *weigh
     char *const ws = reinterpret_cast<char *>(up(reinterpret_cast<intptr_t>(workspace), 1024));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     ProductMaps maps{};
-    if (int rc = describe_rows(&maps, plan, hidden, hidden_stride, ws, false)) return rc;
+    if (int rc = describe_rows(&maps.a, &maps.a2, plan, hidden, hidden_stride, ws, false)) return rc;
     if (int rc = describe_operand(&maps.b, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
-    RowsParams q{};
-    q.targets = targets, q.hidden = static_cast<const __nv_bfloat16 *>(hidden), q.hidden_stride = hidden_stride, q.loss_out = loss, q.lse_out = lse, q.scale = scale;
-    if (int rc = start_rows(q, plan, ws, st)) return rc;
-    const int side = plan.pairs_logits ? 256 : 128;
     LogitsParams p{};
-    p.count = q.count, p.rows = q.rows, p.parts = reinterpret_cast<float2 *>(ws + plan.at_parts), p.at_target = reinterpret_cast<float *>(ws + plan.at_target);
-    p.n = q.n, p.vocab = q.vocab, p.steps = static_cast<int>((dim + K_STEP - 1) / K_STEP), p.from = 0, p.past = q.vocab, p.band = band_of(dim, side), p.scale_log2 = scale * LOG2E;
-    if (int rc = start_either<LossTask>(plan.pairs_logits, maps, p, rows, vocab, 1, st)) return rc;
-    KT_CUDA(launch_behind(k_xent_join, 1, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, static_cast<const int *>(q.count), static_cast<const int *>(q.index), static_cast<const Row *>(q.rows),
-                          static_cast<const float2 *>(p.parts), static_cast<const float *>(p.at_target), q.n, static_cast<int>(tiles_of(vocab, side)), loss, lse));
+    p.parts = reinterpret_cast<float2 *>(ws + plan.at_parts), p.at_target = reinterpret_cast<float *>(ws + plan.at_target);
+    const int side = plan.pairs_logits ? 256 : 128;
+    p.n = static_cast<int>(rows), p.vocab = p.past = static_cast<int>(vocab), p.steps = static_cast<int>((dim + K_STEP - 1) / K_STEP), p.band = band_of(dim, side), p.scale_log2 = scale * LOG2E;
+    const bool leave_out = rows > side;         // one tile takes as long whatever its rows
+    if (leave_out) {
+        RowsParams q{};
+        q.targets = targets, q.hidden = static_cast<const __nv_bfloat16 *>(hidden), q.hidden_stride = hidden_stride, q.loss_out = loss, q.lse_out = lse, q.scale = scale;
+        if (int rc = start_rows(q, plan, ws, st)) return rc;
+        p.count = q.count, p.index = q.index, p.rows = q.rows;
+    } else {
+        p.targets = targets;
+    }
+    if (int rc = start_either<LossTask>(plan.pairs_logits, maps, p, tiles_of(rows, side) * tiles_of(vocab, side), st, leave_out)) return rc;
+    KT_CUDA(launch_behind(k_xent_join, 1, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, p, static_cast<int>(tiles_of(vocab, side)), loss, lse));
     return KT_OK;
 }
 
@@ -554,19 +603,19 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     const bool direct = plan.pieces == 1 && plan.shares == 1;
     const int64_t p_rows = up(rows, TILE), pitch = plan.piece * 2;
 
-    ProductMaps logits{}, to_hidden{}, to_weight{};
-    if (int rc = describe_rows(&logits, plan, hidden, hidden_stride, ws, false)) return rc;
+    ProductMaps logits{}, back{};
+    if (int rc = describe_rows(&logits.a, &logits.a2, plan, hidden, hidden_stride, ws, false)) return rc;
     if (int rc = describe_operand(&logits.b, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
     if (int rc = describe_matrix(&logits.out, "the workspace", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0, 64, 32)) return rc;
     if (dhidden != nullptr) {
-        if (int rc = describe_operand(&to_hidden.a, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
+        if (int rc = describe_operand(&back.a, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
         if (!direct)
-            if (int rc = describe_matrix(&to_hidden.out, "the workspace", CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, sums, dim, rows, plan.shares, dim * 4, rows * dim * 4, 32, 32)) return rc;
+            if (int rc = describe_matrix(&back.out2, "the workspace", CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, sums, dim, rows, plan.shares, dim * 4, rows * dim * 4, 32, 32)) return rc;
     }
     if (dweight != nullptr) {
-        if (int rc = describe_operand(&to_weight.a, "the workspace", false, true, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
-        if (int rc = describe_rows(&to_weight, plan, hidden, hidden_stride, ws, true)) return rc;
-        if (int rc = describe_matrix(&to_weight.out, "dweight", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dweight, dim, vocab, 1, dweight_stride * 2, 0, 64, 32)) return rc;
+        if (int rc = describe_operand(&back.a2, "the workspace", false, true, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
+        if (int rc = describe_rows(&back.b2, &back.b3, plan, hidden, hidden_stride, ws, true)) return rc;
+        if (int rc = describe_matrix(&back.out, "dweight", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dweight, dim, vocab, 1, dweight_stride * 2, 0, 64, 32)) return rc;
     }
 
     RowsParams q{};
@@ -578,23 +627,17 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
         LogitsParams p{};
         p.count = q.count, p.rows = q.rows, p.n = q.n, p.vocab = q.vocab, p.steps = static_cast<int>((dim + K_STEP - 1) / K_STEP);
         p.from = static_cast<int>(from), p.past = static_cast<int>(past), p.band = band_of(dim, plan.pairs_logits ? 256 : 128), p.scale_log2 = scale * LOG2E;
-        if (int rc = start_either<GradTask>(plan.pairs_logits, logits, p, rows, past - from, 1, st)) return rc;
-        if (dhidden != nullptr) {
-            if (int rc = describe_operand(&to_hidden.b, "weight", false, true, static_cast<const __nv_bfloat16 *>(weight) + from * weight_stride, dim, past - from, 1, weight_stride * 2, 0)) return rc;
-            HiddenParams h{};
-            const int64_t steps = (past - from + K_STEP - 1) / K_STEP;
-            h.count = q.count, h.index = q.index, h.to = direct ? q.dhidden : nullptr, h.to_stride = dhidden_stride;
-            h.tiles_n = static_cast<int>(tiles_of(dim, plan.pairs_hidden ? 256 : 128)), h.band = 8, h.dim = q.dim;
-            h.shares = static_cast<int>(plan.shares), h.steps = static_cast<int>(steps), h.add = i > 0;
-            if (int rc = start_either<HiddenTask>(plan.pairs_hidden, to_hidden, h, rows, dim, plan.shares, st)) return rc;
-        }
-        if (dweight != nullptr) {
-            const int side = plan.pairs_weight ? 256 : 128;
-            WeightParams w{};
-            w.count = q.count, w.n = q.n, w.tiles_m = static_cast<int>(tiles_of(past - from, side)), w.tiles_n = static_cast<int>(tiles_of(dim, side)), w.band = 8, w.vocab = static_cast<int>(past), w.dim = q.dim,
-            w.from = static_cast<int>(from);
-            if (int rc = start_either<WeightTask>(plan.pairs_weight, to_weight, w, past - from, dim, 1, st)) return rc;
-        }
+        const int64_t columns = past - from;
+        const int side = plan.pairs_logits ? 256 : 128, back_side = plan.pairs_back ? 256 : 128;
+        if (int rc = start_either<GradTask>(plan.pairs_logits, logits, p, tiles_of(rows, side) * tiles_of(columns, side), st)) return rc;
+        if (dhidden != nullptr)       // the weights' rows from the piece's first on
+            if (int rc = describe_operand(&back.b, "weight", false, true, static_cast<const __nv_bfloat16 *>(weight) + from * weight_stride, dim, columns, 1, weight_stride * 2, 0)) return rc;
+        BackParams b{};
+        b.count = q.count, b.index = q.index, b.to = direct ? q.dhidden : nullptr, b.to_stride = dhidden_stride, b.n = q.n, b.dim = q.dim, b.from = p.from, b.past = p.past;
+        b.tiles_n = static_cast<int>(tiles_of(dim, back_side)), b.tiles_w = dweight != nullptr ? static_cast<int>(tiles_of(columns, back_side)) : 0;
+        b.shares = static_cast<int>(plan.shares), b.steps = static_cast<int>(tiles_of(columns, K_STEP)), b.add = i > 0, b.hidden = dhidden != nullptr;
+        const int64_t tiles = (dhidden != nullptr ? tiles_of(rows, back_side) * b.tiles_n * plan.shares : 0) + static_cast<int64_t>(b.tiles_w) * b.tiles_n;
+        if (int rc = start_either<BackTask>(plan.pairs_back, back, b, tiles, st)) return rc;
     }
     if (dhidden != nullptr && !direct) {
         const int64_t blocks = (rows * (dim / 8) + 255) / 256;
