@@ -183,7 +183,7 @@ struct SumParams {
     void *dweight;
     float *parts;                               // [pieces][2][pitch]: of the row that began before, and of the one that goes on
     int64_t dout_stride, base_stride, dweight_stride, cols, pitch;
-    int length, pieces, across;                 // tokens of a piece, pieces, CTAs across a row
+    int length, pieces, across, across_join;    // tokens of a piece, pieces, CTAs across a row
     int vocab, rows_each;                       // rows of the table to a CTA that fills
     float scale;
 };
@@ -243,17 +243,12 @@ __device__ __forceinline__ void fill_rows(const SumParams &p, int64_t first, int
 }
 
 // A piece of the list to a CTA, eight columns to a thread, AHEAD rows of dout (and of the base, where a row's tokens
-// end) on their way at a time; behind those, CTAs that fill the rows without tokens.
+// end) on their way at a time.
 template <typename D, typename T, bool WHOLE>
 __global__ void __launch_bounds__(256, 3) k_embed_sum(const SumParams p) {
     __shared__ int token[MAX_LENGTH], row[MAX_LENGTH + 2];       // row[0], row[n + 1]: the neighbours' (-1: none)
     let_next_begin();
     after_previous();
-    const int summing = p.pieces * p.across;
-    if (static_cast<int>(blockIdx.x) >= summing) {
-        fill_rows<T, WHOLE>(p, (static_cast<int64_t>(blockIdx.x) - summing) * p.rows_each, blockDim.x);
-        return;
-    }
     const int piece = blockIdx.x / p.across, all = *p.count, begin = piece * p.length, n = min(p.length, all - begin);
     if (n <= 0) return;
     for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {
@@ -305,22 +300,28 @@ __global__ void __launch_bounds__(256, 3) k_embed_sum(const SumParams p) {
 }
 
 // A row whose tokens go on behind the piece in which they begin: that piece's sum, then the next ones', in order, four
-// columns to a thread and up to JOINED pieces on their way at a time.
+// columns to a thread and up to JOINED pieces on their way at a time.  Behind the CTAs of the pieces come those that fill the
+// rows without tokens: a row of many tokens, which one or two CTAs join, does not hold up the memory.
 constexpr int JOINED = 16;
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
     let_next_begin();
     after_previous();
-    const int all = *p.count, begin = blockIdx.x * p.length, end = begin + p.length;
+    const int joining = p.pieces > 1 ? p.pieces * p.across_join : 0;
+    if (static_cast<int>(blockIdx.x) >= joining) {
+        fill_rows<T, WHOLE>(p, (static_cast<int64_t>(blockIdx.x) - joining) * p.rows_each, blockDim.x);
+        return;
+    }
+    const int mine = blockIdx.x / p.across_join, all = *p.count, begin = mine * p.length, end = begin + p.length;
     if (end >= all) return;
     const int row = p.row[end - 1];
     if (p.row[end] != row || (begin > 0 && p.row[begin - 1] == row)) return;
-    const int64_t c = (static_cast<int64_t>(blockIdx.y) * blockDim.x + threadIdx.x) * 4;
+    const int64_t c = (static_cast<int64_t>(blockIdx.x - mine * p.across_join) * blockDim.x + threadIdx.x) * 4;
     if (c >= p.cols) return;
     const float *const parts = p.parts + c;
     const int64_t last = (p.past[row] - 1) / p.length;       // the piece in which the row's tokens end
-    float4 sum = *reinterpret_cast<const float4 *>(parts + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * p.pitch);
-    for (int64_t piece = blockIdx.x + 1; piece <= last; piece += JOINED) {
+    float4 sum = *reinterpret_cast<const float4 *>(parts + (static_cast<int64_t>(mine) * 2 + 1) * p.pitch);
+    for (int64_t piece = mine + 1; piece <= last; piece += JOINED) {
         float4 v[JOINED];
 #pragma unroll
         for (int u = 0; u < JOINED; ++u)       // (past the last: that again, and not added)
@@ -346,12 +347,14 @@ int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // How the gradient's work is cut: from the sizes alone.
 struct Plan {
-    int64_t owners, most, threads, across, length, pieces, pitch, at_row, at_past, at_parts, bytes;
+    int64_t owners, most, threads, across, threads_join, across_join, length, pieces, pitch, at_row, at_past, at_parts, bytes;
     Plan(int64_t tokens, int64_t cols, int64_t vocab) {
         // a CTA for each SM, more where a CTA's counts would not fit its shared memory
         owners = std::max<int64_t>(SMS, (vocab + MOST_ROWS - 1) / MOST_ROWS), most = (vocab + owners - 1) / owners;
         const int64_t vectors = (cols + 7) / 8;
         threads = std::min<int64_t>(256, up(vectors, 32)), across = (vectors + threads - 1) / threads;
+        const int64_t fours = (cols + 3) / 4;
+        threads_join = std::min<int64_t>(256, up(fours, 32)), across_join = (fours + threads_join - 1) / threads_join;
         // six CTAs of 256 threads to an SM or fewer; short pieces leave more rows to be joined
         length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(16, tokens * across / (SMS * 6 * 256 / threads)));
         pieces = (tokens + length - 1) / length;
@@ -399,14 +402,11 @@ int gradient(const ListParams &l, const SumParams &s, const Plan &plan, cudaStre
     if (bytes > 40 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB with what is static need no leave
     k_embed_list<<<static_cast<unsigned>(plan.owners), LIST_THREADS, bytes, st>>>(l);
     KT_CUDA(cudaGetLastError());
-    const int64_t fillers = s.base == s.dweight ? 0 : (s.vocab + s.rows_each - 1) / s.rows_each, blocks = plan.pieces * plan.across + fillers;
-    if (blocks > INT32_MAX) return fail(KT_ERR_SHAPE, "tokens x columns are too many");
-    if (blocks == 0) return KT_OK;
-    KT_CUDA(launch_behind(k_embed_sum<D, T, WHOLE>, 1, dim3(static_cast<unsigned>(blocks)), dim3(static_cast<unsigned>(plan.threads)), 0, st, s));
-    if (plan.pieces > 1) {
-        const int64_t fours = (s.cols + 3) / 4, threads = std::min<int64_t>(256, up(fours, 32));
-        KT_CUDA(launch_behind(k_embed_join<T, WHOLE>, 1, dim3(static_cast<unsigned>(plan.pieces), static_cast<unsigned>((fours + threads - 1) / threads)), dim3(static_cast<unsigned>(threads)), 0, st, s));
-    }
+    const int64_t summing = plan.pieces * plan.across, fillers = s.base == s.dweight ? 0 : (s.vocab + s.rows_each - 1) / s.rows_each;
+    const int64_t ending = (plan.pieces > 1 ? plan.pieces * plan.across_join : 0) + fillers;
+    if (summing > INT32_MAX || ending > INT32_MAX) return fail(KT_ERR_SHAPE, "tokens x columns are too many");
+    if (summing > 0) KT_CUDA(launch_behind(k_embed_sum<D, T, WHOLE>, 1, dim3(static_cast<unsigned>(summing)), dim3(static_cast<unsigned>(plan.threads)), 0, st, s));
+    if (ending > 0) KT_CUDA(launch_behind(k_embed_join<T, WHOLE>, 1, dim3(static_cast<unsigned>(ending)), dim3(static_cast<unsigned>(plan.threads_join)), 0, st, s));
     return KT_OK;
 }
 
@@ -450,9 +450,9 @@ int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids,
     const ListParams l{ids, token, row, count, past, static_cast<int>(tokens), static_cast<int>(vocab), static_cast<int>(plan.owners), static_cast<int>(plan.most),
                        static_cast<unsigned>((UINT64_C(1) << 32) / static_cast<uint64_t>(plan.owners))};
     // CTAs that fill take 16 vectors to a thread
-    const int64_t rows_each = std::max<int64_t>(1, plan.threads * 16 * 8 / cols);
+    const int64_t rows_each = std::max<int64_t>(1, plan.threads_join * 16 * 8 / cols);
     const SumParams s{token, row, count, past, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(plan.length),
-                      static_cast<int>(plan.pieces), static_cast<int>(plan.across), static_cast<int>(vocab), static_cast<int>(rows_each), scale};
+                      static_cast<int>(plan.pieces), static_cast<int>(plan.across), static_cast<int>(plan.across_join), static_cast<int>(vocab), static_cast<int>(rows_each), scale};
     const bool vectors = (tokens == 0 || whole(dout, dout_stride, tokens, dtype)) && whole(dweight, dweight_stride, vocab, param_dtype) && (base == nullptr || whole(base, base_stride, vocab, param_dtype));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (param_dtype == KT_F32) {

@@ -171,9 +171,8 @@ struct SymmetricTask : InTurn<SymmetricTask<PAIR_, DOWN, FACTOR>, OrthParams> {
 #pragma unroll
             for (int u = 0; u < 4; ++u) g[u] = from[u];
         };
-        of_gram(t.n);
-        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
-            const int c0 = t.n + c;
+        of_gram(part.col);
+        over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
             if (c0 >= p.rows) return;
             uint32_t v[16];
             [[maybe_unused]] const int d = part.row - c0;
@@ -224,8 +223,7 @@ struct ApplyTask : InTurn<ApplyTask<PAIR_, WIDE, LAST>, OrthParams> {
     }
     __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
         if (part.warp_row >= p.rows) return;
-        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
-            const int c0 = t.n + c;
+        over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
             if (c0 - half * 32 >= p.cols) return;
             float x[32];
 #pragma unroll

@@ -2,8 +2,8 @@
 // leave the chip: C = A B^T over 16-bit operands with fp32 sums, one tile of C after the other.
 //
 // Roles of a CTA: one thread brings tiles (TMA) into a ring of shared memory, one issues the matrix instructions,
-// and two groups of four warps take the finished sums out of tensor memory, each its own of two buffers, while the
-// next tile is being multiplied.  With PAIR two CTAs of a cluster share a tile of 256 x 256: each brings its own
+// and two groups of four warps take the finished sums out of tensor memory, each half of the columns, while the
+// next tile is being multiplied into the other of two buffers.  With PAIR two CTAs of a cluster share a tile of 256 x 256: each brings its own
 // 128 rows of A and of B and keeps the sums of its own 128 rows of C, and one instruction multiplies in both.  A
 // CTA then reads 32 KB for 2 x 128 x 128 x 64 products, half of what it reads alone.  Without it a CTA works on
 // 128 x 128 by itself: for products too small to give every pair a tile.
@@ -141,9 +141,9 @@ __device__ __forceinline__ void load_operand(uint32_t to, const CUtensorMap *map
 }
 
 // ----------------------------------------------------------------------------- finishing
-// What a thread of the finishing warps has of a tile: a row, and its sums 32 columns at a time.
+// What a thread of the finishing warps has of a tile: half of a row, and its sums 32 columns at a time.
 struct Part {
-    int row;                                    // of C
+    int row, col, half;                         // of C: the row, the first column, which half
     uint32_t at;                                // its sums in tensor memory
     uint8_t *store;                             // of the warp: 32 rows of 128 bytes, of two places the one in turn
     int turn;
@@ -196,8 +196,8 @@ struct Part {
     }
 };
 
-// f(column, whether it is the second of two, sums of 32 columns) for COLS columns of the thread's row, 64 at a time; the next
-// columns are on their way meanwhile.
+// f(column of C, whether it is the second of two, sums of 32 columns) for COLS columns of the thread's row, 64 at a time; the
+// next columns are on their way meanwhile.
 template <int N>
 struct Constant {
     __device__ constexpr operator int() const { return N; }
@@ -211,10 +211,10 @@ __device__ __forceinline__ void over_columns(Part &part, F f) {
     for (int c = 0; c < COLS; c += 64) {
         part.get(r[0]);
         part.ask(c + 32, r[1]);
-        f(c, Constant<0>(), r[0]);
+        f(part.col + c, Constant<0>(), r[0]);
         part.get(r[1]);
         if (c + 64 < COLS) part.ask(c + 64, r[0]);
-        f(c + 32, Constant<1>(), r[1]);
+        f(part.col + c + 32, Constant<1>(), r[1]);
     }
 }
 
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     let_next_begin();
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) bar_init(&sm.full[i], 1), bar_init(&sm.free[i], 1);
-        for (int i = 0; i < 2; ++i) bar_init(&sm.sums_full[i], 1), bar_init(&sm.sums_taken[i], PAIR ? 8 : 4);
+        for (int i = 0; i < 2; ++i) bar_init(&sm.sums_full[i], 1), bar_init(&sm.sums_taken[i], PAIR ? 16 : 8);
         sm.waits = {wait_ns, 0};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
@@ -297,21 +297,23 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     } else if (warp >= PRODUCT_FINISH) {
         const uint32_t group = (warp - PRODUCT_FINISH) / 4, quarter = warp % 4;
         Part part;
-        part.at = tmem + group * SIDE + ((quarter * 32) << 16);
+        part.half = static_cast<int>(group);
         part.store = sm.store[warp - PRODUCT_FINISH][0], part.turn = 0;
-        part.there = true, part.full = &sm.sums_full[group], part.waits = waits;
-        for (int done = static_cast<int>(group); done < tiles; done += 2) {
+        part.there = true, part.waits = waits;
+        for (int done = 0; done < tiles; ++done) {
             const Tile t = Task::tile(p, worker, workers, done);
             part.warp_row = t.m + static_cast<int>(rank * TILE + quarter * 32);
             part.row = part.warp_row + lane;
             part.zero = t.steps == 0;
-            part.parity = done / 2 & 1, part.waited = false;
+            part.col = t.n + static_cast<int>(group) * (SIDE / 2);
+            part.at = tmem + (done & 1) * SIDE + group * (SIDE / 2) + ((quarter * 32) << 16);
+            part.full = &sm.sums_full[done & 1], part.parity = done / 2 & 1, part.waited = false;
             Task::finish(p, maps, t, part);
             part.wait();
             if (part.there) {
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_at(PAIR ? address_in(smem_addr(&sm.sums_taken[group]), 0) : smem_addr(&sm.sums_taken[group]));
+                if (lane == 0) arrive_at(PAIR ? address_in(smem_addr(&sm.sums_taken[done & 1]), 0) : smem_addr(&sm.sums_taken[done & 1]));
             }
         }
         if (lane == 0) stores_done();

@@ -146,7 +146,7 @@ struct LogitsParams {
     const int *count, *index;
     const Row *rows;
     const int64_t *targets;                     // where nothing was left out, because one tile holds all rows: instead of the three
-    float2 *parts;                              // [tiles of columns][n]: maximum (units of log 2) and sum
+    float2 *parts;                              // [half tiles of columns][n]: maximum (units of log 2) and sum
     float *at_target;                           // the target's logit (units of log 2)
     int n, vocab, steps, from, past, band;      // columns from ... past of the vocabulary
     float scale_log2;
@@ -183,8 +183,7 @@ struct LossTask : LogitsTask<PAIR_> {
         const bool counts = part.row < p.counted();
         const int target = counts ? p.row(part.row).target : -1;
         float top = -INFINITY, sum = 0.0f;
-        over_columns<Base::SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
-            const int v0 = t.n + c;
+        over_columns<Base::SIDE / 2>(part, [&](int v0, auto half, uint32_t (&r)[32]) {
             if (v0 >= p.vocab) return;
             if (v0 + 32 > p.vocab)
 #pragma unroll
@@ -215,7 +214,7 @@ struct LossTask : LogitsTask<PAIR_> {
                 p.at_target[part.row] = x * p.scale_log2;
             }
         });
-        if (counts) p.parts[static_cast<int64_t>(t.n / Base::SIDE) * p.n + part.row] = make_float2(top, sum);
+        if (counts) p.parts[static_cast<int64_t>(part.col / (Base::SIDE / 2)) * p.n + part.row] = make_float2(top, sum);
     }
 };
 
@@ -239,8 +238,7 @@ struct GradTask : LogitsTask<PAIR_> {
         if (part.warp_row >= round_to(count, TILE)) return;
         const bool counts = part.row < count;
         const Row row = counts ? p.rows[part.row] : Row{-1, 0.0f, 0.0f, 0.0f};
-        over_columns<Base::SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
-            const int v0 = t.n + c;
+        over_columns<Base::SIDE / 2>(part, [&](int v0, auto half, uint32_t (&r)[32]) {
             if (v0 - half * 32 >= p.past) return;
             if (half == 0) part.store_next();
             const int d = row.target - v0, left = p.past - v0;
@@ -330,8 +328,7 @@ struct BackTask {
         const bool weight = t.kind == 1;
         if (weight ? p.from + part.warp_row >= p.past : part.warp_row >= count) return;
         __nv_bfloat16 *const row = !weight && p.to != nullptr && part.row < count ? p.to + p.index[part.row] * p.to_stride : nullptr;
-        over_columns<SIDE>(part, [&](int c, auto half, uint32_t (&r)[32]) {
-            const int c0 = t.n + c;
+        over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
             if (weight) {
                 if (c0 - half * 32 >= p.dim) return;
                 if (half == 0) part.store_next();
@@ -465,7 +462,7 @@ struct Plan {
         const int64_t workers = pairs_back ? PRODUCT_SMS / 2 : PRODUCT_SMS, hidden = tiles_of(n, side) * tiles_of(dim, side), weight = tiles_of(piece, side) * tiles_of(dim, side);
         const int64_t mean = (hidden * steps + weight * over_rows) / workers, longest = mean < 16 ? 16 : mean;
         shares = (steps + longest - 1) / longest;
-        at_parts = take(backward ? 0 : 8 * n * tiles_of(vocab, pairs_logits ? 256 : 128)), at_target = take(backward ? 0 : 4 * n);
+        at_parts = take(backward ? 0 : 8 * n * 2 * tiles_of(vocab, pairs_logits ? 256 : 128)), at_target = take(backward ? 0 : 4 * n);
         at_p = take(backward ? 2 * up(n, TILE) * piece : 0);
         at_sums = take(backward && (pieces > 1 || shares > 1) ? 4 * shares * n * dim : 0);
         bytes = at;
@@ -572,7 +569,7 @@ int kt_xent_forward(const void *hidden, int64_t hidden_stride, const void *weigh
         p.targets = targets;
     }
     if (int rc = start_either<LossTask>(plan.pairs_logits, maps, p, tiles_of(rows, side) * tiles_of(vocab, side), st, leave_out)) return rc;
-    KT_CUDA(launch_behind(k_xent_join, 1, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, p, static_cast<int>(tiles_of(vocab, side)), loss, lse));
+    KT_CUDA(launch_behind(k_xent_join, 1, dim3(static_cast<unsigned>((rows + 7) / 8)), dim3(256), 0, st, p, static_cast<int>(tiles_of(vocab, side / 2)), loss, lse));
     return KT_OK;
 }
 
