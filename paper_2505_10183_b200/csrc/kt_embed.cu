@@ -183,7 +183,7 @@ struct SumParams {
     void *dweight;
     float *parts;                               // [pieces][2][pitch]: of the row that began before, and of the one that goes on
     int64_t dout_stride, base_stride, dweight_stride, cols, pitch;
-    int length, pieces, across, across_join;    // tokens of a piece, pieces, CTAs across a row
+    int tokens, length, pieces, across, across_join;    // all tokens, those of a piece, pieces, CTAs across a row
     int vocab, rows_each;                       // rows of the table to a CTA that fills
     float scale;
 };
@@ -216,28 +216,32 @@ struct Raw {
     }
 };
 
-// Rows of the table that no token has: zeros, or the base's.
+// Rows of the table that no token has: zeros, or the base's; a row to a warp at a time.
 template <typename T, bool WHOLE>
-__device__ __forceinline__ void fill_rows(const SumParams &p, int64_t first, int threads) {
-    const int vectors = static_cast<int>((p.cols + 7) / 8), all = static_cast<int>(min(static_cast<int64_t>(p.rows_each), p.vocab - first)) * vectors;
-    for (int i0 = threadIdx.x; i0 < all; i0 += 4 * threads) {
-        Raw<T, WHOLE> v[4];
-        bool there[4];
+__device__ __forceinline__ void fill_rows(const SumParams &p, int64_t first) {
+    const int rows = static_cast<int>(min(static_cast<int64_t>(p.rows_each), p.vocab - first)), lane = threadIdx.x % 32, warps = blockDim.x / 32, vectors = static_cast<int>((p.cols + 7) / 8);
+    const unsigned empty = __ballot_sync(0xFFFFFFFFu, lane < rows && p.past[first + min(lane, rows - 1)] == 0);
+    int nth = -1;
+    for (unsigned left = empty; left != 0; left &= left - 1) {
+        if (++nth % warps != static_cast<int>(threadIdx.x) / 32) continue;
+        const int64_t row = first + __ffs(static_cast<int>(left)) - 1;
+        T *const to = static_cast<T *>(p.dweight) + row * p.dweight_stride;
+        const T *const like = p.base != nullptr ? static_cast<const T *>(p.base) + row * p.base_stride : nullptr;
+        for (int c0 = lane; c0 < vectors; c0 += 4 * 32) {
+            Raw<T, WHOLE> v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int i = i0 + u * threads, r = i / vectors;
-            there[u] = i < all && p.past[first + r] == 0;
-            v[u] = {};
-            if (there[u] && p.base != nullptr) v[u].read(static_cast<const T *>(p.base) + (first + r) * p.base_stride, (i - r * vectors) * 8, p.cols);
-        }
+            for (int u = 0; u < 4; ++u) {
+                v[u] = {};
+                if (like != nullptr && c0 + u * 32 < vectors) v[u].read(like, (c0 + u * 32) * static_cast<int64_t>(8), p.cols);
+            }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (!there[u]) continue;
-            const int i = i0 + u * threads, r = i / vectors;
-            float x[8];
-            zeros(x);
-            v[u].add_to(x);
-            write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + (first + r) * p.dweight_stride, (i - r * vectors) * 8, p.cols, x);
+            for (int u = 0; u < 4; ++u)
+                if (c0 + u * 32 < vectors) {
+                    float x[8];
+                    zeros(x);
+                    v[u].add_to(x);
+                    write_eight<T, WHOLE>(to, (c0 + u * 32) * static_cast<int64_t>(8), p.cols, x);
+                }
         }
     }
 }
@@ -249,13 +253,16 @@ __global__ void __launch_bounds__(256, 3) k_embed_sum(const SumParams p) {
     __shared__ int token[MAX_LENGTH], row[MAX_LENGTH + 2];       // row[0], row[n + 1]: the neighbours' (-1: none)
     let_next_begin();
     after_previous();
-    const int piece = blockIdx.x / p.across, all = *p.count, begin = piece * p.length, n = min(p.length, all - begin);
-    if (n <= 0) return;
-    for (int i = threadIdx.x; i < n + 2; i += blockDim.x) {
+    const int piece = blockIdx.x / p.across, begin = piece * p.length;
+    const int all = *p.count, n = min(p.length, all - begin);
+    for (int i = threadIdx.x; i < p.length + 2; i += blockDim.x) {       // (asked for at once; what lies past the list's end is not used)
         const int at = begin + i - 1;
-        row[i] = at >= 0 && at < all ? p.row[at] : -1;
-        if (i >= 1 && i <= n) token[i - 1] = p.token[at];
+        const bool inside = at >= 0 && at < p.tokens;
+        const int r = inside ? p.row[at] : -1, t = inside ? p.token[at] : 0;
+        row[i] = at < all ? r : -1;
+        if (i >= 1 && i <= p.length) token[i - 1] = t;
     }
+    if (n <= 0) return;
     __syncthreads();
     const int64_t c = (static_cast<int64_t>(blockIdx.x - piece * p.across) * blockDim.x + threadIdx.x) * 8;
     if (c >= p.cols) return;
@@ -309,13 +316,13 @@ __global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
     after_previous();
     const int joining = p.pieces > 1 ? p.pieces * p.across_join : 0;
     if (static_cast<int>(blockIdx.x) >= joining) {
-        fill_rows<T, WHOLE>(p, (static_cast<int64_t>(blockIdx.x) - joining) * p.rows_each, blockDim.x);
+        fill_rows<T, WHOLE>(p, (static_cast<int64_t>(blockIdx.x) - joining) * p.rows_each);
         return;
     }
-    const int mine = blockIdx.x / p.across_join, all = *p.count, begin = mine * p.length, end = begin + p.length;
-    if (end >= all) return;
-    const int row = p.row[end - 1];
-    if (p.row[end] != row || (begin > 0 && p.row[begin - 1] == row)) return;
+    const int mine = blockIdx.x / p.across_join, begin = mine * p.length, end = begin + p.length, all = *p.count;
+    if (end >= p.tokens) return;
+    const int row = p.row[end - 1], next = p.row[end], before = begin > 0 ? p.row[begin - 1] : -1;       // (asked for at once)
+    if (end >= all || next != row || before == row) return;
     const int64_t c = (static_cast<int64_t>(blockIdx.x - mine * p.across_join) * blockDim.x + threadIdx.x) * 4;
     if (c >= p.cols) return;
     const float *const parts = p.parts + c;
@@ -356,7 +363,7 @@ struct Plan {
         const int64_t fours = (cols + 3) / 4;
         threads_join = std::min<int64_t>(256, up(fours, 32)), across_join = (fours + threads_join - 1) / threads_join;
         // six CTAs of 256 threads to an SM or fewer; short pieces leave more rows to be joined
-        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(16, tokens * across / (SMS * 6 * 256 / threads)));
+        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(8, tokens * across / (SMS * 6 * 256 / threads)));
         pieces = (tokens + length - 1) / length;
         pitch = up(cols, 8);
         int64_t at = 1024 + up(tokens * 4, 1024);      // the list's length and tokens
@@ -449,9 +456,9 @@ int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids,
     int *const past = reinterpret_cast<int *>(ws + plan.at_past);
     const ListParams l{ids, token, row, count, past, static_cast<int>(tokens), static_cast<int>(vocab), static_cast<int>(plan.owners), static_cast<int>(plan.most),
                        static_cast<unsigned>((UINT64_C(1) << 32) / static_cast<uint64_t>(plan.owners))};
-    // CTAs that fill take 16 vectors to a thread
-    const int64_t rows_each = std::max<int64_t>(1, plan.threads_join * 16 * 8 / cols);
-    const SumParams s{token, row, count, past, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(plan.length),
+    // CTAs that fill take 64 KB, but a row to each warp at least, and as many as a warp has lanes at most
+    const int64_t rows_each = std::min<int64_t>(32, std::max<int64_t>(plan.threads_join / 32, 65536 / (cols * (param_dtype == KT_F32 ? 4 : 2))));
+    const SumParams s{token, row, count, past, dout, base, dweight, reinterpret_cast<float *>(ws + plan.at_parts), dout_stride, base_stride, dweight_stride, cols, plan.pitch, static_cast<int>(tokens), static_cast<int>(plan.length),
                       static_cast<int>(plan.pieces), static_cast<int>(plan.across), static_cast<int>(plan.across_join), static_cast<int>(vocab), static_cast<int>(rows_each), scale};
     const bool vectors = (tokens == 0 || whole(dout, dout_stride, tokens, dtype)) && whole(dweight, dweight_stride, vocab, param_dtype) && (base == nullptr || whole(base, base_stride, vocab, param_dtype));
     cudaStream_t st = static_cast<cudaStream_t>(stream);

@@ -27,6 +27,7 @@ using namespace ktd;
 namespace {
 
 constexpr float X_UNIT = 128.0f, A_UNIT = 16384.0f, FACTOR_UNIT = 8192.0f;
+constexpr int MAX_STEPS = 64;
 constexpr int SUM_BLOCKS = 256;                 // partial sums of squares to a matrix, at most: a thread reads one
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -119,76 +120,100 @@ __global__ void __launch_bounds__(256) k_orth_start(const StartParams p) {
 }
 
 // ------------------------------------------------------------------------------------ products
+struct OrthMaps {
+    CUtensorMap a, b, out, mirror;
+};
+enum { GRAM, FACTOR, APPLY, LAST };             // which product
+
 struct OrthParams {
-    int rows, cols, tiles_m, tiles_n, batch, steps;        // of the result; stages of the reduction
+    int rows, cols, side, batch;
     int whole;                                  // both sides of a symmetric result are computed
-    int64_t pitch;                              // of a symmetric result, in elements
-    const __half *gram;                         // A, for the factor
-    float a, b, c;
-    void *out;                                  // of the last product
+    int by_copies;                              // the result goes out like the others; else by single elements
+    int64_t pitch;                              // of A, in elements
+    const __half *gram;
+    float a, b, c, scale;
+    __nv_bfloat16 *out;
     int64_t out_stride[2];
 };
 
-// 32 values of the thread's row as fp16 into half of the store's rows.
-__device__ __forceinline__ void pack_halves(const Part &part, int half, const float (&x)[32]) {
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        uint4 v;
-        v.x = pack_half(x[u * 8], x[u * 8 + 1]), v.y = pack_half(x[u * 8 + 2], x[u * 8 + 3]), v.z = pack_half(x[u * 8 + 4], x[u * 8 + 5]), v.w = pack_half(x[u * 8 + 6], x[u * 8 + 7]);
-        *part.piece(half * 4 + u) = v;
-    }
-}
-
-// A symmetric matrix: A (FACTOR false, from X along or down its rows) or the factor a I + b A + c A^2 (from A).
-// The mirrored side of 32 x 32 values goes through shared memory, where lanes are columns: two lanes swap halves, so
-// that each writes two neighbours of one row.  (Two-byte stores straight to memory took 27 us to a tile, more than its product.)
-template <bool PAIR_, bool DOWN, bool FACTOR>
-struct SymmetricTask : InTurn<SymmetricTask<PAIR_, DOWN, FACTOR>, OrthParams> {
+// Three products to a step: A, the factor a I + b A + c A^2 from it, and the next X, factor times X (WIDE) or X times factor.
+// A result leaves in boxes of 32 x 32.  The mirrored side of a symmetric one goes through shared memory, where lanes
+// are columns: two lanes swap halves, so that each writes two neighbours of one row.  (Two-byte stores straight to memory
+// took 27 us to a tile, more than its product.)
+template <bool PAIR_, bool WIDE, int KIND>
+struct OrthTask {
     using Params = OrthParams;
+    using Maps = OrthMaps;
     static constexpr bool PAIR = PAIR_, HALF = true;
-    static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int each(const Params &p) { return p.whole ? p.tiles_m * p.tiles_m : p.tiles_m * (p.tiles_m + 1) / 2; }
-    __device__ static int tiles(const Params &p) { return each(p) * p.batch; }
-    __device__ static bool a_down(const Tile &) { return DOWN; }
-    __device__ static bool b_down(const Tile &) { return DOWN; }
-    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &) { return &maps.a; }
-    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
-    __device__ static Tile tile_at(const Params &p, int i) {
-        const int z = i / each(p);
-        int m = 0, n = i - z * each(p);
-        if (p.whole) return {n / p.tiles_m * SIDE, n % p.tiles_m * SIDE, z, 0, p.steps, 0, 0};
-        for (; n >= p.tiles_m - m; ++m) n -= p.tiles_m - m;
-        return {m * SIDE, (m + n) * SIDE, z, 0, p.steps, 0, 0};
-    }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
-        if (part.warp_row >= p.rows) return;
-        const int lane = threadIdx.x % 32;
-        const bool mirrored = !p.whole && t.n != t.m;
+    static constexpr int SIDE = PAIR ? 256 : 128, BAND = 8;
+    static constexpr bool SYMMETRIC = KIND < APPLY;
+    struct Cut {
+        int worker, workers, batch, whole, side_tiles, each, tiles_m, tiles_n, steps;
+        __device__ Cut(const Params &p, int worker_, int workers_) : worker(worker_), workers(workers_), batch(p.batch), whole(p.whole) {
+            side_tiles = (p.side + SIDE - 1) / SIDE;
+            tiles_m = (p.rows + SIDE - 1) / SIDE, tiles_n = (p.cols + SIDE - 1) / SIDE;
+            each = !SYMMETRIC ? tiles_m * tiles_n : whole ? side_tiles * side_tiles : side_tiles * (side_tiles + 1) / 2;
+            steps = ((KIND != GRAM ? p.side : WIDE ? p.cols : p.rows) + K_STEP - 1) / K_STEP;
+        }
+        __device__ int count() const { return (each * batch - worker + workers - 1) / workers; }
+        __device__ Tile tile(int i) const {
+            const int at = worker + i * workers, z = at / each;
+            int m = 0, n = at - z * each;
+            if (!SYMMETRIC) {
+                const int band = n / (BAND * tiles_n), left = n - band * BAND * tiles_n, high = min(BAND, tiles_m - band * BAND);
+                m = band * BAND + left % high, n = left / high;
+            } else if (whole) {
+                m = n / side_tiles, n -= m * side_tiles;
+            } else {
+                for (; n >= side_tiles - m; ++m) n -= side_tiles - m;
+                n += m;
+            }
+            return {m * SIDE, n * SIDE, z, 0, steps, KIND, 0};
+        }
+    };
+    __device__ static bool a_down(const Tile &) { return !WIDE && KIND == GRAM; }
+    __device__ static bool b_down(const Tile &) { return WIDE ? !SYMMETRIC : KIND == GRAM; }
+    __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &, const Tile &) { return &maps.a; }
+    __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &, const Tile &) { return &maps.b; }
+    __device__ static void finish(const Params &p, const Maps &maps, const Cut &, const Tile &t, Part &part) {
+        const bool mirrored = SYMMETRIC && !p.whole && t.n != t.m;
+        const int rows = SYMMETRIC ? p.side : p.rows, cols = SYMMETRIC ? p.side : p.cols, lane = threadIdx.x % 32;
+        if (part.warp_row >= rows) return;
+        const float by = KIND == FACTOR ? p.c * (FACTOR_UNIT / A_UNIT / A_UNIT) : KIND == LAST ? p.scale / (FACTOR_UNIT * X_UNIT) : 1.0f / FACTOR_UNIT;
         uint4 g[4] = {};
-        auto of_gram = [&](int c0) {            // (rows of A are whole vectors, whatever lies past their last element)
-            if (!FACTOR || part.row >= p.rows || c0 >= p.rows) return;
-            const uint4 *from = reinterpret_cast<const uint4 *>(p.gram + (static_cast<int64_t>(t.z) * p.rows + part.row) * p.pitch + c0);
+        // (rows of A are whole vectors, whatever lies past their last element)
+        auto of_gram = [&](int c0) {
+            if (KIND != FACTOR || part.row >= p.side || c0 >= p.side) return;
+            const uint4 *from = reinterpret_cast<const uint4 *>(p.gram + (static_cast<int64_t>(t.z) * p.side + part.row) * p.pitch + c0);
 #pragma unroll
             for (int u = 0; u < 4; ++u) g[u] = from[u];
         };
         of_gram(part.col);
-        over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
-            if (c0 >= p.rows) return;
+        over_columns<SIDE / 2>(part, [&](int c0, auto, uint32_t (&r)[32]) {
+            if (c0 >= cols) return;
             uint32_t v[16];
             [[maybe_unused]] const int d = part.row - c0;
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
-                float2 x = pair_of(r, e);
-                if constexpr (FACTOR) {
+                float2 x = KIND == GRAM ? pair_of(r, e) : mul2(pair_of(r, e), both(by));
+                if constexpr (KIND == FACTOR) {
                     const uint32_t w = e % 8 / 2 == 0 ? g[e / 8].x : e % 8 / 2 == 1 ? g[e / 8].y : e % 8 / 2 == 2 ? g[e / 8].z : g[e / 8].w;
-                    const float2 in = __half22float2(*reinterpret_cast<const __half2 *>(&w));
-                    x = fma2(in, both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(x, both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
+                    x = fma2(__half22float2(*reinterpret_cast<const __half2 *>(&w)), both(p.b * (FACTOR_UNIT / A_UNIT)), x);
                     if (e == d) x.x += p.a * FACTOR_UNIT;
                     if (e + 1 == d) x.y += p.a * FACTOR_UNIT;
                 }
-                v[e / 2] = pack_half(x.x, x.y);
+                v[e / 2] = KIND == LAST ? pack_bf16(x) : pack_half(x.x, x.y);
             }
             of_gram(c0 + 32);
+            if (KIND == LAST && !p.by_copies) {
+                if (part.row < rows) {
+                    __nv_bfloat16 *const row = p.out + t.z * p.out_stride[0] + part.row * p.out_stride[1] + c0;
+#pragma unroll
+                    for (int e = 0; e < 32; ++e)
+                        if (c0 + e < cols) row[e] = __ushort_as_bfloat16(static_cast<unsigned short>(e % 2 ? v[e / 2] >> 16 : v[e / 2] & 0xFFFF));
+                }
+                return;
+            }
             part.store_next();
 #pragma unroll
             for (int u = 0; u < 4; ++u)         // rows of 64 bytes, in the 64-byte swizzle
@@ -201,52 +226,7 @@ struct SymmetricTask : InTurn<SymmetricTask<PAIR_, DOWN, FACTOR>, OrthParams> {
                     *reinterpret_cast<uint32_t *>(mirror + e * 128) = lane & 1 ? (theirs >> 16) | (v[e] & 0xFFFF0000u) : (v[e] & 0xFFFFu) | (theirs << 16);
                 }
             }
-            part.send(&maps.out, c0, part.warp_row, t.z, false, mirrored ? &maps.out2 : nullptr, STORE_BYTES / 2, part.warp_row, c0);
-        });
-    }
-};
-
-// The next X: factor times X (WIDE), or X times factor; the last time to the result.
-template <bool PAIR_, bool WIDE, bool LAST>
-struct ApplyTask : InTurn<ApplyTask<PAIR_, WIDE, LAST>, OrthParams> {
-    using Params = OrthParams;
-    static constexpr bool PAIR = PAIR_, HALF = true;
-    static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles(const Params &p) { return p.tiles_m * p.tiles_n * p.batch; }
-    __device__ static bool a_down(const Tile &) { return false; }
-    __device__ static bool b_down(const Tile &) { return WIDE; }
-    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &) { return &maps.a; }
-    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
-    __device__ static Tile tile_at(const Params &p, int i) {
-        const int each = p.tiles_m * p.tiles_n, z = i / each, in = i - z * each, band = in / (8 * p.tiles_n), left = in - band * 8 * p.tiles_n, high = min(8, p.tiles_m - band * 8);
-        return {(band * 8 + left % high) * SIDE, left / high * SIDE, z, 0, p.steps, 0, 0};
-    }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
-        if (part.warp_row >= p.rows) return;
-        over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
-            if (c0 - half * 32 >= p.cols) return;
-            float x[32];
-#pragma unroll
-            for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(r[e]) * p.a;
-            if constexpr (!LAST) {
-                if (half == 0) part.store_next();
-                pack_halves(part, half, x);
-                if (half == 1) part.send(&maps.out, c0 - 32, part.warp_row, t.z);
-            } else if (part.row < p.rows && c0 < p.cols) {
-                __nv_bfloat16 *const row = static_cast<__nv_bfloat16 *>(p.out) + t.z * p.out_stride[0] + part.row * p.out_stride[1] + c0;
-                if (c0 + 32 <= p.cols && reinterpret_cast<uintptr_t>(row) % 16 == 0) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint4 v;
-                        v.x = pack_bf16(x[e], x[e + 1]), v.y = pack_bf16(x[e + 2], x[e + 3]), v.z = pack_bf16(x[e + 4], x[e + 5]), v.w = pack_bf16(x[e + 6], x[e + 7]);
-                        *reinterpret_cast<uint4 *>(row + e) = v;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (c0 + e < p.cols) row[e] = __float2bfloat16_rn(x[e]);
-                }
-            }
+            part.send(&maps.out, c0, part.warp_row, t.z, false, mirrored ? &maps.mirror : nullptr, STORE_BYTES / 2, part.warp_row, c0);
         });
     }
 };
@@ -286,48 +266,45 @@ int check_polynomial(int steps, float a, float b, float c) {
 
 int64_t tiles_of(int64_t x, int side) { return (x + side - 1) / side; }
 
-template <bool PAIR>
-int run(const Plan &plan, char *ws, int steps, float a, float b, float c, float scale, void *out, const int64_t *out_stride, cudaStream_t st) {
+template <bool PAIR, bool WIDE>
+int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
     constexpr int SIDE = PAIR ? 256 : 128;
-    const int64_t matrix_x = plan.rows * plan.pitch_x * 2, matrix_a = plan.side * plan.pitch_a * 2, symmetric = tiles_of(plan.side, SIDE);
+    const int64_t matrix_x = plan.rows * plan.pitch_x * 2, matrix_a = plan.side * plan.pitch_a * 2, side_tiles = tiles_of(plan.side, SIDE);
     char *const gram = ws + plan.at_gram, *const factor = ws + plan.at_factor;
-    ProductMaps g{}, f{}, x{};
     const CUtensorMapDataType half = CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    for (int i = 0; i < 4; ++i)       // what both write, and its mirrored side
-        if (int rc = describe_matrix(i == 0 ? &g.out : i == 1 ? &g.out2 : i == 2 ? &f.out : &f.out2, "the workspace", half, 2, i < 2 ? gram : factor, plan.side, plan.side, plan.batch, plan.pitch_a * 2,
-                                     matrix_a, 32, 32, i % 2 == 0))
-            return rc;
-    if (int rc = describe_operand(&f.a, "the workspace", true, false, gram, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a)) return rc;
-    f.b = f.a;
-    CUtensorMap of_factor;
-    if (int rc = describe_operand(&of_factor, "the workspace", true, false, factor, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a)) return rc;
-    OrthParams pg{};
-    pg.rows = pg.cols = static_cast<int>(plan.side), pg.tiles_m = pg.tiles_n = static_cast<int>(symmetric), pg.batch = static_cast<int>(plan.batch), pg.pitch = plan.pitch_a;
+    OrthMaps of_gram{}, of_factor{}, apply[2]{};          // apply[i]: from buffer i to the other
+    CUtensorMap x[2], square, out;
+    for (int i = 0; i < 2; ++i) {
+        char *const at = ws + plan.at_x[i];
+        if (int rc = describe_operand(&x[i], "the workspace", true, !WIDE, at, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x)) return rc;
+        if (int rc = describe_operand(WIDE ? &apply[i].b : &apply[i].a, "the workspace", true, WIDE, at, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x)) return rc;
+        if (int rc = describe_matrix(&apply[1 - i].out, "the workspace", half, 2, at, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x, 32, 32)) return rc;
+        OrthMaps &m = i == 0 ? of_gram : of_factor;
+        char *const result = i == 0 ? gram : factor;
+        for (bool mirrored : {false, true})
+            if (int rc = describe_matrix(mirrored ? &m.mirror : &m.out, "the workspace", half, 2, result, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a, 32, 32, !mirrored)) return rc;
+        if (int rc = describe_operand(&square, "the workspace", true, false, result, plan.side, plan.side, plan.batch, plan.pitch_a * 2, matrix_a)) return rc;
+        if (i == 0) of_factor.a = of_factor.b = square;
+        else for (OrthMaps &to : apply) (WIDE ? to.a : to.b) = square;
+    }
+    // the copy engine takes rows and matrices at multiples of 16 bytes
+    p.by_copies = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && (plan.rows == 1 || p.out_stride[1] % 8 == 0) && (plan.batch == 1 || p.out_stride[0] % 8 == 0);
+    if (p.by_copies)
+        if (int rc = describe_matrix(&out, "out", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.out, plan.cols, plan.rows, plan.batch, p.out_stride[1] * 2, p.out_stride[0] * 2, 32, 32)) return rc;
     // Where every tile of the whole square gets a worker of its own, mirroring would only make each take longer.
-    pg.whole = symmetric * symmetric * plan.batch <= PRODUCT_SMS / (PAIR ? 2 : 1);
-    OrthParams pf = pg, px{};
-    pg.steps = static_cast<int>(tiles_of(plan.wide ? plan.cols : plan.rows, K_STEP));
-    pf.steps = static_cast<int>(tiles_of(plan.side, K_STEP)), pf.gram = reinterpret_cast<const __half *>(gram);
-    pf.a = a, pf.b = b, pf.c = c;
-    px.rows = static_cast<int>(plan.rows), px.cols = static_cast<int>(plan.cols), px.tiles_m = static_cast<int>(tiles_of(plan.rows, SIDE)), px.tiles_n = static_cast<int>(tiles_of(plan.cols, SIDE));
-    px.batch = pg.batch, px.steps = pf.steps, px.out = out, px.out_stride[0] = out_stride[0], px.out_stride[1] = out_stride[1];
-    const int64_t tiles_a = (pg.whole ? symmetric * symmetric : symmetric * (symmetric + 1) / 2) * plan.batch, tiles_x = static_cast<int64_t>(px.tiles_m) * px.tiles_n * plan.batch;
+    p.whole = side_tiles * side_tiles * plan.batch <= PRODUCT_SMS / (PAIR ? 2 : 1);
+    const int64_t symmetric = (p.whole ? side_tiles * side_tiles : side_tiles * (side_tiles + 1) / 2) * plan.batch, applied = tiles_of(plan.rows, SIDE) * tiles_of(plan.cols, SIDE) * plan.batch;
     for (int i = 0; i < steps; ++i) {
-        char *const now = ws + plan.at_x[i % 2], *const next = ws + plan.at_x[(i + 1) % 2];
-        const bool last = i + 1 == steps;
-        if (int rc = describe_operand(&g.a, "the workspace", true, !plan.wide, now, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x)) return rc;
-        g.b = g.a;
-        if (int rc = plan.wide ? start_product<SymmetricTask<PAIR, false, false>>(g, pg, tiles_a, st) : start_product<SymmetricTask<PAIR, true, false>>(g, pg, tiles_a, st)) return rc;
-        if (int rc = start_product<SymmetricTask<PAIR, false, true>>(f, pf, tiles_a, st)) return rc;
-        CUtensorMap of_x;
-        if (int rc = describe_operand(&of_x, "the workspace", true, plan.wide, now, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x)) return rc;
-        x.a = plan.wide ? of_factor : of_x, x.b = plan.wide ? of_x : of_factor;
-        if (int rc = describe_matrix(&x.out, "the workspace", half, 2, next, plan.cols, plan.rows, plan.batch, plan.pitch_x * 2, matrix_x, 64, 32)) return rc;
-        px.a = last ? scale / (FACTOR_UNIT * X_UNIT) : 1.0f / FACTOR_UNIT;
-        int rc;
-        if (plan.wide) rc = last ? start_product<ApplyTask<PAIR, true, true>>(x, px, tiles_x, st) : start_product<ApplyTask<PAIR, true, false>>(x, px, tiles_x, st);
-        else rc = last ? start_product<ApplyTask<PAIR, false, true>>(x, px, tiles_x, st) : start_product<ApplyTask<PAIR, false, false>>(x, px, tiles_x, st);
-        if (rc) return rc;
+        of_gram.a = of_gram.b = x[i % 2];
+        if (int rc = start_product<OrthTask<PAIR, WIDE, GRAM>>(of_gram, p, symmetric, st)) return rc;
+        if (int rc = start_product<OrthTask<PAIR, WIDE, FACTOR>>(of_factor, p, symmetric, st)) return rc;
+        OrthMaps m = apply[i % 2];
+        if (i + 1 < steps) {
+            if (int rc = start_product<OrthTask<PAIR, WIDE, APPLY>>(m, p, applied, st)) return rc;
+        } else {
+            if (p.by_copies) m.out = out;
+            if (int rc = start_product<OrthTask<PAIR, WIDE, LAST>>(m, p, applied, st)) return rc;
+        }
     }
     return KT_OK;
 }
@@ -377,7 +354,7 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     if (dtype != KT_F32 && dtype != KT_BF16) return fail(KT_ERR_INVALID, "unknown dtype %d", dtype);
     if (batch < 0 || rows < 0 || cols < 0 || batch > MAX_BATCH || rows > MAX_SIDE || cols > MAX_SIDE)
         return fail(KT_ERR_SHAPE, "%lld matrices of %lld x %lld: up to %lld, and %lld to a side, expected", (long long)batch, (long long)rows, (long long)cols, (long long)MAX_BATCH, (long long)MAX_SIDE);
-    if (steps < 1 || steps > 64) return fail(KT_ERR_INVALID, "%d steps: 1 to 64 expected", steps);
+    if (steps < 1 || steps > MAX_STEPS) return fail(KT_ERR_INVALID, "%d steps: 1 to %d expected", steps, MAX_STEPS);
     if (coefficients == nullptr) return fail(KT_ERR_INVALID, "coefficients is NULL");
     if (!std::isfinite(scale)) return fail(KT_ERR_INVALID, "scale must be finite");
     if (int rc = check_polynomial(steps, coefficients[0], coefficients[1], coefficients[2])) return rc;
@@ -403,8 +380,13 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     // pairs of CTAs where tiles of 256 x 256 give each of them one in the products of symmetric matrices, the smaller ones
     const int64_t symmetric = tiles_of(plan.side, 256);
     const bool pairs = symmetric * (symmetric + 1) / 2 * batch >= PRODUCT_SMS / 2;
-    const float a = coefficients[0], b = coefficients[1], c = coefficients[2];
-    return pairs ? run<true>(plan, ws, steps, a, b, c, scale, out, out_stride, st) : run<false>(plan, ws, steps, a, b, c, scale, out, out_stride, st);
+    OrthParams q{};
+    q.rows = static_cast<int>(rows), q.cols = static_cast<int>(cols), q.side = static_cast<int>(plan.side), q.batch = static_cast<int>(batch);
+    q.pitch = plan.pitch_a, q.gram = reinterpret_cast<const __half *>(ws + plan.at_gram);
+    q.a = coefficients[0], q.b = coefficients[1], q.c = coefficients[2], q.scale = scale;
+    q.out = static_cast<__nv_bfloat16 *>(out), q.out_stride[0] = out_stride[0], q.out_stride[1] = out_stride[1];
+    if (plan.wide) return pairs ? run<true, true>(plan, ws, q, steps, st) : run<false, true>(plan, ws, q, steps, st);
+    return pairs ? run<true, false>(plan, ws, q, steps, st) : run<false, false>(plan, ws, q, steps, st);
 }
 
 }  // extern "C"

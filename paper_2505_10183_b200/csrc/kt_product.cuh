@@ -12,12 +12,11 @@
 // reduction runs from row to row).  What lies outside of a matrix arrives as zeros.
 //
 // A Task says what the tiles are and what becomes of their sums:
-//   Params, PAIR, HALF (fp16 operands instead of bf16)
-//   int count(p, worker, workers)                  how many tiles a worker (a CTA or a pair) does
-//   Tile tile(p, worker, workers, i)               its i-th
-//   bool a_down / b_down(tile)                     how the operands are read
-//   const CUtensorMap *map_a / map_b(maps, p, tile)
-//   void finish(p, maps, tile, part)
+//   Params, Maps (descriptions of matrices, nothing else), PAIR, HALF (fp16 operands instead of bf16)
+//   Cut(p, worker, workers)      what a worker (a CTA or a pair) does: count() tiles, of which tile(i) is the i-th
+//   bool a_down / b_down(tile)   how the operands are read
+//   const CUtensorMap *map_a / map_b(maps, cut, tile)
+//   void finish(p, maps, cut, tile, part)
 // Waits are bounded (kt_tensor.cuh).  A tile whose sums never came is finished with NaN in their place.
 #pragma once
 
@@ -39,18 +38,6 @@ constexpr int PRODUCT_SMS = 148;                          // of a B200, one CTA 
 struct Tile {
     int m, n, z, k, steps;                                // first row and column, matrix of the batch, first element and stages of the reduction (0: zeros)
     int kind, share;                                      // the Task's own
-};
-
-// One 16-bit or fp32 matrix (or a batch of them) as the copy engine sees it, and the operands of a product.
-struct ProductMaps {
-    CUtensorMap a, a2, b, b2, b3, out, out2;
-};
-
-// Tiles that all workers do in turn: a Task with tiles(p) and tile_at(p, i).
-template <class Task, class Params>
-struct InTurn {
-    __device__ static int count(const Params &p, int worker, int workers) { return (Task::tiles(p) - worker + workers - 1) / workers; }
-    __device__ static Tile tile(const Params &p, int worker, int workers, int i) { return Task::tile_at(p, worker + i * workers); }
 };
 
 struct ProductSmem {
@@ -220,7 +207,7 @@ __device__ __forceinline__ void over_columns(Part &part, F f) {
 
 // ---------------------------------------------------------------------------------- kernel
 template <class Task>
-__global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_constant__ ProductMaps maps, const __grid_constant__ typename Task::Params p, const uint64_t wait_ns) {
+__global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_constant__ typename Task::Maps maps, const __grid_constant__ typename Task::Params p, const uint64_t wait_ns) {
     constexpr bool PAIR = Task::PAIR;
     constexpr int SIDE = PAIR ? 256 : 128;
     constexpr uint32_t COLUMNS = 2 * SIDE;                // of tensor memory: two tiles
@@ -238,8 +225,8 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         fence_async_smem();
     }
-    if (warp == PRODUCT_LOAD && lane < static_cast<int>(sizeof(ProductMaps) / sizeof(CUtensorMap)))       
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.a + lane)) : "memory");
+    if (warp == PRODUCT_LOAD && lane < static_cast<int>(sizeof(maps) / sizeof(CUtensorMap)))
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(reinterpret_cast<const CUtensorMap *>(&maps) + lane)) : "memory");
     if (warp == PRODUCT_MEMORY) sums_alloc<PAIR>(&sm.tmem, COLUMNS);
     tmem_fence_before();
     if constexpr (PAIR) cluster_sync();
@@ -248,15 +235,16 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     const uint32_t tmem = sm.tmem;
     volatile Patience *waits = &sm.waits;
     after_previous();
-    const int tiles = Task::count(p, worker, workers);
+    const typename Task::Cut cut(p, worker, workers);
+    const int tiles = cut.count();
 
     if (warp == PRODUCT_LOAD) {
         if (lane == 0) {
             uint32_t stage = 0, round = 0;
             bool ok = true;
             for (int i = 0; ok && i < tiles; ++i) {
-                const Tile t = Task::tile(p, worker, workers, i);
-                const CUtensorMap *const map_a = Task::map_a(maps, p, t), *const map_b = Task::map_b(maps, p, t);
+                const Tile t = cut.tile(i);
+                const CUtensorMap *const map_a = Task::map_a(maps, cut, t), *const map_b = Task::map_b(maps, cut, t);
                 const int m = t.m + static_cast<int>(rank) * TILE, n = t.n + static_cast<int>(rank) * TILE;
                 for (int s = 0; s < t.steps; ++s) {
                     if (!(ok = bar_wait_one(&sm.free[stage], (round + 1) & 1, waits))) break;
@@ -273,14 +261,14 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
         if (rank == 0 && elected()) {
             uint32_t stage = 0, round = 0;
             bool ok = true;
-            for (int done = 0; ok && done < tiles; ++done) {
-                const Tile t = Task::tile(p, worker, workers, done);
+            for (int i = 0; ok && i < tiles; ++i) {
+                const Tile t = cut.tile(i);
                 const bool a_down = Task::a_down(t), b_down = Task::b_down(t);
                 const uint32_t word = product_word<PAIR, Task::HALF>(a_down, b_down), step_a = a_down ? 2048 >> 4 : 32 >> 4, step_b = b_down ? 2048 >> 4 : 32 >> 4;
                 const uint64_t word_a = a_down ? PRODUCT_DOWN : OPERAND_ALONG, word_b = b_down ? PRODUCT_DOWN : OPERAND_ALONG;
-                if (!(ok = bar_wait_one(&sm.sums_taken[done & 1], (done / 2 + 1) & 1, waits))) break;
+                if (!(ok = bar_wait_one(&sm.sums_taken[i & 1], (i / 2 + 1) & 1, waits))) break;
                 tmem_fence_after();
-                const uint32_t d = tmem + (done & 1) * SIDE;
+                const uint32_t d = tmem + (i & 1) * SIDE;
                 for (int s = 0; s < t.steps; ++s) {
                     if (!(ok = bar_wait_one(&sm.full[stage], round & 1, waits))) break;
                     tmem_fence_after();
@@ -291,7 +279,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
                     multiplied<PAIR>(&sm.free[stage]);
                     if (++stage == STAGES) stage = 0, ++round;
                 }
-                if (ok) multiplied<PAIR>(&sm.sums_full[done & 1]);
+                if (ok) multiplied<PAIR>(&sm.sums_full[i & 1]);
             }
         }
     } else if (warp >= PRODUCT_FINISH) {
@@ -300,20 +288,20 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
         part.half = static_cast<int>(group);
         part.store = sm.store[warp - PRODUCT_FINISH][0], part.turn = 0;
         part.there = true, part.waits = waits;
-        for (int done = 0; done < tiles; ++done) {
-            const Tile t = Task::tile(p, worker, workers, done);
+        for (int i = 0; i < tiles; ++i) {
+            const Tile t = cut.tile(i);
             part.warp_row = t.m + static_cast<int>(rank * TILE + quarter * 32);
             part.row = part.warp_row + lane;
             part.zero = t.steps == 0;
             part.col = t.n + static_cast<int>(group) * (SIDE / 2);
-            part.at = tmem + (done & 1) * SIDE + group * (SIDE / 2) + ((quarter * 32) << 16);
-            part.full = &sm.sums_full[done & 1], part.parity = done / 2 & 1, part.waited = false;
-            Task::finish(p, maps, t, part);
+            part.at = tmem + (i & 1) * SIDE + group * (SIDE / 2) + ((quarter * 32) << 16);
+            part.full = &sm.sums_full[i & 1], part.parity = i / 2 & 1, part.waited = false;
+            Task::finish(p, maps, cut, t, part);
             part.wait();
             if (part.there) {
                 tmem_fence_before();
                 __syncwarp();
-                if (lane == 0) arrive_at(PAIR ? address_in(smem_addr(&sm.sums_taken[done & 1]), 0) : smem_addr(&sm.sums_taken[done & 1]));
+                if (lane == 0) arrive_at(PAIR ? address_in(smem_addr(&sm.sums_taken[i & 1]), 0) : smem_addr(&sm.sums_taken[i & 1]));
             }
         }
         if (lane == 0) stores_done();
@@ -354,7 +342,7 @@ inline int describe_operand(CUtensorMap *map, const char *what, bool half, bool 
 // Starts a product of at most `tiles` tiles: behind a kernel of the same call, or as the call's first, which may not begin
 // before all that is in the stream has ended.
 template <class Task>
-int start_product(ProductMaps maps, const typename Task::Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
+int start_product(typename Task::Maps maps, const typename Task::Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
     static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
     constexpr size_t bytes = sizeof(ProductSmem) + 1024;
     static_assert(bytes <= 227 * 1024, "the ring and the stores have to fit");
@@ -368,7 +356,7 @@ int start_product(ProductMaps maps, const typename Task::Params &p, int64_t tile
     if (tiles == 0) return KT_OK;
     // every description is fetched ahead, so those that the Task does not use are copies of one that it does
     const CUtensorMap none{};
-    CUtensorMap *const first = &maps.a, *const past = first + sizeof(maps) / sizeof(CUtensorMap);
+    CUtensorMap *const first = reinterpret_cast<CUtensorMap *>(&maps), *const past = first + sizeof(maps) / sizeof(CUtensorMap);
     const CUtensorMap *described = std::find_if(first, past, [&](const CUtensorMap &m) { return std::memcmp(&m, &none, sizeof(m)) != 0; });
     if (described == past) return ktd::fail(KT_ERR_INVALID, "a product without operands");
     for (CUtensorMap *m = first; m < past; ++m)

@@ -133,6 +133,14 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
 }
 
 // ------------------------------------------------------------------------------------ products
+// Operands, each read in up to two or three ways, and results.
+struct LogitsMaps {
+    CUtensorMap hidden, packed, weight, p;      // rows as they are, or those that count
+};
+struct BackMaps {
+    CUtensorMap p, p_down, weight, hidden, packed, dweight, sums;
+};
+
 // The order of tiles: bands of up to `band` tiles of rows, in a band column after column, so that the tiles
 // in work at one time share rows and columns that the L2 holds.
 __device__ __forceinline__ void in_bands(int i, int tiles_m, int tiles_n, int band, int *m, int *n) {
@@ -159,28 +167,34 @@ struct LogitsParams {
 };
 
 template <bool PAIR_>
-struct LogitsTask : InTurn<LogitsTask<PAIR_>, LogitsParams> {
+struct LogitsTask {
     using Params = LogitsParams;
+    using Maps = LogitsMaps;
     static constexpr bool PAIR = PAIR_, HALF = false;
     static constexpr int SIDE = PAIR ? 256 : 128;
-    __device__ static int tiles_m(const Params &p) { return (p.counted() + SIDE - 1) / SIDE; }
-    __device__ static int tiles(const Params &p) { return tiles_m(p) * ((p.past - p.from + SIDE - 1) / SIDE); }
+    struct Cut {
+        int counted, n, from, steps, tiles_m, tiles_n, band, worker, workers;
+        __device__ Cut(const Params &p, int worker_, int workers_) : counted(p.counted()), n(p.n), from(p.from), steps(p.steps), band(p.band), worker(worker_), workers(workers_) {
+            tiles_m = (counted + SIDE - 1) / SIDE, tiles_n = (p.past - p.from + SIDE - 1) / SIDE;
+        }
+        __device__ int count() const { return (tiles_m * tiles_n - worker + workers - 1) / workers; }
+        __device__ Tile tile(int i) const {
+            int m, n;
+            in_bands(worker + i * workers, tiles_m, tiles_n, band, &m, &n);
+            return {m * SIDE, from + n * SIDE, 0, 0, steps, 0, 0};
+        }
+    };
     __device__ static bool a_down(const Tile &) { return false; }
     __device__ static bool b_down(const Tile &) { return false; }
-    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &p, const Tile &) { return p.counted() < p.n ? &maps.a2 : &maps.a; }
-    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &, const Tile &) { return &maps.b; }
-    __device__ static Tile tile_at(const Params &p, int i) {
-        int m, n;
-        in_bands(i, tiles_m(p), (p.past - p.from + SIDE - 1) / SIDE, p.band, &m, &n);
-        return {m * SIDE, p.from + n * SIDE, 0, 0, p.steps, 0, 0};
-    }
+    __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &c, const Tile &) { return c.counted < c.n ? &maps.packed : &maps.hidden; }
+    __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &, const Tile &) { return &maps.weight; }
 };
 
 template <bool PAIR_>
 struct LossTask : LogitsTask<PAIR_> {
     using Base = LogitsTask<PAIR_>;
-    __device__ static void finish(const LogitsParams &p, const ProductMaps &, const Tile &t, Part &part) {
-        const bool counts = part.row < p.counted();
+    __device__ static void finish(const LogitsParams &p, const LogitsMaps &, const typename Base::Cut &cut, const Tile &, Part &part) {
+        const bool counts = part.row < cut.counted;
         const int target = counts ? p.row(part.row).target : -1;
         float top = -INFINITY, sum = 0.0f;
         over_columns<Base::SIDE / 2>(part, [&](int v0, auto half, uint32_t (&r)[32]) {
@@ -233,8 +247,8 @@ __device__ __forceinline__ void pack_row(const Part &part, int half, F value) {
 template <bool PAIR_>
 struct GradTask : LogitsTask<PAIR_> {
     using Base = LogitsTask<PAIR_>;
-    __device__ static void finish(const LogitsParams &p, const ProductMaps &maps, const Tile &t, Part &part) {
-        const int count = p.counted();
+    __device__ static void finish(const LogitsParams &p, const LogitsMaps &maps, const typename Base::Cut &cut, const Tile &, Part &part) {
+        const int count = cut.counted;
         if (part.warp_row >= round_to(count, TILE)) return;
         const bool counts = part.row < count;
         const Row row = counts ? p.rows[part.row] : Row{-1, 0.0f, 0.0f, 0.0f};
@@ -258,7 +272,7 @@ struct GradTask : LogitsTask<PAIR_> {
                 for (int e = 0; e < 32; ++e)
                     if (!counts || e >= left) x[e] = 0.0f;
             pack_row(part, half, [&](int e) { return x[e]; });
-            if (half == 1) part.send(&maps.out, v0 - 32 - p.from, part.warp_row, 0);
+            if (half == 1) part.send(&maps.p, v0 - 32 - p.from, part.warp_row, 0);
         });
     }
 };
@@ -270,61 +284,51 @@ struct BackParams {
     const int *count, *index;
     __nv_bfloat16 *to;                          // dh where a tile has all of it; else NULL, and its shares are added up in fp32
     int64_t to_stride;
-    int n, dim, from, past;                     // columns of the vocabulary
+    int n, dim, from, past;                     // from ... past: columns of the vocabulary
     int tiles_n, tiles_w, shares, steps, add;   // tiles across dim and (dW) across the piece; shares of the piece's stages; whether to add
     int hidden;                                 // whether dh is wanted
 };
 template <bool PAIR_>
 struct BackTask {
     using Params = BackParams;
+    using Maps = BackMaps;
     static constexpr bool PAIR = PAIR_, HALF = false;
     static constexpr int SIDE = PAIR ? 256 : 128, BAND = 8;
+    static constexpr int FINISH = 2;            // stages' time that a tile's end takes
     struct Cut {
-        int hidden, each, longer, more, weight, weight_steps;
-        // each: tiles of dh to a worker, one more to the first `longer`; more: tiles of dW that the others do meanwhile
-        __device__ Cut(const Params &p, int workers) {
-            const int count = *p.count;
-            hidden = p.hidden ? (count + SIDE - 1) / SIDE * p.tiles_n * p.shares : 0;
-            weight = p.tiles_w * p.tiles_n, weight_steps = (count + K_STEP - 1) / K_STEP;
-            each = hidden / workers, longer = hidden - each * workers;
-            const int others = workers - longer;
-            more = longer == 0 ? 0 : min((p.steps / p.shares + FINISH) / (weight_steps + FINISH), (weight + others - 1) / others);
+        int counted, n, worker, workers, steps, shares, tiles_m, tiles_n, tiles_w, weight_steps;
+        int mine, early, late;                  // tiles of dh; of dW while others are at a tile of dh more; and after
+        int skip, others, meanwhile;            // workers with a tile of dh more, those without, what the latter do before the rest
+        __device__ Cut(const Params &p, int worker_, int workers_) : counted(*p.count), n(p.n), worker(worker_), workers(workers_), steps(p.steps), shares(p.shares), tiles_n(p.tiles_n), tiles_w(p.tiles_w) {
+            tiles_m = (counted + SIDE - 1) / SIDE, weight_steps = (counted + K_STEP - 1) / K_STEP;
+            const int hidden = p.hidden ? tiles_m * tiles_n * shares : 0, weight = tiles_w * tiles_n, each = hidden / workers;
+            skip = hidden - each * workers, others = workers - skip;
+            const int more = skip == 0 ? 0 : min((steps / shares + FINISH) / (weight_steps + FINISH), (weight + others - 1) / others);
+            meanwhile = min(weight, others * more);
+            mine = each + (worker < skip ? 1 : 0);
+            early = worker < skip ? 0 : (meanwhile - (worker - skip) + others - 1) / others;
+            late = (weight - meanwhile + worker) / workers;
+        }
+        __device__ int count() const { return mine + early + late; }
+        __device__ Tile tile(int i) const {
+            int row, col;
+            if (i < mine) {
+                const int at = worker + i * workers, share = at % shares;
+                const int begin = static_cast<int>(static_cast<int64_t>(steps) * share / shares), end = static_cast<int>(static_cast<int64_t>(steps) * (share + 1) / shares);
+                in_bands(at / shares, tiles_m, tiles_n, BAND, &row, &col);
+                return {row * SIDE, col * SIDE, 0, begin * K_STEP, end - begin, 0, share};
+            }
+            i -= mine;
+            in_bands(i < early ? worker - skip + i * others : meanwhile + (workers - 1 - worker) + (i - early) * workers, tiles_w, tiles_n, BAND, &row, &col);
+            return {row * SIDE, col * SIDE, 0, 0, weight_steps, 1, 0};
         }
     };
-    static constexpr int FINISH = 2;            // stages' time that a tile's end takes
-    __device__ static int count(const Params &p, int worker, int workers) {
-        const Cut c(p, workers);
-        const int others = workers - c.longer, meanwhile = min(c.weight, others * c.more), rest = c.weight - meanwhile;
-        int n = c.each + (worker < c.longer ? 1 : 0);
-        if (worker >= c.longer) n += (meanwhile - (worker - c.longer) + others - 1) / others;
-        return n + (rest - (workers - 1 - worker) + workers - 1) / workers;
-    }
-    __device__ static Tile tile(const Params &p, int worker, int workers, int i) {
-        const Cut c(p, workers);
-        const int mine = c.each + (worker < c.longer ? 1 : 0);
-        if (i < mine) {
-            const int at = worker + i * workers, share = at % p.shares;
-            const int begin = static_cast<int>(static_cast<int64_t>(p.steps) * share / p.shares), end = static_cast<int>(static_cast<int64_t>(p.steps) * (share + 1) / p.shares);
-            int m, n;
-            in_bands(at / p.shares, (*p.count + SIDE - 1) / SIDE, p.tiles_n, BAND, &m, &n);
-            return {m * SIDE, n * SIDE, 0, begin * K_STEP, end - begin, 0, share};
-        }
-        i -= mine;
-        const int others = workers - c.longer, meanwhile = min(c.weight, others * c.more);
-        int at;
-        const int early = worker >= c.longer ? (meanwhile - (worker - c.longer) + others - 1) / others : 0;
-        if (i < early) at = worker - c.longer + i * others;
-        else at = meanwhile + (workers - 1 - worker) + (i - early) * workers;
-        int m, n;
-        in_bands(at, p.tiles_w, p.tiles_n, BAND, &m, &n);
-        return {m * SIDE, n * SIDE, 0, 0, c.weight_steps, 1, 0};
-    }
     __device__ static bool a_down(const Tile &t) { return t.kind == 1; }
     __device__ static bool b_down(const Tile &) { return true; }
-    __device__ static const CUtensorMap *map_a(const ProductMaps &maps, const Params &, const Tile &t) { return t.kind == 0 ? &maps.a : &maps.a2; }
-    __device__ static const CUtensorMap *map_b(const ProductMaps &maps, const Params &p, const Tile &t) { return t.kind == 0 ? &maps.b : *p.count < p.n ? &maps.b3 : &maps.b2; }
-    __device__ static void finish(const Params &p, const ProductMaps &maps, const Tile &t, Part &part) {
-        const int count = *p.count;
+    __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &, const Tile &t) { return t.kind == 0 ? &maps.p : &maps.p_down; }
+    __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &c, const Tile &t) { return t.kind == 0 ? &maps.weight : c.counted < c.n ? &maps.packed : &maps.hidden; }
+    __device__ static void finish(const Params &p, const Maps &maps, const Cut &cut, const Tile &t, Part &part) {
+        const int count = cut.counted;
         const bool weight = t.kind == 1;
         if (weight ? p.from + part.warp_row >= p.past : part.warp_row >= count) return;
         __nv_bfloat16 *const row = !weight && p.to != nullptr && part.row < count ? p.to + p.index[part.row] * p.to_stride : nullptr;
@@ -333,13 +337,13 @@ struct BackTask {
                 if (c0 - half * 32 >= p.dim) return;
                 if (half == 0) part.store_next();
                 pack_row(part, half, [&](int e) { return __uint_as_float(r[e]); });
-                if (half == 1) part.send(&maps.out, c0 - 32, p.from + part.warp_row, 0);
+                if (half == 1) part.send(&maps.dweight, c0 - 32, p.from + part.warp_row, 0);
             } else if (p.to == nullptr) {
                 if (c0 >= p.dim) return;
                 part.store_next();
 #pragma unroll
                 for (int u = 0; u < 8; ++u) *part.piece(u) = make_uint4(r[u * 4], r[u * 4 + 1], r[u * 4 + 2], r[u * 4 + 3]);
-                part.send(&maps.out2, c0, part.warp_row, t.share, p.add != 0);
+                part.send(&maps.sums, c0, part.warp_row, t.share, p.add != 0);
             } else if (row != nullptr) {
 #pragma unroll
                 for (int e = 0; e < 32; e += 8)
@@ -521,7 +525,7 @@ int describe_rows(CUtensorMap *own, CUtensorMap *packed, const Plan &plan, const
 }
 
 template <template <bool> class Task, typename Params>
-int start_either(bool pairs, const ProductMaps &maps, const Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
+int start_either(bool pairs, const typename Task<false>::Maps &maps, const Params &p, int64_t tiles, cudaStream_t st, bool behind = true) {
     return pairs ? start_product<Task<true>>(maps, p, tiles, st, behind) : start_product<Task<false>>(maps, p, tiles, st, behind);
 }
 
@@ -552,9 +556,9 @@ int kt_xent_forward(const void *hidden, int64_t hidden_stride, const void *weigh
     if (int rc = check_workspace(workspace, workspace_bytes, plan.bytes + 1024)) return rc;
     char *const ws = reinterpret_cast<char *>(up(reinterpret_cast<intptr_t>(workspace), 1024));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    ProductMaps maps{};
-    if (int rc = describe_rows(&maps.a, &maps.a2, plan, hidden, hidden_stride, ws, false)) return rc;
-    if (int rc = describe_operand(&maps.b, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
+    LogitsMaps maps{};
+    if (int rc = describe_rows(&maps.hidden, &maps.packed, plan, hidden, hidden_stride, ws, false)) return rc;
+    if (int rc = describe_operand(&maps.weight, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
     LogitsParams p{};
     p.parts = reinterpret_cast<float2 *>(ws + plan.at_parts), p.at_target = reinterpret_cast<float *>(ws + plan.at_target);
     const int side = plan.pairs_logits ? 256 : 128;
@@ -600,19 +604,20 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     const bool direct = plan.pieces == 1 && plan.shares == 1;
     const int64_t p_rows = up(rows, TILE), pitch = plan.piece * 2;
 
-    ProductMaps logits{}, back{};
-    if (int rc = describe_rows(&logits.a, &logits.a2, plan, hidden, hidden_stride, ws, false)) return rc;
-    if (int rc = describe_operand(&logits.b, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
-    if (int rc = describe_matrix(&logits.out, "the workspace", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0, 64, 32)) return rc;
+    LogitsMaps logits{};
+    BackMaps back{};
+    if (int rc = describe_rows(&logits.hidden, &logits.packed, plan, hidden, hidden_stride, ws, false)) return rc;
+    if (int rc = describe_operand(&logits.weight, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
+    if (int rc = describe_matrix(&logits.p, "the workspace", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0, 64, 32)) return rc;
     if (dhidden != nullptr) {
-        if (int rc = describe_operand(&back.a, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
+        if (int rc = describe_operand(&back.p, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
         if (!direct)
-            if (int rc = describe_matrix(&back.out2, "the workspace", CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, sums, dim, rows, plan.shares, dim * 4, rows * dim * 4, 32, 32)) return rc;
+            if (int rc = describe_matrix(&back.sums, "the workspace", CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, sums, dim, rows, plan.shares, dim * 4, rows * dim * 4, 32, 32)) return rc;
     }
     if (dweight != nullptr) {
-        if (int rc = describe_operand(&back.a2, "the workspace", false, true, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
-        if (int rc = describe_rows(&back.b2, &back.b3, plan, hidden, hidden_stride, ws, true)) return rc;
-        if (int rc = describe_matrix(&back.out, "dweight", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dweight, dim, vocab, 1, dweight_stride * 2, 0, 64, 32)) return rc;
+        if (int rc = describe_operand(&back.p_down, "the workspace", false, true, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
+        if (int rc = describe_rows(&back.hidden, &back.packed, plan, hidden, hidden_stride, ws, true)) return rc;
+        if (int rc = describe_matrix(&back.dweight, "dweight", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dweight, dim, vocab, 1, dweight_stride * 2, 0, 64, 32)) return rc;
     }
 
     RowsParams q{};
@@ -628,7 +633,7 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
         const int side = plan.pairs_logits ? 256 : 128, back_side = plan.pairs_back ? 256 : 128;
         if (int rc = start_either<GradTask>(plan.pairs_logits, logits, p, tiles_of(rows, side) * tiles_of(columns, side), st)) return rc;
         if (dhidden != nullptr)       // the weights' rows from the piece's first on
-            if (int rc = describe_operand(&back.b, "weight", false, true, static_cast<const __nv_bfloat16 *>(weight) + from * weight_stride, dim, columns, 1, weight_stride * 2, 0)) return rc;
+            if (int rc = describe_operand(&back.weight, "weight", false, true, static_cast<const __nv_bfloat16 *>(weight) + from * weight_stride, dim, columns, 1, weight_stride * 2, 0)) return rc;
         BackParams b{};
         b.count = q.count, b.index = q.index, b.to = direct ? q.dhidden : nullptr, b.to_stride = dhidden_stride, b.n = q.n, b.dim = q.dim, b.from = p.from, b.past = p.past;
         b.tiles_n = static_cast<int>(tiles_of(dim, back_side)), b.tiles_w = dweight != nullptr ? static_cast<int>(tiles_of(columns, back_side)) : 0;
