@@ -250,6 +250,7 @@ struct Plan {
 // The largest singular value that each step can meet, from one on (|G|_F bounds it), tells whether fp16 holds all
 // that is kept between products.
 int check_polynomial(int steps, float a, float b, float c) {
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return fail(KT_ERR_INVALID, "the coefficients must be finite");
     double most = 1.0;
     for (int i = 0; i < steps; ++i) {
         double next = 0.0, factor = 0.0;
