@@ -80,11 +80,15 @@ constexpr int LIST_THREADS = 512, LIST_WARPS = 16, REMEMBERED = 96, MOST_ROWS = 
 // other in a table, are spread.  Every CTA goes over all ids: those with a smaller remainder say where its tokens
 // begin in the list, so no CTA waits for another (64 thousand ids: some 5 us).  Counts are kept by row and warp;
 // a warp has the ids of a run of the batch, which keeps the order.
-__global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p) {
-    extern __shared__ int counts[];             // [LIST_WARPS][most]
-    __shared__ int remembered[LIST_WARPS][REMEMBERED], sums[LIST_WARPS];
+struct ListSmem {
+    int2 remembered[LIST_WARPS][REMEMBERED];    // token and id
+    int sums[LIST_WARPS];
+};
+// This CTA's tokens, each handed to put(place, token, id), the places of a row one after the other in the order of the batch; a
+// row's first place and tokens to row_is(row of the CTA, place, tokens).  counts: [LIST_WARPS][most].  Returns the place past the last.
+template <typename RowIs, typename Put>
+__device__ __forceinline__ int make_list(const ListParams &p, int *counts, ListSmem &sm, bool whole_list, RowIs row_is, Put put) {
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, mine = blockIdx.x, owners = p.owners;
-    let_next_begin();
     for (int i = tid; i < LIST_WARPS * p.most; i += LIST_THREADS) counts[i] = 0;
     __syncthreads();
     int *const of_warp = counts + warp * p.most;
@@ -99,29 +103,38 @@ __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p)
         return r == static_cast<unsigned>(mine) ? static_cast<int>(q) : -1;
     };
     int before = 0, found = 0;
+    int64_t next[4];                            // the ids of the turn to come are on their way during this one
+    auto ask = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) next[u] = i + u * 32 + lane < end ? p.ids[i + u * 32 + lane] : -1;
+    };
+    ask(begin);
     for (int i = begin; i < end; i += 128) {
         int64_t id[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) id[u] = i + u * 32 + lane < end ? p.ids[i + u * 32 + lane] : -1;
+        for (int u = 0; u < 4; ++u) id[u] = next[u];
+        ask(i + 128);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             bool smaller;
             const int q = look(id[u], smaller);
             before += smaller;
             const unsigned mask = __ballot_sync(0xFFFFFFFFu, q >= 0);
+            if (mask == 0) continue;            // four times of five, with 148 CTAs
             if (q >= 0) {
                 atomicAdd(&of_warp[q], 1);
                 const int at = found + __popc(mask & ((1u << lane) - 1));
-                if (at < REMEMBERED) remembered[warp][at] = i + u * 32 + lane;
+                if (at < REMEMBERED) sm.remembered[warp][at] = make_int2(i + u * 32 + lane, static_cast<int>(id[u]));
             }
             found += __popc(mask);
         }
     }
     before = __reduce_add_sync(0xFFFFFFFFu, before);
-    if (lane == 0) sums[warp] = before;
+    if (lane == 0) sm.sums[warp] = before;
     __syncthreads();
     int base = 0;
-    for (int w = 0; w < LIST_WARPS; ++w) base += sums[w];
+    if (whole_list)
+        for (int w = 0; w < LIST_WARPS; ++w) base += sm.sums[w];
     __syncthreads();
     // where the tokens of each row and warp begin
     for (int q0 = 0; q0 < p.most; q0 += LIST_THREADS) {
@@ -135,17 +148,16 @@ __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p)
             const int x = __shfl_up_sync(0xFFFFFFFFu, up, far);
             if (lane >= far) up += x;
         }
-        if (lane == 31) sums[warp] = up;
+        if (lane == 31) sm.sums[warp] = up;
         __syncthreads();
         int at = base + up - total, all = 0;
         for (int w = 0; w < LIST_WARPS; ++w) {
-            if (w < warp) at += sums[w];
-            all += sums[w];
+            if (w < warp) at += sm.sums[w];
+            all += sm.sums[w];
         }
         base += all;
         if (q < p.most) {
-            const int64_t v = static_cast<int64_t>(q) * owners + mine;
-            if (v < p.vocab) p.past[v] = total > 0 ? at + total : 0;
+            row_is(q, at, total);
             for (int w = 0; w < LIST_WARPS; ++w) {
                 const int here = counts[w * p.most + q];
                 counts[w * p.most + q] = at;
@@ -154,25 +166,38 @@ __global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p)
         }
         __syncthreads();
     }
-    if (mine == owners - 1 && tid == 0) *p.count = base;
     // the tokens to their places, 32 at a time in order: those that were remembered, or the whole run again
     const bool all_remembered = found <= REMEMBERED;
     const int from = all_remembered ? 0 : begin, past = all_remembered ? found : end;
     for (int i = from; i < past; i += 32) {
-        const int token = i + lane < past ? (all_remembered ? remembered[warp][i + lane] : i + lane) : -1;
+        const bool there = i + lane < past;
+        const int2 known = there && all_remembered ? sm.remembered[warp][i + lane] : make_int2(i + lane, -1);
+        const int token = known.x;
+        const int64_t id = !there || all_remembered ? known.y : p.ids[token];
         bool smaller;
-        const int64_t id = token >= 0 ? p.ids[token] : -1;
         const int q = look(id, smaller);
         const unsigned same = __match_any_sync(0xFFFFFFFFu, q);
         const int rank = __popc(same & ((1u << lane) - 1));
-        if (q >= 0) {
-            const int at = of_warp[q] + rank;
-            p.token[at] = token, p.row[at] = static_cast<int>(id);
-        }
+        if (q >= 0) put(of_warp[q] + rank, token, static_cast<int>(id));
         __syncwarp();
         if (q >= 0 && rank == 0) of_warp[q] += __popc(same);
         __syncwarp();
     }
+    return base;
+}
+
+__global__ void __launch_bounds__(LIST_THREADS) k_embed_list(const ListParams p) {
+    extern __shared__ int counts[];
+    __shared__ ListSmem sm;
+    let_next_begin();
+    const int past = make_list(
+        p, counts, sm, true,
+        [&](int q, int at, int total) {
+            const int64_t v = static_cast<int64_t>(q) * p.owners + blockIdx.x;
+            if (v < p.vocab) p.past[v] = total > 0 ? at + total : 0;
+        },
+        [&](int at, int token, int id) { p.token[at] = token, p.row[at] = id; });
+    if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *p.count = past;
 }
 
 // ------------------------------------------------------------------------------------ the sums
@@ -349,6 +374,87 @@ __global__ void __launch_bounds__(256) k_embed_join(const SumParams p) {
         }
 }
 
+// Few tokens: all in one launch, since three of them take longer than their work.  A CTA makes the list of its own tokens in
+// shared memory and then its own rows: a group of warps that spans a row's columns takes a row at a time, and rows of more
+// than ALONE tokens are shared by all groups, whose sums are added in order.  (999 tokens, 500 columns, fp32, a table of
+// 8001 rows: 16.4 us in three launches, 12.3 so.)
+constexpr int DIRECT_TOKENS = 2048, ALONE = 8;
+constexpr int64_t DIRECT_ELEMENTS = INT64_C(1) << 20;      // a row that most tokens share is read by one CTA
+
+template <typename D, typename T, bool WHOLE>
+__global__ void __launch_bounds__(LIST_THREADS) k_embed_direct(const ListParams l, const SumParams p) {
+    extern __shared__ int counts[];             // [LIST_WARPS][most], then the rows' first places and the end
+    __shared__ ListSmem sm;
+    __shared__ int token[DIRECT_TOKENS];
+    __shared__ float4 sums[LIST_THREADS][2];
+    __shared__ int shared_rows[DIRECT_TOKENS / ALONE], shared_count;       // rows of more than ALONE tokens, in any order
+    if (threadIdx.x == 0) shared_count = 0;
+    int *const starts = counts + LIST_WARPS * l.most;
+    const int last = make_list(
+        l, counts, sm, false,
+        [&](int q, int at, int n) {
+            starts[q] = at;
+            if (n > ALONE) shared_rows[atomicAdd(&shared_count, 1)] = q;
+        },
+        [&](int at, int t, int) { token[at] = t; });
+    if (threadIdx.x == 0) starts[l.most] = last;
+    __syncthreads();
+    const int vectors = static_cast<int>((p.cols + 7) / 8), span = min(LIST_THREADS, (vectors + 31) / 32 * 32), groups = LIST_THREADS / span, group = threadIdx.x / span, lane = threadIdx.x - group * span;
+    const D *const dout = static_cast<const D *>(p.dout);
+    const T *const base = static_cast<const T *>(p.base);
+    auto add = [&](int from, int past, int64_t c, float (&sum)[8]) {
+        for (int i0 = from; i0 < past; i0 += ALONE) {
+            Raw<D, WHOLE> v[ALONE];
+#pragma unroll
+            for (int u = 0; u < ALONE; ++u)
+                if (i0 + u < past) v[u].read(dout + token[i0 + u] * p.dout_stride, c, p.cols);
+#pragma unroll
+            for (int u = 0; u < ALONE; ++u)
+                if (i0 + u < past) v[u].add_to(sum);
+        }
+    };
+    auto write = [&](int64_t row, int64_t c, const float (&sum)[8]) {
+        Raw<T, WHOLE> before = {};
+        if (base != nullptr) before.read(base + row * p.base_stride, c, p.cols);
+        float x[8];
+        zeros(x);
+        before.add_to(x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = fmaf(sum[e], p.scale, x[e]);
+        write_eight<T, WHOLE>(static_cast<T *>(p.dweight) + row * p.dweight_stride, c, p.cols, x);
+    };
+    for (int i = 0; i < shared_count; ++i) {
+        const int q = shared_rows[i], from = starts[q], n = starts[q + 1] - from;
+        for (int v0 = 0; v0 < vectors; v0 += span) {
+            const int64_t c = (v0 + lane) * static_cast<int64_t>(8);
+            float sum[8];
+            zeros(sum);
+            if (group < groups && c < p.cols) add(from + n * group / groups, from + n * (group + 1) / groups, c, sum);
+            __syncthreads();
+            sums[threadIdx.x][0] = make_float4(sum[0], sum[1], sum[2], sum[3]), sums[threadIdx.x][1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
+            __syncthreads();
+            if (group > 0 || c >= p.cols) continue;
+            for (int g = 1; g < groups; ++g) {
+                const float4 a = sums[g * span + lane][0], b = sums[g * span + lane][1];
+                sum[0] += a.x, sum[1] += a.y, sum[2] += a.z, sum[3] += a.w, sum[4] += b.x, sum[5] += b.y, sum[6] += b.z, sum[7] += b.w;
+            }
+            write(static_cast<int64_t>(q) * l.owners + blockIdx.x, c, sum);
+        }
+    }
+    if (group >= groups) return;
+    const int rows = min(l.most, (l.vocab - static_cast<int>(blockIdx.x) + l.owners - 1) / l.owners);      // the CTA's
+    for (int q = group; q < rows; q += groups) {
+        const int from = starts[q], n = starts[q + 1] - from;
+        if (n > ALONE || (n == 0 && p.base == p.dweight)) continue;       // (an untouched row of the gradient that is there)
+        for (int v = lane; v < vectors; v += span) {
+            float sum[8];
+            zeros(sum);
+            add(from, from + n, v * static_cast<int64_t>(8), sum);
+            write(static_cast<int64_t>(q) * l.owners + blockIdx.x, v * static_cast<int64_t>(8), sum);
+        }
+    }
+}
+
 // ---------------------------------------------------------------------------------- host side
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -362,8 +468,8 @@ struct Plan {
         threads = std::min<int64_t>(256, up(vectors, 32)), across = (vectors + threads - 1) / threads;
         const int64_t fours = (cols + 3) / 4;
         threads_join = std::min<int64_t>(256, up(fours, 32)), across_join = (fours + threads_join - 1) / threads_join;
-        // six CTAs of 256 threads to an SM or fewer; short pieces leave more rows to be joined
-        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(8, tokens * across / (SMS * 6 * 256 / threads)));
+        // one round of three CTAs of 256 threads to an SM (what its registers hold), but short pieces leave more rows to be joined
+        length = std::min<int64_t>(MAX_LENGTH, std::max<int64_t>(8, (tokens * across + SMS * 3 * 256 / threads - 1) / (SMS * 3 * 256 / threads)));
         pieces = (tokens + length - 1) / length;
         pitch = up(cols, 8);
         int64_t at = 1024 + up(tokens * 4, 1024);      // the list's length and tokens
@@ -406,7 +512,14 @@ int lookup(const LookupParams &p, bool vectors, cudaStream_t st) {
 template <typename D, typename T, bool WHOLE>
 int gradient(const ListParams &l, const SumParams &s, const Plan &plan, cudaStream_t st) {
     const size_t bytes = static_cast<size_t>(LIST_WARPS * plan.most * 4);
-    if (bytes > 40 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB with what is static need no leave
+    if (l.n <= DIRECT_TOKENS && l.n * s.cols <= DIRECT_ELEMENTS) {
+        const size_t more = bytes + static_cast<size_t>(plan.most + 1) * 4;
+        if (more > 8 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_direct<D, T, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (LIST_WARPS + 1) * MOST_ROWS * 4 + 4));      // 38 of the 48 KB that need no leave are static
+        k_embed_direct<D, T, WHOLE><<<static_cast<unsigned>(plan.owners), LIST_THREADS, more, st>>>(l, s);
+        KT_CUDA(cudaGetLastError());
+        return KT_OK;
+    }
+    if (bytes > 32 * 1024) KT_CUDA(cudaFuncSetAttribute(k_embed_list, cudaFuncAttributeMaxDynamicSharedMemorySize, LIST_WARPS * MOST_ROWS * 4));      // 48 KB need no leave, 12 of which are static
     k_embed_list<<<static_cast<unsigned>(plan.owners), LIST_THREADS, bytes, st>>>(l);
     KT_CUDA(cudaGetLastError());
     const int64_t summing = plan.pieces * plan.across, fillers = s.base == s.dweight ? 0 : (s.vocab + s.rows_each - 1) / s.rows_each;

@@ -46,30 +46,50 @@ struct StartParams {
     __half *to;
 };
 
-// Sums of squares in 64 bits: no element is too large or too small for them.
+// A warp takes 1024 columns of a row, four pieces of eight to a lane; this is the i-th such chunk's row and first column.
+struct Chunks {
+    uint32_t per_row, all;
+    __device__ explicit Chunks(const StartParams &p) : per_row(static_cast<uint32_t>((p.cols + 1023) / 1024)), all(static_cast<uint32_t>(p.rows) * per_row) {}       // 2^22 at most
+    __device__ void at(uint32_t i, uint32_t *row, uint32_t *col) const { *row = i / per_row, *col = (i - *row * per_row) * 1024 + threadIdx.x % 32 * 8; }
+};
+
+// Sums of squares, 32 at a time in fp32, those in 64 bits.  Where the 32 leave fp32's range, or almost, they are scaled by the power of
+// two of the largest before: no element is too large or too small.
 template <typename T, bool WHOLE>
 __global__ void __launch_bounds__(256) k_orth_squares(const StartParams p) {
     __shared__ double of_warp[8];
     let_next_begin();
-    const uint32_t cols = static_cast<uint32_t>(p.cols), pieces = (cols + 7) / 8, all = static_cast<uint32_t>(p.rows) * pieces, step = gridDim.x * 256;      // 2^29 pieces at most
+    const Chunks chunks(p);
     const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0];
-    double sum[2] = {0.0, 0.0};
-    for (uint32_t i0 = blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
-        float v[4][8];
+    double all_of = 0.0;
+    for (uint32_t i = blockIdx.x * 8 + threadIdx.x / 32; i < chunks.all; i += gridDim.x * 8) {
+        uint32_t row, col;
+        chunks.at(i, &row, &col);
+        float v[4][8], sums[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint32_t i = i0 + u * step, r = i < all ? i / pieces : 0, c = i < all ? (i - r * pieces) * 8 : cols;      // (past the last column: zeros)
-            read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v[u]);
-        }
+        for (int u = 0; u < 4; ++u) read_eight<T, WHOLE>(x + row * p.stride[1], col + u * 256, p.cols, v[u]);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const double d = v[u][e];
-                sum[e % 2] = fma(d, d, sum[e % 2]);
-            }
+            for (int e = 0; e < 8; ++e) sums[e % 2] = fmaf(v[u][e], v[u][e], sums[e % 2]);
+        const float sum = sums[0] + sums[1];
+        if (sum > 0x1p-80f && sum < 0x1p120f) {
+            all_of += sum;
+            continue;
+        }
+        float top = 0.0f, scaled = 0.0f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[u][e]));
+        const uint32_t power = min(__float_as_uint(top) >> 23, 253u);       // an infinity, or a NaN, comes through all the same
+        const float by = __uint_as_float((254u - power) << 23);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scaled = fmaf(v[u][e] * by, v[u][e] * by, scaled);
+        all_of += scaled * __longlong_as_double((2 * (static_cast<long long>(power) - 127) + 1023) << 52);
     }
-    double all_of = sum[0] + sum[1];
 #pragma unroll
     for (int far = 16; far; far /= 2) all_of += __shfl_xor_sync(0xFFFFFFFFu, all_of, far);
     if (threadIdx.x % 32 == 0) of_warp[threadIdx.x / 32] = all_of;
@@ -86,7 +106,6 @@ __global__ void __launch_bounds__(256) k_orth_start(const StartParams p) {
     __shared__ double of_warp[8];
     let_next_begin();
     after_previous();
-    const uint32_t cols = static_cast<uint32_t>(p.cols), pieces = (cols + 7) / 8, all = static_cast<uint32_t>(p.rows) * pieces, step = gridDim.x * 256;      // 2^29 pieces at most
     double sum = static_cast<int>(threadIdx.x) < p.sum_blocks ? p.sums[blockIdx.y * p.sum_blocks + threadIdx.x] : 0.0;
 #pragma unroll
     for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
@@ -97,25 +116,24 @@ __global__ void __launch_bounds__(256) k_orth_start(const StartParams p) {
     const double by = sum == 0.0 ? 0.0 : isfinite(sum) ? X_UNIT / sqrt(sum) : __longlong_as_double(0x7FF8000000000000ll);
     const bool narrow = by < 1e30 && by > 1e-30;       // fp32 holds the factor
     const float by32 = static_cast<float>(by);
-    const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0];
-    __half *const to = p.to + blockIdx.y * p.rows * p.pitch;
-    for (uint32_t i0 = blockIdx.x * 256 + threadIdx.x; i0 < all; i0 += 4 * step) {
-        float v[4][8];
+    const Chunks chunks(p);
+    const uint32_t i = blockIdx.x * 8 + threadIdx.x / 32;
+    if (i >= chunks.all) return;
+    uint32_t row, col;
+    chunks.at(i, &row, &col);
+    const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0] + row * p.stride[1];
+    __half *const to = p.to + (blockIdx.y * p.rows + row) * p.pitch;
+    float v[4][8];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint32_t i = i0 + u * step, r = i < all ? i / pieces : 0, c = i < all ? (i - r * pieces) * 8 : cols;
-            read_eight<T, WHOLE>(x + r * p.stride[1], c, p.cols, v[u]);
-        }
+    for (int u = 0; u < 4; ++u) read_eight<T, WHOLE>(x, col + u * 256, p.cols, v[u]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const uint32_t i = i0 + u * step, r = i / pieces, c = (i - r * pieces) * 8;
-            if (i >= all) break;
+    for (int u = 0; u < 4; ++u) {
+        if (col + u * 256 >= p.cols) break;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[u][e] = narrow ? v[u][e] * by32 : static_cast<float>(v[u][e] * by);
-            uint4 w;
-            w.x = pack_half(v[u][0], v[u][1]), w.y = pack_half(v[u][2], v[u][3]), w.z = pack_half(v[u][4], v[u][5]), w.w = pack_half(v[u][6], v[u][7]);
-            *reinterpret_cast<uint4 *>(to + r * p.pitch + c) = w;
-        }
+        for (int e = 0; e < 8; ++e) v[u][e] = narrow ? v[u][e] * by32 : static_cast<float>(v[u][e] * by);
+        uint4 w;
+        w.x = pack_half(v[u][0], v[u][1]), w.y = pack_half(v[u][2], v[u][3]), w.z = pack_half(v[u][4], v[u][5]), w.w = pack_half(v[u][6], v[u][7]);
+        *reinterpret_cast<uint4 *>(to + col + u * 256) = w;
     }
 }
 
@@ -175,6 +193,7 @@ struct OrthTask {
     __device__ static bool b_down(const Tile &) { return WIDE ? !SYMMETRIC : KIND == GRAM; }
     __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &, const Tile &) { return &maps.a; }
     __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &, const Tile &) { return &maps.b; }
+    __device__ static int rows_a(const Cut &, const Tile &) { return TILE; }
     __device__ static void finish(const Params &p, const Maps &maps, const Cut &, const Tile &t, Part &part) {
         const bool mirrored = SYMMETRIC && !p.whole && t.n != t.m;
         const int rows = SYMMETRIC ? p.side : p.rows, cols = SYMMETRIC ? p.side : p.cols, lane = threadIdx.x % 32;
@@ -312,10 +331,9 @@ int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
 
 template <typename T>
 int start(StartParams &p, const Plan &plan, bool whole, cudaStream_t st) {
-    // a thread takes four pieces at a time; eight CTAs to an SM over all matrices
-    const int64_t blocks = (plan.rows * ((plan.cols + 7) / 8) + 1023) / 1024, most = (8 * PRODUCT_SMS + plan.batch - 1) / plan.batch, used = blocks < most ? blocks : most;
-    p.sum_blocks = static_cast<int>(used < SUM_BLOCKS ? used : SUM_BLOCKS);
-    const dim3 sums(static_cast<unsigned>(p.sum_blocks), static_cast<unsigned>(plan.batch)), grid(static_cast<unsigned>(used), static_cast<unsigned>(plan.batch));
+    const int64_t blocks = (plan.rows * ((plan.cols + 1023) / 1024) + 7) / 8;       // eight warps' chunks
+    p.sum_blocks = static_cast<int>(blocks < SUM_BLOCKS ? blocks : SUM_BLOCKS);
+    const dim3 sums(static_cast<unsigned>(p.sum_blocks), static_cast<unsigned>(plan.batch)), grid(static_cast<unsigned>(blocks), static_cast<unsigned>(plan.batch));
     whole ? k_orth_squares<T, true><<<sums, 256, 0, st>>>(p) : k_orth_squares<T, false><<<sums, 256, 0, st>>>(p);
     KT_CUDA(cudaGetLastError());
     KT_CUDA(launch_behind(whole ? k_orth_start<T, true> : k_orth_start<T, false>, 1, grid, dim3(256), 0, st, p));
@@ -378,9 +396,11 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     const int per = 16 / size;
     const bool whole = reinterpret_cast<uintptr_t>(x) % 16 == 0 && p.stride[0] % per == 0 && p.stride[1] % per == 0;
     if (int rc = dtype == KT_F32 ? start<float>(p, plan, whole, st) : start<__nv_bfloat16>(p, plan, whole, st)) return rc;
-    // pairs of CTAs where tiles of 256 x 256 give each of them one in the products of symmetric matrices, the smaller ones
+    // Pairs of CTAs where there are tiles of 256 x 256 for two thirds of them in the products of symmetric matrices, the smaller ones.
+    // In us, one CTA to a tile and pairs: 2048 x 2048 (36 tiles) 259 and 273, 4 x 1024 x 1024 (40) 181 and 197, 16 x 512 x 512 (48)
+    // 173 and 161, 12 x 768 x 768 (72) 234 and 228.
     const int64_t symmetric = tiles_of(plan.side, 256);
-    const bool pairs = symmetric * (symmetric + 1) / 2 * batch >= PRODUCT_SMS / 2;
+    const bool pairs = symmetric * (symmetric + 1) / 2 * batch >= 45;
     OrthParams q{};
     q.rows = static_cast<int>(rows), q.cols = static_cast<int>(cols), q.side = static_cast<int>(plan.side), q.batch = static_cast<int>(batch);
     q.pitch = plan.pitch_a, q.gram = reinterpret_cast<const __half *>(ws + plan.at_gram);

@@ -16,6 +16,7 @@
 //   Cut(p, worker, workers)      what a worker (a CTA or a pair) does: count() tiles, of which tile(i) is the i-th
 //   bool a_down / b_down(tile)   how the operands are read
 //   const CUtensorMap *map_a / map_b(maps, cut, tile)
+//   int rows_a(cut, tile)        rows that a box of A read along its rows brings: fewer than 128 where the others' results do not matter
 //   void finish(p, maps, cut, tile, part)
 // Waits are bounded (kt_tensor.cuh).  A tile whose sums never came is finished with NaN in their place.
 #pragma once
@@ -31,7 +32,7 @@ namespace {
 
 constexpr int K_STEP = 64;                                // elements of the reduction to a stage: 128 bytes
 constexpr int STAGES = 5;
-constexpr uint32_t OPERAND_BYTES = TILE * K_STEP * 2, STAGE_BYTES = 2 * OPERAND_BYTES, STORE_BYTES = 32 * 128;
+constexpr uint32_t OPERAND_BYTES = TILE * K_STEP * 2, STORE_BYTES = 32 * 128;
 constexpr int PRODUCT_THREADS = 384, PRODUCT_LOAD = 0, PRODUCT_ISSUE = 1, PRODUCT_MEMORY = 2, PRODUCT_FINISH = 4;      // warps
 constexpr int PRODUCT_SMS = 148;                          // of a B200, one CTA to each
 
@@ -246,10 +247,11 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
                 const Tile t = cut.tile(i);
                 const CUtensorMap *const map_a = Task::map_a(maps, cut, t), *const map_b = Task::map_b(maps, cut, t);
                 const int m = t.m + static_cast<int>(rank) * TILE, n = t.n + static_cast<int>(rank) * TILE;
+                const uint32_t bytes = (Task::a_down(t) ? OPERAND_BYTES : Task::rows_a(cut, t) * (K_STEP * 2)) + OPERAND_BYTES;
                 for (int s = 0; s < t.steps; ++s) {
                     if (!(ok = bar_wait_one(&sm.free[stage], (round + 1) & 1, waits))) break;
                     const uint32_t bar = PAIR ? address_in(smem_addr(&sm.full[stage]), 0) : smem_addr(&sm.full[stage]);
-                    if (rank == 0) bar_expect(&sm.full[stage], PAIR ? 2 * STAGE_BYTES : STAGE_BYTES);
+                    if (rank == 0) bar_expect(&sm.full[stage], PAIR ? 2 * bytes : bytes);
                     const int k = t.k + s * K_STEP;
                     load_operand<PAIR>(smem_addr(sm.a[stage]), map_a, bar, Task::a_down(t), m, k, t.z);
                     load_operand<PAIR>(smem_addr(sm.b[stage]), map_b, bar, Task::b_down(t), n, k, t.z);
@@ -334,9 +336,9 @@ inline int describe_matrix(CUtensorMap *map, const char *what, CUtensorMapDataTy
     if (rc != CUDA_SUCCESS) return ktd::fail(KT_ERR_CUDA, "describing %s to the copy engine failed with driver status %d", what, static_cast<int>(rc));
     return KT_OK;
 }
-// An operand of 16-bit elements, read along its rows or down them.
-inline int describe_operand(CUtensorMap *map, const char *what, bool half, bool down, const void *at, int64_t cols, int64_t rows, int64_t matrices, int64_t pitch, int64_t matrix_pitch) {
-    return describe_matrix(map, what, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, at, cols, rows, matrices, pitch, matrix_pitch, 64, down ? K_STEP : TILE);
+// An operand of 16-bit elements, read along its rows (box_rows at a time) or down them.
+inline int describe_operand(CUtensorMap *map, const char *what, bool half, bool down, const void *at, int64_t cols, int64_t rows, int64_t matrices, int64_t pitch, int64_t matrix_pitch, int box_rows = TILE) {
+    return describe_matrix(map, what, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, at, cols, rows, matrices, pitch, matrix_pitch, 64, down ? K_STEP : box_rows);
 }
 
 // Starts a product of at most `tiles` tiles: behind a kernel of the same call, or as the call's first, which may not begin

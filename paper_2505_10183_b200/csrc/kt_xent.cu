@@ -56,39 +56,32 @@ struct RowsParams {
     float scale;
 };
 
-__device__ __forceinline__ int block_sum(int x, int *shared) {
-    x = __reduce_add_sync(0xFFFFFFFFu, x);
-    __syncthreads();
-    if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = x;
-    __syncthreads();
-    int sum = 0;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) sum += shared[w];
-    return sum;
-}
-
 // Every CTA goes over all targets to find out where its own rows begin: a few microseconds for 64 thousand of them
 // from the L2, and no CTA waits for another.
 __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
-    __shared__ int sums[8], place[256];
+    __shared__ int sums[8], sums_before[8], place[256];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     let_next_begin();
     const int begin = min(p.n, static_cast<int>(blockIdx.x) * p.each), end = min(p.n, begin + p.each);
     int before = 0, all = 0;
-#pragma unroll 8
+#pragma unroll 16
     for (int i = tid; i < p.n; i += 256) {
         const int counts = p.targets[i] >= 0;
         all += counts;
         if (i < begin) before += counts;
     }
-    all = block_sum(all, sums);
-    before = block_sum(before, sums);
+    all = __reduce_add_sync(0xFFFFFFFFu, all), before = __reduce_add_sync(0xFFFFFFFFu, before);
+    if (lane == 0) sums[warp] = all, sums_before[warp] = before;
+    __syncthreads();
+    all = before = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) all += sums[w], before += sums_before[w];
     const bool copy = all < p.n;
     const int pieces = p.dim / 8;
     if (blockIdx.x == 0) {
         if (tid == 0) *p.count = all;
         if (copy)       // a stage of the reduction over rows may read past the last: zeros there
-            for (int i = all * pieces + tid; i < round_to(all, K_STEP) * pieces; i += 256) reinterpret_cast<uint4 *>(p.packed)[i] = make_uint4(0, 0, 0, 0);
+            for (int64_t i = static_cast<int64_t>(all) * pieces + tid; i < static_cast<int64_t>(round_to(all, K_STEP)) * pieces; i += 256) reinterpret_cast<uint4 *>(p.packed)[i] = make_uint4(0, 0, 0, 0);
     }
     for (int base = begin; base < end; base += 256) {
         const int i = base + tid;
@@ -141,6 +134,10 @@ struct BackMaps {
     CUtensorMap p, p_down, weight, hidden, packed, dweight, sums;
 };
 
+// Rows that a box of hidden rows, or of P, brings: no more than there are.  (The rest of a tile holds what was there before;
+// its results are nobody's.)
+__host__ __device__ inline int rows_of_box(int64_t n) { return n < TILE ? static_cast<int>((n + 7) / 8 * 8) : TILE; }
+
 // The order of tiles: bands of up to `band` tiles of rows, in a band column after column, so that the tiles
 // in work at one time share rows and columns that the L2 holds.
 __device__ __forceinline__ void in_bands(int i, int tiles_m, int tiles_n, int band, int *m, int *n) {
@@ -188,6 +185,7 @@ struct LogitsTask {
     __device__ static bool b_down(const Tile &) { return false; }
     __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &c, const Tile &) { return c.counted < c.n ? &maps.packed : &maps.hidden; }
     __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &, const Tile &) { return &maps.weight; }
+    __device__ static int rows_a(const Cut &c, const Tile &) { return rows_of_box(c.n); }
 };
 
 template <bool PAIR_>
@@ -314,7 +312,7 @@ struct BackTask {
             int row, col;
             if (i < mine) {
                 const int at = worker + i * workers, share = at % shares;
-                const int begin = static_cast<int>(static_cast<int64_t>(steps) * share / shares), end = static_cast<int>(static_cast<int64_t>(steps) * (share + 1) / shares);
+                const int begin = steps * share / shares, end = steps * (share + 1) / shares;      // (32768 stages at most, 16 to a share)
                 in_bands(at / shares, tiles_m, tiles_n, BAND, &row, &col);
                 return {row * SIDE, col * SIDE, 0, begin * K_STEP, end - begin, 0, share};
             }
@@ -326,6 +324,7 @@ struct BackTask {
     __device__ static bool a_down(const Tile &t) { return t.kind == 1; }
     __device__ static bool b_down(const Tile &) { return true; }
     __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &, const Tile &t) { return t.kind == 0 ? &maps.p : &maps.p_down; }
+    __device__ static int rows_a(const Cut &c, const Tile &) { return rows_of_box(c.n); }
     __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &c, const Tile &t) { return t.kind == 0 ? &maps.weight : c.counted < c.n ? &maps.packed : &maps.hidden; }
     __device__ static void finish(const Params &p, const Maps &maps, const Cut &cut, const Tile &t, Part &part) {
         const int count = cut.counted;
@@ -431,9 +430,17 @@ __global__ void __launch_bounds__(256) k_xent_dhidden(const int *count, const in
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 int64_t tiles_of(int64_t x, int side) { return (x + side - 1) / side; }
 
-// Whether a product of m x n results is worked on by pairs of CTAs: where tiles of 256 x 256 give every pair
-// at least one, and not where half of a tile would be empty rows.
-bool by_pairs(int64_t m, int64_t n) { return m > TILE && tiles_of(m, 256) * tiles_of(n, 256) >= PRODUCT_SMS / 2; }
+// Whether the logits' tiles are worked on by pairs of CTAs: where there are almost as many tiles of 256 x 256 as pairs, and not
+// where half of a tile would be empty rows.  In us, one CTA to a tile and pairs:
+//   forward, 200 x 512 on 8001 (32 tiles)       12.4  14.4        512 x 1024 on 8001 (64)     20.5  18.6
+//   forward, 512 x 512 on 8001 (64)             16.5  16.5        200 x 512 on 32000 (125)    23.8  20.5
+bool by_pairs(int64_t m, int64_t n) { return m > TILE && tiles_of(m, 256) * tiles_of(n, 256) >= 60; }
+
+// The same for the products from P, which differ in length: by the stages of the reductions that a pair would have.
+//   backward, 200 x 768 on 8001 (10 stages)     30.8  33.5        200 x 512 on 32000 (27)     53.3  59.5
+//   backward, 512 x 512 on 8001 (14)            34.9  35.9        512 x 1024 on 8001 (27)     48.0  43.3
+//   backward, 200 x 2048 on 8001 (27)           51.3  49.2        512 x 1024 on 32000 (110)    131   103
+constexpr int64_t PAIR_STAGES = 24;
 
 constexpr int64_t PIECE_BYTES = INT64_C(512) << 20;        // of P, at most
 
@@ -460,11 +467,11 @@ struct Plan {
         pieces = (vocab + piece - 1) / piece;
         pairs_logits = by_pairs(n, piece);
         const int64_t steps = (piece + K_STEP - 1) / K_STEP, over_rows = (n + K_STEP - 1) / K_STEP;
-        pairs_back = tiles_of(dim, 256) * (tiles_of(n, 256) + tiles_of(piece, 256)) >= PRODUCT_SMS / 2;
-        // dh: shares of the piece such that a tile takes no longer than all work on all workers, but 16 stages at least
-        const int side = pairs_back ? 256 : 128;
-        const int64_t workers = pairs_back ? PRODUCT_SMS / 2 : PRODUCT_SMS, hidden = tiles_of(n, side) * tiles_of(dim, side), weight = tiles_of(piece, side) * tiles_of(dim, side);
-        const int64_t mean = (hidden * steps + weight * over_rows) / workers, longest = mean < 16 ? 16 : mean;
+        auto stages = [&](int side, int64_t workers) { return tiles_of(dim, side) * (tiles_of(n, side) * steps + tiles_of(piece, side) * over_rows) / workers; };
+        pairs_back = stages(256, PRODUCT_SMS / 2) >= PAIR_STAGES;
+        // dh: shares of the piece such that a tile takes no longer than all work on all workers, but 16 stages at least (with 8: 38.4 us
+        // instead of 33.5 for 200 x 768 on 8001, with 32 34.9)
+        const int64_t mean = pairs_back ? stages(256, PRODUCT_SMS / 2) : stages(128, PRODUCT_SMS), longest = mean < 16 ? 16 : mean;
         shares = (steps + longest - 1) / longest;
         at_parts = take(backward ? 0 : 8 * n * 2 * tiles_of(vocab, pairs_logits ? 256 : 128)), at_target = take(backward ? 0 : 4 * n);
         at_p = take(backward ? 2 * up(n, TILE) * piece : 0);
@@ -520,8 +527,8 @@ int band_of(int64_t dim, int side) {
 
 // The counted rows: hidden itself where all count, and where they have been copied to.
 int describe_rows(CUtensorMap *own, CUtensorMap *packed, const Plan &plan, const void *hidden, int64_t hidden_stride, const char *ws, bool down) {
-    if (int rc = describe_operand(own, "hidden", false, down, hidden, plan.dim, plan.n, 1, hidden_stride * 2, 0)) return rc;
-    return describe_operand(packed, "the workspace", false, down, ws + plan.at_packed, plan.dim, up(plan.n, K_STEP), 1, plan.dim * 2, 0);
+    if (int rc = describe_operand(own, "hidden", false, down, hidden, plan.dim, plan.n, 1, hidden_stride * 2, 0, rows_of_box(plan.n))) return rc;
+    return describe_operand(packed, "the workspace", false, down, ws + plan.at_packed, plan.dim, up(plan.n, K_STEP), 1, plan.dim * 2, 0, rows_of_box(plan.n));
 }
 
 template <template <bool> class Task, typename Params>
@@ -610,7 +617,7 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     if (int rc = describe_operand(&logits.weight, "weight", false, false, weight, dim, vocab, 1, weight_stride * 2, 0)) return rc;
     if (int rc = describe_matrix(&logits.p, "the workspace", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0, 64, 32)) return rc;
     if (dhidden != nullptr) {
-        if (int rc = describe_operand(&back.p, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
+        if (int rc = describe_operand(&back.p, "the workspace", false, false, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0, rows_of_box(rows))) return rc;
         if (!direct)
             if (int rc = describe_matrix(&back.sums, "the workspace", CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, sums, dim, rows, plan.shares, dim * 4, rows * dim * 4, 32, 32)) return rc;
     }

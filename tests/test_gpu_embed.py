@@ -88,7 +88,7 @@ def gradient(dout, ids, vocab, scale, base):
 
 @pytest.mark.parametrize("tokens,cols,vocab,kind", [(1, 1, 1, "plain"), (1, 9, 5, "plain"), (31, 16, 3, "plain"), (33, 500, 40, "unknown"), (64, 128, 1000, "one"), (999, 130, 300, "skewed"),
                                                     (5000, 72, 149, "one"), (4097, 1032, 149, "unknown"), (3000, 2056, 8001, "skewed"), (20000, 64, 50257, "skewed"), (3000, 24, 310000, "skewed"),
-                                                    (40000, 16, 7, "plain")])
+                                                    (40000, 16, 7, "plain"), (300, 16, 30000, "skewed"), (2048, 511, 90000, "skewed"), (200, 4096, 5, "unknown"), (2049, 8, 20, "one")])
 @pytest.mark.parametrize("dtype,wtype,layout,base", [(F32, F32, "plain", None), (BF16, BF16, "strided", "other"), (BF16, F32, "odd", "itself"), (F32, BF16, "plain", "itself")])
 def test_gradient(kt, tokens, cols, vocab, kind, dtype, wtype, layout, base):
     gen = torch.Generator().manual_seed(tokens * 3 + cols)
@@ -158,3 +158,25 @@ def test_captured_beside_other_streams(kt):
         graph.replay()
         want, slack = gradient(dout, ids, 300, 1.0, None)
         assert ((dw.double() - want).abs() <= U32 * (want.abs() + slack) + slack).all()
+
+
+def test_a_table_of_the_largest_size(kt):
+    """Offsets past 2^31 elements, and more CTAs than SMs for the list."""
+    tokens, cols, vocab = 600, 144, 2 ** 24
+    gen = torch.Generator().manual_seed(11)
+    ids = torch.randint(vocab - 1000, vocab, (tokens,), generator=gen).cuda()
+    ids[:7] = torch.tensor([0, 1, vocab - 1, vocab - 1, -1, vocab, 5])
+    dout = torch.randn(tokens, cols, generator=gen).to(BF16).cuda()
+    dw = torch.full((vocab, cols), 3.0, dtype=BF16, device="cuda")
+    work = torch.empty(kt.kt_embed_workspace(tokens, cols, vocab), dtype=torch.uint8, device="cuda")
+    kt.kt_embed_backward(dout, ids, dw, work)
+    known = (ids >= 0) & (ids < vocab)
+    rows, at = torch.unique(ids[known], return_inverse=True)
+    want = torch.zeros(len(rows), cols, dtype=torch.float64, device="cuda").index_add_(0, at, dout[known].double())
+    assert ((dw[rows].double() - want).abs() <= U16 * want.abs() + 16 * U32 * dout.double().abs().max()).all()
+    dw[rows] = 0
+    assert not dw.any()
+    dw[rows] = 1
+    out = torch.empty(tokens, cols, dtype=BF16, device="cuda")
+    kt.kt_embed_forward(ids, dw, out)
+    assert (out[known] == 1).all()

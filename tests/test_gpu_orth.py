@@ -94,6 +94,12 @@ def test_strides(kt):
     assert torch.equal(turned, want)
 
 
+def test_a_broadcast_batch(kt):
+    x = normal(70, 100)
+    got = update(kt, x.expand(3, 70, 100))
+    assert torch.equal(got[0], update(kt, x)) and torch.equal(got[1], got[0]) and torch.equal(got[2], got[0])
+
+
 def test_a_matrix_of_low_rank(kt):
     """In the directions that x does not have, a rounding of X is raised by a = 3.4445 in every step that follows, where the
     header's tolerance is for directions that x has.  X_0 has the norm 1 and the later ones at most 1.2 sqrt(2) = 1.7, of which

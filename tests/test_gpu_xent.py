@@ -255,6 +255,24 @@ def test_the_same_bits_again_and_captured(kt):
         assert all(torch.equal(a, b) for a, b in zip(want, (loss, lse, dh, dw)))
 
 
+def test_two_calls_at_once(kt):
+    """On streams of their own, with workspaces of their own."""
+    problems, streams, got = [Problem(700, 64, 9000, 0.1, seed=i) for i in range(2)], [torch.cuda.Stream() for _ in range(2)], []
+    want = []
+    for p in problems:
+        loss, lse = p.forward(kt)
+        want.append([loss, lse, *p.backward(kt, lse)])
+    buffers = [([torch.empty_like(t) for t in w], p.work(kt, False), p.work(kt, True)) for w, p in zip(want, problems)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for p, s, (outs, work, back) in zip(problems, streams, buffers):
+            kt.kt_xent_forward(p.hidden, p.weight, p.targets, outs[0], outs[1], work, stream=s)
+            kt.kt_xent_backward(p.dloss, p.hidden, p.weight, p.targets, outs[1], outs[2], outs[3], back, stream=s)
+    torch.cuda.synchronize()
+    for w, (outs, _, _) in zip(want, buffers):
+        assert all(torch.equal(a, b) for a, b in zip(w, outs))
+
+
 def test_on_another_stream(kt):
     p = Problem(300, 64, 4000)
     want = p.forward(kt)
