@@ -704,7 +704,7 @@ int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids,
  * Backward, from lse as the forward pass wrote it and dloss (fp32[rows]), and dlse (fp32[rows] or NULL: zeros) where
  * lse itself is part of the loss:
  *   P_iv = scale ((dloss_i + dlse_i) exp(l_iv - lse_i) - dloss_i [v = targets_i]),  dhidden = P weight,  dweight = P^T hidden
- * dhidden or dweight may be NULL (not both).  P is rounded to bf16, a piece of the vocabulary at a time; sums are fp32.
+ * dhidden or dweight may be NULL (not both).  P, in units of each row, is rounded to bf16, a piece of the vocabulary at a time; sums are fp32.
  * workspace (16-byte aligned) holds kt_xent_workspace bytes (for the forward or the backward pass), which need no
  * initial value and may be used again by the next call on the same stream.  No atomics: the same inputs give the same
  * bits.  Outputs must not overlap inputs.  A wait that gives up (above) leaves NaN where results are not right.

@@ -5,10 +5,14 @@
 //   forward    loss_i = lse_i - l_{i, t_i}
 //   backward   P_iv = scale ((g_i + z_i) exp(l_iv - lse_i) - g_i [v = t_i])  for dloss g and dlse z,
 //              dh = P W,  dW = P^T h
+// P is held as Q_iv = P_iv / u_i with a unit u_i = scale g_i of each row, so that a target's entry is near -1: in bf16 that of
+// P itself would be off by up to 2^-9 in the same direction in all rows of equal g (a mean's 1 / n), which with a large
+// vocabulary is nearly all there is (0.3 % in both gradients, where Q gives 0.17 %, what their own rounding is).  dh_i = u_i (Q W)_i
+// and, where all u_i are the same, dW = u Q^T h; else hidden rows are multiplied by u_i before.
 // Three kinds of products (kt_product.cuh):
 //   loss   a tile of logits becomes a maximum, a sum of exponentials and perhaps the target's logit of each row
-//   grad   the logits are formed again, and leave the chip as P in bf16, a piece of the vocabulary at a time (the second
-//          products of the tensor cores take 16-bit operands; bf16 because P spans the range of probabilities)
+//   grad   the logits are formed again, and leave the chip as Q in bf16, a piece of the vocabulary at a time (the second
+//          products of the tensor cores take 16-bit operands; bf16 because Q spans the range of probabilities)
 //   back   dh and dW from the piece.  dW of the piece's rows is whole; dh is summed over the pieces in fp32.
 // Rows that do not count are left out before the products: the rows that do are numbered in order, and where any are
 // missing their hidden rows are copied next to each other, so what the others hold is never multiplied.
@@ -34,7 +38,13 @@ constexpr int64_t MAX_ROWS = 1 << 20, MAX_VOCAB = 1 << 24, MAX_DIM = 1 << 16;
 struct Row {
     int target;                                 // PAST_VOCAB where it is none of the vocabulary's
     float lse2;                                 // in units of log 2
-    float both, only;                           // scale (g + z), scale g
+    float all, target_part;                     // (g + z) / unit, g / unit (without scale)
+};
+// What the rows have in common, at the start of the workspace.
+struct Common {
+    int count;                                  // rows that count
+    int one_unit;                               // whether all have the same unit
+    float unit;
 };
 constexpr int PAST_VOCAB = 0x7FFFFFFF;
 
@@ -46,8 +56,11 @@ struct RowsParams {
     const __nv_bfloat16 *hidden;
     int64_t hidden_stride;
     __nv_bfloat16 *packed;                      // counted rows of hidden, where some do not count
-    int *count, *index;                         // index[i]: the row that is the i-th to count
+    __nv_bfloat16 *scaled;                      // those times their units, where these differ (backward)
+    Common *common;
+    int *index;                                 // index[i]: the row that is the i-th to count
     Row *rows;
+    float *units;
     const float *dloss, *dlse, *lse;            // backward
     float *loss_out, *lse_out;                  // forward
     __nv_bfloat16 *dhidden;
@@ -58,30 +71,53 @@ struct RowsParams {
 
 // Every CTA goes over all targets to find out where its own rows begin: a few microseconds for 64 thousand of them
 // from the L2, and no CTA waits for another.
+__device__ __forceinline__ float unit_of(float g, float z) { return fabsf(g) * 256.0f < fabsf(g + z) ? g + z : g; }      // (NaN: NaN)
+
+__device__ __forceinline__ uint32_t times(uint32_t two, float by) {
+    return pack_bf16(__uint_as_float(two << 16) * by, __uint_as_float(two & 0xFFFF0000u) * by);
+}
+
 __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
     __shared__ int sums[8], sums_before[8], place[256];
+    __shared__ unsigned least[8], most[8];
+    __shared__ float unit_at[256];
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
     let_next_begin();
     const int begin = min(p.n, static_cast<int>(blockIdx.x) * p.each), end = min(p.n, begin + p.each);
+    const bool back = p.lse != nullptr;
+    auto unit = [&](int i, int64_t target) {
+        const float g = target < p.vocab ? p.dloss[i] : __int_as_float(0x7FFFFFFF);
+        return p.scale * unit_of(g, p.dlse != nullptr ? p.dlse[i] : 0.0f);
+    };
     int before = 0, all = 0;
-#pragma unroll 16
+    unsigned low = 0xFFFFFFFFu, high = 0;       // of the units' bits
+#pragma unroll 8
     for (int i = tid; i < p.n; i += 256) {
-        const int counts = p.targets[i] >= 0;
+        const int64_t target = p.targets[i];
+        const int counts = target >= 0;
         all += counts;
         if (i < begin) before += counts;
+        if (back && counts) {
+            const unsigned bits = __float_as_uint(unit(i, target));
+            low = min(low, bits), high = max(high, bits);
+        }
     }
     all = __reduce_add_sync(0xFFFFFFFFu, all), before = __reduce_add_sync(0xFFFFFFFFu, before);
-    if (lane == 0) sums[warp] = all, sums_before[warp] = before;
+    low = __reduce_min_sync(0xFFFFFFFFu, low), high = __reduce_max_sync(0xFFFFFFFFu, high);
+    if (lane == 0) sums[warp] = all, sums_before[warp] = before, least[warp] = low, most[warp] = high;
     __syncthreads();
     all = before = 0;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) all += sums[w], before += sums_before[w];
-    const bool copy = all < p.n;
+    for (int w = 0; w < 8; ++w) all += sums[w], before += sums_before[w], low = min(low, least[w]), high = max(high, most[w]);
+    const bool copy = all < p.n, one_unit = low >= high, scale_rows = back && !one_unit;       // (no row that counts: one unit)
     const int pieces = p.dim / 8;
     if (blockIdx.x == 0) {
-        if (tid == 0) *p.count = all;
-        if (copy)       // a stage of the reduction over rows may read past the last: zeros there
-            for (int64_t i = static_cast<int64_t>(all) * pieces + tid; i < static_cast<int64_t>(round_to(all, K_STEP)) * pieces; i += 256) reinterpret_cast<uint4 *>(p.packed)[i] = make_uint4(0, 0, 0, 0);
+        if (tid == 0) *p.common = {all, one_unit, __uint_as_float(high)};
+        // a stage of the reduction over rows may read past the last: zeros there
+        for (int64_t i = static_cast<int64_t>(all) * pieces + tid; i < static_cast<int64_t>(round_to(all, K_STEP)) * pieces; i += 256) {
+            if (copy) reinterpret_cast<uint4 *>(p.packed)[i] = make_uint4(0, 0, 0, 0);
+            if (scale_rows) reinterpret_cast<uint4 *>(p.scaled)[i] = make_uint4(0, 0, 0, 0);
+        }
     }
     for (int base = begin; base < end; base += 256) {
         const int i = base + tid;
@@ -100,23 +136,30 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
         if (counts) {
             const bool known = target < p.vocab;
             Row row{known ? static_cast<int>(target) : PAST_VOCAB, 0.0f, 0.0f, 0.0f};
-            if (p.lse != nullptr) {
-                const float g = known ? p.dloss[i] : __int_as_float(0x7FFFFFFF), z = p.dlse != nullptr ? p.dlse[i] : 0.0f;
-                row.lse2 = p.lse[i] * LOG2E, row.both = (g + z) * p.scale, row.only = g * p.scale;
+            if (back) {
+                const float g = known ? p.dloss[i] : __int_as_float(0x7FFFFFFF), z = p.dlse != nullptr ? p.dlse[i] : 0.0f, u = unit_of(g, z);
+                row.lse2 = p.lse[i] * LOG2E;
+                if (u != 0.0f) row.all = (g + z) / u, row.target_part = g / u;       // (exactly 1 where the unit is g)
+                p.units[at] = unit_at[tid] = u * p.scale;
             }
             p.rows[at] = row, p.index[at] = i;
         } else if (i < end && p.loss_out != nullptr) {
             p.loss_out[i] = 0.0f, p.lse_out[i] = 0.0f;
         }
-        if (!copy) continue;
+        if (!copy && !scale_rows) continue;
         __syncthreads();
         for (int r = warp; r < min(256, end - base); r += 8) {
             const int to = place[r];
             if (to >= 0) {
                 const uint4 *from = reinterpret_cast<const uint4 *>(p.hidden + (base + r) * p.hidden_stride);
-                uint4 *const row = reinterpret_cast<uint4 *>(p.packed + static_cast<int64_t>(to) * p.dim);
+                uint4 *const row = reinterpret_cast<uint4 *>(p.packed + static_cast<int64_t>(to) * p.dim), *const scaled = reinterpret_cast<uint4 *>(p.scaled + static_cast<int64_t>(to) * p.dim);
+                const float by = unit_at[r];
 #pragma unroll 8
-                for (int c = lane; c < pieces; c += 32) row[c] = from[c];
+                for (int c = lane; c < pieces; c += 32) {
+                    const uint4 v = from[c];
+                    if (copy) row[c] = v;
+                    if (scale_rows) scaled[c] = make_uint4(times(v.x, by), times(v.y, by), times(v.z, by), times(v.w, by));
+                }
             } else if (p.dhidden != nullptr) {
                 uint4 *const row = reinterpret_cast<uint4 *>(p.dhidden + (base + r) * p.dhidden_stride);
                 for (int c = lane; c < pieces; c += 32) row[c] = make_uint4(0, 0, 0, 0);
@@ -131,7 +174,7 @@ struct LogitsMaps {
     CUtensorMap hidden, packed, weight, p;      // rows as they are, or those that count
 };
 struct BackMaps {
-    CUtensorMap p, p_down, weight, hidden, packed, dweight, sums;
+    CUtensorMap p, p_down, weight, hidden, packed, scaled, dweight, sums;
 };
 
 // Rows that a box of hidden rows, or of P, brings: no more than there are.  (The rest of a tile holds what was there before;
@@ -148,14 +191,15 @@ __device__ __forceinline__ void in_bands(int i, int tiles_m, int tiles_n, int ba
 }
 
 struct LogitsParams {
-    const int *count, *index;
+    const Common *common;
+    const int *index;
     const Row *rows;
     const int64_t *targets;                     // where nothing was left out, because one tile holds all rows: instead of the three
     float2 *parts;                              // [half tiles of columns][n]: maximum (units of log 2) and sum
     float *at_target;                           // the target's logit (units of log 2)
     int n, vocab, steps, from, past, band;      // columns from ... past of the vocabulary
     float scale_log2;
-    __device__ __forceinline__ int counted() const { return targets != nullptr ? n : *count; }
+    __device__ __forceinline__ int counted() const { return targets != nullptr ? n : common->count; }
     __device__ __forceinline__ Row row(int i) const {
         if (targets == nullptr) return rows[i];
         const int64_t t = targets[i];
@@ -258,13 +302,13 @@ struct GradTask : LogitsTask<PAIR_> {
 #pragma unroll
             for (int e = 0; e < 32; e += 2) {
                 const float2 y = fma2(pair_of(r, e), both(p.scale_log2), both(-row.lse2));
-                const float2 g = mul2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), both(row.both));
+                const float2 g = mul2(make_float2(exp2_fast(y.x), exp2_fast(y.y)), both(row.all));
                 x[e] = g.x, x[e + 1] = g.y;
             }
             if (static_cast<unsigned>(d) < 32u)
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                    if (e == d) x[e] -= row.only;
+                    if (e == d) x[e] -= row.target_part;
             if (!counts || left < 32)
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
@@ -279,7 +323,9 @@ struct GradTask : LogitsTask<PAIR_> {
 // piece's columns or a share of them, then those of dW, reduced over the counted rows.  A tile of dh takes long where the piece is wide,
 // and there are few of them: workers that do one less of them do more of dW's.
 struct BackParams {
-    const int *count, *index;
+    const Common *common;
+    const int *index;
+    const float *units;
     __nv_bfloat16 *to;                          // dh where a tile has all of it; else NULL, and its shares are added up in fp32
     int64_t to_stride;
     int n, dim, from, past;                     // from ... past: columns of the vocabulary
@@ -294,10 +340,12 @@ struct BackTask {
     static constexpr int SIDE = PAIR ? 256 : 128, BAND = 8;
     static constexpr int FINISH = 2;            // stages' time that a tile's end takes
     struct Cut {
-        int counted, n, worker, workers, steps, shares, tiles_m, tiles_n, tiles_w, weight_steps;
+        int counted, n, one_unit;
+        float unit;
+        int worker, workers, steps, shares, tiles_m, tiles_n, tiles_w, weight_steps;
         int mine, early, late;                  // tiles of dh; of dW while others are at a tile of dh more; and after
         int skip, others, meanwhile;            // workers with a tile of dh more, those without, what the latter do before the rest
-        __device__ Cut(const Params &p, int worker_, int workers_) : counted(*p.count), n(p.n), worker(worker_), workers(workers_), steps(p.steps), shares(p.shares), tiles_n(p.tiles_n), tiles_w(p.tiles_w) {
+        __device__ Cut(const Params &p, int worker_, int workers_) : counted(p.common->count), n(p.n), one_unit(p.common->one_unit), unit(p.common->unit), worker(worker_), workers(workers_), steps(p.steps), shares(p.shares), tiles_n(p.tiles_n), tiles_w(p.tiles_w) {
             tiles_m = (counted + SIDE - 1) / SIDE, weight_steps = (counted + K_STEP - 1) / K_STEP;
             const int hidden = p.hidden ? tiles_m * tiles_n * shares : 0, weight = tiles_w * tiles_n, each = hidden / workers;
             skip = hidden - each * workers, others = workers - skip;
@@ -325,30 +373,32 @@ struct BackTask {
     __device__ static bool b_down(const Tile &) { return true; }
     __device__ static const CUtensorMap *map_a(const Maps &maps, const Cut &, const Tile &t) { return t.kind == 0 ? &maps.p : &maps.p_down; }
     __device__ static int rows_a(const Cut &c, const Tile &) { return rows_of_box(c.n); }
-    __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &c, const Tile &t) { return t.kind == 0 ? &maps.weight : c.counted < c.n ? &maps.packed : &maps.hidden; }
+    __device__ static const CUtensorMap *map_b(const Maps &maps, const Cut &c, const Tile &t) { return t.kind == 0 ? &maps.weight : !c.one_unit ? &maps.scaled : c.counted < c.n ? &maps.packed : &maps.hidden; }
     __device__ static void finish(const Params &p, const Maps &maps, const Cut &cut, const Tile &t, Part &part) {
         const int count = cut.counted;
         const bool weight = t.kind == 1;
         if (weight ? p.from + part.warp_row >= p.past : part.warp_row >= count) return;
+        const float unit = !weight ? (part.row < count ? p.units[part.row] : 0.0f) : cut.one_unit ? cut.unit : 1.0f;
         __nv_bfloat16 *const row = !weight && p.to != nullptr && part.row < count ? p.to + p.index[part.row] * p.to_stride : nullptr;
         over_columns<SIDE / 2>(part, [&](int c0, auto half, uint32_t (&r)[32]) {
             if (weight) {
                 if (c0 - half * 32 >= p.dim) return;
                 if (half == 0) part.store_next();
-                pack_row(part, half, [&](int e) { return __uint_as_float(r[e]); });
+                pack_row(part, half, [&](int e) { return __uint_as_float(r[e]) * unit; });
                 if (half == 1) part.send(&maps.dweight, c0 - 32, p.from + part.warp_row, 0);
             } else if (p.to == nullptr) {
                 if (c0 >= p.dim) return;
                 part.store_next();
 #pragma unroll
-                for (int u = 0; u < 8; ++u) *part.piece(u) = make_uint4(r[u * 4], r[u * 4 + 1], r[u * 4 + 2], r[u * 4 + 3]);
+                for (int u = 0; u < 8; ++u) *part.piece(u) = make_uint4(r[u * 4], r[u * 4 + 1], r[u * 4 + 2], r[u * 4 + 3]);       // (units come with the shares' sum)
                 part.send(&maps.sums, c0, part.warp_row, t.share, p.add != 0);
             } else if (row != nullptr) {
 #pragma unroll
                 for (int e = 0; e < 32; e += 8)
                     if (c0 + e < p.dim) {
                         uint4 v;
-                        v.x = pack_bf16(pair_of(r, e)), v.y = pack_bf16(pair_of(r, e + 2)), v.z = pack_bf16(pair_of(r, e + 4)), v.w = pack_bf16(pair_of(r, e + 6));
+                        v.x = pack_bf16(mul2(pair_of(r, e), both(unit))), v.y = pack_bf16(mul2(pair_of(r, e + 2), both(unit)));
+                        v.z = pack_bf16(mul2(pair_of(r, e + 4), both(unit))), v.w = pack_bf16(mul2(pair_of(r, e + 6), both(unit)));
                         *reinterpret_cast<uint4 *>(row + c0 + e) = v;
                     }
             }
@@ -401,11 +451,11 @@ __global__ void __launch_bounds__(256) k_xent_join(const LogitsParams p, int til
     loss[to] = !counts ? 0.0f : mine.target == PAST_VOCAB ? __int_as_float(0x7FFFFFFF) : ((top - at) + high) * LN2;
 }
 
-// The shares of dh added up, in order.
-__global__ void __launch_bounds__(256) k_xent_dhidden(const int *count, const int *index, const float *sums, int shares, int64_t share, int dim, __nv_bfloat16 *to, int64_t stride) {
+// The shares of dh added up, in order, and given their rows' units.
+__global__ void __launch_bounds__(256) k_xent_dhidden(const Common *common, const int *index, const float *units, const float *sums, int shares, int64_t share, int dim, __nv_bfloat16 *to, int64_t stride) {
     let_next_begin();
     after_previous();
-    const uint32_t pieces = dim / 8, all = *count, step = gridDim.x * 256, step_rows = step / pieces, step_pieces = step % pieces, first = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t pieces = dim / 8, all = common->count, step = gridDim.x * 256, step_rows = step / pieces, step_pieces = step % pieces, first = blockIdx.x * 256 + threadIdx.x;
     uint32_t piece = first % pieces;
     for (uint32_t row = first / pieces; row < all; row += step_rows, piece += step_pieces) {
         if (piece >= pieces) {
@@ -421,7 +471,8 @@ __global__ void __launch_bounds__(256) k_xent_dhidden(const int *count, const in
             a.x += c0.x, a.y += c0.y, a.z += c0.z, a.w += c0.w, b.x += c1.x, b.y += c1.y, b.z += c1.z, b.w += c1.w;
         }
         uint4 v;
-        v.x = pack_bf16(a.x, a.y), v.y = pack_bf16(a.z, a.w), v.z = pack_bf16(b.x, b.y), v.w = pack_bf16(b.z, b.w);
+        const float u = units[row];
+        v.x = pack_bf16(a.x * u, a.y * u), v.y = pack_bf16(a.z * u, a.w * u), v.z = pack_bf16(b.x * u, b.y * u), v.w = pack_bf16(b.z * u, b.w * u);
         *reinterpret_cast<uint4 *>(to + index[row] * stride + c) = v;
     }
 }
@@ -450,7 +501,7 @@ struct Plan {
     bool backward;
     int64_t piece, pieces, shares;              // columns of the vocabulary to a piece; shares of dh's reduction
     bool pairs_logits, pairs_back;
-    int64_t at_index, at_rows, at_packed, at_parts, at_target, at_p, at_sums, bytes;
+    int64_t at_index, at_rows, at_units, at_packed, at_scaled, at_parts, at_target, at_p, at_sums, bytes;
     Plan(int64_t rows, int64_t dims, int64_t words, bool back) : n(rows), dim(dims), vocab(words), backward(back) {
         int64_t at = 0;
         auto take = [&](int64_t size) {
@@ -458,9 +509,10 @@ struct Plan {
             at += up(size, 1024);
             return here;
         };
-        take(4);                                // the number of rows that count
+        take(sizeof(Common));
         at_index = take(4 * n), at_rows = take(static_cast<int64_t>(sizeof(Row)) * n);
-        at_packed = take(2 * up(n, K_STEP) * dim);
+        at_units = take(backward ? 4 * n : 0);
+        at_packed = take(2 * up(n, K_STEP) * dim), at_scaled = take(backward ? 2 * up(n, K_STEP) * dim : 0);
         const int64_t room = PIECE_BYTES / (2 * up(n, TILE)) / 256 * 256, most = room < 256 ? 256 : room;
         pieces = backward ? tiles_of(vocab, static_cast<int>(most)) : 1;
         piece = backward ? up((vocab + pieces - 1) / pieces, 256) : vocab;
@@ -509,8 +561,8 @@ int check_workspace(const void *workspace, int64_t bytes, int64_t need) {
 }
 
 int start_rows(RowsParams &q, const Plan &plan, char *ws, cudaStream_t st) {
-    q.count = reinterpret_cast<int *>(ws), q.index = reinterpret_cast<int *>(ws + plan.at_index), q.rows = reinterpret_cast<Row *>(ws + plan.at_rows);
-    q.packed = reinterpret_cast<__nv_bfloat16 *>(ws + plan.at_packed);
+    q.common = reinterpret_cast<Common *>(ws), q.units = reinterpret_cast<float *>(ws + plan.at_units), q.index = reinterpret_cast<int *>(ws + plan.at_index), q.rows = reinterpret_cast<Row *>(ws + plan.at_rows);
+    q.packed = reinterpret_cast<__nv_bfloat16 *>(ws + plan.at_packed), q.scaled = reinterpret_cast<__nv_bfloat16 *>(ws + plan.at_scaled);
     q.n = static_cast<int>(plan.n), q.dim = static_cast<int>(plan.dim), q.vocab = static_cast<int>(plan.vocab);
     q.each = static_cast<int>((plan.n + 4 * PRODUCT_SMS - 1) / (4 * PRODUCT_SMS));      // four CTAs to an SM
     if (q.each < 8) q.each = 8;                 // a row to a warp
@@ -575,7 +627,7 @@ int kt_xent_forward(const void *hidden, int64_t hidden_stride, const void *weigh
         RowsParams q{};
         q.targets = targets, q.hidden = static_cast<const __nv_bfloat16 *>(hidden), q.hidden_stride = hidden_stride, q.loss_out = loss, q.lse_out = lse, q.scale = scale;
         if (int rc = start_rows(q, plan, ws, st)) return rc;
-        p.count = q.count, p.index = q.index, p.rows = q.rows;
+        p.common = q.common, p.index = q.index, p.rows = q.rows;
     } else {
         p.targets = targets;
     }
@@ -624,6 +676,7 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     if (dweight != nullptr) {
         if (int rc = describe_operand(&back.p_down, "the workspace", false, true, ws + plan.at_p, plan.piece, p_rows, 1, pitch, 0)) return rc;
         if (int rc = describe_rows(&back.hidden, &back.packed, plan, hidden, hidden_stride, ws, true)) return rc;
+        if (int rc = describe_operand(&back.scaled, "the workspace", false, true, ws + plan.at_scaled, dim, up(rows, K_STEP), 1, dim * 2, 0)) return rc;
         if (int rc = describe_matrix(&back.dweight, "dweight", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dweight, dim, vocab, 1, dweight_stride * 2, 0, 64, 32)) return rc;
     }
 
@@ -634,7 +687,7 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     for (int64_t i = 0; i < plan.pieces; ++i) {
         const int64_t from = i * plan.piece, past = from + plan.piece < vocab ? from + plan.piece : vocab;
         LogitsParams p{};
-        p.count = q.count, p.rows = q.rows, p.n = q.n, p.vocab = q.vocab, p.steps = static_cast<int>((dim + K_STEP - 1) / K_STEP);
+        p.common = q.common, p.rows = q.rows, p.n = q.n, p.vocab = q.vocab, p.steps = static_cast<int>((dim + K_STEP - 1) / K_STEP);
         p.from = static_cast<int>(from), p.past = static_cast<int>(past), p.band = band_of(dim, plan.pairs_logits ? 256 : 128), p.scale_log2 = scale * LOG2E;
         const int64_t columns = past - from;
         const int side = plan.pairs_logits ? 256 : 128, back_side = plan.pairs_back ? 256 : 128;
@@ -642,7 +695,7 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
         if (dhidden != nullptr)       // the weights' rows from the piece's first on
             if (int rc = describe_operand(&back.weight, "weight", false, true, static_cast<const __nv_bfloat16 *>(weight) + from * weight_stride, dim, columns, 1, weight_stride * 2, 0)) return rc;
         BackParams b{};
-        b.count = q.count, b.index = q.index, b.to = direct ? q.dhidden : nullptr, b.to_stride = dhidden_stride, b.n = q.n, b.dim = q.dim, b.from = p.from, b.past = p.past;
+        b.common = q.common, b.index = q.index, b.units = q.units, b.to = direct ? q.dhidden : nullptr, b.to_stride = dhidden_stride, b.n = q.n, b.dim = q.dim, b.from = p.from, b.past = p.past;
         b.tiles_n = static_cast<int>(tiles_of(dim, back_side)), b.tiles_w = dweight != nullptr ? static_cast<int>(tiles_of(columns, back_side)) : 0;
         b.shares = static_cast<int>(plan.shares), b.steps = static_cast<int>(tiles_of(columns, K_STEP)), b.add = i > 0, b.hidden = dhidden != nullptr;
         const int64_t tiles = (dhidden != nullptr ? tiles_of(rows, back_side) * b.tiles_n * plan.shares : 0) + static_cast<int64_t>(b.tiles_w) * b.tiles_n;
@@ -650,8 +703,8 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
     }
     if (dhidden != nullptr && !direct) {
         const int64_t blocks = (rows * (dim / 8) + 255) / 256;
-        KT_CUDA(launch_behind(k_xent_dhidden, 1, dim3(static_cast<unsigned>(blocks < 8 * PRODUCT_SMS ? blocks : 8 * PRODUCT_SMS)), dim3(256), 0, st, static_cast<const int *>(q.count),
-                              static_cast<const int *>(q.index), static_cast<const float *>(sums), static_cast<int>(plan.shares), rows * dim, q.dim, q.dhidden, dhidden_stride));
+        KT_CUDA(launch_behind(k_xent_dhidden, 1, dim3(static_cast<unsigned>(blocks < 8 * PRODUCT_SMS ? blocks : 8 * PRODUCT_SMS)), dim3(256), 0, st, static_cast<const Common *>(q.common),
+                              static_cast<const int *>(q.index), static_cast<const float *>(q.units), static_cast<const float *>(sums), static_cast<int>(plan.shares), rows * dim, q.dim, q.dhidden, dhidden_stride));
     }
     return KT_OK;
 }

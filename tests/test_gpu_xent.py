@@ -6,7 +6,8 @@ most (dim / 16 + 16) * 2^-23 * size with size = scale * sum |h| |w| (the tensor 
 of them (256 columns, the joined tiles) at most 400 * 2^-24, the logarithm 2^-23 of its value.
 
 P = scale (g + z) exp(l - lse) - scale g [target] is off by the logit's error and 2^-21 relative to its first term, and
-by half a step of bf16, 2^-8, relative to itself; the products with W and h add those errors times |W| and |h|, sums in fp32
+by half a step of bf16, 2^-8, relative to itself (it is rounded in units of its row: the same relative to itself); where
+the rows' units differ, dW is formed from hidden rows times their units, rounded to bf16: 2^-8 of P's size times |h| more.  The products with W and h add those errors times |W| and |h|, sums in fp32
 ((terms / 16 + 64) * 2^-23 of the terms' sizes), and the result half a step, 2^-8.  What is below fp32's and bf16's smallest
 normal number, 2^-126, may become zero wherever it appears: an exponential (so P is off by scale |g + z| 2^-126 more), P itself,
 each of the terms and the result."""
@@ -101,7 +102,7 @@ class Problem:
             assert (dh[~used] == 0).all()
         if weight:
             want = p.t() @ h
-            slack = loose.t() @ h.abs() + (self.rows / 16 + 64) * 2.0 ** -23 * (p.abs().t() @ h.abs()) + TINY * (self.rows + 1)
+            slack = (loose + U16 * p.abs()).t() @ h.abs() + (self.rows / 16 + 64) * 2.0 ** -23 * (p.abs().t() @ h.abs()) + TINY * (self.rows + 1)
             assert ((dw.double() - want).abs() <= slack + U16 * (want.abs() + slack)).all()
         return dh, dw
 
@@ -135,6 +136,28 @@ def test_rows_that_do_not_count(kt, rows, dim, vocab, ignored):
     dh, dw = p.check_backward(kt, p.check_forward(kt), dlse=p.dlse)
     if ignored > 1:
         assert (dw == 0).all() and (dh == 0).all()
+
+
+@pytest.mark.parametrize("rows,dim,vocab,ignored", [(5, 64, 300, 0.0), (200, 136, 1000, 0.3), (3000, 200, 5003, 0.1), (4096, 128, 2048, 0.0)])
+@pytest.mark.parametrize("kind", ["mean", "weighted", "some zero", "zero", "only lse"])
+def test_gradients_of_the_rows(kt, rows, dim, vocab, ignored, kind):
+    """Rows that share a gradient (a mean's 1 / n, far from a power of two), that differ, that are zero; lse alone."""
+    p = Problem(rows, dim, vocab, ignored)
+    lse = p.check_forward(kt)
+    p.dloss = {"mean": torch.full_like(p.dloss, 1.0 / 3891), "weighted": p.dloss * 1e-3, "some zero": p.dloss * (torch.arange(rows, device="cuda") % 3 > 0),
+               "zero": torch.zeros_like(p.dloss), "only lse": torch.zeros_like(p.dloss)}[kind]
+    dh, dw = p.check_backward(kt, lse, dlse=p.dlse if kind == "only lse" else None)
+    if kind == "zero":
+        assert (dh == 0).all() and (dw == 0).all()
+    if kind == "mean" and dim == 200:
+        # nearly all of a row is its target's entry, which the unit makes exact: the results' own rounding (2^-8 / sqrt(12) to
+        # 2^-9 / sqrt(12), some 0.17 % rms) and hardly more
+        h, w, logits, _, _, _, used = p.exact()
+        q = torch.exp(logits - torch.logsumexp(logits, 1, keepdim=True))
+        q[torch.arange(rows, device="cuda"), p.targets.clamp(min=0)] -= 1.0
+        q = torch.where(used[:, None], q * p.dloss.double()[:, None], 0.0)
+        for got, want in ((dh, q @ w), (dw, q.t() @ h)):
+            assert (got.double() - want).norm() <= 0.0022 * want.norm()
 
 
 @pytest.mark.parametrize("hidden,weight", [(True, False), (False, True)])
