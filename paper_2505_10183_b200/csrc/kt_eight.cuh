@@ -5,25 +5,48 @@
 #include <cuda_bf16.h>
 
 #include <cstdint>
+#include <cstring>
 
 namespace {
 
+// Eight neighbouring elements as they come from memory, which take the registers of their type only.
+template <typename T, bool WHOLE>
+struct Raw {
+    uint4 v[sizeof(T) / 2];
+    __device__ __forceinline__ void read(const T *row, int64_t c, int64_t cols) {
+        if (WHOLE && c + 8 <= cols) {
+#pragma unroll
+            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) v[i] = reinterpret_cast<const uint4 *>(row + c)[i];
+        } else {
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : T(0.0f);
+            memcpy(v, e, sizeof(e));
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const {
+        const uint32_t *const w = reinterpret_cast<const uint32_t *>(v);
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+        }
+    }
+    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
+        float x[8];
+        get(x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += x[i];
+    }
+};
+
 template <typename T, bool WHOLE>
 __device__ __forceinline__ void read_eight(const T *row, int64_t c, int64_t cols, float (&v)[8]) {
-    if (WHOLE && c + 8 <= cols) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(row + c);
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        } else {
-            const float4 a = *reinterpret_cast<const float4 *>(row + c), b = *reinterpret_cast<const float4 *>(row + c + 4);
-            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = c + i < cols ? static_cast<float>(row[c + i]) : 0.0f;
-    }
+    Raw<T, WHOLE> raw;
+    raw.read(row, c, cols);
+    raw.get(v);
 }
 
 template <typename T, bool WHOLE>

@@ -10,7 +10,6 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
-#include <cstring>
 
 #include "kt_eight.cuh"
 #include "kt_internal.h"
@@ -213,33 +212,6 @@ struct SumParams {
     float scale;
 };
 constexpr int MAX_LENGTH = 256, AHEAD = 4;
-
-// Eight neighbouring elements as they come from memory.
-template <typename T, bool WHOLE>
-struct Raw {
-    uint4 v[sizeof(T) / 2];
-    __device__ __forceinline__ void read(const T *row, int64_t c, int64_t cols) {
-        if (WHOLE && c + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < static_cast<int>(sizeof(T) / 2); ++i) v[i] = reinterpret_cast<const uint4 *>(row + c)[i];
-        } else {
-            T e[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = c + i < cols ? row[c + i] : T(0.0f);
-            memcpy(v, e, sizeof(e));
-        }
-    }
-    __device__ __forceinline__ void add_to(float (&sum)[8]) const {
-        const uint32_t *const w = reinterpret_cast<const uint32_t *>(v);
-        if constexpr (sizeof(T) == 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[2 * i] += __uint_as_float(w[i] << 16), sum[2 * i + 1] += __uint_as_float(w[i] & 0xFFFF0000u);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] += __uint_as_float(w[i]);
-        }
-    }
-};
 
 // Rows of the table that no token has: zeros, or the base's; a row to a warp at a time.
 template <typename T, bool WHOLE>

@@ -123,16 +123,18 @@ __global__ void __launch_bounds__(256) k_orth_start(const StartParams p) {
     chunks.at(i, &row, &col);
     const T *const x = static_cast<const T *>(p.x) + blockIdx.y * p.stride[0] + row * p.stride[1];
     __half *const to = p.to + (blockIdx.y * p.rows + row) * p.pitch;
-    float v[4][8];
+    Raw<T, WHOLE> raw[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) read_eight<T, WHOLE>(x, col + u * 256, p.cols, v[u]);
+    for (int u = 0; u < 4; ++u) raw[u].read(x, col + u * 256, p.cols);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
         if (col + u * 256 >= p.cols) break;
+        float v[8];
+        raw[u].get(v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[u][e] = narrow ? v[u][e] * by32 : static_cast<float>(v[u][e] * by);
+        for (int e = 0; e < 8; ++e) v[e] = narrow ? v[e] * by32 : static_cast<float>(v[e] * by);
         uint4 w;
-        w.x = pack_half(v[u][0], v[u][1]), w.y = pack_half(v[u][2], v[u][3]), w.z = pack_half(v[u][4], v[u][5]), w.w = pack_half(v[u][6], v[u][7]);
+        w.x = pack_half(v[0], v[1]), w.y = pack_half(v[2], v[3]), w.z = pack_half(v[4], v[5]), w.w = pack_half(v[6], v[7]);
         *reinterpret_cast<uint4 *>(to + col + u * 256) = w;
     }
 }

@@ -85,21 +85,25 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
     let_next_begin();
     const int begin = min(p.n, static_cast<int>(blockIdx.x) * p.each), end = min(p.n, begin + p.each);
     const bool back = p.lse != nullptr;
-    auto unit = [&](int i, int64_t target) {
-        const float g = target < p.vocab ? p.dloss[i] : __int_as_float(0x7FFFFFFF);
-        return p.scale * unit_of(g, p.dlse != nullptr ? p.dlse[i] : 0.0f);
-    };
     int before = 0, all = 0;
     unsigned low = 0xFFFFFFFFu, high = 0;       // of the units' bits
-#pragma unroll 8
-    for (int i = tid; i < p.n; i += 256) {
-        const int64_t target = p.targets[i];
-        const int counts = target >= 0;
-        all += counts;
-        if (i < begin) before += counts;
-        if (back && counts) {
-            const unsigned bits = __float_as_uint(unit(i, target));
-            low = min(low, bits), high = max(high, bits);
+    for (int i0 = tid; i0 < p.n; i0 += 8 * 256) {       // (all asked for at once, whether they count or not)
+        int64_t target[8];
+        float g[8], z[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) target[u] = i0 + u * 256 < p.n ? p.targets[i0 + u * 256] : -1;
+        if (back) {
+#pragma unroll
+            for (int u = 0; u < 8; ++u) g[u] = i0 + u * 256 < p.n ? p.dloss[i0 + u * 256] : 0.0f, z[u] = p.dlse != nullptr && i0 + u * 256 < p.n ? p.dlse[i0 + u * 256] : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const bool counts = target[u] >= 0;
+            all += counts, before += counts && i0 + u * 256 < begin;
+            if (back && counts) {
+                const unsigned bits = __float_as_uint(p.scale * unit_of(target[u] < p.vocab ? g[u] : __int_as_float(0x7FFFFFFF), z[u]));
+                low = min(low, bits), high = max(high, bits);
+            }
         }
     }
     all = __reduce_add_sync(0xFFFFFFFFu, all), before = __reduce_add_sync(0xFFFFFFFFu, before);
@@ -122,6 +126,7 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
     for (int base = begin; base < end; base += 256) {
         const int i = base + tid;
         const int64_t target = i < end ? p.targets[i] : -1;
+        const float own_g = back && i < end ? p.dloss[i] : 0.0f, own_z = back && p.dlse != nullptr && i < end ? p.dlse[i] : 0.0f, own_lse = back && i < end ? p.lse[i] : 0.0f;
         const bool counts = target >= 0;
         const unsigned mask = __ballot_sync(0xFFFFFFFFu, counts);
         __syncthreads();
@@ -137,8 +142,8 @@ __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
             const bool known = target < p.vocab;
             Row row{known ? static_cast<int>(target) : PAST_VOCAB, 0.0f, 0.0f, 0.0f};
             if (back) {
-                const float g = known ? p.dloss[i] : __int_as_float(0x7FFFFFFF), z = p.dlse != nullptr ? p.dlse[i] : 0.0f, u = unit_of(g, z);
-                row.lse2 = p.lse[i] * LOG2E;
+                const float g = known ? own_g : __int_as_float(0x7FFFFFFF), z = own_z, u = unit_of(g, z);
+                row.lse2 = own_lse * LOG2E;
                 if (u != 0.0f) row.all = (g + z) / u, row.target_part = g / u;       // (exactly 1 where the unit is g)
                 p.units[at] = unit_at[tid] = u * p.scale;
             }
