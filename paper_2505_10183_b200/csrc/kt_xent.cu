@@ -525,7 +525,7 @@ struct Plan {
         pairs_logits = by_pairs(n, piece);
         const int64_t steps = (piece + K_STEP - 1) / K_STEP, over_rows = (n + K_STEP - 1) / K_STEP;
         auto stages = [&](int side, int64_t workers) { return tiles_of(dim, side) * (tiles_of(n, side) * steps + tiles_of(piece, side) * over_rows) / workers; };
-        pairs_back = stages(256, PRODUCT_SMS / 2) >= PAIR_STAGES;
+        pairs_back = n > TILE && stages(256, PRODUCT_SMS / 2) >= PAIR_STAGES;
         // dh: shares of the piece such that a tile takes no longer than all work on all workers, but 16 stages at least (with 8: 38.4 us
         // instead of 33.5 for 200 x 768 on 8001, with 32 34.9)
         const int64_t mean = pairs_back ? stages(256, PRODUCT_SMS / 2) : stages(128, PRODUCT_SMS), longest = mean < 16 ? 16 : mean;
