@@ -8,6 +8,11 @@
 // CTA then reads 32 KB for 2 x 128 x 128 x 64 products, half of what it reads alone.  Without it a CTA works on
 // 128 x 128 by itself: for products too small to give every pair a tile.
 //
+// Bound by the tensor cores where the reduction is long: with 2048 elements of it and 12000 tiles they are at work 97 % of the cycles
+// (1600 TFLOP/s; a large library product 1670 here), 86 % with 1024 and P to be written.  Small products are bound by
+// what a tile costs besides: from the launch before to the first stage 1.1 us, to the last instruction 0.14 us a stage (0.38 for a
+// pair's), to the end 2 us (5), to the next launch 0.9; and one CTA alone by the L2, 32 KB a stage at some 64 bytes a cycle.
+//
 // An operand is a matrix in memory read along its rows (the reduction runs along the row) or down them (the
 // reduction runs from row to row).  What lies outside of a matrix arrives as zeros.
 //
@@ -218,7 +223,6 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     const uint32_t rank = PAIR ? rank_in_pair() : 0;
     const int worker = PAIR ? blockIdx.x / 2 : blockIdx.x, workers = PAIR ? gridDim.x / 2 : gridDim.x;
 
-    let_next_begin();
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) bar_init(&sm.full[i], 1), bar_init(&sm.free[i], 1);
         for (int i = 0; i < 2; ++i) bar_init(&sm.sums_full[i], 1), bar_init(&sm.sums_taken[i], PAIR ? 16 : 8);
@@ -236,6 +240,7 @@ __global__ void __launch_bounds__(PRODUCT_THREADS, 1) k_product(const __grid_con
     const uint32_t tmem = sm.tmem;
     volatile Patience *waits = &sm.waits;
     after_previous();
+    let_next_begin();           // (not before: a chain of small products would come up all at once and wait on every SM)
     const typename Task::Cut cut(p, worker, workers);
     const int tiles = cut.count();
 
