@@ -313,8 +313,8 @@ int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
         if (i == 0) of_factor.a = of_factor.b = square;
         else for (OrthMaps &to : apply) (WIDE ? to.a : to.b) = square;
     }
-    // the copy engine takes rows and matrices at multiples of 16 bytes
-    p.by_copies = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && (plan.rows == 1 || p.out_stride[1] % 8 == 0) && (plan.batch == 1 || p.out_stride[0] % 8 == 0);
+    // the copy engine takes rows and matrices at multiples of 16 bytes, and writes 16 bytes whole where a row ends inside them
+    p.by_copies = reinterpret_cast<uintptr_t>(p.out) % 16 == 0 && plan.cols % 8 == 0 && (plan.rows == 1 || p.out_stride[1] % 8 == 0) && (plan.batch == 1 || p.out_stride[0] % 8 == 0);
     if (p.by_copies)
         if (int rc = describe_matrix(&out, "out", CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.out, plan.cols, plan.rows, plan.batch, p.out_stride[1] * 2, p.out_stride[0] * 2, 32, 32)) return rc;
     // Where every tile of the whole square gets a worker of its own, mirroring would only make each take longer.

@@ -199,15 +199,18 @@ template <int COLS, typename F>
 __device__ __forceinline__ void over_columns(Part &part, F f) {
     uint32_t r[2][32];
     part.wait();
+    __syncwarp();
     part.ask(0, r[0]);
 #pragma unroll 1
     for (int c = 0; c < COLS; c += 64) {
         part.get(r[0]);
         part.ask(c + 32, r[1]);
         f(part.col + c, Constant<0>(), r[0]);
+        __syncwarp();           // tensor memory is read by whole warps
         part.get(r[1]);
         if (c + 64 < COLS) part.ask(c + 64, r[0]);
         f(part.col + c + 32, Constant<1>(), r[1]);
+        __syncwarp();
     }
 }
 

@@ -69,14 +69,15 @@ struct RowsParams {
     float scale;
 };
 
-// Every CTA goes over all targets to find out where its own rows begin: a few microseconds for 64 thousand of them
-// from the L2, and no CTA waits for another.
+// A row's unit without the scale: g, or g + z where that is far more.
 __device__ __forceinline__ float unit_of(float g, float z) { return fabsf(g) * 256.0f < fabsf(g + z) ? g + z : g; }      // (NaN: NaN)
 
 __device__ __forceinline__ uint32_t times(uint32_t two, float by) {
     return pack_bf16(__uint_as_float(two << 16) * by, __uint_as_float(two & 0xFFFF0000u) * by);
 }
 
+// Every CTA goes over all targets to find out where its own rows begin (and, backward, over the gradients: whether the rows have
+// one unit), so no CTA waits for another.  Latency: 4 us for 200 rows, 12 where 1600 of 4096 rows of 2048 are left out.
 __global__ void __launch_bounds__(256) k_xent_rows(const RowsParams p) {
     __shared__ int sums[8], sums_before[8], place[256];
     __shared__ unsigned least[8], most[8];

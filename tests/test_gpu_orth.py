@@ -89,6 +89,9 @@ def test_strides(kt):
     out = torch.full((4, 60, 99), 5.0, dtype=BF16, device="cuda")
     update(kt, wide[:, :, 3:93], out[:, :, 1:91])
     assert torch.equal(out[:, :, 1:91], want) and (out[:, :, 0] == 5).all() and (out[:, :, 91:] == 5).all()
+    room = torch.full((4, 60, 96), 5.0, dtype=BF16, device="cuda")                       # rows at multiples of 16 bytes, which end inside one
+    update(kt, x[:, :, :83].contiguous(), room[:, :, :83])
+    assert far(room[:, :, :83], exact(x[:, :, :83])) <= TOLERANCE and (room[:, :, 83:] == 5).all()
     turned = torch.empty(60, 4, 90, dtype=BF16, device="cuda").transpose(0, 1)           # rows of all matrices in turn
     update(kt, x.transpose(0, 1).contiguous().transpose(0, 1), turned)
     assert torch.equal(turned, want)
