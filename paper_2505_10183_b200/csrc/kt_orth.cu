@@ -256,6 +256,299 @@ struct OrthTask {
     }
 };
 
+// ------------------------------------------------------------------------------ small matrices
+// A matrix whose shorter side fits a tile, and which fits a CTA's shared memory as a whole, goes through all steps in one CTA: X in
+// fp16, its shorter side as rows, is an operand as it lies there, along its rows for A and down them for the next X, which takes its
+// place two chunks of 64 columns at a time.  Eight warps compute, one thread of the ninth issues the products.  A step of 128 x 640 is
+// 5.5 us: 2.9 of products, 2.6 of ends between them; reading x, twice, 9 (and 23 more down the columns of 640 x 128).
+// In us, in one CTA and as a launch to a product: 64 x 64 15 and 55, 128 x 128 21 and 67, 128 x 640 49 and 76, 640 x 128 72 and 80,
+// 100 x 333 (by elements) 66 and 85, 148 x 128 x 640 52 and 237.  Longer ones do not fit.
+constexpr int SMALL_CHUNKS = 10, SMALL_SIDE = TILE, SMALL_LENGTH = SMALL_CHUNKS * 64, SMALL_THREADS = 288, SMALL_READS = 8;
+constexpr uint32_t SMALL_A = 0, SMALL_SQUARE = TILE, SMALL_NEXT = 2 * TILE;       // columns of tensor memory: A, A^2, and two places for the next X
+
+struct SmallParams {
+    const void *x;
+    int64_t x_stride[2], out_stride[2];
+    __nv_bfloat16 *out;
+    int side, length, steps, whole_out;
+    float a, b, c, scale;
+    uint64_t wait_ns;
+};
+struct SmallSmem {
+    alignas(1024) uint8_t x[SMALL_CHUNKS][CHUNK], gram[2][CHUNK], factor[2][CHUNK];
+    uint64_t square_full, next_full[2], next_taken[2];
+    double sums[8];
+    uint32_t tmem;
+    Patience waits;
+};
+// The 16-byte piece `unit` of a row of a chunk, in the 128-byte swizzle.
+__device__ __forceinline__ uint4 *piece_of(uint8_t *chunk, int row, int unit) { return reinterpret_cast<uint4 *>(chunk + row * 128 + ((unit ^ (row & 7)) << 4)); }
+__device__ __forceinline__ uint32_t small_word(int n, bool b_down) {
+    return (1u << 4) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(TILE / 16) << 24);
+}
+
+// The i-th eight elements along the longer side: of memory's rows one after the other, or, where those are the longer side,
+// of 128 rows (of X) next to each other.
+template <typename T, bool WHOLE, bool WIDE>
+struct SmallPiece {
+    Raw<T, WHOLE> raw;
+    static __device__ void place(int i, int units, int *r, int *unit) { *r = i / units, *unit = i - *r * units; }
+    __device__ void read(const SmallParams &p, const T *x, int i, int units, int all) {
+        int r, unit;
+        place(i, units, &r, &unit);
+        raw.read(x + r * p.x_stride[1], unit * 8, i < all ? p.length : 0);
+    }
+    __device__ void get(float (&v)[8]) const { raw.get(v); }
+};
+template <typename T>
+struct SmallPiece<T, false, false> {
+    T raw[8];
+    static __device__ void place(int i, int, int *r, int *unit) { *unit = i / TILE, *r = i - *unit * TILE; }
+    __device__ void read(const SmallParams &p, const T *x, int i, int units, int) {
+        int r, unit;
+        place(i, units, &r, &unit);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[e] = r < p.side && unit * 8 + e < p.length ? x[(unit * 8 + e) * p.x_stride[1] + r] : static_cast<T>(0.0f);
+    }
+    __device__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(raw[e]);
+    }
+};
+
+template <typename T, bool WHOLE, bool WIDE>
+__global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallParams p) {
+    extern __shared__ uint8_t raw[];
+    auto &sm = *reinterpret_cast<SmallSmem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, chunks = (p.length + 63) / 64, k_side = p.side <= 64 ? 64 : 128, blocks = (chunks + 1) / 2;
+    const T *const x = static_cast<const T *>(p.x) + blockIdx.x * p.x_stride[0];
+    __nv_bfloat16 *const out = p.out + blockIdx.x * p.out_stride[0];
+    if (tid == 0) {
+        bar_init(&sm.square_full, 1);
+        for (int i = 0; i < 2; ++i) bar_init(&sm.next_full[i], 1), bar_init(&sm.next_taken[i], 8);
+        sm.waits = {p.wait_ns, 0};
+        fence_async_smem();
+    }
+    if (warp == 8) tmem_alloc(&sm.tmem, 512);
+    // Threads next to each other take neighbours in memory: pieces of eight columns of a row, or rows.  A thread's pieces are 256
+    // apart; each time SMALL_READS are asked for at once: one after the other they took half of the whole time.
+    const int units = chunks * 8, all = WIDE ? p.side * units : TILE * units;
+    using Piece = SmallPiece<T, WHOLE, WIDE>;
+    auto pieces = [&](int i, Piece (&piece)[SMALL_READS]) {
+#pragma unroll
+        for (int u = 0; u < SMALL_READS; ++u) piece[u].read(p, x, i + u * 256, units, all);
+    };
+    double sum = 0.0;
+    if (warp < 8)
+        for (int i = tid; i < all; i += SMALL_READS * 256) {
+            Piece piece[SMALL_READS];
+            pieces(i, piece);
+            float2 adds = both(0.0f);
+            float v[8], top = 0.0f;
+#pragma unroll
+            for (int u = 0; u < SMALL_READS; ++u) {
+                piece[u].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) adds = fma2(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), adds);
+            }
+            const float add = adds.x + adds.y;
+            if (add > 0x1p-80f && add < 0x1p120f) {
+                sum += add;
+                continue;
+            }
+#pragma unroll
+            for (int u = 0; u < SMALL_READS; ++u) {
+                piece[u].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+            }
+            const uint32_t power = min(__float_as_uint(top) >> 23, 253u);
+            const float by = __uint_as_float((254u - power) << 23);
+            float scaled = 0.0f;
+#pragma unroll
+            for (int u = 0; u < SMALL_READS; ++u) {
+                piece[u].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) scaled = fmaf(v[e] * by, v[e] * by, scaled);
+            }
+            sum += scaled * __longlong_as_double((2 * (static_cast<long long>(power) - 127) + 1023) << 52);
+        }
+#pragma unroll
+    for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
+    if (warp < 8 && lane == 0) sm.sums[warp] = sum;
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    sum = sm.sums[0];
+    for (int w = 1; w < 8; ++w) sum += sm.sums[w];
+    const double by = sum == 0.0 ? 0.0 : isfinite(sum) ? X_UNIT / sqrt(sum) : __longlong_as_double(0x7FF8000000000000ll);
+    const int power = isfinite(sum) && sum != 0.0 ? ilogb(by) / 2 : 0;       // fp32 need not hold the factor: in two parts it does
+    const float by_power = __uint_as_float(static_cast<uint32_t>(power + 127) << 23), by_rest = static_cast<float>(ldexp(by, -power));
+    if (warp < 8) {
+        if (WIDE)       // rows past the last are zeros
+            for (int i = tid + p.side * units; i < TILE * units; i += 256) {
+                int r, unit;
+                Piece::place(i, units, &r, &unit);
+                *piece_of(sm.x[unit / 8], r, unit % 8) = make_uint4(0, 0, 0, 0);
+            }
+        for (int i = tid; i < all; i += SMALL_READS * 256) {
+            Piece piece[SMALL_READS];
+            pieces(i, piece);
+#pragma unroll
+            for (int u = 0; u < SMALL_READS; ++u) {
+                if (i + u * 256 >= all) break;
+                int r, unit;
+                float v[8];
+                Piece::place(i + u * 256, units, &r, &unit);
+                piece[u].get(v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = !WIDE && r >= p.side ? 0.0f : v[e] * by_power * by_rest;       // (by_rest may be NaN)
+                *piece_of(sm.x[unit / 8], r, unit % 8) = make_uint4(pack_half(v[0], v[1]), pack_half(v[2], v[3]), pack_half(v[4], v[5]), pack_half(v[6], v[7]));
+            }
+        }
+    }
+    fence_async_smem();
+    __syncthreads();
+
+    const uint32_t tmem = sm.tmem, x_at = smem_addr(sm.x), gram_at = smem_addr(sm.gram), factor_at = smem_addr(sm.factor);
+    volatile Patience *const waits = &sm.waits;
+    const int group = warp / 4, row = warp % 4 * 32 + lane;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+    const bool columns = group * 64 < k_side;              // the group has a part of the square matrices
+    uint32_t squares = 0, taken = 0;                       // phases so far: of square_full; blocks of the next X
+    bool ok = true;
+    // 32 values of the row as fp16 to half of its part of a chunk
+    auto keep = [&](uint8_t *chunk, int half, const uint32_t (&v)[16]) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) *piece_of(chunk, row, half * 4 + u) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
+    };
+    auto square = [&](uint32_t to, uint32_t at, int stages) {       // D = M M^T of M along its rows, 64 elements to a stage
+        for (int k = 0; k < stages * 4; ++k) {
+            const uint64_t off = ((k / 4) * CHUNK + (k % 4) * 32) >> 4, w = operand(OPERAND_ALONG, at) + off;
+            mma_smem(tmem + to, w, w, small_word(k_side, false), k > 0);
+        }
+        mma_commit(&sm.square_full);
+    };
+    for (int step = 0; step < p.steps; ++step) {
+        const bool last = step + 1 == p.steps;
+        for (int which = 0; which < 2; ++which) {              // A, then the factor
+            if (warp == 8) {
+                if (elected()) {
+                    tmem_fence_after();
+                    if (which == 0) square(SMALL_A, x_at, chunks);
+                    else square(SMALL_SQUARE, gram_at, k_side / 64);
+                }
+                __syncwarp();
+            } else {
+                ok = ok && bar_wait(&sm.square_full, squares & 1, waits);
+                tmem_fence_after();
+                if (ok && columns)
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t r[2][32], v[16];
+                        const int c0 = group * 64 + half * 32, d = row - c0;
+                        tmem_load32(lanes + SMALL_A + c0, r[0]);
+                        if (which == 1) tmem_load32(lanes + SMALL_SQUARE + c0, r[1]);
+                        tmem_wait_loads(r);
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float2 f = pair_of(r[0], e);
+                            if (which == 1) {
+                                f = fma2(f, both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(pair_of(r[1], e), both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
+                                if (e == d) f.x += p.a * FACTOR_UNIT;
+                                if (e + 1 == d) f.y += p.a * FACTOR_UNIT;
+                            }
+                            v[e / 2] = pack_half(f.x, f.y);
+                        }
+                        keep(which == 0 ? sm.gram[group] : sm.factor[group], half, v);
+                    }
+                fence_async_smem();
+            }
+            ++squares;
+            tmem_fence_before();
+            __syncthreads();
+        }
+        if (warp == 8) {
+            if (elected()) {
+                tmem_fence_after();
+                for (int j = 0; j < blocks && ok; ++j) {
+                    const uint32_t n = taken + j, at = n & 1;
+                    if (!(ok = bar_wait_one(&sm.next_taken[at], (n / 2 + 1) & 1, waits))) break;
+                    tmem_fence_after();
+                    const int width = min(2, chunks - 2 * j) * 64;
+                    for (int k = 0; k < k_side / 16; ++k)
+                        mma_smem(tmem + SMALL_NEXT + at * TILE, operand(OPERAND_ALONG, factor_at) + (((k / 4) * CHUNK + (k % 4) * 32) >> 4), operand(OPERAND_DOWN, x_at + 2 * j * CHUNK) + ((k * 2048) >> 4),
+                                 small_word(width, true), k > 0);
+                    mma_commit(&sm.next_full[at]);
+                }
+            }
+            __syncwarp();
+        } else {
+            for (int j = 0; j < blocks; ++j) {
+                const uint32_t n = taken + j, at = n & 1;
+                ok = ok && bar_wait(&sm.next_full[at], n / 2 & 1, waits);
+                if (!ok) break;
+                tmem_fence_after();
+                const int chunk = 2 * j + group;
+                uint32_t r[2][32];
+                __syncwarp();              // rows past the last have skipped the end of the block before
+                if (chunk < chunks) {
+                    tmem_load32(lanes + SMALL_NEXT + at * TILE + group * 64, r[0]);
+                    tmem_load32(lanes + SMALL_NEXT + at * TILE + group * 64 + 32, r[1]);
+                    tmem_wait_loads(r);
+                }
+                tmem_fence_before();
+                bar_arrive_warp(&sm.next_taken[at]);
+                if (chunk >= chunks) continue;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int c0 = chunk * 64 + half * 32;
+                    if (!last) {
+                        uint32_t v[16];
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            const float2 f = mul2(pair_of(r[half], e), both(1.0f / FACTOR_UNIT));
+                            v[e / 2] = pack_half(f.x, f.y);
+                        }
+                        keep(sm.x[chunk], half, v);
+                        continue;
+                    }
+                    if (row >= p.side) continue;
+                    const float to_out = p.scale / (FACTOR_UNIT * X_UNIT);
+                    if (WIDE && p.whole_out && c0 + 32 <= p.length) {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 8) {
+                            uint4 w;
+                            w.x = pack_bf16(mul2(pair_of(r[half], e), both(to_out))), w.y = pack_bf16(mul2(pair_of(r[half], e + 2), both(to_out)));
+                            w.z = pack_bf16(mul2(pair_of(r[half], e + 4), both(to_out))), w.w = pack_bf16(mul2(pair_of(r[half], e + 6), both(to_out)));
+                            *reinterpret_cast<uint4 *>(out + row * p.out_stride[1] + c0 + e) = w;
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)       // (of a tall matrix, lanes are neighbours)
+                            if (c0 + e < p.length) out[WIDE ? row * p.out_stride[1] + c0 + e : (c0 + e) * p.out_stride[1] + row] = __float2bfloat16_rn(__uint_as_float(r[half][e]) * to_out);
+                    }
+                }
+            }
+            fence_async_smem();
+        }
+        taken += blocks;
+        tmem_fence_before();
+        __syncthreads();
+    }
+    if (waits->gave_up) {       // products in flight get two milliseconds to finish; then the result is NaN
+        const uint64_t start = now_ns();
+        for (int i = 0; i < 100000 && now_ns() - start < 2000000; ++i) __nanosleep(1000);
+        for (int i = tid; i < p.side * p.length; i += SMALL_THREADS) {
+            const int r = i / p.length, c = i - r * p.length;
+            out[WIDE ? r * p.out_stride[1] + c : c * p.out_stride[1] + r] = __ushort_as_bfloat16(0x7FFF);
+        }
+        __syncthreads();
+    }
+    tmem_fence_after();
+    if (warp == 8) tmem_free(tmem, 512);
+}
+
 // ---------------------------------------------------------------------------------- host side
 int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
@@ -335,6 +628,28 @@ int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
     return KT_OK;
 }
 
+template <typename T, bool WHOLE, bool WIDE>
+int start_small(const SmallParams &p, int64_t batch, cudaStream_t st) {
+    static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
+    constexpr size_t bytes = sizeof(SmallSmem) + 1024;
+    static_assert(bytes <= 227 * 1024, "the matrix and its squares have to fit");
+    int dev = 0;
+    KT_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+        KT_CUDA(cudaFuncSetAttribute(k_orth_small<T, WHOLE, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+        raised.fetch_or(bit, std::memory_order_relaxed);
+    }
+    k_orth_small<T, WHOLE, WIDE><<<static_cast<unsigned>(batch), SMALL_THREADS, bytes, st>>>(p);
+    KT_CUDA(cudaGetLastError());
+    return KT_OK;
+}
+template <typename T>
+int start_small(const SmallParams &p, int64_t batch, bool whole, bool wide, cudaStream_t st) {
+    if (!wide) return start_small<T, false, false>(p, batch, st);
+    return whole ? start_small<T, true, true>(p, batch, st) : start_small<T, false, true>(p, batch, st);
+}
+
 template <typename T>
 int start(StartParams &p, const Plan &plan, bool whole, cudaStream_t st) {
     const int64_t blocks = (plan.rows * ((plan.cols + 1023) / 1024) + 7) / 8;       // eight warps' chunks
@@ -401,6 +716,14 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     p.sums = reinterpret_cast<double *>(ws), p.to = reinterpret_cast<__half *>(ws + plan.at_x[0]);
     const int per = 16 / size;
     const bool whole = reinterpret_cast<uintptr_t>(x) % 16 == 0 && p.stride[0] % per == 0 && p.stride[1] % per == 0;
+    if (plan.side <= SMALL_SIDE && (plan.wide ? cols : rows) <= SMALL_LENGTH) {
+        SmallParams m{};
+        m.x = x, m.out = static_cast<__nv_bfloat16 *>(out), m.side = static_cast<int>(plan.side), m.length = static_cast<int>(plan.wide ? cols : rows), m.steps = steps;
+        m.x_stride[0] = p.stride[0], m.x_stride[1] = p.stride[1], m.out_stride[0] = batch > 1 ? out_stride[0] : 0, m.out_stride[1] = rows > 1 ? out_stride[1] : 0;
+        m.whole_out = reinterpret_cast<uintptr_t>(out) % 16 == 0 && m.out_stride[0] % 8 == 0 && m.out_stride[1] % 8 == 0;
+        m.a = coefficients[0], m.b = coefficients[1], m.c = coefficients[2], m.scale = scale, m.wait_ns = wait_limit_ns();
+        return dtype == KT_F32 ? start_small<float>(m, batch, whole, plan.wide, st) : start_small<__nv_bfloat16>(m, batch, whole, plan.wide, st);
+    }
     if (int rc = dtype == KT_F32 ? start<float>(p, plan, whole, st) : start<__nv_bfloat16>(p, plan, whole, st)) return rc;
     // Pairs of CTAs where there are tiles of 256 x 256 for two thirds of them in the products of symmetric matrices, the smaller ones.
     // In us, one CTA to a tile and pairs: 2048 x 2048 (36 tiles) 259 and 273, 4 x 1024 x 1024 (40) 181 and 197, 16 x 512 x 512 (48)

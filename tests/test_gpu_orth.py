@@ -81,6 +81,44 @@ def test_each_matrix_on_its_own(kt):
     assert (again[3] == 0).all() and torch.isnan(again[4:]).all()
 
 
+@pytest.mark.parametrize("shape", [(128, 640), (640, 128), (128, 641), (641, 128), (129, 640), (640, 129), (64, 640), (65, 577), (1, 640), (640, 1), (3, 128, 576), (3, 513, 120), (200, 100, 330)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_matrix_to_a_cta(kt, shape, dtype):
+    """Up to 128 x 640, and a little more."""
+    x = normal(*shape, dtype=dtype)
+    assert far(update(kt, x, scale=0.7), exact(x, scale=0.7)) <= TOLERANCE
+
+
+@pytest.mark.parametrize("shape", [(100, 70), (120, 600), (140, 200), (200, 140), (300, 500)])
+def test_any_magnitude(kt, shape):
+    """Powers of two change nothing, down to fp32's smallest numbers; zeros stay zeros, and what is not finite stays in its matrix."""
+    x = normal(6, *shape)
+    x = x.sign() * x.abs().clamp(2.0 ** -9, 8.0).bfloat16().float()       # 17 powers of two and 8 bits: exact wherever they are scaled to here
+    got = update(kt, x)
+    x[0] *= 2.0 ** 120
+    x[1] *= 2.0 ** -126
+    x[3] = 0.0
+    x[4, 3, 5] = float("inf")
+    x[5, 0, 0] = float("nan")
+    again = update(kt, x)
+    assert torch.equal(again[:3], got[:3])
+    assert (again[3] == 0).all() and torch.isnan(again[4:]).all()
+
+
+@pytest.mark.parametrize("shape", [(90, 60), (61, 300), (150, 200), (210, 140)])
+def test_room_around_the_output(kt, shape):
+    rows, cols = shape
+    x = normal(4, *shape)
+    want = update(kt, x)
+    for left, right in ((0, 0), (1, 8), (8, 1), (0, -cols % 8)):
+        out = torch.full((4, rows + 1, left + cols + right), 5.0, dtype=BF16, device="cuda")
+        inner = out[:, :rows, left:left + cols]
+        update(kt, x, inner)
+        assert torch.equal(inner, want)
+        inner.fill_(5.0)
+        assert (out == 5).all()
+
+
 def test_strides(kt):
     x = normal(4, 60, 90)
     want = update(kt, x)
