@@ -260,9 +260,9 @@ struct OrthTask {
 // A matrix whose shorter side fits a tile, and which fits a CTA's shared memory as a whole, goes through all steps in one CTA: X in
 // fp16, its shorter side as rows, is an operand as it lies there, along its rows for A and down them for the next X, which takes its
 // place two chunks of 64 columns at a time.  Eight warps compute, one thread of the ninth issues the products.  A step of 128 x 640 is
-// 5.5 us: 2.9 of products, 2.6 of ends between them; reading x, twice, 9 (and 23 more down the columns of 640 x 128).
-// In us, in one CTA and as a launch to a product: 64 x 64 15 and 55, 128 x 128 21 and 67, 128 x 640 49 and 76, 640 x 128 72 and 80,
-// 100 x 333 (by elements) 66 and 85, 148 x 128 x 640 52 and 237.  Longer ones do not fit.
+// 5.5 us: 2.9 of products, 2.6 of ends between them; reading x, twice, takes 8 us.
+// In us, in one CTA and as a launch to a product: 64 x 64 14 and 52, 128 x 128 20 and 65, 128 x 640 47 and 74, 148 x 128 x 640 52 and 237.
+// Longer ones do not fit.
 constexpr int SMALL_CHUNKS = 10, SMALL_SIDE = TILE, SMALL_LENGTH = SMALL_CHUNKS * 64, SMALL_THREADS = 288, SMALL_READS = 8;
 constexpr uint32_t SMALL_A = 0, SMALL_SQUARE = TILE, SMALL_NEXT = 2 * TILE;       // columns of tensor memory: A, A^2, and two places for the next X
 
@@ -283,38 +283,212 @@ struct SmallSmem {
 };
 // The 16-byte piece `unit` of a row of a chunk, in the 128-byte swizzle.
 __device__ __forceinline__ uint4 *piece_of(uint8_t *chunk, int row, int unit) { return reinterpret_cast<uint4 *>(chunk + row * 128 + ((unit ^ (row & 7)) << 4)); }
+__device__ __forceinline__ uint32_t *pair_place(uint8_t *chunk, int row, int pair) { return reinterpret_cast<uint32_t *>(piece_of(chunk, row, pair / 4)) + pair % 4; }       // of 32 pairs
 __device__ __forceinline__ uint32_t small_word(int n, bool b_down) {
     return (1u << 4) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(TILE / 16) << 24);
 }
 
-// The i-th eight elements along the longer side: of memory's rows one after the other, or, where those are the longer side,
-// of 128 rows (of X) next to each other.
+// The rows of X that a CTA begins with: where they are, how many, how long.
+template <typename T>
+struct SmallRows {
+    const T *x;
+    int64_t stride;
+    int side, length, chunks;
+};
+// The i-th eight elements: of memory's rows one after the other, in whole pieces (of 16 bytes, or two such: the length is a multiple of 8);
 template <typename T, bool WHOLE, bool WIDE>
 struct SmallPiece {
     Raw<T, WHOLE> raw;
-    static __device__ void place(int i, int units, int *r, int *unit) { *r = i / units, *unit = i - *r * units; }
-    __device__ void read(const SmallParams &p, const T *x, int i, int units, int all) {
+    static __device__ int all(const SmallRows<T> &rows) { return rows.side * rows.chunks * 8; }
+    static __device__ void place(const SmallRows<T> &rows, int i, int *r, int *unit) { *r = i / (rows.chunks * 8), *unit = i - *r * (rows.chunks * 8); }
+    __device__ void read(const SmallRows<T> &rows, int i) {
         int r, unit;
-        place(i, units, &r, &unit);
-        raw.read(x + r * p.x_stride[1], unit * 8, i < all ? p.length : 0);
+        place(rows, i, &r, &unit);
+        const bool there = i < all(rows) && unit * 8 < rows.length;
+#pragma unroll
+        for (int w = 0; w < static_cast<int>(sizeof(T) / 2); ++w) raw.v[w] = there ? reinterpret_cast<const uint4 *>(rows.x + r * rows.stride + unit * 8)[w] : make_uint4(0, 0, 0, 0);
     }
     __device__ void get(float (&v)[8]) const { raw.get(v); }
-};
-template <typename T>
-struct SmallPiece<T, false, false> {
-    T raw[8];
-    static __device__ void place(int i, int, int *r, int *unit) { *unit = i / TILE, *r = i - *unit * TILE; }
-    __device__ void read(const SmallParams &p, const T *x, int i, int units, int) {
+    static __device__ void keep(const SmallRows<T> &rows, uint8_t (*to)[CHUNK], int i, const float (&v)[8]) {
         int r, unit;
-        place(i, units, &r, &unit);
+        place(rows, i, &r, &unit);
+        *piece_of(to[unit / 8], r, unit % 8) = make_uint4(pack_half(v[0], v[1]), pack_half(v[2], v[3]), pack_half(v[4], v[5]), pack_half(v[6], v[7]));
+    }
+};
+// by elements, two to a lane of each of four rows;
+template <typename T>
+struct SmallPiece<T, false, true> {
+    T raw[8];
+    static __device__ int all(const SmallRows<T> &rows) { return TILE / 4 * rows.chunks * 32; }
+    static __device__ void place(const SmallRows<T> &rows, int i, int *r, int *chunk) { *r = i / 32 / rows.chunks * 4, *chunk = i / 32 - *r / 4 * rows.chunks; }
+    __device__ void read(const SmallRows<T> &rows, int i) {
+        int r, chunk;
+        place(rows, i, &r, &chunk);
+        const int c = chunk * 64 + i % 32 * 2;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) raw[e] = r < p.side && unit * 8 + e < p.length ? x[(unit * 8 + e) * p.x_stride[1] + r] : static_cast<T>(0.0f);
+        for (int e = 0; e < 8; ++e) raw[e] = i < all(rows) && r + e / 2 < rows.side && c + e % 2 < rows.length ? rows.x[(r + e / 2) * rows.stride + c + e % 2] : static_cast<T>(0.0f);
     }
     __device__ void get(float (&v)[8]) const {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(raw[e]);
     }
+    static __device__ void keep(const SmallRows<T> &rows, uint8_t (*to)[CHUNK], int i, const float (&v)[8]) {
+        int r, chunk;
+        place(rows, i, &r, &chunk);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) *pair_place(to[chunk], r + e / 2, i % 32) = r + e / 2 < rows.side ? pack_half(v[e], v[e + 1]) : 0;
+    }
 };
+// or, where memory's rows are the shorter side, of 128 rows (of X) next to each other.
+template <typename T>
+struct SmallPiece<T, false, false> {
+    T raw[8];
+    static __device__ int all(const SmallRows<T> &rows) { return TILE * rows.chunks * 8; }
+    static __device__ void place(int i, int *r, int *unit) { *unit = i / TILE, *r = i - *unit * TILE; }
+    __device__ void read(const SmallRows<T> &rows, int i) {
+        int r, unit;
+        place(i, &r, &unit);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) raw[e] = r < rows.side && unit * 8 + e < rows.length ? rows.x[(unit * 8 + e) * rows.stride + r] : static_cast<T>(0.0f);
+    }
+    __device__ void get(float (&v)[8]) const {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(raw[e]);
+    }
+    static __device__ void keep(const SmallRows<T> &rows, uint8_t (*to)[CHUNK], int i, const float (&v)[8]) {
+        int r, unit;
+        place(i, &r, &unit);
+        *piece_of(to[unit / 8], r, unit % 8) = r < rows.side ? make_uint4(pack_half(v[0], v[1]), pack_half(v[2], v[3]), pack_half(v[4], v[5]), pack_half(v[6], v[7])) : make_uint4(0, 0, 0, 0);
+    }
+};
+// Threads next to each other take neighbours in memory: pieces of eight columns of a row, or rows.  A thread's pieces are THREADS
+// apart; READS are asked for at once: one after the other they took half of the whole time.
+template <typename T, bool WHOLE, bool WIDE, int THREADS, int READS>
+__device__ __forceinline__ double small_squares(const SmallRows<T> &rows) {
+    double sum = 0.0;
+    const int all = SmallPiece<T, WHOLE, WIDE>::all(rows);
+    for (int i = threadIdx.x; i < all; i += READS * THREADS) {
+        SmallPiece<T, WHOLE, WIDE> piece[READS];
+#pragma unroll
+        for (int u = 0; u < READS; ++u) piece[u].read(rows, i + u * THREADS);
+        float2 adds = both(0.0f);
+        float v[8], top = 0.0f;
+#pragma unroll
+        for (int u = 0; u < READS; ++u) {
+            piece[u].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) adds = fma2(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), adds);
+        }
+        const float add = adds.x + adds.y;
+        if (add > 0x1p-80f && add < 0x1p120f) {
+            sum += add;
+            continue;
+        }
+#pragma unroll
+        for (int u = 0; u < READS; ++u) {       // as in k_orth_squares
+            piece[u].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+        }
+        const uint32_t power = min(__float_as_uint(top) >> 23, 253u);
+        const float by = __uint_as_float((254u - power) << 23);
+        float scaled = 0.0f;
+#pragma unroll
+        for (int u = 0; u < READS; ++u) {
+            piece[u].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) scaled = fmaf(v[e] * by, v[e] * by, scaled);
+        }
+        sum += scaled * __longlong_as_double((2 * (static_cast<long long>(power) - 127) + 1023) << 52);
+    }
+    return sum;
+}
+// X = G / |G| in fp16, and zeros in rows past the last.
+template <typename T, bool WHOLE, bool WIDE, int THREADS, int READS>
+__device__ __forceinline__ void small_start(const SmallRows<T> &rows, double sum, uint8_t (*to)[CHUNK]) {
+    using Piece = SmallPiece<T, WHOLE, WIDE>;
+    const double by = sum == 0.0 ? 0.0 : isfinite(sum) ? X_UNIT / sqrt(sum) : __longlong_as_double(0x7FF8000000000000ll);
+    const int power = isfinite(sum) && sum != 0.0 ? ilogb(by) / 2 : 0;       // fp32 need not hold the factor: in two parts it does
+    const float by_power = __uint_as_float(static_cast<uint32_t>(power + 127) << 23), by_rest = static_cast<float>(ldexp(by, -power));
+    const int all = Piece::all(rows);
+    for (int i = threadIdx.x + all; i < TILE * rows.chunks * 8; i += THREADS) *piece_of(to[i / 8 % rows.chunks], i / 8 / rows.chunks, i % 8) = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x; i < all; i += READS * THREADS) {
+        Piece piece[READS];
+#pragma unroll
+        for (int u = 0; u < READS; ++u) piece[u].read(rows, i + u * THREADS);
+#pragma unroll
+        for (int u = 0; u < READS; ++u) {
+            if (i + u * THREADS >= all) break;
+            float v[8];
+            piece[u].get(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] * by_power * by_rest;       // (by_rest may be NaN)
+            Piece::keep(rows, to, i + u * THREADS, v);
+        }
+    }
+}
+// 32 values of the factor's row, from those of A and A^2; d: which is the diagonal's.  (Asking first whether any is costs more than it saves.)
+__device__ __forceinline__ void small_factor(const SmallParams &p, const uint32_t (&gram)[32], const uint32_t (&square)[32], int d, uint32_t (&v)[16]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        float2 f = fma2(pair_of(gram, e), both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(pair_of(square, e), both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
+        if (e == d) f.x += p.a * FACTOR_UNIT;
+        if (e + 1 == d) f.y += p.a * FACTOR_UNIT;
+        v[e / 2] = pack_half(f.x, f.y);
+    }
+}
+__device__ __forceinline__ void small_half(const uint32_t (&sums)[32], float by, uint32_t (&v)[16]) {
+#pragma unroll
+    for (int e = 0; e < 32; e += 2) {
+        const float2 f = mul2(pair_of(sums, e), both(by));
+        v[e / 2] = pack_half(f.x, f.y);
+    }
+}
+// 32 columns of a row as fp16 to half of a chunk
+__device__ __forceinline__ void small_keep(uint8_t *chunk, int row, int half, const uint32_t (&v)[16]) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) *piece_of(chunk, row, half * 4 + u) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
+}
+// 32 columns of a row of the result: to memory, of a tall matrix (lanes are neighbours) or in whole pieces of 16 bytes, or else to
+// half of a chunk, from where small_rows_out takes it.
+template <bool WIDE>
+__device__ __forceinline__ void small_out(const SmallParams &p, __nv_bfloat16 *out, int side, int row, int c0, const uint32_t (&sums)[32], uint8_t *chunk) {
+    const float to_out = p.scale / (FACTOR_UNIT * X_UNIT);
+    if (WIDE) {
+        uint32_t v[16];
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) v[e / 2] = pack_bf16(mul2(pair_of(sums, e), both(to_out)));
+        if (!p.whole_out) {
+            small_keep(chunk, row, c0 / 32 % 2, v);
+        } else if (row < side && c0 < p.length) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<uint4 *>(out + row * p.out_stride[1] + c0 + u * 8) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
+        }
+    } else if (row < side) {
+#pragma unroll
+        for (int e = 0; e < 32; ++e)
+            if (c0 + e < p.length) out[(c0 + e) * p.out_stride[1] + row] = __float2bfloat16_rn(__uint_as_float(sums[e]) * to_out);
+    }
+}
+__device__ __forceinline__ void small_rows_out(const SmallParams &p, __nv_bfloat16 *out, int side, int chunks, uint8_t (*from)[CHUNK]) {
+    for (int i = threadIdx.x; i < side * chunks * 32; i += blockDim.x) {
+        const int r = i / 32 / chunks, chunk = i / 32 - r * chunks, c = chunk * 64 + i % 32 * 2;
+        const uint32_t v = *pair_place(from[chunk], r, i % 32);
+        __nv_bfloat16 *const to = out + r * p.out_stride[1] + c;
+        if (c < p.length) to[0] = __ushort_as_bfloat16(static_cast<unsigned short>(v));
+        if (c + 1 < p.length) to[1] = __ushort_as_bfloat16(static_cast<unsigned short>(v >> 16));
+    }
+}
+// After a wait that gave up: products in flight get two milliseconds to finish; then the result is NaN.
+template <bool WIDE>
+__device__ __forceinline__ void small_given_up(const SmallParams &p, __nv_bfloat16 *out, int side) {
+    const uint64_t start = now_ns();
+    for (int i = 0; i < 100000 && now_ns() - start < 2000000; ++i) __nanosleep(1000);
+    for (int i = threadIdx.x; i < side * p.length; i += blockDim.x) {
+        const int r = i / p.length, c = i - r * p.length;
+        out[WIDE ? r * p.out_stride[1] + c : c * p.out_stride[1] + r] = __ushort_as_bfloat16(0x7FFF);
+    }
+}
 
 template <typename T, bool WHOLE, bool WIDE>
 __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallParams p) {
@@ -330,49 +504,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
         fence_async_smem();
     }
     if (warp == 8) tmem_alloc(&sm.tmem, 512);
-    // Threads next to each other take neighbours in memory: pieces of eight columns of a row, or rows.  A thread's pieces are 256
-    // apart; each time SMALL_READS are asked for at once: one after the other they took half of the whole time.
-    const int units = chunks * 8, all = WIDE ? p.side * units : TILE * units;
-    using Piece = SmallPiece<T, WHOLE, WIDE>;
-    auto pieces = [&](int i, Piece (&piece)[SMALL_READS]) {
-#pragma unroll
-        for (int u = 0; u < SMALL_READS; ++u) piece[u].read(p, x, i + u * 256, units, all);
-    };
-    double sum = 0.0;
-    if (warp < 8)
-        for (int i = tid; i < all; i += SMALL_READS * 256) {
-            Piece piece[SMALL_READS];
-            pieces(i, piece);
-            float2 adds = both(0.0f);
-            float v[8], top = 0.0f;
-#pragma unroll
-            for (int u = 0; u < SMALL_READS; ++u) {
-                piece[u].get(v);
-#pragma unroll
-                for (int e = 0; e < 8; e += 2) adds = fma2(make_float2(v[e], v[e + 1]), make_float2(v[e], v[e + 1]), adds);
-            }
-            const float add = adds.x + adds.y;
-            if (add > 0x1p-80f && add < 0x1p120f) {
-                sum += add;
-                continue;
-            }
-#pragma unroll
-            for (int u = 0; u < SMALL_READS; ++u) {
-                piece[u].get(v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-            }
-            const uint32_t power = min(__float_as_uint(top) >> 23, 253u);
-            const float by = __uint_as_float((254u - power) << 23);
-            float scaled = 0.0f;
-#pragma unroll
-            for (int u = 0; u < SMALL_READS; ++u) {
-                piece[u].get(v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) scaled = fmaf(v[e] * by, v[e] * by, scaled);
-            }
-            sum += scaled * __longlong_as_double((2 * (static_cast<long long>(power) - 127) + 1023) << 52);
-        }
+    const SmallRows<T> rows{x, p.x_stride[1], p.side, p.length, chunks};
+    double sum = warp < 8 ? small_squares<T, WHOLE, WIDE, 256, SMALL_READS>(rows) : 0.0;
 #pragma unroll
     for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
     if (warp < 8 && lane == 0) sm.sums[warp] = sum;
@@ -381,32 +514,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
     tmem_fence_after();
     sum = sm.sums[0];
     for (int w = 1; w < 8; ++w) sum += sm.sums[w];
-    const double by = sum == 0.0 ? 0.0 : isfinite(sum) ? X_UNIT / sqrt(sum) : __longlong_as_double(0x7FF8000000000000ll);
-    const int power = isfinite(sum) && sum != 0.0 ? ilogb(by) / 2 : 0;       // fp32 need not hold the factor: in two parts it does
-    const float by_power = __uint_as_float(static_cast<uint32_t>(power + 127) << 23), by_rest = static_cast<float>(ldexp(by, -power));
-    if (warp < 8) {
-        if (WIDE)       // rows past the last are zeros
-            for (int i = tid + p.side * units; i < TILE * units; i += 256) {
-                int r, unit;
-                Piece::place(i, units, &r, &unit);
-                *piece_of(sm.x[unit / 8], r, unit % 8) = make_uint4(0, 0, 0, 0);
-            }
-        for (int i = tid; i < all; i += SMALL_READS * 256) {
-            Piece piece[SMALL_READS];
-            pieces(i, piece);
-#pragma unroll
-            for (int u = 0; u < SMALL_READS; ++u) {
-                if (i + u * 256 >= all) break;
-                int r, unit;
-                float v[8];
-                Piece::place(i + u * 256, units, &r, &unit);
-                piece[u].get(v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = !WIDE && r >= p.side ? 0.0f : v[e] * by_power * by_rest;       // (by_rest may be NaN)
-                *piece_of(sm.x[unit / 8], r, unit % 8) = make_uint4(pack_half(v[0], v[1]), pack_half(v[2], v[3]), pack_half(v[4], v[5]), pack_half(v[6], v[7]));
-            }
-        }
-    }
+    if (warp < 8) small_start<T, WHOLE, WIDE, 256, SMALL_READS>(rows, sum, sm.x);
     fence_async_smem();
     __syncthreads();
 
@@ -417,11 +525,6 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
     const bool columns = group * 64 < k_side;              // the group has a part of the square matrices
     uint32_t squares = 0, taken = 0;                       // phases so far: of square_full; blocks of the next X
     bool ok = true;
-    // 32 values of the row as fp16 to half of its part of a chunk
-    auto keep = [&](uint8_t *chunk, int half, const uint32_t (&v)[16]) {
-#pragma unroll
-        for (int u = 0; u < 4; ++u) *piece_of(chunk, row, half * 4 + u) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
-    };
     auto square = [&](uint32_t to, uint32_t at, int stages) {       // D = M M^T of M along its rows, 64 elements to a stage
         for (int k = 0; k < stages * 4; ++k) {
             const uint64_t off = ((k / 4) * CHUNK + (k % 4) * 32) >> 4, w = operand(OPERAND_ALONG, at) + off;
@@ -446,21 +549,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         uint32_t r[2][32], v[16];
-                        const int c0 = group * 64 + half * 32, d = row - c0;
+                        const int c0 = group * 64 + half * 32;
                         tmem_load32(lanes + SMALL_A + c0, r[0]);
                         if (which == 1) tmem_load32(lanes + SMALL_SQUARE + c0, r[1]);
                         tmem_wait_loads(r);
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            float2 f = pair_of(r[0], e);
-                            if (which == 1) {
-                                f = fma2(f, both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(pair_of(r[1], e), both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
-                                if (e == d) f.x += p.a * FACTOR_UNIT;
-                                if (e + 1 == d) f.y += p.a * FACTOR_UNIT;
-                            }
-                            v[e / 2] = pack_half(f.x, f.y);
-                        }
-                        keep(which == 0 ? sm.gram[group] : sm.factor[group], half, v);
+                        if (which == 0) small_half(r[0], 1.0f, v);
+                        else small_factor(p, r[0], r[1], row - c0, v);
+                        small_keep(which == 0 ? sm.gram[group] : sm.factor[group], row, half, v);
                     }
                 fence_async_smem();
             }
@@ -505,28 +600,10 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
                     const int c0 = chunk * 64 + half * 32;
                     if (!last) {
                         uint32_t v[16];
-#pragma unroll
-                        for (int e = 0; e < 32; e += 2) {
-                            const float2 f = mul2(pair_of(r[half], e), both(1.0f / FACTOR_UNIT));
-                            v[e / 2] = pack_half(f.x, f.y);
-                        }
-                        keep(sm.x[chunk], half, v);
-                        continue;
-                    }
-                    if (row >= p.side) continue;
-                    const float to_out = p.scale / (FACTOR_UNIT * X_UNIT);
-                    if (WIDE && p.whole_out && c0 + 32 <= p.length) {
-#pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint4 w;
-                            w.x = pack_bf16(mul2(pair_of(r[half], e), both(to_out))), w.y = pack_bf16(mul2(pair_of(r[half], e + 2), both(to_out)));
-                            w.z = pack_bf16(mul2(pair_of(r[half], e + 4), both(to_out))), w.w = pack_bf16(mul2(pair_of(r[half], e + 6), both(to_out)));
-                            *reinterpret_cast<uint4 *>(out + row * p.out_stride[1] + c0 + e) = w;
-                        }
+                        small_half(r[half], 1.0f / FACTOR_UNIT, v);
+                        small_keep(sm.x[chunk], row, half, v);
                     } else {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)       // (of a tall matrix, lanes are neighbours)
-                            if (c0 + e < p.length) out[WIDE ? row * p.out_stride[1] + c0 + e : (c0 + e) * p.out_stride[1] + row] = __float2bfloat16_rn(__uint_as_float(r[half][e]) * to_out);
+                        small_out<WIDE>(p, out, p.side, row, c0, r[half], sm.x[chunk]);
                     }
                 }
             }
@@ -536,17 +613,221 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
         tmem_fence_before();
         __syncthreads();
     }
-    if (waits->gave_up) {       // products in flight get two milliseconds to finish; then the result is NaN
-        const uint64_t start = now_ns();
-        for (int i = 0; i < 100000 && now_ns() - start < 2000000; ++i) __nanosleep(1000);
-        for (int i = tid; i < p.side * p.length; i += SMALL_THREADS) {
-            const int r = i / p.length, c = i - r * p.length;
-            out[WIDE ? r * p.out_stride[1] + c : c * p.out_stride[1] + r] = __ushort_as_bfloat16(0x7FFF);
-        }
+    if (WIDE && !p.whole_out) small_rows_out(p, out, p.side, chunks, sm.x);
+    if (waits->gave_up) {
+        __syncthreads();
+        small_given_up<WIDE>(p, out, p.side);
         __syncthreads();
     }
     tmem_fence_after();
     if (warp == 8) tmem_free(tmem, 512);
+}
+
+// A matrix whose shorter side fits two tiles goes through all steps in a pair of CTAs, where its length fits.  Each has 128 rows
+// of X, an operand of A as they lie there; its rows of A, and then of the factor, take their place (X is read no more by then);
+// and, for the next X, of which a CTA's part of the operand is half of the columns, every row of every other chunk of 64 columns.
+// The sums of all of the next X stay in tensor memory until the products have ended.  Then they go to the rows, and to the CTA's own
+// columns; the copy engine brings the other CTA's (15 bytes a cycle between two CTAs, 3300 cycles) while the next A is multiplied.
+// A step of 256 x 384 is 9.8 us: 4.3 of products, the rest ends of 64 columns of a row to a thread, their way to the copies that the
+// tensor cores see (0.4 us each), and arrivals from the other CTA (0.3 to 0.5).  Parts of the rows multiplied as they come are slower
+// (66 us in all instead of 64): each has to be made visible by itself.  Reading x, twice, takes 7 us.
+// In us, in a pair and as a launch to a product: 129 x 129 53 and 85, 256 x 256 53 and 70, 256 x 384 64 and 74, 384 x 250 74 and 92, 250 x 333
+// (by elements) 78 and 91, 74 x 256 x 384 66 and 161, 200 x 192 x 192 146 and 238.  Longer ones do not fit.
+constexpr int PAIR_CHUNKS = 6, PAIR_BLOCKS = PAIR_CHUNKS / 2, PAIR_SIDE = 2 * TILE, PAIR_LENGTH = PAIR_CHUNKS * 64, PAIR_WARPS = 16, PAIR_THREADS = PAIR_WARPS * 32;
+constexpr uint32_t PAIR_A = 0, PAIR_SQUARE = 256, PAIR_NEXT = 0;        // columns of tensor memory; the next X after both have been read
+
+struct PairSmem {
+    alignas(1024) uint8_t rows[PAIR_CHUNKS][CHUNK], cols[PAIR_CHUNKS][CHUNK];       // cols: two, of 256 rows, to each of the CTA's chunks of columns
+    uint64_t ready, rows_ready, rows_here;                                      // by warps: those of both CTAs (in the first), and of this one
+    uint64_t square_full, next_full[PAIR_BLOCKS], cols_full, cols_late, sent;    // late: of chunks that no row of A takes the place of
+    double sums[2 * PAIR_WARPS];
+    uint32_t tmem;
+    Patience waits;
+};
+__device__ __forceinline__ uint32_t pair_word(int n, bool b_down) {
+    return (1u << 4) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(PAIR_SIDE / 16) << 24);
+}
+__device__ __forceinline__ void copy_to_cta(uint32_t to, uint32_t from, uint32_t bytes, uint32_t bar) {         // to a CTA of the pair, counted there
+    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "r"(from), "r"(bytes), "r"(bar) : "memory");
+}
+// After a wait for arrivals from both CTAs: what was done there before them is seen here.
+__device__ __forceinline__ void seen_of_pair(uint64_t *bar, uint32_t parity) {
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(smem_addr(bar)), "r"(parity) : "memory");
+}
+
+template <typename T, bool WHOLE, bool WIDE>
+__global__ void __launch_bounds__(PAIR_THREADS, 1) k_orth_pair(const SmallParams p) {
+    extern __shared__ uint8_t raw[];
+    auto &sm = *reinterpret_cast<PairSmem *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, chunks = (p.length + 63) / 64, blocks = (chunks + 1) / 2, matrix = blockIdx.x / 2;
+    const int rank = static_cast<int>(rank_in_pair()), side = min(p.side - rank * TILE, TILE);       // (its rows)
+    const T *const x = static_cast<const T *>(p.x) + matrix * p.x_stride[0] + rank * TILE * (WIDE ? p.x_stride[1] : 1);
+    __nv_bfloat16 *const out = p.out + matrix * p.out_stride[0] + rank * TILE * (WIDE ? p.out_stride[1] : 1);
+    if (tid == 0) {
+        bar_init(&sm.ready, 2 * PAIR_WARPS);
+        bar_init(&sm.square_full, 1);
+        for (int j = 0; j < PAIR_BLOCKS; ++j) bar_init(&sm.next_full[j], 1);
+        bar_init(&sm.rows_ready, 2 * PAIR_WARPS);
+        bar_init(&sm.rows_here, PAIR_WARPS);
+        bar_init(&sm.cols_full, 1);
+        bar_init(&sm.cols_late, 1);
+        bar_init(&sm.sent, 2);
+        sm.waits = {p.wait_ns, 0};
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        fence_async_smem();
+    }
+    if (warp == 0) sums_alloc<true>(&sm.tmem, 512);
+    constexpr int READS = WHOLE ? 4 : 2;        // more take too many registers by elements
+    const SmallRows<T> rows{x, p.x_stride[1], side, p.length, chunks};
+    double sum = small_squares<T, WHOLE, WIDE, PAIR_THREADS, READS>(rows);
+#pragma unroll
+    for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
+    cluster_sync();             // the other CTA is there
+    if (lane < 2) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(address_in(smem_addr(&sm.sums[rank * PAIR_WARPS + warp]), lane)), "d"(sum) : "memory");
+    tmem_fence_before();
+    cluster_sync();
+    tmem_fence_after();
+    sum = sm.sums[lane];
+#pragma unroll
+    for (int far = 16; far; far /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, far);
+    small_start<T, WHOLE, WIDE, PAIR_THREADS, READS>(rows, sum, sm.rows);
+
+    const uint32_t tmem = sm.tmem, rows_at = smem_addr(sm.rows), cols_at = smem_addr(sm.cols);
+    volatile Patience *const waits = &sm.waits;
+    const int group = warp / 4, row = warp % 4 * 32 + lane, k_side = (p.side + 15) / 16;
+    const uint32_t lanes = tmem + (static_cast<uint32_t>(warp % 4 * 32) << 16);
+    const bool issues = warp == 0 && rank == 0;
+    uint32_t squares = 0;                       // phases so far
+    bool ok = true, copies = true;              // copies: every one so far has come, so that the barrier may be told of more; the other CTA's then stop as well, for want of these
+    auto written = [&](uint64_t *bar, uint64_t *here) {        // the warp's part of an operand
+        fence_async_smem();
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+            arrive_at(address_in(smem_addr(bar), 0));
+            if (here != nullptr) bar_arrive(here);
+        }
+    };
+    // One thread, once the operands are there: products, and an arrival in both CTAs.
+    auto may_issue = [&](uint64_t *bar, uint32_t parity) {
+        if (!bar_wait_one(bar, parity, waits)) return false;
+        seen_of_pair(bar, parity);
+        tmem_fence_after();
+        return true;
+    };
+    auto square = [&](uint32_t to, int steps) {       // D = M M^T of M along its rows, `steps` times 16 elements
+        for (int k = 0; k < steps; ++k) {
+            const uint64_t w = operand(OPERAND_ALONG, rows_at) + (((k / 4) * CHUNK + (k % 4) * 32) >> 4);
+            multiply<true>(tmem + to, w, w, pair_word(PAIR_SIDE, false), k > 0);
+        }
+        multiplied<true>(&sm.square_full);
+    };
+    __syncthreads();
+    for (int c = rank; c < chunks; c += 2)
+        for (int i = tid; i < static_cast<int>(CHUNK / 16); i += PAIR_THREADS) reinterpret_cast<uint4 *>(sm.cols[c])[i] = reinterpret_cast<const uint4 *>(sm.rows[c])[i];
+    written(&sm.rows_ready, &sm.rows_here);
+    for (int step = 0;; ++step) {
+        const uint32_t parity = step & 1;
+        if (issues) {
+            if (elected() && may_issue(&sm.rows_ready, parity)) square(PAIR_A, (p.length + 15) / 16);
+            __syncwarp();
+        }
+        // behind A: the rows to the other CTA's columns
+        if (warp == 1) {
+            if (lane == 0 && copies) {
+                const int mine = (chunks + 1 - rank) / 2;        // of the other CTA's rows
+                bar_expect(&sm.cols_full, min(mine, 2) * CHUNK);
+                bar_expect(&sm.cols_late, max(mine - 2, 0) * CHUNK);
+                copies = bar_wait_one(&sm.rows_here, parity, waits);
+                for (int c = rank ^ 1; copies && c < chunks; c += 2)
+                    copy_to_cta(address_in(smem_addr(sm.cols[c / 2 * 2 + rank]), rank ^ 1), smem_addr(sm.rows[c]), CHUNK, address_in(smem_addr(c < 4 ? &sm.cols_full : &sm.cols_late), rank ^ 1));
+                copies = copies && bar_wait_one(&sm.cols_full, parity, waits);
+                if (copies)
+                    for (int to = 0; to < 2; ++to) arrive_at(address_in(smem_addr(&sm.sent), to));
+            }
+            __syncwarp();
+        }
+        for (int which = 0; which < 2; ++which) {              // A, then the factor
+            if (which == 1 && issues) {
+                if (elected() && may_issue(&sm.ready, 0)) square(PAIR_SQUARE, k_side);
+                __syncwarp();
+            }
+            ok = ok && bar_wait(&sm.square_full, squares & 1, waits);
+            ++squares;
+            if (which == 0) {       // rows may be written
+                ok = ok && bar_wait(&sm.sent, parity, waits);
+                seen_of_pair(&sm.sent, parity);
+            }
+            __syncwarp();
+            tmem_fence_after();
+            if (ok)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t r[2][32], v[16];
+                    const int c0 = group * 64 + half * 32;
+                    tmem_load32(lanes + PAIR_A + c0, r[0]);
+                    if (which == 1) tmem_load32(lanes + PAIR_SQUARE + c0, r[1]);
+                    tmem_wait_loads(r);
+                    if (which == 0) small_half(r[0], 1.0f, v);
+                    else small_factor(p, r[0], r[1], rank * TILE + row - c0, v);
+                    small_keep(sm.rows[group], row, half, v);
+                }
+            if (which == 1 && warp == 1 && lane == 0 && copies) copies = bar_wait_one(&sm.cols_late, parity, waits);
+            written(&sm.ready, nullptr);
+        }
+        if (issues) {
+            if (elected() && may_issue(&sm.ready, 1))
+                for (int j = 0; j < blocks; ++j) {
+                    for (int k = 0; k < k_side; ++k)
+                        multiply<true>(tmem + PAIR_NEXT + j * 128, operand(OPERAND_ALONG, rows_at) + (((k / 4) * CHUNK + (k % 4) * 32) >> 4), operand(OPERAND_DOWN, cols_at + j * (2 * CHUNK)) + ((k * 2048) >> 4),
+                                       pair_word(128, true), k > 0);
+                    multiplied<true>(&sm.next_full[j]);
+                }
+            __syncwarp();
+        }
+        // Each group has 32 columns of a block of 128.
+        auto block = [&](int j, uint32_t (&r)[32]) {
+            ok = ok && bar_wait(&sm.next_full[j], parity, waits);
+            __syncwarp();
+            if (!ok || j * 4 + group >= 2 * chunks) return false;
+            tmem_fence_after();
+            tmem_load32(lanes + PAIR_NEXT + j * 128 + group * 32, r);
+            tmem_wait_loads(r);
+            return true;
+        };
+        if (step + 1 == p.steps) {
+#pragma unroll 1
+            for (int j = 0; j < blocks; ++j) {
+                uint32_t r[32];
+                if (block(j, r)) small_out<WIDE>(p, out, side, row, j * 128 + group * 32, r, sm.cols[2 * j + group / 2]);
+            }
+            break;
+        }
+        uint32_t v[PAIR_BLOCKS][16];            // held until the last product has read the factor
+#pragma unroll
+        for (int j = 0; j < PAIR_BLOCKS; ++j) {
+            uint32_t r[32];
+            if (j < blocks && block(j, r)) small_half(r, 1.0f / FACTOR_UNIT, v[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < PAIR_BLOCKS; ++j) {
+            if (!ok || j * 4 + group >= 2 * chunks) break;
+            small_keep(sm.rows[2 * j + group / 2], row, group % 2, v[j]);
+            if (group / 2 == rank) small_keep(sm.cols[2 * j + rank], row, group % 2, v[j]);
+        }
+        written(&sm.rows_ready, &sm.rows_here);
+    }
+    tmem_fence_before();
+    cluster_sync();
+    uint32_t gave_up;           // here, or in the other CTA, whose rows are in every product
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(gave_up) : "r"(address_in(smem_addr(&sm.waits.gave_up), rank ^ 1)) : "memory");
+    if (WIDE && !p.whole_out) small_rows_out(p, out, side, chunks, sm.cols);       // (a block's columns are free when its products have ended)
+    __syncthreads();
+    if (gave_up | waits->gave_up) small_given_up<WIDE>(p, out, side);
+    __syncwarp();
+    cluster_sync();             // the other CTA's reads and products here are done
+    tmem_fence_after();
+    if (warp == 0) sums_free<true>(tmem, 512);
 }
 
 // ---------------------------------------------------------------------------------- host side
@@ -628,26 +909,31 @@ int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
     return KT_OK;
 }
 
-template <typename T, bool WHOLE, bool WIDE>
+template <bool PAIR, typename T, bool WHOLE, bool WIDE>
 int start_small(const SmallParams &p, int64_t batch, cudaStream_t st) {
     static std::atomic<uint64_t> raised{0};      // a bit for each device on which the kernel's limit has been raised
-    constexpr size_t bytes = sizeof(SmallSmem) + 1024;
+    constexpr auto kernel = PAIR ? k_orth_pair<T, WHOLE, WIDE> : k_orth_small<T, WHOLE, WIDE>;
+    constexpr size_t bytes = (PAIR ? sizeof(PairSmem) : sizeof(SmallSmem)) + 1024;
     static_assert(bytes <= 227 * 1024, "the matrix and its squares have to fit");
     int dev = 0;
     KT_CUDA(cudaGetDevice(&dev));
     const uint64_t bit = 1ull << (dev & 63);
     if (dev > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
-        KT_CUDA(cudaFuncSetAttribute(k_orth_small<T, WHOLE, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
+        KT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes)));
         raised.fetch_or(bit, std::memory_order_relaxed);
     }
-    k_orth_small<T, WHOLE, WIDE><<<static_cast<unsigned>(batch), SMALL_THREADS, bytes, st>>>(p);
-    KT_CUDA(cudaGetLastError());
+    if constexpr (PAIR) {
+        KT_CUDA(launch_joint(kernel, 2, dim3(static_cast<unsigned>(2 * batch)), dim3(PAIR_THREADS), bytes, st, p));
+    } else {
+        kernel<<<static_cast<unsigned>(batch), SMALL_THREADS, bytes, st>>>(p);
+        KT_CUDA(cudaGetLastError());
+    }
     return KT_OK;
 }
-template <typename T>
+template <bool PAIR, typename T>
 int start_small(const SmallParams &p, int64_t batch, bool whole, bool wide, cudaStream_t st) {
-    if (!wide) return start_small<T, false, false>(p, batch, st);
-    return whole ? start_small<T, true, true>(p, batch, st) : start_small<T, false, true>(p, batch, st);
+    if (!wide) return start_small<PAIR, T, false, false>(p, batch, st);
+    return whole ? start_small<PAIR, T, true, true>(p, batch, st) : start_small<PAIR, T, false, true>(p, batch, st);
 }
 
 template <typename T>
@@ -716,13 +1002,17 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     p.sums = reinterpret_cast<double *>(ws), p.to = reinterpret_cast<__half *>(ws + plan.at_x[0]);
     const int per = 16 / size;
     const bool whole = reinterpret_cast<uintptr_t>(x) % 16 == 0 && p.stride[0] % per == 0 && p.stride[1] % per == 0;
-    if (plan.side <= SMALL_SIDE && (plan.wide ? cols : rows) <= SMALL_LENGTH) {
+    const int64_t length = plan.wide ? cols : rows;
+    const bool small = plan.side <= SMALL_SIDE && length <= SMALL_LENGTH, pair = plan.side <= PAIR_SIDE && length <= PAIR_LENGTH;
+    if (small || pair) {
         SmallParams m{};
-        m.x = x, m.out = static_cast<__nv_bfloat16 *>(out), m.side = static_cast<int>(plan.side), m.length = static_cast<int>(plan.wide ? cols : rows), m.steps = steps;
+        m.x = x, m.out = static_cast<__nv_bfloat16 *>(out), m.side = static_cast<int>(plan.side), m.length = static_cast<int>(length), m.steps = steps;
         m.x_stride[0] = p.stride[0], m.x_stride[1] = p.stride[1], m.out_stride[0] = batch > 1 ? out_stride[0] : 0, m.out_stride[1] = rows > 1 ? out_stride[1] : 0;
-        m.whole_out = reinterpret_cast<uintptr_t>(out) % 16 == 0 && m.out_stride[0] % 8 == 0 && m.out_stride[1] % 8 == 0;
+        m.whole_out = reinterpret_cast<uintptr_t>(out) % 16 == 0 && m.out_stride[0] % 8 == 0 && m.out_stride[1] % 8 == 0 && length % 32 == 0;
         m.a = coefficients[0], m.b = coefficients[1], m.c = coefficients[2], m.scale = scale, m.wait_ns = wait_limit_ns();
-        return dtype == KT_F32 ? start_small<float>(m, batch, whole, plan.wide, st) : start_small<__nv_bfloat16>(m, batch, whole, plan.wide, st);
+        const bool pieces = whole && length % 8 == 0;
+        if (small) return dtype == KT_F32 ? start_small<false, float>(m, batch, pieces, plan.wide, st) : start_small<false, __nv_bfloat16>(m, batch, pieces, plan.wide, st);
+        return dtype == KT_F32 ? start_small<true, float>(m, batch, pieces, plan.wide, st) : start_small<true, __nv_bfloat16>(m, batch, pieces, plan.wide, st);
     }
     if (int rc = dtype == KT_F32 ? start<float>(p, plan, whole, st) : start<__nv_bfloat16>(p, plan, whole, st)) return rc;
     // Pairs of CTAs where there are tiles of 256 x 256 for two thirds of them in the products of symmetric matrices, the smaller ones.
