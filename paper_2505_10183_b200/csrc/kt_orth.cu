@@ -9,9 +9,9 @@
 // bf16, whose range is not needed, has 8: the result is as far from 64 bits as one in 32 bits rounded to bf16.
 // Powers of two keep small entries off fp16's subnormals: X is held times 2^7, A times 2^14, the factor times 2^13.
 // A and the factor are symmetric: tiles on and above the diagonal are computed, and written to both sides.
-// Every product waits for the one before, so a small matrix is bound by 15 times what a launch of one tile takes (256 x 384:
-// 73 us, 4.9 each), and all products in one launch, with a count of arrivals between them, were slower (110 us: the
-// fences and the count's way through the L2 cost more than a launch).  4 x 4096 x 2048: 59 + 38 + 93 us a step, the tensor cores busy
+// Every product waits for the one before, so a matrix of few tiles is bound by 15 times what a launch of one takes (256 x 448:
+// 75 us, 5 each), and all products in one launch, with a count of arrivals between them, were slower (256 x 384: 110 us instead of 74: the
+// fences and the count's way through the L2 cost more than a launch).  What fits the shared memory of a CTA or two needs neither (below).  4 x 4096 x 2048: 59 + 38 + 93 us a step, the tensor cores busy
 // 76, 58 and 86 % of it (two rounds of 144 tiles on 74 pairs in the first two); power sets the clocks.
 #include "../../include/kaitian.h"
 
@@ -32,6 +32,7 @@ namespace {
 
 constexpr float X_UNIT = 128.0f, A_UNIT = 16384.0f, FACTOR_UNIT = 8192.0f;
 constexpr int MAX_STEPS = 64;
+constexpr int REST_SIDE = 64;                   // up to which the factor's diagonal is kept beyond fp16
 constexpr int SUM_BLOCKS = 256;                 // partial sums of squares to a matrix, at most: a thread reads one
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -155,10 +156,50 @@ struct OrthParams {
     int by_copies;                              // the result goes out like the others; else by single elements
     int64_t pitch;                              // of A, in elements
     const __half *gram;
+    float *diagonal, *rest;                     // of A; what fp16 leaves of the factor's (rest: NULL where it does not matter); pitch to a matrix
+    const __half *x;                            // where rest matters, the X that the factor goes to
+    int64_t x_pitch;
     float a, b, c, scale;
     __nv_bfloat16 *out;
     int64_t out_stride[2];
 };
+__device__ __forceinline__ float2 of_half(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }       // a pair of fp16
+
+// The factor is computed from the diagonal D of A, kept in fp32, and what is beside it, R, in fp16: A^2 = R^2 + D R + R D + D^2.  The
+// diagonal's elements are by far the largest, and alike where X is far from square: their rounding to fp16 would move all singular
+// values the same way, and a step takes what is beyond 1.2 four times as far (4 x 465: 0.8 % off the formula, 300 x 3000 0.34; without it
+// 0.2).  What is added to the diagonal, in units of the factor:
+__device__ __forceinline__ float factor_diagonal(float a, float b, float per_square, float own) { return fmaf(own, fmaf(own, per_square, b * (FACTOR_UNIT / A_UNIT)), a * FACTOR_UNIT); }
+// The lane's own of 32 values (a block of 32 rows and columns has its diagonal there).
+__device__ __forceinline__ float own_of(const uint32_t (&r)[32]) {
+    const int lane = threadIdx.x % 32;
+    uint32_t v[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = r[i];
+#pragma unroll
+    for (int n = 16; n; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = lane & n ? v[i + n] : v[i];
+    return __uint_as_float(v[0]);
+}
+__device__ __forceinline__ float beyond_half(float x) { return x - __half2float(__float2half_rn(x)); }
+// Eight values at `at` that are the same for a whole warp
+struct Eight {
+    float4 v[2];
+    __device__ explicit Eight(const float *at) { v[0] = reinterpret_cast<const float4 *>(at)[0], v[1] = reinterpret_cast<const float4 *>(at)[1]; }
+    __device__ float2 pair(int e) const { return e % 4 == 0 ? make_float2(v[e / 4].x, v[e / 4].y) : make_float2(v[e / 4].z, v[e / 4].w); }
+};
+// The factor's own diagonal is rounded too, which counts where there are few of them (4 x 465: 0.4 %): `rest` of it times x is added.
+template <typename F>
+__device__ __forceinline__ void add_rest(uint32_t (&sums)[32], int at, uint4 x, F rest_of) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        const float2 f = of_half(w[e / 2]);
+        sums[at + e] = __float_as_uint(fmaf(f.x, rest_of(at + e), __uint_as_float(sums[at + e])));
+        sums[at + e + 1] = __float_as_uint(fmaf(f.y, rest_of(at + e + 1), __uint_as_float(sums[at + e + 1])));
+    }
+}
 
 // Three products to a step: A, the factor a I + b A + c A^2 from it, and the next X, factor times X (WIDE) or X times factor.
 // A result leaves in boxes of 32 x 32.  The mirrored side of a symmetric one goes through shared memory, where lanes
@@ -214,20 +255,34 @@ struct OrthTask {
             for (int u = 0; u < 4; ++u) g[u] = from[u];
         };
         of_gram(part.col);
+        float *const diagonal = p.diagonal + t.z * p.pitch;
+        const float per_square = p.c * (FACTOR_UNIT / A_UNIT / A_UNIT), own = KIND == FACTOR && part.row < p.side ? diagonal[part.row] : 0.0f;
+        const float per_gram = fmaf(per_square, own, p.b * (FACTOR_UNIT / A_UNIT));
+        const bool rest = KIND >= APPLY && p.rest != nullptr && part.row < rows;
+        const float rest_of = WIDE && rest ? p.rest[t.z * p.pitch + part.row] : 0.0f;
         over_columns<SIDE / 2>(part, [&](int c0, auto, uint32_t (&r)[32]) {
             if (c0 >= cols) return;
             uint32_t v[16];
-            [[maybe_unused]] const int d = part.row - c0;
+            if (rest) {
+                const uint4 *const from = reinterpret_cast<const uint4 *>(p.x + (static_cast<int64_t>(t.z) * p.rows + part.row) * p.x_pitch + c0);
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) {
-                float2 x = KIND == GRAM ? pair_of(r, e) : mul2(pair_of(r, e), both(by));
-                if constexpr (KIND == FACTOR) {
-                    const uint32_t w = e % 8 / 2 == 0 ? g[e / 8].x : e % 8 / 2 == 1 ? g[e / 8].y : e % 8 / 2 == 2 ? g[e / 8].z : g[e / 8].w;
-                    x = fma2(__half22float2(*reinterpret_cast<const __half2 *>(&w)), both(p.b * (FACTOR_UNIT / A_UNIT)), x);
-                    if (e == d) x.x += p.a * FACTOR_UNIT;
-                    if (e + 1 == d) x.y += p.a * FACTOR_UNIT;
+                for (int u = 0; u < 4; ++u) {
+                    const uint4 x = from[u];
+                    add_rest(r, u * 8, x, [&](int e) { return WIDE ? rest_of : p.rest[t.z * p.pitch + c0 + e]; });
                 }
-                v[e / 2] = KIND == LAST ? pack_bf16(x) : pack_half(x.x, x.y);
+            }
+#pragma unroll
+            for (int e0 = 0; e0 < 32; e0 += 8) {
+                const Eight diagonals(KIND == FACTOR ? diagonal + c0 + e0 : diagonal);
+#pragma unroll
+                for (int e = e0; e < e0 + 8; e += 2) {
+                    float2 x = KIND == GRAM ? pair_of(r, e) : mul2(pair_of(r, e), both(by));
+                    if constexpr (KIND == FACTOR) {
+                        const uint32_t w = e % 8 / 2 == 0 ? g[e / 8].x : e % 8 / 2 == 1 ? g[e / 8].y : e % 8 / 2 == 2 ? g[e / 8].z : g[e / 8].w;
+                        x = fma2(of_half(w), fma2(diagonals.pair(e - e0), both(per_square), both(per_gram)), x);
+                    }
+                    v[e / 2] = KIND == LAST ? pack_bf16(x) : pack_half(x.x, x.y);
+                }
             }
             of_gram(c0 + 32);
             if (KIND == LAST && !p.by_copies) {
@@ -243,6 +298,14 @@ struct OrthTask {
 #pragma unroll
             for (int u = 0; u < 4; ++u)         // rows of 64 bytes, in the 64-byte swizzle
                 *reinterpret_cast<uint4 *>(part.store + lane * 64 + ((u ^ (lane / 2 & 3)) << 4)) = make_uint4(v[u * 4], v[u * 4 + 1], v[u * 4 + 2], v[u * 4 + 3]);
+            if (SYMMETRIC && c0 == part.warp_row) {       // a block of the diagonal
+                const float there = own_of(r), on = KIND == GRAM ? there : fmaf(per_square, there, factor_diagonal(p.a, p.b, per_square, own));
+                *reinterpret_cast<__half *>(part.store + lane * 64 + ((lane / 8 ^ (lane / 2 & 3)) << 4) + lane % 8 * 2) = KIND == GRAM ? __half(0.0f) : __float2half_rn(on);
+                if (part.row < p.side) {
+                    if (KIND == GRAM) diagonal[part.row] = on;
+                    else if (p.rest != nullptr) p.rest[t.z * p.pitch + part.row] = beyond_half(on);
+                }
+            }
             if (mirrored) {
                 uint8_t *const mirror = part.store + STORE_BYTES / 2 + (lane & 1) * 64 + (lane & ~1) * 2;
 #pragma unroll
@@ -278,6 +341,7 @@ struct SmallSmem {
     alignas(1024) uint8_t x[SMALL_CHUNKS][CHUNK], gram[2][CHUNK], factor[2][CHUNK];
     uint64_t square_full, next_full[2], next_taken[2];
     double sums[8];
+    alignas(16) float diagonal[TILE], rest[TILE];       // as in k_product's tasks
     uint32_t tmem;
     Patience waits;
 };
@@ -427,15 +491,33 @@ __device__ __forceinline__ void small_start(const SmallRows<T> &rows, double sum
         }
     }
 }
-// 32 values of the factor's row, from those of A and A^2; d: which is the diagonal's.  (Asking first whether any is costs more than it saves.)
-__device__ __forceinline__ void small_factor(const SmallParams &p, const uint32_t (&gram)[32], const uint32_t (&square)[32], int d, uint32_t (&v)[16]) {
+// 32 values of the factor's row but for the diagonal's: first what A gives, from the row's element of A's diagonal and those of the
+// columns, then what R^2 does.  (All at once would be too many registers.)
+__device__ __forceinline__ void small_of_gram(const SmallParams &p, uint32_t (&gram)[32], float own, const float *diagonal) {
+    const float per_square = p.c * (FACTOR_UNIT / A_UNIT / A_UNIT), per_gram = fmaf(per_square, own, p.b * (FACTOR_UNIT / A_UNIT));
+#pragma unroll
+    for (int e0 = 0; e0 < 32; e0 += 8) {
+        const Eight diagonals(diagonal + e0);
+#pragma unroll
+        for (int e = e0; e < e0 + 8; e += 2) {
+            const float2 f = mul2(pair_of(gram, e), fma2(diagonals.pair(e - e0), both(per_square), both(per_gram)));
+            gram[e] = __float_as_uint(f.x), gram[e + 1] = __float_as_uint(f.y);
+        }
+    }
+}
+__device__ __forceinline__ void small_factor(const SmallParams &p, const uint32_t (&of_gram)[32], const uint32_t (&square)[32], uint32_t (&v)[16]) {
 #pragma unroll
     for (int e = 0; e < 32; e += 2) {
-        float2 f = fma2(pair_of(gram, e), both(p.b * (FACTOR_UNIT / A_UNIT)), mul2(pair_of(square, e), both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT))));
-        if (e == d) f.x += p.a * FACTOR_UNIT;
-        if (e + 1 == d) f.y += p.a * FACTOR_UNIT;
+        const float2 f = fma2(pair_of(square, e), both(p.c * (FACTOR_UNIT / A_UNIT / A_UNIT)), pair_of(of_gram, e));
         v[e / 2] = pack_half(f.x, f.y);
     }
+}
+// An element of a chunk
+__device__ __forceinline__ __half *half_place(uint8_t *chunk, int row, int col) { return reinterpret_cast<__half *>(pair_place(chunk, row, col / 2)) + col % 2; }
+// The factor's element of the diagonal
+__device__ __forceinline__ float small_diagonal(const SmallParams &p, float own, float square) {
+    const float per_square = p.c * (FACTOR_UNIT / A_UNIT / A_UNIT);
+    return fmaf(per_square, square, factor_diagonal(p.a, p.b, per_square, own));
 }
 __device__ __forceinline__ void small_half(const uint32_t (&sums)[32], float by, uint32_t (&v)[16]) {
 #pragma unroll
@@ -504,6 +586,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
         fence_async_smem();
     }
     if (warp == 8) tmem_alloc(&sm.tmem, 512);
+    if (tid < TILE) sm.diagonal[tid] = sm.rest[tid] = 0.0f;
     const SmallRows<T> rows{x, p.x_stride[1], p.side, p.length, chunks};
     double sum = warp < 8 ? small_squares<T, WHOLE, WIDE, 256, SMALL_READS>(rows) : 0.0;
 #pragma unroll
@@ -546,17 +629,33 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
                 ok = ok && bar_wait(&sm.square_full, squares & 1, waits);
                 tmem_fence_after();
                 if (ok && columns)
-#pragma unroll
+#pragma unroll 1
                     for (int half = 0; half < 2; ++half) {
-                        uint32_t r[2][32], v[16];
+                        uint32_t r[32], v[16];
                         const int c0 = group * 64 + half * 32;
-                        tmem_load32(lanes + SMALL_A + c0, r[0]);
-                        if (which == 1) tmem_load32(lanes + SMALL_SQUARE + c0, r[1]);
+                        tmem_load32(lanes + SMALL_A + c0, r);
                         tmem_wait_loads(r);
-                        if (which == 0) small_half(r[0], 1.0f, v);
-                        else small_factor(p, r[0], r[1], row - c0, v);
+                        if (which == 0) {
+                            small_half(r, 1.0f, v);
+                        } else {
+                            uint32_t square[32];
+                            tmem_load32(lanes + SMALL_SQUARE + c0, square);
+                            small_of_gram(p, r, sm.diagonal[row], &sm.diagonal[c0]);
+                            tmem_wait_loads(square);
+                            small_factor(p, r, square, v);
+                        }
                         small_keep(which == 0 ? sm.gram[group] : sm.factor[group], row, half, v);
                     }
+                if (ok && columns && group == warp % 4 / 2) {       // the block of the diagonal, read once more: its elements and the rest are too many registers at once
+                    const int c = warp % 4 * 32;
+                    uint32_t r[32];
+                    tmem_load32(lanes + (which == 0 ? SMALL_A : SMALL_SQUARE) + c, r);
+                    tmem_wait_loads(r);
+                    const float there = own_of(r), own = sm.diagonal[row], on = small_diagonal(p, own, there);
+                    *half_place(which == 0 ? sm.gram[group] : sm.factor[group], row, c % 64 + lane) = which == 0 ? __half(0.0f) : __float2half_rn(on);
+                    if (which == 0) sm.diagonal[row] = there;
+                    else sm.rest[row] = beyond_half(on);
+                }
                 fence_async_smem();
             }
             ++squares;
@@ -595,9 +694,13 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
                 tmem_fence_before();
                 bar_arrive_warp(&sm.next_taken[at]);
                 if (chunk >= chunks) continue;
+                const float rest = sm.rest[row];
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
                     const int c0 = chunk * 64 + half * 32;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (p.side <= REST_SIDE) add_rest(r[half], u * 8, *piece_of(sm.x[chunk], row, half * 4 + u), [&](int) { return rest; });
                     if (!last) {
                         uint32_t v[16];
                         small_half(r[half], 1.0f / FACTOR_UNIT, v);
@@ -641,6 +744,7 @@ struct PairSmem {
     uint64_t ready, rows_ready, rows_here;                                      // by warps: those of both CTAs (in the first), and of this one
     uint64_t square_full, next_full[PAIR_BLOCKS], cols_full, cols_late, sent;    // late: of chunks that no row of A takes the place of
     double sums[2 * PAIR_WARPS];
+    alignas(16) float diagonal[PAIR_SIDE];                                       // of A, as in k_product's tasks
     uint32_t tmem;
     Patience waits;
 };
@@ -753,6 +857,7 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_orth_pair(const SmallParams
                 __syncwarp();
             }
             ok = ok && bar_wait(&sm.square_full, squares & 1, waits);
+            seen_of_pair(&sm.square_full, squares & 1);
             ++squares;
             if (which == 0) {       // rows may be written
                 ok = ok && bar_wait(&sm.sent, parity, waits);
@@ -761,17 +866,33 @@ __global__ void __launch_bounds__(PAIR_THREADS, 1) k_orth_pair(const SmallParams
             __syncwarp();
             tmem_fence_after();
             if (ok)
-#pragma unroll
+#pragma unroll 1
                 for (int half = 0; half < 2; ++half) {
-                    uint32_t r[2][32], v[16];
+                    uint32_t r[32], v[16];
                     const int c0 = group * 64 + half * 32;
-                    tmem_load32(lanes + PAIR_A + c0, r[0]);
-                    if (which == 1) tmem_load32(lanes + PAIR_SQUARE + c0, r[1]);
+                    tmem_load32(lanes + PAIR_A + c0, r);
                     tmem_wait_loads(r);
-                    if (which == 0) small_half(r[0], 1.0f, v);
-                    else small_factor(p, r[0], r[1], rank * TILE + row - c0, v);
+                    if (which == 0) {
+                        small_half(r, 1.0f, v);
+                    } else {
+                        uint32_t square[32];
+                        tmem_load32(lanes + PAIR_SQUARE + c0, square);
+                        small_of_gram(p, r, sm.diagonal[rank * TILE + row], &sm.diagonal[c0]);
+                        tmem_wait_loads(square);
+                        small_factor(p, r, square, v);
+                    }
                     small_keep(sm.rows[group], row, half, v);
                 }
+            if (ok && group == rank * 2 + warp % 4 / 2) {           // the block of the diagonal, as in k_orth_small
+                const int mine = rank * TILE + row;
+                uint32_t r[32];
+                tmem_load32(lanes + (which == 0 ? PAIR_A : PAIR_SQUARE) + mine - lane, r);
+                tmem_wait_loads(r);
+                const float there = own_of(r), on = small_diagonal(p, sm.diagonal[mine], there);
+                *half_place(sm.rows[group], row, (mine - lane) % 64 + lane) = which == 0 ? __half(0.0f) : __float2half_rn(on);
+                if (which == 0)
+                    for (int to = 0; to < 2; ++to) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(address_in(smem_addr(&sm.diagonal[mine]), to)), "f"(there) : "memory");
+            }
             if (which == 1 && warp == 1 && lane == 0 && copies) copies = bar_wait_one(&sm.cols_late, parity, waits);
             written(&sm.ready, nullptr);
         }
@@ -836,12 +957,14 @@ int64_t up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 struct Plan {
     int64_t batch, rows, cols, side, pitch_x, pitch_a;
     bool wide;
-    int64_t at_x[2], at_gram, at_factor, bytes;           // the sums of squares come first
+    int64_t at_x[2], at_gram, at_factor, at_diagonal, at_rest, bytes;           // the sums of squares come first
     Plan(int64_t b, int64_t r, int64_t c) : batch(b), rows(r), cols(c), side(r < c ? r : c), pitch_x(up(c, 64)), pitch_a(up(side, 64)), wide(r <= c) {
         int64_t at = up(batch * SUM_BLOCKS * 8, 1024);
         for (int64_t &x : at_x) x = at, at += up(batch * rows * pitch_x * 2, 1024);
         at_gram = at, at += up(batch * side * pitch_a * 2, 1024);
         at_factor = at, at += up(batch * side * pitch_a * 2, 1024);
+        at_diagonal = at, at += up(batch * pitch_a * 4, 1024);
+        at_rest = at, at += up(batch * pitch_a * 4, 1024);
         bytes = at;
     }
 };
@@ -899,6 +1022,7 @@ int run(const Plan &plan, char *ws, OrthParams p, int steps, cudaStream_t st) {
         if (int rc = start_product<OrthTask<PAIR, WIDE, GRAM>>(of_gram, p, symmetric, st)) return rc;
         if (int rc = start_product<OrthTask<PAIR, WIDE, FACTOR>>(of_factor, p, symmetric, st)) return rc;
         OrthMaps m = apply[i % 2];
+        p.x = reinterpret_cast<const __half *>(ws + plan.at_x[i % 2]);
         if (i + 1 < steps) {
             if (int rc = start_product<OrthTask<PAIR, WIDE, APPLY>>(m, p, applied, st)) return rc;
         } else {
@@ -1022,7 +1146,8 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     const bool pairs = symmetric * (symmetric + 1) / 2 * batch >= 45;
     OrthParams q{};
     q.rows = static_cast<int>(rows), q.cols = static_cast<int>(cols), q.side = static_cast<int>(plan.side), q.batch = static_cast<int>(batch);
-    q.pitch = plan.pitch_a, q.gram = reinterpret_cast<const __half *>(ws + plan.at_gram);
+    q.pitch = plan.pitch_a, q.gram = reinterpret_cast<const __half *>(ws + plan.at_gram), q.x_pitch = plan.pitch_x;
+    q.diagonal = reinterpret_cast<float *>(ws + plan.at_diagonal), q.rest = plan.side <= REST_SIDE ? reinterpret_cast<float *>(ws + plan.at_rest) : nullptr;
     q.a = coefficients[0], q.b = coefficients[1], q.c = coefficients[2], q.scale = scale;
     q.out = static_cast<__nv_bfloat16 *>(out), q.out_stride[0] = out_stride[0], q.out_stride[1] = out_stride[1];
     if (plan.wide) return pairs ? run<true, true>(plan, ws, q, steps, st) : run<false, true>(plan, ws, q, steps, st);
