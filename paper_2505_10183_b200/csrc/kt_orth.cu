@@ -10,8 +10,8 @@
 // Powers of two keep small entries off fp16's subnormals: X is held times 2^7, A times 2^14, the factor times 2^13.
 // A and the factor are symmetric: tiles on and above the diagonal are computed, and written to both sides.
 // Every product waits for the one before, so a matrix of few tiles is bound by 15 times what a launch of one takes (256 x 448:
-// 75 us, 5 each), and all products in one launch, with a count of arrivals between them, were slower (256 x 384: 110 us instead of 74: the
-// fences and the count's way through the L2 cost more than a launch).  What fits the shared memory of a CTA or two needs neither (below).  4 x 4096 x 2048: 59 + 38 + 93 us a step, the tensor cores busy
+// 81 us, 5 each), and all products in one launch, with a count of arrivals between them, were slower (256 x 384: 110 us instead of 74: the
+// fences and the count's way through the L2 cost more than a launch).  What fits the shared memory of a CTA or two needs neither (below).  4 x 4096 x 2048: some 60 + 40 + 93 us a step, the tensor cores busy
 // 76, 58 and 86 % of it (two rounds of 144 tiles on 74 pairs in the first two); power sets the clocks.
 #include "../../include/kaitian.h"
 
@@ -32,7 +32,9 @@ namespace {
 
 constexpr float X_UNIT = 128.0f, A_UNIT = 16384.0f, FACTOR_UNIT = 8192.0f;
 constexpr int MAX_STEPS = 64;
-constexpr int REST_SIDE = 64;                   // up to which the factor's diagonal is kept beyond fp16
+// Whether the factor's diagonal is kept beyond fp16: where its elements are few, or alike because X is far from square (40 x 5000 with
+// and without: 0.17 and 0.31 % off the formula, 30 x 438 0.17 and 0.30; the time of 64 x 640 36 and 38 us).  Elsewhere it changes little.
+bool keeps_rest(int64_t side, int64_t length) { return side <= 64 || length >= 8 * side; }
 constexpr int SUM_BLOCKS = 256;                 // partial sums of squares to a matrix, at most: a thread reads one
 
 __device__ __forceinline__ uint32_t pack_half(float lo, float hi) {
@@ -189,7 +191,7 @@ struct Eight {
     __device__ explicit Eight(const float *at) { v[0] = reinterpret_cast<const float4 *>(at)[0], v[1] = reinterpret_cast<const float4 *>(at)[1]; }
     __device__ float2 pair(int e) const { return e % 4 == 0 ? make_float2(v[e / 4].x, v[e / 4].y) : make_float2(v[e / 4].z, v[e / 4].w); }
 };
-// The factor's own diagonal is rounded too, which counts where there are few of them (4 x 465: 0.4 %): `rest` of it times x is added.
+// The factor's own diagonal is rounded too, which may count (keeps_rest): what fp16 leaves of it times x is added.
 template <typename F>
 __device__ __forceinline__ void add_rest(uint32_t (&sums)[32], int at, uint4 x, F rest_of) {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
@@ -323,9 +325,9 @@ struct OrthTask {
 // A matrix whose shorter side fits a tile, and which fits a CTA's shared memory as a whole, goes through all steps in one CTA: X in
 // fp16, its shorter side as rows, is an operand as it lies there, along its rows for A and down them for the next X, which takes its
 // place two chunks of 64 columns at a time.  Eight warps compute, one thread of the ninth issues the products.  A step of 128 x 640 is
-// 5.5 us: 2.9 of products, 2.6 of ends between them; reading x, twice, takes 8 us.
-// In us, in one CTA and as a launch to a product: 64 x 64 14 and 52, 128 x 128 20 and 65, 128 x 640 47 and 74, 148 x 128 x 640 52 and 237.
-// Longer ones do not fit.
+// 6 us: 2.9 of products, 3 of ends between them; reading x, twice, takes 8 us (down the columns of 640 x 128, 25).
+// In us, in one CTA and as a launch to a product: 64 x 64 17 and 54, 128 x 128 23 and 66, 128 x 640 49 and 72, 640 x 128 70 and 76, 100 x 333 (by
+// elements) 57 and 85, 638 x 126 (so too) 97 and 93, but 117 and 124 with the call; 148 x 128 x 640 52 and 237.  Longer ones do not fit.
 constexpr int SMALL_CHUNKS = 10, SMALL_SIDE = TILE, SMALL_LENGTH = SMALL_CHUNKS * 64, SMALL_THREADS = 288, SMALL_READS = 8;
 constexpr uint32_t SMALL_A = 0, SMALL_SQUARE = TILE, SMALL_NEXT = 2 * TILE;       // columns of tensor memory: A, A^2, and two places for the next X
 
@@ -333,7 +335,7 @@ struct SmallParams {
     const void *x;
     int64_t x_stride[2], out_stride[2];
     __nv_bfloat16 *out;
-    int side, length, steps, whole_out;
+    int side, length, steps, whole_out, rest;   // rest: the factor's diagonal beyond fp16 counts
     float a, b, c, scale;
     uint64_t wait_ns;
 };
@@ -348,6 +350,7 @@ struct SmallSmem {
 // The 16-byte piece `unit` of a row of a chunk, in the 128-byte swizzle.
 __device__ __forceinline__ uint4 *piece_of(uint8_t *chunk, int row, int unit) { return reinterpret_cast<uint4 *>(chunk + row * 128 + ((unit ^ (row & 7)) << 4)); }
 __device__ __forceinline__ uint32_t *pair_place(uint8_t *chunk, int row, int pair) { return reinterpret_cast<uint32_t *>(piece_of(chunk, row, pair / 4)) + pair % 4; }       // of 32 pairs
+__device__ __forceinline__ __half *half_place(uint8_t *chunk, int row, int col) { return reinterpret_cast<__half *>(pair_place(chunk, row, col / 2)) + col % 2; }
 __device__ __forceinline__ uint32_t small_word(int n, bool b_down) {
     return (1u << 4) | (b_down ? 1u << 16 : 0u) | (static_cast<uint32_t>(n / 8) << 17) | (static_cast<uint32_t>(TILE / 16) << 24);
 }
@@ -403,15 +406,37 @@ struct SmallPiece<T, false, true> {
         for (int e = 0; e < 8; e += 2) *pair_place(to[chunk], r + e / 2, i % 32) = r + e / 2 < rows.side ? pack_half(v[e], v[e + 1]) : 0;
     }
 };
-// or, where memory's rows are the shorter side, of 128 rows (of X) next to each other.
+// or, where memory's rows are the shorter side (X's columns), in whole pieces again, lanes on one row each after the other,
+template <typename T>
+struct SmallPiece<T, true, false> {
+    Raw<T, true> raw;
+    static __device__ int all(const SmallRows<T> &rows) { return rows.side / 8 * rows.chunks * 64; }
+    static __device__ void place(const SmallRows<T> &rows, int i, int *r, int *c) { *r = i / (rows.chunks * 64) * 8, *c = i - *r / 8 * (rows.chunks * 64); }
+    __device__ void read(const SmallRows<T> &rows, int i) {
+        int r, c;
+        place(rows, i, &r, &c);
+        const bool there = i < all(rows) && c < rows.length;
+#pragma unroll
+        for (int w = 0; w < static_cast<int>(sizeof(T) / 2); ++w) raw.v[w] = there ? reinterpret_cast<const uint4 *>(rows.x + c * rows.stride + r)[w] : make_uint4(0, 0, 0, 0);
+    }
+    __device__ void get(float (&v)[8]) const { raw.get(v); }
+    static __device__ void keep(const SmallRows<T> &rows, uint8_t (*to)[CHUNK], int i, const float (&v)[8]) {
+        int r, c;
+        place(rows, i, &r, &c);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) *half_place(to[c / 64], r + e, c % 64) = __float2half_rn(v[e]);
+    }
+};
+// or by elements of rows (of X, to a multiple of 32) next to each other.
 template <typename T>
 struct SmallPiece<T, false, false> {
     T raw[8];
-    static __device__ int all(const SmallRows<T> &rows) { return TILE * rows.chunks * 8; }
-    static __device__ void place(int i, int *r, int *unit) { *unit = i / TILE, *r = i - *unit * TILE; }
+    static __device__ int across(const SmallRows<T> &rows) { return (rows.side + 31) & ~31; }
+    static __device__ int all(const SmallRows<T> &rows) { return across(rows) * rows.chunks * 8; }
+    static __device__ void place(const SmallRows<T> &rows, int i, int *r, int *unit) { *unit = i / across(rows), *r = i - *unit * across(rows); }
     __device__ void read(const SmallRows<T> &rows, int i) {
         int r, unit;
-        place(i, &r, &unit);
+        place(rows, i, &r, &unit);
 #pragma unroll
         for (int e = 0; e < 8; ++e) raw[e] = r < rows.side && unit * 8 + e < rows.length ? rows.x[(unit * 8 + e) * rows.stride + r] : static_cast<T>(0.0f);
     }
@@ -421,7 +446,7 @@ struct SmallPiece<T, false, false> {
     }
     static __device__ void keep(const SmallRows<T> &rows, uint8_t (*to)[CHUNK], int i, const float (&v)[8]) {
         int r, unit;
-        place(i, &r, &unit);
+        place(rows, i, &r, &unit);
         *piece_of(to[unit / 8], r, unit % 8) = r < rows.side ? make_uint4(pack_half(v[0], v[1]), pack_half(v[2], v[3]), pack_half(v[4], v[5]), pack_half(v[6], v[7])) : make_uint4(0, 0, 0, 0);
     }
 };
@@ -512,8 +537,6 @@ __device__ __forceinline__ void small_factor(const SmallParams &p, const uint32_
         v[e / 2] = pack_half(f.x, f.y);
     }
 }
-// An element of a chunk
-__device__ __forceinline__ __half *half_place(uint8_t *chunk, int row, int col) { return reinterpret_cast<__half *>(pair_place(chunk, row, col / 2)) + col % 2; }
 // The factor's element of the diagonal
 __device__ __forceinline__ float small_diagonal(const SmallParams &p, float own, float square) {
     const float per_square = p.c * (FACTOR_UNIT / A_UNIT / A_UNIT);
@@ -700,7 +723,7 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
                     const int c0 = chunk * 64 + half * 32;
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
-                        if (p.side <= REST_SIDE) add_rest(r[half], u * 8, *piece_of(sm.x[chunk], row, half * 4 + u), [&](int) { return rest; });
+                        if (p.rest) add_rest(r[half], u * 8, *piece_of(sm.x[chunk], row, half * 4 + u), [&](int) { return rest; });
                     if (!last) {
                         uint32_t v[16];
                         small_half(r[half], 1.0f / FACTOR_UNIT, v);
@@ -731,11 +754,11 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
 // and, for the next X, of which a CTA's part of the operand is half of the columns, every row of every other chunk of 64 columns.
 // The sums of all of the next X stay in tensor memory until the products have ended.  Then they go to the rows, and to the CTA's own
 // columns; the copy engine brings the other CTA's (15 bytes a cycle between two CTAs, 3300 cycles) while the next A is multiplied.
-// A step of 256 x 384 is 9.8 us: 4.3 of products, the rest ends of 64 columns of a row to a thread, their way to the copies that the
+// A step of 256 x 384 is 10 us: 4.3 of products, the rest ends of 64 columns of a row to a thread, their way to the copies that the
 // tensor cores see (0.4 us each), and arrivals from the other CTA (0.3 to 0.5).  Parts of the rows multiplied as they come are slower
-// (66 us in all instead of 64): each has to be made visible by itself.  Reading x, twice, takes 7 us.
-// In us, in a pair and as a launch to a product: 129 x 129 53 and 85, 256 x 256 53 and 70, 256 x 384 64 and 74, 384 x 250 74 and 92, 250 x 333
-// (by elements) 78 and 91, 74 x 256 x 384 66 and 161, 200 x 192 x 192 146 and 238.  Longer ones do not fit.
+// (by 2 us in all): each has to be made visible by itself.  Reading x, twice, takes 7 us.
+// In us, in a pair and as a launch to a product: 129 x 129 55 and 86, 256 x 256 56 and 73, 256 x 384 65 and 76, 384 x 256 69 and 75, 250 x 333
+// (by elements) 79 and 94, 74 x 256 x 384 67 and 161, 200 x 192 x 192 153 and 238.  Longer ones do not fit.
 constexpr int PAIR_CHUNKS = 6, PAIR_BLOCKS = PAIR_CHUNKS / 2, PAIR_SIDE = 2 * TILE, PAIR_LENGTH = PAIR_CHUNKS * 64, PAIR_WARPS = 16, PAIR_THREADS = PAIR_WARPS * 32;
 constexpr uint32_t PAIR_A = 0, PAIR_SQUARE = 256, PAIR_NEXT = 0;        // columns of tensor memory; the next X after both have been read
 
@@ -1056,7 +1079,7 @@ int start_small(const SmallParams &p, int64_t batch, cudaStream_t st) {
 }
 template <bool PAIR, typename T>
 int start_small(const SmallParams &p, int64_t batch, bool whole, bool wide, cudaStream_t st) {
-    if (!wide) return start_small<PAIR, T, false, false>(p, batch, st);
+    if (!wide) return whole ? start_small<PAIR, T, true, false>(p, batch, st) : start_small<PAIR, T, false, false>(p, batch, st);
     return whole ? start_small<PAIR, T, true, true>(p, batch, st) : start_small<PAIR, T, false, true>(p, batch, st);
 }
 
@@ -1133,8 +1156,9 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
         m.x = x, m.out = static_cast<__nv_bfloat16 *>(out), m.side = static_cast<int>(plan.side), m.length = static_cast<int>(length), m.steps = steps;
         m.x_stride[0] = p.stride[0], m.x_stride[1] = p.stride[1], m.out_stride[0] = batch > 1 ? out_stride[0] : 0, m.out_stride[1] = rows > 1 ? out_stride[1] : 0;
         m.whole_out = reinterpret_cast<uintptr_t>(out) % 16 == 0 && m.out_stride[0] % 8 == 0 && m.out_stride[1] % 8 == 0 && length % 32 == 0;
+        m.rest = keeps_rest(plan.side, length);
         m.a = coefficients[0], m.b = coefficients[1], m.c = coefficients[2], m.scale = scale, m.wait_ns = wait_limit_ns();
-        const bool pieces = whole && length % 8 == 0;
+        const bool pieces = whole && cols % 8 == 0;
         if (small) return dtype == KT_F32 ? start_small<false, float>(m, batch, pieces, plan.wide, st) : start_small<false, __nv_bfloat16>(m, batch, pieces, plan.wide, st);
         return dtype == KT_F32 ? start_small<true, float>(m, batch, pieces, plan.wide, st) : start_small<true, __nv_bfloat16>(m, batch, pieces, plan.wide, st);
     }
@@ -1147,7 +1171,7 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     OrthParams q{};
     q.rows = static_cast<int>(rows), q.cols = static_cast<int>(cols), q.side = static_cast<int>(plan.side), q.batch = static_cast<int>(batch);
     q.pitch = plan.pitch_a, q.gram = reinterpret_cast<const __half *>(ws + plan.at_gram), q.x_pitch = plan.pitch_x;
-    q.diagonal = reinterpret_cast<float *>(ws + plan.at_diagonal), q.rest = plan.side <= REST_SIDE ? reinterpret_cast<float *>(ws + plan.at_rest) : nullptr;
+    q.diagonal = reinterpret_cast<float *>(ws + plan.at_diagonal), q.rest = keeps_rest(plan.side, length) ? reinterpret_cast<float *>(ws + plan.at_rest) : nullptr;
     q.a = coefficients[0], q.b = coefficients[1], q.c = coefficients[2], q.scale = scale;
     q.out = static_cast<__nv_bfloat16 *>(out), q.out_stride[0] = out_stride[0], q.out_stride[1] = out_stride[1];
     if (plan.wide) return pairs ? run<true, true>(plan, ws, q, steps, st) : run<false, true>(plan, ws, q, steps, st);
