@@ -139,10 +139,12 @@ def synchronised_step(shape: Shape, layers: int, params: Dict[str, torch.Tensor]
 
 
 class Update:
-    """One step of all parameters: the blocks' matrices along their orthogonalised momentum, the others along the gradient."""
+    """One step of all parameters: the blocks' matrices along their orthogonalised momentum, the others along the gradient.  A matrix with
+    more outputs than inputs moves by the root of their ratio more.  `inputs_first`: whether matrices are [inputs, outputs], as
+    those of Model are (x @ up), or [outputs, inputs], as stock linear layers have them."""
 
-    def __init__(self, layers: int, params: Dict[str, torch.Tensor], rate: float = 0.02, momentum: float = 0.95, rate_others: float = 0.1):
-        self.layers, self.params, self.rate, self.momentum, self.rate_others = layers, params, rate, momentum, rate_others
+    def __init__(self, layers: int, params: Dict[str, torch.Tensor], rate: float = 0.02, momentum: float = 0.95, rate_others: float = 0.1, inputs_first: bool = False):
+        self.layers, self.params, self.rate, self.momentum, self.rate_others, self.inputs_first = layers, params, rate, momentum, rate_others, inputs_first
         self.state = {n: torch.zeros(layers, *params["0." + n].shape, device=params["0." + n].device) for n in MATRICES} if layers else {}
         self.work = {n: torch.empty(kt.kt_orth_workspace(*s.shape), dtype=torch.uint8, device=s.device) for n, s in self.state.items()}
 
@@ -152,7 +154,8 @@ class Update:
         for n, s in self.state.items():
             s.mul_(self.momentum).add_(torch.stack([grads["%d.%s" % (i, n)] for i in range(self.layers)]))
             out[n] = torch.empty_like(s, dtype=torch.bfloat16)
-            kt.kt_orth_update(s, out[n], self.work[n], scale=max(1.0, s.size(1) / s.size(2)) ** 0.5)
+            inputs, outputs = s.shape[1:] if self.inputs_first else s.shape[:0:-1]
+            kt.kt_orth_update(s, out[n], self.work[n], scale=max(1.0, outputs / inputs) ** 0.5)
         return out
 
     def step(self, grads: Dict[str, torch.Tensor]) -> None:
@@ -174,7 +177,7 @@ def example(tokens: int = 512, width: int = 1024, layers: int = 2, vocab: int = 
     _, got = synchronised_step(shape, layers, params, data, shares, [0, 0, 1, 1])
     want = plain_gradients(shape, layers, params, *data)
     errors = {n: float((got[n].float() - want[n]).norm() / want[n].norm()) for n in got}
-    Update(layers, params).step(got)
+    Update(layers, params, inputs_first=True).step(got)
     return shares, errors
 
 
@@ -192,7 +195,7 @@ def main() -> None:
         print("%-16s relative error against the fp32 model %.4f" % (n, e))
     shape = Shape(width=a.width, heads=a.width // 64, heads_kv=max(1, a.width // 256), hidden=4 * a.width)
     params, data = parameters(shape, a.layers, a.vocab, 0), batch_of(a.vocab, 8, a.tokens, 1)
-    model, update = Model(shape, a.layers, params), Update(a.layers, params)
+    model, update = Model(shape, a.layers, params), Update(a.layers, params, inputs_first=True)
 
     def step():
         model.forward(*data)
