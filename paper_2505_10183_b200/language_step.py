@@ -62,7 +62,7 @@ class Model:
     def forward(self, ids: torch.Tensor, targets: torch.Tensor, used: torch.Tensor) -> torch.Tensor:
         """The loss of each token (0 where there is no target)."""
         p, (B, L), C, dev = self.params, ids.shape, self.shape.width, ids.device
-        self.ids, self.targets = ids.reshape(-1), targets.reshape(-1)
+        self.size, self.ids, self.targets = (B, L, C), ids.reshape(-1), targets.reshape(-1)
         x = torch.empty(B * L, C, dtype=torch.bfloat16, device=dev)
         kt.kt_embed_forward(self.ids, p["embed"], x, scale=self.scale)
         x = x.view(B, L, C)
@@ -78,7 +78,7 @@ class Model:
 
     def backward(self) -> None:
         p, g, dev = self.params, self.grads, self.hidden.device
-        B, L, C = self.blocks[0].size if self.blocks else (1, self.hidden.size(0), self.shape.width)
+        B, L, C = self.size
         counted = (self.targets.view(B, L) >= 0).sum(1, keepdim=True).clamp(min=1)
         dloss = (1.0 / (B * counted)).expand(B, L).reshape(-1).contiguous()
         dh = torch.empty_like(self.hidden)
