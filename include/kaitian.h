@@ -682,8 +682,8 @@ int kt_waits_given_up(int64_t *count);
  * gradient is then added to what is there (of a table that is the output layer too, what kt_xent_backward left), and rows that
  * no token has are not touched.  workspace (16-byte aligned) holds kt_embed_workspace bytes, which need no initial value and
  * may be used again by the next call on the same stream.  Sums in fp32, in an order that the ids alone set.
- * Rows at any element-aligned address and stride; those at multiples of 16 bytes are faster.  Outputs must not overlap
- * inputs (base aside).  At most 2^30 tokens, 2^24 columns and a vocabulary of 2^24.
+ * Rows at any element-aligned address and stride (an input's may overlap, or be one row with a stride of 0; an output's may
+ * not); those at multiples of 16 bytes are faster.  Outputs must not overlap inputs (base aside).  At most 2^30 tokens, 2^24 columns and a vocabulary of 2^24.
  * Errors: KT_ERR_INVALID, KT_ERR_SHAPE, KT_ERR_ALIGN, KT_ERR_CUDA. */
 int kt_embed_forward(const int64_t *ids, const void *weight, int64_t weight_stride, int param_dtype, void *out,
                      int64_t out_stride, int64_t tokens, int64_t cols, int64_t vocab, int dtype, float scale,

@@ -473,11 +473,12 @@ struct Plan {
 
 int64_t bytes_needed(int64_t tokens, int64_t cols, int64_t vocab) { return std::max(Plan(tokens, cols, vocab, true).bytes, Plan(tokens, cols, vocab, false).bytes); }
 
-int check_matrix(const char *what, const void *at, int64_t stride, int64_t rows, int64_t cols, int dtype) {
+// (Rows that are only read may overlap, or be one row with a stride of 0.)
+int check_matrix(const char *what, const void *at, int64_t stride, int64_t rows, int64_t cols, int dtype, bool written) {
     if (rows == 0 || cols == 0) return KT_OK;
     if (at == nullptr) return fail(KT_ERR_INVALID, "%s is NULL", what);
     if (reinterpret_cast<uintptr_t>(at) % (dtype == KT_F32 ? 4 : 2)) return fail(KT_ERR_ALIGN, "%s is not aligned to its elements", what);
-    if (rows > 1 && (stride < cols || stride > INT64_C(1) << 38)) return fail(KT_ERR_SHAPE, "%s: rows of %lld elements cannot be %lld apart", what, (long long)cols, (long long)stride);
+    if (rows > 1 && (stride < (written ? cols : 0) || stride > INT64_C(1) << 38)) return fail(KT_ERR_SHAPE, "%s: rows of %lld elements cannot be %lld apart", what, (long long)cols, (long long)stride);
     return KT_OK;
 }
 int check_common(int64_t tokens, int64_t cols, int64_t vocab, int dtype, int param_dtype, float scale, const int64_t *ids) {
@@ -532,8 +533,8 @@ int kt_embed_forward(const int64_t *ids, const void *weight, int64_t weight_stri
                      void *stream) {
     if (int rc = check_common(tokens, cols, vocab, dtype, param_dtype, scale, ids)) return rc;
     if (tokens == 0) return KT_OK;
-    if (int rc = check_matrix("weight", weight, weight_stride, vocab, cols, param_dtype)) return rc;
-    if (int rc = check_matrix("out", out, out_stride, tokens, cols, dtype)) return rc;
+    if (int rc = check_matrix("weight", weight, weight_stride, vocab, cols, param_dtype, false)) return rc;
+    if (int rc = check_matrix("out", out, out_stride, tokens, cols, dtype, true)) return rc;
     const LookupParams p{ids, weight, out, weight_stride, out_stride, tokens, cols, static_cast<int>(vocab), scale};
     const bool vectors = whole(weight, weight_stride, vocab, param_dtype) && whole(out, out_stride, tokens, dtype);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -549,10 +550,10 @@ int64_t kt_embed_workspace(int64_t tokens, int64_t cols, int64_t vocab) {
 int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids, const void *base, int64_t base_stride, void *dweight, int64_t dweight_stride, int param_dtype, void *workspace,
                       int64_t workspace_bytes, int64_t tokens, int64_t cols, int64_t vocab, int dtype, float scale, void *stream) {
     if (int rc = check_common(tokens, cols, vocab, dtype, param_dtype, scale, ids)) return rc;
-    if (int rc = check_matrix("dout", dout, dout_stride, tokens, cols, dtype)) return rc;
-    if (int rc = check_matrix("dweight", dweight, dweight_stride, vocab, cols, param_dtype)) return rc;
+    if (int rc = check_matrix("dout", dout, dout_stride, tokens, cols, dtype, false)) return rc;
+    if (int rc = check_matrix("dweight", dweight, dweight_stride, vocab, cols, param_dtype, true)) return rc;
     if (base != nullptr)
-        if (int rc = check_matrix("base", base, base_stride, vocab, cols, param_dtype)) return rc;
+        if (int rc = check_matrix("base", base, base_stride, vocab, cols, param_dtype, false)) return rc;
     if (base == dweight && vocab > 1 && base_stride != dweight_stride) return fail(KT_ERR_SHAPE, "base is dweight, with another stride");
     const bool vectors = (tokens == 0 || whole(dout, dout_stride, tokens, dtype)) && whole(dweight, dweight_stride, vocab, param_dtype) && (base == nullptr || whole(base, base_stride, vocab, param_dtype));
     const Plan plan(tokens, cols, vocab, vectors);
