@@ -726,8 +726,11 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
  * strides of matrix and row in elements, columns are contiguous, any element-aligned address.  Each matrix is on its own;
  * one of zeros gives zeros, one with an infinity or a NaN gives NaN.  Whatever the size of x, results are the same
  * but for rounding.  steps: 1 to 64; coefficients that would take a singular value above 1.9 are refused.  Products
- * of fp16 (what is held between them has a known range) with fp32 sums: directions in which x has less than 2^-12 of
- * |x|_F are those of roundings.  Up to 2^16 rows and columns, 2^15 matrices.
+ * of fp16 (what is held between them has a known range) with fp32 sums, whatever the type of x: a rounding of x / |x|_F is
+ * raised by up to a in every step, in the directions that x has little of.  Of the result (2-norm; its own rounding is 0.17 %), with five steps
+ * of the usual coefficients (a = 3.4445), is off: normal numbers 0.18 to 0.23 %; singular values that fall evenly in the logarithm to
+ * 10^-3 of the largest 0.35 to 1.2, to 10^-6 0.6 to 2.3; n alike and no others, of a matrix with a side of 512: 64 2.6 %, 8 4.3, 1 15 (directions
+ * in which x has less than 2^-12 of |x|_F are those of roundings).  Up to 2^16 rows and columns, 2^15 matrices.
  * workspace (16-byte aligned) holds kt_orth_workspace bytes, which need no initial value and may be used again by the
  * next call on the same stream.  out must not overlap x, nor its own rows each other.  No atomics: the same inputs
  * give the same bits.  A wait that gives up (above) leaves NaN where results are not right.
