@@ -5,17 +5,19 @@
 // a s + b s^3 + c s^5 takes every singular value s towards one.
 //
 // Three products a step (kt_product.cuh), in fp16 with fp32 sums: everything that is held between products has a known
-// range (singular values of X at most some 1.2, of A 1.5, of the factor |a|), so that fp16's 11 bits can be had where
+// range (singular values of X up to 1.9, of A 3.7, of the factor 7.5 are admitted: kt_orth_update's check of the coefficients; the usual ones
+// reach 1.2, 1.5 and a = 3.4), so that fp16's 11 bits can be had where
 // bf16, whose range is not needed, has 8: of normal numbers the result is 0.17 to 0.23 % from 64 bits, one in 32 bits rounded to bf16 0.17.
 // A rounding of X grows by up to a factor of a a step in the directions that X has little of, so singular values that fall evenly to 10^-3 of
 // the largest make it 0.34 to 1.2 %, and few of them beside none more (512 x 512 of rank 64 2.6, of 8 4.3).
-// Powers of two keep small entries off fp16's subnormals: X is held times 2^7, A times 2^14, the factor times 2^13.
+// Powers of two keep small entries off fp16's subnormals: X is held times 2^7, A times 2^14, the factor times 2^13 (so that the largest
+// admitted A and factor are 60300 and 61440; fp16 ends at 65504).
 // A and the factor are symmetric: tiles on and above the diagonal are computed, and written to both sides.
 // Every product waits for the one before, so a matrix of few tiles is bound by 15 times what a launch of one takes (256 x 448:
-// 81 us, 5 each), and all products in one launch, with a count of arrivals between them, were slower (256 x 384: 110 us instead of 74: the
-// fences and the count's way through the L2 cost more than a launch).  What fits the shared memory of a CTA or two needs neither
-// (below).  4 x 4096 x 2048: some 60 + 40 + 93 us a step, the tensor cores busy
-// 76, 58 and 86 % of it (two rounds of 144 tiles on 74 pairs in the first two); power sets the clocks.
+// 79 us, 5 each), and all products in one launch, with a count of arrivals between them, were slower (256 x 384: 110 us where a
+// launch to each took 89 then, 74 later: the fences and the count's way through the L2 cost more than a launch).  What fits the shared memory of a CTA or two needs neither
+// (below).  4 x 4096 x 2048: some 60 + 41 + 92 us a step, the tensor cores busy
+// 76, 55 and 86 % of it (two rounds of 144 tiles on 74 pairs in the first two); power sets the clocks.
 #include "../../include/kaitian.h"
 
 #include <cuda_bf16.h>
@@ -36,7 +38,7 @@ namespace {
 constexpr float X_UNIT = 128.0f, A_UNIT = 16384.0f, FACTOR_UNIT = 8192.0f;
 constexpr int MAX_STEPS = 64;
 // Whether the factor's diagonal is kept beyond fp16: where its elements are few, or alike because X is far from square (40 x 5000 with
-// and without: 0.17 and 0.31 % off the formula, 30 x 438 0.17 and 0.30; the time of 64 x 640 36 and 38 us).  Elsewhere it changes
+// and without: 0.17 and 0.31 % off the formula, 30 x 438 0.17 and 0.30; the time of 64 x 640 42 and 36 us).  Elsewhere it changes
 // little but for multiples of orthogonal matrices, which are alike too (424 x 424: 0.41 % off).
 bool keeps_rest(int64_t side, int64_t length) { return side <= 64 || length >= 8 * side; }
 constexpr int SUM_BLOCKS = 256;                 // partial sums of squares to a matrix, at most: a thread reads one
@@ -330,8 +332,8 @@ struct OrthTask {
 // fp16, its shorter side as rows, is an operand as it lies there, along its rows for A and down them for the next X, which takes its
 // place two chunks of 64 columns at a time.  Eight warps compute, one thread of the ninth issues the products.  A step of 128 x 640 is
 // 6 us: 2.9 of products, 3 of ends between them; reading x, twice, takes 8 us (down the columns of 640 x 128, 25).
-// In us, in one CTA and as a launch to a product: 64 x 64 17 and 54, 128 x 128 23 and 66, 128 x 640 49 and 72, 640 x 128 70 and 76, 100 x 333 (by
-// elements) 57 and 85, 638 x 126 (so too) 97 and 93, but 117 and 124 with the call; 148 x 128 x 640 52 and 237.  Longer ones do not fit.
+// In us, in one CTA and as a launch to a product: 64 x 64 17 and 58, 128 x 128 22 and 67, 128 x 640 50 and 77, 640 x 128 72 and 80, 100 x 333 (by
+// elements) 57 and 86, 638 x 126 (so too) 97 and 96, but 117 and 130 with the call; 148 x 128 x 640 52 and 256.  Longer ones do not fit.
 constexpr int SMALL_CHUNKS = 10, SMALL_SIDE = TILE, SMALL_LENGTH = SMALL_CHUNKS * 64, SMALL_THREADS = 288, SMALL_READS = 8;
 constexpr uint32_t SMALL_A = 0, SMALL_SQUARE = TILE, SMALL_NEXT = 2 * TILE;       // columns of tensor memory: A, A^2, and two places for the next X
 
@@ -761,8 +763,8 @@ __global__ void __launch_bounds__(SMALL_THREADS, 1) k_orth_small(const SmallPara
 // A step of 256 x 384 is 10 us: 4.3 of products, the rest ends of 64 columns of a row to a thread, their way to the copies that the
 // tensor cores see (0.4 us each), and arrivals from the other CTA (0.3 to 0.5).  Parts of the rows multiplied as they come are slower
 // (by 2 us in all): each has to be made visible by itself.  Reading x, twice, takes 7 us.
-// In us, in a pair and as a launch to a product: 129 x 129 55 and 86, 256 x 256 56 and 73, 256 x 384 65 and 76, 384 x 256 69 and 75, 250 x 333
-// (by elements) 79 and 94, 74 x 256 x 384 67 and 161, 200 x 192 x 192 153 and 238.  Longer ones do not fit.
+// In us, in a pair and as a launch to a product: 129 x 129 55 and 89, 256 x 256 56 and 76, 256 x 384 64 and 80, 384 x 256 69 and 80, 250 x 333
+// (by elements) 79 and 97, 74 x 256 x 384 67 and 171, 200 x 192 x 192 152 and 267.  Longer ones do not fit.
 constexpr int PAIR_CHUNKS = 6, PAIR_BLOCKS = PAIR_CHUNKS / 2, PAIR_SIDE = 2 * TILE, PAIR_LENGTH = PAIR_CHUNKS * 64, PAIR_WARPS = 16, PAIR_THREADS = PAIR_WARPS * 32;
 constexpr uint32_t PAIR_A = 0, PAIR_SQUARE = 256, PAIR_NEXT = 0;        // columns of tensor memory; the next X after both have been read
 
@@ -1168,8 +1170,9 @@ int kt_orth_update(const void *x, const int64_t *x_stride, int dtype, void *out,
     }
     if (int rc = dtype == KT_F32 ? start<float>(p, plan, whole, st) : start<__nv_bfloat16>(p, plan, whole, st)) return rc;
     // Pairs of CTAs where there are tiles of 256 x 256 for two thirds of them in the products of symmetric matrices, the smaller ones.
-    // In us, one CTA to a tile and pairs: 2048 x 2048 (36 tiles) 259 and 273, 4 x 1024 x 1024 (40) 181 and 197, 16 x 512 x 512 (48)
-    // 173 and 161, 12 x 768 x 768 (72) 234 and 228.
+    // In us, one CTA to a tile and pairs: 2048 x 2048 (36 tiles) 243 and 266, 4 x 1024 x 1024 (40) 171 and 196, 16 x 512 x 512 (48)
+    // 163 and 159, 20 x 512 x 512 (60) 181 and 185, 12 x 768 x 768 (72) 218 and 215.  Where a side ends early in a tile of 256, which the rule does
+    // not look at, pairs lose: 15 x 1000 x 300 (45) 201 and 249.
     const int64_t symmetric = tiles_of(plan.side, 256);
     const bool pairs = symmetric * (symmetric + 1) / 2 * batch >= 45;
     OrthParams q{};

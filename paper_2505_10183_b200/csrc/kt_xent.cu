@@ -239,8 +239,9 @@ struct LogitsTask {
 };
 
 // A thread has half of a row of a tile: maximum and sum of exponentials (base 2) in one pass, 32 columns at a time.  With 512
-// elements of reduction and less this, not the product, is what a tile takes (4 us to 3: 8192 rows, 512, 32000: 225 us,
-// floor 161); 4096 and up the tensor cores at the power limit (8192 rows, 65536: 2762 to 3054 us as the clocks go).
+// elements of reduction and less this, not the product, is what a tile takes (4.2 us of which the tensor cores are busy 59 %: 8192 rows, 512,
+// 32000: 225 us, floor 161).  No rate bounds it (exponentials' unit 32 % busy, instructions in 35 % of the cycles): most of what a warp waits for is the instruction before, in
+// the chain of maximum, rescaling, exponentials and sum to every 32 columns, with two warps to a scheduler.  With 4096 and up the tensor cores at the power limit (8192 rows, 65536: 2762 to 3054 us as the clocks go).
 template <bool PAIR_>
 struct LossTask : LogitsTask<PAIR_> {
     using Base = LogitsTask<PAIR_>;
@@ -498,10 +499,15 @@ int64_t tiles_of(int64_t x, int side) { return (x + side - 1) / side; }
 //   forward, 512 x 512 on 8001 (64)             16.5  16.5        200 x 512 on 32000 (125)    23.8  20.5
 bool by_pairs(int64_t m, int64_t n) { return m > TILE && tiles_of(m, 256) * tiles_of(n, 256) >= 60; }
 
-// The same for the products from P, which differ in length: by the stages of the reductions that a pair would have.
-//   backward, 200 x 768 on 8001 (10 stages)     30.8  33.5        200 x 512 on 32000 (27)     53.3  59.5
-//   backward, 512 x 512 on 8001 (14)            34.9  35.9        512 x 1024 on 8001 (27)     48.0  43.3
-//   backward, 200 x 2048 on 8001 (27)           51.3  49.2        512 x 1024 on 32000 (110)    131   103
+// The same for the products from P, which differ in length: by the stages of the reductions that a pair would have.  In us, one CTA to a tile
+// and pairs (all kernels of the backward pass):
+//   200 x 768 on 8001 (10 stages)     28.2  29.6        512 x 1024 on 8001 (27)     43.2  39.5        400 x 512 on 32000 (50)     74.3  66.8
+//   512 x 512 on 8001 (13)            30.9  32.0        1000 x 512 on 8001 (27)     44.6  40.1        1000 x 768 on 8001 (41)     57.6  46.5
+//   256 x 512 on 16000 (13)           32.3  38.3        200 x 4096 on 4001 (27)     55.3  51.0        200 x 1024 on 32000 (54)    80.4  78.8
+//   200 x 2048 on 8001 (27)           48.7  45.4        512 x 512 on 16000 (27)     46.3  43.7        512 x 1024 on 32000 (108)    129   101
+// Up to 300 rows with up to 1024 elements pairs are the slower ones up to some 43 stages, since dW's tiles have 4 or 5 stages each and wait for their ends, which
+// the rule does not look at: 200 x 512 on 32000 (27) 50.2 and 56.4, 200 x 1024 on 16000 (27) 46.8 and 48.5, 300 x 768 on 16000 (33) 48.2 and 50.5,
+// 200 x 768 on 32000 (40) 64.0 and 66.2, 300 x 512 on 32000 (43) 64.5 and 69.5.
 constexpr int64_t PAIR_STAGES = 24;
 
 constexpr int64_t PIECE_BYTES = INT64_C(512) << 20;        // of P, at most
