@@ -696,7 +696,7 @@ int kt_embed_backward(const void *dout, int64_t dout_stride, const int64_t *ids,
 
 /* Softmax cross entropy of hidden rows against the weights of a vocabulary, without keeping the logits.
  * hidden[rows][dim] and weight[vocab][dim] are KT_BF16, as are their gradients; addresses are 16-byte aligned, row
- * strides multiples of 8 elements, dim a multiple of 8 up to 2^16; at most 2^20 rows and a vocabulary of 2^24.
+ * strides multiples of 8 elements and at least dim, dim a multiple of 8 up to 2^16; at most 2^20 rows and a vocabulary of 2^24.
  * targets (device, int64[rows]).  With logits l_iv = scale * hidden_i . weight_v:
  *   lse_i = log sum_v exp(l_iv),  loss_i = lse_i - l_{i, targets_i}      (fp32[rows])
  * A row whose target is negative does not count: its loss, lse and gradients are zeros, and what hidden holds there does
@@ -723,7 +723,8 @@ int kt_xent_backward(const float *dloss, const float *dlse, const void *hidden, 
 /* A matrix-shaped update orthogonalised by Newton-Schulz products: with X = x / |x|_F, `steps` times
  *   A = X X^T,  X <- (a I + b A + c A^2) X      (a, b, c = coefficients[3], host),
  * then out = scale * X.  x is [batch][rows][cols] of KT_F32 or KT_BF16 and out KT_BF16; a stride array (host) holds the
- * strides of matrix and row in elements, columns are contiguous, any element-aligned address.  Each matrix is on its own;
+ * strides of matrix and row in elements, columns are contiguous, rows at least cols apart (matrices of x may be one, with a
+ * stride of 0), any element-aligned address.  Each matrix is on its own;
  * one of zeros gives zeros, one with an infinity or a NaN gives NaN.  Whatever the size of x, results are the same
  * but for rounding.  steps: 1 to 64; coefficients that would take a singular value above 1.9 are refused.  Products
  * of fp16 (what is held between them has a known range) with fp32 sums, whatever the type of x: a rounding of x / |x|_F is
